@@ -311,9 +311,9 @@ def _gather(s, name, pages):
 def _plain_sample(s):
     V = s["case"]["vocab"]
     z = s["logits"].float()
+    z = z - z.amax(-1, keepdim=True)
     y = z * (1.0 / s["temperature"])[:, None]
-    top = y.amax(-1, keepdim=True)
-    w = torch.exp(y - top)
+    w = torch.exp(y)
     if s["truncated"]:
         order = torch.sort(y, dim=-1, descending=True, stable=True).indices
         k = torch.where(s["top_k"] > 0, s["top_k"], torch.full_like(s["top_k"], V)).clamp_max(V)
@@ -324,14 +324,14 @@ def _plain_sample(s):
         in_p[:, 0] = True
         in_k = torch.arange(V, device="cuda") < k[:, None]
         kept = torch.empty_like(in_k).scatter_(1, order, in_p & in_k)
-        kept &= (y >= top + torch.log(s["min_p"])[:, None]) | (s["min_p"] <= 0)[:, None]
+        kept &= (y >= torch.log(s["min_p"])[:, None]) | (s["min_p"] <= 0)[:, None]
         key = torch.where(kept, y + s["noise"], torch.full_like(y, -math.inf))
         total = torch.where(kept, w, torch.zeros_like(w)).sum(-1)
     else:
         key, total = y + s["noise"], w.sum(-1)
     token = key.argmax(-1)
     at = token[:, None]
-    full = torch.exp(z - z.amax(-1, keepdim=True))
+    full = torch.exp(z)
     return {"token": token.to(torch.int32), "prob": torch.gather(w, 1, at).squeeze(1) / total,
             "conf": torch.gather(full, 1, at).squeeze(1) / full.sum(-1)}
 
