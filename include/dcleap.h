@@ -293,6 +293,96 @@ dcl_status dcl_accept_noalloc(const void* logits_dev, int32_t B, int32_t P, int3
  * dcl_last_error(NULL)). */
 dcl_status dcl_fp8_quantise(const uint16_t* w, int64_t rows, int64_t cols, uint8_t* codes, int32_t* exps);
 
+/* ---- serving many sequences: a paged key / value cache, its attention, drawing tokens ----
+ *
+ * A serving refinement outside the paper, whose steps hold one dense cache of max_batch x
+ * max_seq positions.  The cache here is the caller's memory, in pages that belong to any
+ * sequence: position t of a sequence is at slot page_table[t / page_len] * page_len +
+ * t % page_len.  All calls below are asynchronous on the context stream.  What they find
+ * wrong in device data (a slot, page or length outside the cache) is not followed; it is
+ * recorded and reported as INVALID_ARG by the next call that reports device-side faults,
+ * such as dcl_synchronise. */
+
+#define DCL_KV_BF16 0 /* keys and values in bf16 */
+#define DCL_KV_FP8 1  /* E4M3 codes and one exponent per (position, kv head) vector */
+/* Smallest exponent of a stored vector: components below 2^-74 are rounded to zero. */
+#define DCL_KV_EXP_MIN (-64)
+
+/* A paged cache for one layer.  k_dev, v_dev: [n_pages][n_kv_heads][page_len][head_dim] bf16, or
+ * for DCL_KV_FP8 codes (uint8); k_exp_dev, v_exp_dev (DCL_KV_FP8 only): int8 [n_pages]
+ * [n_kv_heads][page_len].  A stored vector is code * 2^exp as in dcl_fp8_quantise (its format,
+ * with the exponent at least DCL_KV_EXP_MIN), so that every stored value is a bf16 value (but for
+ * components from 1.9375 * 2^127 on, whose nearest code stands for 2^128 and reads as infinity);
+ * infinities and NaN are stored as NaN.  page_len 16, 32, 64, 128 or 256; head_dim 64 or 128;
+ * n_pages * page_len < 2^31; every pointer 16-byte aligned. */
+typedef struct {
+  int32_t n_pages, page_len, n_kv_heads, head_dim, format;
+  void *k_dev, *v_dev;
+  int8_t *k_exp_dev, *v_exp_dev;
+} dcl_kv_cache;
+
+/* Store (and for DCL_KV_FP8 quantise) the keys and values of n positions: row i of k_dev / v_dev
+ * (bf16 [n_kv_heads][head_dim], rows row_stride elements apart, so that they may stand in the
+ * q | k | v rows of dcl_op_attention) goes to slot slot_dev[i] (int32; negative: the row is
+ * skipped).  The slots of a call are distinct.  row_stride a multiple of 8, pointers 16-byte
+ * aligned.  Errors: INVALID_ARG, CUDA. */
+dcl_status dcl_kv_write(dcl_ctx* ctx, const dcl_kv_cache* cache, const void* k_dev, const void* v_dev,
+                        int64_t row_stride, const int32_t* slot_dev, int32_t n);
+
+/* Read n positions back as bf16 (exactly what is stored): the inverse of dcl_kv_write's layout.
+ * A row of a negative slot is filled with zeros.  Errors: INVALID_ARG, CUDA. */
+dcl_status dcl_kv_read(dcl_ctx* ctx, const dcl_kv_cache* cache, const int32_t* slot_dev, int32_t n,
+                       void* k_dev, void* v_dev, int64_t row_stride);
+
+/* Attention of the new positions of each sequence over its cached ones (the new ones' keys and
+ * values are written first, if they are to be seen):
+ *   out = softmax(scale * q k^T) v,  lse = ln sum exp(scale * q k^T).
+ *   q_dev       bf16 rows of [n_heads][head_dim], q_stride elements apart (RoPE applied; a
+ *               multiple of 8; 16-byte aligned); n_heads a multiple of the cache's n_kv_heads.
+ *   q_start_dev int32 [batch + 1]: rows [q_start[b], q_start[b + 1]) of the n_q rows are the new
+ *               positions of sequence b (from none to many; rows of no sequence stay untouched).
+ *   page_table_dev int32 [batch][max_pages], seq_len_dev int32 [batch]: the pages of sequence b
+ *               and how many positions it has cached (entries past them are not read).
+ *   max_new     no sequence has more rows than this (a choice of kernel: results do not depend
+ *               on it beyond rounding).
+ *   causal      0: a row sees every cached position; 1: row i of the r rows of sequence b sees
+ *               positions up to seq_len[b] - r + i.
+ *   scale       > 0, or 0 for 1 / sqrt(head_dim).
+ *   out_dev     bf16 [n_q][n_heads][head_dim]; lse_dev float [n_q][n_heads] or NULL.  A row that
+ *               sees nothing gets zeros and -inf.
+ * Scores, softmax statistics and sums are held in fp32 and reproduce bit for bit.
+ * Errors: INVALID_ARG, OOM (scratch), CUDA. */
+dcl_status dcl_kv_attention(dcl_ctx* ctx, const dcl_kv_cache* cache, const void* q_dev, int64_t q_stride,
+                            const int32_t* q_start_dev, const int32_t* page_table_dev, int32_t max_pages,
+                            const int32_t* seq_len_dev, int32_t batch, int32_t n_q, int32_t max_new,
+                            int32_t n_heads, int32_t causal, float scale, void* out_dev, float* lse_dev);
+
+/* Draw one token per row of logits_dev (bf16 [rows][V], rows logits_stride elements apart).  With
+ * y = (z - max z) / temperature and the tokens ordered by (z descending, index ascending), the
+ * tokens kept are
+ *   the first top_k (0 or less: all), of them the shortest prefix whose softmax mass reaches
+ *   top_p of theirs (1 or more: all; at least one token), and of these the ones with
+ *   exp(y) >= min_p (0 or less: all);
+ * the token drawn is the kept one with the largest y + noise (lowest index on ties).  With noise
+ * of independent standard Gumbel numbers -ln(-ln u) that is a draw from the kept tokens'
+ * renormalised softmax; noise_dev NULL takes the largest y.  noise_dev float [rows][V], rows
+ * noise_stride elements apart, read for kept tokens only.  temperature, top_k, top_p, min_p:
+ * one value per row, or NULL for 1, 0, 1, 0; a temperature of 0 (or less, or NaN) takes the
+ * largest logit.  Logits of -inf and NaN are never drawn; a row of nothing else gets token -1 and
+ * zeros.  token_dev int32 [rows]; prob_dev float [rows] (may be NULL): the token's probability
+ * among the kept ones; conf_dev float [rows] (may be NULL): its probability under softmax(z)
+ * over all V, the confidence of Eq. threshold_pd.  V at most 2^19.
+ * Errors: INVALID_ARG, UNSUPPORTED (V), CUDA. */
+dcl_status dcl_sample(dcl_ctx* ctx, const void* logits_dev, int64_t logits_stride, const float* noise_dev,
+                      int64_t noise_stride, int32_t rows, int32_t V, const float* temperature_dev,
+                      const int32_t* top_k_dev, const float* top_p_dev, const float* min_p_dev,
+                      int32_t* token_dev, float* prob_dev, float* conf_dev);
+
+/* Wait for the context stream and report what its kernels recorded since the last report.
+ * Errors: INVALID_ARG (a slot, page or length outside a paged cache; a token id out of range),
+ * TIMEOUT, CUDA. */
+dcl_status dcl_synchronise(dcl_ctx* ctx);
+
 /* ---- single-kernel entry points (the kernels of the step, for parity tests) ---- */
 
 /* y = x / sqrt(mean(x^2) + eps) * gain.  x_dev float [rows][d], gain_dev bf16 [d],

@@ -21,6 +21,8 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libdcleap.so")
 
 DCL_TILE_PAIR = 2
+DCL_KV_BF16, DCL_KV_FP8 = range(2)
+DCL_KV_EXP_MIN = -64
 DCL_OK, DCL_ERR_INVALID_ARG, DCL_ERR_STATE, DCL_ERR_OOM, DCL_ERR_CUDA, DCL_ERR_TIMEOUT, \
     DCL_ERR_UNSUPPORTED = range(7)
 STATUS_NAMES = ["OK", "INVALID_ARG", "STATE", "OOM", "CUDA", "TIMEOUT", "UNSUPPORTED"]
@@ -58,8 +60,15 @@ class Allocator(ctypes.Structure):
     _fields_ = [("alloc", ctypes.c_void_p), ("free", ctypes.c_void_p), ("user", ctypes.c_void_p)]
 
 
+class KvCacheDesc(ctypes.Structure):
+    _fields_ = [("n_pages", ctypes.c_int32), ("page_len", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("format", ctypes.c_int32), ("k_dev", ctypes.c_void_p),
+                ("v_dev", ctypes.c_void_p), ("k_exp_dev", ctypes.c_void_p), ("v_exp_dev", ctypes.c_void_p)]
+
+
 _P = ctypes.c_void_p
 _I = ctypes.c_int32
+_L = ctypes.c_int64
 _F = ctypes.c_float
 # name: (restype, argtypes)
 SIGNATURES = {
@@ -80,6 +89,11 @@ SIGNATURES = {
     "dcl_accept": (_I, [_P, _P, _I, _I, _I, _P, _P, ctypes.POINTER(DecodeConfig), _P]),
     "dcl_accept_noalloc": (_I, [_P, _I, _I, _I, _P, _P, ctypes.POINTER(DecodeConfig), _P, _P]),
     "dcl_fp8_quantise": (_I, [_P, ctypes.c_int64, ctypes.c_int64, _P, _P]),
+    "dcl_kv_write": (_I, [_P, _P, _P, _P, _L, _P, _I]),
+    "dcl_kv_read": (_I, [_P, _P, _P, _I, _P, _P, _L]),
+    "dcl_kv_attention": (_I, [_P, _P, _P, _L, _P, _P, _I, _P, _I, _I, _I, _I, _I, _F, _P, _P]),
+    "dcl_sample": (_I, [_P, _P, _L, _P, _L, _I, _I, _P, _P, _P, _P, _P, _P, _P]),
+    "dcl_synchronise": (_I, [_P]),
     "dcl_op_rmsnorm": (_I, [_P, _P, _P, _P, _I, _I, _F]),
     "dcl_op_linear": (_I, [_P, _P, _P, _P, _I, _I, _I, _I, _I]),
     "dcl_op_attention": (_I, [_P, _P, _P, _I, _I, _I, _I, _I, _I]),
@@ -154,6 +168,64 @@ def _dev(t, name, itemsize, count=0):
     if t.numel() < count:
         raise ValueError(f"{name}: at least {count} elements needed, {t.numel()} given")
     return _ptr(t)
+
+
+def _dev_rows(t, name, itemsize, rows, cols):
+    """Device pointer and row stride (elements) of `rows` rows of `cols` elements each: a CUDA tensor
+    whose first dimension may be strided and whose rows are contiguous (a column block of a
+    wider matrix is)."""
+    if isinstance(t, np.ndarray) or not getattr(t, "is_cuda", False):
+        raise ValueError(f"{name}: a device buffer (a CUDA tensor) is required")
+    if t.element_size() != itemsize:
+        raise TypeError(f"{name}: elements of {itemsize} bytes expected, got {t.dtype}")
+    shape, stride = t.shape, t.stride()
+    have, inner = 1, 1
+    for size, step in zip(reversed(shape[1:]), reversed(stride[1:])):
+        if size != 1 and step != inner:
+            raise ValueError(f"{name}: the elements of a row must be contiguous")
+        inner *= size
+        have *= size
+    if shape[0] < rows or have != cols:
+        raise ValueError(f"{name}: {rows} rows of {cols} elements expected, got {tuple(shape)}")
+    if rows > 1 and stride[0] < cols:
+        raise ValueError(f"{name}: rows overlap")
+    return t.data_ptr(), max(stride[0], cols) if shape[0] > 1 else cols
+
+
+class KvCache:
+    """A paged key / value cache of one layer in the caller's tensors (dcl_kv_cache): k, v
+    [pages][kv heads][page_len][head_dim], bf16, or 1-byte E4M3 codes with k_exp, v_exp int8
+    [pages][kv heads][page_len].  ``KvCache.empty`` allocates one."""
+
+    def __init__(self, k, v, k_exp=None, v_exp=None):
+        if len(k.shape) != 4:
+            raise ValueError("k: [pages][kv heads][page_len][head_dim] expected")
+        pages, heads, page_len, hd = k.shape
+        fp8 = k.element_size() == 1
+        if fp8 and (k_exp is None or v_exp is None):
+            raise ValueError("an FP8 cache needs k_exp and v_exp")
+        if not fp8 and (k_exp is not None or v_exp is not None):
+            raise ValueError("a bf16 cache has no exponents")
+        n, size = pages * heads * page_len, 1 if fp8 else 2
+        if tuple(v.shape) != tuple(k.shape):
+            raise ValueError("k and v differ in shape")
+        self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
+        self.n_pages, self.n_kv_heads, self.page_len, self.head_dim = pages, heads, page_len, hd
+        self.format = DCL_KV_FP8 if fp8 else DCL_KV_BF16
+        self.desc = KvCacheDesc(pages, page_len, heads, hd, self.format, _dev(k, "k", size, n * hd),
+                                _dev(v, "v", size, n * hd), _dev(k_exp, "k_exp", 1, n), _dev(v_exp, "v_exp", 1, n))
+        self.ptr = ctypes.addressof(self.desc)
+
+    @classmethod
+    def empty(cls, n_pages, page_len, n_kv_heads, head_dim, fp8=True, device="cuda"):
+        """A cache in new, uninitialised memory (FP8 unless fp8 is False)."""
+        import torch
+        shape = (n_pages, n_kv_heads, page_len, head_dim)
+        new = lambda s, t: torch.empty(s, dtype=t, device=device)
+        if not fp8:
+            return cls(new(shape, torch.bfloat16), new(shape, torch.bfloat16))
+        return cls(new(shape, torch.uint8), new(shape, torch.uint8), new(shape[:3], torch.int8),
+                   new(shape[:3], torch.int8))
 
 
 def weight_elements(shape, kind) -> int:
@@ -327,6 +399,55 @@ class Context:
         self._check(self._L.dcl_accept(self.ptr, _dev(logits, "logits", 2, B * P * V),
                                        B, P, V, _dev(committed, "committed", 4, B), _dev(x, "x", 4, B * P),
                                        ctypes.byref(cfg), _dev(k, "k", 4, B)))
+
+    def synchronise(self):
+        """Wait for the context stream; raises what its kernels recorded."""
+        self._check(self._L.dcl_synchronise(self.ptr))
+
+    def kv_write(self, cache, k, v, slots):
+        """Store rows k, v [n][kv heads][head_dim] (bf16, rows may be strided) at slots (int32 [n],
+        negative: skipped)."""
+        n, cols = k.shape[0], cache.n_kv_heads * cache.head_dim
+        kp, ks = _dev_rows(k, "k", 2, n, cols)
+        vp, vs = _dev_rows(v, "v", 2, n, cols)
+        if ks != vs and n > 1:
+            raise ValueError("k and v differ in row stride")
+        self._check(self._L.dcl_kv_write(self.ptr, cache.ptr, kp, vp, ks, _dev(slots, "slots", 4, n), n))
+
+    def kv_read(self, cache, slots, k, v):
+        """Read the positions at slots (int32 [n], negative: zeros) into k, v [n][kv heads][head_dim]."""
+        n, cols = slots.shape[0], cache.n_kv_heads * cache.head_dim
+        kp, ks = _dev_rows(k, "k", 2, n, cols)
+        vp, vs = _dev_rows(v, "v", 2, n, cols)
+        if ks != vs and n > 1:
+            raise ValueError("k and v differ in row stride")
+        self._check(self._L.dcl_kv_read(self.ptr, cache.ptr, _dev(slots, "slots", 4, n), n, kp, vp, ks))
+
+    def kv_attention(self, cache, q, q_start, page_table, seq_len, out, max_new, causal=False, scale=0.0, lse=None):
+        """Attention of the rows q [n_q][heads][head_dim] (bf16, rows may be strided; rows
+        [q_start[b], q_start[b + 1]) are sequence b's) over the first seq_len[b] positions of the
+        pages page_table[b]; out [n_q][heads][head_dim] bf16, lse [n_q][heads] float."""
+        n_q, heads, hd = q.shape
+        batch, max_pages = page_table.shape
+        if hd != cache.head_dim:
+            raise ValueError(f"q: head_dim {cache.head_dim} expected, got {hd}")
+        qp, qs = _dev_rows(q, "q", 2, n_q, heads * hd)
+        self._check(self._L.dcl_kv_attention(
+            self.ptr, cache.ptr, qp, qs, _dev(q_start, "q_start", 4, batch + 1), _dev(page_table, "page_table", 4),
+            max_pages, _dev(seq_len, "seq_len", 4, batch), batch, n_q, max_new, heads, int(bool(causal)), scale,
+            _dev(out, "out", 2, n_q * heads * hd), _dev(lse, "lse", 4, n_q * heads)))
+
+    def sample(self, logits, token, noise=None, temperature=None, top_k=None, top_p=None, min_p=None, prob=None,
+               conf=None):
+        """Draw token [rows] from logits [rows][V] (bf16, rows may be strided) and Gumbel numbers noise
+        [rows][V]; temperature, top_k, top_p, min_p, prob, conf [rows] each (see dcl_sample)."""
+        rows, V = logits.shape
+        zp, zs = _dev_rows(logits, "logits", 2, rows, V)
+        np_, ns = _dev_rows(noise, "noise", 4, rows, V) if noise is not None else (None, V)
+        self._check(self._L.dcl_sample(
+            self.ptr, zp, zs, np_, ns, rows, V, _dev(temperature, "temperature", 4, rows),
+            _dev(top_k, "top_k", 4, rows), _dev(top_p, "top_p", 4, rows), _dev(min_p, "min_p", 4, rows),
+            _dev(token, "token", 4, rows), _dev(prob, "prob", 4, rows), _dev(conf, "conf", 4, rows)))
 
     def op_rmsnorm(self, x, gain, y, eps):
         rows, d = x.shape

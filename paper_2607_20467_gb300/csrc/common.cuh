@@ -18,6 +18,7 @@ enum DevErr : int {
   DERR_TOKEN_RANGE = 1,     // a token id outside [0, vocab) reached the embedding
   DERR_WAIT_TIMEOUT = 2,    // a bounded wait gave up (GEMM / attention pipeline)
   DERR_BAD_SHAPE = 3,       // a kernel was launched with a shape it does not support
+  DERR_KV_RANGE = 4,        // a slot, page or length outside the paged cache (not followed)
 };
 
 __device__ __forceinline__ void report_error(int* err, int code) {

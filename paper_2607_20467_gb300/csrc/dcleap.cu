@@ -3,6 +3,7 @@
 // loop of Algorithm 1, and single-kernel entry points for parity tests.
 #include <algorithm>
 #include <chrono>
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstdlib>
@@ -12,6 +13,7 @@
 
 #include "../../include/dcleap.h"
 #include "common.cuh"
+#include "kv_cache.cuh"
 
 using namespace dcl;
 
@@ -219,6 +221,7 @@ dcl_status check_device(dcl_ctx* c) {
     if (c->gemm_flags) cudaMemset(c->gemm_flags, 0, sizeof(int) * c->gemm_flags_n);
     if (e == DERR_WAIT_TIMEOUT)
       return fail(c, DCL_ERR_TIMEOUT, "a pipeline wait timed out on the device (kernel returned)");
+    if (e == DERR_KV_RANGE) return fail(c, DCL_ERR_INVALID_ARG, "a slot, page or length outside the paged cache");
     if (e == DERR_TOKEN_RANGE) return fail(c, DCL_ERR_INVALID_ARG, "a token id outside [0, vocab) reached the embedding");
     return fail(c, DCL_ERR_CUDA, "device error code %d", e);
   }
@@ -1405,6 +1408,111 @@ dcl_status dcl_accept(dcl_ctx* c, const void* logits_dev, int32_t B, int32_t P, 
   CUDA_TRY(c, accept_commit_launch(committed_dev, c->acc_part, V, cfg->confidence, c->acc_ids, c->acc_c1, x_dev, k_dev,
                                    B, P, prm, c->stream));
   return DCL_OK;
+}
+
+namespace {
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+// The cache as the kernels see it; NULL, or why it is refused.
+const char* kv_pool(const dcl_kv_cache* kv, KvPool* out) {
+  if (!kv || !kv->k_dev || !kv->v_dev) return "NULL cache";
+  if (kv->format != DCL_KV_BF16 && kv->format != DCL_KV_FP8) return "cache format must be DCL_KV_BF16 or DCL_KV_FP8";
+  int shift = 4;
+  while (shift <= 8 && (1 << shift) != kv->page_len) ++shift;
+  if (shift > 8) return "page_len must be 16, 32, 64, 128 or 256";
+  if (kv->head_dim != 64 && kv->head_dim != 128) return "head_dim must be 64 or 128";
+  if (kv->n_kv_heads <= 0 || kv->n_pages <= 0 || (int64_t)kv->n_pages * kv->page_len >= (1ll << 31))
+    return "cache needs n_kv_heads, n_pages > 0 and n_pages * page_len < 2^31";
+  if (kv->format == DCL_KV_FP8 && (!kv->k_exp_dev || !kv->v_exp_dev)) return "an FP8 cache needs its exponents";
+  if (!aligned16(kv->k_dev) || !aligned16(kv->v_dev) || !aligned16(kv->k_exp_dev) || !aligned16(kv->v_exp_dev))
+    return "cache pointers must be 16-byte aligned";
+  *out = KvPool{kv->k_dev, kv->v_dev, kv->k_exp_dev, kv->v_exp_dev, kv->n_pages, shift, kv->n_kv_heads,
+                kv->head_dim, kv->format == DCL_KV_FP8};
+  return nullptr;
+}
+
+// Rows of k or v (or their copies): NULL, or why they are refused.
+const char* kv_rows(const KvPool& kv, const void* k, const void* v, int64_t stride, const void* slots, int32_t n) {
+  if (n < 0) return "n must be >= 0";
+  if (n && (!k || !v || !slots)) return "NULL argument";
+  if (stride < (int64_t)kv.G * kv.hd || stride % 8) return "row_stride must be a multiple of 8 and hold a row";
+  if (!aligned16(k) || !aligned16(v)) return "rows must be 16-byte aligned";
+  return nullptr;
+}
+
+}  // namespace
+
+dcl_status dcl_kv_write(dcl_ctx* c, const dcl_kv_cache* cache, const void* k_dev, const void* v_dev, int64_t row_stride,
+                        const int32_t* slot_dev, int32_t n) {
+  if (!c) return DCL_ERR_INVALID_ARG;
+  KvPool kv;
+  const char* why = kv_pool(cache, &kv);
+  if (!why) why = kv_rows(kv, k_dev, v_dev, row_stride, slot_dev, n);
+  if (why) return fail(c, DCL_ERR_INVALID_ARG, "kv_write: %s", why);
+  if (n == 0) return DCL_OK;
+  CUDA_TRY(c, kv_write_launch(kv, static_cast<const __nv_bfloat16*>(k_dev), static_cast<const __nv_bfloat16*>(v_dev),
+                              row_stride, slot_dev, n, c->derr, c->stream));
+  return DCL_OK;
+}
+
+dcl_status dcl_kv_read(dcl_ctx* c, const dcl_kv_cache* cache, const int32_t* slot_dev, int32_t n, void* k_dev,
+                       void* v_dev, int64_t row_stride) {
+  if (!c) return DCL_ERR_INVALID_ARG;
+  KvPool kv;
+  const char* why = kv_pool(cache, &kv);
+  if (!why) why = kv_rows(kv, k_dev, v_dev, row_stride, slot_dev, n);
+  if (why) return fail(c, DCL_ERR_INVALID_ARG, "kv_read: %s", why);
+  if (n == 0) return DCL_OK;
+  CUDA_TRY(c, kv_read_launch(kv, slot_dev, n, static_cast<__nv_bfloat16*>(k_dev), static_cast<__nv_bfloat16*>(v_dev),
+                             row_stride, c->derr, c->stream));
+  return DCL_OK;
+}
+
+dcl_status dcl_kv_attention(dcl_ctx* c, const dcl_kv_cache* cache, const void* q_dev, int64_t q_stride,
+                            const int32_t* q_start_dev, const int32_t* page_table_dev, int32_t max_pages,
+                            const int32_t* seq_len_dev, int32_t batch, int32_t n_q, int32_t max_new, int32_t n_heads,
+                            int32_t causal, float scale, void* out_dev, float* lse_dev) {
+  if (!c) return DCL_ERR_INVALID_ARG;
+  KvPool kv;
+  if (const char* why = kv_pool(cache, &kv)) return fail(c, DCL_ERR_INVALID_ARG, "kv_attention: %s", why);
+  if (batch < 0 || n_q < 0 || n_heads <= 0 || n_heads % kv.G || (causal != 0 && causal != 1))
+    return fail(c, DCL_ERR_INVALID_ARG, "kv_attention: bad batch, n_q, n_heads (a multiple of n_kv_heads) or causal");
+  if (batch == 0 || n_q == 0) return DCL_OK;
+  if (!q_dev || !q_start_dev || !page_table_dev || !seq_len_dev || !out_dev)
+    return fail(c, DCL_ERR_INVALID_ARG, "kv_attention: NULL argument");
+  if (max_pages <= 0 || max_new <= 0 || (int64_t)max_pages * cache->page_len >= (1ll << 31) ||
+      (int64_t)n_q * n_heads >= (1ll << 31))
+    return fail(c, DCL_ERR_INVALID_ARG, "kv_attention: max_pages, max_new must be > 0 and sizes below 2^31");
+  if (q_stride < (int64_t)n_heads * kv.hd || q_stride % 8 || !aligned16(q_dev) || !aligned16(out_dev))
+    return fail(c, DCL_ERR_INVALID_ARG, "kv_attention: q_stride must be a multiple of 8 and hold a row, q and out 16-byte aligned");
+  if (!(scale >= 0.f) || scale > 3e38f) return fail(c, DCL_ERR_INVALID_ARG, "kv_attention: scale must be >= 0");
+  KvAttn a{static_cast<const __nv_bfloat16*>(q_dev), q_stride, q_start_dev, page_table_dev, seq_len_dev, batch,
+           max_pages, n_q, max_new, n_heads, causal, scale > 0.f ? scale : 1.f / sqrtf((float)kv.hd),
+           static_cast<__nv_bfloat16*>(out_dev), lse_dev};
+  CUDA_TRY(c, kv_attention_launch(kv, a, c->derr, c->stream));
+  return DCL_OK;
+}
+
+dcl_status dcl_sample(dcl_ctx* c, const void* logits_dev, int64_t logits_stride, const float* noise_dev,
+                      int64_t noise_stride, int32_t rows, int32_t V, const float* temperature_dev,
+                      const int32_t* top_k_dev, const float* top_p_dev, const float* min_p_dev, int32_t* token_dev,
+                      float* prob_dev, float* conf_dev) {
+  if (!c) return DCL_ERR_INVALID_ARG;
+  if (rows < 0 || V <= 0 || logits_stride < V || (noise_dev && noise_stride < V))
+    return fail(c, DCL_ERR_INVALID_ARG, "sample: bad rows, V or strides");
+  if (V > (1 << 19)) return fail(c, DCL_ERR_UNSUPPORTED, "sample: V above 2^19");
+  if (rows == 0) return DCL_OK;
+  if (!logits_dev || !token_dev) return fail(c, DCL_ERR_INVALID_ARG, "sample: NULL argument");
+  SampleArgs a{static_cast<const __nv_bfloat16*>(logits_dev), noise_dev, logits_stride, noise_stride, rows, V,
+               temperature_dev, top_k_dev, top_p_dev, min_p_dev, token_dev, prob_dev, conf_dev};
+  CUDA_TRY(c, sample_launch(a, c->stream));
+  return DCL_OK;
+}
+
+dcl_status dcl_synchronise(dcl_ctx* c) {
+  if (!c) return DCL_ERR_INVALID_ARG;
+  return check_device(c);
 }
 
 dcl_status dcl_op_rmsnorm(dcl_ctx* c, const float* x_dev, const void* gain_dev, void* y_dev, int32_t rows, int32_t d,
