@@ -122,6 +122,7 @@ struct dcl_ctx {
   // scratch of the single-kernel entry points, kept from call to call up to OP_SCRATCH_KEEP
   void* op_buf = nullptr;
   size_t op_cap = 0;
+  void* kv_scratch = nullptr;  // kv_attention's parts and counters, from the first call on
   cudaEvent_t ev_done[2] = {nullptr, nullptr};
 };
 
@@ -1490,7 +1491,13 @@ dcl_status dcl_kv_attention(dcl_ctx* c, const dcl_kv_cache* cache, const void* q
   KvAttn a{static_cast<const __nv_bfloat16*>(q_dev), q_stride, q_start_dev, page_table_dev, seq_len_dev, batch,
            max_pages, n_q, max_new, n_heads, causal, scale > 0.f ? scale : 1.f / sqrtf((float)kv.hd),
            static_cast<__nv_bfloat16*>(out_dev), lse_dev};
-  CUDA_TRY(c, kv_attention_launch(kv, a, c->derr, c->stream));
+  if (!c->kv_scratch) {
+    const size_t bytes = kv_attention_scratch(c->num_sms);
+    c->kv_scratch = dev_alloc(c, bytes);
+    if (!c->kv_scratch) return fail(c, DCL_ERR_OOM, "kv_attention: scratch allocation failed");
+    CUDA_TRY(c, cudaMemsetAsync(c->kv_scratch, 0, bytes, c->stream));
+  }
+  CUDA_TRY(c, kv_attention_launch(kv, a, c->kv_scratch, c->num_sms, c->derr, c->stream));
   return DCL_OK;
 }
 

@@ -1,5 +1,28 @@
 // Attention of a few new positions of every sequence over its paged keys and values:
 // out = softmax(scale q k^T) v over the sequence's cached positions.
+//
+// The rows of one kv head (new positions x the query heads that share it) form row tiles of 16 or
+// 32, the most that one pass over the keys serves.  A warp takes 16 keys at a time: S = q k^T and
+// O += P v as m16n8k16 products with the rows on the M side, its own running maximum m, sum l and
+// O in registers, its own ring of key / value tiles in shared memory (16-byte asynchronous copies;
+// no barrier in the loop).  The tensor work is far below its limit as long as the keys arrive from
+// memory, which is what bounds a call of few rows.
+//
+// Work is shared out in units of 128 keys of one (sequence, kv head, row tile), all of a launch in
+// one line, every CTA an equal part of it: a long sequence is spread over many CTAs, many short
+// ones share one, and no CTA waits for another's longer sequence.  A CTA's warps join their
+// (m, l, O) in shared memory; where a line's cut falls inside an item its CTAs leave them in
+// scratch, and the one that comes last joins them in the order of the keys, so that a result does
+// not depend on which that was.
+//
+// FP8 pages.  Codes are widened to fp16, which holds them exactly, q is scaled per row by a power of
+// two into fp16 (its 8 bits fit; what falls below fp16's range is 2^-24 of the row's largest).  A
+// key's exponent scales its score.  A value's exponent e_j goes into the exponent of its
+// probability: P_j = exp2(s_j + e_j - m) with m the running maximum of s_j + e_j, so that P <= 1
+// whatever the values' sizes, and l = sum P_j 2^-e_j.  P is rounded to fp16 (2^-12 of itself;
+// below 2^-14 of the largest term, 2^-25 of that).  bf16 pages: the instruction wants both operands of
+// one type, and bf16 alone would round P by 2^-8 of itself, as much as the output's own rounding;
+// P is given in two bf16 parts (2^-16), the second a product more.
 #include <cuda_fp8.h>
 
 #include "common.cuh"
@@ -8,80 +31,676 @@
 namespace dcl {
 namespace {
 
-constexpr int KA_WARPS = 4;
+constexpr int KA_WARPS = 8;
+constexpr int KA_THREADS = 32 * KA_WARPS;
+constexpr int KA_UNIT = 128;  // keys of a unit of work
 
-// One block: one (row, query head).  Each warp takes every fourth key, a lane HD / 32 components.
+template <int HD, bool FP8, int MT>
+struct KaCfg {
+  static constexpr int ES = FP8 ? 1 : 2;
+  static constexpr int ROWS = 16 * MT;              // rows of an item
+  static constexpr int ROWB = HD * ES;              // bytes of a key
+  static constexpr int TILE = 16 * ROWB;            // 16 keys (or values)
+  static constexpr int STAGE = 2 * TILE + (FP8 ? 32 : 0);
+  static constexpr int STAGES = FP8 ? (HD == 128 ? 5 : 8) : (HD == 128 ? 3 : 5);
+  static constexpr int RING = STAGES * STAGE;       // one warp's
+  static constexpr int O_PITCH = HD + 4;            // floats; a warp's O [ROWS][O_PITCH] takes the ring's place
+  static constexpr int RING_B = RING > ROWS * O_PITCH * 4 ? RING : ROWS * O_PITCH * 4;
+  static constexpr int ML = KA_WARPS * RING_B;      // {m, l} [warp][ROWS], then of the joined rows
+  static constexpr int QF = ML + (KA_WARPS + 1) * ROWS * 8;  // q fragments [MT][HD / 16][lane] of 16 bytes (MT > 1)
+  static constexpr int QA = QF + (MT > 1 ? MT * (HD / 16) * 32 * 16 : 0);
+  static constexpr int HEAD = QA;                   // the walk's variables
+  static constexpr size_t SMEM = HEAD + 64;
+};
+
+struct KaScratch {
+  float* part;  // [2 * CTAs][ROWS][HD + 2]: O, m, l
+  int* count;   // [CTAs], zero between launches
+};
+
+__device__ __forceinline__ uint32_t smem_addr(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ uint4 lds128(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t a) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ uint32_t lds_u16(uint32_t a) {
+  uint16_t v;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ void sts128(uint32_t a, uint4 v) {
+  asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+// two E4M3 codes to two fp16
+__device__ __forceinline__ uint32_t widen_lo(uint32_t w) {
+  uint32_t r;
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\t}" : "=r"(r) : "r"(w));
+  return r;
+}
+__device__ __forceinline__ uint32_t widen_hi(uint32_t w) {
+  uint32_t r;
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, h;\n\t}" : "=r"(r) : "r"(w));
+  return r;
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+template <bool FP8>
+__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  if (FP8)
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  else
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// Byte offset of 16-byte chunk c of row r of a tile.  The order of a row's chunks depends on the row,
+// so that the eight lanes of a 16-byte load (two keys x four places, or four keys x two) meet
+// all the banks.
+template <int ROWB>
+__device__ __forceinline__ uint32_t chunk_at(int r, int c) {
+  return (uint32_t)(r * ROWB + ((c ^ (ROWB == 64 ? (r >> 1) & 3 : r & 7)) << 4));
+}
+// The order in which hd enters the two products is free as long as q and k, and v and the output,
+// agree: a lane's operands are taken from whole 16-byte chunks.  k_chunk: the i-th chunk of 8
+// components of q that lane place t covers.  v_comp: the component of column n of product tile j.
 template <int HD, bool FP8>
-__global__ void __launch_bounds__(32 * KA_WARPS) kv_attention_kernel(KvPool kv, KvAttn a, int* err) {
-  constexpr int E = HD / 32;
-  __shared__ float part[KA_WARPS][HD + 2];
-  const int row = blockIdx.x / a.H, h = blockIdx.x - row * a.H, g = h / (a.H / kv.G);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  int b = 0;  // the sequence whose rows hold this one
-  for (; b < a.batch; ++b)
-    if (row >= a.q_start[b] && row < a.q_start[b + 1]) break;
-  if (b == a.batch) return;
-  const int room = a.max_pages << kv.page_shift, len = min(max(a.lens[b], 0), room);
-  if (a.lens[b] != len && threadIdx.x == 0) report_error(err, DERR_KV_RANGE);
-  const int n = a.causal ? min(len, len - (a.q_start[b + 1] - a.q_start[b]) + (row - a.q_start[b]) + 1) : len;
-  float q[E], o[E], m = -INFINITY, l = 0.f;
-  for (int i = 0; i < E; ++i) {
-    q[i] = __bfloat162float(a.q[row * a.q_stride + (int64_t)h * HD + lane * E + i]) * a.scale;
-    o[i] = 0.f;
+__device__ __forceinline__ int k_chunk(int t, int i) {
+  if (FP8) return t * (HD / 32) + i;
+  return 2 * t + (i & 1) + 8 * (i >> 1);
+}
+template <int HD, bool FP8>
+__device__ __forceinline__ int v_comp(int n, int j) {
+  if (FP8) return n * (HD / 8) + j;
+  return (j >> 3) * 64 + 8 * n + (j & 7);
+}
+
+// Values of a tile that are no numbers: whether this lane's share of its chunks holds any, the value of
+// one component, and zeros in their place.
+template <bool FP8>
+__device__ __forceinline__ uint32_t nonfinite_bits(uint32_t w) {  // all ones in each such element
+  if (FP8) return __vcmpeq4(w & 0x7f7f7f7fu, 0x7f7f7f7fu);
+  return __vcmpeq2(w & 0x7f807f80u, 0x7f807f80u);
+}
+template <bool FP8>
+__device__ __noinline__ bool has_nonfinite(uint32_t tile, int bytes, int lane) {
+  uint32_t any = 0;
+  for (int c = 16 * lane; c < bytes; c += 512) {
+    const uint4 w = lds128(tile + c);
+    any |= nonfinite_bits<FP8>(w.x) | nonfinite_bits<FP8>(w.y) | nonfinite_bits<FP8>(w.z) | nonfinite_bits<FP8>(w.w);
   }
-  auto load = [&](const void* base, const int8_t* exps, int64_t vec, float (&x)[E]) {
-    const float s = FP8 ? kv_pow2(exps[vec]) : 1.f;
-    for (int i = 0; i < E; ++i) {
-      const int64_t at = vec * HD + lane * E + i;
-      x[i] = FP8 ? s * __half2float(__half(__nv_cvt_fp8_to_halfraw(static_cast<const uint8_t*>(base)[at], __NV_E4M3)))
-                 : __bfloat162float(static_cast<const __nv_bfloat16*>(base)[at]);
-    }
+  return any != 0;
+}
+template <bool FP8>
+__device__ __noinline__ void clear_nonfinite(uint32_t tile, int bytes, int lane) {
+  for (int c = 16 * lane; c < bytes; c += 512) {
+    const uint4 w = lds128(tile + c);
+    sts128(tile + c, make_uint4(w.x & ~nonfinite_bits<FP8>(w.x), w.y & ~nonfinite_bits<FP8>(w.y),
+                                w.z & ~nonfinite_bits<FP8>(w.z), w.w & ~nonfinite_bits<FP8>(w.w)));
+  }
+}
+template <int ROWB, bool FP8>
+__device__ __forceinline__ float value_at(uint32_t tile, int row, int comp) {
+  const int byte = comp * (FP8 ? 1 : 2);
+  const uint32_t two = lds_u16(tile + chunk_at<ROWB>(row, byte >> 4) + (byte & 14));
+  if (!FP8) return __uint_as_float(two << 16);
+  const uint32_t code = byte & 1 ? two >> 8 : two & 0xffu;
+  return __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)code, __NV_E4M3)));
+}
+
+// An item: the rows of one row tile of kv head g of sequence b.
+struct KaItem {
+  int b, g, first, rows;  // its rows [first, first + rows) of the nq * rep of the sequence's kv head
+  int row0, nq, len;      // the sequence's first row of q, its new positions, its cached ones
+};
+
+template <int HD, bool FP8, int MT>
+__global__ void __launch_bounds__(KA_THREADS, 1) kv_attention_kernel(KvPool kv, KvAttn a, KaScratch scratch, int* err) {
+  using C = KaCfg<HD, FP8, MT>;
+  constexpr int KS = HD / 16;  // k steps of S, and pairs of column tiles of O
+  constexpr int NT = HD / 8;   // column tiles of O
+  extern __shared__ __align__(128) uint8_t smem[];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = lane >> 2, place = lane & 3;
+  const int rep = a.H / kv.G, room = a.max_pages << kv.page_shift, P = kv.page_len();
+  const uint32_t ring = smem_addr(smem) + warp * C::RING_B;
+  float2* ml = reinterpret_cast<float2*>(smem + C::ML);
+
+  auto seq_rows = [&](int b, int& row0) {
+    row0 = min(max(a.q_start[b], 0), a.rows);
+    return min(max(a.q_start[b + 1], row0), a.rows) - row0;
   };
-  for (int j = warp; j < n; j += KA_WARPS) {
-    const int page = a.table[(int64_t)b * a.max_pages + (j >> kv.page_shift)];
-    if (page < 0 || page >= kv.pages) {
-      if (lane == 0) report_error(err, DERR_KV_RANGE);
-      continue;
+  auto seq_len = [&](int b) { return min(max(a.lens[b], 0), room); };
+  auto tiles_of = [&](int nq) { return (int)(((int64_t)nq * rep + C::ROWS - 1) / C::ROWS); };
+  auto units_of = [&](int len) { return max(1, (len + KA_UNIT - 1) / KA_UNIT); };  // (no key: the rows are still written)
+
+  // ---- this CTA's part [u, end) of the line, and the sequence it begins in
+  int64_t* walk = reinterpret_cast<int64_t*>(smem + C::HEAD);
+  if (warp == 0) {
+    auto scan = [&](int b0, int64_t& own) {  // units of sequences b0 .. b0 + 31: inclusive prefix
+      int row0;
+      const int b = b0 + lane;
+      own = 0;
+      if (b < a.batch) {
+        const int nq = seq_rows(b, row0);
+        if (a.lens[b] != seq_len(b) && blockIdx.x == 0) report_error(err, DERR_KV_RANGE);
+        if (nq) own = (int64_t)kv.G * tiles_of(nq) * units_of(seq_len(b));
+      }
+      int64_t upto = own;
+      for (int d = 1; d < 32; d <<= 1) {
+        const int64_t x = __shfl_up_sync(0xffffffffu, upto, d);
+        if (lane >= d) upto += x;
+      }
+      return upto;
+    };
+    int64_t total = 0, own;
+    int b0 = 0;
+    for (; b0 < a.batch; b0 += 32) total += __shfl_sync(0xffffffffu, scan(b0, own), 31);
+    const int64_t n = min((int64_t)gridDim.x, total);  // (CTAs past it have nothing)
+    const int64_t u = blockIdx.x < n ? total * blockIdx.x / n : 0, end = blockIdx.x < n ? total * (blockIdx.x + 1) / n : 0;
+    int64_t before = 0;
+    int b = 0;
+    if (u < end)
+      for (b0 = 0; b0 < a.batch; b0 += 32) {
+        const int64_t upto = before + scan(b0, own);
+        const unsigned hit = __ballot_sync(0xffffffffu, u < upto);
+        if (hit) {
+          const int l = __ffs(hit) - 1;
+          b = b0 + l;
+          before = __shfl_sync(0xffffffffu, upto - own, l);
+          break;
+        }
+        before = __shfl_sync(0xffffffffu, upto, 31);
+      }
+    if (lane == 0) {
+      walk[0] = u;
+      walk[1] = end;
+      walk[2] = total;
+      walk[3] = before;
+      walk[4] = b;
     }
-    const int64_t vec = kv.vector_of((page << kv.page_shift) + (j & (kv.page_len() - 1)), g);
-    float x[E], s = 0.f;
-    load(kv.k, kv.k_exp, vec, x);
-    for (int i = 0; i < E; ++i) s = fmaf(q[i], x[i], s);
-    for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-    const float top = fmaxf(m, s), c = expf(m - top), p = expf(s - top);
-    load(kv.v, kv.v_exp, vec, x);
-    for (int i = 0; i < E; ++i) o[i] = fmaf(o[i], c, p * x[i]);
-    l = fmaf(l, c, p);
-    m = top;
-  }
-  for (int i = 0; i < E; ++i) part[warp][lane * E + i] = o[i];
-  if (lane == 0) {
-    part[warp][HD] = m;
-    part[warp][HD + 1] = l;
   }
   __syncthreads();
-  float top = -INFINITY, total = 0.f;
-  for (int w = 0; w < KA_WARPS; ++w) top = fmaxf(top, part[w][HD]);
-  for (int w = 0; w < KA_WARPS; ++w)
-    if (part[w][HD + 1] > 0.f) total += part[w][HD + 1] * expf(part[w][HD] - top);
-  for (int i = threadIdx.x; i < HD; i += 32 * KA_WARPS) {
-    float s = 0.f;
-    for (int w = 0; w < KA_WARPS; ++w)
-      if (part[w][HD + 1] > 0.f) s += part[w][i] * expf(part[w][HD] - top);
-    a.out[((int64_t)row * a.H + h) * HD + i] = __float2bfloat16_rn(n > 0 ? s / total : 0.f);
+  int64_t u = walk[0], before = walk[3];  // before: units of the sequences before b
+  const int64_t end = walk[1], total = walk[2];
+  int b = (int)walk[4];
+
+  while (u < end) {
+    // ---- the item of unit u
+    KaItem it;
+    it.nq = seq_rows(b, it.row0);
+    it.len = seq_len(b);
+    const int per = units_of(it.len), nt = tiles_of(it.nq);
+    if (it.nq == 0 || u - before >= (int64_t)kv.G * nt * per) {
+      if (it.nq) before += (int64_t)kv.G * nt * per;
+      ++b;
+      continue;
+    }
+    const int64_t item0 = before + (u - before) / per * per;  // its first unit
+    const int which = (int)((u - before) / per);
+    it.b = b;
+    it.g = which / nt;
+    it.first = (which - it.g * nt) * C::ROWS;
+    it.rows = min(C::ROWS, it.nq * rep - it.first);
+    const int64_t upto = min(end, item0 + per);
+    const int key0 = (int)(u - item0) * KA_UNIT, key1 = min(it.len, (int)(upto - item0) * KA_UNIT);
+
+    // ---- this lane's rows: quad + 8 i of the tile; q as the product's operand; keys each sees
+    int lim[2 * MT];
+    float qa[2 * MT];  // scale * log2(e) * the power of two that q was divided by
+    uint32_t qf[MT == 1 ? KS : 1][4];
+    int lim_min = it.len, lim_max = 0;
+    {
+      // (of all rows of the item: the first sees the fewest keys, the last the most)
+      if (a.causal) {
+        lim_min = it.len - it.nq + it.first / rep + 1;
+        lim_max = min(it.len, it.len - it.nq + (it.first + it.rows - 1) / rep + 1);
+      } else {
+        lim_max = it.len;
+      }
+      uint32_t(*qs)[32][4] = reinterpret_cast<uint32_t(*)[32][4]>(smem + C::QF);
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        uint4 raw[2][HD / 32];
+        float amax[2] = {0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int r = 16 * mt + 8 * i + quad, rr = it.first + r;
+          const bool live = r < it.rows;
+          const int tok = rr / rep, h = it.g * rep + rr - tok * rep;
+          lim[2 * mt + i] = !live ? 0 : a.causal ? min(it.len, it.len - it.nq + tok + 1) : it.len;
+          const __nv_bfloat16* src = a.q + (it.row0 + tok) * a.q_stride + (int64_t)h * HD;
+#pragma unroll
+          for (int c = 0; c < HD / 32; ++c) {
+            raw[i][c] = make_uint4(0, 0, 0, 0);
+            if (live) raw[i][c] = *reinterpret_cast<const uint4*>(src + 8 * k_chunk<HD, FP8>(place, c));
+            if (FP8) {
+              const uint32_t w[4] = {raw[i][c].x, raw[i][c].y, raw[i][c].z, raw[i][c].w};
+#pragma unroll
+              for (int j = 0; j < 4; ++j) amax[i] = fmaxf(amax[i], fmaxf(fabsf(bf16_lo(w[j])), fabsf(bf16_hi(w[j]))));
+            }
+          }
+          float up = 1.f, down = 1.f;
+          if (FP8) {
+            amax[i] = fmaxf(amax[i], __shfl_xor_sync(0xffffffffu, amax[i], 1));
+            amax[i] = fmaxf(amax[i], __shfl_xor_sync(0xffffffffu, amax[i], 2));
+            const int x = max(-120, min(120, (int)(__float_as_uint(amax[i]) >> 23) - 127));
+            up = kv_pow2(x);
+            down = kv_pow2(-x);
+#pragma unroll
+            for (int c = 0; c < HD / 32; ++c) {
+              uint32_t* w = &raw[i][c].x;
+#pragma unroll
+              for (int j = 0; j < 4; ++j) w[j] = pack_f16x2(bf16_lo(w[j]) * down, bf16_hi(w[j]) * down);
+            }
+          }
+          qa[2 * mt + i] = a.scale * kLog2e * up;
+        }
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {  // step s: components 4 s .. 4 s + 3 of this lane's
+          const uint32_t* w0 = &raw[0][s >> 1].x + 2 * (s & 1);
+          const uint32_t* w1 = &raw[1][s >> 1].x + 2 * (s & 1);
+          if (MT == 1) {
+            qf[s][0] = w0[0];
+            qf[s][1] = w1[0];
+            qf[s][2] = w0[1];
+            qf[s][3] = w1[1];
+          } else if (warp == 0) {
+            *reinterpret_cast<uint4*>(qs[mt * KS + s][lane]) = make_uint4(w0[0], w1[0], w0[1], w1[1]);
+          }
+        }
+      }
+      if (MT > 1) __syncthreads();
+    }
+    const uint32_t qs_addr = smem_addr(smem) + C::QF + lane * 16;
+
+    float o[MT][NT][4], m[2 * MT], l[2 * MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o[i][j][k] = 0.f;
+#pragma unroll
+    for (int i = 0; i < 2 * MT; ++i) {
+      m[i] = -INFINITY;
+      l[i] = 0.f;
+    }
+
+    // ---- this warp's key tiles: key0 / 16 + warp, then every KA_WARPS-th
+    const int stop = min(key1, lim_max);
+    const int* table = a.table + (int64_t)it.b * a.max_pages;
+    int next = key0 + 16 * warp;  // first key of the next tile to copy
+    uint32_t bad = 0;             // stages whose page is not the cache's
+    int slot = 0;
+    int page = next < stop ? table[next >> kv.page_shift] : 0;
+    auto issue = [&]() {
+      if (next < stop) {
+        const bool ok = page >= 0 && page < kv.pages;
+        bad = ok ? bad & ~(1u << slot) : bad | 1u << slot;
+        if (ok) {
+          const int64_t vec = kv.vector_of((page << kv.page_shift) + (next & (P - 1)), it.g);
+          const uint8_t* k = static_cast<const uint8_t*>(kv.k) + vec * C::ROWB;
+          const uint8_t* v = static_cast<const uint8_t*>(kv.v) + vec * C::ROWB;
+          const uint32_t dst = ring + slot * C::STAGE;
+#pragma unroll
+          for (int i = 0; i < C::TILE / 512; ++i) {
+            const int c = i * 32 + lane;
+            const uint32_t at = chunk_at<C::ROWB>(c / (C::ROWB / 16), c % (C::ROWB / 16));
+            copy16(dst + at, k + 16 * c);
+            copy16(dst + C::TILE + at, v + 16 * c);
+          }
+          if (FP8 && lane < 2) copy16(dst + 2 * C::TILE + 16 * lane, (lane ? kv.v_exp : kv.k_exp) + vec);
+        } else if (lane == 0) {
+          report_error(err, DERR_KV_RANGE);
+        }
+        next += 16 * KA_WARPS;
+        if (next < stop) page = table[next >> kv.page_shift];
+      }
+      copy_commit();
+      slot = slot + 1 == C::STAGES ? 0 : slot + 1;
+    };
+#pragma unroll
+    for (int s = 0; s < C::STAGES - 1; ++s) issue();
+
+    int cur = 0;
+    for (int key = key0 + 16 * warp; key < stop; key += 16 * KA_WARPS) {
+      copy_wait<C::STAGES - 2>();
+      __syncwarp();
+      const uint32_t sk = ring + cur * C::STAGE, sv = sk + C::TILE, se = sv + C::TILE;
+      const bool skip = bad >> cur & 1;
+      cur = cur + 1 == C::STAGES ? 0 : cur + 1;
+      if (!skip) {
+        const bool masked = key + 16 > lim_min;
+        if (key + 16 > it.len) {  // values past the sequence's end may be anything: 0 * NaN
+          for (int c = lane; c < C::TILE / 16; c += 32)
+            if (key + c / (C::ROWB / 16) >= it.len)
+              sts128(sv + chunk_at<C::ROWB>(c / (C::ROWB / 16), c % (C::ROWB / 16)), make_uint4(0, 0, 0, 0));
+          __syncwarp();
+        }
+        // S = q k^T: two column tiles of 8 keys
+        float s[MT][2][4];
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) s[i][j][k] = 0.f;
+        constexpr int KCH = FP8 ? HD / 64 : HD / 32;  // 16-byte chunks of a key per lane
+        constexpr int SPC = FP8 ? 4 : 2;              // k steps of a chunk
+#pragma unroll
+        for (int c = 0; c < KCH; ++c) {
+          uint4 w[2];
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+            w[j] = lds128(sk + chunk_at<C::ROWB>(8 * j + quad, FP8 ? place * KCH + c : k_chunk<HD, FP8>(place, c)));
+#pragma unroll
+          for (int x = 0; x < SPC; ++x) {
+            const int st = c * SPC + x;
+            uint32_t qreg[MT][4];
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+              if (MT == 1) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) qreg[i][k] = qf[MT == 1 ? st : 0][k];
+              } else {
+                const uint4 q4 = lds128(qs_addr + (i * KS + st) * 512);
+                qreg[i][0] = q4.x;
+                qreg[i][1] = q4.y;
+                qreg[i][2] = q4.z;
+                qreg[i][3] = q4.w;
+              }
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              const uint32_t* ww = &w[j].x;
+              const uint32_t b0 = FP8 ? widen_lo(ww[x]) : ww[2 * (x & 1)];
+              const uint32_t b1 = FP8 ? widen_hi(ww[x]) : ww[2 * (x & 1) + 1];
+#pragma unroll
+              for (int i = 0; i < MT; ++i) mma16816<FP8>(s[i][j], qreg[i], b0, b1);
+            }
+          }
+        }
+        // scores in units of log2; with FP8 values their exponent added
+        float kf[4], ev[4], vi[4];
+        if (FP8) {
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const uint32_t ek = lds_u16(se + 8 * j + 2 * place), e2 = lds_u16(se + 16 + 8 * j + 2 * place);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const int x = (int)(int8_t)(ek >> (8 * k)), y = max(-126, (int)(int8_t)(e2 >> (8 * k)));
+              kf[2 * j + k] = kv_pow2(x);
+              ev[2 * j + k] = (float)y;
+              vi[2 * j + k] = kv_pow2(-y);
+            }
+          }
+        }
+        uint32_t p[MT][4], p_lo[MT][4];
+        bool grew = false;
+        float alpha[2 * MT];
+#pragma unroll
+        for (int i = 0; i < 2 * MT; ++i) {
+          float x[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float raw = s[i >> 1][j >> 1][2 * (i & 1) + (j & 1)];
+            x[j] = FP8 ? fmaf(raw, qa[i] * kf[j], ev[j]) : raw * qa[i];
+          }
+          if (masked) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (key + 8 * (j >> 1) + 2 * place + (j & 1) >= lim[i]) x[j] = -INFINITY;
+          }
+          float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+          const float mn = fmaxf(m[i], top);
+          grew |= mn > m[i];
+          const float ref = mn == -INFINITY ? 0.f : mn;  // (nothing seen yet: exp2(-inf) = 0)
+          alpha[i] = exp2_fast(m[i] - ref);
+          m[i] = mn;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) x[j] = exp2_fast(x[j] - ref);
+          float sum = 0.f;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) sum = FP8 ? fmaf(x[j], vi[j], sum) : sum + x[j];
+          l[i] = fmaf(l[i], alpha[i], sum);
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const uint32_t hi = FP8 ? pack_f16x2(x[2 * j], x[2 * j + 1]) : pack_bf16x2(x[2 * j], x[2 * j + 1]);
+            p[i >> 1][2 * j + (i & 1)] = hi;
+            if (!FP8) p_lo[i >> 1][2 * j + (i & 1)] = pack_bf16x2(x[2 * j] - bf16_lo(hi), x[2 * j + 1] - bf16_hi(hi));
+          }
+        }
+        if (__any_sync(0xffffffffu, grew)) {
+#pragma unroll
+          for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+              o[i][j][0] *= alpha[2 * i];
+              o[i][j][1] *= alpha[2 * i];
+              o[i][j][2] *= alpha[2 * i + 1];
+              o[i][j][3] *= alpha[2 * i + 1];
+            }
+        }
+        // A value that is no number and that only some of the rows see (0 * NaN): it is added to the
+        // rows that do, one by one, and out of the product.
+        if (masked && a.causal && __any_sync(0xffffffffu, has_nonfinite<FP8>(sv, C::TILE, lane))) {
+#pragma unroll 1
+          for (int jj = 0; jj < 16; ++jj) {
+#pragma unroll
+            for (int i = 0; i < 2 * MT; ++i) {
+              const uint32_t pair = __shfl_sync(0xffffffffu, jj < 8 ? p[i >> 1][i & 1] : p[i >> 1][2 + (i & 1)],
+                                                4 * quad + ((jj & 7) >> 1));
+              if (key + jj >= lim[i]) continue;
+              const uint32_t half = jj & 1 ? pair >> 16 : pair & 0xffffu;
+              const float pj = FP8 ? __half2float(__ushort_as_half((unsigned short)half)) : __uint_as_float(half << 16);
+#pragma unroll
+              for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                  const float v = value_at<C::ROWB, FP8>(sv, jj, v_comp<HD, FP8>(2 * place + k, j));
+                  if (!isfinite(v)) o[i >> 1][j][2 * (i & 1) + k] += pj * v;
+                }
+            }
+          }
+          __syncwarp();
+          clear_nonfinite<FP8>(sv, C::TILE, lane);
+          __syncwarp();
+        }
+        // O += P v
+        if (FP8) {
+          constexpr int W = HD / 32;  // 4-code words of a value per lane
+          uint32_t v[4][W];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {  // keys 2 place, 2 place + 1, and 8 on
+            const int row = 2 * place + (r & 1) + 8 * (r >> 1);
+            if (W == 4) {
+              const uint4 x = lds128(sv + chunk_at<C::ROWB>(row, quad));
+              v[r][0] = x.x;
+              v[r][1] = x.y;
+              v[r][W - 2] = x.z;
+              v[r][W - 1] = x.w;
+            } else {
+              const uint2 x = lds64(sv + chunk_at<C::ROWB>(row, quad >> 1) + 8 * (quad & 1));
+              v[r][0] = x.x;
+              v[r][1] = x.y;
+            }
+          }
+#pragma unroll
+          for (int w = 0; w < W; ++w) {
+            const uint32_t x0 = __byte_perm(v[0][w], v[1][w], 0x5140), x1 = __byte_perm(v[0][w], v[1][w], 0x7362);
+            const uint32_t y0 = __byte_perm(v[2][w], v[3][w], 0x5140), y1 = __byte_perm(v[2][w], v[3][w], 0x7362);
+            const uint32_t b0[4] = {widen_lo(x0), widen_hi(x0), widen_lo(x1), widen_hi(x1)};
+            const uint32_t b1[4] = {widen_lo(y0), widen_hi(y0), widen_lo(y1), widen_hi(y1)};
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+              for (int i = 0; i < MT; ++i) mma16816<FP8>(o[i][4 * w + j], p[i], b0[j], b1[j]);
+          }
+        } else {
+#pragma unroll
+          for (int c = 0; c < HD / 64; ++c) {
+            uint4 v[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              v[r] = lds128(sv + chunk_at<C::ROWB>(2 * place + (r & 1) + 8 * (r >> 1), quad + 8 * c));
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+              const uint32_t *v0 = &v[0].x, *v1 = &v[1].x, *v2 = &v[2].x, *v3 = &v[3].x;
+#pragma unroll
+              for (int x = 0; x < 2; ++x) {
+                const uint32_t sel = x ? 0x7632 : 0x5410;
+                const uint32_t b0 = __byte_perm(v0[w], v1[w], sel), b1 = __byte_perm(v2[w], v3[w], sel);
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                  mma16816<FP8>(o[i][8 * c + 2 * w + x], p[i], b0, b1);
+                  mma16816<FP8>(o[i][8 * c + 2 * w + x], p_lo[i], b0, b1);
+                }
+              }
+            }
+          }
+        }
+      }
+      __syncwarp();
+      issue();
+    }
+    copy_wait<0>();
+    __syncwarp();
+
+    // ---- join the warps
+#pragma unroll
+    for (int i = 0; i < 2 * MT; ++i) {
+      l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
+      l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
+      if (place == 0) ml[warp * C::ROWS + 8 * i + quad] = make_float2(m[i], l[i]);
+    }
+    float* mine = reinterpret_cast<float*>(smem + warp * C::RING_B);
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          mine[(16 * i + quad + 8 * (k >> 1)) * C::O_PITCH + v_comp<HD, FP8>(2 * place + (k & 1), j)] = o[i][j][k];
+    __syncthreads();
+    const bool whole = u == item0 && upto == item0 + per;
+    auto finish = [&](int r, int d, float top, float sum, float acc) {  // component d of row r
+      const int rr = it.first + r, tok = rr / rep, h = it.g * rep + rr - tok * rep;
+      const int64_t at = (int64_t)(it.row0 + tok) * a.H + h;
+      a.out[at * HD + d] = __float2bfloat16_rn(sum == 0.f ? 0.f : acc / sum);
+      if (d == 0 && a.lse) a.lse[at] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+    };
+    constexpr int PART = HD + 2;
+    const int64_t my_part = 2 * (int64_t)blockIdx.x + (u == item0);
+    for (int i = threadIdx.x; i < it.rows * HD; i += KA_THREADS) {
+      const int r = i / HD, d = i - r * HD;
+      float top = -INFINITY, sum = 0.f, acc = 0.f;
+#pragma unroll
+      for (int w = 0; w < KA_WARPS; ++w) top = fmaxf(top, ml[w * C::ROWS + r].x);
+      {
+#pragma unroll
+        for (int w = 0; w < KA_WARPS; ++w) {
+          const float2 x = ml[w * C::ROWS + r];
+          const float f = x.x == -INFINITY ? 0.f : exp2_fast(x.x - top);
+          sum = fmaf(x.y, f, sum);
+          acc = fmaf(reinterpret_cast<float*>(smem + w * C::RING_B)[r * C::O_PITCH + d], f, acc);
+        }
+      }
+      if (whole) {
+        finish(r, d, top, sum, acc);
+      } else {
+        float* part = scratch.part + (my_part * C::ROWS + r) * PART;
+        part[d] = acc;
+        if (d == 0) {
+          part[HD] = top;
+          part[HD + 1] = sum;
+        }
+      }
+    }
+    if (!whole) {  // the CTAs c0 .. c1 share this item
+      const int64_t n = min((int64_t)gridDim.x, total);
+      const int c0 = (int)(((item0 + 1) * n - 1) / total), c1 = (int)(((item0 + per) * n - 1) / total);
+      int* last = reinterpret_cast<int*>(smem + C::HEAD + 48);
+      __threadfence();
+      __syncthreads();
+      if (threadIdx.x == 0) {
+        const int done = atomicAdd(&scratch.count[c0], 1);
+        *last = done == c1 - c0;
+        if (*last) scratch.count[c0] = 0;
+        __threadfence();
+      }
+      __syncthreads();
+      if (*last) {
+        for (int i = threadIdx.x; i < it.rows * HD; i += KA_THREADS) {
+          const int r = i / HD, d = i - r * HD;
+          auto part_of = [&](int c) {
+            return scratch.part + ((2 * (int64_t)c + (c == c0)) * C::ROWS + r) * PART;
+          };
+          float top = -INFINITY, sum = 0.f, acc = 0.f;
+          for (int c = c0; c <= c1; ++c) top = fmaxf(top, __ldcg(part_of(c) + HD));
+          for (int c = c0; c <= c1; ++c) {
+            const float* x = part_of(c);
+            const float mc = __ldcg(x + HD), f = mc == -INFINITY ? 0.f : exp2_fast(mc - top);
+            sum = fmaf(__ldcg(x + HD + 1), f, sum);
+            acc = fmaf(__ldcg(x + d), f, acc);
+          }
+          finish(r, d, top, sum, acc);
+        }
+      }
+    }
+    __syncthreads();
+    u = upto;
   }
-  if (threadIdx.x == 0 && a.lse) a.lse[(int64_t)row * a.H + h] = n > 0 ? top + logf(total) : -INFINITY;
+}
+
+template <int HD, bool FP8, int MT>
+cudaError_t launch_as(const KvPool& kv, const KvAttn& a, const KaScratch& s, int ctas, int* err, cudaStream_t stream) {
+  using C = KaCfg<HD, FP8, MT>;
+  static_assert(C::SMEM <= 232448, "shared memory per CTA");
+  static_assert(2 * C::ROWS * (HD + 2) * 4 <= KV_ATTN_PART_BYTES, "scratch per CTA");
+  auto kern = kv_attention_kernel<HD, FP8, MT>;
+  static const cudaError_t set =
+      cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM);
+  if (set != cudaSuccess) return set;
+  kern<<<ctas, KA_THREADS, C::SMEM, stream>>>(kv, a, s, err);
+  return cudaGetLastError();
+}
+
+template <int HD, bool FP8>
+cudaError_t launch_rows(const KvPool& kv, const KvAttn& a, const KaScratch& s, int ctas, int* err, cudaStream_t stream) {
+  if ((int64_t)a.max_new * (a.H / kv.G) <= 16) return launch_as<HD, FP8, 1>(kv, a, s, ctas, err, stream);
+  return launch_as<HD, FP8, 2>(kv, a, s, ctas, err, stream);
 }
 
 }  // namespace
 
-cudaError_t kv_attention_launch(const KvPool& kv, const KvAttn& a, int* err, cudaStream_t stream) {
-  const unsigned grid = (unsigned)a.rows * (unsigned)a.H;
-  if (kv.hd == 128 && kv.fp8) kv_attention_kernel<128, true><<<grid, 32 * KA_WARPS, 0, stream>>>(kv, a, err);
-  else if (kv.hd == 128) kv_attention_kernel<128, false><<<grid, 32 * KA_WARPS, 0, stream>>>(kv, a, err);
-  else if (kv.fp8) kv_attention_kernel<64, true><<<grid, 32 * KA_WARPS, 0, stream>>>(kv, a, err);
-  else kv_attention_kernel<64, false><<<grid, 32 * KA_WARPS, 0, stream>>>(kv, a, err);
-  return cudaGetLastError();
+size_t kv_attention_scratch(int sms) { return (size_t)sms * (KV_ATTN_PART_BYTES + sizeof(int)); }
+
+cudaError_t kv_attention_launch(const KvPool& kv, const KvAttn& a, void* scratch, int sms, int* err, cudaStream_t stream) {
+  KaScratch s{static_cast<float*>(scratch),
+              reinterpret_cast<int*>(static_cast<uint8_t*>(scratch) + (size_t)sms * KV_ATTN_PART_BYTES)};
+  if (kv.hd == 128) return kv.fp8 ? launch_rows<128, true>(kv, a, s, sms, err, stream) : launch_rows<128, false>(kv, a, s, sms, err, stream);
+  return kv.fp8 ? launch_rows<64, true>(kv, a, s, sms, err, stream) : launch_rows<64, false>(kv, a, s, sms, err, stream);
 }
 
 }  // namespace dcl

@@ -39,7 +39,11 @@ struct KvAttn {
   __nv_bfloat16* out;       // [rows][H][hd]
   float* lse;               // [rows][H] or NULL
 };
-cudaError_t kv_attention_launch(const KvPool& kv, const KvAttn& a, int* err, cudaStream_t stream);
+// Scratch of a launch on `sms` SMs: the parts of rows whose keys several CTAs share, then counters,
+// zero before the first launch and left zero by each.
+constexpr size_t KV_ATTN_PART_BYTES = 2 * 32 * (128 + 2) * sizeof(float);  // per CTA
+size_t kv_attention_scratch(int sms);
+cudaError_t kv_attention_launch(const KvPool& kv, const KvAttn& a, void* scratch, int sms, int* err, cudaStream_t stream);
 
 // Drawing tokens (sample.cu).
 struct SampleArgs {

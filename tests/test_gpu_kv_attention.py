@@ -197,6 +197,34 @@ def test_nan_in_a_seen_vector_reaches_the_row_and_no_other(ops):
     assert nan[0, 0, 5] and nan.sum() == 1
 
 
+@pytest.mark.parametrize("fp8_format", [True, False])
+@pytest.mark.parametrize("heads,kv,hd,new", [(2, 2, 64, 5), (2, 2, 128, 12), (4, 1, 128, 40), (8, 2, 64, 20)])
+def test_causal_rows_before_a_value_that_is_no_number_do_not_see_it(ops, heads, kv, hd, new, fp8_format):
+    rng = np.random.default_rng(16)
+    n = 50
+    cache, table, values = _pool(rng, [n], heads, kv, hd, 16, fp8_format)
+    at = n - 3  # seen by the last three rows only
+    page, pos = int(table[0, at // 16]), at % 16
+    cache.v[page, 0, pos, 7] = 0xFF if fp8_format else float("nan")
+    if not fp8_format:
+        cache.v[page, 0, pos, 9] = float("inf")
+    q = torch.from_numpy(rng.normal(0, 1, (new, heads, hd))).to(torch.bfloat16).cuda()
+    out = torch.zeros(new, heads, hd, dtype=torch.bfloat16, device="cuda")
+    ops.kv_attention(cache, q, torch.tensor([0, new], dtype=torch.int32, device="cuda"), table,
+                     torch.tensor([n], dtype=torch.int32, device="cuda"), out, max_new=new, causal=True)
+    ops.synchronise()
+    got = out.float().cpu().numpy().astype(np.float64)
+    o, _, A, _ = _reference(q.float().cpu().numpy().astype(np.float64), values["k"][0], values["v"][0], new, True,
+                            hd ** -0.5)
+    strange = np.zeros_like(o, bool)
+    strange[-3:, :heads // kv, 7] = True
+    if not fp8_format:
+        strange[-3:, :heads // kv, 9] = True
+        assert np.isinf(got[-3:, :heads // kv, 9]).all()
+    assert np.isnan(got[-3:, :heads // kv, 7]).all()
+    assert (np.abs(got - o)[~strange] <= ((2.0 ** -8 + 2.0 ** -12) * A)[~strange]).all()
+
+
 def test_a_page_or_length_outside_the_cache_is_reported(ops):
     rng = np.random.default_rng(7)
     cache, table, values = _pool(rng, [40, 40], 2, 2, 64, 16, True)
