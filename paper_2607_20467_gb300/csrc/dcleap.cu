@@ -1506,8 +1506,8 @@ dcl_status dcl_sample(dcl_ctx* c, const void* logits_dev, int64_t logits_stride,
                       const int32_t* top_k_dev, const float* top_p_dev, const float* min_p_dev, int32_t* token_dev,
                       float* prob_dev, float* conf_dev) {
   if (!c) return DCL_ERR_INVALID_ARG;
-  if (rows < 0 || V <= 0 || logits_stride < V || (noise_dev && noise_stride < V))
-    return fail(c, DCL_ERR_INVALID_ARG, "sample: bad rows, V or strides");
+  if (rows < 0 || rows > (1 << 24) || V <= 0 || logits_stride < V || (noise_dev && noise_stride < V))
+    return fail(c, DCL_ERR_INVALID_ARG, "sample: bad rows (at most 2^24), V or strides");
   if (V > (1 << 19)) return fail(c, DCL_ERR_UNSUPPORTED, "sample: V above 2^19");
   if (rows == 0) return DCL_OK;
   if (!logits_dev || !token_dev) return fail(c, DCL_ERR_INVALID_ARG, "sample: NULL argument");
