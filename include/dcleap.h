@@ -367,8 +367,8 @@ dcl_status dcl_kv_attention(dcl_ctx* ctx, const dcl_kv_cache* cache, const void*
  * of independent standard Gumbel numbers -ln(-ln u) that is a draw from the kept tokens'
  * renormalised softmax; noise_dev NULL takes the largest y.  noise_dev float [rows][V], rows
  * noise_stride elements apart, read for kept tokens only.  temperature, top_k, top_p, min_p:
- * one value per row, or NULL for 1, 0, 1, 0; a temperature of 0 (or less, or NaN) takes the
- * largest logit.  Logits of -inf and NaN are never drawn; a row of nothing else gets token -1 and
+ * one value per row, or NULL for 1, 0, 1, 0; a temperature of 0 (or below 1e-37, or
+ * NaN) takes the largest logit.  Logits of -inf and NaN are never drawn; a row of nothing else gets token -1 and
  * zeros.  token_dev int32 [rows]; prob_dev float [rows] (may be NULL): the token's probability
  * among the kept ones; conf_dev float [rows] (may be NULL): its probability under softmax(z)
  * over all V, the confidence of Eq. threshold_pd.  V at most 2^19.

@@ -10,7 +10,8 @@
 // large vocabulary each) and exchange what they find through distributed shared memory.  bf16
 // logits take few distinct values where it matters (16 octaves below the largest are 2048), so the
 // order is found by counting them: a histogram over the values themselves in whole numbers,
-// one scan of counts and masses (count times the value's weight, summed in fp64), and both
+// one scan of counts and masses (count times the value's weight, in fixed point of 2^-44, which
+// 2^19 tokens of weight 1 do not overflow; in fp64 the scan took longer than all else), and both
 // boundaries are exact up to the rounding of the weights; nothing is sorted and nothing depends on
 // the order in which threads arrive.  A prefix that ends below the histogram's window (flat rows)
 // takes a window further down, empty stretches skipped.
@@ -29,8 +30,8 @@ namespace {
 constexpr int SM_THREADS = 256;
 constexpr int SM_WARPS = SM_THREADS / 32;
 constexpr int SM_BINS = 2048;      // distinct logits of a window
+constexpr int SM_FIRST = 256;      // of the first one
 constexpr int SM_CLUSTER = 8;      // most CTAs of a row
-constexpr int SM_PER_THREAD = SM_BINS / SM_THREADS;
 constexpr uint32_t NEG_INF = 0xff80u;
 constexpr uint32_t KEY_NEG_INF = 0x007fu;
 
@@ -50,14 +51,21 @@ __device__ __forceinline__ float exp_fast(float x) {  // e^x, x <= 0: |x| 2^-24 
   return y;
 }
 
+using mass_t = unsigned long long;  // units of 2^-44 of the largest token's weight
+constexpr float MASS_ONE = 17592186044416.f;
+__device__ __forceinline__ mass_t mass_share(float p, mass_t m) {  // p m, 0 <= p < 1
+  return p > 0.f ? (mass_t)((double)p * (double)m) : 0;
+}
+
 struct Decision {
   int more;         // 1: another window is needed, from bin `start`
   int start;
   int last, ties;   // bin of the last kept logit, tokens of it that are kept
   int count;        // tokens above the window
-  double mass;      // their mass
+  mass_t mass;      // their mass
   int k_bin, k_ties;  // the top-k prefix (k_bin < 0: not found yet)
-  double goal;      // mass that the top-p prefix has to reach (negative: not known yet)
+  int goal_known;
+  mass_t goal;      // mass that the top-p prefix has to reach
 };
 
 struct SampleShared {
@@ -70,7 +78,7 @@ struct SampleShared {
   uint32_t red_u[SM_WARPS];
   unsigned long long red_b[SM_WARPS];
   int scan_c[SM_WARPS];
-  double scan_m[SM_WARPS];
+  mass_t scan_m[SM_WARPS];
   int pick;
 };
 
@@ -95,12 +103,13 @@ __device__ __forceinline__ T block_reduce(T v, Op op, T* buf) {
   return v;
 }
 
-struct Best {  // largest s, the lower index of equals
+constexpr float LOWEST = -3.402823466e38f;
+
+struct Best {  // largest s, the lower index of equals (a thread meets its tokens in order)
   float s = -INFINITY;
   int at = -1;
-  __device__ __forceinline__ void take(float x, int i, bool valid) {
-    x = fmaxf(x, -INFINITY);  // (NaN noise: never the largest)
-    if (x > s || (at < 0 && valid)) {
+  __device__ __forceinline__ void take(float x, int i) {
+    if (x > s) {
       s = x;
       at = i;
     }
@@ -113,15 +122,175 @@ struct Best {  // largest s, the lower index of equals
     return (unsigned long long)ord << 32 | (0xffffffffu - (uint32_t)at);
   }
 };
+// y + noise.  Noise of -inf or NaN counts as the lowest number, so that a kept token (y finite)
+// always beats one that is not (y = -inf).
+__device__ __forceinline__ float perturbed(float y, float noise) { return __fadd_rn(y, fmaxf(noise, LOWEST)); }
+
+// What the leader needs to look for the ends of the prefix in a window.
+struct PrefixArgs {
+  cg::cluster_group& cluster;
+  SampleShared& sh;
+  uint32_t* hist;
+  int C, V;
+  uint32_t kmax;
+  float zmax, inv;
+  int k;
+  float p;
+  bool by_k, by_p;
+  int start, width;
+};
+
+// The leader's step: scans the row's counts and masses over the window (PER consecutive bins a
+// thread) and writes the decision.  All its threads call it.
+template <int PER>
+__device__ __forceinline__ void scan_window(const PrefixArgs& q) {
+  SampleShared& sh = q.sh;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, start = q.start, k = q.k;
+  uint32_t n[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) n[i] = 0;
+#pragma unroll
+  for (int c = 0; c < SM_CLUSTER; ++c) {
+    if (c >= q.C) break;
+    const uint32_t* from = q.cluster.map_shared_rank(q.hist, c) + tid * PER;
+    if constexpr (PER % 4 == 0) {
+#pragma unroll
+      for (int i = 0; i < PER / 4; ++i) {
+        const uint4 y = reinterpret_cast<const uint4*>(from)[i];
+        n[4 * i] += y.x;
+        n[4 * i + 1] += y.y;
+        n[4 * i + 2] += y.z;
+        n[4 * i + 3] += y.w;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) n[i] += from[i];
+    }
+  }
+  mass_t w[PER];
+  int count = 0;
+  mass_t own = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int bin = start + tid * PER + i;
+    const uint32_t key = q.kmax - (uint32_t)bin;
+    w[i] = 0;
+    if (n[i]) w[i] = __float2ull_rn(MASS_ONE * exp_fast(__fmul_rn(bin == 0 ? 0.f : __fsub_rn(key_value(key), q.zmax), q.inv)));
+    count += (int)n[i];
+    own += (mass_t)n[i] * w[i];
+  }
+  int c_up = count;
+  mass_t m_up = own;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int c = __shfl_up_sync(0xffffffffu, c_up, d);
+    const mass_t m = __shfl_up_sync(0xffffffffu, m_up, d);
+    if (lane >= d) {
+      c_up += c;
+      m_up += m;
+    }
+  }
+  if (lane == 31) {
+    sh.scan_c[warp] = c_up;
+    sh.scan_m[warp] = m_up;
+  }
+  if (tid == 0) sh.pick = -1;
+  __syncthreads();
+  int c_all = 0, c_before = sh.dec.count + c_up - count;
+  mass_t m_all = 0, m_before = sh.dec.mass + m_up - own;
+  for (int i = 0; i < SM_WARPS; ++i) {
+    if (i < warp) {
+      c_before += sh.scan_c[i];
+      m_before += sh.scan_m[i];
+    }
+    c_all += sh.scan_c[i];
+    m_all += sh.scan_m[i];
+  }
+  const int c_end = sh.dec.count + c_all;
+  const mass_t m_end = sh.dec.mass + m_all, m_start = sh.dec.mass;
+  int k_bin = sh.dec.k_bin;
+  const bool goal_known = sh.dec.goal_known;
+  __syncthreads();  // (dec has been read)
+  if (k_bin < 0 && c_end >= k) {  // the top-k prefix ends in this window
+    int c = c_before;
+    mass_t m = m_before;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      if (c < k && c + (int)n[i] >= k) {
+        sh.dec.k_bin = start + tid * PER + i;
+        sh.dec.k_ties = k - c;
+        sh.dec.goal = q.by_p ? mass_share(q.p, m + (mass_t)(k - c) * w[i]) : 0;
+      }
+      c += (int)n[i];
+      m += (mass_t)n[i] * w[i];
+    }
+  } else if (!q.by_k && !goal_known && tid == 0) {
+    float all = 0.f;
+    for (int c = 0; c < q.C; ++c) all += sh.mass[c];
+    sh.dec.goal_known = 1;
+    sh.dec.goal = mass_share(q.p, __float2ull_rn(MASS_ONE * all));
+  }
+  __syncthreads();
+  k_bin = sh.dec.k_bin;
+  const mass_t goal = sh.dec.goal;
+  uint32_t below = 0xffffffffu;  // where the next window would begin, if any token is left
+  for (int c = 0; c < q.C; ++c) below = min(below, sh.next[c]);
+  const bool k_known = k_bin >= 0, rest = c_end < q.V;
+  if (k_known && q.by_p && (m_start < goal || start == 0) && (m_end >= goal || k_bin < start + q.width || !rest)) {
+    // the top-p prefix ends in this window: the last logit with less than the goal before it
+    int mine = -1, most = 0;
+    mass_t m = m_before, room = 0, each = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int bin = start + tid * PER + i;
+      if (n[i] && bin <= k_bin && (m < goal || bin == 0)) {
+        mine = bin;
+        most = (int)n[i];
+        each = w[i];
+        room = goal > m ? goal - m : 0;
+      }
+      m += (mass_t)n[i] * w[i];
+    }
+    if (mine >= 0) atomicMax(&sh.pick, mine);
+    __syncthreads();
+    if (mine >= 0 && mine == sh.pick) {
+      // token i of the logit (from 0) is kept where i of them do not fill the room
+      const mass_t need = each ? (room + each - 1) / each : (mass_t)most;
+      const int ties = need < 1 ? 1 : need < (mass_t)most ? (int)need : most;
+      sh.dec.last = mine;
+      sh.dec.ties = mine == k_bin ? min(ties, sh.dec.k_ties) : ties;
+      sh.dec.more = 0;
+    }
+  } else if (tid == 0) {
+    if (k_known && !q.by_p) {
+      sh.dec.last = k_bin;
+      sh.dec.ties = sh.dec.k_ties;
+      sh.dec.more = 0;
+    } else {
+      sh.dec.more = 1;
+      if (k_known && m_start >= goal) {  // the top-p prefix ended in an earlier window
+        sh.dec.start = 0;
+        sh.dec.count = 0;
+        sh.dec.mass = 0;
+      } else {
+        sh.dec.start = (int)below;
+        sh.dec.count = c_end;
+        sh.dec.mass = m_end;
+      }
+    }
+  }
+}
+
+// (a call of its own: inlined it took the registers of the loops over the row)
+__device__ __noinline__ void scan_wide(const PrefixArgs& q) { scan_window<SM_BINS / SM_THREADS>(q); }
 
 template <bool TRUNC>
-__global__ void __launch_bounds__(SM_THREADS) sample_kernel(SampleArgs a, int seg) {
+__global__ void __launch_bounds__(SM_THREADS, TRUNC ? 3 : 5) sample_kernel(SampleArgs a, int seg) {
   extern __shared__ __align__(16) uint8_t smem[];
   SampleShared& sh = *reinterpret_cast<SampleShared*>(smem);
   constexpr int HEAD = (sizeof(SampleShared) + 15) / 16 * 16;
   uint32_t* hist = reinterpret_cast<uint32_t*>(smem + HEAD);  // this CTA's counts of the window
-  uint32_t* sum = hist + SM_BINS;                             // the leader's: the row's
-  uint16_t* zs = reinterpret_cast<uint16_t*>(smem + HEAD + (TRUNC ? 8 * SM_BINS : 0));
+  uint16_t* zs = reinterpret_cast<uint16_t*>(smem + HEAD + (TRUNC ? 4 * SM_BINS : 0));
   cg::cluster_group cluster = cg::this_cluster();
   const int rank = (int)cluster.block_rank(), C = (int)cluster.num_blocks();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -134,36 +303,67 @@ __global__ void __launch_bounds__(SM_THREADS) sample_kernel(SampleArgs a, int se
   const int shift = (int)((reinterpret_cast<uintptr_t>(z) >> 1) & 7);
   const int base = rank * seg - shift, lo = max(0, -base), hi = min(seg, V - base), nv = hi > 0 ? (hi + 7) / 8 : 0;
 
+  // (asked for before the row, used after it)
+  const float T = a.temperature ? a.temperature[row] : 1.f;
+  int k = 0;
+  float p = 1.f, mp = 0.f;
+  if (TRUNC) {
+    if (a.top_k) k = a.top_k[row];
+    if (a.top_p) p = a.top_p[row];
+    if (a.min_p) mp = a.min_p[row];
+  }
+
   // ---- the row into shared memory, its largest logit
-  uint32_t top = 0;
-  for (int v = tid; v < nv; v += SM_THREADS) {
-    uint32_t w[4];
-    if (8 * v >= lo && 8 * v + 8 <= hi) {
-      const uint4 x = *reinterpret_cast<const uint4*>(z + base + 8 * v);
-      w[0] = x.x;
-      w[1] = x.y;
-      w[2] = x.z;
-      w[3] = x.w;
-    } else {
+  const int v_lo = (lo + 7) / 8, v_hi = max(v_lo, hi / 8);  // vectors that lie inside the row
+  // (the others: at most 7 elements at either end)
+  const int n_head = min(8 * v_lo, hi) - min(lo, hi), n_edge = n_head + max(0, hi - 8 * v_hi);
+  auto edge = [&](int i) { return i < n_head ? lo + i : 8 * v_hi + i - n_head; };
+  float top_z = -INFINITY;
+  auto keep = [&](int v, uint32_t (&w)[4]) {
+    uint32_t odd = 0;  // a sign bit for each NaN (magnitude above 0x7f80) and -0
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t t = w[i] ^ 0x80008000u;
+      odd |= (((w[i] & 0x7fff7fffu) + 0x007f007fu) | ((t - 0x00010001u) & ~t)) & 0x80008000u;
+    }
+    if (odd) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = canonical(w[i] & 0xffffu) | canonical(w[i] >> 16) << 16;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top_z = fmaxf(top_z, fmaxf(bf16_lo(w[i]), bf16_hi(w[i])));
+    reinterpret_cast<uint4*>(zs)[v] = make_uint4(w[0], w[1], w[2], w[3]);
+  };
+  constexpr int LD = 4;  // loads in flight
+  for (int v0 = v_lo + tid; v0 < v_hi; v0 += LD * SM_THREADS) {
+    uint4 x[LD];
+#pragma unroll
+    for (int i = 0; i < LD; ++i)
+      if (v0 + i * SM_THREADS < v_hi) x[i] = __ldcs(reinterpret_cast<const uint4*>(z + base) + v0 + i * SM_THREADS);
+#pragma unroll
+    for (int i = 0; i < LD; ++i)
+      if (v0 + i * SM_THREADS < v_hi) {
+        uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+        keep(v0 + i * SM_THREADS, w);
+      }
+  }
+  if (tid < 2) {  // the vectors that the row begins and ends in
+    const int v = tid ? v_hi : v_lo - 1;
+    if (v >= 0 && v < nv && (tid == 0 || v != v_lo - 1)) {
+      uint32_t w[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int j = 8 * v + 2 * i;
         const uint32_t p = j >= lo && j < hi ? z[base + j] : NEG_INF, q = j + 1 >= lo && j + 1 < hi ? z[base + j + 1] : NEG_INF;
         w[i] = p | q << 16;
       }
+      keep(v, w);
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t p = canonical(w[i] & 0xffffu), q = canonical(w[i] >> 16);
-      top = max(top, max(order_key(p), order_key(q)));
-      w[i] = p | q << 16;
-    }
-    reinterpret_cast<uint4*>(zs)[v] = make_uint4(w[0], w[1], w[2], w[3]);
   }
   auto maxu = [](uint32_t x, uint32_t y) { return max(x, y); };
   auto minu = [](uint32_t x, uint32_t y) { return min(x, y); };
   auto addf = [](float x, float y) { return x + y; };
-  top = block_reduce(top, maxu, sh.red_u);
+  const uint32_t top = block_reduce(order_key(__float_as_uint(top_z) >> 16), maxu, sh.red_u);
   cluster.barrier_wait(std::move(started));
   if (warp == 0 && lane < C) cluster.map_shared_rank(&sh, lane)->kmax[rank] = top;
   if (TRUNC)
@@ -180,15 +380,8 @@ __global__ void __launch_bounds__(SM_THREADS) sample_kernel(SampleArgs a, int se
     return;
   }
   const float zmax = key_value(kmax);
-  const float T = a.temperature ? a.temperature[row] : 1.f, inv = __fdiv_rn(1.f, fminf(T, 1e30f));
-  const bool greedy = !(T > 0.f) || isinf(inv);
-  int k = 0;
-  float p = 1.f, mp = 0.f;
-  if (TRUNC) {
-    if (a.top_k) k = a.top_k[row];
-    if (a.top_p) p = a.top_p[row];
-    if (a.min_p) mp = a.min_p[row];
-  }
+  const float inv = __fdiv_rn(1.f, fminf(T, 1e30f));
+  const bool greedy = !(T > 0.f) || inv > 1e37f;
   if (k <= 0 || k > V) k = V;
   const bool by_k = k < V, by_p = p < 1.f;  // (NaN: off)
   // (z - max z, 0 at the maximum even where it is infinite)
@@ -203,81 +396,129 @@ __global__ void __launch_bounds__(SM_THREADS) sample_kernel(SampleArgs a, int se
   if (greedy || !TRUNC || !(by_k || by_p)) {
     // ---- no prefix to find: one pass over the row and its noise
     const float floor_y = mp > 0.f ? logf(fminf(mp, 1.f)) : -INFINITY;
-    auto element = [&](uint32_t bits, int i, float noise) {
-      const float d = rel(bits), e = exp_fast(d);
-      full += e;
-      if (greedy) {
-        if (d == 0.f) best.take(0.f, i, true);
-        return;
-      }
-      const float y = scaled(d);
-      if (TRUNC && !(y >= floor_y)) return;
-      total += inv == 1.f ? e : exp_fast(y);
-      best.take(__fadd_rn(y, noise), i, bits != NEG_INF);
-    };
     const bool with_noise = g && !greedy;
-    if (with_noise && ((reinterpret_cast<uintptr_t>(g + base) & 15) == 0)) {
+    // (infinite maxima take the plain loop: z - max z is 0 or -inf there)
+    const bool plain = inv == 1.f, vectors = with_noise && ((reinterpret_cast<uintptr_t>(g + base) & 15) == 0) && !isinf(zmax);
+    auto element = [&](int j) {
+      const float d = rel(zs[j]), e = exp_fast(d);
+      full += e;
+      const float y = greedy ? (d == 0.f ? 0.f : -INFINITY) : scaled(d);
+      if (TRUNC && !(y >= floor_y)) return;
+      total += exp_fast(y);
+      best.take(with_noise ? perturbed(y, g[base + j]) : y, base + j);
+    };
+    if (vectors) {
       constexpr int U = 2;  // vectors of 8 in flight
-      for (int v0 = tid; v0 < nv; v0 += U * SM_THREADS) {
+      for (int v0 = v_lo + tid; v0 < v_hi; v0 += U * SM_THREADS) {
         float4 n[U][2];
 #pragma unroll
         for (int x = 0; x < U; ++x) {
-          const int j = 8 * (v0 + x * SM_THREADS);
-          if (j >= lo && j + 8 <= hi) {
-            n[x][0] = __ldcs(reinterpret_cast<const float4*>(g + base + j));
-            n[x][1] = __ldcs(reinterpret_cast<const float4*>(g + base + j) + 1);
+          const int v = v0 + x * SM_THREADS;
+          if (v < v_hi) {
+            n[x][0] = __ldcs(reinterpret_cast<const float4*>(g + base + 8 * v));
+            n[x][1] = __ldcs(reinterpret_cast<const float4*>(g + base + 8 * v) + 1);
           }
         }
 #pragma unroll
         for (int x = 0; x < U; ++x) {
-          const int v = v0 + x * SM_THREADS, j = 8 * v;
-          if (v >= nv) break;
+          const int v = v0 + x * SM_THREADS;
+          if (v >= v_hi) break;
           const uint4 w4 = reinterpret_cast<const uint4*>(zs)[v];
           const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
-          if (j >= lo && j + 8 <= hi) {
-            const float* f = &n[x][0].x;
+          const float* f = &n[x][0].x;
+          float s[8], most = -INFINITY;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              element(w[i] & 0xffffu, base + j + 2 * i, f[2 * i]);
-              element(w[i] >> 16, base + j + 2 * i + 1, f[2 * i + 1]);
+          for (int i = 0; i < 8; ++i) {
+            const float d = __fsub_rn(i & 1 ? bf16_hi(w[i >> 1]) : bf16_lo(w[i >> 1]), zmax);
+            const float y = scaled(d), e = exp_fast(d), ey = plain ? e : exp_fast(y);
+            full += e;
+            if (TRUNC) {
+              const bool in = y >= floor_y;
+              total += in ? ey : 0.f;
+              s[i] = in ? perturbed(y, f[i]) : -INFINITY;
+            } else {
+              total += ey;
+              s[i] = perturbed(y, f[i]);
             }
-          } else {
-            for (int i = max(j, lo); i < min(j + 8, hi); ++i) element(zs[i], base + i, g[base + i]);
+            most = fmaxf(most, s[i]);
+          }
+          if (most > best.s) {
+#pragma unroll
+            for (int i = 7; i >= 0; --i)
+              if (s[i] == most) best.at = base + 8 * v + i;
+            best.s = most;
           }
         }
       }
-    } else {
-      for (int j = lo + tid; j < hi; j += SM_THREADS) element(zs[j], base + j, with_noise ? g[base + j] : 0.f);
     }
+    // without vectors all of the row, else what its first and last vectors hold of it
+    const int n_rest = vectors ? n_edge : max(0, hi - lo);
+    for (int i = tid; i < n_rest; i += SM_THREADS) element(vectors ? edge(i) : lo + i);
   } else if constexpr (TRUNC) {
     // ---- the prefix: windows of SM_BINS distinct logits from the largest down
     float mass = 0.f;
     if (rank == 0 && tid == 0) {
       sh.dec = Decision{};
       sh.dec.k_bin = by_k ? -1 : 1 << 20;  // (past every logit)
-      sh.dec.goal = -1.0;
     }
     Decision dec{};
+    const float per_y = inv * kLog2e;  // y in units of log2
     for (int start = 0, turn = 0;; ++turn) {
-      uint32_t next = 0xffffffffu;
-      for (int v = tid; v < nv; v += SM_THREADS) {
+      // a first window of few logits holds what is usually kept and little of the bulk
+      const int width = turn == 0 ? SM_FIRST : SM_BINS;
+      // bins start .. start + width - 1 are the logits from `upper` down to `lower`
+      const float upper = key_value(kmax - start);
+      const int low_key = (int)kmax - start - width + 1;
+      const float lower = low_key > (int)KEY_NEG_INF ? key_value((uint32_t)low_key) : -INFINITY;
+      float below = -INFINITY;  // the largest logit under the window
+      auto sums = [&](float x) {
+        const float d = x == zmax ? 0.f : __fsub_rn(x, zmax);
+        full += exp_fast(d);
+        float e;
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(d * per_y));
+        mass += e;
+      };
+      const uint32_t hist_at = static_cast<uint32_t>(__cvta_generic_to_shared(hist)) + 4 * (kmax - start);
+      auto count = [&](uint32_t bits) {  // without a branch: lanes differ in what they count
+        const float x = __uint_as_float(bits);
+        const uint32_t key = (bits ^ ((uint32_t)((int)bits >> 31) | 0x80000000u)) >> 16;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "setp.ne.u32 p, %1, 0;\n\t"
+            "@p red.shared.add.u32 [%0], 1;\n\t}" ::"r"(hist_at - 4 * key),
+            "r"((uint32_t)(x >= lower && x <= upper))
+            : "memory");
+        below = fmaxf(below, x >= lower ? -INFINITY : x);
+      };
+      for (int v = v_lo + tid; v < v_hi; v += SM_THREADS) {
         const uint4 w4 = reinterpret_cast<const uint4*>(zs)[v];
         const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
-        const bool inner = 8 * v >= lo && 8 * v + 8 <= hi;
+        if (turn == 0) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const uint32_t bits = i & 1 ? w[i >> 1] >> 16 : w[i >> 1] & 0xffffu;
-          if (!inner && (8 * v + i < lo || 8 * v + i >= hi)) continue;
-          if (turn == 0) {
-            const float d = rel(bits), e = exp_fast(d);
-            full += e;
-            mass += inv == 1.f ? e : exp_fast(scaled(d));
+          for (int i = 0; i < 4; ++i) {
+            sums(bf16_lo(w[i]));
+            sums(bf16_hi(w[i]));
           }
-          const uint32_t bin = kmax - order_key(bits);
-          if (bin - (uint32_t)start < SM_BINS) atomicAdd(&hist[bin - start], 1u);
-          else if ((int)bin >= start) next = min(next, bin);
+        }
+        float most = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) most = fmaxf(most, fmaxf(bf16_lo(w[i]), bf16_hi(w[i])));
+        if (most < lower) {  // most vectors: all under the window
+          below = fmaxf(below, most);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            count(w[i] << 16);
+            count(w[i] & 0xffff0000u);
+          }
         }
       }
+      if (tid < n_edge) {
+        const uint32_t bits = (uint32_t)zs[edge(tid)] << 16;
+        if (turn == 0) sums(__uint_as_float(bits));
+        count(bits);
+      }
+      uint32_t next = kmax - order_key(__float_as_uint(below) >> 16);
       if (turn == 0) {
         full = block_reduce(full, addf, sh.red_f[0]);
         mass = block_reduce(mass, addf, sh.red_f[1]);
@@ -291,128 +532,12 @@ __global__ void __launch_bounds__(SM_THREADS) sample_kernel(SampleArgs a, int se
         leader->next[rank] = next;
       }
       cluster.sync();
-      // the row's counts, a share of the bins each, into the leader
-      {
-        uint32_t* to = cluster.map_shared_rank(sum, 0);
-        const int share = SM_BINS / C;
-        for (int i = rank * share + tid; i < (rank + 1) * share; i += SM_THREADS) {
-          uint32_t n = 0;
-          for (int c = 0; c < C; ++c) n += cluster.map_shared_rank(hist, c)[i];
-          to[i] = n;
-        }
-      }
-      cluster.sync();
       if (rank == 0) {
-        // scan: thread t holds bins 8 t .. 8 t + 7
-        uint32_t n[SM_PER_THREAD];
-        double w[SM_PER_THREAD];
-        int count = 0;
-        double own = 0.0;
-#pragma unroll
-        for (int i = 0; i < SM_PER_THREAD; ++i) {
-          const int bin = start + tid * SM_PER_THREAD + i;
-          n[i] = sum[tid * SM_PER_THREAD + i];
-          const uint32_t key = kmax - (uint32_t)bin;
-          w[i] = 0.0;
-          if (n[i]) w[i] = exp_fast(scaled(bin == 0 ? 0.f : __fsub_rn(key_value(key), zmax)));
-          count += (int)n[i];
-          own += n[i] * w[i];
-        }
-        int c_up = count;
-        double m_up = own;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-          const int c = __shfl_up_sync(0xffffffffu, c_up, d);
-          const double m = __shfl_up_sync(0xffffffffu, m_up, d);
-          if (lane >= d) {
-            c_up += c;
-            m_up += m;
-          }
-        }
-        if (lane == 31) {
-          sh.scan_c[warp] = c_up;
-          sh.scan_m[warp] = m_up;
-        }
-        if (tid == 0) sh.pick = -1;
-        __syncthreads();
-        int c_all = 0, c_before = sh.dec.count + c_up - count;
-        double m_all = 0.0, m_before = sh.dec.mass + m_up - own;
-        for (int i = 0; i < SM_WARPS; ++i) {
-          if (i < warp) {
-            c_before += sh.scan_c[i];
-            m_before += sh.scan_m[i];
-          }
-          c_all += sh.scan_c[i];
-          m_all += sh.scan_m[i];
-        }
-        const int c_end = sh.dec.count + c_all;
-        const double m_end = sh.dec.mass + m_all, m_start = sh.dec.mass;
-        int k_bin = sh.dec.k_bin;
-        double goal = sh.dec.goal;
-        __syncthreads();  // (dec has been read)
-        if (k_bin < 0 && c_end >= k) {  // the top-k prefix ends in this window
-          int c = c_before;
-          double m = m_before;
-#pragma unroll
-          for (int i = 0; i < SM_PER_THREAD; ++i) {
-            if (c < k && c + (int)n[i] >= k) {
-              sh.dec.k_bin = start + tid * SM_PER_THREAD + i;
-              sh.dec.k_ties = k - c;
-              sh.dec.goal = (double)p * (m + (k - c) * w[i]);
-            }
-            c += (int)n[i];
-            m += n[i] * w[i];
-          }
-        } else if (!by_k && goal < 0.0 && tid == 0) {
-          float all = 0.f;
-          for (int c = 0; c < C; ++c) all += sh.mass[c];
-          sh.dec.goal = (double)p * all;
-        }
-        __syncthreads();
-        k_bin = sh.dec.k_bin;
-        goal = sh.dec.goal;
-        uint32_t below = 0xffffffffu;  // where the next window would begin
-        for (int c = 0; c < C; ++c) below = min(below, sh.next[c]);
-        const bool k_known = k_bin >= 0, rest = below != 0xffffffffu;
-        if (k_known && by_p && (m_start < goal || start == 0) && (m_end >= goal || k_bin < start + SM_BINS || !rest)) {
-          // the top-p prefix ends in this window: the last logit with less than the goal before it
-          int mine = -1, ties = 1;
-          double m = m_before;
-#pragma unroll
-          for (int i = 0; i < SM_PER_THREAD; ++i) {
-            const int bin = start + tid * SM_PER_THREAD + i;
-            if (n[i] && bin <= k_bin && (m < goal || bin == 0)) {
-              mine = bin;
-              const double need = w[i] > 0.0 ? ceil((goal - m) / w[i]) : 2e9;
-              ties = need < 1.0 ? 1 : need < (double)n[i] ? (int)need : (int)n[i];
-            }
-            m += n[i] * w[i];
-          }
-          if (mine >= 0) atomicMax(&sh.pick, mine);
-          __syncthreads();
-          if (mine >= 0 && mine == sh.pick) {
-            sh.dec.last = mine;
-            sh.dec.ties = mine == k_bin ? min(ties, sh.dec.k_ties) : ties;
-            sh.dec.more = 0;
-          }
-        } else if (tid == 0) {
-          if (k_known && !by_p) {
-            sh.dec.last = k_bin;
-            sh.dec.ties = sh.dec.k_ties;
-            sh.dec.more = 0;
-          } else {
-            sh.dec.more = 1;
-            if (k_known && m_start >= goal) {  // the top-p prefix ended in an earlier window
-              sh.dec.start = 0;
-              sh.dec.count = 0;
-              sh.dec.mass = 0.0;
-            } else {
-              sh.dec.start = (int)below;
-              sh.dec.count = c_end;
-              sh.dec.mass = m_end;
-            }
-          }
-        }
+        const PrefixArgs pa{cluster, sh, hist, C, V, kmax, zmax, inv, k, p, by_k, by_p, start, width};
+        if (turn == 0)
+          scan_window<1>(pa);
+        else
+          scan_wide(pa);
       }
       cluster.sync();
       dec = leader->dec;
@@ -459,20 +584,26 @@ __global__ void __launch_bounds__(SM_THREADS) sample_kernel(SampleArgs a, int se
     }
     // ---- the kept tokens
     const float floor_y = mp > 0.f ? logf(fminf(mp, 1.f)) : -INFINITY;
-    for (int v = tid; v < nv; v += SM_THREADS) {
+    const float least = key_value(kmax - last);
+    auto element = [&](uint32_t bits, int j) {
+      const float x = __uint_as_float(bits);
+      if (!(x >= least) || (x == least && j >= at) || x == -INFINITY) return;
+      const float y = scaled(x == zmax ? 0.f : __fsub_rn(x, zmax));
+      if (!(y >= floor_y)) return;
+      total += exp_fast(y);
+      best.take(g ? perturbed(y, g[base + j]) : y, base + j);
+    };
+    for (int v = v_lo + tid; v < v_hi; v += SM_THREADS) {
       const uint4 w4 = reinterpret_cast<const uint4*>(zs)[v];
       const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
+      float most = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const uint32_t bits = i & 1 ? w[i >> 1] >> 16 : w[i >> 1] & 0xffffu;
-        const int j = 8 * v + i, bin = (int)(kmax - order_key(bits));
-        if (bin > last || (bin == last && j >= at) || bits == NEG_INF || j < lo || j >= hi) continue;
-        const float y = scaled(rel(bits));
-        if (!(y >= floor_y)) continue;
-        total += exp_fast(y);
-        best.take(g ? __fadd_rn(y, g[base + j]) : y, base + j, true);
-      }
+      for (int i = 0; i < 4; ++i) most = fmaxf(most, fmaxf(bf16_lo(w[i]), bf16_hi(w[i])));
+      if (most >= least)
+#pragma unroll 1
+        for (int i = 0; i < 8; ++i) element((uint32_t)zs[8 * v + i] << 16, 8 * v + i);
     }
+    if (tid < n_edge) element((uint32_t)zs[edge(tid)] << 16, edge(tid));
   }
 
   // ---- the row's token
@@ -496,7 +627,9 @@ __global__ void __launch_bounds__(SM_THREADS) sample_kernel(SampleArgs a, int se
       all += sh.total[c];
       whole += sh.full[c];
     }
-    const int token = (int)(0xffffffffu - (uint32_t)top_b);
+    int token = (int)(0xffffffffu - (uint32_t)top_b);
+    if (!top_b)  // every kept y + noise overflowed to -inf: the largest logit
+      for (token = 0; token < V - 1 && order_key(canonical(z[token])) != kmax;) ++token;
     const float d = rel(canonical(z[token]));
     a.token[row] = token;
     if (a.prob) a.prob[row] = greedy ? 1.f : exp_fast(scaled(d)) / all;
@@ -507,7 +640,7 @@ __global__ void __launch_bounds__(SM_THREADS) sample_kernel(SampleArgs a, int se
 template <bool TRUNC>
 cudaError_t launch_as(const SampleArgs& a, int C, cudaStream_t stream) {
   const int seg = ((a.V + 7 + C - 1) / C + 7) / 8 * 8;  // (7: a row's first vector may hold one token)
-  const size_t smem = (sizeof(SampleShared) + 15) / 16 * 16 + (TRUNC ? 8 * SM_BINS : 0) + 2 * (size_t)seg;
+  const size_t smem = (sizeof(SampleShared) + 15) / 16 * 16 + (TRUNC ? 4 * SM_BINS : 0) + 2 * (size_t)seg;
   static const cudaError_t set = cudaFuncSetAttribute(sample_kernel<TRUNC>, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
   if (set != cudaSuccess) return set;
   cudaLaunchConfig_t cfg = {};
