@@ -314,7 +314,7 @@ dcl_status dcl_fp8_quantise(const uint16_t* w, int64_t rows, int64_t cols, uint8
  * with the exponent at least DCL_KV_EXP_MIN), so that every stored value is a bf16 value (but for
  * components from 1.9375 * 2^127 on, whose nearest code stands for 2^128 and reads as infinity);
  * infinities and NaN are stored as NaN.  page_len 16, 32, 64, 128 or 256; head_dim 64 or 128;
- * n_pages * page_len < 2^31; every pointer 16-byte aligned. */
+ * n_kv_heads at most 1024; n_pages * page_len < 2^31; every pointer 16-byte aligned. */
 typedef struct {
   int32_t n_pages, page_len, n_kv_heads, head_dim, format;
   void *k_dev, *v_dev;

@@ -1423,8 +1423,8 @@ const char* kv_pool(const dcl_kv_cache* kv, KvPool* out) {
   while (shift <= 8 && (1 << shift) != kv->page_len) ++shift;
   if (shift > 8) return "page_len must be 16, 32, 64, 128 or 256";
   if (kv->head_dim != 64 && kv->head_dim != 128) return "head_dim must be 64 or 128";
-  if (kv->n_kv_heads <= 0 || kv->n_pages <= 0 || (int64_t)kv->n_pages * kv->page_len >= (1ll << 31))
-    return "cache needs n_kv_heads, n_pages > 0 and n_pages * page_len < 2^31";
+  if (kv->n_kv_heads <= 0 || kv->n_kv_heads > 1024 || kv->n_pages <= 0 || (int64_t)kv->n_pages * kv->page_len >= (1ll << 31))
+    return "cache needs n_kv_heads in 1 .. 1024, n_pages > 0 and n_pages * page_len < 2^31";
   if (kv->format == DCL_KV_FP8 && (!kv->k_exp_dev || !kv->v_exp_dev)) return "an FP8 cache needs its exponents";
   if (!aligned16(kv->k_dev) || !aligned16(kv->v_dev) || !aligned16(kv->k_exp_dev) || !aligned16(kv->v_exp_dev))
     return "cache pointers must be 16-byte aligned";
