@@ -178,18 +178,21 @@ def _dev_rows(t, name, itemsize, rows, cols):
         raise ValueError(f"{name}: a device buffer (a CUDA tensor) is required")
     if t.element_size() != itemsize:
         raise TypeError(f"{name}: elements of {itemsize} bytes expected, got {t.dtype}")
+    if t.is_contiguous():  # (a call's host time is a few microseconds: the common case is looked at once)
+        if t.numel() < rows * cols or t.numel() != t.shape[0] * cols:
+            raise ValueError(f"{name}: {rows} rows of {cols} elements expected, got {tuple(t.shape)}")
+        return t.data_ptr(), cols
     shape, stride = t.shape, t.stride()
-    have, inner = 1, 1
-    for size, step in zip(reversed(shape[1:]), reversed(stride[1:])):
-        if size != 1 and step != inner:
+    inner = 1
+    for i in range(len(shape) - 1, 0, -1):
+        if shape[i] != 1 and stride[i] != inner:
             raise ValueError(f"{name}: the elements of a row must be contiguous")
-        inner *= size
-        have *= size
-    if shape[0] < rows or have != cols:
+        inner *= shape[i]
+    if shape[0] < rows or inner != cols:
         raise ValueError(f"{name}: {rows} rows of {cols} elements expected, got {tuple(shape)}")
-    if rows > 1 and stride[0] < cols:
+    if shape[0] > 1 and stride[0] < cols:
         raise ValueError(f"{name}: rows overlap")
-    return t.data_ptr(), max(stride[0], cols) if shape[0] > 1 else cols
+    return t.data_ptr(), stride[0] if shape[0] > 1 else cols
 
 
 class KvCache:

@@ -2,7 +2,7 @@
 // out = softmax(scale q k^T) v over the sequence's cached positions.
 //
 // The rows of one kv head (new positions x the query heads that share it) form row tiles of 16 or
-// 32, the most that one pass over the keys serves.  A warp takes 16 keys at a time: S = q k^T and
+// 32, the most that one pass over the keys serves.  A warp takes 16 or 32 keys at a time: S = q k^T and
 // O += P v as m16n8k16 products with the rows on the M side, its own running maximum m, sum l and
 // O in registers, its own ring of key / value tiles in shared memory (16-byte asynchronous copies;
 // no barrier in the loop).  The tensor work is far below its limit as long as the keys arrive from
@@ -31,26 +31,30 @@
 namespace dcl {
 namespace {
 
-constexpr int KA_WARPS = 8;
-constexpr int KA_THREADS = 32 * KA_WARPS;
 constexpr int KA_UNIT = 128;  // keys of a unit of work
 
 template <int HD, bool FP8, int MT>
 struct KaCfg {
   static constexpr int ES = FP8 ? 1 : 2;
+  static constexpr int WARPS = MT == 1 ? 12 : 8;    // (as many as the registers allow)
+  static constexpr int THREADS = 32 * WARPS;
+  static constexpr int KT = FP8 && MT == 1 ? 32 : 16;  // keys that a warp takes at a time
+  static constexpr int NK = KT / 8;                 // column tiles of S
   static constexpr int ROWS = 16 * MT;              // rows of an item
   static constexpr int ROWB = HD * ES;              // bytes of a key
-  static constexpr int TILE = 16 * ROWB;            // 16 keys (or values)
-  static constexpr int STAGE = 2 * TILE + (FP8 ? 32 : 0);
-  static constexpr int STAGES = FP8 ? (HD == 128 ? 5 : 8) : (HD == 128 ? 3 : 5);
+  static constexpr int TILE = KT * ROWB;            // the keys (or values) of a step
+  static constexpr int STAGE = 2 * TILE + (FP8 ? 2 * KT : 0);
+  static constexpr int LIMIT = 220 * 1024 / WARPS / STAGE;
+  static constexpr int STAGES = LIMIT > 8 ? 8 : LIMIT;
   static constexpr int RING = STAGES * STAGE;       // one warp's
   static constexpr int O_PITCH = HD + 4;            // floats; a warp's O [ROWS][O_PITCH] takes the ring's place
   static constexpr int RING_B = RING > ROWS * O_PITCH * 4 ? RING : ROWS * O_PITCH * 4;
-  static constexpr int ML = KA_WARPS * RING_B;      // {m, l} [warp][ROWS], then of the joined rows
-  static constexpr int QF = ML + (KA_WARPS + 1) * ROWS * 8;  // q fragments [MT][HD / 16][lane] of 16 bytes (MT > 1)
-  static constexpr int QA = QF + (MT > 1 ? MT * (HD / 16) * 32 * 16 : 0);
-  static constexpr int HEAD = QA;                   // the walk's variables
+  static constexpr int ML = WARPS * RING_B;         // {m, l} [warp][ROWS]
+  static constexpr int QF = ML + WARPS * ROWS * 8;  // q fragments [MT][HD / 16][lane] of 16 bytes
+  static constexpr int SC = QF + MT * (HD / 16) * 32 * 16;  // what the keys' exponents give [warp][3][KT] floats
+  static constexpr int HEAD = SC + (FP8 ? WARPS * 3 * KT * 4 : 0);  // the walk's variables
   static constexpr size_t SMEM = HEAD + 64;
+  static_assert(STAGES >= 2, "a step in flight");
 };
 
 struct KaScratch {
@@ -82,6 +86,17 @@ __device__ __forceinline__ uint32_t lds_u16(uint32_t a) {
   asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(a));
   return v;
 }
+__device__ __forceinline__ uint32_t lds_u8(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ float2 lds_f2(uint32_t a) {
+  float2 v;
+  asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ void sts32(uint32_t a, float v) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(a), "f"(v) : "memory"); }
 __device__ __forceinline__ void sts128(uint32_t a, uint4 v) {
   asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
@@ -174,10 +189,11 @@ struct KaItem {
 };
 
 template <int HD, bool FP8, int MT>
-__global__ void __launch_bounds__(KA_THREADS, 1) kv_attention_kernel(KvPool kv, KvAttn a, KaScratch scratch, int* err) {
+__global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, 1) kv_attention_kernel(KvPool kv, KvAttn a, KaScratch scratch, int* err) {
   using C = KaCfg<HD, FP8, MT>;
   constexpr int KS = HD / 16;  // k steps of S, and pairs of column tiles of O
   constexpr int NT = HD / 8;   // column tiles of O
+  constexpr int KT = C::KT, NK = C::NK;
   extern __shared__ __align__(128) uint8_t smem[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = lane >> 2, place = lane & 3;
   const int rep = a.H / kv.G, room = a.max_pages << kv.page_shift, P = kv.page_len();
@@ -266,7 +282,6 @@ __global__ void __launch_bounds__(KA_THREADS, 1) kv_attention_kernel(KvPool kv, 
     // ---- this lane's rows: quad + 8 i of the tile; q as the product's operand; keys each sees
     int lim[2 * MT];
     float qa[2 * MT];  // scale * log2(e) * the power of two that q was divided by
-    uint32_t qf[MT == 1 ? KS : 1][4];
     int lim_min = it.len, lim_max = 0;
     {
       // (of all rows of the item: the first sees the fewest keys, the last the most)
@@ -318,17 +333,10 @@ __global__ void __launch_bounds__(KA_THREADS, 1) kv_attention_kernel(KvPool kv, 
         for (int s = 0; s < KS; ++s) {  // step s: components 4 s .. 4 s + 3 of this lane's
           const uint32_t* w0 = &raw[0][s >> 1].x + 2 * (s & 1);
           const uint32_t* w1 = &raw[1][s >> 1].x + 2 * (s & 1);
-          if (MT == 1) {
-            qf[s][0] = w0[0];
-            qf[s][1] = w1[0];
-            qf[s][2] = w0[1];
-            qf[s][3] = w1[1];
-          } else if (warp == 0) {
-            *reinterpret_cast<uint4*>(qs[mt * KS + s][lane]) = make_uint4(w0[0], w1[0], w0[1], w1[1]);
-          }
+          if (warp == 0) *reinterpret_cast<uint4*>(qs[mt * KS + s][lane]) = make_uint4(w0[0], w1[0], w0[1], w1[1]);
         }
       }
-      if (MT > 1) __syncthreads();
+      __syncthreads();
     }
     const uint32_t qs_addr = smem_addr(smem) + C::QF + lane * 16;
 
@@ -345,35 +353,45 @@ __global__ void __launch_bounds__(KA_THREADS, 1) kv_attention_kernel(KvPool kv, 
       l[i] = 0.f;
     }
 
-    // ---- this warp's key tiles: key0 / 16 + warp, then every KA_WARPS-th
+    // ---- this warp's steps: keys key0 + KT warp on, then every WARPS-th
     const int stop = min(key1, lim_max);
     const int* table = a.table + (int64_t)it.b * a.max_pages;
-    int next = key0 + 16 * warp;  // first key of the next tile to copy
-    uint32_t bad = 0;             // stages whose page is not the cache's
+    int next = key0 + KT * warp;  // first key of the next step to copy
+    uint32_t bad = 0;             // two bits a stage: 16 keys whose page is not the cache's
     int slot = 0;
-    int page = next < stop ? table[next >> kv.page_shift] : 0;
+    int page[KT / 16];
+    auto look_up = [&]() {
+#pragma unroll
+      for (int h = 0; h < KT / 16; ++h) page[h] = next + 16 * h < stop ? table[(next + 16 * h) >> kv.page_shift] : 0;
+    };
+    look_up();
     auto issue = [&]() {
       if (next < stop) {
-        const bool ok = page >= 0 && page < kv.pages;
-        bad = ok ? bad & ~(1u << slot) : bad | 1u << slot;
-        if (ok) {
-          const int64_t vec = kv.vector_of((page << kv.page_shift) + (next & (P - 1)), it.g);
-          const uint8_t* k = static_cast<const uint8_t*>(kv.k) + vec * C::ROWB;
-          const uint8_t* v = static_cast<const uint8_t*>(kv.v) + vec * C::ROWB;
-          const uint32_t dst = ring + slot * C::STAGE;
+        bad &= ~(3u << (2 * slot));
 #pragma unroll
-          for (int i = 0; i < C::TILE / 512; ++i) {
-            const int c = i * 32 + lane;
-            const uint32_t at = chunk_at<C::ROWB>(c / (C::ROWB / 16), c % (C::ROWB / 16));
-            copy16(dst + at, k + 16 * c);
-            copy16(dst + C::TILE + at, v + 16 * c);
+        for (int h = 0; h < KT / 16; ++h) {
+          const int key = next + 16 * h;
+          if (key >= stop) break;
+          if (page[h] >= 0 && page[h] < kv.pages) {
+            const int64_t vec = kv.vector_of((page[h] << kv.page_shift) + (key & (P - 1)), it.g);
+            const uint8_t* k = static_cast<const uint8_t*>(kv.k) + vec * C::ROWB + 16 * lane;
+            const uint8_t* v = static_cast<const uint8_t*>(kv.v) + vec * C::ROWB + 16 * lane;
+            const uint32_t dst = ring + slot * C::STAGE;
+#pragma unroll
+            for (int i = 0; i < C::ROWB / 32; ++i) {
+              const int c = i * 32 + lane;
+              const uint32_t at = chunk_at<C::ROWB>(16 * h + c / (C::ROWB / 16), c % (C::ROWB / 16));
+              copy16(dst + at, k + 512 * i);
+              copy16(dst + C::TILE + at, v + 512 * i);
+            }
+            if (FP8 && lane < 2) copy16(dst + 2 * C::TILE + KT * lane + 16 * h, (lane ? kv.v_exp : kv.k_exp) + vec);
+          } else {
+            bad |= 1u << (2 * slot + h);
+            if (lane == 0) report_error(err, DERR_KV_RANGE);
           }
-          if (FP8 && lane < 2) copy16(dst + 2 * C::TILE + 16 * lane, (lane ? kv.v_exp : kv.k_exp) + vec);
-        } else if (lane == 0) {
-          report_error(err, DERR_KV_RANGE);
         }
-        next += 16 * KA_WARPS;
-        if (next < stop) page = table[next >> kv.page_shift];
+        next += KT * C::WARPS;
+        look_up();
       }
       copy_commit();
       slot = slot + 1 == C::STAGES ? 0 : slot + 1;
@@ -382,35 +400,47 @@ __global__ void __launch_bounds__(KA_THREADS, 1) kv_attention_kernel(KvPool kv, 
     for (int s = 0; s < C::STAGES - 1; ++s) issue();
 
     int cur = 0;
-    for (int key = key0 + 16 * warp; key < stop; key += 16 * KA_WARPS) {
-      copy_wait<C::STAGES - 2>();
+    const uint32_t sc = smem_addr(smem) + C::SC + warp * 3 * KT * 4;
+    for (int key = key0 + KT * warp; key < stop; key += KT * C::WARPS) {
+      issue();  // into the stage that the last step left
+      copy_wait<C::STAGES - 1>();
       __syncwarp();
       const uint32_t sk = ring + cur * C::STAGE, sv = sk + C::TILE, se = sv + C::TILE;
-      const bool skip = bad >> cur & 1;
+      const uint32_t skip = bad >> (2 * cur) & 3u;
       cur = cur + 1 == C::STAGES ? 0 : cur + 1;
-      if (!skip) {
-        const bool masked = key + 16 > lim_min;
-        if (key + 16 > it.len) {  // values past the sequence's end may be anything: 0 * NaN
-          for (int c = lane; c < C::TILE / 16; c += 32)
-            if (key + c / (C::ROWB / 16) >= it.len)
-              sts128(sv + chunk_at<C::ROWB>(c / (C::ROWB / 16), c % (C::ROWB / 16)), make_uint4(0, 0, 0, 0));
-          __syncwarp();
+      {
+        const bool masked = key + KT > lim_min || skip;
+        if (key + KT > lim_max || skip) {  // values that no row sees may be anything: 0 * NaN
+          for (int c = lane; c < C::TILE / 16; c += 32) {
+            const int r = c / (C::ROWB / 16);
+            if (key + r >= lim_max || (skip >> (r >> 4) & 1))
+              sts128(sv + chunk_at<C::ROWB>(r, c % (C::ROWB / 16)), make_uint4(0, 0, 0, 0));
+          }
         }
-        // S = q k^T: two column tiles of 8 keys
-        float s[MT][2][4];
+        if (FP8) {  // what a key's exponents give: 2^e of the key, e and 2^-e of the value
+          if (KT == 32 || lane < KT) {
+            const int x = (int)(int8_t)lds_u8(se + lane), y = max(-126, (int)(int8_t)lds_u8(se + KT + lane));
+            sts32(sc + 4 * lane, kv_pow2(x));
+            sts32(sc + 4 * (KT + lane), (float)y);
+            sts32(sc + 4 * (2 * KT + lane), kv_pow2(-y));
+          }
+        }
+        __syncwarp();
+        // S = q k^T: column tiles of 8 keys
+        float s[MT][NK][4];
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
-          for (int j = 0; j < 2; ++j)
+          for (int j = 0; j < NK; ++j)
 #pragma unroll
             for (int k = 0; k < 4; ++k) s[i][j][k] = 0.f;
         constexpr int KCH = FP8 ? HD / 64 : HD / 32;  // 16-byte chunks of a key per lane
         constexpr int SPC = FP8 ? 4 : 2;              // k steps of a chunk
 #pragma unroll
         for (int c = 0; c < KCH; ++c) {
-          uint4 w[2];
+          uint4 w[NK];
 #pragma unroll
-          for (int j = 0; j < 2; ++j)
+          for (int j = 0; j < NK; ++j)
             w[j] = lds128(sk + chunk_at<C::ROWB>(8 * j + quad, FP8 ? place * KCH + c : k_chunk<HD, FP8>(place, c)));
 #pragma unroll
           for (int x = 0; x < SPC; ++x) {
@@ -418,19 +448,14 @@ __global__ void __launch_bounds__(KA_THREADS, 1) kv_attention_kernel(KvPool kv, 
             uint32_t qreg[MT][4];
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
-              if (MT == 1) {
-#pragma unroll
-                for (int k = 0; k < 4; ++k) qreg[i][k] = qf[MT == 1 ? st : 0][k];
-              } else {
-                const uint4 q4 = lds128(qs_addr + (i * KS + st) * 512);
-                qreg[i][0] = q4.x;
-                qreg[i][1] = q4.y;
-                qreg[i][2] = q4.z;
-                qreg[i][3] = q4.w;
-              }
+              const uint4 q4 = lds128(qs_addr + (i * KS + st) * 512);
+              qreg[i][0] = q4.x;
+              qreg[i][1] = q4.y;
+              qreg[i][2] = q4.z;
+              qreg[i][3] = q4.w;
             }
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
+            for (int j = 0; j < NK; ++j) {
               const uint32_t* ww = &w[j].x;
               const uint32_t b0 = FP8 ? widen_lo(ww[x]) : ww[2 * (x & 1)];
               const uint32_t b1 = FP8 ? widen_hi(ww[x]) : ww[2 * (x & 1) + 1];
@@ -440,141 +465,152 @@ __global__ void __launch_bounds__(KA_THREADS, 1) kv_attention_kernel(KvPool kv, 
           }
         }
         // scores in units of log2; with FP8 values their exponent added
-        float kf[4], ev[4], vi[4];
-        if (FP8) {
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const uint32_t ek = lds_u16(se + 8 * j + 2 * place), e2 = lds_u16(se + 16 + 8 * j + 2 * place);
+        for (int j = 0; j < NK; ++j) {
+          float2 kf, ev;
+          if (FP8) {
+            kf = lds_f2(sc + 4 * (8 * j + 2 * place));
+            ev = lds_f2(sc + 4 * (KT + 8 * j + 2 * place));
+          }
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              const int x = (int)(int8_t)(ek >> (8 * k)), y = max(-126, (int)(int8_t)(e2 >> (8 * k)));
-              kf[2 * j + k] = kv_pow2(x);
-              ev[2 * j + k] = (float)y;
-              vi[2 * j + k] = kv_pow2(-y);
-            }
+          for (int i = 0; i < 2 * MT; ++i) {
+            float &x0 = s[i >> 1][j][2 * (i & 1)], &x1 = s[i >> 1][j][2 * (i & 1) + 1];
+            x0 = FP8 ? fmaf(x0, qa[i] * kf.x, ev.x) : x0 * qa[i];
+            x1 = FP8 ? fmaf(x1, qa[i] * kf.y, ev.y) : x1 * qa[i];
           }
         }
-        uint32_t p[MT][4], p_lo[MT][4];
+        if (masked) {
+#pragma unroll
+          for (int i = 0; i < 2 * MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NK; ++j)
+#pragma unroll
+              for (int k = 0; k < 2; ++k)
+                if (key + 8 * j + 2 * place + k >= lim[i] || (skip >> (j >> 1) & 1)) s[i >> 1][j][2 * (i & 1) + k] = -INFINITY;
+        }
+        // The reference m of a row moves only when a score passes it by more than 8 (P <= 2^8), so that
+        // most steps neither exchange maxima nor scale O.
         bool grew = false;
-        float alpha[2 * MT];
+        float top[2 * MT];
 #pragma unroll
         for (int i = 0; i < 2 * MT; ++i) {
-          float x[4];
+          top[i] = -INFINITY;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float raw = s[i >> 1][j >> 1][2 * (i & 1) + (j & 1)];
-            x[j] = FP8 ? fmaf(raw, qa[i] * kf[j], ev[j]) : raw * qa[i];
-          }
-          if (masked) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              if (key + 8 * (j >> 1) + 2 * place + (j & 1) >= lim[i]) x[j] = -INFINITY;
-          }
-          float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
-          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-          const float mn = fmaxf(m[i], top);
-          grew |= mn > m[i];
-          const float ref = mn == -INFINITY ? 0.f : mn;  // (nothing seen yet: exp2(-inf) = 0)
-          alpha[i] = exp2_fast(m[i] - ref);
-          m[i] = mn;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) x[j] = exp2_fast(x[j] - ref);
-          float sum = 0.f;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) sum = FP8 ? fmaf(x[j], vi[j], sum) : sum + x[j];
-          l[i] = fmaf(l[i], alpha[i], sum);
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const uint32_t hi = FP8 ? pack_f16x2(x[2 * j], x[2 * j + 1]) : pack_bf16x2(x[2 * j], x[2 * j + 1]);
-            p[i >> 1][2 * j + (i & 1)] = hi;
-            if (!FP8) p_lo[i >> 1][2 * j + (i & 1)] = pack_bf16x2(x[2 * j] - bf16_lo(hi), x[2 * j + 1] - bf16_hi(hi));
-          }
+          for (int j = 0; j < NK; ++j)
+            top[i] = fmaxf(top[i], fmaxf(s[i >> 1][j][2 * (i & 1)], s[i >> 1][j][2 * (i & 1) + 1]));
+          grew |= top[i] > m[i] + 8.f;
         }
         if (__any_sync(0xffffffffu, grew)) {
 #pragma unroll
-          for (int i = 0; i < MT; ++i)
+          for (int i = 0; i < 2 * MT; ++i) {
+            top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
+            top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
+            const float mn = fmaxf(m[i], top[i]), alpha = exp2_fast(m[i] - (mn == -INFINITY ? 0.f : mn));
+            m[i] = mn;
+            l[i] *= alpha;
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
-              o[i][j][0] *= alpha[2 * i];
-              o[i][j][1] *= alpha[2 * i];
-              o[i][j][2] *= alpha[2 * i + 1];
-              o[i][j][3] *= alpha[2 * i + 1];
+              o[i >> 1][j][2 * (i & 1)] *= alpha;
+              o[i >> 1][j][2 * (i & 1) + 1] *= alpha;
             }
+          }
+        }
+        uint32_t p[NK / 2][MT][4], p_lo[FP8 ? 1 : NK / 2][MT][4];
+#pragma unroll
+        for (int i = 0; i < 2 * MT; ++i) {
+          const float ref = m[i] == -INFINITY ? 0.f : m[i];  // (nothing seen yet: exp2(-inf) = 0)
+#pragma unroll
+          for (int j = 0; j < NK; ++j) {
+            const float x0 = exp2_fast(s[i >> 1][j][2 * (i & 1)] - ref), x1 = exp2_fast(s[i >> 1][j][2 * (i & 1) + 1] - ref);
+            if (FP8) {
+              const float2 vi = lds_f2(sc + 4 * (2 * KT + 8 * j + 2 * place));
+              l[i] = fmaf(x1, vi.y, fmaf(x0, vi.x, l[i]));
+            } else {
+              l[i] += x0 + x1;
+            }
+            const uint32_t hi = FP8 ? pack_f16x2(x0, x1) : pack_bf16x2(x0, x1);
+            p[j >> 1][i >> 1][2 * (j & 1) + (i & 1)] = hi;
+            if (!FP8) p_lo[FP8 ? 0 : j >> 1][i >> 1][2 * (j & 1) + (i & 1)] = pack_bf16x2(x0 - bf16_lo(hi), x1 - bf16_hi(hi));
+          }
         }
         // A value that is no number and that only some of the rows see (0 * NaN): it is added to the
         // rows that do, one by one, and out of the product.
         if (masked && a.causal && __any_sync(0xffffffffu, has_nonfinite<FP8>(sv, C::TILE, lane))) {
+#pragma unroll
+          for (int half = 0; half < NK / 2; ++half)
 #pragma unroll 1
-          for (int jj = 0; jj < 16; ++jj) {
+            for (int jj = 0; jj < 16; ++jj) {
 #pragma unroll
-            for (int i = 0; i < 2 * MT; ++i) {
-              const uint32_t pair = __shfl_sync(0xffffffffu, jj < 8 ? p[i >> 1][i & 1] : p[i >> 1][2 + (i & 1)],
-                                                4 * quad + ((jj & 7) >> 1));
-              if (key + jj >= lim[i]) continue;
-              const uint32_t half = jj & 1 ? pair >> 16 : pair & 0xffffu;
-              const float pj = FP8 ? __half2float(__ushort_as_half((unsigned short)half)) : __uint_as_float(half << 16);
+              for (int i = 0; i < 2 * MT; ++i) {
+                const uint32_t pair = __shfl_sync(0xffffffffu, jj < 8 ? p[half][i >> 1][i & 1] : p[half][i >> 1][2 + (i & 1)],
+                                                  4 * quad + ((jj & 7) >> 1));
+                if (key + 16 * half + jj >= lim[i]) continue;
+                const uint32_t bits = jj & 1 ? pair >> 16 : pair & 0xffffu;
+                const float pj = FP8 ? __half2float(__ushort_as_half((unsigned short)bits)) : __uint_as_float(bits << 16);
 #pragma unroll
-              for (int j = 0; j < NT; ++j)
+                for (int j = 0; j < NT; ++j)
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                  const float v = value_at<C::ROWB, FP8>(sv, jj, v_comp<HD, FP8>(2 * place + k, j));
-                  if (!isfinite(v)) o[i >> 1][j][2 * (i & 1) + k] += pj * v;
-                }
+                  for (int k = 0; k < 2; ++k) {
+                    const float v = value_at<C::ROWB, FP8>(sv, 16 * half + jj, v_comp<HD, FP8>(2 * place + k, j));
+                    if (!isfinite(v)) o[i >> 1][j][2 * (i & 1) + k] += pj * v;
+                  }
+              }
             }
-          }
           __syncwarp();
           clear_nonfinite<FP8>(sv, C::TILE, lane);
           __syncwarp();
         }
-        // O += P v
-        if (FP8) {
-          constexpr int W = HD / 32;  // 4-code words of a value per lane
-          uint32_t v[4][W];
+        // O += P v, 16 keys at a time
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {  // keys 2 place, 2 place + 1, and 8 on
-            const int row = 2 * place + (r & 1) + 8 * (r >> 1);
-            if (W == 4) {
-              const uint4 x = lds128(sv + chunk_at<C::ROWB>(row, quad));
-              v[r][0] = x.x;
-              v[r][1] = x.y;
-              v[r][W - 2] = x.z;
-              v[r][W - 1] = x.w;
-            } else {
-              const uint2 x = lds64(sv + chunk_at<C::ROWB>(row, quad >> 1) + 8 * (quad & 1));
-              v[r][0] = x.x;
-              v[r][1] = x.y;
+        for (int half = 0; half < NK / 2; ++half) {
+          if (FP8) {
+            constexpr int W = HD / 32;  // 4-code words of a value per lane
+            uint32_t v[4][W];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {  // keys 2 place, 2 place + 1, and 8 on
+              const int row = 16 * half + 2 * place + (r & 1) + 8 * (r >> 1);
+              if (W == 4) {
+                const uint4 x = lds128(sv + chunk_at<C::ROWB>(row, quad));
+                v[r][0] = x.x;
+                v[r][1] = x.y;
+                v[r][W - 2] = x.z;
+                v[r][W - 1] = x.w;
+              } else {
+                const uint2 x = lds64(sv + chunk_at<C::ROWB>(row, quad >> 1) + 8 * (quad & 1));
+                v[r][0] = x.x;
+                v[r][1] = x.y;
+              }
             }
-          }
 #pragma unroll
-          for (int w = 0; w < W; ++w) {
-            const uint32_t x0 = __byte_perm(v[0][w], v[1][w], 0x5140), x1 = __byte_perm(v[0][w], v[1][w], 0x7362);
-            const uint32_t y0 = __byte_perm(v[2][w], v[3][w], 0x5140), y1 = __byte_perm(v[2][w], v[3][w], 0x7362);
-            const uint32_t b0[4] = {widen_lo(x0), widen_hi(x0), widen_lo(x1), widen_hi(x1)};
-            const uint32_t b1[4] = {widen_lo(y0), widen_hi(y0), widen_lo(y1), widen_hi(y1)};
+            for (int w = 0; w < W; ++w) {
+              const uint32_t x0 = __byte_perm(v[0][w], v[1][w], 0x5140), x1 = __byte_perm(v[0][w], v[1][w], 0x7362);
+              const uint32_t y0 = __byte_perm(v[2][w], v[3][w], 0x5140), y1 = __byte_perm(v[2][w], v[3][w], 0x7362);
+              const uint32_t b0[4] = {widen_lo(x0), widen_hi(x0), widen_lo(x1), widen_hi(x1)};
+              const uint32_t b1[4] = {widen_lo(y0), widen_hi(y0), widen_lo(y1), widen_hi(y1)};
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+              for (int j = 0; j < 4; ++j)
 #pragma unroll
-              for (int i = 0; i < MT; ++i) mma16816<FP8>(o[i][4 * w + j], p[i], b0[j], b1[j]);
-          }
-        } else {
+                for (int i = 0; i < MT; ++i) mma16816<FP8>(o[i][4 * w + j], p[half][i], b0[j], b1[j]);
+            }
+          } else {
 #pragma unroll
-          for (int c = 0; c < HD / 64; ++c) {
-            uint4 v[4];
+            for (int c = 0; c < HD / 64; ++c) {
+              uint4 v[4];
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-              v[r] = lds128(sv + chunk_at<C::ROWB>(2 * place + (r & 1) + 8 * (r >> 1), quad + 8 * c));
+              for (int r = 0; r < 4; ++r)
+                v[r] = lds128(sv + chunk_at<C::ROWB>(16 * half + 2 * place + (r & 1) + 8 * (r >> 1), quad + 8 * c));
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-              const uint32_t *v0 = &v[0].x, *v1 = &v[1].x, *v2 = &v[2].x, *v3 = &v[3].x;
+              for (int w = 0; w < 4; ++w) {
+                const uint32_t *v0 = &v[0].x, *v1 = &v[1].x, *v2 = &v[2].x, *v3 = &v[3].x;
 #pragma unroll
-              for (int x = 0; x < 2; ++x) {
-                const uint32_t sel = x ? 0x7632 : 0x5410;
-                const uint32_t b0 = __byte_perm(v0[w], v1[w], sel), b1 = __byte_perm(v2[w], v3[w], sel);
+                for (int x = 0; x < 2; ++x) {
+                  const uint32_t sel = x ? 0x7632 : 0x5410;
+                  const uint32_t b0 = __byte_perm(v0[w], v1[w], sel), b1 = __byte_perm(v2[w], v3[w], sel);
 #pragma unroll
-                for (int i = 0; i < MT; ++i) {
-                  mma16816<FP8>(o[i][8 * c + 2 * w + x], p[i], b0, b1);
-                  mma16816<FP8>(o[i][8 * c + 2 * w + x], p_lo[i], b0, b1);
+                  for (int i = 0; i < MT; ++i) {
+                    mma16816<FP8>(o[i][8 * c + 2 * w + x], p[half][i], b0, b1);
+                    mma16816<FP8>(o[i][8 * c + 2 * w + x], p_lo[FP8 ? 0 : half][i], b0, b1);
+                  }
                 }
               }
             }
@@ -582,7 +618,6 @@ __global__ void __launch_bounds__(KA_THREADS, 1) kv_attention_kernel(KvPool kv, 
         }
       }
       __syncwarp();
-      issue();
     }
     copy_wait<0>();
     __syncwarp();
@@ -612,14 +647,14 @@ __global__ void __launch_bounds__(KA_THREADS, 1) kv_attention_kernel(KvPool kv, 
     };
     constexpr int PART = HD + 2;
     const int64_t my_part = 2 * (int64_t)blockIdx.x + (u == item0);
-    for (int i = threadIdx.x; i < it.rows * HD; i += KA_THREADS) {
+    for (int i = threadIdx.x; i < it.rows * HD; i += C::THREADS) {
       const int r = i / HD, d = i - r * HD;
       float top = -INFINITY, sum = 0.f, acc = 0.f;
 #pragma unroll
-      for (int w = 0; w < KA_WARPS; ++w) top = fmaxf(top, ml[w * C::ROWS + r].x);
+      for (int w = 0; w < C::WARPS; ++w) top = fmaxf(top, ml[w * C::ROWS + r].x);
       {
 #pragma unroll
-        for (int w = 0; w < KA_WARPS; ++w) {
+        for (int w = 0; w < C::WARPS; ++w) {
           const float2 x = ml[w * C::ROWS + r];
           const float f = x.x == -INFINITY ? 0.f : exp2_fast(x.x - top);
           sum = fmaf(x.y, f, sum);
@@ -651,7 +686,7 @@ __global__ void __launch_bounds__(KA_THREADS, 1) kv_attention_kernel(KvPool kv, 
       }
       __syncthreads();
       if (*last) {
-        for (int i = threadIdx.x; i < it.rows * HD; i += KA_THREADS) {
+        for (int i = threadIdx.x; i < it.rows * HD; i += C::THREADS) {
           const int r = i / HD, d = i - r * HD;
           auto part_of = [&](int c) {
             return scratch.part + ((2 * (int64_t)c + (c == c0)) * C::ROWS + r) * PART;
@@ -682,7 +717,7 @@ cudaError_t launch_as(const KvPool& kv, const KvAttn& a, const KaScratch& s, int
   static const cudaError_t set =
       cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM);
   if (set != cudaSuccess) return set;
-  kern<<<ctas, KA_THREADS, C::SMEM, stream>>>(kv, a, s, err);
+  kern<<<ctas, C::THREADS, C::SMEM, stream>>>(kv, a, s, err);
   return cudaGetLastError();
 }
 
