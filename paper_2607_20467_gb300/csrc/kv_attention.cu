@@ -32,6 +32,7 @@ namespace dcl {
 namespace {
 
 constexpr int KA_UNIT = 128;  // keys of a unit of work
+constexpr int KA_START = 3;   // units that beginning an item and joining its parts take
 
 template <int HD, bool FP8, int MT>
 struct KaCfg {
@@ -47,7 +48,9 @@ struct KaCfg {
   static constexpr int LIMIT = 220 * 1024 / WARPS / STAGE;
   static constexpr int STAGES = LIMIT > 8 ? 8 : LIMIT;
   static constexpr int RING = STAGES * STAGE;       // one warp's
-  static constexpr int O_PITCH = HD + 4;            // floats; a warp's O [ROWS][O_PITCH] takes the ring's place
+  // a warp's O takes the ring's place: [ROWS][O_PITCH] floats, a lane's runs of components 4 apart
+  // from the next lane's, so that 16-byte stores meet all the banks
+  static constexpr int O_PITCH = FP8 ? HD + 36 : HD + HD / 2 + 4;
   static constexpr int RING_B = RING > ROWS * O_PITCH * 4 ? RING : ROWS * O_PITCH * 4;
   static constexpr int ML = WARPS * RING_B;         // {m, l} [warp][ROWS]
   static constexpr int QF = ML + WARPS * ROWS * 8;  // q fragments [MT][HD / 16][lane] of 16 bytes
@@ -58,7 +61,7 @@ struct KaCfg {
 };
 
 struct KaScratch {
-  float* part;  // [2 * CTAs][ROWS][HD + 2]: O, m, l
+  float* part;  // [2 * CTAs][ROWS][HD + 4]: O, m, l
   int* count;   // [CTAs], zero between launches
 };
 
@@ -182,6 +185,45 @@ __device__ __forceinline__ float value_at(uint32_t tile, int row, int comp) {
   return __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)code, __NV_E4M3)));
 }
 
+// Where component c of a row of O stands in a warp's part of shared memory.
+template <int HD, bool FP8>
+__device__ __forceinline__ int o_place(int c) {
+  if (FP8) return c + 4 * (c / (HD / 8));
+  return (c >> 6) * 96 + ((c >> 3) & 7) * 12 + (c & 7);
+}
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+  for (int d = 16; d; d >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
+  return v;
+}
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+  return v;
+}
+
+// The line of work in equal parts: CTA c of n has positions [start(c), start(c + 1)).
+struct KaShare {
+  int64_t each;
+  int extra, n;
+  __device__ KaShare(int64_t total, int ctas) {
+    n = (int)min((int64_t)ctas, total);  // (CTAs past it have nothing)
+    if (total < (1ll << 31)) {
+      each = n ? (int)total / n : 0;
+    } else {
+      each = total / n;
+    }
+    extra = (int)(total - each * n);
+  }
+  __device__ int64_t start(int c) const { return c >= n ? each * n + extra : each * c + min(c, extra); }
+  __device__ int owner(int64_t u) const {
+    const int64_t big = extra * (each + 1);
+    const int64_t at = u < big ? u : u - big, size = u < big ? each + 1 : each;
+    const int c = at < (1ll << 31) && size < (1ll << 31) ? (int)at / (int)size : (int)(at / size);
+    return u < big ? c : extra + c;
+  }
+};
+
 // An item: the rows of one row tile of kv head g of sequence b.
 struct KaItem {
   int b, g, first, rows;  // its rows [first, first + rows) of the nq * rep of the sequence's kv head
@@ -206,19 +248,21 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, 1) kv_attention_k
   };
   auto seq_len = [&](int b) { return min(max(a.lens[b], 0), room); };
   auto tiles_of = [&](int nq) { return (int)(((int64_t)nq * rep + C::ROWS - 1) / C::ROWS); };
-  auto units_of = [&](int len) { return max(1, (len + KA_UNIT - 1) / KA_UNIT); };  // (no key: the rows are still written)
+  // An item is a line of KA_START positions and one for every unit of its keys (at least one: the rows
+  // of a sequence without keys are still written).
+  auto line_of = [&](int len) { return KA_START + max(1, (len + KA_UNIT - 1) / KA_UNIT); };
 
-  // ---- this CTA's part [u, end) of the line, and the sequence it begins in
+  // ---- this CTA's part [u, end) of the line of all items, and the sequence it begins in
   int64_t* walk = reinterpret_cast<int64_t*>(smem + C::HEAD);
   if (warp == 0) {
-    auto scan = [&](int b0, int64_t& own) {  // units of sequences b0 .. b0 + 31: inclusive prefix
+    auto scan = [&](int b0, int64_t& own) {  // positions of sequences b0 .. b0 + 31: inclusive prefix
       int row0;
       const int b = b0 + lane;
       own = 0;
       if (b < a.batch) {
-        const int nq = seq_rows(b, row0);
-        if (a.lens[b] != seq_len(b) && blockIdx.x == 0) report_error(err, DERR_KV_RANGE);
-        if (nq) own = (int64_t)kv.G * tiles_of(nq) * units_of(seq_len(b));
+        const int raw = a.lens[b], nq = seq_rows(b, row0);
+        if (raw != min(max(raw, 0), room) && blockIdx.x == 0) report_error(err, DERR_KV_RANGE);
+        if (nq) own = (int64_t)kv.G * tiles_of(nq) * line_of(min(max(raw, 0), room));
       }
       int64_t upto = own;
       for (int d = 1; d < 32; d <<= 1) {
@@ -227,24 +271,26 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, 1) kv_attention_k
       }
       return upto;
     };
-    int64_t total = 0, own;
-    int b0 = 0;
-    for (; b0 < a.batch; b0 += 32) total += __shfl_sync(0xffffffffu, scan(b0, own), 31);
-    const int64_t n = min((int64_t)gridDim.x, total);  // (CTAs past it have nothing)
-    const int64_t u = blockIdx.x < n ? total * blockIdx.x / n : 0, end = blockIdx.x < n ? total * (blockIdx.x + 1) / n : 0;
+    int64_t total = 0, own, upto = 0;
+    for (int b0 = 0; b0 < a.batch; b0 += 32) {
+      upto = scan(b0, own);
+      total += __shfl_sync(0xffffffffu, upto, 31);
+    }
+    const KaShare share(total, gridDim.x);
+    const int64_t u = share.start(blockIdx.x), end = share.start(blockIdx.x + 1);
     int64_t before = 0;
     int b = 0;
     if (u < end)
-      for (b0 = 0; b0 < a.batch; b0 += 32) {
-        const int64_t upto = before + scan(b0, own);
-        const unsigned hit = __ballot_sync(0xffffffffu, u < upto);
+      for (int b0 = 0; b0 < a.batch; b0 += 32) {
+        if (a.batch > 32) upto = scan(b0, own);
+        const unsigned hit = __ballot_sync(0xffffffffu, u < before + upto);
         if (hit) {
           const int l = __ffs(hit) - 1;
           b = b0 + l;
-          before = __shfl_sync(0xffffffffu, upto - own, l);
+          before += __shfl_sync(0xffffffffu, upto - own, l);
           break;
         }
-        before = __shfl_sync(0xffffffffu, upto, 31);
+        before += __shfl_sync(0xffffffffu, upto, 31);
       }
     if (lane == 0) {
       walk[0] = u;
@@ -255,42 +301,89 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, 1) kv_attention_k
     }
   }
   __syncthreads();
-  int64_t u = walk[0], before = walk[3];  // before: units of the sequences before b
+  int64_t u = walk[0], before = walk[3];  // before: positions of the sequences before b
   const int64_t end = walk[1], total = walk[2];
-  int b = (int)walk[4];
+  KaItem it;
+  it.b = -1;
 
-  while (u < end) {
-    // ---- the item of unit u
-    KaItem it;
-    it.nq = seq_rows(b, it.row0);
-    it.len = seq_len(b);
-    const int per = units_of(it.len), nt = tiles_of(it.nq);
-    if (it.nq == 0 || u - before >= (int64_t)kv.G * nt * per) {
-      if (it.nq) before += (int64_t)kv.G * nt * per;
+  for (int b = (int)walk[4]; u < end;) {
+    // ---- the item of position u
+    if (it.b != b) {
+      it.b = b;
+      it.nq = seq_rows(b, it.row0);
+      it.len = seq_len(b);
+    }
+    const int line = line_of(it.len), nt = tiles_of(it.nq);
+    if (it.nq == 0 || u - before >= (int64_t)kv.G * nt * line) {
+      if (it.nq) before += (int64_t)kv.G * nt * line;
       ++b;
       continue;
     }
-    const int64_t item0 = before + (u - before) / per * per;  // its first unit
-    const int which = (int)((u - before) / per);
-    it.b = b;
+    const int which = u - before < (1ll << 31) ? (int)(u - before) / line : (int)((u - before) / line);
+    const int64_t item0 = before + (int64_t)which * line, upto = min(end, item0 + line);  // its first position
+    const int from = max(0, (int)(u - item0) - KA_START), until = (int)(upto - item0) - KA_START;  // units of keys
+    u = upto;
+    if (until <= from) continue;  // (this part of the line holds the item's beginning only)
+    const bool whole = from == 0 && until == line - KA_START;
     it.g = which / nt;
     it.first = (which - it.g * nt) * C::ROWS;
     it.rows = min(C::ROWS, it.nq * rep - it.first);
-    const int64_t upto = min(end, item0 + per);
-    const int key0 = (int)(u - item0) * KA_UNIT, key1 = min(it.len, (int)(upto - item0) * KA_UNIT);
+    const int key0 = from * KA_UNIT, key1 = min(it.len, until * KA_UNIT);
+
+    // the keys that the item's rows see: its first row the fewest, its last the most
+    const int lim_min = a.causal ? it.len - it.nq + it.first / rep + 1 : it.len;
+    const int lim_max = a.causal ? min(it.len, it.len - it.nq + (it.first + it.rows - 1) / rep + 1) : it.len;
+
+    // ---- this warp's steps: keys key0 + KT warp on, then every WARPS-th
+    const int stop = min(key1, lim_max);
+    const int* table = a.table + (int64_t)it.b * a.max_pages;
+    int next = key0 + KT * warp;  // first key of the next step to copy
+    uint32_t bad = 0;             // two bits a stage: 16 keys whose page is not the cache's
+    int slot = 0;
+    int page[KT / 16];
+    auto look_up = [&]() {
+#pragma unroll
+      for (int h = 0; h < KT / 16; ++h) page[h] = next + 16 * h < stop ? table[(next + 16 * h) >> kv.page_shift] : 0;
+    };
+    look_up();
+    auto issue = [&]() {
+      if (next < stop) {
+        bad &= ~(3u << (2 * slot));
+#pragma unroll
+        for (int h = 0; h < KT / 16; ++h) {
+          const int key = next + 16 * h;
+          if (key >= stop) break;
+          if (page[h] >= 0 && page[h] < kv.pages) {
+            const int64_t vec = kv.vector_of((page[h] << kv.page_shift) + (key & (P - 1)), it.g);
+            const uint8_t* k = static_cast<const uint8_t*>(kv.k) + vec * C::ROWB + 16 * lane;
+            const uint8_t* v = static_cast<const uint8_t*>(kv.v) + vec * C::ROWB + 16 * lane;
+            const uint32_t dst = ring + slot * C::STAGE;
+#pragma unroll
+            for (int i = 0; i < C::ROWB / 32; ++i) {
+              const int c = i * 32 + lane;
+              const uint32_t at = chunk_at<C::ROWB>(16 * h + c / (C::ROWB / 16), c % (C::ROWB / 16));
+              copy16(dst + at, k + 512 * i);
+              copy16(dst + C::TILE + at, v + 512 * i);
+            }
+            if (FP8 && lane < 2) copy16(dst + 2 * C::TILE + KT * lane + 16 * h, (lane ? kv.v_exp : kv.k_exp) + vec);
+          } else {
+            bad |= 1u << (2 * slot + h);
+            if (lane == 0) report_error(err, DERR_KV_RANGE);
+          }
+        }
+        next += KT * C::WARPS;
+        look_up();
+      }
+      copy_commit();
+      slot = slot + 1 == C::STAGES ? 0 : slot + 1;
+    };
+#pragma unroll
+    for (int s = 0; s < C::STAGES - 1; ++s) issue();
 
     // ---- this lane's rows: quad + 8 i of the tile; q as the product's operand; keys each sees
     int lim[2 * MT];
     float qa[2 * MT];  // scale * log2(e) * the power of two that q was divided by
-    int lim_min = it.len, lim_max = 0;
     {
-      // (of all rows of the item: the first sees the fewest keys, the last the most)
-      if (a.causal) {
-        lim_min = it.len - it.nq + it.first / rep + 1;
-        lim_max = min(it.len, it.len - it.nq + (it.first + it.rows - 1) / rep + 1);
-      } else {
-        lim_max = it.len;
-      }
       uint32_t(*qs)[32][4] = reinterpret_cast<uint32_t(*)[32][4]>(smem + C::QF);
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
@@ -352,52 +445,6 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, 1) kv_attention_k
       m[i] = -INFINITY;
       l[i] = 0.f;
     }
-
-    // ---- this warp's steps: keys key0 + KT warp on, then every WARPS-th
-    const int stop = min(key1, lim_max);
-    const int* table = a.table + (int64_t)it.b * a.max_pages;
-    int next = key0 + KT * warp;  // first key of the next step to copy
-    uint32_t bad = 0;             // two bits a stage: 16 keys whose page is not the cache's
-    int slot = 0;
-    int page[KT / 16];
-    auto look_up = [&]() {
-#pragma unroll
-      for (int h = 0; h < KT / 16; ++h) page[h] = next + 16 * h < stop ? table[(next + 16 * h) >> kv.page_shift] : 0;
-    };
-    look_up();
-    auto issue = [&]() {
-      if (next < stop) {
-        bad &= ~(3u << (2 * slot));
-#pragma unroll
-        for (int h = 0; h < KT / 16; ++h) {
-          const int key = next + 16 * h;
-          if (key >= stop) break;
-          if (page[h] >= 0 && page[h] < kv.pages) {
-            const int64_t vec = kv.vector_of((page[h] << kv.page_shift) + (key & (P - 1)), it.g);
-            const uint8_t* k = static_cast<const uint8_t*>(kv.k) + vec * C::ROWB + 16 * lane;
-            const uint8_t* v = static_cast<const uint8_t*>(kv.v) + vec * C::ROWB + 16 * lane;
-            const uint32_t dst = ring + slot * C::STAGE;
-#pragma unroll
-            for (int i = 0; i < C::ROWB / 32; ++i) {
-              const int c = i * 32 + lane;
-              const uint32_t at = chunk_at<C::ROWB>(16 * h + c / (C::ROWB / 16), c % (C::ROWB / 16));
-              copy16(dst + at, k + 512 * i);
-              copy16(dst + C::TILE + at, v + 512 * i);
-            }
-            if (FP8 && lane < 2) copy16(dst + 2 * C::TILE + KT * lane + 16 * h, (lane ? kv.v_exp : kv.k_exp) + vec);
-          } else {
-            bad |= 1u << (2 * slot + h);
-            if (lane == 0) report_error(err, DERR_KV_RANGE);
-          }
-        }
-        next += KT * C::WARPS;
-        look_up();
-      }
-      copy_commit();
-      slot = slot + 1 == C::STAGES ? 0 : slot + 1;
-    };
-#pragma unroll
-    for (int s = 0; s < C::STAGES - 1; ++s) issue();
 
     int cur = 0;
     const uint32_t sc = smem_addr(smem) + C::SC + warp * 3 * KT * 4;
@@ -629,56 +676,78 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, 1) kv_attention_k
       l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
       if (place == 0) ml[warp * C::ROWS + 8 * i + quad] = make_float2(m[i], l[i]);
     }
-    float* mine = reinterpret_cast<float*>(smem + warp * C::RING_B);
+    if (key0 + KT * warp < stop) {
+      float* mine = reinterpret_cast<float*>(smem + warp * C::RING_B);
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
+      for (int i = 0; i < MT; ++i)
 #pragma unroll
-      for (int j = 0; j < NT; ++j)
+        for (int j = 0; j < NT; j += 4)
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          mine[(16 * i + quad + 8 * (k >> 1)) * C::O_PITCH + v_comp<HD, FP8>(2 * place + (k & 1), j)] = o[i][j][k];
+          for (int k = 0; k < 4; ++k)
+            *reinterpret_cast<float4*>(mine + (16 * i + quad + 8 * (k >> 1)) * C::O_PITCH +
+                                       o_place<HD, FP8>(v_comp<HD, FP8>(2 * place + (k & 1), j))) =
+                make_float4(o[i][j][k], o[i][j + 1][k], o[i][j + 2][k], o[i][j + 3][k]);
+    }
     __syncthreads();
-    const bool whole = u == item0 && upto == item0 + per;
-    auto finish = [&](int r, int d, float top, float sum, float acc) {  // component d of row r
+    constexpr int E = HD / 32, PART = HD + 4;  // a lane's components of a row
+    auto load = [&](float (&x)[E], const float* from_, bool shared_) {
+      if (E == 4) {
+        const float4 y = shared_ ? *reinterpret_cast<const float4*>(from_) : __ldcg(reinterpret_cast<const float4*>(from_));
+        x[0] = y.x;
+        x[1] = y.y;
+        x[E - 2] = y.z;
+        x[E - 1] = y.w;
+      } else {
+        const float2 y = shared_ ? *reinterpret_cast<const float2*>(from_) : __ldcg(reinterpret_cast<const float2*>(from_));
+        x[0] = y.x;
+        x[1] = y.y;
+      }
+    };
+    auto finish = [&](int r, float top, float sum, const float (&acc)[E]) {
       const int rr = it.first + r, tok = rr / rep, h = it.g * rep + rr - tok * rep;
       const int64_t at = (int64_t)(it.row0 + tok) * a.H + h;
-      a.out[at * HD + d] = __float2bfloat16_rn(sum == 0.f ? 0.f : acc / sum);
-      if (d == 0 && a.lse) a.lse[at] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+      uint32_t w[E / 2];
+#pragma unroll
+      for (int j = 0; j < E / 2; ++j)
+        w[j] = sum == 0.f ? 0u : pack_bf16x2(acc[2 * j] * inv, acc[2 * j + 1] * inv);
+#pragma unroll
+      for (int j = 0; j < E / 2; ++j) reinterpret_cast<uint32_t*>(a.out + at * HD + lane * E)[j] = w[j];
+      if (lane == 0 && a.lse) a.lse[at] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
     };
-    constexpr int PART = HD + 2;
-    const int64_t my_part = 2 * (int64_t)blockIdx.x + (u == item0);
-    for (int i = threadIdx.x; i < it.rows * HD; i += C::THREADS) {
-      const int r = i / HD, d = i - r * HD;
-      float top = -INFINITY, sum = 0.f, acc = 0.f;
+    // a warp per row: lane w has the weight of warp w's part
+    for (int r = warp; r < it.rows; r += C::WARPS) {
+      const float2 x = lane < C::WARPS ? ml[lane * C::ROWS + r] : make_float2(-INFINITY, 0.f);
+      const float top = warp_max(x.x), f = x.x == -INFINITY ? 0.f : exp2_fast(x.x - top);
+      const float sum = warp_sum(x.y * f);
+      float acc[E] = {};
+      const float* o_row = reinterpret_cast<const float*>(smem) + r * C::O_PITCH + o_place<HD, FP8>(lane * E);
+#pragma unroll 4
+      for (int w = 0; w < C::WARPS; ++w) {
+        const float fw = __shfl_sync(0xffffffffu, f, w);
+        if (fw == 0.f) continue;  // (a warp without keys has written nothing)
+        float y[E];
+        load(y, o_row + w * (C::RING_B / 4), true);
 #pragma unroll
-      for (int w = 0; w < C::WARPS; ++w) top = fmaxf(top, ml[w * C::ROWS + r].x);
-      {
-#pragma unroll
-        for (int w = 0; w < C::WARPS; ++w) {
-          const float2 x = ml[w * C::ROWS + r];
-          const float f = x.x == -INFINITY ? 0.f : exp2_fast(x.x - top);
-          sum = fmaf(x.y, f, sum);
-          acc = fmaf(reinterpret_cast<float*>(smem + w * C::RING_B)[r * C::O_PITCH + d], f, acc);
-        }
+        for (int j = 0; j < E; ++j) acc[j] = fmaf(y[j], fw, acc[j]);
       }
       if (whole) {
-        finish(r, d, top, sum, acc);
+        finish(r, top, sum, acc);
       } else {
-        float* part = scratch.part + (my_part * C::ROWS + r) * PART;
-        part[d] = acc;
-        if (d == 0) {
-          part[HD] = top;
-          part[HD + 1] = sum;
-        }
+        float* part = scratch.part + ((2 * (int64_t)blockIdx.x + (from == 0)) * C::ROWS + r) * PART;
+#pragma unroll
+        for (int j = 0; j < E / 2; ++j)
+          *reinterpret_cast<float2*>(part + lane * E + 2 * j) = make_float2(acc[2 * j], acc[2 * j + 1]);
+        if (lane == 0) *reinterpret_cast<float2*>(part + HD) = make_float2(top, sum);
       }
     }
     if (!whole) {  // the CTAs c0 .. c1 share this item
-      const int64_t n = min((int64_t)gridDim.x, total);
-      const int c0 = (int)(((item0 + 1) * n - 1) / total), c1 = (int)(((item0 + per) * n - 1) / total);
+      const KaShare share(total, gridDim.x);
+      const int c0 = share.owner(item0 + KA_START), c1 = share.owner(item0 + line - 1);
       int* last = reinterpret_cast<int*>(smem + C::HEAD + 48);
-      __threadfence();
       __syncthreads();
       if (threadIdx.x == 0) {
+        __threadfence();  // (the block's writes, which the barrier ordered before)
         const int done = atomicAdd(&scratch.count[c0], 1);
         *last = done == c1 - c0;
         if (*last) scratch.count[c0] = 0;
@@ -686,25 +755,32 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, 1) kv_attention_k
       }
       __syncthreads();
       if (*last) {
-        for (int i = threadIdx.x; i < it.rows * HD; i += C::THREADS) {
-          const int r = i / HD, d = i - r * HD;
-          auto part_of = [&](int c) {
-            return scratch.part + ((2 * (int64_t)c + (c == c0)) * C::ROWS + r) * PART;
-          };
-          float top = -INFINITY, sum = 0.f, acc = 0.f;
-          for (int c = c0; c <= c1; ++c) top = fmaxf(top, __ldcg(part_of(c) + HD));
-          for (int c = c0; c <= c1; ++c) {
-            const float* x = part_of(c);
-            const float mc = __ldcg(x + HD), f = mc == -INFINITY ? 0.f : exp2_fast(mc - top);
-            sum = fmaf(__ldcg(x + HD + 1), f, sum);
-            acc = fmaf(__ldcg(x + d), f, acc);
+        for (int r = warp; r < it.rows; r += C::WARPS) {
+          auto part_of = [&](int c) { return scratch.part + ((2 * (int64_t)c + (c == c0)) * C::ROWS + r) * PART; };
+          float top = -INFINITY;
+          for (int c = c0 + lane; c <= c1; c += 32) top = fmaxf(top, __ldcg(part_of(c) + HD));
+          top = warp_max(top);
+          float acc[E] = {}, sum = 0.f;
+          for (int c32 = c0; c32 <= c1; c32 += 32) {
+            const float2 x = c32 + lane <= c1 ? __ldcg(reinterpret_cast<const float2*>(part_of(c32 + lane) + HD))
+                                              : make_float2(-INFINITY, 0.f);
+            const float f = x.x == -INFINITY ? 0.f : exp2_fast(x.x - top);
+            sum += warp_sum(x.y * f);
+            const int n = min(32, c1 - c32 + 1);
+#pragma unroll 4
+            for (int i = 0; i < n; ++i) {
+              const float fc = __shfl_sync(0xffffffffu, f, i);
+              float y[E];
+              load(y, part_of(c32 + i) + lane * E, false);
+#pragma unroll
+              for (int j = 0; j < E; ++j) acc[j] = fmaf(y[j], fc, acc[j]);
+            }
           }
-          finish(r, d, top, sum, acc);
+          finish(r, top, sum, acc);
         }
       }
     }
     __syncthreads();
-    u = upto;
   }
 }
 
@@ -712,7 +788,7 @@ template <int HD, bool FP8, int MT>
 cudaError_t launch_as(const KvPool& kv, const KvAttn& a, const KaScratch& s, int ctas, int* err, cudaStream_t stream) {
   using C = KaCfg<HD, FP8, MT>;
   static_assert(C::SMEM <= 232448, "shared memory per CTA");
-  static_assert(2 * C::ROWS * (HD + 2) * 4 <= KV_ATTN_PART_BYTES, "scratch per CTA");
+  static_assert(2 * C::ROWS * (HD + 4) * 4 <= KV_ATTN_PART_BYTES, "scratch per CTA");
   auto kern = kv_attention_kernel<HD, FP8, MT>;
   static const cudaError_t set =
       cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM);

@@ -41,7 +41,7 @@ struct KvAttn {
 };
 // Scratch of a launch on `sms` SMs: the parts of rows whose keys several CTAs share, then counters,
 // zero before the first launch and left zero by each.
-constexpr size_t KV_ATTN_PART_BYTES = 2 * 32 * (128 + 2) * sizeof(float);  // per CTA
+constexpr size_t KV_ATTN_PART_BYTES = 2 * 32 * (128 + 4) * sizeof(float);  // per CTA
 size_t kv_attention_scratch(int sms);
 cudaError_t kv_attention_launch(const KvPool& kv, const KvAttn& a, void* scratch, int sms, int* err, cudaStream_t stream);
 
