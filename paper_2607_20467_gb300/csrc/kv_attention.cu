@@ -25,6 +25,8 @@
 // P is given in two bf16 parts (2^-16), the second a product more.
 #include <cuda_fp8.h>
 
+#include <algorithm>
+
 #include "common.cuh"
 #include "kv_cache.cuh"
 
@@ -32,12 +34,15 @@ namespace dcl {
 namespace {
 
 constexpr int KA_UNIT = 128;  // keys of a unit of work
+constexpr int KA_CTAS = 2;    // CTAs of an SM: one loads while the other begins or ends an item
 constexpr int KA_START = 3;   // units that beginning an item and joining its parts take
+
+constexpr int KA_MOST = 304;  // most CTAs of a launch
 
 template <int HD, bool FP8, int MT>
 struct KaCfg {
   static constexpr int ES = FP8 ? 1 : 2;
-  static constexpr int WARPS = MT == 1 ? 12 : 8;    // (as many as the registers allow)
+  static constexpr int WARPS = MT == 1 ? 6 : 4;     // (with KA_CTAS of them on an SM as many as the registers allow)
   static constexpr int THREADS = 32 * WARPS;
   static constexpr int KT = FP8 && MT == 1 ? 32 : 16;  // keys that a warp takes at a time
   static constexpr int NK = KT / 8;                 // column tiles of S
@@ -45,8 +50,8 @@ struct KaCfg {
   static constexpr int ROWB = HD * ES;              // bytes of a key
   static constexpr int TILE = KT * ROWB;            // the keys (or values) of a step
   static constexpr int STAGE = 2 * TILE + (FP8 ? 2 * KT : 0);
-  static constexpr int LIMIT = 220 * 1024 / WARPS / STAGE;
-  static constexpr int STAGES = LIMIT > 8 ? 8 : LIMIT;
+  static constexpr int LIMIT = 220 * 1024 / KA_CTAS / WARPS / STAGE;
+  static constexpr int STAGES = LIMIT > 12 ? 12 : LIMIT;
   static constexpr int RING = STAGES * STAGE;       // one warp's
   // a warp's O takes the ring's place: [ROWS][O_PITCH] floats, a lane's runs of components 4 apart
   // from the next lane's, so that 16-byte stores meet all the banks
@@ -56,7 +61,9 @@ struct KaCfg {
   static constexpr int QF = ML + WARPS * ROWS * 8;  // q fragments [MT][HD / 16][lane] of 16 bytes
   static constexpr int SC = QF + MT * (HD / 16) * 32 * 16;  // what the keys' exponents give [warp][3][KT] floats
   static constexpr int HEAD = SC + (FP8 ? WARPS * 3 * KT * 4 : 0);  // the walk's variables
-  static constexpr size_t SMEM = HEAD + 64;
+  static constexpr int TODO = HEAD + 48;            // joins left to this CTA: their number, and two at most
+  static constexpr size_t SMEM = TODO + 3 * 24;
+  static_assert(ML >= ROWS * KA_MOST * 8, "the weights of an item's parts take the rings' place");
   static_assert(STAGES >= 2, "a step in flight");
 };
 
@@ -230,8 +237,103 @@ struct KaItem {
   int row0, nq, len;      // the sequence's first row of q, its new positions, its cached ones
 };
 
+// An item whose parts are all there: `parts` of them, from CTA c0 on.
+struct KaJoin {
+  int row0, head0, first, rows, c0, parts;
+};
+
+template <int E>
+__device__ __forceinline__ void load_row(float (&x)[E], const float* from) {
+  if constexpr (E == 4) {
+    const float4 y = *reinterpret_cast<const float4*>(from);
+    x[0] = y.x;
+    x[1] = y.y;
+    x[2] = y.z;
+    x[3] = y.w;
+  } else {
+    const float2 y = *reinterpret_cast<const float2*>(from);
+    x[0] = y.x;
+    x[1] = y.y;
+  }
+}
+template <int E>
+__device__ __forceinline__ void load_row_l2(float (&x)[E], const float* from) {
+  if constexpr (E == 4) {
+    const float4 y = __ldcg(reinterpret_cast<const float4*>(from));
+    x[0] = y.x;
+    x[1] = y.y;
+    x[2] = y.z;
+    x[3] = y.w;
+  } else {
+    const float2 y = __ldcg(reinterpret_cast<const float2*>(from));
+    x[0] = y.x;
+    x[1] = y.y;
+  }
+}
+// A row, joined: O / l and the log-sum-exp (a warp; a lane has HD / 32 components).
+template <int HD>
+__device__ __forceinline__ void finish_row(__nv_bfloat16* out, float* lse, int64_t at, float top, float sum,
+                                           const float (&acc)[HD / 32]) {
+  const int lane = threadIdx.x & 31;
+  const float inv = 1.f / sum;
+#pragma unroll
+  for (int j = 0; j < HD / 64; ++j)
+    reinterpret_cast<uint32_t*>(out + at * HD + lane * (HD / 32))[j] =
+        sum == 0.f ? 0u : pack_bf16x2(acc[2 * j] * inv, acc[2 * j + 1] * inv);
+  if (lane == 0 && lse) lse[at] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+}
+
+// The n parts of an item, left by CTAs c0 on, joined by the whole block: every part's {m, l} into
+// shared memory at once, then a warp per row, U parts in flight (a load takes about 1000 cycles
+// here: 38 parts joined in turn took 35000).
 template <int HD, bool FP8, int MT>
-__global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, 1) kv_attention_kernel(KvPool kv, KvAttn a, KaScratch scratch, int* err) {
+__device__ __forceinline__ void join_parts(const KvAttn& a, const KaJoin& it, int rep, const float* parts, uint8_t* smem) {
+  using C = KaCfg<HD, FP8, MT>;
+  constexpr int E = HD / 32, PART = HD + 4, U = 16;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = it.parts, rows = it.rows, c0 = it.c0;
+  // (the first CTA's part is its second, the others' their first)
+  const float* first = parts + (2 * (int64_t)c0 + 1) * C::ROWS * PART;
+  auto part_of = [&](int c, int r) { return first + (int64_t)(c ? 2 * c - 1 : 0) * C::ROWS * PART + r * PART; };
+  float2* w = reinterpret_cast<float2*>(smem);  // [row][part]
+  for (int i = threadIdx.x; i < rows * n; i += C::THREADS) {
+    const int r = i / n;
+    w[i] = __ldcg(reinterpret_cast<const float2*>(part_of(i - r * n, r) + HD));
+  }
+  __syncthreads();
+  for (int r = warp; r < rows; r += C::WARPS) {
+    float2* wr = w + r * n;
+    float top = -INFINITY, sum = 0.f;
+    for (int c = lane; c < n; c += 32) top = fmaxf(top, wr[c].x);
+    top = warp_max(top);
+    for (int c = lane; c < n; c += 32) {
+      const float2 x = wr[c];
+      const float f = x.x == -INFINITY ? 0.f : exp2_fast(x.x - top);
+      wr[c].x = f;
+      sum = fmaf(x.y, f, sum);
+    }
+    sum = warp_sum(sum);
+    __syncwarp();
+    float acc[E] = {};
+    for (int c = 0; c < n; c += U) {
+      float y[U][E];
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+        if (c + i < n) load_row_l2<E>(y[i], part_of(c + i, r) + lane * E);
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+        if (c + i < n) {
+          const float f = wr[c + i].x;
+#pragma unroll
+          for (int j = 0; j < E; ++j) acc[j] = fmaf(y[i][j], f, acc[j]);
+        }
+    }
+    const int tok = (it.first + r) / rep;
+    finish_row<HD>(a.out, a.lse, (int64_t)(it.row0 + tok) * a.H + it.head0 + it.first + r - tok * rep, top, sum, acc);
+  }
+}
+
+template <int HD, bool FP8, int MT>
+__global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_attention_kernel(KvPool kv, KvAttn a, KaScratch scratch, int* err) {
   using C = KaCfg<HD, FP8, MT>;
   constexpr int KS = HD / 16;  // k steps of S, and pairs of column tiles of O
   constexpr int NT = HD / 8;   // column tiles of O
@@ -254,6 +356,7 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, 1) kv_attention_k
 
   // ---- this CTA's part [u, end) of the line of all items, and the sequence it begins in
   int64_t* walk = reinterpret_cast<int64_t*>(smem + C::HEAD);
+  KaJoin* todo = reinterpret_cast<KaJoin*>(smem + C::TODO);
   if (warp == 0) {
     auto scan = [&](int b0, int64_t& own) {  // positions of sequences b0 .. b0 + 31: inclusive prefix
       int row0;
@@ -293,6 +396,7 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, 1) kv_attention_k
         before += __shfl_sync(0xffffffffu, upto, 31);
       }
     if (lane == 0) {
+      todo[0].rows = 0;
       walk[0] = u;
       walk[1] = end;
       walk[2] = total;
@@ -333,6 +437,24 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, 1) kv_attention_k
     // the keys that the item's rows see: its first row the fewest, its last the most
     const int lim_min = a.causal ? it.len - it.nq + it.first / rep + 1 : it.len;
     const int lim_max = a.causal ? min(it.len, it.len - it.nq + (it.first + it.rows - 1) / rep + 1) : it.len;
+
+    // ---- this lane's rows: quad + 8 i of the tile; asked for before the keys, which would be in the way
+    int lim[2 * MT];  // keys each sees
+    float qa[2 * MT];  // scale * log2(e) * the power of two that q was divided by
+    uint4 raw[2 * MT][HD / 32];
+#pragma unroll
+    for (int i = 0; i < 2 * MT; ++i) {
+      const int r = 8 * i + quad, rr = it.first + r;
+      const bool live = r < it.rows;
+      const int tok = rr / rep, h = it.g * rep + rr - tok * rep;
+      lim[i] = !live ? 0 : a.causal ? min(it.len, it.len - it.nq + tok + 1) : it.len;
+      const __nv_bfloat16* src = a.q + (it.row0 + tok) * a.q_stride + (int64_t)h * HD;
+#pragma unroll
+      for (int c = 0; c < HD / 32; ++c) {
+        raw[i][c] = make_uint4(0, 0, 0, 0);
+        if (live) raw[i][c] = *reinterpret_cast<const uint4*>(src + 8 * k_chunk<HD, FP8>(place, c));
+      }
+    }
 
     // ---- this warp's steps: keys key0 + KT warp on, then every WARPS-th
     const int stop = min(key1, lim_max);
@@ -380,53 +502,44 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, 1) kv_attention_k
 #pragma unroll
     for (int s = 0; s < C::STAGES - 1; ++s) issue();
 
-    // ---- this lane's rows: quad + 8 i of the tile; q as the product's operand; keys each sees
-    int lim[2 * MT];
-    float qa[2 * MT];  // scale * log2(e) * the power of two that q was divided by
+    // q as the product's operand
     {
       uint32_t(*qs)[32][4] = reinterpret_cast<uint32_t(*)[32][4]>(smem + C::QF);
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
-        uint4 raw[2][HD / 32];
-        float amax[2] = {0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const int r = 16 * mt + 8 * i + quad, rr = it.first + r;
-          const bool live = r < it.rows;
-          const int tok = rr / rep, h = it.g * rep + rr - tok * rep;
-          lim[2 * mt + i] = !live ? 0 : a.causal ? min(it.len, it.len - it.nq + tok + 1) : it.len;
-          const __nv_bfloat16* src = a.q + (it.row0 + tok) * a.q_stride + (int64_t)h * HD;
-#pragma unroll
-          for (int c = 0; c < HD / 32; ++c) {
-            raw[i][c] = make_uint4(0, 0, 0, 0);
-            if (live) raw[i][c] = *reinterpret_cast<const uint4*>(src + 8 * k_chunk<HD, FP8>(place, c));
-            if (FP8) {
-              const uint32_t w[4] = {raw[i][c].x, raw[i][c].y, raw[i][c].z, raw[i][c].w};
-#pragma unroll
-              for (int j = 0; j < 4; ++j) amax[i] = fmaxf(amax[i], fmaxf(fabsf(bf16_lo(w[j])), fabsf(bf16_hi(w[j]))));
-            }
-          }
-          float up = 1.f, down = 1.f;
+          uint4(&rq)[HD / 32] = raw[2 * mt + i];
+          float up = 1.f;
           if (FP8) {
-            amax[i] = fmaxf(amax[i], __shfl_xor_sync(0xffffffffu, amax[i], 1));
-            amax[i] = fmaxf(amax[i], __shfl_xor_sync(0xffffffffu, amax[i], 2));
-            const int x = max(-120, min(120, (int)(__float_as_uint(amax[i]) >> 23) - 127));
-            up = kv_pow2(x);
-            down = kv_pow2(-x);
+            float amax = 0.f;
 #pragma unroll
             for (int c = 0; c < HD / 32; ++c) {
-              uint32_t* w = &raw[i][c].x;
+              const uint32_t w[4] = {rq[c].x, rq[c].y, rq[c].z, rq[c].w};
+#pragma unroll
+              for (int j = 0; j < 4; ++j) amax = fmaxf(amax, fmaxf(fabsf(bf16_lo(w[j])), fabsf(bf16_hi(w[j]))));
+            }
+            amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+            amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+            const int x = max(-120, min(120, (int)(__float_as_uint(amax) >> 23) - 127));
+            up = kv_pow2(x);
+            const float down = kv_pow2(-x);
+#pragma unroll
+            for (int c = 0; c < HD / 32; ++c) {
+              uint32_t* w = &rq[c].x;
 #pragma unroll
               for (int j = 0; j < 4; ++j) w[j] = pack_f16x2(bf16_lo(w[j]) * down, bf16_hi(w[j]) * down);
             }
           }
           qa[2 * mt + i] = a.scale * kLog2e * up;
         }
+        if (warp == 0) {
 #pragma unroll
-        for (int s = 0; s < KS; ++s) {  // step s: components 4 s .. 4 s + 3 of this lane's
-          const uint32_t* w0 = &raw[0][s >> 1].x + 2 * (s & 1);
-          const uint32_t* w1 = &raw[1][s >> 1].x + 2 * (s & 1);
-          if (warp == 0) *reinterpret_cast<uint4*>(qs[mt * KS + s][lane]) = make_uint4(w0[0], w1[0], w0[1], w1[1]);
+          for (int s = 0; s < KS; ++s) {  // step s: components 4 s .. 4 s + 3 of this lane's
+            const uint32_t* w0 = &raw[2 * mt][s >> 1].x + 2 * (s & 1);
+            const uint32_t* w1 = &raw[2 * mt + 1][s >> 1].x + 2 * (s & 1);
+            *reinterpret_cast<uint4*>(qs[mt * KS + s][lane]) = make_uint4(w0[0], w1[0], w0[1], w1[1]);
+          }
         }
       }
       __syncthreads();
@@ -690,31 +803,6 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, 1) kv_attention_k
     }
     __syncthreads();
     constexpr int E = HD / 32, PART = HD + 4;  // a lane's components of a row
-    auto load = [&](float (&x)[E], const float* from_, bool shared_) {
-      if (E == 4) {
-        const float4 y = shared_ ? *reinterpret_cast<const float4*>(from_) : __ldcg(reinterpret_cast<const float4*>(from_));
-        x[0] = y.x;
-        x[1] = y.y;
-        x[E - 2] = y.z;
-        x[E - 1] = y.w;
-      } else {
-        const float2 y = shared_ ? *reinterpret_cast<const float2*>(from_) : __ldcg(reinterpret_cast<const float2*>(from_));
-        x[0] = y.x;
-        x[1] = y.y;
-      }
-    };
-    auto finish = [&](int r, float top, float sum, const float (&acc)[E]) {
-      const int rr = it.first + r, tok = rr / rep, h = it.g * rep + rr - tok * rep;
-      const int64_t at = (int64_t)(it.row0 + tok) * a.H + h;
-      const float inv = sum == 0.f ? 0.f : 1.f / sum;
-      uint32_t w[E / 2];
-#pragma unroll
-      for (int j = 0; j < E / 2; ++j)
-        w[j] = sum == 0.f ? 0u : pack_bf16x2(acc[2 * j] * inv, acc[2 * j + 1] * inv);
-#pragma unroll
-      for (int j = 0; j < E / 2; ++j) reinterpret_cast<uint32_t*>(a.out + at * HD + lane * E)[j] = w[j];
-      if (lane == 0 && a.lse) a.lse[at] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
-    };
     // a warp per row: lane w has the weight of warp w's part
     for (int r = warp; r < it.rows; r += C::WARPS) {
       const float2 x = lane < C::WARPS ? ml[lane * C::ROWS + r] : make_float2(-INFINITY, 0.f);
@@ -727,12 +815,13 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, 1) kv_attention_k
         const float fw = __shfl_sync(0xffffffffu, f, w);
         if (fw == 0.f) continue;  // (a warp without keys has written nothing)
         float y[E];
-        load(y, o_row + w * (C::RING_B / 4), true);
+        load_row<E>(y, o_row + w * (C::RING_B / 4));
 #pragma unroll
         for (int j = 0; j < E; ++j) acc[j] = fmaf(y[j], fw, acc[j]);
       }
       if (whole) {
-        finish(r, top, sum, acc);
+        const int tok = (it.first + r) / rep;
+        finish_row<HD>(a.out, a.lse, (int64_t)(it.row0 + tok) * a.H + it.g * rep + it.first + r - tok * rep, top, sum, acc);
       } else {
         float* part = scratch.part + ((2 * (int64_t)blockIdx.x + (from == 0)) * C::ROWS + r) * PART;
 #pragma unroll
@@ -744,42 +833,22 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, 1) kv_attention_k
     if (!whole) {  // the CTAs c0 .. c1 share this item
       const KaShare share(total, gridDim.x);
       const int c0 = share.owner(item0 + KA_START), c1 = share.owner(item0 + line - 1);
-      int* last = reinterpret_cast<int*>(smem + C::HEAD + 48);
       __syncthreads();
       if (threadIdx.x == 0) {
         __threadfence();  // (the block's writes, which the barrier ordered before)
         const int done = atomicAdd(&scratch.count[c0], 1);
-        *last = done == c1 - c0;
-        if (*last) scratch.count[c0] = 0;
+        if (done == c1 - c0) {  // the last to come joins the parts, when it is through with its own
+          scratch.count[c0] = 0;
+          todo[todo[0].rows++ ? 2 : 1] = KaJoin{it.row0, it.g * rep, it.first, it.rows, c0, c1 - c0 + 1};
+        }
         __threadfence();
       }
-      __syncthreads();
-      if (*last) {
-        for (int r = warp; r < it.rows; r += C::WARPS) {
-          auto part_of = [&](int c) { return scratch.part + ((2 * (int64_t)c + (c == c0)) * C::ROWS + r) * PART; };
-          float top = -INFINITY;
-          for (int c = c0 + lane; c <= c1; c += 32) top = fmaxf(top, __ldcg(part_of(c) + HD));
-          top = warp_max(top);
-          float acc[E] = {}, sum = 0.f;
-          for (int c32 = c0; c32 <= c1; c32 += 32) {
-            const float2 x = c32 + lane <= c1 ? __ldcg(reinterpret_cast<const float2*>(part_of(c32 + lane) + HD))
-                                              : make_float2(-INFINITY, 0.f);
-            const float f = x.x == -INFINITY ? 0.f : exp2_fast(x.x - top);
-            sum += warp_sum(x.y * f);
-            const int n = min(32, c1 - c32 + 1);
-#pragma unroll 4
-            for (int i = 0; i < n; ++i) {
-              const float fc = __shfl_sync(0xffffffffu, f, i);
-              float y[E];
-              load(y, part_of(c32 + i) + lane * E, false);
-#pragma unroll
-              for (int j = 0; j < E; ++j) acc[j] = fmaf(y[j], fc, acc[j]);
-            }
-          }
-          finish(r, top, sum, acc);
-        }
-      }
     }
+    __syncthreads();
+  }
+  for (int i = 0; i < todo[0].rows; ++i) {
+    const KaJoin j = todo[1 + i];
+    join_parts<HD, FP8, MT>(a, j, rep, scratch.part, smem);
     __syncthreads();
   }
 }
@@ -787,7 +856,7 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, 1) kv_attention_k
 template <int HD, bool FP8, int MT>
 cudaError_t launch_as(const KvPool& kv, const KvAttn& a, const KaScratch& s, int ctas, int* err, cudaStream_t stream) {
   using C = KaCfg<HD, FP8, MT>;
-  static_assert(C::SMEM <= 232448, "shared memory per CTA");
+  static_assert(KA_CTAS * (C::SMEM + 1024) <= 233472, "shared memory of an SM");
   static_assert(2 * C::ROWS * (HD + 4) * 4 <= KV_ATTN_PART_BYTES, "scratch per CTA");
   auto kern = kv_attention_kernel<HD, FP8, MT>;
   static const cudaError_t set =
@@ -805,13 +874,14 @@ cudaError_t launch_rows(const KvPool& kv, const KvAttn& a, const KaScratch& s, i
 
 }  // namespace
 
-size_t kv_attention_scratch(int sms) { return (size_t)sms * (KV_ATTN_PART_BYTES + sizeof(int)); }
+size_t kv_attention_scratch(int sms) { return (size_t)KA_CTAS * sms * (KV_ATTN_PART_BYTES + sizeof(int)); }
 
 cudaError_t kv_attention_launch(const KvPool& kv, const KvAttn& a, void* scratch, int sms, int* err, cudaStream_t stream) {
+  sms = std::min(sms, KA_MOST / KA_CTAS);
   KaScratch s{static_cast<float*>(scratch),
-              reinterpret_cast<int*>(static_cast<uint8_t*>(scratch) + (size_t)sms * KV_ATTN_PART_BYTES)};
-  if (kv.hd == 128) return kv.fp8 ? launch_rows<128, true>(kv, a, s, sms, err, stream) : launch_rows<128, false>(kv, a, s, sms, err, stream);
-  return kv.fp8 ? launch_rows<64, true>(kv, a, s, sms, err, stream) : launch_rows<64, false>(kv, a, s, sms, err, stream);
+              reinterpret_cast<int*>(static_cast<uint8_t*>(scratch) + (size_t)KA_CTAS * sms * KV_ATTN_PART_BYTES)};
+  if (kv.hd == 128) return kv.fp8 ? launch_rows<128, true>(kv, a, s, KA_CTAS * sms, err, stream) : launch_rows<128, false>(kv, a, s, KA_CTAS * sms, err, stream);
+  return kv.fp8 ? launch_rows<64, true>(kv, a, s, KA_CTAS * sms, err, stream) : launch_rows<64, false>(kv, a, s, KA_CTAS * sms, err, stream);
 }
 
 }  // namespace dcl
