@@ -26,6 +26,7 @@
 #include <cuda_fp8.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "common.cuh"
 #include "kv_cache.cuh"
@@ -35,7 +36,15 @@ namespace {
 
 constexpr int KA_UNIT = 128;  // keys of a unit of work
 constexpr int KA_CTAS = 2;    // CTAs of an SM: one loads while the other begins or ends an item
-constexpr int KA_START = 3;   // units that beginning an item and joining its parts take
+constexpr int KA_START = 3;   // units that beginning an item takes
+// Sharing an item costs each of its CTAs the writing of a part and one of them the join (3 and 4 to
+// 20 thousand cycles; a unit of 16 rows takes about 1500).  So a cut that falls less than KA_LOW
+// positions after an item's beginning or KA_HIGH before its end goes there, and a CTA has at least
+// KA_LEAST positions where the launch is small.
+constexpr int KA_LOW = KA_START + 3, KA_HIGH = 4, KA_LEAST = 4;
+__device__ __forceinline__ int cut_at(int pos, int line) {
+  return pos >= KA_LOW && pos <= line - KA_HIGH ? pos : 2 * pos < line ? 0 : line;
+}
 
 constexpr int KA_MOST = 304;  // most CTAs of a launch
 
@@ -58,7 +67,8 @@ struct KaCfg {
   static constexpr int O_PITCH = FP8 ? HD + 36 : HD + HD / 2 + 4;
   static constexpr int RING_B = RING > ROWS * O_PITCH * 4 ? RING : ROWS * O_PITCH * 4;
   static constexpr int ML = WARPS * RING_B;         // {m, l} [warp][ROWS]
-  static constexpr int QF = ML + WARPS * ROWS * 8;  // q fragments [MT][HD / 16][lane] of 16 bytes
+  static constexpr int WT = ML + WARPS * ROWS * 8;  // weights of the warps' parts [ROWS][8], then {m, l} of the rows
+  static constexpr int QF = WT + ROWS * (8 * 4 + 8);  // q fragments [MT][HD / 16][lane] of 16 bytes
   static constexpr int SC = QF + MT * (HD / 16) * 32 * 16;  // what the keys' exponents give [warp][3][KT] floats
   static constexpr int HEAD = SC + (FP8 ? WARPS * 3 * KT * 4 : 0);  // the walk's variables
   static constexpr int TODO = HEAD + 48;            // joins left to this CTA: their number, and two at most
@@ -209,12 +219,13 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
-// The line of work in equal parts: CTA c of n has positions [start(c), start(c + 1)).
+// The line of work in equal parts: CTA c of n has positions [start(c), start(c + 1)), each end moved
+// as cut_at says.
 struct KaShare {
   int64_t each;
   int extra, n;
   __device__ KaShare(int64_t total, int ctas) {
-    n = (int)min((int64_t)ctas, total);  // (CTAs past it have nothing)
+    n = (int)min((int64_t)ctas, (total + KA_LEAST - 1) / KA_LEAST);  // (CTAs past it have nothing)
     if (total < (1ll << 31)) {
       each = n ? (int)total / n : 0;
     } else {
@@ -242,94 +253,110 @@ struct KaJoin {
   int row0, head0, first, rows, c0, parts;
 };
 
-template <int E>
-__device__ __forceinline__ void load_row(float (&x)[E], const float* from) {
-  if constexpr (E == 4) {
-    const float4 y = *reinterpret_cast<const float4*>(from);
-    x[0] = y.x;
-    x[1] = y.y;
-    x[2] = y.z;
-    x[3] = y.w;
-  } else {
-    const float2 y = *reinterpret_cast<const float2*>(from);
-    x[0] = y.x;
-    x[1] = y.y;
-  }
+// Four components of a row, joined: O / l, and the row's log-sum-exp.
+__device__ __forceinline__ void finish4(const KvAttn& a, int64_t at, int HD, int c, float2 row, const float4& o) {
+  const float inv = 1.f / row.y;
+  uint2 w = make_uint2(0, 0);
+  if (row.y != 0.f) w = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
+  *reinterpret_cast<uint2*>(a.out + at * HD + c) = w;
+  if (c == 0 && a.lse) a.lse[at] = row.y == 0.f ? -INFINITY : (row.x + log2f(row.y)) * kLn2;
 }
-template <int E>
-__device__ __forceinline__ void load_row_l2(float (&x)[E], const float* from) {
-  if constexpr (E == 4) {
-    const float4 y = __ldcg(reinterpret_cast<const float4*>(from));
-    x[0] = y.x;
-    x[1] = y.y;
-    x[2] = y.z;
-    x[3] = y.w;
-  } else {
-    const float2 y = __ldcg(reinterpret_cast<const float2*>(from));
-    x[0] = y.x;
-    x[1] = y.y;
-  }
-}
-// A row, joined: O / l and the log-sum-exp (a warp; a lane has HD / 32 components).
-template <int HD>
-__device__ __forceinline__ void finish_row(__nv_bfloat16* out, float* lse, int64_t at, float top, float sum,
-                                           const float (&acc)[HD / 32]) {
-  const int lane = threadIdx.x & 31;
-  const float inv = 1.f / sum;
-#pragma unroll
-  for (int j = 0; j < HD / 64; ++j)
-    reinterpret_cast<uint32_t*>(out + at * HD + lane * (HD / 32))[j] =
-        sum == 0.f ? 0u : pack_bf16x2(acc[2 * j] * inv, acc[2 * j + 1] * inv);
-  if (lane == 0 && lse) lse[at] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+__device__ __forceinline__ void add_scaled(float4& acc, const float4& y, float f) {
+  acc.x = fmaf(y.x, f, acc.x);
+  acc.y = fmaf(y.y, f, acc.y);
+  acc.z = fmaf(y.z, f, acc.z);
+  acc.w = fmaf(y.w, f, acc.w);
 }
 
-// The n parts of an item, left by CTAs c0 on, joined by the whole block: every part's {m, l} into
-// shared memory at once, then a warp per row, U parts in flight (a load takes about 1000 cycles
-// here: 38 parts joined in turn took 35000).
+// The parts of an item, left by its CTAs, joined by the whole block: every part's {m, l} into shared
+// memory at once, a row's weights by a thread or a warp; then four components of a row a thread, eight
+// to sixteen loads in flight (one takes about 1000 cycles here: a warp per row, part after part,
+// took 35000 for 38 parts and 17000 for two parts of 32 rows).
 template <int HD, bool FP8, int MT>
 __device__ __forceinline__ void join_parts(const KvAttn& a, const KaJoin& it, int rep, const float* parts, uint8_t* smem) {
   using C = KaCfg<HD, FP8, MT>;
-  constexpr int E = HD / 32, PART = HD + 4, U = 16;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = it.parts, rows = it.rows, c0 = it.c0;
+  constexpr int PART = HD + 4, Q = HD / 4;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = it.parts;
   // (the first CTA's part is its second, the others' their first)
-  const float* first = parts + (2 * (int64_t)c0 + 1) * C::ROWS * PART;
-  auto part_of = [&](int c, int r) { return first + (int64_t)(c ? 2 * c - 1 : 0) * C::ROWS * PART + r * PART; };
+  const float* first = parts + (2 * (int64_t)it.c0 + 1) * C::ROWS * PART;
+  auto part_of = [&](int c) { return first + (int64_t)max(2 * c - 1, 0) * (C::ROWS * PART); };
   float2* w = reinterpret_cast<float2*>(smem);  // [row][part]
-  for (int i = threadIdx.x; i < rows * n; i += C::THREADS) {
+  float2* row = reinterpret_cast<float2*>(smem + C::WT + C::ROWS * 32);
+  for (int i = threadIdx.x; i < it.rows * n; i += C::THREADS) {
     const int r = i / n;
-    w[i] = __ldcg(reinterpret_cast<const float2*>(part_of(i - r * n, r) + HD));
+    w[i] = __ldcg(reinterpret_cast<const float2*>(part_of(i - r * n) + r * PART + HD));
   }
   __syncthreads();
-  for (int r = warp; r < rows; r += C::WARPS) {
-    float2* wr = w + r * n;
-    float top = -INFINITY, sum = 0.f;
-    for (int c = lane; c < n; c += 32) top = fmaxf(top, wr[c].x);
-    top = warp_max(top);
-    for (int c = lane; c < n; c += 32) {
-      const float2 x = wr[c];
-      const float f = x.x == -INFINITY ? 0.f : exp2_fast(x.x - top);
-      wr[c].x = f;
-      sum = fmaf(x.y, f, sum);
+  if (n <= 8) {
+    if ((int)threadIdx.x < it.rows) {
+      float2* wr = w + threadIdx.x * n;
+      float top = -INFINITY, sum = 0.f;
+      for (int c = 0; c < n; ++c) top = fmaxf(top, wr[c].x);
+      for (int c = 0; c < n; ++c) {
+        const float2 x = wr[c];
+        const float f = x.x == -INFINITY ? 0.f : exp2_fast(x.x - top);
+        wr[c].x = f;
+        sum = fmaf(x.y, f, sum);
+      }
+      row[threadIdx.x] = make_float2(top, sum);
     }
-    sum = warp_sum(sum);
-    __syncwarp();
-    float acc[E] = {};
-    for (int c = 0; c < n; c += U) {
-      float y[U][E];
-#pragma unroll
-      for (int i = 0; i < U; ++i)
-        if (c + i < n) load_row_l2<E>(y[i], part_of(c + i, r) + lane * E);
-#pragma unroll
-      for (int i = 0; i < U; ++i)
-        if (c + i < n) {
-          const float f = wr[c + i].x;
-#pragma unroll
-          for (int j = 0; j < E; ++j) acc[j] = fmaf(y[i][j], f, acc[j]);
-        }
+  } else {
+    for (int r = warp; r < it.rows; r += C::WARPS) {
+      float2* wr = w + r * n;
+      float top = -INFINITY, sum = 0.f;
+      for (int c = lane; c < n; c += 32) top = fmaxf(top, wr[c].x);
+      top = warp_max(top);
+      for (int c = lane; c < n; c += 32) {
+        const float2 x = wr[c];
+        const float f = x.x == -INFINITY ? 0.f : exp2_fast(x.x - top);
+        wr[c].x = f;
+        sum = fmaf(x.y, f, sum);
+      }
+      sum = warp_sum(sum);
+      if (lane == 0) row[r] = make_float2(top, sum);
     }
-    const int tok = (it.first + r) / rep;
-    finish_row<HD>(a.out, a.lse, (int64_t)(it.row0 + tok) * a.H + it.head0 + it.first + r - tok * rep, top, sum, acc);
   }
+  __syncthreads();
+  auto tasks = [&](auto tasks_, auto parts_) {
+    constexpr int T = decltype(tasks_)::value, U = decltype(parts_)::value;
+#pragma unroll 1
+    for (int t0 = threadIdx.x; t0 < it.rows * Q; t0 += T * C::THREADS) {
+      float4 acc[T];
+      const float* from[T];
+      const float2* wr[T];
+#pragma unroll
+      for (int k = 0; k < T; ++k) {
+        const int t = min(t0 + k * C::THREADS, it.rows * Q - 1), r = t / Q;
+        acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        from[k] = first + r * PART + 4 * (t % Q);
+        wr[k] = w + r * n;
+      }
+#pragma unroll 1
+      for (int c = 0; c < n; c += U) {
+        float4 y[T][U];
+#pragma unroll
+        for (int i = 0; i < U; ++i)  // (past the end: the last again, without weight)
+#pragma unroll
+          for (int k = 0; k < T; ++k)
+            y[k][i] = __ldcg(reinterpret_cast<const float4*>(from[k] + (int64_t)max(2 * min(c + i, n - 1) - 1, 0) * (C::ROWS * PART)));
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+#pragma unroll
+          for (int k = 0; k < T; ++k) add_scaled(acc[k], y[k][i], c + i < n ? wr[k][c + i].x : 0.f);
+      }
+#pragma unroll
+      for (int k = 0; k < T; ++k) {
+        const int t = t0 + k * C::THREADS;
+        if (t >= it.rows * Q) break;
+        const int r = t / Q, tok = (it.first + r) / rep;
+        finish4(a, (int64_t)(it.row0 + tok) * a.H + it.head0 + it.first + r - tok * rep, HD, 4 * (t % Q), row[r], acc[k]);
+      }
+    }
+  };
+  if (n <= 4)
+    tasks(std::integral_constant<int, 4>{}, std::integral_constant<int, 2>{});
+  else
+    tasks(std::integral_constant<int, 2>{}, std::integral_constant<int, 8>{});
 }
 
 template <int HD, bool FP8, int MT>
@@ -380,10 +407,10 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
       total += __shfl_sync(0xffffffffu, upto, 31);
     }
     const KaShare share(total, gridDim.x);
-    const int64_t u = share.start(blockIdx.x), end = share.start(blockIdx.x + 1);
-    int64_t before = 0;
-    int b = 0;
-    if (u < end)
+    // where the cut before CTA c goes: the position, its sequence and the positions before that
+    auto cut = [&](int c, int& b, int64_t& before) -> int64_t {
+      const int64_t u = share.start(c);
+      before = 0;
       for (int b0 = 0; b0 < a.batch; b0 += 32) {
         if (a.batch > 32) upto = scan(b0, own);
         const unsigned hit = __ballot_sync(0xffffffffu, u < before + upto);
@@ -391,10 +418,22 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
           const int l = __ffs(hit) - 1;
           b = b0 + l;
           before += __shfl_sync(0xffffffffu, upto - own, l);
-          break;
+          const int line = line_of(seq_len(b));
+          const int64_t in = u - before;
+          const int pos = in < (1ll << 31) ? (int)in % line : (int)(in % line);
+          return u - pos + cut_at(pos, line);
         }
         before += __shfl_sync(0xffffffffu, upto, 31);
       }
+      b = a.batch;
+      return total;
+    };
+    int b = 0, b_end;
+    int64_t before = 0, before_end, u = 0, end = 0;
+    if ((int)blockIdx.x < share.n) {
+      u = cut(blockIdx.x, b, before);
+      end = cut(blockIdx.x + 1, b_end, before_end);
+    }
     if (lane == 0) {
       todo[0].rows = 0;
       walk[0] = u;
@@ -802,37 +841,49 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
                 make_float4(o[i][j][k], o[i][j + 1][k], o[i][j + 2][k], o[i][j + 3][k]);
     }
     __syncthreads();
-    constexpr int E = HD / 32, PART = HD + 4;  // a lane's components of a row
-    // a warp per row: lane w has the weight of warp w's part
-    for (int r = warp; r < it.rows; r += C::WARPS) {
-      const float2 x = lane < C::WARPS ? ml[lane * C::ROWS + r] : make_float2(-INFINITY, 0.f);
-      const float top = warp_max(x.x), f = x.x == -INFINITY ? 0.f : exp2_fast(x.x - top);
-      const float sum = warp_sum(x.y * f);
-      float acc[E] = {};
-      const float* o_row = reinterpret_cast<const float*>(smem) + r * C::O_PITCH + o_place<HD, FP8>(lane * E);
-#pragma unroll 4
-      for (int w = 0; w < C::WARPS; ++w) {
-        const float fw = __shfl_sync(0xffffffffu, f, w);
-        if (fw == 0.f) continue;  // (a warp without keys has written nothing)
-        float y[E];
-        load_row<E>(y, o_row + w * (C::RING_B / 4));
+    // a row's weights by a thread, then four components of a row a thread
+    float* wt = reinterpret_cast<float*>(smem + C::WT);
+    float2* row = reinterpret_cast<float2*>(smem + C::WT + C::ROWS * 32);
+    if (threadIdx.x < it.rows) {
+      const int r = threadIdx.x;
+      float2 x[C::WARPS];
+      float top = -INFINITY, sum = 0.f;
 #pragma unroll
-        for (int j = 0; j < E; ++j) acc[j] = fmaf(y[j], fw, acc[j]);
+      for (int w = 0; w < C::WARPS; ++w) {
+        x[w] = ml[w * C::ROWS + r];
+        top = fmaxf(top, x[w].x);
       }
+#pragma unroll
+      for (int w = 0; w < C::WARPS; ++w) {
+        const float f = x[w].x == -INFINITY ? 0.f : exp2_fast(x[w].x - top);
+        wt[r * 8 + w] = f;
+        sum = fmaf(x[w].y, f, sum);
+      }
+      row[r] = make_float2(top, sum);
+    }
+    __syncthreads();
+    constexpr int PART = HD + 4, Q = HD / 4;
+    const int active = min(C::WARPS, (stop - key0 + KT - 1) / KT);  // (warps without keys have written no O)
+#pragma unroll 4
+    for (int t = threadIdx.x; t < it.rows * Q; t += C::THREADS) {
+      const int r = t / Q, c = 4 * (t % Q);
+      const float* o_row = reinterpret_cast<const float*>(smem) + r * C::O_PITCH + o_place<HD, FP8>(c);
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < C::WARPS; ++w)
+        if (w < active) add_scaled(acc, *reinterpret_cast<const float4*>(o_row + w * (C::RING_B / 4)), wt[r * 8 + w]);
       if (whole) {
         const int tok = (it.first + r) / rep;
-        finish_row<HD>(a.out, a.lse, (int64_t)(it.row0 + tok) * a.H + it.g * rep + it.first + r - tok * rep, top, sum, acc);
+        finish4(a, (int64_t)(it.row0 + tok) * a.H + it.g * rep + it.first + r - tok * rep, HD, c, row[r], acc);
       } else {
         float* part = scratch.part + ((2 * (int64_t)blockIdx.x + (from == 0)) * C::ROWS + r) * PART;
-#pragma unroll
-        for (int j = 0; j < E / 2; ++j)
-          *reinterpret_cast<float2*>(part + lane * E + 2 * j) = make_float2(acc[2 * j], acc[2 * j + 1]);
-        if (lane == 0) *reinterpret_cast<float2*>(part + HD) = make_float2(top, sum);
+        *reinterpret_cast<float4*>(part + c) = acc;
+        if (c == 0) *reinterpret_cast<float2*>(part + HD) = row[r];
       }
     }
     if (!whole) {  // the CTAs c0 .. c1 share this item
       const KaShare share(total, gridDim.x);
-      const int c0 = share.owner(item0 + KA_START), c1 = share.owner(item0 + line - 1);
+      const int c0 = share.owner(item0 + KA_LOW - 1), c1 = share.owner(item0 + line - KA_HIGH);
       __syncthreads();
       if (threadIdx.x == 0) {
         __threadfence();  // (the block's writes, which the barrier ordered before)
