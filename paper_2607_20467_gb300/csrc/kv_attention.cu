@@ -30,22 +30,12 @@
 
 #include "common.cuh"
 #include "kv_cache.cuh"
+#include "kv_share.cuh"
 
 namespace dcl {
 namespace {
 
-constexpr int KA_UNIT = 128;  // keys of a unit of work
 constexpr int KA_CTAS = 2;    // CTAs of an SM: one loads while the other begins or ends an item
-constexpr int KA_START = 3;   // units that beginning an item takes
-// Sharing an item costs each of its CTAs the writing of a part and one of them the join (3 and 4 to
-// 20 thousand cycles; a unit of 16 rows takes about 1500).  So a cut that falls less than KA_LOW
-// positions after an item's beginning or KA_HIGH before its end goes there, and a CTA has at least
-// KA_LEAST positions where the launch is small.
-constexpr int KA_LOW = KA_START + 3, KA_HIGH = 4, KA_LEAST = 4;
-__device__ __forceinline__ int cut_at(int pos, int line) {
-  return pos >= KA_LOW && pos <= line - KA_HIGH ? pos : 2 * pos < line ? 0 : line;
-}
-
 constexpr int KA_MOST = 304;  // most CTAs of a launch
 
 template <int HD, bool FP8, int MT>
@@ -75,11 +65,6 @@ struct KaCfg {
   static constexpr size_t SMEM = TODO + 3 * 24;
   static_assert(ML >= ROWS * KA_MOST * 8, "the weights of an item's parts take the rings' place");
   static_assert(STAGES >= 2, "a step in flight");
-};
-
-struct KaScratch {
-  float* part;  // [2 * CTAs][ROWS][HD + 4]: O, m, l
-  int* count;   // [CTAs], zero between launches
 };
 
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
@@ -130,11 +115,6 @@ __device__ __forceinline__ uint32_t widen_hi(uint32_t w) {
   uint32_t r;
   asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, h;\n\t}" : "=r"(r) : "r"(w));
   return r;
-}
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
 }
 template <bool FP8>
 __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -208,157 +188,6 @@ __device__ __forceinline__ int o_place(int c) {
   if (FP8) return c + 4 * (c / (HD / 8));
   return (c >> 6) * 96 + ((c >> 3) & 7) * 12 + (c & 7);
 }
-__device__ __forceinline__ float warp_max(float v) {
-#pragma unroll
-  for (int d = 16; d; d >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
-  return v;
-}
-__device__ __forceinline__ float warp_sum(float v) {
-#pragma unroll
-  for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
-  return v;
-}
-
-// The line of work in equal parts: CTA c of n has positions [start(c), start(c + 1)), each end moved
-// as cut_at says.
-struct KaShare {
-  int64_t each;
-  int extra, n;
-  __device__ KaShare(int64_t total, int ctas) {
-    n = (int)min((int64_t)ctas, (total + KA_LEAST - 1) / KA_LEAST);  // (CTAs past it have nothing)
-    if (total < (1ll << 31)) {
-      each = n ? (int)total / n : 0;
-    } else {
-      each = total / n;
-    }
-    extra = (int)(total - each * n);
-  }
-  __device__ int64_t start(int c) const { return c >= n ? each * n + extra : each * c + min(c, extra); }
-  __device__ int owner(int64_t u) const {
-    const int64_t big = extra * (each + 1);
-    const int64_t at = u < big ? u : u - big, size = u < big ? each + 1 : each;
-    const int c = at < (1ll << 31) && size < (1ll << 31) ? (int)at / (int)size : (int)(at / size);
-    return u < big ? c : extra + c;
-  }
-};
-
-// An item: the rows of one row tile of kv head g of sequence b.
-struct KaItem {
-  int b, g, first, rows;  // its rows [first, first + rows) of the nq * rep of the sequence's kv head
-  int row0, nq, len;      // the sequence's first row of q, its new positions, its cached ones
-};
-
-// An item whose parts are all there: `parts` of them, from CTA c0 on.
-struct KaJoin {
-  int row0, head0, first, rows, c0, parts;
-};
-
-// Four components of a row, joined: O / l, and the row's log-sum-exp.
-__device__ __forceinline__ void finish4(const KvAttn& a, int64_t at, int HD, int c, float2 row, const float4& o) {
-  const float inv = 1.f / row.y;
-  uint2 w = make_uint2(0, 0);
-  if (row.y != 0.f) w = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
-  *reinterpret_cast<uint2*>(a.out + at * HD + c) = w;
-  if (c == 0 && a.lse) a.lse[at] = row.y == 0.f ? -INFINITY : (row.x + log2f(row.y)) * kLn2;
-}
-__device__ __forceinline__ void add_scaled(float4& acc, const float4& y, float f) {
-  acc.x = fmaf(y.x, f, acc.x);
-  acc.y = fmaf(y.y, f, acc.y);
-  acc.z = fmaf(y.z, f, acc.z);
-  acc.w = fmaf(y.w, f, acc.w);
-}
-
-// The parts of an item, left by its CTAs, joined by the whole block: every part's {m, l} into shared
-// memory at once, a row's weights by a thread or a warp; then four components of a row a thread, eight
-// to sixteen loads in flight (one takes about 1000 cycles here: a warp per row, part after part,
-// took 35000 for 38 parts and 17000 for two parts of 32 rows).
-template <int HD, bool FP8, int MT>
-__device__ __forceinline__ void join_parts(const KvAttn& a, const KaJoin& it, int rep, const float* parts, uint8_t* smem) {
-  using C = KaCfg<HD, FP8, MT>;
-  constexpr int PART = HD + 4, Q = HD / 4;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = it.parts;
-  // (the first CTA's part is its second, the others' their first)
-  const float* first = parts + (2 * (int64_t)it.c0 + 1) * C::ROWS * PART;
-  auto part_of = [&](int c) { return first + (int64_t)max(2 * c - 1, 0) * (C::ROWS * PART); };
-  float2* w = reinterpret_cast<float2*>(smem);  // [row][part]
-  float2* row = reinterpret_cast<float2*>(smem + C::WT + C::ROWS * 32);
-  for (int i = threadIdx.x; i < it.rows * n; i += C::THREADS) {
-    const int r = i / n;
-    w[i] = __ldcg(reinterpret_cast<const float2*>(part_of(i - r * n) + r * PART + HD));
-  }
-  __syncthreads();
-  if (n <= 8) {
-    if ((int)threadIdx.x < it.rows) {
-      float2* wr = w + threadIdx.x * n;
-      float top = -INFINITY, sum = 0.f;
-      for (int c = 0; c < n; ++c) top = fmaxf(top, wr[c].x);
-      for (int c = 0; c < n; ++c) {
-        const float2 x = wr[c];
-        const float f = x.x == -INFINITY ? 0.f : exp2_fast(x.x - top);
-        wr[c].x = f;
-        sum = fmaf(x.y, f, sum);
-      }
-      row[threadIdx.x] = make_float2(top, sum);
-    }
-  } else {
-    for (int r = warp; r < it.rows; r += C::WARPS) {
-      float2* wr = w + r * n;
-      float top = -INFINITY, sum = 0.f;
-      for (int c = lane; c < n; c += 32) top = fmaxf(top, wr[c].x);
-      top = warp_max(top);
-      for (int c = lane; c < n; c += 32) {
-        const float2 x = wr[c];
-        const float f = x.x == -INFINITY ? 0.f : exp2_fast(x.x - top);
-        wr[c].x = f;
-        sum = fmaf(x.y, f, sum);
-      }
-      sum = warp_sum(sum);
-      if (lane == 0) row[r] = make_float2(top, sum);
-    }
-  }
-  __syncthreads();
-  auto tasks = [&](auto tasks_, auto parts_) {
-    constexpr int T = decltype(tasks_)::value, U = decltype(parts_)::value;
-#pragma unroll 1
-    for (int t0 = threadIdx.x; t0 < it.rows * Q; t0 += T * C::THREADS) {
-      float4 acc[T];
-      const float* from[T];
-      const float2* wr[T];
-#pragma unroll
-      for (int k = 0; k < T; ++k) {
-        const int t = min(t0 + k * C::THREADS, it.rows * Q - 1), r = t / Q;
-        acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-        from[k] = first + r * PART + 4 * (t % Q);
-        wr[k] = w + r * n;
-      }
-#pragma unroll 1
-      for (int c = 0; c < n; c += U) {
-        float4 y[T][U];
-#pragma unroll
-        for (int i = 0; i < U; ++i)  // (past the end: the last again, without weight)
-#pragma unroll
-          for (int k = 0; k < T; ++k)
-            y[k][i] = __ldcg(reinterpret_cast<const float4*>(from[k] + (int64_t)max(2 * min(c + i, n - 1) - 1, 0) * (C::ROWS * PART)));
-#pragma unroll
-        for (int i = 0; i < U; ++i)
-#pragma unroll
-          for (int k = 0; k < T; ++k) add_scaled(acc[k], y[k][i], c + i < n ? wr[k][c + i].x : 0.f);
-      }
-#pragma unroll
-      for (int k = 0; k < T; ++k) {
-        const int t = t0 + k * C::THREADS;
-        if (t >= it.rows * Q) break;
-        const int r = t / Q, tok = (it.first + r) / rep;
-        finish4(a, (int64_t)(it.row0 + tok) * a.H + it.head0 + it.first + r - tok * rep, HD, 4 * (t % Q), row[r], acc[k]);
-      }
-    }
-  };
-  if (n <= 4)
-    tasks(std::integral_constant<int, 4>{}, std::integral_constant<int, 2>{});
-  else
-    tasks(std::integral_constant<int, 2>{}, std::integral_constant<int, 8>{});
-}
-
 template <int HD, bool FP8, int MT>
 __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_attention_kernel(KvPool kv, KvAttn a, KaScratch scratch, int* err) {
   using C = KaCfg<HD, FP8, MT>;
@@ -367,111 +196,26 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
   constexpr int KT = C::KT, NK = C::NK;
   extern __shared__ __align__(128) uint8_t smem[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = lane >> 2, place = lane & 3;
-  const int rep = a.H / kv.G, room = a.max_pages << kv.page_shift, P = kv.page_len();
+  const int rep = a.H / kv.G, P = kv.page_len();
   const uint32_t ring = smem_addr(smem) + warp * C::RING_B;
   float2* ml = reinterpret_cast<float2*>(smem + C::ML);
 
-  auto seq_rows = [&](int b, int& row0) {
-    row0 = min(max(a.q_start[b], 0), a.rows);
-    return min(max(a.q_start[b + 1], row0), a.rows) - row0;
-  };
-  auto seq_len = [&](int b) { return min(max(a.lens[b], 0), room); };
-  auto tiles_of = [&](int nq) { return (int)(((int64_t)nq * rep + C::ROWS - 1) / C::ROWS); };
-  // An item is a line of KA_START positions and one for every unit of its keys (at least one: the rows
-  // of a sequence without keys are still written).
-  auto line_of = [&](int len) { return KA_START + max(1, (len + KA_UNIT - 1) / KA_UNIT); };
+  const KaLine<C::ROWS> line(kv, a);
 
-  // ---- this CTA's part [u, end) of the line of all items, and the sequence it begins in
-  int64_t* walk = reinterpret_cast<int64_t*>(smem + C::HEAD);
+  // ---- this CTA's part of the line of all items
+  KaWalk& shared_walk = *reinterpret_cast<KaWalk*>(smem + C::HEAD);
   KaJoin* todo = reinterpret_cast<KaJoin*>(smem + C::TODO);
   if (warp == 0) {
-    auto scan = [&](int b0, int64_t& own) {  // positions of sequences b0 .. b0 + 31: inclusive prefix
-      int row0;
-      const int b = b0 + lane;
-      own = 0;
-      if (b < a.batch) {
-        const int raw = a.lens[b], nq = seq_rows(b, row0);
-        if (raw != min(max(raw, 0), room) && blockIdx.x == 0) report_error(err, DERR_KV_RANGE);
-        if (nq) own = (int64_t)kv.G * tiles_of(nq) * line_of(min(max(raw, 0), room));
-      }
-      int64_t upto = own;
-      for (int d = 1; d < 32; d <<= 1) {
-        const int64_t x = __shfl_up_sync(0xffffffffu, upto, d);
-        if (lane >= d) upto += x;
-      }
-      return upto;
-    };
-    int64_t total = 0, own, upto = 0;
-    for (int b0 = 0; b0 < a.batch; b0 += 32) {
-      upto = scan(b0, own);
-      total += __shfl_sync(0xffffffffu, upto, 31);
-    }
-    const KaShare share(total, gridDim.x);
-    // where the cut before CTA c goes: the position, its sequence and the positions before that
-    auto cut = [&](int c, int& b, int64_t& before) -> int64_t {
-      const int64_t u = share.start(c);
-      before = 0;
-      for (int b0 = 0; b0 < a.batch; b0 += 32) {
-        if (a.batch > 32) upto = scan(b0, own);
-        const unsigned hit = __ballot_sync(0xffffffffu, u < before + upto);
-        if (hit) {
-          const int l = __ffs(hit) - 1;
-          b = b0 + l;
-          before += __shfl_sync(0xffffffffu, upto - own, l);
-          const int line = line_of(seq_len(b));
-          const int64_t in = u - before;
-          const int pos = in < (1ll << 31) ? (int)in % line : (int)(in % line);
-          return u - pos + cut_at(pos, line);
-        }
-        before += __shfl_sync(0xffffffffu, upto, 31);
-      }
-      b = a.batch;
-      return total;
-    };
-    int b = 0, b_end;
-    int64_t before = 0, before_end, u = 0, end = 0;
-    if ((int)blockIdx.x < share.n) {
-      u = cut(blockIdx.x, b, before);
-      end = cut(blockIdx.x + 1, b_end, before_end);
-    }
-    if (lane == 0) {
-      todo[0].rows = 0;
-      walk[0] = u;
-      walk[1] = end;
-      walk[2] = total;
-      walk[3] = before;
-      walk[4] = b;
-    }
+    line.begin(&shared_walk, err);
+    if (lane == 0) todo[0].rows = 0;
   }
   __syncthreads();
-  int64_t u = walk[0], before = walk[3];  // before: positions of the sequences before b
-  const int64_t end = walk[1], total = walk[2];
+  KaWalk walk = shared_walk;
   KaItem it;
   it.b = -1;
 
-  for (int b = (int)walk[4]; u < end;) {
-    // ---- the item of position u
-    if (it.b != b) {
-      it.b = b;
-      it.nq = seq_rows(b, it.row0);
-      it.len = seq_len(b);
-    }
-    const int line = line_of(it.len), nt = tiles_of(it.nq);
-    if (it.nq == 0 || u - before >= (int64_t)kv.G * nt * line) {
-      if (it.nq) before += (int64_t)kv.G * nt * line;
-      ++b;
-      continue;
-    }
-    const int which = u - before < (1ll << 31) ? (int)(u - before) / line : (int)((u - before) / line);
-    const int64_t item0 = before + (int64_t)which * line, upto = min(end, item0 + line);  // its first position
-    const int from = max(0, (int)(u - item0) - KA_START), until = (int)(upto - item0) - KA_START;  // units of keys
-    u = upto;
-    if (until <= from) continue;  // (this part of the line holds the item's beginning only)
-    const bool whole = from == 0 && until == line - KA_START;
-    it.g = which / nt;
-    it.first = (which - it.g * nt) * C::ROWS;
-    it.rows = min(C::ROWS, it.nq * rep - it.first);
-    const int key0 = from * KA_UNIT, key1 = min(it.len, until * KA_UNIT);
+  while (line.next(walk, it)) {
+    const int key0 = it.from * KA_UNIT, key1 = min(it.len, it.until * KA_UNIT);
 
     // the keys that the item's rows see: its first row the fewest, its last the most
     const int lim_min = a.causal ? it.len - it.nq + it.first / rep + 1 : it.len;
@@ -872,18 +616,18 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
 #pragma unroll
       for (int w = 0; w < C::WARPS; ++w)
         if (w < active) add_scaled(acc, *reinterpret_cast<const float4*>(o_row + w * (C::RING_B / 4)), wt[r * 8 + w]);
-      if (whole) {
+      if (it.whole()) {
         const int tok = (it.first + r) / rep;
         finish4(a, (int64_t)(it.row0 + tok) * a.H + it.g * rep + it.first + r - tok * rep, HD, c, row[r], acc);
       } else {
-        float* part = scratch.part + ((2 * (int64_t)blockIdx.x + (from == 0)) * C::ROWS + r) * PART;
+        float* part = scratch.part + ((2 * (int64_t)blockIdx.x + (it.from == 0)) * C::ROWS + r) * PART;
         *reinterpret_cast<float4*>(part + c) = acc;
         if (c == 0) *reinterpret_cast<float2*>(part + HD) = row[r];
       }
     }
-    if (!whole) {  // the CTAs c0 .. c1 share this item
-      const KaShare share(total, gridDim.x);
-      const int c0 = share.owner(item0 + KA_LOW - 1), c1 = share.owner(item0 + line - KA_HIGH);
+    if (!it.whole()) {
+      int c0, c1;
+      line.sharers(walk, it, c0, c1);
       __syncthreads();
       if (threadIdx.x == 0) {
         __threadfence();  // (the block's writes, which the barrier ordered before)
@@ -899,7 +643,9 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
   }
   for (int i = 0; i < todo[0].rows; ++i) {
     const KaJoin j = todo[1 + i];
-    join_parts<HD, FP8, MT>(a, j, rep, scratch.part, smem);
+    join_parts<HD, C::ROWS, C::THREADS>(a, j, rep, scratch.part, reinterpret_cast<float2*>(smem),
+                                        reinterpret_cast<float2*>(smem + C::WT + C::ROWS * 32), threadIdx.x,
+                                        [] { __syncthreads(); });
     __syncthreads();
   }
 }

@@ -1,0 +1,305 @@
+// How the kernels of kv_attention.cu and kv_attention_tc.cu share their work out.
+//
+// An item is the rows of one row tile (new positions x the query heads of one kv head) of one
+// sequence; its keys come in units of 128.  All items of a launch stand in one line, each with
+// KA_START positions for its beginning and one for every unit; every CTA takes an equal part of the
+// line, so that a long sequence is spread over many CTAs, many short ones share one, and none waits
+// for another's longer sequence.
+#pragma once
+
+#include "common.cuh"
+#include "kv_cache.cuh"
+
+namespace dcl {
+namespace {
+
+constexpr int KA_UNIT = 128;  // keys of a unit of work
+constexpr int KA_START = 3;   // units that beginning an item takes
+// Sharing an item costs each of its CTAs the writing of a part and one of them the join (3 and 4 to
+// 20 thousand cycles; a unit of 16 rows takes about 1500).  So a cut that falls less than KA_LOW
+// positions after an item's beginning or KA_HIGH before its end goes there, and a CTA has at least
+// KA_LEAST positions where the launch is small.
+constexpr int KA_LOW = KA_START + 3, KA_HIGH = 4, KA_LEAST = 4;
+__device__ __forceinline__ int cut_at(int pos, int line) {
+  if (line < KA_LOW + KA_HIGH) return 2 * pos < line ? 0 : line;
+  return pos < KA_LOW ? 0 : pos > line - KA_HIGH ? line : pos;
+}
+
+// The line in equal parts: CTA c of n has positions [start(c), start(c + 1)), each end moved as cut_at
+// says.
+struct KaShare {
+  int64_t each;
+  int extra, n;
+  __device__ KaShare(int64_t total, int ctas) {
+    n = (int)min((int64_t)ctas, (total + KA_LEAST - 1) / KA_LEAST);  // (CTAs past it have nothing)
+    if (total < (1ll << 31)) {
+      each = n ? (int)total / n : 0;
+    } else {
+      each = total / n;
+    }
+    extra = (int)(total - each * n);
+  }
+  __device__ int64_t start(int c) const { return c >= n ? each * n + extra : each * c + min(c, extra); }
+  __device__ int owner(int64_t u) const {
+    const int64_t big = extra * (each + 1);
+    const int64_t at = u < big ? u : u - big, size = u < big ? each + 1 : each;
+    const int c = at < (1ll << 31) && size < (1ll << 31) ? (int)at / (int)size : (int)(at / size);
+    return u < big ? c : extra + c;
+  }
+};
+
+// The rows of one row tile of kv head g of sequence b, and this CTA's units of its keys.
+struct KaItem {
+  int b, g, first, rows;  // its rows [first, first + rows) of the nq * rep of the sequence's kv head
+  int row0, nq, len;      // the sequence's first row of q, its new positions, its cached ones
+  int from, until, line;  // units [from, until) of the line - KA_START there are
+  int64_t item0;          // its first position
+  __device__ __forceinline__ bool whole() const { return from == 0 && until == line - KA_START; }
+};
+// An item whose parts are all there: `parts` of them, from CTA c0 on.
+struct KaJoin {
+  int row0, head0, first, rows, c0, parts;
+};
+
+struct KaWalk {
+  int64_t u, end, total, before;  // this CTA's part of the line; positions of the sequences before b
+  int b;
+};
+
+template <int ROWS>  // of an item
+struct KaLine {
+  const KvAttn& a;
+  int G, rep, room;
+  __device__ KaLine(const KvPool& kv, const KvAttn& a_)
+      : a(a_), G(kv.G), rep(a_.H / kv.G), room(a_.max_pages << kv.page_shift) {}
+  __device__ __forceinline__ int seq_rows(int b, int& row0) const {
+    row0 = min(max(a.q_start[b], 0), a.rows);
+    return min(max(a.q_start[b + 1], row0), a.rows) - row0;
+  }
+  __device__ __forceinline__ int seq_len(int b) const { return min(max(a.lens[b], 0), room); }
+  __device__ __forceinline__ int tiles_of(int nq) const { return (int)(((int64_t)nq * rep + ROWS - 1) / ROWS); }
+  // (at least one unit: the rows of a sequence without keys are still written)
+  __device__ __forceinline__ int line_of(int len) const { return KA_START + max(1, (len + KA_UNIT - 1) / KA_UNIT); }
+
+  // This CTA's part (a warp; lane 0 writes it).
+  __device__ __forceinline__ void begin(KaWalk* walk, int* err) const {
+    const int lane = threadIdx.x & 31;
+    auto scan = [&](int b0, int64_t& own) {  // positions of sequences b0 .. b0 + 31: inclusive prefix
+      int row0;
+      const int b = b0 + lane;
+      own = 0;
+      if (b < a.batch) {
+        const int raw = a.lens[b], nq = seq_rows(b, row0);
+        if (raw != min(max(raw, 0), room) && blockIdx.x == 0) report_error(err, DERR_KV_RANGE);
+        if (nq) own = (int64_t)G * tiles_of(nq) * line_of(min(max(raw, 0), room));
+      }
+      int64_t upto = own;
+      for (int d = 1; d < 32; d <<= 1) {
+        const int64_t x = __shfl_up_sync(0xffffffffu, upto, d);
+        if (lane >= d) upto += x;
+      }
+      return upto;
+    };
+    int64_t total = 0, own, upto = 0;
+    for (int b0 = 0; b0 < a.batch; b0 += 32) {
+      upto = scan(b0, own);
+      total += __shfl_sync(0xffffffffu, upto, 31);
+    }
+    const KaShare share(total, gridDim.x);
+    // where the cut before CTA c goes: the position, its sequence and the positions before that
+    auto cut = [&](int c, int& b, int64_t& before) -> int64_t {
+      const int64_t u = share.start(c);
+      before = 0;
+      for (int b0 = 0; b0 < a.batch; b0 += 32) {
+        if (a.batch > 32) upto = scan(b0, own);
+        const unsigned hit = __ballot_sync(0xffffffffu, u < before + upto);
+        if (hit) {
+          const int l = __ffs(hit) - 1;
+          b = b0 + l;
+          before += __shfl_sync(0xffffffffu, upto - own, l);
+          const int line = line_of(seq_len(b));
+          const int64_t in = u - before;
+          const int pos = in < (1ll << 31) ? (int)in % line : (int)(in % line);
+          return u - pos + cut_at(pos, line);
+        }
+        before += __shfl_sync(0xffffffffu, upto, 31);
+      }
+      b = a.batch;
+      return total;
+    };
+    int b = 0, b_end;
+    int64_t before = 0, before_end, u = 0, end = 0;
+    if ((int)blockIdx.x < share.n) {
+      u = cut(blockIdx.x, b, before);
+      end = cut(blockIdx.x + 1, b_end, before_end);
+    }
+    if (lane == 0) *walk = KaWalk{u, end, total, before, b};
+  }
+
+  // The next item of the part; false at its end.  (it.b < 0 before the first)
+  __device__ __forceinline__ bool next(KaWalk& w, KaItem& it) const {
+    while (w.u < w.end) {
+      if (it.b != w.b) {
+        it.b = w.b;
+        it.nq = seq_rows(w.b, it.row0);
+        it.len = seq_len(w.b);
+      }
+      const int line = line_of(it.len), nt = tiles_of(it.nq);
+      if (it.nq == 0 || w.u - w.before >= (int64_t)G * nt * line) {
+        if (it.nq) w.before += (int64_t)G * nt * line;
+        ++w.b;
+        continue;
+      }
+      const int64_t in = w.u - w.before;
+      const int which = in < (1ll << 31) ? (int)in / line : (int)(in / line);
+      it.item0 = w.before + (int64_t)which * line;
+      it.line = line;
+      const int64_t upto = min(w.end, it.item0 + line);
+      it.from = max(0, (int)(w.u - it.item0) - KA_START);
+      it.until = (int)(upto - it.item0) - KA_START;
+      w.u = upto;
+      if (it.until <= it.from) continue;  // (this part of the line holds the item's beginning only)
+      it.g = which / nt;
+      it.first = (which - it.g * nt) * ROWS;
+      it.rows = min(ROWS, it.nq * rep - it.first);
+      return true;
+    }
+    return false;
+  }
+  // The CTAs c0 .. c1 that share an item that is not whole.
+  __device__ __forceinline__ void sharers(const KaWalk& w, const KaItem& it, int& c0, int& c1) const {
+    const KaShare share(w.total, gridDim.x);
+    c0 = share.owner(it.item0 + KA_LOW - 1);
+    c1 = share.owner(it.item0 + it.line - KA_HIGH);
+  }
+};
+
+// Scratch of a launch: the parts of shared items, and how many of each have come.
+struct KaScratch {
+  float* part;  // [2 * CTAs][ROWS][HD + 4]: O, m, l (a CTA's items that it does not begin, and does)
+  int* count;   // [CTAs], by the CTA that begins the item; zero between launches
+};
+
+// Four components of a row, joined: O / l, and the row's log-sum-exp.
+__device__ __forceinline__ void finish4(const KvAttn& a, int64_t at, int HD, int c, float2 row, const float4& o) {
+  const float inv = 1.f / row.y;
+  uint2 w = make_uint2(0, 0);
+  if (row.y != 0.f) w = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
+  *reinterpret_cast<uint2*>(a.out + at * HD + c) = w;
+  if (c == 0 && a.lse) a.lse[at] = row.y == 0.f ? -INFINITY : (row.x + log2f(row.y)) * kLn2;
+}
+__device__ __forceinline__ void add_scaled(float4& acc, const float4& y, float f) {
+  acc.x = fmaf(y.x, f, acc.x);
+  acc.y = fmaf(y.y, f, acc.y);
+  acc.z = fmaf(y.z, f, acc.z);
+  acc.w = fmaf(y.w, f, acc.w);
+}
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+  for (int d = 16; d; d >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
+  return v;
+}
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+  return v;
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// The parts of an item, left by its CTAs, joined by THREADS threads (tid of them; sync: their barrier):
+// every part's {m, l} into shared memory (w, [rows][parts]) at once, a row's weights by a thread or
+// a warp (its {m, l} in row); then four components of a row a thread, eight to sixteen loads in
+// flight (one takes about 1000 cycles here: a warp per row, part after part, took 35000 for 38
+// parts and 17000 for two parts of 32 rows).
+template <int HD, int ROWS, int THREADS, typename Sync>
+__device__ __forceinline__ void join_parts(const KvAttn& a, const KaJoin& it, int rep, const float* parts, float2* w,
+                                           float2* row, int tid, Sync sync) {
+  constexpr int PART = HD + 4, Q = HD / 4;
+  const int warp = tid >> 5, lane = tid & 31, n = it.parts;
+  // (the first CTA's part is its second, the others' their first)
+  const float* first = parts + (2 * (int64_t)it.c0 + 1) * ROWS * PART;
+  auto part_of = [&](int c) { return first + (int64_t)max(2 * c - 1, 0) * (ROWS * PART); };
+  for (int i = tid; i < it.rows * n; i += THREADS) {
+    const int r = i / n;
+    w[i] = __ldcg(reinterpret_cast<const float2*>(part_of(i - r * n) + r * PART + HD));
+  }
+  sync();
+  if (n <= 8) {
+    for (int r = tid; r < it.rows; r += THREADS) {
+      float2* wr = w + r * n;
+      float top = -INFINITY, sum = 0.f;
+      for (int c = 0; c < n; ++c) top = fmaxf(top, wr[c].x);
+      for (int c = 0; c < n; ++c) {
+        const float2 x = wr[c];
+        const float f = x.x == -INFINITY ? 0.f : exp2_fast(x.x - top);
+        wr[c].x = f;
+        sum = fmaf(x.y, f, sum);
+      }
+      row[r] = make_float2(top, sum);
+    }
+  } else {
+    for (int r = warp; r < it.rows; r += THREADS / 32) {
+      float2* wr = w + r * n;
+      float top = -INFINITY, sum = 0.f;
+      for (int c = lane; c < n; c += 32) top = fmaxf(top, wr[c].x);
+      top = warp_max(top);
+      for (int c = lane; c < n; c += 32) {
+        const float2 x = wr[c];
+        const float f = x.x == -INFINITY ? 0.f : exp2_fast(x.x - top);
+        wr[c].x = f;
+        sum = fmaf(x.y, f, sum);
+      }
+      sum = warp_sum(sum);
+      if (lane == 0) row[r] = make_float2(top, sum);
+    }
+  }
+  sync();
+  auto tasks = [&](auto tasks_, auto parts_) {
+    constexpr int T = decltype(tasks_)::value, U = decltype(parts_)::value;
+#pragma unroll 1
+    for (int t0 = tid; t0 < it.rows * Q; t0 += T * THREADS) {
+      float4 acc[T];
+      const float* from[T];
+      const float2* wr[T];
+#pragma unroll
+      for (int k = 0; k < T; ++k) {
+        const int t = min(t0 + k * THREADS, it.rows * Q - 1), r = t / Q;
+        acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        from[k] = first + r * PART + 4 * (t % Q);
+        wr[k] = w + r * n;
+      }
+#pragma unroll 1
+      for (int c = 0; c < n; c += U) {
+        float4 y[T][U];
+#pragma unroll
+        for (int i = 0; i < U; ++i)  // (past the end: the last again, without weight)
+#pragma unroll
+          for (int k = 0; k < T; ++k)
+            y[k][i] = __ldcg(reinterpret_cast<const float4*>(from[k] + (int64_t)max(2 * min(c + i, n - 1) - 1, 0) * (ROWS * PART)));
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+#pragma unroll
+          for (int k = 0; k < T; ++k)
+            if (c + i < n) add_scaled(acc[k], y[k][i], wr[k][c + i].x);
+      }
+#pragma unroll
+      for (int k = 0; k < T; ++k) {
+        const int t = t0 + k * THREADS;
+        if (t >= it.rows * Q) break;
+        const int r = t / Q, tok = (it.first + r) / rep;
+        finish4(a, (int64_t)(it.row0 + tok) * a.H + it.head0 + it.first + r - tok * rep, HD, 4 * (t % Q), row[r], acc[k]);
+      }
+    }
+  };
+  if (n <= 4)
+    tasks(std::integral_constant<int, 4>{}, std::integral_constant<int, 2>{});
+  else
+    tasks(std::integral_constant<int, 2>{}, std::integral_constant<int, 8>{});
+}
+
+}  // namespace
+}  // namespace dcl
