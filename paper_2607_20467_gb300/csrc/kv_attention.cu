@@ -671,6 +671,10 @@ cudaError_t launch_rows(const KvPool& kv, const KvAttn& a, const KaScratch& s, i
 
 }  // namespace
 
+bool kv_attention_many_rows(const KvPool& kv, const KvAttn& a) {
+  return !a.causal && (int64_t)a.max_new * (a.H / kv.G) > 32;
+}
+
 size_t kv_attention_scratch(int sms) { return (size_t)KA_CTAS * sms * (KV_ATTN_PART_BYTES + sizeof(int)); }
 
 cudaError_t kv_attention_launch(const KvPool& kv, const KvAttn& a, void* scratch, int sms, int* err, cudaStream_t stream) {

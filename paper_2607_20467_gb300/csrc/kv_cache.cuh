@@ -39,11 +39,16 @@ struct KvAttn {
   __nv_bfloat16* out;       // [rows][H][hd]
   float* lse;               // [rows][H] or NULL
 };
-// Scratch of a launch on `sms` SMs: the parts of rows whose keys several CTAs share, then counters,
-// zero before the first launch and left zero by each.
-constexpr size_t KV_ATTN_PART_BYTES = 2 * 32 * (128 + 4) * sizeof(float);  // per CTA
+// Two kernels: for up to 32 rows (new positions x query heads of a kv head) that share a kv head's keys,
+// and for more (not causal).  Scratch of a launch on `sms` SMs: the parts of rows whose keys several
+// CTAs share, then counters, zero before the first launch and left zero by each.
+constexpr size_t KV_ATTN_PART_BYTES = 2 * 32 * (128 + 4) * sizeof(float);      // per CTA
+constexpr size_t KV_ATTN_TC_PART_BYTES = 2 * 256 * (128 + 4) * sizeof(float);
+bool kv_attention_many_rows(const KvPool& kv, const KvAttn& a);
 size_t kv_attention_scratch(int sms);
+size_t kv_attention_tc_scratch(int sms);
 cudaError_t kv_attention_launch(const KvPool& kv, const KvAttn& a, void* scratch, int sms, int* err, cudaStream_t stream);
+cudaError_t kv_attention_tc_launch(const KvPool& kv, const KvAttn& a, void* scratch, int sms, int* err, cudaStream_t stream);
 
 // Drawing tokens (sample.cu).
 struct SampleArgs {
