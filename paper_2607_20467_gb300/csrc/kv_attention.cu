@@ -18,11 +18,13 @@
 // FP8 pages.  Codes are widened to fp16, which holds them exactly, q is scaled per row by a power of
 // two into fp16 (its 8 bits fit; what falls below fp16's range is 2^-24 of the row's largest).  A
 // key's exponent scales its score.  A value's exponent e_j goes into the exponent of its
-// probability: P_j = exp2(s_j + e_j - m) with m the running maximum of s_j + e_j, so that P <= 1
-// whatever the values' sizes, and l = sum P_j 2^-e_j.  P is rounded to fp16 (2^-12 of itself;
-// below 2^-14 of the largest term, 2^-25 of that).  bf16 pages: the instruction wants both operands of
-// one type, and bf16 alone would round P by 2^-8 of itself, as much as the output's own rounding;
-// P is given in two bf16 parts (2^-16), the second a product more.
+// probability: P_j = exp2(s_j + e_j - m) with m near the running maximum of s_j + e_j, so that P is
+// bounded whatever the values' sizes, and l = sum P_j 2^-e_j.  P is rounded to fp16 (2^-11 of itself;
+// below 2^-21 of the largest term, 2^-32 of that); O is divided by the same sum of the rounded P, so that a
+// row which one key dominates shows nothing of it, while l, of the unrounded, gives the log-sum-exp.
+// bf16 pages: the instruction wants both operands of one type, and bf16 alone would round P by 2^-8
+// of itself, as much as the output's own rounding; P is given in two bf16 parts (2^-16), the second
+// a product more.
 #include <cuda_fp8.h>
 
 #include <algorithm>
@@ -35,6 +37,7 @@
 namespace dcl {
 namespace {
 
+constexpr int KA_START = 3;   // units of keys that beginning an item takes
 constexpr int KA_CTAS = 2;    // CTAs of an SM: one loads while the other begins or ends an item
 constexpr int KA_MOST = 304;  // most CTAs of a launch
 
@@ -200,7 +203,7 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
   const uint32_t ring = smem_addr(smem) + warp * C::RING_B;
   float2* ml = reinterpret_cast<float2*>(smem + C::ML);
 
-  const KaLine<C::ROWS> line(kv, a);
+  const KaLine<C::ROWS, KA_START> line(kv, a);
 
   // ---- this CTA's part of the line of all items
   KaWalk& shared_walk = *reinterpret_cast<KaWalk*>(smem + C::HEAD);
@@ -329,7 +332,7 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
     }
     const uint32_t qs_addr = smem_addr(smem) + C::QF + lane * 16;
 
-    float o[MT][NT][4], m[2 * MT], l[2 * MT];
+    float o[MT][NT][4], m[2 * MT], l[2 * MT], l_r[FP8 ? 2 * MT : 1];
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -340,6 +343,7 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
     for (int i = 0; i < 2 * MT; ++i) {
       m[i] = -INFINITY;
       l[i] = 0.f;
+      if (FP8) l_r[FP8 ? i : 0] = 0.f;
     }
 
     int cur = 0;
@@ -431,8 +435,9 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
               for (int k = 0; k < 2; ++k)
                 if (key + 8 * j + 2 * place + k >= lim[i] || (skip >> (j >> 1) & 1)) s[i >> 1][j][2 * (i & 1) + k] = -INFINITY;
         }
-        // The reference m of a row moves only when a score passes it by more than 8 (P <= 2^8), so that
-        // most steps neither exchange maxima nor scale O.
+        // The reference m of a row, 7 below its largest score when it is taken, moves only when a score passes
+        // it by more than 15 (P <= 2^15), so that most steps neither exchange maxima nor scale O; P fills
+        // fp16's range, for the sake of small ones that carry large values.
         bool grew = false;
         float top[2 * MT];
 #pragma unroll
@@ -441,16 +446,17 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
 #pragma unroll
           for (int j = 0; j < NK; ++j)
             top[i] = fmaxf(top[i], fmaxf(s[i >> 1][j][2 * (i & 1)], s[i >> 1][j][2 * (i & 1) + 1]));
-          grew |= top[i] > m[i] + 8.f;
+          grew |= top[i] > m[i] + 15.f;
         }
         if (__any_sync(0xffffffffu, grew)) {
 #pragma unroll
           for (int i = 0; i < 2 * MT; ++i) {
             top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
             top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
-            const float mn = fmaxf(m[i], top[i]), alpha = exp2_fast(m[i] - (mn == -INFINITY ? 0.f : mn));
+            const float mn = fmaxf(m[i], top[i] - 7.f), alpha = exp2_fast(m[i] - (mn == -INFINITY ? 0.f : mn));
             m[i] = mn;
             l[i] *= alpha;
+            if (FP8) l_r[FP8 ? i : 0] *= alpha;
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
               o[i >> 1][j][2 * (i & 1)] *= alpha;
@@ -465,13 +471,15 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
 #pragma unroll
           for (int j = 0; j < NK; ++j) {
             const float x0 = exp2_fast(s[i >> 1][j][2 * (i & 1)] - ref), x1 = exp2_fast(s[i >> 1][j][2 * (i & 1) + 1] - ref);
+            const uint32_t hi = FP8 ? pack_f16x2(x0, x1) : pack_bf16x2(x0, x1);
             if (FP8) {
               const float2 vi = lds_f2(sc + 4 * (2 * KT + 8 * j + 2 * place));
+              const float2 q = __half22float2(*reinterpret_cast<const __half2*>(&hi));
               l[i] = fmaf(x1, vi.y, fmaf(x0, vi.x, l[i]));
+              l_r[FP8 ? i : 0] = fmaf(q.y, vi.y, fmaf(q.x, vi.x, l_r[FP8 ? i : 0]));
             } else {
               l[i] += x0 + x1;
             }
-            const uint32_t hi = FP8 ? pack_f16x2(x0, x1) : pack_bf16x2(x0, x1);
             p[j >> 1][i >> 1][2 * (j & 1) + (i & 1)] = hi;
             if (!FP8) p_lo[FP8 ? 0 : j >> 1][i >> 1][2 * (j & 1) + (i & 1)] = pack_bf16x2(x0 - bf16_lo(hi), x1 - bf16_hi(hi));
           }
@@ -571,6 +579,17 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
       l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
       l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
       if (place == 0) ml[warp * C::ROWS + 8 * i + quad] = make_float2(m[i], l[i]);
+      if (FP8) {
+        float& r = l_r[FP8 ? i : 0];
+        r += __shfl_xor_sync(0xffffffffu, r, 1);
+        r += __shfl_xor_sync(0xffffffffu, r, 2);
+        const float right = r != 0.f ? l[i] / r : 1.f;
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          o[i >> 1][j][2 * (i & 1)] *= right;
+          o[i >> 1][j][2 * (i & 1) + 1] *= right;
+        }
+      }
     }
     if (key0 + KT * warp < stop) {
       float* mine = reinterpret_cast<float*>(smem + warp * C::RING_B);

@@ -2,27 +2,27 @@
 // tensor cores: the rows of an item (up to 256: new positions x the query heads of one kv head)
 // fill one or two tiles of 128, and one pass over the keys serves them all.
 //
-// Per unit of 128 keys: S = Q K^T into TMEM, P = exp2(S scaled + e - m) in fp16 through shared memory,
-// O += P V in TMEM.  P, m, l and the exponents e of the values are those of kv_attention.cu; a
-// thread owns a row, so its statistics need no exchange.
+// Per unit of 128 keys: S = Q K^T into TMEM; P = exp2(S scaled + e - m) takes the place of its scores
+// there, as fp16 and a second fp16 part of what that lacks (2^-22 of P, two products: in one part
+// P's rounding is 2^-11, an eighth of the output's); O += P V in TMEM.  P, m, l and the exponents e of
+// the values are those of kv_attention.cu; a thread owns a row, so its statistics need no exchange.
 //
-// FP8 pages.  Four warps copy codes into shared memory (16-byte asynchronous copies, one unit
-// ahead) and widen them into the fp16 operand tiles: keys times 2^(e_j - e_max), e_max the unit's
-// largest exponent (a key more than 2^15 below the unit's largest loses low bits that its scores,
-// so much smaller, do not show), values as they are (e_j enters P).  bf16 pages: keys are copied
-// straight into their tile and multiplied in bf16; a value is scaled by the power of two of its
-// largest component into fp16, in place (exact but for components below 2^-14 of that one).
+// FP8 pages.  Eight warps copy codes into shared memory (16-byte asynchronous copies, one unit
+// ahead) and widen them into the fp16 operand tiles, each code times 2^(e_j - e_max + 6) with e_max
+// the largest exponent of the 32 keys that the warp has: that fills fp16 (448 * 2^6 = 28672), and is
+// exact but for a vector more than 2^21 below the largest of the 32, which loses low bits.  What is
+// left of the exponents is one number for 32 columns of S, so that the rows' loop loads none (an
+// exponent for every column cost it half its time).  bf16 pages: keys are copied straight into
+// their tile and multiplied in bf16; values are scaled into fp16 in place, the largest component of
+// 32 vectors to 2^14 .. 2^15 (bf16's 8 bits are kept by components down to 2^-31 of that one).
 // V's tile is [key][hd], the transposed ("MN-major") form of the B operand, as it comes.
 //
-// The reference m moves only when a score passes it by more than 8: a pass over a unit takes m as it
-// is, and is repeated with a larger one if a row's maximum shows that (the scores are still in
-// TMEM); O is scaled then.  A unit's first pass is nearly always its last.
+// The reference m, 7 below a row's largest score when it is taken, moves only when a unit's passes it by
+// more than 15; O is scaled then.
 //
-// What bounds it: shared memory, per unit of two tiles 256 KB of operand reads, 64 KB of P, and for
-// FP8 96 KB of widening (about 3500 cycles), against 2200 of tensor time.
-//
-// Roles (512 threads): warps 0-3 copy and widen; warp 4 allocates TMEM and issues the MMAs; warps
-// 8-11 and 12-15 have the rows of the two tiles.  Every wait is bounded (DERR_WAIT_TIMEOUT).
+// Roles (544 threads): warps 0-3 and 4-7 have the rows of the two tiles; warps 8-11 copy and widen
+// keys, 12-15 values (one group for both was the slowest link: 7800 cycles a unit); warp 16
+// allocates TMEM and issues the MMAs.  Every wait is bounded (DERR_WAIT_TIMEOUT).
 #include <cuda_fp8.h>
 
 #include <algorithm>
@@ -37,28 +37,35 @@ namespace dcl {
 namespace {
 
 constexpr int TC_ROWS = 256;      // rows of an item
-constexpr int TC_THREADS = 512;
+constexpr int TC_START = 6;       // units of keys that beginning an item takes
+constexpr int TC_THREADS = 544;
 constexpr int TC_BOX = 128 * 128; // 128 rows of 128 bytes, swizzled
-constexpr int TC_JOIN = 64;       // rows joined at a time
+constexpr int TC_JOIN = 8000;     // rows x parts joined at a time
 
 template <int HD, bool FP8>
 struct TcCfg {
   static constexpr int KB = HD / 64;                  // boxes along hd
   static constexpr int TILE = KB * TC_BOX;            // 128 rows of q, keys or values, 16 bits each
-  static constexpr int NS = FP8 ? 2 : 3;              // operand tiles of keys and values, in turn
-  static constexpr int P = 2 * TILE;                  // after q: P of two tiles [128][128 keys]
-  static constexpr int KV = P + 4 * TC_BOX;
-  static constexpr int RAW = KV + NS * TILE;          // FP8: codes of a unit's keys, then of its values
-  static constexpr int EXP = RAW + (FP8 ? 2 * 128 * HD : 0);  // [2 units][e, 2^-e][128] floats
-  static constexpr int SCALE = EXP + 2 * 2 * 128 * 4; // [2 units] 2^e_max
-  static constexpr int BAR = SCALE + 8;
+  static constexpr int NS = FP8 ? 2 : 4;              // operand tiles of keys and values, in turn
+  static constexpr int KV = 2 * TILE;                 // (q comes first)
+  static constexpr int RAW = KV + NS * TILE;          // FP8: codes, [2 units][keys, values]
+  static constexpr int RAW_UNIT = 2 * 128 * HD;
+  static constexpr int EXP = RAW + (FP8 ? 2 * RAW_UNIT : 0);  // [4 units][4 x 32 keys] of KeyScale (keys may be two units ahead)
+  static constexpr int BAR = EXP + 4 * 4 * 16;
   static constexpr int NBARS = 2 * NS + 4 * 2 + 1;
   static constexpr int HOLDER = BAR + 8 * NBARS;      // TMEM address, abort flag
   static constexpr int WALK = HOLDER + 8;
   static constexpr int TODO = WALK + (int)sizeof(KaWalk);
   static constexpr size_t SMEM = TODO + 3 * sizeof(KaJoin);
   static_assert(SMEM <= 232448, "shared memory per CTA");
-  static_assert(TC_JOIN * 152 * 8 + TC_JOIN * 8 <= KV, "a join's weights take the place of q and P");
+  static_assert(TC_JOIN * 8 + TC_ROWS * 8 <= EXP, "a join's weights take the place of the operands");
+};
+
+// Of 32 keys: the power of two that their scores lack, the exponent e that their values lack and 2^-e, and
+// a bit for each key that is there.
+struct KeyScale {
+  float key, e, inv;
+  uint32_t there;
 };
 
 // Descriptor of a [key][hd] tile as the transposed B operand: 128-byte rows of 64 components (the next
@@ -73,6 +80,22 @@ __device__ __forceinline__ uint64_t sw128_desc_mn(uint32_t saddr) {
   return d;
 }
 constexpr uint32_t IDESC_B_MN = 1u << 16;
+__device__ __forceinline__ void tmem_st32u(uint32_t taddr, const uint32_t (&v)[32]) {
+  float f[32];
+#pragma unroll
+  for (int i = 0; i < 32; ++i) f[i] = __uint_as_float(v[i]);
+  tmem_st32(taddr, f);
+}
+
+// D += A B with A (fp16 pairs) in TMEM.
+__device__ __forceinline__ void umma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}\n" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
 
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
@@ -119,10 +142,10 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::HOLDER + 4);
   KaWalk& shared_walk = *reinterpret_cast<KaWalk*>(smem + C::WALK);
   KaJoin* todo = reinterpret_cast<KaJoin*>(smem + C::TODO);
-  const KaLine<TC_ROWS> line(kv, a);
+  const KaLine<TC_ROWS, TC_START> line(kv, a);
 
   if (warp == 0) line.begin(&shared_walk, err);
-  if (warp == 4) {
+  if (warp == 16) {
     if (lane == 0) {
       for (int s = 0; s < C::NS; ++s) {
         mbar_init(full0 + 8 * s, 4);   // the copying warps
@@ -157,230 +180,167 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     if (lane == 0) report_error(err, DERR_WAIT_TIMEOUT);
   };
 
-  if (warp < 4) {
+  if (warp >= 8 && warp < 16) {
     // ================================================================ copies, widening
-    // A unit's keys: lane l knows of keys 4 l .. 4 l + 3 (their page and exponents); this warp copies
-    // groups 2 warp and 2 warp + 1 of 16 keys.  Chunks of 16 bytes: K's and V's alike.
+    // Keys or values of a unit: warp w of the four has keys 32 w .. 32 w + 31, lane l knows of key 32 w + l
+    // (its page and exponents); they are copied in chunks of 16 bytes.
+    const int values = warp >= 12, w4 = warp & 3;
     constexpr int CH = FP8 ? HD / 16 : HD / 8;       // chunks of a vector
-    constexpr int PER = 16 * CH / 32;                // of a group, per lane
-    const int shift = kv.page_shift, P = kv.page_len();
-    uint32_t seq = 0;  // operand tiles so far (keys and values in turn): stage seq % NS
+    constexpr int PK = CH / 4;                       // this lane's of a key: key (lane >> 2) + 8 i, chunk (lane & 3) + 4 j
+    const int shift = kv.page_shift, P = kv.page_len(), at_key = 32 * w4 + (lane >> 2), at_chunk = lane & 3;
+    const void* pool = values ? kv.v : kv.k;
+    auto raw_of = [&](int unit) { return base + C::RAW + (unit & 1) * C::RAW_UNIT + values * (128 * HD); };
+    uint32_t seq = values;  // operand tiles (keys and values in turn): stage seq % NS
     bool ok = true;
-    // (lane -> key and chunk of a group: eight lanes store into two rows of one box)
-    auto key_of = [&](int i) { return (lane >> 2) + 8 * (i / (CH / 4)); };
-    auto chunk_of = [&](int i) { return (lane & 3) + 4 * (i % (CH / 4)); };
+    // (codes: eight lanes read two keys, whose chunks lie in each other's halves of 128 bytes)
+    auto raw_at = [&](int k, int c) { return (uint32_t)(k * CH + (CH == 8 ? c ^ (4 * (k & 1)) : c)) * 16; };
+    auto tile_at = [&](int k, int c) { return (uint32_t)(c >> 3) * TC_BOX + swz(k, c & 7); };  // 16-bit elements
+    auto stage_of = [&](uint32_t s) { return base + C::KV + (s % C::NS) * C::TILE; };
+    auto wait_empty = [&](uint32_t s) { return wait(empty0 + 8 * (s % C::NS), ((s / C::NS) & 1u) ^ 1u); };
     while (ok && line.next(walk, it)) {
-      const int stop = min(it.len, it.until * KA_UNIT), n = it.until - it.from, key0 = it.from * KA_UNIT;
+      const int stop = min(it.len, it.until * KA_UNIT), n = it.until - it.from, first = it.from * KA_UNIT + 32 * w4;
       const int* table = a.table + (int64_t)it.b * a.max_pages;
-      auto page_at = [&](int unit) {  // of this lane's keys; negative: no key of them is to be read
-        const int key = key0 + unit * KA_UNIT + 4 * lane;
+      auto page_at = [&](int unit) {  // of this lane's key; negative: it is not to be read
+        const int key = first + unit * KA_UNIT + lane;
         if (unit >= n || key >= stop) return -1;
         const int page = table[key >> shift];
-        if (page < 0 || page >= kv.pages) {
-          report_error(err, DERR_KV_RANGE);
-          return -1;
-        }
-        return page;
+        if (page >= 0 && page < kv.pages) return page;
+        report_error(err, DERR_KV_RANGE);
+        return -1;
       };
       auto vec_of = [&](int page, int key) { return kv.vector_of((page << shift) + (key & (P - 1)), it.g); };
-      // copies of this warp's groups of a unit into `dst` (K or V: what follows the pool's pointer)
-      auto issue = [&](int unit, int pages, const void* pool, uint32_t dst) {
+      auto issue = [&](int unit, int pages, uint32_t dst) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int gr = 2 * warp + h, page = __shfl_sync(0xffffffffu, pages, 4 * gr);
+        for (int h = 0; h < 2; ++h) {  // 16 keys of one page
+          const int page = __shfl_sync(0xffffffffu, pages, 16 * h);
           if (page < 0) continue;
-          const uint8_t* src = static_cast<const uint8_t*>(pool) + vec_of(page, key0 + unit * KA_UNIT + 16 * gr) * (CH * 16);
+          const uint8_t* src = static_cast<const uint8_t*>(pool) + vec_of(page, first + unit * KA_UNIT + 16 * h) * (CH * 16) +
+                               ((lane >> 2) * CH + at_chunk) * 16;
 #pragma unroll
-          for (int i = 0; i < PER; ++i) {
-            const int k = key_of(i), c = chunk_of(i);
-            const uint32_t to = FP8 ? dst + (uint32_t)((16 * gr + k) * CH + c) * 16
-                                    : dst + (uint32_t)(c >> 3) * TC_BOX + swz(16 * gr + k, c & 7);
-            copy16(to, src + (k * CH + c) * 16);
-          }
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < PK; ++j) {
+              const int k = at_key + 16 * h + 8 * i, c = at_chunk + 4 * j;
+              copy16(dst + (FP8 ? raw_at(k, c) : tile_at(k, c)), src + (8 * i * CH + 4 * j) * 16);
+            }
         }
         copy_commit();
       };
-      auto exps_at = [&](int unit, int page, const int8_t* exps) -> uint32_t {
-        if (!FP8 || page < 0) return 0;
-        return *reinterpret_cast<const uint32_t*>(exps + vec_of(page, key0 + unit * KA_UNIT + 4 * lane));
+      auto exp_at = [&](int unit, int page, const int8_t* exps) {
+        return FP8 && page >= 0 ? (int)exps[vec_of(page, first + unit * KA_UNIT + lane)] : -128;
       };
-      auto stage_of = [&](uint32_t s) { return base + C::KV + (s % C::NS) * C::TILE; };
-      auto wait_empty = [&](uint32_t s) { return wait(empty0 + 8 * (s % C::NS), ((s / C::NS) & 1u) ^ 1u); };
-      auto ready = [&](uint32_t s) {
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(full0 + 8 * (s % C::NS));
-      };
-      const uint32_t raw = base + C::RAW;
-      int pages = page_at(0), pages2 = page_at(1);
-      uint32_t ek = exps_at(0, pages, kv.k_exp), ev = exps_at(0, pages, kv.v_exp);
+      auto largest = [&](int e) { return __reduce_max_sync(0xffffffffu, e); };
+      int pages = page_at(0), pages2 = page_at(1), pages3 = FP8 ? page_at(2) : -1;
+      int ek = 0, ev = 0;  // (the keys' warps look up both)
       if (FP8) {
-        issue(0, pages, kv.k, raw);
-        issue(0, pages, kv.v, raw + 128 * HD);
-      } else {
-        ok = wait_empty(seq);
-        if (ok) issue(0, pages, kv.k, stage_of(seq));
-        if (ok) ok = wait_empty(seq + 1);
-        if (ok) issue(0, pages, kv.v, stage_of(seq + 1));
+        if (!values) ek = exp_at(0, pages, kv.k_exp);
+        ev = exp_at(0, pages, kv.v_exp);
       }
+      if (!FP8) ok = wait_empty(seq);
+      if (ok) issue(0, pages, FP8 ? raw_of(0) : stage_of(seq));
+      if (FP8) issue(1, pages2, raw_of(1));
       for (int u = 0; ok && u < n; ++u) {
-        const uint32_t blk = seq >> 1;
-        const int live = min(KA_UNIT, stop - key0 - u * KA_UNIT);  // keys of the unit
-        // (a key is there if it lies before `live` and its page is the cache's)
-        auto there = [&](int key) { return __shfl_sync(0xffffffffu, pages, key >> 2) >= 0 && key < live; };
-        const int next_page = pages2;
-        uint32_t next_ek = 0, next_ev = 0;
-        // ---- keys
-        copy_wait<1>();
+        const uint32_t dst = stage_of(seq), here = __ballot_sync(0xffffffffu, pages >= 0);
+        KeyScale* out = reinterpret_cast<KeyScale*>(smem + C::EXP) + ((seq >> 1) & 3) * 4 + w4;
+        copy_wait<FP8 ? 1 : 0>();
         __syncwarp();
         if (FP8) {
-          int top = -128;  // the largest exponent of the keys there
+          const uint32_t raw = raw_of(u);
+          const int top_k = largest(ek), top_v = largest(ev), top = values ? top_v : top_k;
+          const float mine = kv_pow2((values ? ev : ek) - top + 6);  // (0 exponents of keys that are not there: zeros below)
+          ok = wait_empty(seq);
+          if (!ok) break;
+          if (!values && lane == 0) *out = KeyScale{kv_pow2(top_k - 6), (float)(top_v - 6), kv_pow2(6 - top_v), here};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int k = at_key + 8 * i;
+            const __half2 f = __float2half2_rn(__shfl_sync(0xffffffffu, mine, k & 31));
+            const bool in = here >> (k & 31) & 1;
+            uint4 x[PK];
+#pragma unroll
+            for (int j = 0; j < PK; ++j) x[j] = lds128(raw + raw_at(k, at_chunk + 4 * j));
+#pragma unroll
+            for (int j = 0; j < PK; ++j) {
+              const uint32_t w[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
+              uint32_t y[8];
+#pragma unroll
+              for (int z = 0; z < 8; ++z) y[z] = in ? times(widen(w[z >> 1], z & 1), f) : 0u;
+              const int c = 2 * (at_chunk + 4 * j);
+              st_shared_v4(dst + tile_at(k, c), y[0], y[1], y[2], y[3]);
+              st_shared_v4(dst + tile_at(k, c + 1), y[4], y[5], y[6], y[7]);
+            }
+          }
+        } else if (!values) {
+          if (here != 0xffffffffu) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int j = 0; j < PK; ++j)
+                if (!(here >> ((at_key + 8 * i) & 31) & 1)) st_shared_v4(dst + tile_at(at_key + 8 * i, at_chunk + 4 * j), 0, 0, 0, 0);
+          }
+          if (lane == 0) {
+            out->key = 1.f;
+            out->there = here;
+          }
+        } else {
+          uint32_t top = 0;  // largest finite magnitude, as bf16 bits
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if (pages >= 0 && 4 * lane + i < live) top = max(top, (int)(int8_t)(ek >> (8 * i)));
-          top = __reduce_max_sync(0xffffffffu, top);
-          if (warp == 0) {
-            float e[4], inv[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const bool in = pages >= 0 && 4 * lane + i < live;
-              const int y = max(-126, (int)(int8_t)(ev >> (8 * i)));
-              e[i] = in ? (float)y : -INFINITY;
-              inv[i] = in ? kv_pow2(-y) : 0.f;
-            }
-            float4* to = reinterpret_cast<float4*>(smem + C::EXP + (blk & 1) * 1024) + lane;
-            to[0] = make_float4(e[0], e[1], e[2], e[3]);
-            to[32] = make_float4(inv[0], inv[1], inv[2], inv[3]);
-            if (lane == 0) *reinterpret_cast<float*>(smem + C::SCALE + 4 * (blk & 1)) = kv_pow2(top);
-          }
-          ok = wait_empty(seq);
-          if (!ok) break;
-          const uint32_t dst = stage_of(seq);
+            for (int j = 0; j < PK; ++j) {
+              const int k = at_key + 8 * i;
+              const uint4 x = here >> (k & 31) & 1 ? lds128(dst + tile_at(k, at_chunk + 4 * j)) : make_uint4(0, 0, 0, 0);
+              const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            uint4 x[PER];
-#pragma unroll
-            for (int i = 0; i < PER; ++i) x[i] = lds128(raw + (uint32_t)((32 * warp + 16 * h + key_of(i)) * CH + chunk_of(i)) * 16);
-#pragma unroll
-            for (int i = 0; i < PER; ++i) {
-              const int k = 32 * warp + 16 * h + key_of(i), c = chunk_of(i);
-              const int e = (int)(int8_t)(__shfl_sync(0xffffffffu, ek, k >> 2) >> (8 * (k & 3)));
-              const bool in = there(k);
-              const __half2 f = __float2half2_rn(in ? kv_pow2(e - top) : 0.f);
-              const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-              uint32_t y[8];
-#pragma unroll
-              for (int j = 0; j < 8; ++j) y[j] = in ? times(widen(w[j >> 1], j & 1), f) : 0u;
-              const uint32_t row = dst + (uint32_t)(c >> 2) * TC_BOX;
-              st_shared_v4(row + swz(k, 2 * (c & 3)), y[0], y[1], y[2], y[3]);
-              st_shared_v4(row + swz(k, 2 * (c & 3) + 1), y[4], y[5], y[6], y[7]);
-            }
-          }
-        } else {
-          const uint32_t dst = stage_of(seq);
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int i = 0; i < PER; ++i) {
-              const int k = 32 * warp + 16 * h + key_of(i), c = chunk_of(i);
-              if (!there(k)) st_shared_v4(dst + (uint32_t)(c >> 3) * TC_BOX + swz(k, c & 7), 0, 0, 0, 0);
-            }
-        }
-        ready(seq);
-        if (FP8) {
-          next_ek = exps_at(u + 1, next_page, kv.k_exp);
-          next_ev = exps_at(u + 1, next_page, kv.v_exp);
-          issue(u + 1, u + 1 < n ? next_page : -1, kv.k, raw);
-        } else {
-          if (u + 1 < n) ok = wait_empty(seq + 2);
-          if (!ok) break;
-          issue(u + 1, u + 1 < n ? next_page : -1, kv.k, stage_of(seq + 2));
-        }
-        ++seq;
-        // ---- values
-        copy_wait<1>();
-        __syncwarp();
-        if (FP8) {
-          ok = wait_empty(seq);
-          if (!ok) break;
-          const uint32_t dst = stage_of(seq);
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            uint4 x[PER];
-#pragma unroll
-            for (int i = 0; i < PER; ++i)
-              x[i] = lds128(raw + 128 * HD + (uint32_t)((32 * warp + 16 * h + key_of(i)) * CH + chunk_of(i)) * 16);
-#pragma unroll
-            for (int i = 0; i < PER; ++i) {
-              const int k = 32 * warp + 16 * h + key_of(i), c = chunk_of(i);
-              const bool in = there(k);
-              const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-              uint32_t y[8];
-#pragma unroll
-              for (int j = 0; j < 8; ++j) y[j] = in ? widen(w[j >> 1], j & 1) : 0u;
-              const uint32_t row = dst + (uint32_t)(c >> 2) * TC_BOX;
-              st_shared_v4(row + swz(k, 2 * (c & 3)), y[0], y[1], y[2], y[3]);
-              st_shared_v4(row + swz(k, 2 * (c & 3) + 1), y[4], y[5], y[6], y[7]);
-            }
-          }
-        } else {
-          const uint32_t dst = stage_of(seq);
-          constexpr int PK = CH / 4;  // this lane's chunks of a key
-#pragma unroll
-          for (int h = 0; h < 4; ++h) {  // eight keys at a time: key (lane >> 2) + 8 h of the warp's 32
-            const int k = 32 * warp + 8 * h + (lane >> 2);
-            const bool in = there(k);
-            uint4 x[PK];
-            uint32_t top = 0;
-#pragma unroll
-            for (int i = 0; i < PK; ++i) {
-              const int c = (lane & 3) + 4 * i;
-              x[i] = in ? lds128(dst + (uint32_t)(c >> 3) * TC_BOX + swz(k, c & 7)) : make_uint4(0, 0, 0, 0);
-              const uint32_t* w = &x[i].x;
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                const uint32_t lo = w[j] & 0x7fffu, hi = (w[j] >> 16) & 0x7fffu;
+              for (int z = 0; z < 4; ++z) {
+                const uint32_t lo = w[z] & 0x7fffu, hi = (w[z] >> 16) & 0x7fffu;
                 top = max(top, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
               }
             }
-            top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            const int e = top ? max(-100, min(126, (int)(top >> 7) - 127)) : 0;
-            const float f = kv_pow2(-e);
+          top = __reduce_max_sync(0xffffffffu, top);
+          const int e = top ? max(-100, (int)(top >> 7) - 127 - 14) : 0;
+          const float f = kv_pow2(-e);
 #pragma unroll
-            for (int i = 0; i < PK; ++i) {
-              const int c = (lane & 3) + 4 * i;
-              uint32_t* w = &x[i].x;
+          for (int i = 0; i < 4; ++i)
 #pragma unroll
-              for (int j = 0; j < 4; ++j) w[j] = pack_f16x2(bf16_lo(w[j]) * f, bf16_hi(w[j]) * f);
-              st_shared_v4(dst + (uint32_t)(c >> 3) * TC_BOX + swz(k, c & 7), w[0], w[1], w[2], w[3]);
+            for (int j = 0; j < PK; ++j) {
+              const int k = at_key + 8 * i;
+              const uint32_t at = dst + tile_at(k, at_chunk + 4 * j);
+              const uint4 x = here >> (k & 31) & 1 ? lds128(at) : make_uint4(0, 0, 0, 0);
+              uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+              for (int z = 0; z < 4; ++z) w[z] = pack_f16x2(bf16_lo(w[z]) * f, bf16_hi(w[z]) * f);
+              st_shared_v4(at, w[0], w[1], w[2], w[3]);
             }
-            if ((lane & 3) == 0) {
-              float* to = reinterpret_cast<float*>(smem + C::EXP + (blk & 1) * 1024) + k;
-              to[0] = in ? (float)e : -INFINITY;
-              to[128] = in ? f : 0.f;
-            }
+          if (lane == 0) {
+            out->e = (float)e;
+            out->inv = f;
           }
         }
-        ready(seq);
-        if (FP8) {
-          issue(u + 1, u + 1 < n ? next_page : -1, kv.v, raw + 128 * HD);
-        } else {
-          if (u + 1 < n) ok = wait_empty(seq + 2);
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(full0 + 8 * (seq % C::NS));
+        seq += 2;
+        if (FP8) {  // (nothing, past the end)
+          issue(u + 2, pages3, raw_of(u));
+          if (!values) ek = exp_at(u + 1, pages2, kv.k_exp);
+          ev = exp_at(u + 1, pages2, kv.v_exp);
+          pages = pages2;
+          pages2 = pages3;
+          pages3 = page_at(u + 3);
+        } else if (u + 1 < n) {
+          ok = wait_empty(seq);
           if (!ok) break;
-          issue(u + 1, u + 1 < n ? next_page : -1, kv.v, stage_of(seq + 2));
+          issue(u + 1, pages2, stage_of(seq));
+          pages = pages2;
+          pages2 = page_at(u + 2);
         }
-        ++seq;
-        pages = next_page;
-        ek = next_ek;
-        ev = next_ev;
-        pages2 = page_at(u + 2);
       }
       copy_wait<0>();
     }
     copy_wait<0>();
     if (!ok) gave_up();
-  } else if (warp == 4) {
+  } else if (warp == 16) {
     // ================================================================ MMAs
     constexpr uint32_t idesc_s = FP8 ? make_idesc_f16(128, 128) : make_idesc(128, 128);
     constexpr uint32_t idesc_o = make_idesc_f16(128, HD) | IDESC_B_MN;
@@ -416,12 +376,14 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
           if (!ok) break;
           ++count[t];
           tc_fence_after();
-          const uint64_t dp = sw128_desc(base + C::P + t * 2 * TC_BOX), dv = sw128_desc_mn(tile_at(seq + 1));
+          const uint64_t dv = sw128_desc_mn(tile_at(seq + 1));
           if (leader) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-              umma_bf16(tmem + 256u + (uint32_t)(HD * t), dp + (k >> 2) * (TC_BOX >> 4) + 2 * (k & 3), dv + k * (2048 >> 4),
-                        idesc_o, (u > 0 || k > 0) ? 1u : 0u);
+            for (int k = 0; k < 8; ++k)  // P stands where its scores were: per 32 keys 16 columns of it, 16 of its rest
+#pragma unroll
+              for (int part = 0; part < 2; ++part)
+                umma_f16_ts(tmem + 256u + (uint32_t)(HD * t), tmem + 128u * t + 32 * (k >> 1) + 16 * part + 8 * (k & 1),
+                            dv + k * (2048 >> 4), idesc_o, (u > 0 || k > 0 || part > 0) ? 1u : 0u);
             umma_commit(p_empty0 + 8 * t);
             if (t + 1 == tiles) umma_commit(empty0 + 8 * ((seq + 1) % C::NS));
           }
@@ -439,12 +401,11 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     __syncwarp();
     volatile int no_abort = 0;
     mbar_wait(drain, 0, &no_abort);
-  } else if (warp >= 8) {
+  } else {
     // ================================================================ rows
-    const int t = (warp - 8) >> 2, quarter = warp & 3, r = 32 * quarter + lane;  // row r of tile t
+    const int t = warp >> 2, quarter = warp & 3, r = 32 * quarter + lane;  // row r of tile t
     const uint32_t s_at = tmem + 128u * t + ((uint32_t)(32 * quarter) << 16);
     const uint32_t o_at = tmem + 256u + (uint32_t)(HD * t) + ((uint32_t)(32 * quarter) << 16);
-    const uint32_t p_row = base + C::P + t * 2 * TC_BOX;
     auto rows_bar = [] { asm volatile("bar.sync 1, 256;" ::: "memory"); };
     uint32_t count = 0, seq = 0;
     // After a wait that ran out a warp goes on through the items without work: the barrier of the rows'
@@ -463,33 +424,42 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
       const bool live = row < it.rows, band = 128 * t + 32 * quarter < it.rows;
       const int rr = it.first + row, tok = rr / rep, h = it.g * rep + rr - tok * rep;
       float qa = a.scale * kLog2e;
-      // ---- q: this thread's row into its tile
+      // ---- q: the band's rows into their tile, 16-byte chunks of a row by neighbouring lanes
       if (ok && t < tiles) {
-        const uint4* src = reinterpret_cast<const uint4*>(a.q + (it.row0 + tok) * a.q_stride + (int64_t)h * HD);
-        uint4 x[HD / 8];
+        constexpr int CPR = HD / 8, RPL = 32 / CPR, HALF = 16 / RPL;  // chunks of a row, rows of a load, loads in flight
+        const int c = lane % CPR;
+        int e_row = 0;  // exponent of this thread's row
+#pragma unroll 1
+        for (int i0 = 0; i0 < 2 * HALF; i0 += HALF) {
+          uint4 x[HALF];
 #pragma unroll
-        for (int c = 0; c < HD / 8; ++c) x[c] = live ? src[c] : make_uint4(0, 0, 0, 0);
-        if (FP8) {
-          float top = 0.f;
-#pragma unroll
-          for (int c = 0; c < HD / 8; ++c) {
-            const uint32_t* w = &x[c].x;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) top = fmaxf(top, fmaxf(fabsf(bf16_lo(w[j])), fabsf(bf16_hi(w[j]))));
+          for (int i = 0; i < HALF; ++i) {
+            const int rb = 32 * quarter + RPL * (i0 + i) + lane / CPR, q = it.first + 128 * t + rb, tk = q / rep;
+            x[i] = make_uint4(0, 0, 0, 0);
+            if (128 * t + rb < it.rows)
+              x[i] = *reinterpret_cast<const uint4*>(a.q + (it.row0 + tk) * a.q_stride + (int64_t)(it.g * rep + q - tk * rep) * HD + 8 * c);
           }
-          const int e = max(-120, min(120, (int)(__float_as_uint(top) >> 23) - 127));
-          const float down = kv_pow2(-e);
-          qa *= kv_pow2(e);
 #pragma unroll
-          for (int c = 0; c < HD / 8; ++c) {
-            uint32_t* w = &x[c].x;
+          for (int i = 0; i < HALF; ++i) {
+            uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+            if (FP8) {
+              float top = 0.f;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) w[j] = pack_f16x2(bf16_lo(w[j]) * down, bf16_hi(w[j]) * down);
+              for (int j = 0; j < 4; ++j) top = fmaxf(top, fmaxf(fabsf(bf16_lo(w[j])), fabsf(bf16_hi(w[j]))));
+#pragma unroll
+              for (int d = CPR / 2; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+              const int e = max(-120, min(120, (int)(__float_as_uint(top) >> 23) - 127));
+              const float down = kv_pow2(-e);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) w[j] = pack_f16x2(bf16_lo(w[j]) * down, bf16_hi(w[j]) * down);
+              const int own = __shfl_sync(0xffffffffu, e, (lane % RPL) * CPR);
+              if (lane / RPL == i0 + i) e_row = own;
+            }
+            st_shared_v4(base + t * C::TILE + (uint32_t)(c >> 3) * TC_BOX + swz(32 * quarter + RPL * (i0 + i) + lane / CPR, c & 7),
+                         w[0], w[1], w[2], w[3]);
           }
         }
-#pragma unroll
-        for (int c = 0; c < HD / 8; ++c)
-          st_shared_v4(base + t * C::TILE + (uint32_t)(c >> 3) * TC_BOX + swz(r, c & 7), x[c].x, x[c].y, x[c].z, x[c].w);
+        if (FP8) qa *= kv_pow2(e_row);
         fence_proxy_async_smem();
         tc_fence_before();
         __syncwarp();
@@ -503,48 +473,42 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
         if (!row_wait(s_full0 + 8 * t, count & 1u)) break;
         // (bf16: the values' exponents come with their tile)
         if (!FP8 && !row_wait(full0 + 8 * ((seq + 1) % C::NS), ((seq + 1) / C::NS) & 1u)) break;
-        if (u > 0 && !row_wait(p_empty0 + 8 * t, (count & 1u) ^ 1u)) break;  // P and O of the unit before are done with
         tc_fence_after();
         if (band) {
-          const uint32_t exps = base + C::EXP + (blk & 1) * 1024;
-          const float qf = FP8 ? qa * *reinterpret_cast<volatile float*>(smem + C::SCALE + 4 * (blk & 1)) : qa;
-          float sum;
-          for (;;) {
-            const float ref = m == -INFINITY ? 0.f : m;
-            float top = -INFINITY;
-            sum = 0.f;
+          const uint32_t scales = base + C::EXP + (blk & 3) * 64;
+          uint32_t s[32], ahead[32];  // 32 scores, and the next ones
+          // ---- the row's largest score
+          float top = -INFINITY;
+          tmem_ld32(s_at, ahead);
 #pragma unroll 1
-            for (int c = 0; c < 4; ++c) {
-              uint32_t s[32];
-              tmem_ld32(s_at + 32 * c, s);
-              tmem_ld_wait();
-              uint32_t w[16];
+          for (int c = 0; c < 4; ++c) {
+            const float4 scale = ld_shared_v4(scales + 16 * c);
+            const uint32_t there = __float_as_uint(scale.w);
+            tmem_ld_wait();
 #pragma unroll
-              for (int i = 0; i < 32; i += 4) {
-                const float4 e = ld_shared_v4(exps + 4 * (32 * c + i)), f = ld_shared_v4(exps + 512 + 4 * (32 * c + i));
-                const float x0 = fmaf(f32(s[i]), qf, e.x) - ref, x1 = fmaf(f32(s[i + 1]), qf, e.y) - ref;
-                const float x2 = fmaf(f32(s[i + 2]), qf, e.z) - ref, x3 = fmaf(f32(s[i + 3]), qf, e.w) - ref;
-                top = fmaxf(top, fmaxf(fmaxf(x0, x1), fmaxf(x2, x3)));
-                const float p0 = ex2_approx(x0), p1 = ex2_approx(x1), p2 = ex2_approx(x2), p3 = ex2_approx(x3);
-                sum = fmaf(p0, f.x, sum);
-                sum = fmaf(p1, f.y, sum);
-                sum = fmaf(p2, f.z, sum);
-                sum = fmaf(p3, f.w, sum);
-                w[i / 2] = pack_f16x2(p0, p1);
-                w[i / 2 + 1] = pack_f16x2(p2, p3);
-              }
+            for (int i = 0; i < 32; ++i) s[i] = ahead[i];
+            if (c < 3) tmem_ld32(s_at + 32 * (c + 1), ahead);
+            if (there != 0xffffffffu) {
 #pragma unroll
-              for (int k = 0; k < 4; ++k)
-                st_shared_v4(p_row + (uint32_t)(c >> 1) * TC_BOX + swz(r, (c & 1) * 4 + k), w[4 * k], w[4 * k + 1], w[4 * k + 2],
-                             w[4 * k + 3]);
+              for (int i = 0; i < 32; ++i) s[i] = there >> i & 1 ? s[i] : 0xff800000u;
             }
-            // a larger reference where a row's maximum passes it by more than 8, or is its first
-            const bool grew = m == -INFINITY ? top > -INFINITY : top > 8.f;
-            if (!__any_sync(0xffffffffu, grew)) break;
-            const float mn = grew ? ref + top : m, alpha = grew ? (m == -INFINITY ? 0.f : ex2_approx(m - mn)) : 1.f;
+            float a0 = -INFINITY, a1 = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 32; i += 4) {
+              a0 = max3f(a0, f32(s[i]), f32(s[i + 1]));
+              a1 = max3f(a1, f32(s[i + 2]), f32(s[i + 3]));
+            }
+            top = fmaxf(top, fmaf(fmaxf(a0, a1), qa * scale.x, scale.y));
+          }
+          tmem_ld32(s_at, ahead);
+          // ---- a larger reference where that passes it by more than 15, or is the row's first
+          const bool grew = top > m + 15.f;
+          if (__any_sync(0xffffffffu, grew)) {
+            const float mn = grew ? top - 7.f : m, alpha = grew ? ex2_approx(m - mn) : 1.f;
             m = mn;
             l *= alpha;
-            if (u > 0) {
+            if (u > 0) {  // (the product before this unit's scores is done: they came after it)
+              tmem_ld_wait();
 #pragma unroll 1
               for (int c = 0; c < HD / 32; ++c) {
                 uint32_t o[32];
@@ -555,13 +519,47 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
                 for (int i = 0; i < 32; ++i) y[i] = f32(o[i]) * alpha;
                 tmem_st32(o_at + 32 * c, y);
               }
-              tmem_st_wait();
             }
           }
-          l += sum;
+          // ---- P, into the places of its scores: per 32 keys 16 columns of fp16 pairs, 16 of what they lack
+          const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll 1
+          for (int c = 0; c < 4; ++c) {
+            const float4 scale = ld_shared_v4(scales + 16 * c);
+            const uint32_t there = __float_as_uint(scale.w);
+            const float qf = qa * scale.x, add = scale.y - ref;
+            const unsigned long long qf2 = pk2(qf, qf), add2 = pk2(add, add);
+            unsigned long long sum2 = pk2(0.f, 0.f);
+            float x[32];
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 32; i += 2)  // (pairs: one instruction for two scores)
+              upk2(ffma2(pk2(f32(ahead[i]), f32(ahead[i + 1])), qf2, add2), x[i], x[i + 1]);
+            if (c < 3) tmem_ld32(s_at + 32 * (c + 1), ahead);
+            if (there != 0xffffffffu) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) x[i] = there >> i & 1 ? x[i] : -INFINITY;
+            }
+#pragma unroll
+            for (int i = 0; i < 32; i += 2) {
+              const float p0 = ex2_approx(x[i]), p1 = ex2_approx(x[i + 1]);
+              const unsigned long long p2 = pk2(p0, p1);
+              sum2 = fadd2(p2, sum2);
+              const uint32_t hi = pack_f16x2(p0, p1);
+              const float2 q = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+              float r0, r1;
+              upk2(fadd2(p2, pk2(-q.x, -q.y)), r0, r1);
+              s[i / 2] = hi;
+              s[16 + i / 2] = pack_f16x2(r0, r1);
+            }
+            tmem_st32u(s_at + 32 * c, s);
+            float lo, hi;
+            upk2(sum2, lo, hi);
+            l = fmaf(lo + hi, scale.z, l);
+          }
+          tmem_st_wait();
         }
         ++count;
-        fence_proxy_async_smem();
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(p_full0 + 8 * t);
@@ -593,7 +591,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
         int c0, c1;
         line.sharers(walk, it, c0, c1);
         rows_bar();
-        if (threadIdx.x == 256) {
+        if (threadIdx.x == 0) {
           __threadfence();  // (the rows' writes, which the barrier ordered before)
           const int done = atomicAdd(&scratch.count[c0], 1);
           if (done == c1 - c0) {  // the last to come joins the parts, when it is through with its own
@@ -604,23 +602,24 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
         }
       }
     }
-    rows_bar();
-    for (int i = 0; i < todo[0].rows; ++i) {
-      const KaJoin j = todo[1 + i];
-      for (int r0 = 0; r0 < j.rows; r0 += TC_JOIN) {
-        KaJoin k = j;
-        k.first += r0;
-        k.rows = min(TC_JOIN, j.rows - r0);
-        join_parts<HD, TC_ROWS, 256>(a, k, rep, scratch.part + (int64_t)r0 * (HD + 4), reinterpret_cast<float2*>(smem + TC_JOIN * 8),
-                                     reinterpret_cast<float2*>(smem), (int)threadIdx.x - 256, rows_bar);
-        rows_bar();
-      }
-    }
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp == 4) tmem_dealloc(tmem, 512);
+  if (warp == 16) tmem_dealloc(tmem, 512);
+  for (int i = 0; i < todo[0].rows; ++i) {
+    const KaJoin j = todo[1 + i];
+    const int some = min(TC_ROWS, TC_JOIN / j.parts);  // rows whose weights fit
+    for (int r0 = 0; r0 < j.rows; r0 += some) {
+      KaJoin k = j;
+      k.first += r0;
+      k.rows = min(some, j.rows - r0);
+      join_parts<HD, TC_ROWS, TC_THREADS>(a, k, rep, scratch.part + (int64_t)r0 * (HD + 4),
+                                          reinterpret_cast<float2*>(smem + TC_ROWS * 8), reinterpret_cast<float2*>(smem),
+                                          threadIdx.x, [] { __syncthreads(); });
+      __syncthreads();
+    }
+  }
 }
 
 template <int HD, bool FP8>

@@ -2,7 +2,7 @@
 //
 // An item is the rows of one row tile (new positions x the query heads of one kv head) of one
 // sequence; its keys come in units of 128.  All items of a launch stand in one line, each with
-// KA_START positions for its beginning and one for every unit; every CTA takes an equal part of the
+// a few positions for its beginning and one for every unit; every CTA takes an equal part of the
 // line, so that a long sequence is spread over many CTAs, many short ones share one, and none waits
 // for another's longer sequence.
 #pragma once
@@ -14,18 +14,22 @@ namespace dcl {
 namespace {
 
 constexpr int KA_UNIT = 128;  // keys of a unit of work
-constexpr int KA_START = 3;   // units that beginning an item takes
-// Sharing an item costs each of its CTAs the writing of a part and one of them the join (3 and 4 to
-// 20 thousand cycles; a unit of 16 rows takes about 1500).  So a cut that falls less than KA_LOW
-// positions after an item's beginning or KA_HIGH before its end goes there, and a CTA has at least
-// KA_LEAST positions where the launch is small.
-constexpr int KA_LOW = KA_START + 3, KA_HIGH = 4, KA_LEAST = 4;
-__device__ __forceinline__ int cut_at(int pos, int line) {
-  if (line < KA_LOW + KA_HIGH) return 2 * pos < line ? 0 : line;
-  return pos < KA_LOW ? 0 : pos > line - KA_HIGH ? line : pos;
-}
+// START: units that beginning an item takes.  Sharing an item costs each of its CTAs the writing of a
+// part and one of them the join (for up to 32 rows 3 and 4 to 20 thousand cycles; a unit of 16 rows
+// takes about 1500).  So a cut that falls less than START + 3 positions after an item's beginning or
+// START + 1 before its end goes there, and a CTA has at least KA_LEAST positions where the launch is
+// small.
+constexpr int KA_LEAST = 4;
+template <int START>
+struct KaCut {
+  static constexpr int LOW = START + 3, HIGH = START + 1;
+  static __device__ __forceinline__ int at(int pos, int line) {
+    if (line < LOW + HIGH) return 2 * pos < line ? 0 : line;
+    return pos < LOW ? 0 : pos > line - HIGH ? line : pos;
+  }
+};
 
-// The line in equal parts: CTA c of n has positions [start(c), start(c + 1)), each end moved as cut_at
+// The line in equal parts: CTA c of n has positions [start(c), start(c + 1)), each end moved as KaCut
 // says.
 struct KaShare {
   int64_t each;
@@ -52,9 +56,10 @@ struct KaShare {
 struct KaItem {
   int b, g, first, rows;  // its rows [first, first + rows) of the nq * rep of the sequence's kv head
   int row0, nq, len;      // the sequence's first row of q, its new positions, its cached ones
-  int from, until, line;  // units [from, until) of the line - KA_START there are
+  int from, until, units; // units [from, until) of those there are
+  int line;               // its positions
   int64_t item0;          // its first position
-  __device__ __forceinline__ bool whole() const { return from == 0 && until == line - KA_START; }
+  __device__ __forceinline__ bool whole() const { return from == 0 && until == units; }
 };
 // An item whose parts are all there: `parts` of them, from CTA c0 on.
 struct KaJoin {
@@ -66,7 +71,7 @@ struct KaWalk {
   int b;
 };
 
-template <int ROWS>  // of an item
+template <int ROWS, int START>  // rows of an item; positions for its beginning
 struct KaLine {
   const KvAttn& a;
   int G, rep, room;
@@ -79,7 +84,7 @@ struct KaLine {
   __device__ __forceinline__ int seq_len(int b) const { return min(max(a.lens[b], 0), room); }
   __device__ __forceinline__ int tiles_of(int nq) const { return (int)(((int64_t)nq * rep + ROWS - 1) / ROWS); }
   // (at least one unit: the rows of a sequence without keys are still written)
-  __device__ __forceinline__ int line_of(int len) const { return KA_START + max(1, (len + KA_UNIT - 1) / KA_UNIT); }
+  __device__ __forceinline__ int line_of(int len) const { return START + max(1, (len + KA_UNIT - 1) / KA_UNIT); }
 
   // This CTA's part (a warp; lane 0 writes it).
   __device__ __forceinline__ void begin(KaWalk* walk, int* err) const {
@@ -120,7 +125,7 @@ struct KaLine {
           const int line = line_of(seq_len(b));
           const int64_t in = u - before;
           const int pos = in < (1ll << 31) ? (int)in % line : (int)(in % line);
-          return u - pos + cut_at(pos, line);
+          return u - pos + KaCut<START>::at(pos, line);
         }
         before += __shfl_sync(0xffffffffu, upto, 31);
       }
@@ -154,9 +159,10 @@ struct KaLine {
       const int which = in < (1ll << 31) ? (int)in / line : (int)(in / line);
       it.item0 = w.before + (int64_t)which * line;
       it.line = line;
+      it.units = line - START;
       const int64_t upto = min(w.end, it.item0 + line);
-      it.from = max(0, (int)(w.u - it.item0) - KA_START);
-      it.until = (int)(upto - it.item0) - KA_START;
+      it.from = max(0, (int)(w.u - it.item0) - START);
+      it.until = (int)(upto - it.item0) - START;
       w.u = upto;
       if (it.until <= it.from) continue;  // (this part of the line holds the item's beginning only)
       it.g = which / nt;
@@ -169,8 +175,8 @@ struct KaLine {
   // The CTAs c0 .. c1 that share an item that is not whole.
   __device__ __forceinline__ void sharers(const KaWalk& w, const KaItem& it, int& c0, int& c1) const {
     const KaShare share(w.total, gridDim.x);
-    c0 = share.owner(it.item0 + KA_LOW - 1);
-    c1 = share.owner(it.item0 + it.line - KA_HIGH);
+    c0 = share.owner(it.item0 + KaCut<START>::LOW - 1);
+    c1 = share.owner(it.item0 + it.line - KaCut<START>::HIGH);
   }
 };
 
