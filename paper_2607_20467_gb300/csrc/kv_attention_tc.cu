@@ -2,10 +2,10 @@
 // tensor cores: the rows of an item (up to 256: new positions x the query heads of one kv head)
 // fill one or two tiles of 128, and one pass over the keys serves them all.
 //
-// Per unit of 128 keys: S = Q K^T into TMEM; P = exp2(S scaled + e - m) takes the place of its scores
-// there, as fp16 and a second fp16 part of what that lacks (2^-22 of P, two products: in one part
-// P's rounding is 2^-11, an eighth of the output's); O += P V in TMEM.  P, m, l and the exponents e of
-// the values are those of kv_attention.cu; a thread owns a row, so its statistics need no exchange.
+// Per unit of 128 keys: S = Q K^T into TMEM; P = exp2(S scaled + e - m) in fp16 takes the place of its
+// scores there; O += P V in TMEM.  P, m, l, the exponents e of the values and O's division by the sum of
+// the rounded P are those of kv_attention.cu; a thread owns a row, so its statistics need no
+// exchange.
 //
 // FP8 pages.  Eight warps copy codes into shared memory (16-byte asynchronous copies, one unit
 // ahead) and widen them into the fp16 operand tiles, each code times 2^(e_j - e_max + 6) with e_max
@@ -46,11 +46,10 @@ template <int HD, bool FP8>
 struct TcCfg {
   static constexpr int KB = HD / 64;                  // boxes along hd
   static constexpr int TILE = KB * TC_BOX;            // 128 rows of q, keys or values, 16 bits each
-  static constexpr int NS = FP8 ? 2 : 4;              // operand tiles of keys and values, in turn
+  static constexpr int NS = 4;                        // operand tiles of keys and values, in turn
   static constexpr int KV = 2 * TILE;                 // (q comes first)
-  static constexpr int RAW = KV + NS * TILE;          // FP8: codes, [2 units][keys, values]
-  static constexpr int RAW_UNIT = 2 * 128 * HD;
-  static constexpr int EXP = RAW + (FP8 ? 2 * RAW_UNIT : 0);  // [4 units][4 x 32 keys] of KeyScale (keys may be two units ahead)
+  static constexpr int RAW = KV + NS * TILE;          // FP8: codes of a unit's keys, then of its values
+  static constexpr int EXP = RAW + (FP8 ? 2 * 128 * HD : 0);  // [4 units][4 x 32 keys] of KeyScale (keys may be two units ahead)
   static constexpr int BAR = EXP + 4 * 4 * 16;
   static constexpr int NBARS = 2 * NS + 4 * 2 + 1;
   static constexpr int HOLDER = BAR + 8 * NBARS;      // TMEM address, abort flag
@@ -80,13 +79,14 @@ __device__ __forceinline__ uint64_t sw128_desc_mn(uint32_t saddr) {
   return d;
 }
 constexpr uint32_t IDESC_B_MN = 1u << 16;
-__device__ __forceinline__ void tmem_st32u(uint32_t taddr, const uint32_t (&v)[32]) {
-  float f[32];
-#pragma unroll
-  for (int i = 0; i < 32; ++i) f[i] = __uint_as_float(v[i]);
-  tmem_st32(taddr, f);
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
+      "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]),
+      "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+      : "memory");
 }
-
 // D += A B with A (fp16 pairs) in TMEM.
 __device__ __forceinline__ void umma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
@@ -189,7 +189,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     constexpr int PK = CH / 4;                       // this lane's of a key: key (lane >> 2) + 8 i, chunk (lane & 3) + 4 j
     const int shift = kv.page_shift, P = kv.page_len(), at_key = 32 * w4 + (lane >> 2), at_chunk = lane & 3;
     const void* pool = values ? kv.v : kv.k;
-    auto raw_of = [&](int unit) { return base + C::RAW + (unit & 1) * C::RAW_UNIT + values * (128 * HD); };
+    const uint32_t raw = base + C::RAW + values * (128 * HD);
     uint32_t seq = values;  // operand tiles (keys and values in turn): stage seq % NS
     bool ok = true;
     // (codes: eight lanes read two keys, whose chunks lie in each other's halves of 128 bytes)
@@ -230,22 +230,20 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
         return FP8 && page >= 0 ? (int)exps[vec_of(page, first + unit * KA_UNIT + lane)] : -128;
       };
       auto largest = [&](int e) { return __reduce_max_sync(0xffffffffu, e); };
-      int pages = page_at(0), pages2 = page_at(1), pages3 = FP8 ? page_at(2) : -1;
+      int pages = page_at(0), pages2 = page_at(1);
       int ek = 0, ev = 0;  // (the keys' warps look up both)
       if (FP8) {
         if (!values) ek = exp_at(0, pages, kv.k_exp);
         ev = exp_at(0, pages, kv.v_exp);
       }
       if (!FP8) ok = wait_empty(seq);
-      if (ok) issue(0, pages, FP8 ? raw_of(0) : stage_of(seq));
-      if (FP8) issue(1, pages2, raw_of(1));
+      if (ok) issue(0, pages, FP8 ? raw : stage_of(seq));
       for (int u = 0; ok && u < n; ++u) {
         const uint32_t dst = stage_of(seq), here = __ballot_sync(0xffffffffu, pages >= 0);
         KeyScale* out = reinterpret_cast<KeyScale*>(smem + C::EXP) + ((seq >> 1) & 3) * 4 + w4;
-        copy_wait<FP8 ? 1 : 0>();
+        copy_wait<0>();
         __syncwarp();
         if (FP8) {
-          const uint32_t raw = raw_of(u);
           const int top_k = largest(ek), top_v = largest(ev), top = values ? top_v : top_k;
           const float mine = kv_pow2((values ? ev : ek) - top + 6);  // (0 exponents of keys that are not there: zeros below)
           ok = wait_empty(seq);
@@ -264,7 +262,11 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
               const uint32_t w[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
               uint32_t y[8];
 #pragma unroll
-              for (int z = 0; z < 8; ++z) y[z] = in ? times(widen(w[z >> 1], z & 1), f) : 0u;
+              for (int z = 0; z < 8; ++z) y[z] = times(widen(w[z >> 1], z & 1), f);
+              if (here != 0xffffffffu) {
+#pragma unroll
+                for (int z = 0; z < 8; ++z) y[z] = in ? y[z] : 0u;
+              }
               const int c = 2 * (at_chunk + 4 * j);
               st_shared_v4(dst + tile_at(k, c), y[0], y[1], y[2], y[3]);
               st_shared_v4(dst + tile_at(k, c + 1), y[4], y[5], y[6], y[7]);
@@ -321,17 +323,14 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
         __syncwarp();
         if (lane == 0) mbar_arrive(full0 + 8 * (seq % C::NS));
         seq += 2;
-        if (FP8) {  // (nothing, past the end)
-          issue(u + 2, pages3, raw_of(u));
-          if (!values) ek = exp_at(u + 1, pages2, kv.k_exp);
-          ev = exp_at(u + 1, pages2, kv.v_exp);
-          pages = pages2;
-          pages2 = pages3;
-          pages3 = page_at(u + 3);
-        } else if (u + 1 < n) {
-          ok = wait_empty(seq);
+        if (u + 1 < n) {
+          if (!FP8) ok = wait_empty(seq);
           if (!ok) break;
-          issue(u + 1, pages2, stage_of(seq));
+          issue(u + 1, pages2, FP8 ? raw : stage_of(seq));
+          if (FP8) {
+            if (!values) ek = exp_at(u + 1, pages2, kv.k_exp);
+            ev = exp_at(u + 1, pages2, kv.v_exp);
+          }
           pages = pages2;
           pages2 = page_at(u + 2);
         }
@@ -379,11 +378,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
           const uint64_t dv = sw128_desc_mn(tile_at(seq + 1));
           if (leader) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k)  // P stands where its scores were: per 32 keys 16 columns of it, 16 of its rest
-#pragma unroll
-              for (int part = 0; part < 2; ++part)
-                umma_f16_ts(tmem + 256u + (uint32_t)(HD * t), tmem + 128u * t + 32 * (k >> 1) + 16 * part + 8 * (k & 1),
-                            dv + k * (2048 >> 4), idesc_o, (u > 0 || k > 0 || part > 0) ? 1u : 0u);
+            for (int k = 0; k < 8; ++k)  // (P stands where its scores were: per 32 keys 16 of their columns)
+              umma_f16_ts(tmem + 256u + (uint32_t)(HD * t), tmem + 128u * t + 32 * (k >> 1) + 8 * (k & 1), dv + k * (2048 >> 4),
+                          idesc_o, (u > 0 || k > 0) ? 1u : 0u);
             umma_commit(p_empty0 + 8 * t);
             if (t + 1 == tiles) umma_commit(empty0 + 8 * ((seq + 1) % C::NS));
           }
@@ -467,7 +464,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
       } else {
         seq += 2 * n;
       }
-      float m = -INFINITY, l = 0.f;
+      float m = -INFINITY, l = 0.f, l_r = 0.f;  // l: the sum of P; l_r: of P as rounded, which O is made of
       for (int u = 0; ok && t < tiles && u < n; ++u, seq += 2) {
         const uint32_t blk = seq >> 1;
         if (!row_wait(s_full0 + 8 * t, count & 1u)) break;
@@ -507,6 +504,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
             const float mn = grew ? top - 7.f : m, alpha = grew ? ex2_approx(m - mn) : 1.f;
             m = mn;
             l *= alpha;
+            l_r *= alpha;
             if (u > 0) {  // (the product before this unit's scores is done: they came after it)
               tmem_ld_wait();
 #pragma unroll 1
@@ -521,7 +519,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
               }
             }
           }
-          // ---- P, into the places of its scores: per 32 keys 16 columns of fp16 pairs, 16 of what they lack
+          // ---- P, into the places of its scores: per 32 keys 16 columns of fp16 pairs
           const float ref = m == -INFINITY ? 0.f : m;
 #pragma unroll 1
           for (int c = 0; c < 4; ++c) {
@@ -529,7 +527,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
             const uint32_t there = __float_as_uint(scale.w);
             const float qf = qa * scale.x, add = scale.y - ref;
             const unsigned long long qf2 = pk2(qf, qf), add2 = pk2(add, add);
-            unsigned long long sum2 = pk2(0.f, 0.f);
+            unsigned long long sum2 = pk2(0.f, 0.f), sum_r2 = sum2;
             float x[32];
             tmem_ld_wait();
 #pragma unroll
@@ -540,20 +538,20 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
 #pragma unroll
               for (int i = 0; i < 32; ++i) x[i] = there >> i & 1 ? x[i] : -INFINITY;
             }
+            uint32_t w[16];
 #pragma unroll
             for (int i = 0; i < 32; i += 2) {
               const float p0 = ex2_approx(x[i]), p1 = ex2_approx(x[i + 1]);
-              const unsigned long long p2 = pk2(p0, p1);
-              sum2 = fadd2(p2, sum2);
+              sum2 = fadd2(pk2(p0, p1), sum2);
               const uint32_t hi = pack_f16x2(p0, p1);
               const float2 q = __half22float2(*reinterpret_cast<const __half2*>(&hi));
-              float r0, r1;
-              upk2(fadd2(p2, pk2(-q.x, -q.y)), r0, r1);
-              s[i / 2] = hi;
-              s[16 + i / 2] = pack_f16x2(r0, r1);
+              sum_r2 = fadd2(pk2(q.x, q.y), sum_r2);
+              w[i / 2] = hi;
             }
-            tmem_st32u(s_at + 32 * c, s);
+            tmem_st16(s_at + 32 * c, w);
             float lo, hi;
+            upk2(sum_r2, lo, hi);
+            l_r = fmaf(lo + hi, scale.z, l_r);
             upk2(sum2, lo, hi);
             l = fmaf(lo + hi, scale.z, l);
           }
@@ -569,6 +567,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
       tc_fence_after();
       if (ok && band) {
         float* part = scratch.part + ((2 * (int64_t)blockIdx.x + (it.from == 0)) * TC_ROWS + row) * (HD + 4);
+        const float right = l_r != 0.f ? l / l_r : 1.f;
         const int64_t at = (int64_t)(it.row0 + tok) * a.H + h;
 #pragma unroll 1
         for (int c = 0; c < HD / 32; ++c) {
@@ -578,7 +577,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
           if (!live) continue;
 #pragma unroll
           for (int i = 0; i < 32; i += 4) {
-            const float4 x = make_float4(f32(o[i]), f32(o[i + 1]), f32(o[i + 2]), f32(o[i + 3]));
+            const float4 x = make_float4(f32(o[i]) * right, f32(o[i + 1]) * right, f32(o[i + 2]) * right, f32(o[i + 3]) * right);
             if (it.whole())
               finish4(a, at, HD, 32 * c + i, make_float2(m, l), x);
             else
