@@ -67,6 +67,9 @@ struct KeyScale {
   uint32_t there;
 };
 
+// The value of lane 0, which the compiler then knows to be the whole warp's (uniform registers).
+__device__ __forceinline__ int warp_uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
+
 // Descriptor of a [key][hd] tile as the transposed B operand: 128-byte rows of 64 components (the next
 // 64 a box on), 8-row swizzle atoms along the keys.
 __device__ __forceinline__ uint64_t sw128_desc_mn(uint32_t saddr) {
@@ -121,6 +124,72 @@ __device__ __forceinline__ uint32_t widen(uint32_t w, int half) {  // two E4M3 c
 __device__ __forceinline__ uint32_t times(uint32_t x, __half2 f) {
   __half2 y = __hmul2(*reinterpret_cast<__half2*>(&x), f);
   return *reinterpret_cast<uint32_t*>(&y);
+}
+
+// The MMAs of an item (the whole warp; one lane issues).  Its operands are made known as the warp's, in
+// uniform registers: else an issue takes about 100 cycles, more than most of the products.
+template <int HD, bool FP8>
+__device__ __forceinline__ bool tc_mma(uint32_t base, uint32_t tmem, int tiles, int n, uint32_t& seq_, uint32_t& items,
+                                       uint32_t& units, volatile int* abort_flag) {
+  using C = TcCfg<HD, FP8>;
+  constexpr uint32_t idesc_s = FP8 ? make_idesc_f16(128, 128) : make_idesc(128, 128);
+  constexpr uint32_t idesc_o = make_idesc_f16(128, HD) | IDESC_B_MN;
+  base = (uint32_t)warp_uniform((int)base);
+  tmem = (uint32_t)warp_uniform((int)tmem);
+  tiles = warp_uniform(tiles);
+  n = warp_uniform(n);
+  uint32_t seq = (uint32_t)warp_uniform((int)seq_);
+  const uint32_t full0 = base + C::BAR, empty0 = full0 + 8 * C::NS, s_full0 = empty0 + 8 * C::NS, p_full0 = s_full0 + 16;
+  const uint32_t p_empty0 = p_full0 + 16, q_full0 = p_empty0 + 16;
+  const bool leader = elect_one();
+  auto wait = [&](uint32_t bar, uint32_t parity) {
+    return (bool)__all_sync(0xffffffffu, mbar_wait_inline(bar, parity, abort_flag));
+  };
+  auto full = [&](uint32_t s) { return wait(full0 + 8 * (s % C::NS), (s / C::NS) & 1u); };
+  auto issue_s = [&](int t, uint32_t s, bool last) {  // S of the keys at place s
+    const uint64_t dq = sw128_desc(base + t * C::TILE), dk = sw128_desc(base + C::KV + (s % C::NS) * C::TILE);
+    if (leader) {
+#pragma unroll
+      for (int k = 0; k < HD / 16; ++k)
+        umma_bf16(tmem + 128u * t, dq + (k >> 2) * (TC_BOX >> 4) + 2 * (k & 3), dk + (k >> 2) * (TC_BOX >> 4) + 2 * (k & 3),
+                  idesc_s, k > 0 ? 1u : 0u);
+      umma_commit(s_full0 + 8 * t);
+      if (last) umma_commit(empty0 + 8 * (s % C::NS));
+    }
+    __syncwarp();
+  };
+  if (!full(seq)) return false;
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    if (t >= tiles) break;
+    if (!wait(q_full0 + 8 * t, (items >> (16 * t)) & 1u)) return false;
+    items ^= 1u << (16 * t);
+    tc_fence_after();
+    issue_s(t, seq, t + 1 == tiles);
+  }
+  for (int u = 0; u < n; ++u, seq += 2) {
+    if (!full(seq + 1) || (u + 1 < n && !full(seq + 2))) return false;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      if (t >= tiles) break;
+      if (!wait(p_full0 + 8 * t, (units >> (16 * t)) & 1u)) return false;
+      units ^= 1u << (16 * t);
+      tc_fence_after();
+      const uint64_t dv = sw128_desc_mn(base + C::KV + ((seq + 1) % C::NS) * C::TILE);
+      if (leader) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)  // (P stands where its scores were: per 32 keys 16 of their columns)
+          umma_f16_ts(tmem + 256u + (uint32_t)(HD * t), tmem + 128u * t + 32 * (k >> 1) + 8 * (k & 1), dv + k * (2048 >> 4),
+                      idesc_o, (u > 0 || k > 0) ? 1u : 0u);
+        umma_commit(p_empty0 + 8 * t);
+        if (t + 1 == tiles) umma_commit(empty0 + 8 * ((seq + 1) % C::NS));
+      }
+      __syncwarp();
+      if (u + 1 < n) issue_s(t, seq + 2, t + 1 == tiles);
+    }
+  }
+  seq_ = seq;
+  return true;
 }
 
 template <int HD, bool FP8>
@@ -341,58 +410,11 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     if (!ok) gave_up();
   } else if (warp == 16) {
     // ================================================================ MMAs
-    constexpr uint32_t idesc_s = FP8 ? make_idesc_f16(128, 128) : make_idesc(128, 128);
-    constexpr uint32_t idesc_o = make_idesc_f16(128, HD) | IDESC_B_MN;
-    const bool leader = elect_one();
-    uint32_t seq = 0, items[2] = {0, 0}, count[2] = {0, 0};  // items and units of each tile
+    uint32_t seq = 0, items = 0, units = 0;  // items, units: of tile 0 in the low half, of tile 1 in the high
     bool ok = true;
-    auto issue_s = [&](int t, uint32_t tile) {
-      const uint64_t dq = sw128_desc(base + t * C::TILE), dk = sw128_desc(tile);
-      if (leader) {
-#pragma unroll
-        for (int k = 0; k < HD / 16; ++k)
-          umma_bf16(tmem + 128u * t, dq + (k >> 2) * (TC_BOX >> 4) + 2 * (k & 3), dk + (k >> 2) * (TC_BOX >> 4) + 2 * (k & 3),
-                    idesc_s, k > 0 ? 1u : 0u);
-        umma_commit(s_full0 + 8 * t);
-      }
-      __syncwarp();
-    };
-    auto full = [&](uint32_t s) { return wait(full0 + 8 * (s % C::NS), (s / C::NS) & 1u); };
-    auto tile_at = [&](uint32_t s) { return base + C::KV + (s % C::NS) * C::TILE; };
-    while (ok && line.next(walk, it)) {
-      const int n = it.until - it.from, tiles = it.rows > 128 ? 2 : 1;
-      ok = full(seq);
-      for (int t = 0; ok && t < tiles; ++t) ok = wait(q_full0 + 8 * t, items[t]++ & 1u);
-      if (!ok) break;
-      tc_fence_after();
-      for (int t = 0; t < tiles; ++t) issue_s(t, tile_at(seq));
-      if (leader) umma_commit(empty0 + 8 * (seq % C::NS));
-      __syncwarp();
-      for (int u = 0; ok && u < n; ++u, seq += 2) {
-        ok = full(seq + 1) && (u + 1 == n || full(seq + 2));
-        for (int t = 0; ok && t < tiles; ++t) {
-          ok = wait(p_full0 + 8 * t, count[t] & 1u);
-          if (!ok) break;
-          ++count[t];
-          tc_fence_after();
-          const uint64_t dv = sw128_desc_mn(tile_at(seq + 1));
-          if (leader) {
-#pragma unroll
-            for (int k = 0; k < 8; ++k)  // (P stands where its scores were: per 32 keys 16 of their columns)
-              umma_f16_ts(tmem + 256u + (uint32_t)(HD * t), tmem + 128u * t + 32 * (k >> 1) + 8 * (k & 1), dv + k * (2048 >> 4),
-                          idesc_o, (u > 0 || k > 0) ? 1u : 0u);
-            umma_commit(p_empty0 + 8 * t);
-            if (t + 1 == tiles) umma_commit(empty0 + 8 * ((seq + 1) % C::NS));
-          }
-          __syncwarp();
-          if (u + 1 < n) {
-            issue_s(t, tile_at(seq + 2));
-            if (leader && t + 1 == tiles) umma_commit(empty0 + 8 * ((seq + 2) % C::NS));
-            __syncwarp();
-          }
-        }
-      }
-    }
+    const bool leader = elect_one();
+    while (warp_uniform(ok && line.next(walk, it)))
+      ok = tc_mma<HD, FP8>(base, tmem, it.rows > 128 ? 2 : 1, it.until - it.from, seq, items, units, abort_flag);
     if (!ok) gave_up();
     if (leader) umma_commit(drain);  // every MMA issued here completes before the end
     __syncwarp();
@@ -473,18 +495,12 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
         tc_fence_after();
         if (band) {
           const uint32_t scales = base + C::EXP + (blk & 3) * 64;
-          uint32_t s[32], ahead[32];  // 32 scores, and the next ones
+          uint32_t s0[32], s1[32];  // 32 scores, and the next ones
           // ---- the row's largest score
           float top = -INFINITY;
-          tmem_ld32(s_at, ahead);
-#pragma unroll 1
-          for (int c = 0; c < 4; ++c) {
+          auto largest = [&](uint32_t (&s)[32], int c) {
             const float4 scale = ld_shared_v4(scales + 16 * c);
             const uint32_t there = __float_as_uint(scale.w);
-            tmem_ld_wait();
-#pragma unroll
-            for (int i = 0; i < 32; ++i) s[i] = ahead[i];
-            if (c < 3) tmem_ld32(s_at + 32 * (c + 1), ahead);
             if (there != 0xffffffffu) {
 #pragma unroll
               for (int i = 0; i < 32; ++i) s[i] = there >> i & 1 ? s[i] : 0xff800000u;
@@ -496,8 +512,17 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
               a1 = max3f(a1, f32(s[i + 2]), f32(s[i + 3]));
             }
             top = fmaxf(top, fmaf(fmaxf(a0, a1), qa * scale.x, scale.y));
+          };
+          tmem_ld32(s_at, s0);
+#pragma unroll 1
+          for (int c = 0; c < 4; c += 2) {
+            tmem_ld_wait();
+            tmem_ld32(s_at + 32 * (c + 1), s1);
+            largest(s0, c);
+            tmem_ld_wait();
+            tmem_ld32(s_at + 32 * ((c + 2) & 3), s0);  // (in the end the first again)
+            largest(s1, c + 1);
           }
-          tmem_ld32(s_at, ahead);
           // ---- a larger reference where that passes it by more than 15, or is the row's first
           const bool grew = top > m + 15.f;
           if (__any_sync(0xffffffffu, grew)) {
@@ -521,27 +546,22 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
           }
           // ---- P, into the places of its scores: per 32 keys 16 columns of fp16 pairs
           const float ref = m == -INFINITY ? 0.f : m;
-#pragma unroll 1
-          for (int c = 0; c < 4; ++c) {
+          auto weigh = [&](const uint32_t (&s)[32], int c) {
             const float4 scale = ld_shared_v4(scales + 16 * c);
             const uint32_t there = __float_as_uint(scale.w);
             const float qf = qa * scale.x, add = scale.y - ref;
             const unsigned long long qf2 = pk2(qf, qf), add2 = pk2(add, add);
             unsigned long long sum2 = pk2(0.f, 0.f), sum_r2 = sum2;
-            float x[32];
-            tmem_ld_wait();
-#pragma unroll
-            for (int i = 0; i < 32; i += 2)  // (pairs: one instruction for two scores)
-              upk2(ffma2(pk2(f32(ahead[i]), f32(ahead[i + 1])), qf2, add2), x[i], x[i + 1]);
-            if (c < 3) tmem_ld32(s_at + 32 * (c + 1), ahead);
-            if (there != 0xffffffffu) {
-#pragma unroll
-              for (int i = 0; i < 32; ++i) x[i] = there >> i & 1 ? x[i] : -INFINITY;
-            }
             uint32_t w[16];
 #pragma unroll
-            for (int i = 0; i < 32; i += 2) {
-              const float p0 = ex2_approx(x[i]), p1 = ex2_approx(x[i + 1]);
+            for (int i = 0; i < 32; i += 2) {  // (pairs: one instruction for two scores)
+              float x0, x1;
+              upk2(ffma2(pk2(f32(s[i]), f32(s[i + 1])), qf2, add2), x0, x1);
+              if (there != 0xffffffffu) {
+                x0 = there >> i & 1 ? x0 : -INFINITY;
+                x1 = there >> (i + 1) & 1 ? x1 : -INFINITY;
+              }
+              const float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
               sum2 = fadd2(pk2(p0, p1), sum2);
               const uint32_t hi = pack_f16x2(p0, p1);
               const float2 q = __half22float2(*reinterpret_cast<const __half2*>(&hi));
@@ -554,6 +574,15 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
             l_r = fmaf(lo + hi, scale.z, l_r);
             upk2(sum2, lo, hi);
             l = fmaf(lo + hi, scale.z, l);
+          };
+#pragma unroll 1
+          for (int c = 0; c < 4; c += 2) {
+            tmem_ld_wait();
+            tmem_ld32(s_at + 32 * (c + 1), s1);
+            weigh(s0, c);
+            tmem_ld_wait();
+            if (c == 0) tmem_ld32(s_at + 64, s0);
+            weigh(s1, c + 1);
           }
           tmem_st_wait();
         }
