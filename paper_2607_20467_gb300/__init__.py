@@ -161,38 +161,39 @@ def _dev(t, name, itemsize, count=0):
     refused here, before a kernel could read or write past it."""
     if t is None or isinstance(t, int):
         return t
-    if isinstance(t, np.ndarray) or not getattr(t, "is_cuda", False):
+    if not getattr(t, "is_cuda", False):
         raise ValueError(f"{name}: a device buffer (a CUDA tensor) is required")
     if t.element_size() != itemsize:
         raise TypeError(f"{name}: elements of {itemsize} bytes expected, got {t.dtype}")
     if t.numel() < count:
         raise ValueError(f"{name}: at least {count} elements needed, {t.numel()} given")
-    return _ptr(t)
+    if not t.is_contiguous():
+        raise ValueError("tensor must be contiguous")
+    return t.data_ptr()
 
 
 def _dev_rows(t, name, itemsize, rows, cols):
     """Device pointer and row stride (elements) of `rows` rows of `cols` elements each: a CUDA tensor
     whose first dimension may be strided and whose rows are contiguous (a column block of a
     wider matrix is)."""
-    if isinstance(t, np.ndarray) or not getattr(t, "is_cuda", False):
+    if not getattr(t, "is_cuda", False):
         raise ValueError(f"{name}: a device buffer (a CUDA tensor) is required")
     if t.element_size() != itemsize:
         raise TypeError(f"{name}: elements of {itemsize} bytes expected, got {t.dtype}")
-    if t.is_contiguous():  # (a call's host time is a few microseconds: the common case is looked at once)
-        if t.numel() < rows * cols or t.numel() != t.shape[0] * cols:
-            raise ValueError(f"{name}: {rows} rows of {cols} elements expected, got {tuple(t.shape)}")
-        return t.data_ptr(), cols
-    shape, stride = t.shape, t.stride()
-    inner = 1
+    shape, stride = t.shape, t.stride()  # (looked at once each: a call's host time is a few microseconds)
+    n, inner = shape[0], 1
     for i in range(len(shape) - 1, 0, -1):
-        if shape[i] != 1 and stride[i] != inner:
+        size = shape[i]
+        if stride[i] != inner and size != 1:
             raise ValueError(f"{name}: the elements of a row must be contiguous")
-        inner *= shape[i]
-    if shape[0] < rows or inner != cols:
+        inner *= size
+    if n < rows or inner != cols:
         raise ValueError(f"{name}: {rows} rows of {cols} elements expected, got {tuple(shape)}")
-    if shape[0] > 1 and stride[0] < cols:
+    if n <= 1:
+        return t.data_ptr(), cols
+    if stride[0] < cols:
         raise ValueError(f"{name}: rows overlap")
-    return t.data_ptr(), stride[0] if shape[0] > 1 else cols
+    return t.data_ptr(), stride[0]
 
 
 class KvCache:
@@ -218,6 +219,7 @@ class KvCache:
         self.desc = KvCacheDesc(pages, page_len, heads, hd, self.format, _dev(k, "k", size, n * hd),
                                 _dev(v, "v", size, n * hd), _dev(k_exp, "k_exp", 1, n), _dev(v_exp, "v_exp", 1, n))
         self.ptr = ctypes.addressof(self.desc)
+        self.row = heads * hd  # elements of a position's keys
 
     @classmethod
     def empty(cls, n_pages, page_len, n_kv_heads, head_dim, fp8=True, device="cuda"):
@@ -410,21 +412,25 @@ class Context:
     def kv_write(self, cache, k, v, slots):
         """Store rows k, v [n][kv heads][head_dim] (bf16, rows may be strided) at slots (int32 [n],
         negative: skipped)."""
-        n, cols = k.shape[0], cache.n_kv_heads * cache.head_dim
+        n, cols = k.shape[0], cache.row
         kp, ks = _dev_rows(k, "k", 2, n, cols)
         vp, vs = _dev_rows(v, "v", 2, n, cols)
         if ks != vs and n > 1:
             raise ValueError("k and v differ in row stride")
-        self._check(self._L.dcl_kv_write(self.ptr, cache.ptr, kp, vp, ks, _dev(slots, "slots", 4, n), n))
+        st = self._L.dcl_kv_write(self.ptr, cache.ptr, kp, vp, ks, _dev(slots, "slots", 4, n), n)
+        if st:
+            self._check(st)
 
     def kv_read(self, cache, slots, k, v):
         """Read the positions at slots (int32 [n], negative: zeros) into k, v [n][kv heads][head_dim]."""
-        n, cols = slots.shape[0], cache.n_kv_heads * cache.head_dim
+        n, cols = slots.shape[0], cache.row
         kp, ks = _dev_rows(k, "k", 2, n, cols)
         vp, vs = _dev_rows(v, "v", 2, n, cols)
         if ks != vs and n > 1:
             raise ValueError("k and v differ in row stride")
-        self._check(self._L.dcl_kv_read(self.ptr, cache.ptr, _dev(slots, "slots", 4, n), n, kp, vp, ks))
+        st = self._L.dcl_kv_read(self.ptr, cache.ptr, _dev(slots, "slots", 4, n), n, kp, vp, ks)
+        if st:
+            self._check(st)
 
     def kv_attention(self, cache, q, q_start, page_table, seq_len, out, max_new, causal=False, scale=0.0, lse=None):
         """Attention of the rows q [n_q][heads][head_dim] (bf16, rows may be strided; rows
