@@ -606,7 +606,8 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
     __syncthreads();
     // a row's weights by a thread, then four components of a row a thread
     float* wt = reinterpret_cast<float*>(smem + C::WT);
-    float2* row = reinterpret_cast<float2*>(smem + C::WT + C::ROWS * 32);
+    KaRow* row = reinterpret_cast<KaRow*>(smem + C::WT + C::ROWS * 32);
+    float* part = scratch.part + (2 * (int64_t)blockIdx.x + (it.from == 0)) * C::ROWS * (HD + 4);
     if (threadIdx.x < it.rows) {
       const int r = threadIdx.x;
       float2 x[C::WARPS];
@@ -622,7 +623,10 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
         wt[r * 8 + w] = f;
         sum = fmaf(x[w].y, f, sum);
       }
-      row[r] = make_float2(top, sum);
+      if (it.whole())
+        row[r] = finish_row(a, it.row0, it.g * rep, it.first, rep, r, top, sum);
+      else
+        *reinterpret_cast<float2*>(part + r * (HD + 4) + HD) = make_float2(top, sum);
     }
     __syncthreads();
     constexpr int PART = HD + 4, Q = HD / 4;
@@ -635,14 +639,10 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
 #pragma unroll
       for (int w = 0; w < C::WARPS; ++w)
         if (w < active) add_scaled(acc, *reinterpret_cast<const float4*>(o_row + w * (C::RING_B / 4)), wt[r * 8 + w]);
-      if (it.whole()) {
-        const int tok = (it.first + r) / rep;
-        finish4(a, (int64_t)(it.row0 + tok) * a.H + it.g * rep + it.first + r - tok * rep, HD, c, row[r], acc);
-      } else {
-        float* part = scratch.part + ((2 * (int64_t)blockIdx.x + (it.from == 0)) * C::ROWS + r) * PART;
-        *reinterpret_cast<float4*>(part + c) = acc;
-        if (c == 0) *reinterpret_cast<float2*>(part + HD) = row[r];
-      }
+      if (it.whole())
+        finish4<HD>(a, row[r], c, acc);
+      else
+        *reinterpret_cast<float4*>(part + r * PART + c) = acc;
     }
     if (!it.whole()) {
       int c0, c1;
@@ -663,7 +663,7 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
   for (int i = 0; i < todo[0].rows; ++i) {
     const KaJoin j = todo[1 + i];
     join_parts<HD, C::ROWS, C::THREADS>(a, j, rep, scratch.part, reinterpret_cast<float2*>(smem),
-                                        reinterpret_cast<float2*>(smem + C::WT + C::ROWS * 32), threadIdx.x,
+                                        reinterpret_cast<KaRow*>(smem + C::WT + C::ROWS * 32), threadIdx.x,
                                         [] { __syncthreads(); });
     __syncthreads();
   }

@@ -441,7 +441,6 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
       const int n = it.until - it.from, tiles = it.rows > 128 ? 2 : 1;
       const int row = 128 * t + r;
       const bool live = row < it.rows, band = 128 * t + 32 * quarter < it.rows;
-      const int rr = it.first + row, tok = rr / rep, h = it.g * rep + rr - tok * rep;
       float qa = a.scale * kLog2e;
       // ---- q: the band's rows into their tile, 16-byte chunks of a row by neighbouring lanes
       if (ok && t < tiles) {
@@ -597,7 +596,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
       if (ok && band) {
         float* part = scratch.part + ((2 * (int64_t)blockIdx.x + (it.from == 0)) * TC_ROWS + row) * (HD + 4);
         const float right = l_r != 0.f ? l / l_r : 1.f;
-        const int64_t at = (int64_t)(it.row0 + tok) * a.H + h;
+        KaRow mine{};
+        if (live && it.whole()) mine = finish_row(a, it.row0, it.g * rep, it.first, rep, row, m, l);
 #pragma unroll 1
         for (int c = 0; c < HD / 32; ++c) {
           uint32_t o[32];
@@ -608,7 +608,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
           for (int i = 0; i < 32; i += 4) {
             const float4 x = make_float4(f32(o[i]) * right, f32(o[i + 1]) * right, f32(o[i + 2]) * right, f32(o[i + 3]) * right);
             if (it.whole())
-              finish4(a, at, HD, 32 * c + i, make_float2(m, l), x);
+              finish4<HD>(a, mine, 32 * c + i, x);
             else
               *reinterpret_cast<float4*>(part + 32 * c + i) = x;
           }
@@ -643,7 +643,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
       k.first += r0;
       k.rows = min(some, j.rows - r0);
       join_parts<HD, TC_ROWS, TC_THREADS>(a, k, rep, scratch.part + (int64_t)r0 * (HD + 4),
-                                          reinterpret_cast<float2*>(smem + TC_ROWS * 8), reinterpret_cast<float2*>(smem),
+                                          reinterpret_cast<float2*>(smem + TC_ROWS * 8), reinterpret_cast<KaRow*>(smem),
                                           threadIdx.x, [] { __syncthreads(); });
       __syncthreads();
     }

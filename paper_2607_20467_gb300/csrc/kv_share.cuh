@@ -186,13 +186,22 @@ struct KaScratch {
   int* count;   // [CTAs], by the CTA that begins the item; zero between launches
 };
 
-// Four components of a row, joined: O / l, and the row's log-sum-exp.
-__device__ __forceinline__ void finish4(const KvAttn& a, int64_t at, int HD, int c, float2 row, const float4& o) {
-  const float inv = 1.f / row.y;
-  uint2 w = make_uint2(0, 0);
-  if (row.y != 0.f) w = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
-  *reinterpret_cast<uint2*>(a.out + at * HD + c) = w;
-  if (c == 0 && a.lse) a.lse[at] = row.y == 0.f ? -INFINITY : (row.x + log2f(row.y)) * kLn2;
+// A joined row: 1 / l (0 for a row that sees nothing), and its place in the output.
+struct KaRow {
+  float inv;
+  int at;
+};
+// Row r of an item (its first of the sequence's kv head: first), {m, l} joined: what its components need,
+// and its log-sum-exp.
+__device__ __forceinline__ KaRow finish_row(const KvAttn& a, int row0, int head0, int first, int rep, int r, float m, float l) {
+  const int tok = (first + r) / rep, at = (row0 + tok) * a.H + head0 + first + r - tok * rep;
+  if (a.lse) a.lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+  return KaRow{l == 0.f ? 0.f : 1.f / l, at};
+}
+template <int HD>
+__device__ __forceinline__ void finish4(const KvAttn& a, const KaRow& row, int c, const float4& o) {
+  const float f = row.inv;
+  *reinterpret_cast<uint2*>(a.out + (int64_t)row.at * HD + c) = make_uint2(pack_bf16x2(o.x * f, o.y * f), pack_bf16x2(o.z * f, o.w * f));
 }
 __device__ __forceinline__ void add_scaled(float4& acc, const float4& y, float f) {
   acc.x = fmaf(y.x, f, acc.x);
@@ -218,12 +227,12 @@ __device__ __forceinline__ float exp2_fast(float x) {
 
 // The parts of an item, left by its CTAs, joined by THREADS threads (tid of them; sync: their barrier):
 // every part's {m, l} into shared memory (w, [rows][parts]) at once, a row's weights by a thread or
-// a warp (its {m, l} in row); then four components of a row a thread, eight to sixteen loads in
+// a warp (what its components need in row); then four components of a row a thread, 12 to 16 loads in
 // flight (one takes about 1000 cycles here: a warp per row, part after part, took 35000 for 38
 // parts and 17000 for two parts of 32 rows).
 template <int HD, int ROWS, int THREADS, typename Sync>
 __device__ __forceinline__ void join_parts(const KvAttn& a, const KaJoin& it, int rep, const float* parts, float2* w,
-                                           float2* row, int tid, Sync sync) {
+                                           KaRow* row, int tid, Sync sync) {
   constexpr int PART = HD + 4, Q = HD / 4;
   const int warp = tid >> 5, lane = tid & 31, n = it.parts;
   // (the first CTA's part is its second, the others' their first)
@@ -245,7 +254,7 @@ __device__ __forceinline__ void join_parts(const KvAttn& a, const KaJoin& it, in
         wr[c].x = f;
         sum = fmaf(x.y, f, sum);
       }
-      row[r] = make_float2(top, sum);
+      row[r] = finish_row(a, it.row0, it.head0, it.first, rep, r, top, sum);
     }
   } else {
     for (int r = warp; r < it.rows; r += THREADS / 32) {
@@ -260,7 +269,7 @@ __device__ __forceinline__ void join_parts(const KvAttn& a, const KaJoin& it, in
         sum = fmaf(x.y, f, sum);
       }
       sum = warp_sum(sum);
-      if (lane == 0) row[r] = make_float2(top, sum);
+      if (lane == 0) row[r] = finish_row(a, it.row0, it.head0, it.first, rep, r, top, sum);
     }
   }
   sync();
@@ -296,13 +305,14 @@ __device__ __forceinline__ void join_parts(const KvAttn& a, const KaJoin& it, in
       for (int k = 0; k < T; ++k) {
         const int t = t0 + k * THREADS;
         if (t >= it.rows * Q) break;
-        const int r = t / Q, tok = (it.first + r) / rep;
-        finish4(a, (int64_t)(it.row0 + tok) * a.H + it.head0 + it.first + r - tok * rep, HD, 4 * (t % Q), row[r], acc[k]);
+        finish4<HD>(a, row[t / Q], 4 * (t % Q), acc[k]);
       }
     }
   };
-  if (n <= 4)
-    tasks(std::integral_constant<int, 4>{}, std::integral_constant<int, 2>{});
+  if (n == 2)  // (most often; what a thread has is loaded at once)
+    tasks(std::integral_constant<int, 6>{}, std::integral_constant<int, 2>{});
+  else if (n <= 4)
+    tasks(std::integral_constant<int, 4>{}, std::integral_constant<int, 4>{});
   else
     tasks(std::integral_constant<int, 2>{}, std::integral_constant<int, 8>{});
 }
