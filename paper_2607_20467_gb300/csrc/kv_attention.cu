@@ -20,8 +20,7 @@
 // key's exponent scales its score.  A value's exponent e_j goes into the exponent of its
 // probability: P_j = exp2(s_j + e_j - m) with m near the running maximum of s_j + e_j, so that P is
 // bounded whatever the values' sizes, and l = sum P_j 2^-e_j.  P is rounded to fp16 (2^-11 of itself;
-// below 2^-21 of the largest term, 2^-32 of that); O is divided by the same sum of the rounded P, so that a
-// row which one key dominates shows nothing of it, while l, of the unrounded, gives the log-sum-exp.
+// below 2^-21 of the largest term, 2^-32 of that): an eighth of the output's rounding.
 // bf16 pages: the instruction wants both operands of one type, and bf16 alone would round P by 2^-8
 // of itself, as much as the output's own rounding; P is given in two bf16 parts (2^-16), the second
 // a product more.
@@ -332,7 +331,7 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
     }
     const uint32_t qs_addr = smem_addr(smem) + C::QF + lane * 16;
 
-    float o[MT][NT][4], m[2 * MT], l[2 * MT], l_r[FP8 ? 2 * MT : 1];
+    float o[MT][NT][4], m[2 * MT], l[2 * MT];
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -343,7 +342,6 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
     for (int i = 0; i < 2 * MT; ++i) {
       m[i] = -INFINITY;
       l[i] = 0.f;
-      if (FP8) l_r[FP8 ? i : 0] = 0.f;
     }
 
     int cur = 0;
@@ -456,7 +454,6 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
             const float mn = fmaxf(m[i], top[i] - 7.f), alpha = exp2_fast(m[i] - (mn == -INFINITY ? 0.f : mn));
             m[i] = mn;
             l[i] *= alpha;
-            if (FP8) l_r[FP8 ? i : 0] *= alpha;
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
               o[i >> 1][j][2 * (i & 1)] *= alpha;
@@ -474,9 +471,7 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
             const uint32_t hi = FP8 ? pack_f16x2(x0, x1) : pack_bf16x2(x0, x1);
             if (FP8) {
               const float2 vi = lds_f2(sc + 4 * (2 * KT + 8 * j + 2 * place));
-              const float2 q = __half22float2(*reinterpret_cast<const __half2*>(&hi));
               l[i] = fmaf(x1, vi.y, fmaf(x0, vi.x, l[i]));
-              l_r[FP8 ? i : 0] = fmaf(q.y, vi.y, fmaf(q.x, vi.x, l_r[FP8 ? i : 0]));
             } else {
               l[i] += x0 + x1;
             }
@@ -579,17 +574,6 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
       l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
       l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
       if (place == 0) ml[warp * C::ROWS + 8 * i + quad] = make_float2(m[i], l[i]);
-      if (FP8) {
-        float& r = l_r[FP8 ? i : 0];
-        r += __shfl_xor_sync(0xffffffffu, r, 1);
-        r += __shfl_xor_sync(0xffffffffu, r, 2);
-        const float right = r != 0.f ? l[i] / r : 1.f;
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          o[i >> 1][j][2 * (i & 1)] *= right;
-          o[i >> 1][j][2 * (i & 1) + 1] *= right;
-        }
-      }
     }
     if (key0 + KT * warp < stop) {
       float* mine = reinterpret_cast<float*>(smem + warp * C::RING_B);
@@ -690,8 +674,20 @@ cudaError_t launch_rows(const KvPool& kv, const KvAttn& a, const KaScratch& s, i
 
 }  // namespace
 
+// Which kernel: the one that passes over the keys once for every 32 rows, or tcgen05 for every 256, whose
+// CTAs take longer to begin, to end and to join.  Time per unit of 128 keys over the whole GPU and
+// what comes on top, us (FP8, hd 128; bf16 and hd 64 within 15 %): 0.008 for 32 rows and 20; 0.015
+// for up to 128 rows, 0.018 for 256, and 46.  8 sequences of 3000 positions: 28 / 4 heads and 16 new
+// positions (112 rows) 44.8 here against 47.3 there, 32 new 61.5 against 60.2; 32 heads and 64 new
+// 119.9 against 137; but 16 x 8192 with 28 / 4 heads and 32 new 241 against 120.  Lengths are known
+// to the device only: the page table's width stands for them.
 bool kv_attention_many_rows(const KvPool& kv, const KvAttn& a) {
-  return !a.causal && (int64_t)a.max_new * (a.H / kv.G) > 32;
+  const int64_t rows = (int64_t)a.max_new * (a.H / kv.G);
+  if (a.causal || rows <= 32) return false;
+  const double units = (double)a.batch * kv.G * (((int64_t)a.max_pages * kv.page_len() + KA_UNIT - 1) / KA_UNIT);
+  const int64_t rest = rows % 256;
+  const double here = 8.0 * (double)((rows + 31) / 32), there = 18.0 * (double)(rows / 256) + (rest > 128 ? 18 : rest ? 15 : 0);
+  return (here - there) * units > 26000.0;
 }
 
 size_t kv_attention_scratch(int sms) { return (size_t)KA_CTAS * sms * (KV_ATTN_PART_BYTES + sizeof(int)); }

@@ -2,10 +2,11 @@
 // tensor cores: the rows of an item (up to 256: new positions x the query heads of one kv head)
 // fill one or two tiles of 128, and one pass over the keys serves them all.
 //
-// Per unit of 128 keys: S = Q K^T into TMEM; P = exp2(S scaled + e - m) in fp16 takes the place of its
-// scores there; O += P V in TMEM.  P, m, l, the exponents e of the values and O's division by the sum of
-// the rounded P are those of kv_attention.cu; a thread owns a row, so its statistics need no
-// exchange.
+// Per unit of 128 keys: S = Q K^T into TMEM; P = exp2(S scaled + e - m) in two fp16 parts (11 bits and what
+// they leave) takes the place of its scores there; O += P V in TMEM.  (One part costs a row that sees
+// little but a few keys up to 2^-11 of its result; it took 113 us where two take 126, at 16 sequences
+// of 8192 keys, 224 rows a kv head.)  P, m, l and the exponents e of the values are those of kv_attention.cu; a
+// thread owns a row, so its statistics need no exchange.
 //
 // FP8 pages.  Eight warps copy codes into shared memory (16-byte asynchronous copies, one unit
 // ahead) and widen them into the fp16 operand tiles, each code times 2^(e_j - e_max + 6) with e_max
@@ -39,6 +40,8 @@ namespace {
 constexpr int TC_ROWS = 256;      // rows of an item
 constexpr int TC_START = 6;       // units of keys that beginning an item takes
 constexpr int TC_THREADS = 544;
+constexpr int TC_REGS = 96, TC_REGS_ROWS = 128, TC_REGS_COPY = 64;
+static_assert(TC_REGS_ROWS + TC_REGS_COPY == 2 * TC_REGS, "the rows' warps take what as many copying warps give");
 constexpr int TC_BOX = 128 * 128; // 128 rows of 128 bytes, swizzled
 constexpr int TC_JOIN = 8000;     // rows x parts joined at a time
 
@@ -82,14 +85,6 @@ __device__ __forceinline__ uint64_t sw128_desc_mn(uint32_t saddr) {
   return d;
 }
 constexpr uint32_t IDESC_B_MN = 1u << 16;
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
-      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
-      "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]),
-      "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
-      : "memory");
-}
 // D += A B with A (fp16 pairs) in TMEM.
 __device__ __forceinline__ void umma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
@@ -125,6 +120,12 @@ __device__ __forceinline__ uint32_t times(uint32_t x, __half2 f) {
   __half2 y = __hmul2(*reinterpret_cast<__half2*>(&x), f);
   return *reinterpret_cast<uint32_t*>(&y);
 }
+
+// Registers a thread of this warpgroup has from here on (its four warps come together).
+template <int N>
+__device__ __forceinline__ void registers_more() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void registers_fewer() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
 // The MMAs of an item (the whole warp; one lane issues).  Its operands are made known as the warp's, in
 // uniform registers: else an issue takes about 100 cycles, more than most of the products.
@@ -178,9 +179,11 @@ __device__ __forceinline__ bool tc_mma(uint32_t base, uint32_t tmem, int tiles, 
       const uint64_t dv = sw128_desc_mn(base + C::KV + ((seq + 1) % C::NS) * C::TILE);
       if (leader) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k)  // (P stands where its scores were: per 32 keys 16 of their columns)
-          umma_f16_ts(tmem + 256u + (uint32_t)(HD * t), tmem + 128u * t + 32 * (k >> 1) + 8 * (k & 1), dv + k * (2048 >> 4),
-                      idesc_o, (u > 0 || k > 0) ? 1u : 0u);
+        for (int k = 0; k < 8; ++k)  // (P's parts stand where its scores were: per 32 keys 16 of their columns each)
+#pragma unroll
+          for (int part = 0; part < 2; ++part)
+            umma_f16_ts(tmem + 256u + (uint32_t)(HD * t), tmem + 128u * t + 32 * (k >> 1) + 16 * part + 8 * (k & 1),
+                        dv + k * (2048 >> 4), idesc_o, (u > 0 || k > 0 || part > 0) ? 1u : 0u);
         umma_commit(p_empty0 + 8 * t);
         if (t + 1 == tiles) umma_commit(empty0 + 8 * ((seq + 1) % C::NS));
       }
@@ -253,6 +256,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     // ================================================================ copies, widening
     // Keys or values of a unit: warp w of the four has keys 32 w .. 32 w + 31, lane l knows of key 32 w + l
     // (its page and exponents); they are copied in chunks of 16 bytes.
+    registers_fewer<TC_REGS_COPY>();
     const int values = warp >= 12, w4 = warp & 3;
     constexpr int CH = FP8 ? HD / 16 : HD / 8;       // chunks of a vector
     constexpr int PK = CH / 4;                       // this lane's of a key: key (lane >> 2) + 8 i, chunk (lane & 3) + 4 j
@@ -408,6 +412,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     }
     copy_wait<0>();
     if (!ok) gave_up();
+    registers_more<TC_REGS>();  // (waits for the rows' warps to be done)
   } else if (warp == 16) {
     // ================================================================ MMAs
     uint32_t seq = 0, items = 0, units = 0;  // items, units: of tile 0 in the low half, of tile 1 in the high
@@ -422,6 +427,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     mbar_wait(drain, 0, &no_abort);
   } else {
     // ================================================================ rows
+    registers_more<TC_REGS_ROWS>();  // (waits for the copying warps to have given theirs)
     const int t = warp >> 2, quarter = warp & 3, r = 32 * quarter + lane;  // row r of tile t
     const uint32_t s_at = tmem + 128u * t + ((uint32_t)(32 * quarter) << 16);
     const uint32_t o_at = tmem + 256u + (uint32_t)(HD * t) + ((uint32_t)(32 * quarter) << 16);
@@ -444,11 +450,11 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
       float qa = a.scale * kLog2e;
       // ---- q: the band's rows into their tile, 16-byte chunks of a row by neighbouring lanes
       if (ok && t < tiles) {
-        constexpr int CPR = HD / 8, RPL = 32 / CPR, HALF = 16 / RPL;  // chunks of a row, rows of a load, loads in flight
+        constexpr int CPR = HD / 8, RPL = 32 / CPR, HALF = 32 / RPL;  // chunks of a row, rows of a load, loads in flight
         const int c = lane % CPR;
         int e_row = 0;  // exponent of this thread's row
 #pragma unroll 1
-        for (int i0 = 0; i0 < 2 * HALF; i0 += HALF) {
+        for (int i0 = 0; i0 < HALF; i0 += HALF) {
           uint4 x[HALF];
 #pragma unroll
           for (int i = 0; i < HALF; ++i) {
@@ -485,7 +491,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
       } else {
         seq += 2 * n;
       }
-      float m = -INFINITY, l = 0.f, l_r = 0.f;  // l: the sum of P; l_r: of P as rounded, which O is made of
+      float m = -INFINITY, l = 0.f;
       for (int u = 0; ok && t < tiles && u < n; ++u, seq += 2) {
         const uint32_t blk = seq >> 1;
         if (!row_wait(s_full0 + 8 * t, count & 1u)) break;
@@ -528,7 +534,6 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
             const float mn = grew ? top - 7.f : m, alpha = grew ? ex2_approx(m - mn) : 1.f;
             m = mn;
             l *= alpha;
-            l_r *= alpha;
             if (u > 0) {  // (the product before this unit's scores is done: they came after it)
               tmem_ld_wait();
 #pragma unroll 1
@@ -550,27 +555,30 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
             const uint32_t there = __float_as_uint(scale.w);
             const float qf = qa * scale.x, add = scale.y - ref;
             const unsigned long long qf2 = pk2(qf, qf), add2 = pk2(add, add);
-            unsigned long long sum2 = pk2(0.f, 0.f), sum_r2 = sum2;
-            uint32_t w[16];
+            const unsigned long long minus1 = pk2(-1.f, -1.f);
+            unsigned long long sum2 = pk2(0.f, 0.f);
 #pragma unroll
-            for (int i = 0; i < 32; i += 2) {  // (pairs: one instruction for two scores)
-              float x0, x1;
-              upk2(ffma2(pk2(f32(s[i]), f32(s[i + 1])), qf2, add2), x0, x1);
-              if (there != 0xffffffffu) {
-                x0 = there >> i & 1 ? x0 : -INFINITY;
-                x1 = there >> (i + 1) & 1 ? x1 : -INFINITY;
+            for (int i0 = 0; i0 < 32; i0 += 16) {
+              uint32_t w[8], rest[8];
+#pragma unroll
+              for (int i = i0; i < i0 + 16; i += 2) {  // (pairs: one instruction for two scores)
+                float x0, x1;
+                upk2(ffma2(pk2(f32(s[i]), f32(s[i + 1])), qf2, add2), x0, x1);
+                if (there != 0xffffffffu) {
+                  x0 = there >> i & 1 ? x0 : -INFINITY;
+                  x1 = there >> (i + 1) & 1 ? x1 : -INFINITY;
+                }
+                const float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
+                sum2 = fadd2(pk2(p0, p1), sum2);
+                const float h0 = f32(__float_as_uint(p0) & 0xffffe000u), h1 = f32(__float_as_uint(p1) & 0xffffe000u);
+                w[(i - i0) / 2] = pack_f16x2(h0, h1);
+                upk2(ffma2(pk2(h0, h1), minus1, pk2(p0, p1)), x0, x1);
+                rest[(i - i0) / 2] = pack_f16x2(x0, x1);
               }
-              const float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
-              sum2 = fadd2(pk2(p0, p1), sum2);
-              const uint32_t hi = pack_f16x2(p0, p1);
-              const float2 q = __half22float2(*reinterpret_cast<const __half2*>(&hi));
-              sum_r2 = fadd2(pk2(q.x, q.y), sum_r2);
-              w[i / 2] = hi;
+              tmem_st8(s_at + 32 * c + i0 / 2, w);
+              tmem_st8(s_at + 32 * c + 16 + i0 / 2, rest);
             }
-            tmem_st16(s_at + 32 * c, w);
             float lo, hi;
-            upk2(sum_r2, lo, hi);
-            l_r = fmaf(lo + hi, scale.z, l_r);
             upk2(sum2, lo, hi);
             l = fmaf(lo + hi, scale.z, l);
           };
@@ -595,7 +603,6 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
       tc_fence_after();
       if (ok && band) {
         float* part = scratch.part + ((2 * (int64_t)blockIdx.x + (it.from == 0)) * TC_ROWS + row) * (HD + 4);
-        const float right = l_r != 0.f ? l / l_r : 1.f;
         KaRow mine{};
         if (live && it.whole()) mine = finish_row(a, it.row0, it.g * rep, it.first, rep, row, m, l);
 #pragma unroll 1
@@ -606,7 +613,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
           if (!live) continue;
 #pragma unroll
           for (int i = 0; i < 32; i += 4) {
-            const float4 x = make_float4(f32(o[i]) * right, f32(o[i + 1]) * right, f32(o[i + 2]) * right, f32(o[i + 3]) * right);
+            const float4 x = make_float4(f32(o[i]), f32(o[i + 1]), f32(o[i + 2]), f32(o[i + 3]));
             if (it.whole())
               finish4<HD>(a, mine, 32 * c + i, x);
             else
@@ -630,6 +637,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
         }
       }
     }
+    registers_fewer<TC_REGS>();
   }
   tc_fence_before();
   __syncthreads();

@@ -24,7 +24,7 @@ def ops():
     ctx.close()
 
 
-def _pool(rng, lens, heads, kv, hd, page_len, fp8_format, spread=3, k_scale=1.0):
+def _pool(rng, lens, heads, kv, hd, page_len, fp8_format, spread=3, k_scale=1.0, jump=0):
     """A cache holding sequences of these lengths in shuffled pages, every place past a length filled
     with NaN, and the values it stores in 64 bits (per sequence [n][kv][hd])."""
     need = [-(-n // page_len) for n in lens]
@@ -36,6 +36,8 @@ def _pool(rng, lens, heads, kv, hd, page_len, fp8_format, spread=3, k_scale=1.0)
     host = {}
     for name in ("k", "v"):
         size = np.exp2(rng.integers(-spread, spread + 1, (pages, kv, page_len, 1)).astype(np.float64))
+        if name == "v" and jump:  # whole pages of large and of small values
+            size = size * np.exp2(jump * (np.arange(pages) % 2 * 2.0 - 1.0))[:, None, None, None]
         a = rng.normal(0, 1, (pages, kv, page_len, hd)) * size * (k_scale if name == "k" else 1.0)
         if fp8_format:
             flat = a.reshape(-1, hd)
@@ -97,8 +99,11 @@ def _reference(q, k, v, new, causal, scale):
 
 
 def _check(ops, rng, lens, news, heads, kv, hd, page_len, fp8_format, causal=False, scale=None, max_new=None,
-           q_scale=1.0, **pool):
+           q_scale=1.0, wide=0, **pool):
     cache, table, values = _pool(rng, lens, heads, kv, hd, page_len, fp8_format, **pool)
+    if wide:  # a page table for sequences of up to `wide` positions
+        pad = torch.full((len(lens), -(-wide // page_len)), -1, dtype=torch.int32, device="cuda")
+        table = torch.cat([table, pad], 1).contiguous()
     rows = sum(news)
     gap = 2  # rows of no sequence, before the first
     q = torch.from_numpy(rng.normal(0, q_scale, (rows + gap, heads + 2, hd))).to(torch.bfloat16).cuda()
@@ -152,6 +157,67 @@ def test_ragged_blocks(ops, heads, kv, hd, page_len, causal, fp8_format):
     lens = [40, 0, 300, 129, 5, 64, 70, 257, 1]
     news = [32, 3, 1, 17, 9, 0, 70, 33, 1]
     _check(ops, rng, lens, news, heads, kv, hd, page_len, fp8_format, causal=causal)
+
+
+# Many rows that share a kv head are given to another kernel where the table's width promises enough
+# keys: at this width all that follow (the most that any row count asks for is 26000 units of 128
+# keys of a kv head).
+WIDE = 3_400_000
+
+
+@pytest.mark.parametrize("fp8_format", [True, False])
+@pytest.mark.parametrize("heads,kv,hd,page_len", [(4, 4, 64, 32), (2, 2, 128, 64), (14, 2, 128, 16), (8, 1, 64, 128),
+                                                  (28, 4, 128, 256), (20, 1, 128, 16)])
+def test_many_rows(ops, heads, kv, hd, page_len, fp8_format):
+    """Up to 70 new positions (1400 rows of a kv head), ragged, one and two row tiles and several."""
+    rng = np.random.default_rng(heads * hd + page_len + 1)
+    lens = [40, 0, 300, 129, 5, 64, 70, 257, 1, 128, 511]
+    news = [32, 3, 1, 17, 9, 0, 70, 33, 1, 40, 13]
+    _check(ops, rng, lens, news, heads, kv, hd, page_len, fp8_format, wide=WIDE)
+
+
+@pytest.mark.parametrize("fp8_format", [True, False])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_many_rows_split_and_joined(ops, hd, fp8_format):
+    rng = np.random.default_rng(20 + hd)
+    _check(ops, rng, [9001, 700], [33, 40], 7, 1, hd, 64, fp8_format, wide=WIDE)
+    _check(ops, rng, [5000], [70], 2, 2, hd, 16, fp8_format, wide=WIDE)
+
+
+@pytest.mark.parametrize("fp8_format", [True, False])
+@pytest.mark.parametrize("wide,news", [(0, [1, 3]), (0, [20, 30]), (WIDE, [40, 64])])
+def test_values_of_unlike_size(ops, wide, news, fp8_format):
+    """Values that differ by 2^24 from page to page, and by 2^40 within one: what is small is not lost where
+    it is all that a row sees much of, and what it adds to the sum of the weights counts."""
+    rng = np.random.default_rng(21)
+    _check(ops, rng, [100, 999], news, 4, 1, 64, 64, fp8_format, wide=wide, jump=12, spread=0, k_scale=2.0 ** -6)
+    _check(ops, rng, [150, 600], news, 4, 1, 128, 32, fp8_format, wide=wide, jump=12, spread=1, k_scale=6.0)
+    _check(ops, rng, [100, 999], news, 4, 1, 128, 32, fp8_format, wide=wide, spread=20, k_scale=2.0 ** -20)
+
+
+@pytest.mark.parametrize("fp8_format", [True, False])
+def test_many_rows_of_peaked_scores(ops, fp8_format):
+    rng = np.random.default_rng(22)
+    _check(ops, rng, [100, 999], [40, 64], 4, 1, 64, 32, fp8_format, wide=WIDE, k_scale=30.0, q_scale=3.0)
+
+
+@pytest.mark.parametrize("fp8_format", [True, False])
+def test_many_rows_a_page_outside_the_cache_is_reported(ops, fp8_format):
+    rng = np.random.default_rng(23)
+    cache, table, values = _pool(rng, [40, 200], 4, 1, 64, 16, fp8_format)
+    q = torch.from_numpy(rng.normal(0, 1, (64, 4, 64))).to(torch.bfloat16).cuda()
+    starts = torch.tensor([0, 24, 64], dtype=torch.int32, device="cuda")
+    out = torch.zeros(64, 4, 64, dtype=torch.bfloat16, device="cuda")
+    lens = torch.tensor([40, 200], dtype=torch.int32, device="cuda")
+    wide = torch.full((2, 212_500), -1, dtype=torch.int32, device="cuda")
+    wide[:, :table.shape[1]] = table
+    wide[0, 1] = cache.n_pages
+    ops.kv_attention(cache, q, starts, wide, lens, out, max_new=40)
+    with pytest.raises(dcl.DcleapError, match="outside the paged cache"):
+        ops.synchronise()
+    o, _, A, _ = _reference(q[24:].float().cpu().numpy().astype(np.float64), values["k"][1], values["v"][1], 40, False,
+                            64 ** -0.5)
+    assert (np.abs(out[24:].float().cpu().numpy() - o) <= (2.0 ** -8 + 2.0 ** -12) * A).all()
 
 
 @pytest.mark.parametrize("fp8_format", [True, False])
