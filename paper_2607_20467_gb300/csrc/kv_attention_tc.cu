@@ -4,8 +4,8 @@
 //
 // Per unit of 128 keys: S = Q K^T into TMEM; P = exp2(S scaled + e - m) in two fp16 parts (11 bits and what
 // they leave) takes the place of its scores there; O += P V in TMEM.  (One part costs a row that sees
-// little but a few keys up to 2^-11 of its result; it took 113 us where two take 126, at 16 sequences
-// of 8192 keys, 224 rows a kv head.)  P, m, l and the exponents e of the values are those of kv_attention.cu; a
+// little but a few keys up to 2^-11 of its result, and saves 5 us of 112 at 16 sequences of 8192 keys,
+// 224 rows a kv head.)  P, m, l and the exponents e of the values are those of kv_attention.cu; a
 // thread owns a row, so its statistics need no exchange.
 //
 // FP8 pages.  Eight warps copy codes into shared memory (16-byte asynchronous copies, one unit
@@ -38,7 +38,7 @@ namespace dcl {
 namespace {
 
 constexpr int TC_ROWS = 256;      // rows of an item
-constexpr int TC_START = 6;       // units of keys that beginning an item takes
+constexpr int TC_START = 2;       // units of keys that beginning an item takes
 constexpr int TC_THREADS = 544;
 constexpr int TC_REGS = 96, TC_REGS_ROWS = 128, TC_REGS_COPY = 64;
 static_assert(TC_REGS_ROWS + TC_REGS_COPY == 2 * TC_REGS, "the rows' warps take what as many copying warps give");
@@ -412,6 +412,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     }
     copy_wait<0>();
     if (!ok) gave_up();
+    __syncwarp();
     registers_more<TC_REGS>();  // (waits for the rows' warps to be done)
   } else if (warp == 16) {
     // ================================================================ MMAs
@@ -550,13 +551,17 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
           }
           // ---- P, into the places of its scores: per 32 keys 16 columns of fp16 pairs
           const float ref = m == -INFINITY ? 0.f : m;
-          auto weigh = [&](const uint32_t (&s)[32], int c) {
+          auto weigh = [&](uint32_t (&s)[32], int c) {
             const float4 scale = ld_shared_v4(scales + 16 * c);
             const uint32_t there = __float_as_uint(scale.w);
-            const float qf = qa * scale.x, add = scale.y - ref;
+            const float qf = fmaxf(qa * scale.x, 1.2e-38f), add = scale.y - ref;  // (not 0: a masked score is -inf)
             const unsigned long long qf2 = pk2(qf, qf), add2 = pk2(add, add);
             const unsigned long long minus1 = pk2(-1.f, -1.f);
             unsigned long long sum2 = pk2(0.f, 0.f);
+            if (there != 0xffffffffu) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) s[i] = there >> i & 1 ? s[i] : 0xff800000u;
+            }
 #pragma unroll
             for (int i0 = 0; i0 < 32; i0 += 16) {
               uint32_t w[8], rest[8];
@@ -564,10 +569,6 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
               for (int i = i0; i < i0 + 16; i += 2) {  // (pairs: one instruction for two scores)
                 float x0, x1;
                 upk2(ffma2(pk2(f32(s[i]), f32(s[i + 1])), qf2, add2), x0, x1);
-                if (there != 0xffffffffu) {
-                  x0 = there >> i & 1 ? x0 : -INFINITY;
-                  x1 = there >> (i + 1) & 1 ? x1 : -INFINITY;
-                }
                 const float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
                 sum2 = fadd2(pk2(p0, p1), sum2);
                 const float h0 = f32(__float_as_uint(p0) & 0xffffe000u), h1 = f32(__float_as_uint(p1) & 0xffffe000u);
@@ -608,6 +609,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
 #pragma unroll 1
         for (int c = 0; c < HD / 32; ++c) {
           uint32_t o[32];
+          __syncwarp();
           tmem_ld32(o_at + 32 * c, o);
           tmem_ld_wait();
           if (!live) continue;
@@ -625,6 +627,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
       if (!it.whole()) {
         int c0, c1;
         line.sharers(walk, it, c0, c1);
+        __syncwarp();
         rows_bar();
         if (threadIdx.x == 0) {
           __threadfence();  // (the rows' writes, which the barrier ordered before)
@@ -635,11 +638,13 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
           }
           __threadfence();
         }
+        __syncwarp();  // (aligned instructions follow)
       }
     }
     registers_fewer<TC_REGS>();
   }
   tc_fence_before();
+  __syncwarp();
   __syncthreads();
   tc_fence_after();
   if (warp == 16) tmem_dealloc(tmem, 512);
