@@ -21,9 +21,19 @@
 // The reference m, 7 below a row's largest score when it is taken, moves only when a unit's passes it by
 // more than 15; O is scaled then.
 //
+// 16 sequences of 8192 positions, FP8, 28 / 4 heads of 128, 32 new positions each (224 rows a kv head;
+// 143 MB, 60 GFLOP): 112.5 us, 0.27 of the tensor rate.  Neither memory
+// (0.18) nor the tensor pipe (0.4 busy) bounds it but the chain S -> maximum -> weights -> O of a
+// tile, with two tiles in turn: of 6600 cycles a unit a row's warp takes 3300 for the weights, 650 for
+// the maximum, waits 1800 for S and has 900 for an item's q and results; leaving any one of them out
+// saves 5 us or less.  The rest is the spread of the CTAs' work (74 - 97 us) and the joins (12 - 14 us).
+//
 // Roles (544 threads): warps 0-3 and 4-7 have the rows of the two tiles; warps 8-11 copy and widen
 // keys, 12-15 values (one group for both was the slowest link: 7800 cycles a unit); warp 16
-// allocates TMEM and issues the MMAs.  Every wait is bounded (DERR_WAIT_TIMEOUT).
+// allocates TMEM and issues the MMAs.  17 warps leave 96 registers a thread; the copying warps give 32 of
+// theirs to the rows' while they run (126 us against 141, before the last steps).  Two warps for a
+// tile's 32 rows, half the keys each, were no faster (115 us).  Every wait is bounded
+// (DERR_WAIT_TIMEOUT).
 #include <cuda_fp8.h>
 
 #include <algorithm>

@@ -6,6 +6,12 @@
 // codes (E4M3) and one exponent e, a ~ code * 2^e with e the least integer that fits the largest
 // finite component into 448 * 2^e (at least KV_EXP_MIN), so scaling by 2^-e and widening a code to
 // bf16 are both exact: the code's rounding is the only one.
+//
+// Both kernels are bound by memory.  A thread has 16 components of a vector (two 16-byte loads, one
+// 16-byte store of codes) of two vectors at once; hd / 16 threads find a vector's maximum by
+// shuffles.  12288 positions of 32 heads x 128 (302 MB): written in 47.2 us, 6.4 TB/s, 0.94 of the
+// measured copy rate; read back in 52.9 us, 5.7 TB/s, 0.84 (two thirds of that traffic are
+// writes).  32 positions: 2 to 3 us of kernel in a call of 5.1.
 #include <cuda_fp8.h>
 
 #include "common.cuh"
