@@ -652,7 +652,7 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
   }
   for (int i = 0; i < todo[0].rows; ++i) {
     const KaJoin j = todo[1 + i];
-    join_parts<HD, C::ROWS, C::THREADS>(a, j, rep, scratch.part, reinterpret_cast<float2*>(smem),
+    join_parts<HD, C::ROWS, C::THREADS, false>(a, j, 0, rep, scratch.part, reinterpret_cast<float2*>(smem),
                                         reinterpret_cast<KaRow*>(smem + C::WT + C::ROWS * 32), threadIdx.x,
                                         [] { __syncthreads(); });
     __syncthreads();
@@ -685,7 +685,7 @@ cudaError_t launch_rows(const KvPool& kv, const KvAttn& a, const KaScratch& s, i
 // what comes on top, us (FP8, hd 128; bf16 and hd 64 within 15 %): 0.008 for 32 rows and 20; 0.015
 // for up to 128 rows, 0.018 for 256, and 46.  8 sequences of 3000 positions: 28 / 4 heads and 16 new
 // positions (112 rows) 44.8 here against 47.3 there, 32 new 61.5 against 60.2; 32 heads and 64 new
-// 119.9 against 137; but 16 x 8192 with 28 / 4 heads and 32 new 241 against 113.  Lengths are known
+// 119.9 against 137; but 16 x 8192 with 28 / 4 heads and 32 new 241 against 108.  Lengths are known
 // to the device only: the page table's width stands for them.
 bool kv_attention_many_rows(const KvPool& kv, const KvAttn& a) {
   const int64_t rows = (int64_t)a.max_new * (a.H / kv.G);

@@ -613,7 +613,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
       if (t < tiles) row_wait(p_empty0 + 8 * t, (count & 1u) ^ 1u);
       tc_fence_after();
       if (ok && band) {
-        float* part = scratch.part + ((2 * (int64_t)blockIdx.x + (it.from == 0)) * TC_ROWS + row) * (HD + 4);
+        using Part = KaPart<HD, TC_ROWS, true>;
+        float* part = scratch.part + (2 * (int64_t)blockIdx.x + (it.from == 0)) * Part::FLOATS;
         KaRow mine{};
         if (live && it.whole()) mine = finish_row(a, it.row0, it.g * rep, it.first, rep, row, m, l);
 #pragma unroll 1
@@ -629,10 +630,10 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
             if (it.whole())
               finish4<HD>(a, mine, 32 * c + i, x);
             else
-              *reinterpret_cast<float4*>(part + 32 * c + i) = x;
+              *reinterpret_cast<float4*>(part + Part::four(row, 8 * c + i / 4)) = x;
           }
         }
-        if (live && !it.whole()) *reinterpret_cast<float2*>(part + HD) = make_float2(m, l);
+        if (live && !it.whole()) *reinterpret_cast<float2*>(part + Part::ml(row)) = make_float2(m, l);
       }
       if (!it.whole()) {
         int c0, c1;
@@ -665,7 +666,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
       KaJoin k = j;
       k.first += r0;
       k.rows = min(some, j.rows - r0);
-      join_parts<HD, TC_ROWS, TC_THREADS>(a, k, rep, scratch.part + (int64_t)r0 * (HD + 4),
+      join_parts<HD, TC_ROWS, TC_THREADS, true>(a, k, r0, rep, scratch.part,
                                           reinterpret_cast<float2*>(smem + TC_ROWS * 8), reinterpret_cast<KaRow*>(smem),
                                           threadIdx.x, [] { __syncthreads(); });
       __syncthreads();

@@ -180,9 +180,18 @@ struct KaLine {
   }
 };
 
+// Where a part of an item's rows has four components of a row, and its {m, l}: row by row, or
+// (BY_FOUR) rows next to one another, for writers that have a row a thread.
+template <int HD, int ROWS, bool BY_FOUR>
+struct KaPart {
+  static constexpr int FLOATS = ROWS * (HD + 4);
+  static __device__ __forceinline__ int four(int r, int q) { return BY_FOUR ? (q * ROWS + r) * 4 : r * (HD + 4) + 4 * q; }
+  static __device__ __forceinline__ int ml(int r) { return BY_FOUR ? HD * ROWS + 2 * r : r * (HD + 4) + HD; }
+};
+
 // Scratch of a launch: the parts of shared items, and how many of each have come.
 struct KaScratch {
-  float* part;  // [2 * CTAs][ROWS][HD + 4]: O, m, l (a CTA's items that it does not begin, and does)
+  float* part;  // [2 * CTAs] of KaPart: O, m, l (a CTA's items that it does not begin, and does)
   int* count;   // [CTAs], by the CTA that begins the item; zero between launches
 };
 
@@ -229,18 +238,19 @@ __device__ __forceinline__ float exp2_fast(float x) {
 // every part's {m, l} into shared memory (w, [rows][parts]) at once, a row's weights by a thread or
 // a warp (what its components need in row); then four components of a row a thread, 12 to 16 loads in
 // flight (one takes about 1000 cycles here: a warp per row, part after part, took 35000 for 38
-// parts and 17000 for two parts of 32 rows).
-template <int HD, int ROWS, int THREADS, typename Sync>
-__device__ __forceinline__ void join_parts(const KvAttn& a, const KaJoin& it, int rep, const float* parts, float2* w,
+// parts and 17000 for two parts of 32 rows).  it's rows begin at row r0 of the parts.
+template <int HD, int ROWS, int THREADS, bool BY_FOUR, typename Sync>
+__device__ __forceinline__ void join_parts(const KvAttn& a, const KaJoin& it, int r0, int rep, const float* parts, float2* w,
                                            KaRow* row, int tid, Sync sync) {
-  constexpr int PART = HD + 4, Q = HD / 4;
+  using P = KaPart<HD, ROWS, BY_FOUR>;
+  constexpr int Q = HD / 4;
   const int warp = tid >> 5, lane = tid & 31, n = it.parts;
   // (the first CTA's part is its second, the others' their first)
-  const float* first = parts + (2 * (int64_t)it.c0 + 1) * ROWS * PART;
-  auto part_of = [&](int c) { return first + (int64_t)max(2 * c - 1, 0) * (ROWS * PART); };
+  const float* first = parts + (2 * (int64_t)it.c0 + 1) * P::FLOATS;
+  auto part_of = [&](int c) { return first + (int64_t)max(2 * c - 1, 0) * P::FLOATS; };
   for (int i = tid; i < it.rows * n; i += THREADS) {
     const int r = i / n;
-    w[i] = __ldcg(reinterpret_cast<const float2*>(part_of(i - r * n) + r * PART + HD));
+    w[i] = __ldcg(reinterpret_cast<const float2*>(part_of(i - r * n) + P::ml(r0 + r)));
   }
   sync();
   if (n <= 8) {
@@ -273,18 +283,22 @@ __device__ __forceinline__ void join_parts(const KvAttn& a, const KaJoin& it, in
     }
   }
   sync();
+  // (by fours: a warp has eight rows of four neighbouring fours, whole sectors to read and to write)
+  auto row_of = [&](int t) { return BY_FOUR ? t / (8 * Q) * 8 + (t >> 2 & 7) : t / Q; };
+  auto four_of = [&](int t) { return BY_FOUR ? (t / 32) % (Q / 4) * 4 + (t & 3) : t % Q; };
+  const int all = (BY_FOUR ? (it.rows + 7) / 8 * 8 : it.rows) * Q;
   auto tasks = [&](auto tasks_, auto parts_) {
     constexpr int T = decltype(tasks_)::value, U = decltype(parts_)::value;
 #pragma unroll 1
-    for (int t0 = tid; t0 < it.rows * Q; t0 += T * THREADS) {
+    for (int t0 = tid; t0 < all; t0 += T * THREADS) {
       float4 acc[T];
       const float* from[T];
       const float2* wr[T];
 #pragma unroll
       for (int k = 0; k < T; ++k) {
-        const int t = min(t0 + k * THREADS, it.rows * Q - 1), r = t / Q;
+        const int t = min(t0 + k * THREADS, all - 1), r = min(row_of(t), it.rows - 1);
         acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-        from[k] = first + r * PART + 4 * (t % Q);
+        from[k] = first + P::four(r0 + r, four_of(t));
         wr[k] = w + r * n;
       }
 #pragma unroll 1
@@ -294,7 +308,7 @@ __device__ __forceinline__ void join_parts(const KvAttn& a, const KaJoin& it, in
         for (int i = 0; i < U; ++i)  // (past the end: the last again, without weight)
 #pragma unroll
           for (int k = 0; k < T; ++k)
-            y[k][i] = __ldcg(reinterpret_cast<const float4*>(from[k] + (int64_t)max(2 * min(c + i, n - 1) - 1, 0) * (ROWS * PART)));
+            y[k][i] = __ldcg(reinterpret_cast<const float4*>(from[k] + (int64_t)max(2 * min(c + i, n - 1) - 1, 0) * P::FLOATS));
 #pragma unroll
         for (int i = 0; i < U; ++i)
 #pragma unroll
@@ -304,8 +318,8 @@ __device__ __forceinline__ void join_parts(const KvAttn& a, const KaJoin& it, in
 #pragma unroll
       for (int k = 0; k < T; ++k) {
         const int t = t0 + k * THREADS;
-        if (t >= it.rows * Q) break;
-        finish4<HD>(a, row[t / Q], 4 * (t % Q), acc[k]);
+        if (t >= all) break;
+        if (!BY_FOUR || row_of(t) < it.rows) finish4<HD>(a, row[row_of(t)], 4 * four_of(t), acc[k]);
       }
     }
   };
