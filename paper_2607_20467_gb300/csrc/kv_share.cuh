@@ -249,8 +249,8 @@ __device__ __forceinline__ void join_parts(const KvAttn& a, const KaJoin& it, in
   const float* first = parts + (2 * (int64_t)it.c0 + 1) * P::FLOATS;
   auto part_of = [&](int c) { return first + (int64_t)max(2 * c - 1, 0) * P::FLOATS; };
   for (int i = tid; i < it.rows * n; i += THREADS) {
-    const int r = i / n;
-    w[i] = __ldcg(reinterpret_cast<const float2*>(part_of(i - r * n) + P::ml(r0 + r)));
+    const int c = i / it.rows, r = i - c * it.rows;
+    w[r * n + c] = __ldcg(reinterpret_cast<const float2*>(part_of(c) + P::ml(r0 + r)));
   }
   sync();
   if (n <= 8) {
