@@ -22,7 +22,7 @@
 // more than 15; O is scaled then.
 //
 // 16 sequences of 8192 positions, FP8, 28 / 4 heads of 128, 32 new positions each (224 rows a kv head;
-// 143 MB, 60 GFLOP): 112.5 us, 0.27 of the tensor rate.  Neither memory
+// 143 MB, 60 GFLOP): 108.5 us, 0.28 of the tensor rate.  Neither memory
 // (0.18) nor the tensor pipe (0.4 busy) bounds it but the chain S -> maximum -> weights -> O of a
 // tile, with two tiles in turn: of 6600 cycles a unit a row's warp takes 3300 for the weights, 650 for
 // the maximum, waits 1800 for S and has 900 for an item's q and results; leaving any one of them out
@@ -30,10 +30,9 @@
 //
 // Roles (544 threads): warps 0-3 and 4-7 have the rows of the two tiles; warps 8-11 copy and widen
 // keys, 12-15 values (one group for both was the slowest link: 7800 cycles a unit); warp 16
-// allocates TMEM and issues the MMAs.  17 warps leave 96 registers a thread; the copying warps give 32 of
-// theirs to the rows' while they run (126 us against 141, before the last steps).  Two warps for a
-// tile's 32 rows, half the keys each, were no faster (115 us).  Every wait is bounded
-// (DERR_WAIT_TIMEOUT).
+// allocates TMEM and issues the MMAs.  17 warps leave 96 registers a thread: a row's warp holds 32 scores at
+// a time (the next 32 on their way as well spill: 137 us).  Two warps for a tile's 32 rows, half the
+// keys each, were no faster (115 us).  Every wait is bounded (DERR_WAIT_TIMEOUT).
 #include <cuda_fp8.h>
 
 #include <algorithm>
@@ -50,8 +49,6 @@ namespace {
 constexpr int TC_ROWS = 256;      // rows of an item
 constexpr int TC_START = 2;       // units of keys that beginning an item takes
 constexpr int TC_THREADS = 544;
-constexpr int TC_REGS = 96, TC_REGS_ROWS = 128, TC_REGS_COPY = 64;
-static_assert(TC_REGS_ROWS + TC_REGS_COPY == 2 * TC_REGS, "the rows' warps take what as many copying warps give");
 constexpr int TC_BOX = 128 * 128; // 128 rows of 128 bytes, swizzled
 constexpr int TC_JOIN = 8000;     // rows x parts joined at a time
 
@@ -130,12 +127,6 @@ __device__ __forceinline__ uint32_t times(uint32_t x, __half2 f) {
   __half2 y = __hmul2(*reinterpret_cast<__half2*>(&x), f);
   return *reinterpret_cast<uint32_t*>(&y);
 }
-
-// Registers a thread of this warpgroup has from here on (its four warps come together).
-template <int N>
-__device__ __forceinline__ void registers_more() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
-template <int N>
-__device__ __forceinline__ void registers_fewer() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
 // The MMAs of an item (the whole warp; one lane issues).  Its operands are made known as the warp's, in
 // uniform registers: else an issue takes about 100 cycles, more than most of the products.
@@ -266,7 +257,6 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     // ================================================================ copies, widening
     // Keys or values of a unit: warp w of the four has keys 32 w .. 32 w + 31, lane l knows of key 32 w + l
     // (its page and exponents); they are copied in chunks of 16 bytes.
-    registers_fewer<TC_REGS_COPY>();
     const int values = warp >= 12, w4 = warp & 3;
     constexpr int CH = FP8 ? HD / 16 : HD / 8;       // chunks of a vector
     constexpr int PK = CH / 4;                       // this lane's of a key: key (lane >> 2) + 8 i, chunk (lane & 3) + 4 j
@@ -422,8 +412,6 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     }
     copy_wait<0>();
     if (!ok) gave_up();
-    __syncwarp();
-    registers_more<TC_REGS>();  // (waits for the rows' warps to be done)
   } else if (warp == 16) {
     // ================================================================ MMAs
     uint32_t seq = 0, items = 0, units = 0;  // items, units: of tile 0 in the low half, of tile 1 in the high
@@ -438,7 +426,6 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     mbar_wait(drain, 0, &no_abort);
   } else {
     // ================================================================ rows
-    registers_more<TC_REGS_ROWS>();  // (waits for the copying warps to have given theirs)
     const int t = warp >> 2, quarter = warp & 3, r = 32 * quarter + lane;  // row r of tile t
     const uint32_t s_at = tmem + 128u * t + ((uint32_t)(32 * quarter) << 16);
     const uint32_t o_at = tmem + 256u + (uint32_t)(HD * t) + ((uint32_t)(32 * quarter) << 16);
@@ -511,7 +498,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
         tc_fence_after();
         if (band) {
           const uint32_t scales = base + C::EXP + (blk & 3) * 64;
-          uint32_t s0[32], s1[32];  // 32 scores, and the next ones
+          uint32_t s0[32];  // 32 scores
           // ---- the row's largest score
           float top = -INFINITY;
           auto largest = [&](uint32_t (&s)[32], int c) {
@@ -529,15 +516,11 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
             }
             top = fmaxf(top, fmaf(fmaxf(a0, a1), qa * scale.x, scale.y));
           };
-          tmem_ld32(s_at, s0);
 #pragma unroll 1
-          for (int c = 0; c < 4; c += 2) {
+          for (int c = 0; c < 4; ++c) {
+            tmem_ld32(s_at + 32 * c, s0);
             tmem_ld_wait();
-            tmem_ld32(s_at + 32 * (c + 1), s1);
             largest(s0, c);
-            tmem_ld_wait();
-            tmem_ld32(s_at + 32 * ((c + 2) & 3), s0);  // (in the end the first again)
-            largest(s1, c + 1);
           }
           // ---- a larger reference where that passes it by more than 15, or is the row's first
           const bool grew = top > m + 15.f;
@@ -594,13 +577,12 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
             l = fmaf(lo + hi, scale.z, l);
           };
 #pragma unroll 1
-          for (int c = 0; c < 4; c += 2) {
-            tmem_ld_wait();
-            tmem_ld32(s_at + 32 * (c + 1), s1);
+          for (int c = 3; c >= 0; --c) {  // (the last 32 are here still)
+            if (c < 3) {
+              tmem_ld32(s_at + 32 * c, s0);
+              tmem_ld_wait();
+            }
             weigh(s0, c);
-            tmem_ld_wait();
-            if (c == 0) tmem_ld32(s_at + 64, s0);
-            weigh(s1, c + 1);
           }
           tmem_st_wait();
         }
@@ -652,7 +634,6 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
         __syncwarp();  // (aligned instructions follow)
       }
     }
-    registers_fewer<TC_REGS>();
   }
   tc_fence_before();
   __syncwarp();
