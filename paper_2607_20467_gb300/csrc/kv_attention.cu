@@ -7,9 +7,9 @@
 // O in registers, its own ring of key / value tiles in shared memory (16-byte asynchronous copies;
 // no barrier in the loop).  The tensor work is far below its limit as long as the keys arrive from
 // memory, which is what bounds a call of few rows.  With FP8 pages, 28 / 4 heads of 128, one row a
-// sequence: 2 sequences of 131071 positions (271 MB) in 58.5 us, 4.6 TB/s over the whole launch, of
-// which beginning and joining 38 parts an item take about 11; 64 ragged sequences to 4096 (140 MB) in
-// 37 us, 3.8 TB/s, of which ragged ends, beginning and joins take about 12; one of 512 positions,
+// sequence: 2 sequences of 131071 positions (271 MB) in 57.2 us, 4.7 TB/s over the whole launch, of
+// which beginning takes 2, joining 38 parts an item 7 to 9; 64 ragged sequences to 4096 (140 MB) in
+// 37 us, 3.8 TB/s: beginning 3.4, the keys 25 on average and 31 in the last CTA, joins 2; one of 512 positions,
 // 32 heads, 9.2 us, all latency.  bf16 pages, 8 sequences of 1536, 32 heads, 32 rows each (201 MB):
 // 50 us, 4.1 TB/s, the products' issue (P in two parts) as near its limit as memory.
 //
@@ -685,7 +685,7 @@ cudaError_t launch_rows(const KvPool& kv, const KvAttn& a, const KaScratch& s, i
 // what comes on top, us (FP8, hd 128; bf16 and hd 64 within 15 %): 0.008 for 32 rows and 20; 0.015
 // for up to 128 rows, 0.018 for 256, and 46.  8 sequences of 3000 positions: 28 / 4 heads and 16 new
 // positions (112 rows) 44.8 here against 47.3 there, 32 new 61.5 against 60.2; 32 heads and 64 new
-// 119.9 against 137; but 16 x 8192 with 28 / 4 heads and 32 new 241 against 108.  Lengths are known
+// 119.9 against 137; but 16 x 8192 with 28 / 4 heads and 32 new 241 against 109.  Lengths are known
 // to the device only: the page table's width stands for them.
 bool kv_attention_many_rows(const KvPool& kv, const KvAttn& a) {
   const int64_t rows = (int64_t)a.max_new * (a.H / kv.G);

@@ -22,11 +22,11 @@
 // more than 15; O is scaled then.
 //
 // 16 sequences of 8192 positions, FP8, 28 / 4 heads of 128, 32 new positions each (224 rows a kv head;
-// 143 MB, 60 GFLOP): 108.5 us, 0.28 of the tensor rate.  Neither memory
-// (0.18) nor the tensor pipe (0.4 busy) bounds it but the chain S -> maximum -> weights -> O of a
+// 143 MB, 60 GFLOP): 108.5 us, 0.28 of the tensor rate.  Neither memory (0.18) nor the tensor pipe
+// (0.45 busy, P's second part included) bounds it but the chain S -> maximum -> weights -> O of a
 // tile, with two tiles in turn: of 6600 cycles a unit a row's warp takes 3300 for the weights, 650 for
 // the maximum, waits 1800 for S and has 900 for an item's q and results; leaving any one of them out
-// saves 5 us or less.  The rest is the spread of the CTAs' work (74 - 97 us) and the joins (12 - 14 us).
+// saves 5 us or less.  The CTAs' work spreads over 74 to 97 us, and the joins come after it.
 //
 // Roles (544 threads): warps 0-3 and 4-7 have the rows of the two tiles; warps 8-11 copy and widen
 // keys, 12-15 values (one group for both was the slowest link: 7800 cycles a unit); warp 16
@@ -542,7 +542,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
               }
             }
           }
-          // ---- P, into the places of its scores: per 32 keys 16 columns of fp16 pairs
+          // ---- P, into the places of its scores: per 32 keys 16 columns of fp16 pairs, and 16 of what they leave
           const float ref = m == -INFINITY ? 0.f : m;
           auto weigh = [&](uint32_t (&s)[32], int c) {
             const float4 scale = ld_shared_v4(scales + 16 * c);
