@@ -343,8 +343,9 @@ dcl_status dcl_kv_read(dcl_ctx* ctx, const dcl_kv_cache* cache, const int32_t* s
  *               positions of sequence b (from none to many; rows of no sequence stay untouched).
  *   page_table_dev int32 [batch][max_pages], seq_len_dev int32 [batch]: the pages of sequence b
  *               and how many positions it has cached (entries past them are not read).
- *   max_new     no sequence has more rows than this (a choice of kernel: results do not depend
- *               on it beyond rounding).
+ *   max_new     no sequence has more rows than this (with batch, heads and max_pages it chooses the
+ *               kernel: results do not depend on them beyond rounding; a table much wider than
+ *               the sequences are long may get the one for long sequences).
  *   causal      0: a row sees every cached position; 1: row i of the r rows of sequence b sees
  *               positions up to seq_len[b] - r + i.
  *   scale       > 0, or 0 for 1 / sqrt(head_dim).

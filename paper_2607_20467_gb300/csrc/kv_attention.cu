@@ -680,20 +680,23 @@ cudaError_t launch_rows(const KvPool& kv, const KvAttn& a, const KaScratch& s, i
 
 }  // namespace
 
-// Which kernel: the one that passes over the keys once for every 32 rows, or tcgen05 for every 256, whose
-// CTAs take longer to begin, to end and to join.  Time per unit of 128 keys over the whole GPU and
-// what comes on top, us (FP8, hd 128; bf16 and hd 64 within 15 %): 0.008 for 32 rows and 20; 0.015
-// for up to 128 rows, 0.018 for 256, and 46.  8 sequences of 3000 positions: 28 / 4 heads and 16 new
-// positions (112 rows) 44.8 here against 47.3 there, 32 new 61.5 against 60.2; 32 heads and 64 new
-// 119.9 against 137; but 16 x 8192 with 28 / 4 heads and 32 new 241 against 109.  Lengths are known
-// to the device only: the page table's width stands for them.
+// Which kernel: the one that passes over the keys once for every 32 rows, or tcgen05 for every 256, where
+// beginning an item and joining its parts (32 rows' worth here, up to 256 there) take longer.  In
+// thousandths of a us of the whole GPU a unit of 128 keys takes 8 for 32 rows here; there 15 for up to
+// 128 rows, 18 for 256, and on top 10 us an item of a CTA and 0.0175 us a row and part.  Measured, us here /
+// there, FP8, 28 / 4 heads of 128: 16 x 8192 positions, 224 rows a kv head 241 / 109; 8 x 3000: 84 rows
+// 35.7 / 37.5, 112 43.2 / 38.8, 168 52.6 / 45.8, 224 59.4 / 50.5; 4 x 8192 (ten parts an item): 112
+// rows 50.7 / 57.2, 224 72.6 / 82.1; 2 x 1000, 224 rows 21 / 37; 32 / 32 heads, 64 rows, 8 x 3000 116 /
+// 133.  bf16 and heads of 64 fall on the same sides, or within 7 %.  Lengths are known to the device
+// only: the page table's width stands for them.
 bool kv_attention_many_rows(const KvPool& kv, const KvAttn& a) {
   const int64_t rows = (int64_t)a.max_new * (a.H / kv.G);
   if (a.causal || rows <= 32) return false;
   const double units = (double)a.batch * kv.G * (((int64_t)a.max_pages * kv.page_len() + KA_UNIT - 1) / KA_UNIT);
   const int64_t rest = rows % 256;
   const double here = 8.0 * (double)((rows + 31) / 32), there = 18.0 * (double)(rows / 256) + (rest > 128 ? 18 : rest ? 15 : 0);
-  return (here - there) * units > 26000.0;
+  const double items = (double)a.batch * kv.G * (double)((rows + 255) / 256), ctas = KA_MOST / KA_CTAS;
+  return (here - there) * units > 17.5 * (double)std::min<int64_t>(rows, 256) * (ctas / items + 1) + 10000.0 * items / ctas;
 }
 
 size_t kv_attention_scratch(int sms) { return (size_t)KA_CTAS * sms * (KV_ATTN_PART_BYTES + sizeof(int)); }

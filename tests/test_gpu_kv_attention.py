@@ -160,8 +160,7 @@ def test_ragged_blocks(ops, heads, kv, hd, page_len, causal, fp8_format):
 
 
 # Many rows that share a kv head are given to another kernel where the table's width promises enough
-# keys: at this width all that follow (the most that any row count asks for is 26000 units of 128
-# keys of a kv head).
+# keys: at this width all that follow.
 WIDE = 3_400_000
 
 
