@@ -216,11 +216,12 @@ dcl_status check_device(dcl_ctx* c) {
   CUDA_TRY(c, cudaStreamSynchronize(c->stream));
   const int e = *c->h_err;
   if (e != DERR_NONE) {
-    const int zero = 0;
-    cudaMemcpy(c->derr, &zero, sizeof(int), cudaMemcpyHostToDevice);
+    // On the context's stream, whose next launch may come at once: a caller's stream need not be
+    // ordered with the default one.
+    CUDA_TRY(c, cudaMemsetAsync(c->derr, 0, sizeof(int), c->stream));
     // an aborted split-K launch may leave its counters set: clear them for the next one
-    if (c->gemm_flags) cudaMemset(c->gemm_flags, 0, sizeof(int) * c->gemm_flags_n);
-    if (c->kv_tc_scratch) cudaMemset(c->kv_tc_scratch, 0, kv_attention_tc_scratch(c->num_sms));
+    if (c->gemm_flags) CUDA_TRY(c, cudaMemsetAsync(c->gemm_flags, 0, sizeof(int) * c->gemm_flags_n, c->stream));
+    if (c->kv_tc_scratch) CUDA_TRY(c, cudaMemsetAsync(c->kv_tc_scratch, 0, KV_ATTN_COUNTERS, c->stream));
     if (e == DERR_WAIT_TIMEOUT)
       return fail(c, DCL_ERR_TIMEOUT, "a pipeline wait timed out on the device (kernel returned)");
     if (e == DERR_KV_RANGE) return fail(c, DCL_ERR_INVALID_ARG, "a slot, page or length outside the paged cache");
@@ -1498,7 +1499,7 @@ dcl_status dcl_kv_attention(dcl_ctx* c, const dcl_kv_cache* cache, const void* q
     const size_t bytes = many ? kv_attention_tc_scratch(c->num_sms) : kv_attention_scratch(c->num_sms);
     scratch = dev_alloc(c, bytes);
     if (!scratch) return fail(c, DCL_ERR_OOM, "kv_attention: scratch allocation failed");
-    CUDA_TRY(c, cudaMemsetAsync(scratch, 0, bytes, c->stream));
+    CUDA_TRY(c, cudaMemsetAsync(scratch, 0, KV_ATTN_COUNTERS, c->stream));
   }
   CUDA_TRY(c, many ? kv_attention_tc_launch(kv, a, scratch, c->num_sms, c->derr, c->stream)
                    : kv_attention_launch(kv, a, scratch, c->num_sms, c->derr, c->stream));

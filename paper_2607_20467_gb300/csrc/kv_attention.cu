@@ -45,6 +45,7 @@ namespace {
 constexpr int KA_START = 3;   // units of keys that beginning an item takes
 constexpr int KA_CTAS = 2;    // CTAs of an SM: one loads while the other begins or ends an item
 constexpr int KA_MOST = 304;  // most CTAs of a launch
+static_assert(KA_MOST * sizeof(int) <= KV_ATTN_COUNTERS, "a counter per CTA");
 
 template <int HD, bool FP8, int MT>
 struct KaCfg {
@@ -699,12 +700,11 @@ bool kv_attention_many_rows(const KvPool& kv, const KvAttn& a) {
   return (here - there) * units > 17.5 * (double)std::min<int64_t>(rows, 256) * (ctas / items + 1) + 10000.0 * items / ctas;
 }
 
-size_t kv_attention_scratch(int sms) { return (size_t)KA_CTAS * sms * (KV_ATTN_PART_BYTES + sizeof(int)); }
+size_t kv_attention_scratch(int sms) { return KV_ATTN_COUNTERS + (size_t)KA_CTAS * sms * KV_ATTN_PART_BYTES; }
 
 cudaError_t kv_attention_launch(const KvPool& kv, const KvAttn& a, void* scratch, int sms, int* err, cudaStream_t stream) {
   sms = std::min(sms, KA_MOST / KA_CTAS);
-  KaScratch s{static_cast<float*>(scratch),
-              reinterpret_cast<int*>(static_cast<uint8_t*>(scratch) + (size_t)KA_CTAS * sms * KV_ATTN_PART_BYTES)};
+  KaScratch s{reinterpret_cast<float*>(static_cast<uint8_t*>(scratch) + KV_ATTN_COUNTERS), static_cast<int*>(scratch)};
   if (kv.hd == 128) return kv.fp8 ? launch_rows<128, true>(kv, a, s, KA_CTAS * sms, err, stream) : launch_rows<128, false>(kv, a, s, KA_CTAS * sms, err, stream);
   return kv.fp8 ? launch_rows<64, true>(kv, a, s, KA_CTAS * sms, err, stream) : launch_rows<64, false>(kv, a, s, KA_CTAS * sms, err, stream);
 }

@@ -668,12 +668,11 @@ cudaError_t launch_as(const KvPool& kv, const KvAttn& a, const KaScratch& s, int
 
 }  // namespace
 
-size_t kv_attention_tc_scratch(int sms) { return (size_t)std::min(sms, 152) * (KV_ATTN_TC_PART_BYTES + sizeof(int)); }
+size_t kv_attention_tc_scratch(int sms) { return KV_ATTN_COUNTERS + (size_t)std::min(sms, 152) * KV_ATTN_TC_PART_BYTES; }
 
 cudaError_t kv_attention_tc_launch(const KvPool& kv, const KvAttn& a, void* scratch, int sms, int* err, cudaStream_t stream) {
   sms = std::min(sms, 152);
-  KaScratch s{static_cast<float*>(scratch),
-              reinterpret_cast<int*>(static_cast<uint8_t*>(scratch) + (size_t)sms * KV_ATTN_TC_PART_BYTES)};
+  KaScratch s{reinterpret_cast<float*>(static_cast<uint8_t*>(scratch) + KV_ATTN_COUNTERS), static_cast<int*>(scratch)};
   if (kv.hd == 128) return kv.fp8 ? launch_as<128, true>(kv, a, s, sms, err, stream) : launch_as<128, false>(kv, a, s, sms, err, stream);
   return kv.fp8 ? launch_as<64, true>(kv, a, s, sms, err, stream) : launch_as<64, false>(kv, a, s, sms, err, stream);
 }

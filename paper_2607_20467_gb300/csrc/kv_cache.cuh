@@ -40,8 +40,9 @@ struct KvAttn {
   float* lse;               // [rows][H] or NULL
 };
 // Two kernels: for up to 32 rows (new positions x query heads of a kv head) that share a kv head's keys,
-// and for more (not causal).  Scratch of a launch on `sms` SMs: the parts of rows whose keys several
-// CTAs share, then counters, zero before the first launch and left zero by each.
+// and for more (not causal).  Scratch of a launch on `sms` SMs: counters, zero before the first launch
+// and left zero by each, then the parts of rows whose keys several CTAs share.
+constexpr size_t KV_ATTN_COUNTERS = 4096;                                      // bytes (an int per CTA)
 constexpr size_t KV_ATTN_PART_BYTES = 2 * 32 * (128 + 4) * sizeof(float);      // per CTA
 constexpr size_t KV_ATTN_TC_PART_BYTES = 2 * 256 * (128 + 4) * sizeof(float);
 bool kv_attention_many_rows(const KvPool& kv, const KvAttn& a);

@@ -1,0 +1,101 @@
+"""dcl_kv_attention over the range of what a cache can hold, by each of its kernels, against a plain
+attention in 64 bits over the stored values (dcl_kv_read gives them exactly).
+
+Tolerance.  A component's error is at most 2^-8 of itself for the output's bf16 (half a unit in the last place
+of a number just above a power of two), and 2^-12 of A = sum p |v| for the weights' two parts (2^-16
+of each and less), the scores and the sums."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2607_20467_gb300 as dcl
+
+pytestmark = pytest.mark.gpu
+
+# (query heads of a kv head, new positions, positions that the page table has room for): how many rows share
+# a kv head's keys, and a table wide enough for the kernel of many rows
+KERNELS = {"8 rows": (4, 2, 0), "16 rows": (4, 4, 0), "32 rows": (4, 8, 0), "many rows": (4, 40, 3_400_000)}
+FEW = ["8 rows", "16 rows", "32 rows"]
+
+
+@pytest.fixture(scope="module")
+def ops():
+    import __graft_entry__
+    __graft_entry__.build()
+    ctx = dcl.Context(None, 1, 1)
+    yield ctx
+    ctx.close()
+
+
+class Case:
+    """One sequence of the keys and values k, v [n][kv][hd] (rounded to bf16, then stored), and what a
+    cache returns of them in 64 bits."""
+
+    def __init__(self, ops, k, v, fp8, page_len=32, seed=0):
+        n, kv, hd = k.shape
+        self.n, self.page_len = n, page_len
+        pages = -(-n // page_len)
+        self.cache = dcl.KvCache.empty(pages, page_len, kv, hd, fp8=fp8)
+        for t in (self.cache.k, self.cache.v):
+            t.view(torch.uint8).fill_(0x7F)  # (what no key was written to is no number)
+        order = np.random.default_rng(seed).permutation(pages)
+        at = np.arange(n)
+        slots = torch.from_numpy((order[at // page_len] * page_len + at % page_len).astype(np.int32)).cuda()
+        bf = [torch.as_tensor(x).to(torch.bfloat16).cuda().contiguous() for x in (k, v)]
+        ops.kv_write(self.cache, bf[0], bf[1], slots)
+        back = [torch.empty_like(x) for x in bf]
+        ops.kv_read(self.cache, slots, *back)
+        ops.synchronise()
+        self.k, self.v = (x.double() for x in back)
+        self.order = order
+
+    def attend(self, ops, q, causal=False, scale=None, wide=0):
+        """out, lse of the rows q [new][heads][hd]."""
+        new, heads, hd = q.shape
+        width = max(len(self.order), -(-wide // self.page_len))
+        table = torch.full((1, width), -1, dtype=torch.int32, device="cuda")
+        table[0, :len(self.order)] = torch.from_numpy(self.order.astype(np.int32))
+        out = torch.full((new, heads, hd), 77.0, dtype=torch.bfloat16, device="cuda")
+        lse = torch.full((new, heads), 77.0, device="cuda")
+        i32 = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")
+        ops.kv_attention(self.cache, q, i32([0, new]), table, i32([self.n]), out, max_new=new, causal=causal,
+                         scale=scale or 0.0, lse=lse)
+        ops.synchronise()
+        return out.double(), lse.double()
+
+    def reference(self, q, causal=False, scale=None):
+        """o, A, lse in 64 bits."""
+        new, heads, hd = q.shape
+        kv = self.k.shape[1]
+        rep = heads // kv
+        k, v = (x.repeat_interleave(rep, 1) for x in (self.k, self.v))
+        s = torch.einsum("ihd,jhd->hij", q.double(), k) * (scale or hd ** -0.5)
+        if causal:
+            j, i = torch.arange(self.n, device="cuda"), torch.arange(new, device="cuda")
+            s = s.masked_fill(j[None, :] > (self.n - new + i)[:, None], -np.inf)
+        p = torch.softmax(s, -1)
+        return (torch.einsum("hij,jhd->ihd", p, v), torch.einsum("hij,jhd->ihd", p, v.abs()), torch.logsumexp(s, -1).T)
+
+    def check(self, ops, q, causal=False, scale=None, wide=0):
+        out, lse = self.attend(ops, q, causal, scale, wide)
+        o, A, l = self.reference(q, causal, scale)
+        bad = (out - o).abs() - (2.0 ** -8 * o.abs() + 2.0 ** -12 * A)
+        assert (bad <= 0).all(), float(((out - o).abs() / A).max())
+        S = torch.einsum("ihd,jhd->ihj", q.double().abs(), self.k.abs().repeat_interleave(q.shape[1] // self.k.shape[1], 1))
+        S = S.amax(-1) * (scale or q.shape[2] ** -0.5)
+        assert ((lse - l).abs() <= 1e-5 * (1 + S)).all()
+
+
+def _q(rng, kernel, kv, hd, scale=1.0):
+    rep, new, _ = KERNELS[kernel]
+    return torch.from_numpy(rng.normal(0, scale, (new, rep * kv, hd))).to(torch.bfloat16).cuda()
+
+
+def _sharp(rng, kernel, k):
+    """Rows that each see one key of its own (77 binades above the rest, and more), and which."""
+    rep, new, _ = KERNELS[kernel]
+    n, kv, hd = k.shape
+    which = rng.integers(0, n, (new, rep * kv))
+    unit = k / np.sqrt((k ** 2).mean(-1, keepdims=True))
+    q = np.stack([unit[which[:, h], h // rep] for h in range(rep * kv)], 1) / np.sqrt((k ** 2).mean())
+    return torch.from_numpy(8.0 * q).to(torch.bfloat16).cuda()
