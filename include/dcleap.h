@@ -352,7 +352,9 @@ dcl_status dcl_kv_read(dcl_ctx* ctx, const dcl_kv_cache* cache, const int32_t* s
  *   out_dev     bf16 [n_q][n_heads][head_dim]; lse_dev float [n_q][n_heads] or NULL.  A row that
  *               sees nothing gets zeros and -inf.
  * Scores, softmax statistics and sums are held in fp32 and reproduce bit for bit.
- * Errors: INVALID_ARG, OOM (scratch), CUDA. */
+ * A context's first call that has rows allocates its scratch (41 MB, for calls of every size) and is
+ * refused with STATE while the stream is being captured; every later call may be captured.
+ * Errors: INVALID_ARG, STATE, OOM (scratch), CUDA. */
 dcl_status dcl_kv_attention(dcl_ctx* ctx, const dcl_kv_cache* cache, const void* q_dev, int64_t q_stride,
                             const int32_t* q_start_dev, const int32_t* page_table_dev, int32_t max_pages,
                             const int32_t* seq_len_dev, int32_t batch, int32_t n_q, int32_t max_new,

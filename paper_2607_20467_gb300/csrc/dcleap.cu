@@ -122,7 +122,7 @@ struct dcl_ctx {
   // scratch of the single-kernel entry points, kept from call to call up to OP_SCRATCH_KEEP
   void* op_buf = nullptr;
   size_t op_cap = 0;
-  void *kv_scratch = nullptr, *kv_tc_scratch = nullptr;  // kv_attention's parts and counters, from the first call on
+  void* kv_scratch = nullptr;  // kv_attention's counters and parts, from the first call on
   cudaEvent_t ev_done[2] = {nullptr, nullptr};
 };
 
@@ -221,7 +221,7 @@ dcl_status check_device(dcl_ctx* c) {
     CUDA_TRY(c, cudaMemsetAsync(c->derr, 0, sizeof(int), c->stream));
     // an aborted split-K launch may leave its counters set: clear them for the next one
     if (c->gemm_flags) CUDA_TRY(c, cudaMemsetAsync(c->gemm_flags, 0, sizeof(int) * c->gemm_flags_n, c->stream));
-    if (c->kv_tc_scratch) CUDA_TRY(c, cudaMemsetAsync(c->kv_tc_scratch, 0, KV_ATTN_COUNTERS, c->stream));
+    if (c->kv_scratch) CUDA_TRY(c, cudaMemsetAsync(c->kv_scratch, 0, KV_ATTN_COUNTERS, c->stream));
     if (e == DERR_WAIT_TIMEOUT)
       return fail(c, DCL_ERR_TIMEOUT, "a pipeline wait timed out on the device (kernel returned)");
     if (e == DERR_KV_RANGE) return fail(c, DCL_ERR_INVALID_ARG, "a slot, page or length outside the paged cache");
@@ -1493,16 +1493,24 @@ dcl_status dcl_kv_attention(dcl_ctx* c, const dcl_kv_cache* cache, const void* q
   KvAttn a{static_cast<const __nv_bfloat16*>(q_dev), q_stride, q_start_dev, page_table_dev, seq_len_dev, batch,
            max_pages, n_q, max_new, n_heads, causal, scale > 0.f ? scale : 1.f / sqrtf((float)kv.hd),
            static_cast<__nv_bfloat16*>(out_dev), lse_dev};
-  const bool many = kv_attention_many_rows(kv, a);
-  void*& scratch = many ? c->kv_tc_scratch : c->kv_scratch;
-  if (!scratch) {
-    const size_t bytes = many ? kv_attention_tc_scratch(c->num_sms) : kv_attention_scratch(c->num_sms);
-    scratch = dev_alloc(c, bytes);
+  if (!c->kv_scratch) {
+    // (zeroed by a node of a graph it would hold anything until that graph has run)
+    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+    CUDA_TRY(c, cudaStreamIsCapturing(c->stream, &capture));
+    if (capture != cudaStreamCaptureStatusNone)
+      return fail(c, DCL_ERR_STATE, "kv_attention: a context's first call allocates scratch and cannot be captured");
+    const size_t few = kv_attention_scratch(c->num_sms), many = kv_attention_tc_scratch(c->num_sms);
+    void* scratch = dev_alloc(c, few > many ? few : many);
     if (!scratch) return fail(c, DCL_ERR_OOM, "kv_attention: scratch allocation failed");
-    CUDA_TRY(c, cudaMemsetAsync(scratch, 0, KV_ATTN_COUNTERS, c->stream));
+    const cudaError_t e = cudaMemsetAsync(scratch, 0, KV_ATTN_COUNTERS, c->stream);
+    if (e != cudaSuccess) {
+      dev_free_one(c, scratch);
+      return fail(c, DCL_ERR_CUDA, "kv_attention: clearing the scratch failed: %s", cudaGetErrorString(e));
+    }
+    c->kv_scratch = scratch;
   }
-  CUDA_TRY(c, many ? kv_attention_tc_launch(kv, a, scratch, c->num_sms, c->derr, c->stream)
-                   : kv_attention_launch(kv, a, scratch, c->num_sms, c->derr, c->stream));
+  CUDA_TRY(c, kv_attention_many_rows(kv, a) ? kv_attention_tc_launch(kv, a, c->kv_scratch, c->num_sms, c->derr, c->stream)
+                                            : kv_attention_launch(kv, a, c->kv_scratch, c->num_sms, c->derr, c->stream));
   return DCL_OK;
 }
 

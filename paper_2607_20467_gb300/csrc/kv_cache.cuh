@@ -41,7 +41,8 @@ struct KvAttn {
 };
 // Two kernels: for up to 32 rows (new positions x query heads of a kv head) that share a kv head's keys,
 // and for more (not causal).  Scratch of a launch on `sms` SMs: counters, zero before the first launch
-// and left zero by each, then the parts of rows whose keys several CTAs share.
+// and left zero by each, then the parts of rows whose keys several CTAs share.  The launches of a
+// context run one after another on its stream, so that both kernels use the same.
 constexpr size_t KV_ATTN_COUNTERS = 4096;                                      // bytes (an int per CTA)
 constexpr size_t KV_ATTN_PART_BYTES = 2 * 32 * (128 + 4) * sizeof(float);      // per CTA
 constexpr size_t KV_ATTN_TC_PART_BYTES = 2 * 256 * (128 + 4) * sizeof(float);

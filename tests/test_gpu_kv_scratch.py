@@ -67,3 +67,59 @@ def test_a_call_right_after_a_reported_error(kind):
             call.run(ctx, out)
         ctx.synchronise()
         assert all(torch.equal(out, want) for out in outs)
+
+
+def _captured(ctx, s, call, out):
+    """A graph of one call, made on the stream s (the context's)."""
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        call.run(ctx, out)
+    return g
+
+
+@pytest.mark.parametrize("first", list(KINDS))
+def test_one_call_of_any_size_prepares_every_capture(first):
+    """After a small call of either kernel a call of both can be captured, and replays give what they gave."""
+    calls = {kind: Call(*KINDS[kind]) for kind in KINDS}
+    s = torch.cuda.Stream()
+    with dcl.Context(None, 1, 1, stream=s.cuda_stream) as ctx:
+        with torch.cuda.stream(s):
+            n, new, wide = KINDS[first]
+            small = Call(100, new, wide)
+            small.run(ctx, small.out())
+            outs = {kind: call.out() for kind, call in calls.items()}
+            ctx.synchronise()
+        graphs = {kind: _captured(ctx, s, call, outs[kind]) for kind, call in calls.items()}
+        with torch.cuda.stream(s):
+            want = {kind: call.out() for kind, call in calls.items()}
+            for kind, call in calls.items():
+                call.run(ctx, want[kind])
+            for _ in range(3):
+                for out in outs.values():
+                    out.fill_(7.0)
+                for g in graphs.values():
+                    g.replay()
+                ctx.synchronise()
+                for kind in KINDS:
+                    assert torch.equal(outs[kind], want[kind])
+
+
+@pytest.mark.parametrize("kind", list(KINDS))
+def test_the_first_call_is_not_captured(kind):
+    """It is refused, and the capture and the context stay usable."""
+    call = Call(*KINDS[kind])
+    s = torch.cuda.Stream()
+    with dcl.Context(None, 1, 1, stream=s.cuda_stream) as ctx:
+        out, other = call.out(), torch.zeros(4, device="cuda")
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            other.add_(1.0)
+            with pytest.raises(dcl.DcleapError, match="cannot be captured") as e:
+                call.run(ctx, out)
+        assert e.value.status == dcl.DCL_ERR_STATE
+        with torch.cuda.stream(s):
+            g.replay()
+            call.run(ctx, out)
+            ctx.synchronise()
+        assert (other == 1).all() and (out != 7).any()
