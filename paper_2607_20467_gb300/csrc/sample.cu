@@ -416,6 +416,7 @@ __global__ void __launch_bounds__(SM_THREADS, TRUNC ? 3 : 5) sample_kernel(Sampl
       best.take(with_noise ? perturbed(y, g[base + j]) : y, base + j);
     };
     if (vectors) {
+      if (tid < n_head) element(edge(tid));  // (before the vectors: a thread's tokens in order)
       constexpr int U = 2;  // vectors of 8 in flight
       for (int v0 = v_lo + tid; v0 < v_hi; v0 += U * SM_THREADS) {
         float4 n[U][2];
@@ -459,9 +460,12 @@ __global__ void __launch_bounds__(SM_THREADS, TRUNC ? 3 : 5) sample_kernel(Sampl
         }
       }
     }
-    // without vectors all of the row, else what its first and last vectors hold of it
-    const int n_rest = vectors ? n_edge : max(0, hi - lo);
-    for (int i = tid; i < n_rest; i += SM_THREADS) element(vectors ? edge(i) : lo + i);
+    // what the last vector holds of the row, or without vectors all of it
+    if (!vectors) {
+      for (int j = lo + tid; j < hi; j += SM_THREADS) element(j);
+    } else if (tid >= n_head && tid < n_edge) {
+      element(edge(tid));
+    }
   } else if constexpr (TRUNC) {
     // ---- the prefix: windows of SM_BINS distinct logits from the largest down
     float mass = 0.f;
@@ -601,6 +605,7 @@ __global__ void __launch_bounds__(SM_THREADS, TRUNC ? 3 : 5) sample_kernel(Sampl
       total += exp_fast(y);
       best.take(g ? perturbed(y, g[base + j]) : y, base + j);
     };
+    if (tid < n_head) element((uint32_t)zs[edge(tid)] << 16, edge(tid));  // (a thread's tokens in order)
     for (int v = v_lo + tid; v < v_hi; v += SM_THREADS) {
       const uint4 w4 = reinterpret_cast<const uint4*>(zs)[v];
       const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
@@ -611,7 +616,7 @@ __global__ void __launch_bounds__(SM_THREADS, TRUNC ? 3 : 5) sample_kernel(Sampl
 #pragma unroll 1
         for (int i = 0; i < 8; ++i) element((uint32_t)zs[8 * v + i] << 16, 8 * v + i);
     }
-    if (tid < n_edge) element((uint32_t)zs[edge(tid)] << 16, edge(tid));
+    if (tid >= n_head && tid < n_edge) element((uint32_t)zs[edge(tid)] << 16, edge(tid));
   }
 
   // ---- the row's token
