@@ -1,7 +1,7 @@
 // Attention of a few new positions of every sequence over its paged keys and values:
 // out = softmax(scale q k^T) v over the sequence's cached positions.
 //
-// The rows of one kv head (new positions x the query heads that share it) form row tiles of 16 or
+// The rows of one kv head (new positions x the query heads that share it) form row tiles of 8, 16 or
 // 32, the most that one pass over the keys serves.  A warp takes 16 or 32 keys at a time: S = q k^T and
 // O += P v as m16n8k16 products with the rows on the M side, its own running maximum m, sum l and
 // O in registers, its own ring of key / value tiles in shared memory (16-byte asynchronous copies;
@@ -24,12 +24,13 @@
 // two into fp16 (its 8 bits fit; what falls below fp16's range is 2^-24 of the row's largest).  A
 // key's exponent scales its score.  A value's exponent e_j goes into the exponent of its
 // probability: P_j = exp2(s_j + e_j - m) with m near the running maximum of s_j + e_j, so that P is
-// bounded whatever the values' sizes, and l = sum P_j 2^-e_j.  P is rounded to fp16 (2^-11 of itself;
-// below 2^-21 of the largest term, 2^-32 of that): an eighth of the output's rounding.  (What it
-// leaves as a second part: 37 -> 42.5 us for the 64 sequences, 58.5 -> 61 for the long ones.)
-// bf16 pages: the instruction wants both operands of one type, and bf16 alone would round P by 2^-8
-// of itself, as much as the output's own rounding; P is given in two bf16 parts (2^-16), the second
-// a product more.
+// bounded whatever the values' sizes, and l = sum P_j 2^-e_j.
+//
+// P is given in two parts, fp16 with FP8 pages (2^-21 of itself; 2^-32 of the largest term where that is
+// more) and bf16 with bf16 pages (2^-16; the instruction wants both operands of one type).  One part
+// would leave up to 2^-11 or 2^-8 of a result, beside 2^-8 of the output's own rounding.  Up to 8 rows
+// fill half of a product's 16, and the other half takes the second part, so that it costs no product;
+// for more it is a product of its own.
 #include <cuda_fp8.h>
 
 #include <algorithm>
@@ -47,14 +48,16 @@ constexpr int KA_CTAS = 2;    // CTAs of an SM: one loads while the other begins
 constexpr int KA_MOST = 304;  // most CTAs of a launch
 static_assert(KA_MOST * sizeof(int) <= KV_ATTN_COUNTERS, "a counter per CTA");
 
-template <int HD, bool FP8, int MT>
+// RS: rows of an item that a lane has (quad + 8 i), 8 rows of the item each.
+template <int HD, bool FP8, int RS>
 struct KaCfg {
   static constexpr int ES = FP8 ? 1 : 2;
+  static constexpr int MT = RS == 1 ? 1 : RS / 2;   // tiles of 16 rows (or of 8 and the second parts of their weights)
   static constexpr int WARPS = MT == 1 ? 6 : 4;     // (with KA_CTAS of them on an SM as many as the registers allow)
   static constexpr int THREADS = 32 * WARPS;
   static constexpr int KT = FP8 && MT == 1 ? 32 : 16;  // keys that a warp takes at a time
   static constexpr int NK = KT / 8;                 // column tiles of S
-  static constexpr int ROWS = 16 * MT;              // rows of an item
+  static constexpr int ROWS = 8 * RS;               // rows of an item
   static constexpr int ROWB = HD * ES;              // bytes of a key
   static constexpr int TILE = KT * ROWB;            // the keys (or values) of a step
   static constexpr int STAGE = 2 * TILE + (FP8 ? 2 * KT : 0);
@@ -197,9 +200,11 @@ __device__ __forceinline__ int o_place(int c) {
   if (FP8) return c + 4 * (c / (HD / 8));
   return (c >> 6) * 96 + ((c >> 3) & 7) * 12 + (c & 7);
 }
-template <int HD, bool FP8, int MT>
-__global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_attention_kernel(KvPool kv, KvAttn a, KaScratch scratch, int* err) {
-  using C = KaCfg<HD, FP8, MT>;
+template <int HD, bool FP8, int RS>
+__global__ void __launch_bounds__(KaCfg<HD, FP8, RS>::THREADS, KA_CTAS) kv_attention_kernel(KvPool kv, KvAttn a, KaScratch scratch, int* err) {
+  using C = KaCfg<HD, FP8, RS>;
+  constexpr int MT = C::MT;
+  constexpr bool OWN_LO = RS > 1;  // the weights' second parts are products of their own
   constexpr int KS = HD / 16;  // k steps of S, and pairs of column tiles of O
   constexpr int NT = HD / 8;   // column tiles of O
   constexpr int KT = C::KT, NK = C::NK;
@@ -231,11 +236,11 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
     const int lim_max = a.causal ? min(it.len, it.len - it.nq + (it.first + it.rows - 1) / rep + 1) : it.len;
 
     // ---- this lane's rows: quad + 8 i of the tile; asked for before the keys, which would be in the way
-    int lim[2 * MT];  // keys each sees
-    float qa[2 * MT];  // scale * log2(e) * the power of two that q was divided by
-    uint4 raw[2 * MT][HD / 32];
+    int lim[RS];  // keys each sees
+    float qa[RS];  // scale * log2(e) * the power of two that q was divided by
+    uint4 raw[RS][HD / 32];
 #pragma unroll
-    for (int i = 0; i < 2 * MT; ++i) {
+    for (int i = 0; i < RS; ++i) {
       const int r = 8 * i + quad, rr = it.first + r;
       const bool live = r < it.rows;
       const int tok = rr / rep, h = it.g * rep + rr - tok * rep;
@@ -300,7 +305,7 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < (RS > 1 ? 2 : 1); ++i) {
           uint4(&rq)[HD / 32] = raw[2 * mt + i];
           float up = 1.f;
           if (FP8) {
@@ -329,8 +334,9 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
 #pragma unroll
           for (int s = 0; s < KS; ++s) {  // step s: components 4 s .. 4 s + 3 of this lane's
             const uint32_t* w0 = &raw[2 * mt][s >> 1].x + 2 * (s & 1);
-            const uint32_t* w1 = &raw[2 * mt + 1][s >> 1].x + 2 * (s & 1);
-            *reinterpret_cast<uint4*>(qs[mt * KS + s][lane]) = make_uint4(w0[0], w1[0], w0[1], w1[1]);
+            const uint32_t* w1 = &raw[RS > 1 ? 2 * mt + 1 : 0][s >> 1].x + 2 * (s & 1);
+            *reinterpret_cast<uint4*>(qs[mt * KS + s][lane]) =
+                RS > 1 ? make_uint4(w0[0], w1[0], w0[1], w1[1]) : make_uint4(w0[0], 0, w0[1], 0);
           }
         }
       }
@@ -338,7 +344,7 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
     }
     const uint32_t qs_addr = smem_addr(smem) + C::QF + lane * 16;
 
-    float o[MT][NT][4], m[2 * MT], l[2 * MT];
+    float o[MT][NT][4], m[RS], l[RS];
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -346,7 +352,7 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
 #pragma unroll
         for (int k = 0; k < 4; ++k) o[i][j][k] = 0.f;
 #pragma unroll
-    for (int i = 0; i < 2 * MT; ++i) {
+    for (int i = 0; i < RS; ++i) {
       m[i] = -INFINITY;
       l[i] = 0.f;
     }
@@ -425,7 +431,7 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
             ev = lds_f2(sc + 4 * (KT + 8 * j + 2 * place));
           }
 #pragma unroll
-          for (int i = 0; i < 2 * MT; ++i) {
+          for (int i = 0; i < RS; ++i) {
             float &x0 = s[i >> 1][j][2 * (i & 1)], &x1 = s[i >> 1][j][2 * (i & 1) + 1];
             x0 = FP8 ? fmaf(x0, qa[i] * kf.x, ev.x) : x0 * qa[i];
             x1 = FP8 ? fmaf(x1, qa[i] * kf.y, ev.y) : x1 * qa[i];
@@ -433,7 +439,7 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
         }
         if (masked) {
 #pragma unroll
-          for (int i = 0; i < 2 * MT; ++i)
+          for (int i = 0; i < RS; ++i)
 #pragma unroll
             for (int j = 0; j < NK; ++j)
 #pragma unroll
@@ -444,9 +450,9 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
         // it by more than 15 (P <= 2^15), so that most steps neither exchange maxima nor scale O; P fills
         // fp16's range, for the sake of small ones that carry large values.
         bool grew = false;
-        float top[2 * MT];
+        float top[RS];
 #pragma unroll
-        for (int i = 0; i < 2 * MT; ++i) {
+        for (int i = 0; i < RS; ++i) {
           top[i] = -INFINITY;
 #pragma unroll
           for (int j = 0; j < NK; ++j)
@@ -455,7 +461,7 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
         }
         if (__any_sync(0xffffffffu, grew)) {
 #pragma unroll
-          for (int i = 0; i < 2 * MT; ++i) {
+          for (int i = 0; i < RS; ++i) {
             top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
             top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
             const float mn = fmaxf(m[i], top[i] - 7.f), alpha = exp2_fast(m[i] - (mn == -INFINITY ? 0.f : mn));
@@ -465,17 +471,24 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
             for (int j = 0; j < NT; ++j) {
               o[i >> 1][j][2 * (i & 1)] *= alpha;
               o[i >> 1][j][2 * (i & 1) + 1] *= alpha;
+              if (!OWN_LO) {
+                o[0][j][2] *= alpha;
+                o[0][j][3] *= alpha;
+              }
             }
           }
         }
-        uint32_t p[NK / 2][MT][4], p_lo[FP8 ? 1 : NK / 2][MT][4];
+        uint32_t p[NK / 2][MT][4], p_lo[OWN_LO ? NK / 2 : 1][MT][4];
 #pragma unroll
-        for (int i = 0; i < 2 * MT; ++i) {
+        for (int i = 0; i < RS; ++i) {
           const float ref = m[i] == -INFINITY ? 0.f : m[i];  // (nothing seen yet: exp2(-inf) = 0)
 #pragma unroll
           for (int j = 0; j < NK; ++j) {
             const float x0 = exp2_fast(s[i >> 1][j][2 * (i & 1)] - ref), x1 = exp2_fast(s[i >> 1][j][2 * (i & 1) + 1] - ref);
-            const uint32_t hi = FP8 ? pack_f16x2(x0, x1) : pack_bf16x2(x0, x1);
+            // (fp16: 11 bits cut off, so that what they leave needs no widening)
+            const float h0 = __uint_as_float(__float_as_uint(x0) & 0xffffe000u), h1 = __uint_as_float(__float_as_uint(x1) & 0xffffe000u);
+            const uint32_t hi = FP8 ? pack_f16x2(h0, h1) : pack_bf16x2(x0, x1);
+            const uint32_t lo = FP8 ? pack_f16x2(x0 - h0, x1 - h1) : pack_bf16x2(x0 - bf16_lo(hi), x1 - bf16_hi(hi));
             if (FP8) {
               const float2 vi = lds_f2(sc + 4 * (2 * KT + 8 * j + 2 * place));
               l[i] = fmaf(x1, vi.y, fmaf(x0, vi.x, l[i]));
@@ -483,7 +496,10 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
               l[i] += x0 + x1;
             }
             p[j >> 1][i >> 1][2 * (j & 1) + (i & 1)] = hi;
-            if (!FP8) p_lo[FP8 ? 0 : j >> 1][i >> 1][2 * (j & 1) + (i & 1)] = pack_bf16x2(x0 - bf16_lo(hi), x1 - bf16_hi(hi));
+            if (OWN_LO)
+              p_lo[OWN_LO ? j >> 1 : 0][i >> 1][2 * (j & 1) + (i & 1)] = lo;
+            else
+              p[j >> 1][0][2 * (j & 1) + 1] = lo;
           }
         }
         // A value that is no number and that only some of the rows see (0 * NaN): it is added to the
@@ -494,7 +510,7 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
 #pragma unroll 1
             for (int jj = 0; jj < 16; ++jj) {
 #pragma unroll
-              for (int i = 0; i < 2 * MT; ++i) {
+              for (int i = 0; i < RS; ++i) {
                 const uint32_t pair = __shfl_sync(0xffffffffu, jj < 8 ? p[half][i >> 1][i & 1] : p[half][i >> 1][2 + (i & 1)],
                                                   4 * quad + ((jj & 7) >> 1));
                 if (key + 16 * half + jj >= lim[i]) continue;
@@ -543,7 +559,10 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
 #pragma unroll
               for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int i = 0; i < MT; ++i) mma16816<FP8>(o[i][4 * w + j], p[half][i], b0[j], b1[j]);
+                for (int i = 0; i < MT; ++i) {
+                  mma16816<FP8>(o[i][4 * w + j], p[half][i], b0[j], b1[j]);
+                  if (OWN_LO) mma16816<FP8>(o[i][4 * w + j], p_lo[OWN_LO ? half : 0][i], b0[j], b1[j]);
+                }
             }
           } else {
 #pragma unroll
@@ -562,7 +581,7 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
 #pragma unroll
                   for (int i = 0; i < MT; ++i) {
                     mma16816<FP8>(o[i][8 * c + 2 * w + x], p[half][i], b0, b1);
-                    mma16816<FP8>(o[i][8 * c + 2 * w + x], p_lo[FP8 ? 0 : half][i], b0, b1);
+                    if (OWN_LO) mma16816<FP8>(o[i][8 * c + 2 * w + x], p_lo[OWN_LO ? half : 0][i], b0, b1);
                   }
                 }
               }
@@ -577,19 +596,26 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
 
     // ---- join the warps
 #pragma unroll
-    for (int i = 0; i < 2 * MT; ++i) {
+    for (int i = 0; i < RS; ++i) {
       l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
       l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
       if (place == 0) ml[warp * C::ROWS + 8 * i + quad] = make_float2(m[i], l[i]);
     }
     if (key0 + KT * warp < stop) {
       float* mine = reinterpret_cast<float*>(smem + warp * C::RING_B);
+      if (!OWN_LO) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          o[0][j][0] += o[0][j][2];
+          o[0][j][1] += o[0][j][3];
+        }
+      }
 #pragma unroll
       for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int j = 0; j < NT; j += 4)
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
+          for (int k = 0; k < (RS > 1 ? 4 : 2); ++k)
             *reinterpret_cast<float4*>(mine + (16 * i + quad + 8 * (k >> 1)) * C::O_PITCH +
                                        o_place<HD, FP8>(v_comp<HD, FP8>(2 * place + (k & 1), j))) =
                 make_float4(o[i][j][k], o[i][j + 1][k], o[i][j + 2][k], o[i][j + 3][k]);
@@ -660,12 +686,12 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, MT>::THREADS, KA_CTAS) kv_atten
   }
 }
 
-template <int HD, bool FP8, int MT>
+template <int HD, bool FP8, int RS>
 cudaError_t launch_as(const KvPool& kv, const KvAttn& a, const KaScratch& s, int ctas, int* err, cudaStream_t stream) {
-  using C = KaCfg<HD, FP8, MT>;
+  using C = KaCfg<HD, FP8, RS>;
   static_assert(KA_CTAS * (C::SMEM + 1024) <= 233472, "shared memory of an SM");
   static_assert(2 * C::ROWS * (HD + 4) * 4 <= KV_ATTN_PART_BYTES, "scratch per CTA");
-  auto kern = kv_attention_kernel<HD, FP8, MT>;
+  auto kern = kv_attention_kernel<HD, FP8, RS>;
   static const cudaError_t set =
       cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM);
   if (set != cudaSuccess) return set;
@@ -675,8 +701,10 @@ cudaError_t launch_as(const KvPool& kv, const KvAttn& a, const KaScratch& s, int
 
 template <int HD, bool FP8>
 cudaError_t launch_rows(const KvPool& kv, const KvAttn& a, const KaScratch& s, int ctas, int* err, cudaStream_t stream) {
-  if ((int64_t)a.max_new * (a.H / kv.G) <= 16) return launch_as<HD, FP8, 1>(kv, a, s, ctas, err, stream);
-  return launch_as<HD, FP8, 2>(kv, a, s, ctas, err, stream);
+  const int64_t rows = (int64_t)a.max_new * (a.H / kv.G);
+  if (rows <= 8) return launch_as<HD, FP8, 1>(kv, a, s, ctas, err, stream);
+  if (rows <= 16) return launch_as<HD, FP8, 2>(kv, a, s, ctas, err, stream);
+  return launch_as<HD, FP8, 4>(kv, a, s, ctas, err, stream);
 }
 
 }  // namespace

@@ -99,3 +99,24 @@ def _sharp(rng, kernel, k):
     unit = k / np.sqrt((k ** 2).mean(-1, keepdims=True))
     q = np.stack([unit[which[:, h], h // rep] for h in range(rep * kv)], 1) / np.sqrt((k ** 2).mean())
     return torch.from_numpy(8.0 * q).to(torch.bfloat16).cuda()
+
+
+@pytest.mark.parametrize("kernel", FEW)
+@pytest.mark.parametrize("fp8", [True, False])
+def test_weights_keep_more_bits_than_the_output(ops, kernel, fp8):
+    """Fifteen of sixteen keys have a weight just under half-way between two numbers of 11 bits, all to the same
+    side, and every component another mixture of 1 and 1.125: weights of 11 bits would be off by 2^-11 in all of
+    them, on top of the output's rounding wherever that comes out at its worst."""
+    hd, n = 64, 4096
+    rep, new, wide = KERNELS[kernel]
+    first = np.arange(n) % 16 == 5  # (one in every step of 16 keys: the reference is theirs)
+    k = np.zeros((n, 1, hd))
+    k[~first, 0, 0], k[~first, 0, 1] = -1.0, 1.0
+    order = np.random.default_rng(3).permutation(np.flatnonzero(~first))
+    v = np.ones((n, 1, hd))
+    for d in range(hd):
+        v[order[:100 + 2 * d], 0, d] = 1.125
+    q = torch.zeros(new, rep, hd, dtype=torch.bfloat16, device="cuda")
+    q[:, :, 0] = 1.0
+    q[:, :, 1] = 0.97 * 2.0 ** -11 * np.log2(np.e)
+    Case(ops, k, v, fp8).check(ops, q, scale=float(np.log(2.0)), wide=wide)
