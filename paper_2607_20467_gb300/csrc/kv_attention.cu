@@ -24,7 +24,9 @@
 // two into fp16 (its 8 bits fit; what falls below fp16's range is 2^-24 of the row's largest).  A
 // key's exponent scales its score.  A value's exponent e_j goes into the exponent of its
 // probability: P_j = exp2(s_j + e_j - m) with m near the running maximum of s_j + e_j, so that P is
-// bounded whatever the values' sizes, and l = sum P_j 2^-e_j.
+// bounded whatever the values' sizes; l = sum exp2(s_j - m), an exponential of its own, as P_j 2^-e_j
+// loses weights where exponents lie 100 apart.  A vector of zeros is stored with exponent 0 whatever the
+// others' sizes and has no term to bound: where one would move m it is given an exponent far down.
 //
 // P is given in two parts, fp16 with FP8 pages (2^-21 of itself; 2^-32 of the largest term where that is
 // more) and bf16 with bf16 pages (2^-16; the instruction wants both operands of one type).  One part
@@ -71,8 +73,8 @@ struct KaCfg {
   static constexpr int ML = WARPS * RING_B;         // {m, l} [warp][ROWS]
   static constexpr int WT = ML + WARPS * ROWS * 8;  // weights of the warps' parts [ROWS][8], then {m, l} of the rows
   static constexpr int QF = WT + ROWS * (8 * 4 + 8);  // q fragments [MT][HD / 16][lane] of 16 bytes
-  static constexpr int SC = QF + MT * (HD / 16) * 32 * 16;  // what the keys' exponents give [warp][3][KT] floats
-  static constexpr int HEAD = SC + (FP8 ? WARPS * 3 * KT * 4 : 0);  // the walk's variables
+  static constexpr int SC = QF + MT * (HD / 16) * 32 * 16;  // what the keys' exponents give [warp][2][KT] floats
+  static constexpr int HEAD = SC + (FP8 ? WARPS * 2 * KT * 4 : 0);  // the walk's variables
   static constexpr int TODO = HEAD + 48;            // joins left to this CTA: their number, and two at most
   static constexpr size_t SMEM = TODO + 3 * 24;
   static_assert(ML >= ROWS * KA_MOST * 8, "the weights of an item's parts take the rings' place");
@@ -110,7 +112,12 @@ __device__ __forceinline__ uint32_t lds_u8(uint32_t a) {
 }
 __device__ __forceinline__ float2 lds_f2(uint32_t a) {
   float2 v;
-  asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(a));
+  asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ float lds_f32(uint32_t a) {
+  float v;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
   return v;
 }
 __device__ __forceinline__ void sts32(uint32_t a, float v) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(a), "f"(v) : "memory"); }
@@ -184,6 +191,23 @@ __device__ __noinline__ void clear_nonfinite(uint32_t tile, int bytes, int lane)
     sts128(tile + c, make_uint4(w.x & ~nonfinite_bits<FP8>(w.x), w.y & ~nonfinite_bits<FP8>(w.y),
                                 w.z & ~nonfinite_bits<FP8>(w.z), w.w & ~nonfinite_bits<FP8>(w.w)));
   }
+}
+// Keys of a step whose values are nothing but zeros (stored with exponent 0) get the exponent KA_ZERO in ev,
+// the step's values' exponents; whether there are any.
+constexpr float KA_ZERO = -90.f;  // (l holds their weights up to 2^97 times those that m is taken from)
+template <int ROWB, int KT>
+__device__ __noinline__ bool lower_zeros(uint32_t tile, uint32_t ev, int lane) {
+  bool zero = lane < KT && lds_f32(ev + 4 * (lane & (KT - 1))) == 0.f;
+  if (zero) {
+    uint32_t any = 0;
+    for (int c = 0; c < ROWB / 16; ++c) {
+      const uint4 w = lds128(tile + chunk_at<ROWB>(lane, c));
+      any |= w.x | w.y | w.z | w.w;
+    }
+    zero = (any & 0x7f7f7f7fu) == 0;
+    if (zero) sts32(ev + 4 * lane, KA_ZERO);
+  }
+  return __any_sync(0xffffffffu, zero);
 }
 template <int ROWB, bool FP8>
 __device__ __forceinline__ float value_at(uint32_t tile, int row, int comp) {
@@ -358,7 +382,7 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, RS>::THREADS, KA_CTAS) kv_atten
     }
 
     int cur = 0;
-    const uint32_t sc = smem_addr(smem) + C::SC + warp * 3 * KT * 4;
+    const uint32_t sc = smem_addr(smem) + C::SC + warp * 2 * KT * 4;
     for (int key = key0 + KT * warp; key < stop; key += KT * C::WARPS) {
       issue();  // into the stage that the last step left
       copy_wait<C::STAGES - 1>();
@@ -375,12 +399,11 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, RS>::THREADS, KA_CTAS) kv_atten
               sts128(sv + chunk_at<C::ROWB>(r, c % (C::ROWB / 16)), make_uint4(0, 0, 0, 0));
           }
         }
-        if (FP8) {  // what a key's exponents give: 2^e of the key, e and 2^-e of the value
+        if (FP8) {  // what a key's exponents give: 2^e of the key, e of the value
           if (KT == 32 || lane < KT) {
             const int x = (int)(int8_t)lds_u8(se + lane), y = max(-126, (int)(int8_t)lds_u8(se + KT + lane));
             sts32(sc + 4 * lane, kv_pow2(x));
             sts32(sc + 4 * (KT + lane), (float)y);
-            sts32(sc + 4 * (2 * KT + lane), kv_pow2(-y));
           }
         }
         __syncwarp();
@@ -422,19 +445,23 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, RS>::THREADS, KA_CTAS) kv_atten
             }
           }
         }
-        // scores in units of log2; with FP8 values their exponent added
+        // scores in units of log2, and what FP8 values add to the exponent of their weight
+        float2 ev[NK];
+        auto exponents = [&]() {
+#pragma unroll
+          for (int j = 0; j < NK; ++j) ev[j] = lds_f2(sc + 4 * (KT + 8 * j + 2 * place));
+        };
+        auto term = [](float x, float e) { return FP8 ? x + e : x; };
+        if (FP8) exponents();
 #pragma unroll
         for (int j = 0; j < NK; ++j) {
-          float2 kf, ev;
-          if (FP8) {
-            kf = lds_f2(sc + 4 * (8 * j + 2 * place));
-            ev = lds_f2(sc + 4 * (KT + 8 * j + 2 * place));
-          }
+          float2 kf;
+          if (FP8) kf = lds_f2(sc + 4 * (8 * j + 2 * place));
 #pragma unroll
           for (int i = 0; i < RS; ++i) {
             float &x0 = s[i >> 1][j][2 * (i & 1)], &x1 = s[i >> 1][j][2 * (i & 1) + 1];
-            x0 = FP8 ? fmaf(x0, qa[i] * kf.x, ev.x) : x0 * qa[i];
-            x1 = FP8 ? fmaf(x1, qa[i] * kf.y, ev.y) : x1 * qa[i];
+            x0 *= FP8 ? qa[i] * kf.x : qa[i];
+            x1 *= FP8 ? qa[i] * kf.y : qa[i];
           }
         }
         if (masked) {
@@ -449,24 +476,35 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, RS>::THREADS, KA_CTAS) kv_atten
         // The reference m of a row, 7 below its largest score when it is taken, moves only when a score passes
         // it by more than 15 (P <= 2^15), so that most steps neither exchange maxima nor scale O; P fills
         // fp16's range, for the sake of small ones that carry large values.
-        bool grew = false;
         float top[RS];
+        auto grew = [&]() {
+          bool any = false;
 #pragma unroll
-        for (int i = 0; i < RS; ++i) {
-          top[i] = -INFINITY;
+          for (int i = 0; i < RS; ++i) {
+            top[i] = -INFINITY;
 #pragma unroll
-          for (int j = 0; j < NK; ++j)
-            top[i] = fmaxf(top[i], fmaxf(s[i >> 1][j][2 * (i & 1)], s[i >> 1][j][2 * (i & 1) + 1]));
-          grew |= top[i] > m[i] + 15.f;
+            for (int j = 0; j < NK; ++j)
+              top[i] = fmaxf(top[i], fmaxf(term(s[i >> 1][j][2 * (i & 1)], ev[j].x), term(s[i >> 1][j][2 * (i & 1) + 1], ev[j].y)));
+            any |= top[i] > m[i] + 15.f;
+          }
+          return __any_sync(0xffffffffu, any);
+        };
+        bool grown = grew();
+        if (FP8 && grown && lower_zeros<C::ROWB, KT>(sv, sc + 4 * KT, lane)) {
+          __syncwarp();
+          exponents();
+          grown = grew();
         }
-        if (__any_sync(0xffffffffu, grew)) {
+        if (grown) {
 #pragma unroll
           for (int i = 0; i < RS; ++i) {
             top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
             top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
-            const float mn = fmaxf(m[i], top[i] - 7.f), alpha = exp2_fast(m[i] - (mn == -INFINITY ? 0.f : mn));
+            const float mn = fmaxf(m[i], top[i] - 7.f);
+            // (in two steps: l may be as far above 1 as the factor is below it)
+            const float half = exp2_fast(0.5f * (m[i] - (mn == -INFINITY ? 0.f : mn))), alpha = half * half;
             m[i] = mn;
-            l[i] *= alpha;
+            l[i] = l[i] * half * half;
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
               o[i >> 1][j][2 * (i & 1)] *= alpha;
@@ -484,17 +522,13 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, RS>::THREADS, KA_CTAS) kv_atten
           const float ref = m[i] == -INFINITY ? 0.f : m[i];  // (nothing seen yet: exp2(-inf) = 0)
 #pragma unroll
           for (int j = 0; j < NK; ++j) {
-            const float x0 = exp2_fast(s[i >> 1][j][2 * (i & 1)] - ref), x1 = exp2_fast(s[i >> 1][j][2 * (i & 1) + 1] - ref);
+            const float s0 = s[i >> 1][j][2 * (i & 1)], s1 = s[i >> 1][j][2 * (i & 1) + 1];
+            const float x0 = exp2_fast(term(s0, ev[j].x) - ref), x1 = exp2_fast(term(s1, ev[j].y) - ref);
             // (fp16: 11 bits cut off, so that what they leave needs no widening)
             const float h0 = __uint_as_float(__float_as_uint(x0) & 0xffffe000u), h1 = __uint_as_float(__float_as_uint(x1) & 0xffffe000u);
             const uint32_t hi = FP8 ? pack_f16x2(h0, h1) : pack_bf16x2(x0, x1);
             const uint32_t lo = FP8 ? pack_f16x2(x0 - h0, x1 - h1) : pack_bf16x2(x0 - bf16_lo(hi), x1 - bf16_hi(hi));
-            if (FP8) {
-              const float2 vi = lds_f2(sc + 4 * (2 * KT + 8 * j + 2 * place));
-              l[i] = fmaf(x1, vi.y, fmaf(x0, vi.x, l[i]));
-            } else {
-              l[i] += x0 + x1;
-            }
+            l[i] += FP8 ? exp2_fast(s0 - ref) + exp2_fast(s1 - ref) : x0 + x1;
             p[j >> 1][i >> 1][2 * (j & 1) + (i & 1)] = hi;
             if (OWN_LO)
               p_lo[OWN_LO ? j >> 1 : 0][i >> 1][2 * (j & 1) + (i & 1)] = lo;
@@ -636,9 +670,9 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, RS>::THREADS, KA_CTAS) kv_atten
       }
 #pragma unroll
       for (int w = 0; w < C::WARPS; ++w) {
-        const float f = x[w].x == -INFINITY ? 0.f : exp2_fast(x[w].x - top);
-        wt[r * 8 + w] = f;
-        sum = fmaf(x[w].y, f, sum);
+        const float half = part_half(x[w].x, top);
+        wt[r * 8 + w] = half * half;
+        sum = fmaf(x[w].y * half, half, sum);
       }
       if (it.whole())
         row[r] = finish_row(a, it.row0, it.g * rep, it.first, rep, r, top, sum);

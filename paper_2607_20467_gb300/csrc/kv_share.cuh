@@ -234,6 +234,10 @@ __device__ __forceinline__ float exp2_fast(float x) {
   return y;
 }
 
+// The root of a part's weight, the largest reference top: l is scaled by it twice, as l may be as far above
+// 1 as the weight is below it (values' exponents, which the references hold and l does not).
+__device__ __forceinline__ float part_half(float m, float top) { return m == -INFINITY ? 0.f : exp2_fast(0.5f * (m - top)); }
+
 // The parts of an item, left by its CTAs, joined by THREADS threads (tid of them; sync: their barrier):
 // every part's {m, l} into shared memory (w, [rows][parts]) at once, a row's weights by a thread or
 // a warp (what its components need in row); then four components of a row a thread, 12 to 16 loads in
@@ -260,9 +264,9 @@ __device__ __forceinline__ void join_parts(const KvAttn& a, const KaJoin& it, in
       for (int c = 0; c < n; ++c) top = fmaxf(top, wr[c].x);
       for (int c = 0; c < n; ++c) {
         const float2 x = wr[c];
-        const float f = x.x == -INFINITY ? 0.f : exp2_fast(x.x - top);
-        wr[c].x = f;
-        sum = fmaf(x.y, f, sum);
+        const float half = part_half(x.x, top);
+        wr[c].x = half * half;
+        sum = fmaf(x.y * half, half, sum);
       }
       row[r] = finish_row(a, it.row0, it.head0, it.first, rep, r, top, sum);
     }
@@ -274,9 +278,9 @@ __device__ __forceinline__ void join_parts(const KvAttn& a, const KaJoin& it, in
       top = warp_max(top);
       for (int c = lane; c < n; c += 32) {
         const float2 x = wr[c];
-        const float f = x.x == -INFINITY ? 0.f : exp2_fast(x.x - top);
-        wr[c].x = f;
-        sum = fmaf(x.y, f, sum);
+        const float half = part_half(x.x, top);
+        wr[c].x = half * half;
+        sum = fmaf(x.y * half, half, sum);
       }
       sum = warp_sum(sum);
       if (lane == 0) row[r] = finish_row(a, it.row0, it.head0, it.first, rep, r, top, sum);

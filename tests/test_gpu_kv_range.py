@@ -120,3 +120,44 @@ def test_weights_keep_more_bits_than_the_output(ops, kernel, fp8):
     q[:, :, 0] = 1.0
     q[:, :, 1] = 0.97 * 2.0 ** -11 * np.log2(np.e)
     Case(ops, k, v, fp8).check(ops, q, scale=float(np.log(2.0)), wide=wide)
+
+
+@pytest.mark.parametrize("kernel", FEW)
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("down", [16, 24, 32, 50])
+def test_zero_vectors_do_not_cost_small_values_their_bits(ops, kernel, hd, down):
+    """Zero vectors are stored with exponent 0, whatever the others' sizes."""
+    rng = np.random.default_rng(down)
+    n = 300
+    for zero in (rng.random(n) < 0.3, np.arange(n) < 150, np.arange(n) >= 150, np.arange(n) % 32 != 7):
+        k, v = rng.normal(0, 1, (2, n, 2, hd))
+        v = np.where(zero[:, None, None], 0.0, v * 2.0 ** -down)
+        c = Case(ops, k, v, True)
+        c.check(ops, _q(rng, kernel, 2, hd), wide=KERNELS[kernel][2])
+        c.check(ops, _q(rng, kernel, 2, hd, 5.0), causal=True, wide=KERNELS[kernel][2])
+
+
+@pytest.mark.parametrize("kernel", FEW)
+def test_zero_vectors_alone(ops, kernel):
+    rng = np.random.default_rng(1)
+    k = rng.normal(0, 1, (200, 1, 64))
+    Case(ops, k, np.zeros_like(k), True).check(ops, _q(rng, kernel, 1, 64), wide=KERNELS[kernel][2])
+
+
+@pytest.mark.parametrize("kernel", FEW)
+@pytest.mark.parametrize("hd", [64, 128])
+def test_sizes_at_both_ends_of_the_exponents(ops, kernel, hd):
+    """Values of 2^-55 that have nearly all of the weight beside some of 2^118 that have 2^-30 of it, and so
+    decide the result: the sum of the weights counts the first."""
+    rng = np.random.default_rng(2)
+    n, rep, new = 260, *KERNELS[kernel][:2]
+    large = rng.permutation(n) < 40
+    k = np.zeros((n, 1, hd))
+    k[:, 0, 0] = np.where(large, -30.0, 0.0)
+    k[:, 0, 1:] = 0.05 * rng.normal(0, 1, (n, hd - 1))
+    v = rng.normal(0, 1, (n, 1, hd)) * np.where(large, 2.0 ** 118, 2.0 ** -55)[:, None, None]
+    c = Case(ops, k, v, True)
+    q = rng.normal(0, 1, (new, rep, hd))
+    q[:, :, 0] = 1.0
+    q = torch.from_numpy(q).to(torch.bfloat16).cuda()
+    c.check(ops, q, scale=float(np.log(2.0)), wide=KERNELS[kernel][2])
