@@ -2,24 +2,19 @@
 // tensor cores: the rows of an item (up to 256: new positions x the query heads of one kv head)
 // fill one or two tiles of 128, and one pass over the keys serves them all.
 //
-// Per unit of 128 keys: S = Q K^T into TMEM; P = exp2(S scaled + e - m) in two fp16 parts (11 bits and what
-// they leave) takes the place of its scores there; O += P V in TMEM.  (One part costs a row that sees
-// little but a few keys up to 2^-11 of its result, and saves 5 us of 112 at 16 sequences of 8192 keys,
-// 224 rows a kv head.)  P, m, l and the exponents e of the values are those of kv_attention.cu; a
-// thread owns a row, so its statistics need no exchange.
+// Per unit of 128 keys: S = Q K^T into TMEM; P = exp2(S scaled - m) in two bf16 parts (2^-16 of itself) takes
+// the place of its scores there; O += P V in TMEM.  A thread owns a row, so its statistics need no
+// exchange.
 //
-// FP8 pages.  Eight warps copy codes into shared memory (16-byte asynchronous copies, one unit
-// ahead) and widen them into the fp16 operand tiles, each code times 2^(e_j - e_max + 6) with e_max
-// the largest exponent of the 32 keys that the warp has: that fills fp16 (448 * 2^6 = 28672), and is
-// exact but for a vector more than 2^21 below the largest of the 32, which loses low bits.  What is
-// left of the exponents is one number for 32 columns of S, so that the rows' loop loads none (an
-// exponent for every column cost it half its time).  bf16 pages: keys are copied straight into
-// their tile and multiplied in bf16; values are scaled into fp16 in place, the largest component of
-// 32 vectors to 2^14 .. 2^15 (bf16's 8 bits are kept by components down to 2^-31 of that one).
+// All operands are bf16, which holds every value that a cache stores: FP8 codes are widened with their
+// exponents, so that nothing is lost whatever the sizes of neighbouring keys and values, and the rows'
+// loop knows of no exponents.  Eight warps copy the pages into shared memory (16-byte asynchronous
+// copies, one unit ahead), bf16 straight into the operand tiles, FP8 codes into a buffer from which
+// they widen them.  (fp16 operands, scaled by the largest exponent of 32 keys, lost those far below it.)
 // V's tile is [key][hd], the transposed ("MN-major") form of the B operand, as it comes.
 //
-// The reference m, 7 below a row's largest score when it is taken, moves only when a unit's passes it by
-// more than 15; O is scaled then.
+// The reference m, 32 above a row's largest score when it is taken, moves only when a unit's passes it
+// by more than 8; O is scaled then.  (P stays far below 1, so that no sum of large values overflows.)
 //
 // 16 sequences of 8192 positions, FP8, 28 / 4 heads of 128, 32 new positions each (224 rows a kv head;
 // 143 MB, 60 GFLOP): 108.5 us, 0.28 of the tensor rate.  Neither memory (0.18) nor the tensor pipe
@@ -48,6 +43,8 @@ namespace {
 
 constexpr int TC_ROWS = 256;      // rows of an item
 constexpr int TC_START = 2;       // units of keys that beginning an item takes
+constexpr float TC_ABOVE = 32.f;  // of a row's largest score, where its reference is taken
+constexpr float TC_SLACK = 8.f;   // by how much a later score may pass that one
 constexpr int TC_THREADS = 544;
 constexpr int TC_BOX = 128 * 128; // 128 rows of 128 bytes, swizzled
 constexpr int TC_JOIN = 8000;     // rows x parts joined at a time
@@ -59,22 +56,15 @@ struct TcCfg {
   static constexpr int NS = 4;                        // operand tiles of keys and values, in turn
   static constexpr int KV = 2 * TILE;                 // (q comes first)
   static constexpr int RAW = KV + NS * TILE;          // FP8: codes of a unit's keys, then of its values
-  static constexpr int EXP = RAW + (FP8 ? 2 * 128 * HD : 0);  // [4 units][4 x 32 keys] of KeyScale (keys may be two units ahead)
-  static constexpr int BAR = EXP + 4 * 4 * 16;
+  static constexpr int THERE = RAW + (FP8 ? 2 * 128 * HD : 0);  // [4 units][4 x 32 keys]: a bit for each key that is there
+  static constexpr int BAR = THERE + 4 * 4 * 4;                 // (keys may be two units ahead)
   static constexpr int NBARS = 2 * NS + 4 * 2 + 1;
   static constexpr int HOLDER = BAR + 8 * NBARS;      // TMEM address, abort flag
   static constexpr int WALK = HOLDER + 8;
   static constexpr int TODO = WALK + (int)sizeof(KaWalk);
   static constexpr size_t SMEM = TODO + 3 * sizeof(KaJoin);
   static_assert(SMEM <= 232448, "shared memory per CTA");
-  static_assert(TC_JOIN * 8 + TC_ROWS * 8 <= EXP, "a join's weights take the place of the operands");
-};
-
-// Of 32 keys: the power of two that their scores lack, the exponent e that their values lack and 2^-e, and
-// a bit for each key that is there.
-struct KeyScale {
-  float key, e, inv;
-  uint32_t there;
+  static_assert(TC_JOIN * 8 + TC_ROWS * 8 <= THERE, "a join's weights take the place of the operands");
 };
 
 // The value of lane 0, which the compiler then knows to be the whole warp's (uniform registers).
@@ -92,8 +82,8 @@ __device__ __forceinline__ uint64_t sw128_desc_mn(uint32_t saddr) {
   return d;
 }
 constexpr uint32_t IDESC_B_MN = 1u << 16;
-// D += A B with A (fp16 pairs) in TMEM.
-__device__ __forceinline__ void umma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+// D += A B with A (bf16 pairs) in TMEM.
+__device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
@@ -115,17 +105,16 @@ __device__ __forceinline__ uint4 lds128(uint32_t a) {
   asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
   return v;
 }
-__device__ __forceinline__ uint32_t widen(uint32_t w, int half) {  // two E4M3 codes to two fp16
+// Two E4M3 codes times f (bf16 pairs), exactly: the code by way of fp16 and fp32, which hold it.
+__device__ __forceinline__ uint32_t widen(uint32_t w, int half, __nv_bfloat162 f) {
   uint32_t r;
   if (half)
     asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, h;\n\t}" : "=r"(r) : "r"(w));
   else
     asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\t}" : "=r"(r) : "r"(w));
-  return r;
-}
-__device__ __forceinline__ uint32_t times(uint32_t x, __half2 f) {
-  __half2 y = __hmul2(*reinterpret_cast<__half2*>(&x), f);
-  return *reinterpret_cast<uint32_t*>(&y);
+  const float2 x = __half22float2(*reinterpret_cast<__half2*>(&r));
+  const __nv_bfloat162 y = __hmul2(__floats2bfloat162_rn(x.x, x.y), f);
+  return *reinterpret_cast<const uint32_t*>(&y);
 }
 
 // The MMAs of an item (the whole warp; one lane issues).  Its operands are made known as the warp's, in
@@ -134,8 +123,8 @@ template <int HD, bool FP8>
 __device__ __forceinline__ bool tc_mma(uint32_t base, uint32_t tmem, int tiles, int n, uint32_t& seq_, uint32_t& items,
                                        uint32_t& units, volatile int* abort_flag) {
   using C = TcCfg<HD, FP8>;
-  constexpr uint32_t idesc_s = FP8 ? make_idesc_f16(128, 128) : make_idesc(128, 128);
-  constexpr uint32_t idesc_o = make_idesc_f16(128, HD) | IDESC_B_MN;
+  constexpr uint32_t idesc_s = make_idesc(128, 128);
+  constexpr uint32_t idesc_o = make_idesc(128, HD) | IDESC_B_MN;
   base = (uint32_t)warp_uniform((int)base);
   tmem = (uint32_t)warp_uniform((int)tmem);
   tiles = warp_uniform(tiles);
@@ -183,7 +172,7 @@ __device__ __forceinline__ bool tc_mma(uint32_t base, uint32_t tmem, int tiles, 
         for (int k = 0; k < 8; ++k)  // (P's parts stand where its scores were: per 32 keys 16 of their columns each)
 #pragma unroll
           for (int part = 0; part < 2; ++part)
-            umma_f16_ts(tmem + 256u + (uint32_t)(HD * t), tmem + 128u * t + 32 * (k >> 1) + 16 * part + 8 * (k & 1),
+            umma_bf16_ts(tmem + 256u + (uint32_t)(HD * t), tmem + 128u * t + 32 * (k >> 1) + 16 * part + 8 * (k & 1),
                         dv + k * (2048 >> 4), idesc_o, (u > 0 || k > 0 || part > 0) ? 1u : 0u);
         umma_commit(p_empty0 + 8 * t);
         if (t + 1 == tiles) umma_commit(empty0 + 8 * ((seq + 1) % C::NS));
@@ -262,6 +251,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     constexpr int PK = CH / 4;                       // this lane's of a key: key (lane >> 2) + 8 i, chunk (lane & 3) + 4 j
     const int shift = kv.page_shift, P = kv.page_len(), at_key = 32 * w4 + (lane >> 2), at_chunk = lane & 3;
     const void* pool = values ? kv.v : kv.k;
+    const int8_t* exps = values ? kv.v_exp : kv.k_exp;
     const uint32_t raw = base + C::RAW + values * (128 * HD);
     uint32_t seq = values;  // operand tiles (keys and values in turn): stage seq % NS
     bool ok = true;
@@ -299,33 +289,27 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
         }
         copy_commit();
       };
-      auto exp_at = [&](int unit, int page, const int8_t* exps) {
-        return FP8 && page >= 0 ? (int)exps[vec_of(page, first + unit * KA_UNIT + lane)] : -128;
+      auto exp_at = [&](int unit, int page) {
+        return FP8 && page >= 0 ? (int)exps[vec_of(page, first + unit * KA_UNIT + lane)] : 0;
       };
-      auto largest = [&](int e) { return __reduce_max_sync(0xffffffffu, e); };
       int pages = page_at(0), pages2 = page_at(1);
-      int ek = 0, ev = 0;  // (the keys' warps look up both)
-      if (FP8) {
-        if (!values) ek = exp_at(0, pages, kv.k_exp);
-        ev = exp_at(0, pages, kv.v_exp);
-      }
+      int e = exp_at(0, pages);
       if (!FP8) ok = wait_empty(seq);
       if (ok) issue(0, pages, FP8 ? raw : stage_of(seq));
       for (int u = 0; ok && u < n; ++u) {
         const uint32_t dst = stage_of(seq), here = __ballot_sync(0xffffffffu, pages >= 0);
-        KeyScale* out = reinterpret_cast<KeyScale*>(smem + C::EXP) + ((seq >> 1) & 3) * 4 + w4;
         copy_wait<0>();
         __syncwarp();
         if (FP8) {
-          const int top_k = largest(ek), top_v = largest(ev), top = values ? top_v : top_k;
-          const float mine = kv_pow2((values ? ev : ek) - top + 6);  // (0 exponents of keys that are not there: zeros below)
+          const float scale = kv_pow2(e);
+          const uint32_t mine = pack_bf16x2(scale, scale);  // (exact)
           ok = wait_empty(seq);
           if (!ok) break;
-          if (!values && lane == 0) *out = KeyScale{kv_pow2(top_k - 6), (float)(top_v - 6), kv_pow2(6 - top_v), here};
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int k = at_key + 8 * i;
-            const __half2 f = __float2half2_rn(__shfl_sync(0xffffffffu, mine, k & 31));
+            const uint32_t f2 = __shfl_sync(0xffffffffu, mine, k & 31);
+            const __nv_bfloat162 f = *reinterpret_cast<const __nv_bfloat162*>(&f2);
             const bool in = here >> (k & 31) & 1;
             uint4 x[PK];
 #pragma unroll
@@ -335,7 +319,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
               const uint32_t w[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
               uint32_t y[8];
 #pragma unroll
-              for (int z = 0; z < 8; ++z) y[z] = times(widen(w[z >> 1], z & 1), f);
+              for (int z = 0; z < 8; ++z) y[z] = widen(w[z >> 1], z & 1, f);
               if (here != 0xffffffffu) {
 #pragma unroll
                 for (int z = 0; z < 8; ++z) y[z] = in ? y[z] : 0u;
@@ -345,53 +329,14 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
               st_shared_v4(dst + tile_at(k, c + 1), y[4], y[5], y[6], y[7]);
             }
           }
-        } else if (!values) {
-          if (here != 0xffffffffu) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-              for (int j = 0; j < PK; ++j)
-                if (!(here >> ((at_key + 8 * i) & 31) & 1)) st_shared_v4(dst + tile_at(at_key + 8 * i, at_chunk + 4 * j), 0, 0, 0, 0);
-          }
-          if (lane == 0) {
-            out->key = 1.f;
-            out->there = here;
-          }
-        } else {
-          uint32_t top = 0;  // largest finite magnitude, as bf16 bits
+        } else if (here != 0xffffffffu) {
 #pragma unroll
           for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int j = 0; j < PK; ++j) {
-              const int k = at_key + 8 * i;
-              const uint4 x = here >> (k & 31) & 1 ? lds128(dst + tile_at(k, at_chunk + 4 * j)) : make_uint4(0, 0, 0, 0);
-              const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-              for (int z = 0; z < 4; ++z) {
-                const uint32_t lo = w[z] & 0x7fffu, hi = (w[z] >> 16) & 0x7fffu;
-                top = max(top, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
-              }
-            }
-          top = __reduce_max_sync(0xffffffffu, top);
-          const int e = top ? max(-100, (int)(top >> 7) - 127 - 14) : 0;
-          const float f = kv_pow2(-e);
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < PK; ++j) {
-              const int k = at_key + 8 * i;
-              const uint32_t at = dst + tile_at(k, at_chunk + 4 * j);
-              const uint4 x = here >> (k & 31) & 1 ? lds128(at) : make_uint4(0, 0, 0, 0);
-              uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-              for (int z = 0; z < 4; ++z) w[z] = pack_f16x2(bf16_lo(w[z]) * f, bf16_hi(w[z]) * f);
-              st_shared_v4(at, w[0], w[1], w[2], w[3]);
-            }
-          if (lane == 0) {
-            out->e = (float)e;
-            out->inv = f;
-          }
+            for (int j = 0; j < PK; ++j)
+              if (!(here >> ((at_key + 8 * i) & 31) & 1)) st_shared_v4(dst + tile_at(at_key + 8 * i, at_chunk + 4 * j), 0, 0, 0, 0);
         }
+        if (!values && lane == 0) *reinterpret_cast<volatile uint32_t*>(smem + C::THERE + (((seq >> 1) & 3) * 4 + w4) * 4) = here;
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(full0 + 8 * (seq % C::NS));
@@ -400,10 +345,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
           if (!FP8) ok = wait_empty(seq);
           if (!ok) break;
           issue(u + 1, pages2, FP8 ? raw : stage_of(seq));
-          if (FP8) {
-            if (!values) ek = exp_at(u + 1, pages2, kv.k_exp);
-            ev = exp_at(u + 1, pages2, kv.v_exp);
-          }
+          e = exp_at(u + 1, pages2);
           pages = pages2;
           pages2 = page_at(u + 2);
         }
@@ -430,6 +372,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     const uint32_t s_at = tmem + 128u * t + ((uint32_t)(32 * quarter) << 16);
     const uint32_t o_at = tmem + 256u + (uint32_t)(HD * t) + ((uint32_t)(32 * quarter) << 16);
     auto rows_bar = [] { asm volatile("bar.sync 1, 256;" ::: "memory"); };
+    const float qf = fmaxf(a.scale * kLog2e, 1.2e-38f);  // (not 0: a masked score is -inf)
     uint32_t count = 0, seq = 0;
     // After a wait that ran out a warp goes on through the items without work: the barrier of the rows'
     // warps has one count for all of them.
@@ -445,43 +388,22 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
       const int n = it.until - it.from, tiles = it.rows > 128 ? 2 : 1;
       const int row = 128 * t + r;
       const bool live = row < it.rows, band = 128 * t + 32 * quarter < it.rows;
-      float qa = a.scale * kLog2e;
       // ---- q: the band's rows into their tile, 16-byte chunks of a row by neighbouring lanes
       if (ok && t < tiles) {
-        constexpr int CPR = HD / 8, RPL = 32 / CPR, HALF = 32 / RPL;  // chunks of a row, rows of a load, loads in flight
+        constexpr int CPR = HD / 8, RPL = 32 / CPR, LOADS = 32 / RPL;  // chunks of a row, rows of a load, loads
         const int c = lane % CPR;
-        int e_row = 0;  // exponent of this thread's row
-#pragma unroll 1
-        for (int i0 = 0; i0 < HALF; i0 += HALF) {
-          uint4 x[HALF];
+        uint4 x[LOADS];
 #pragma unroll
-          for (int i = 0; i < HALF; ++i) {
-            const int rb = 32 * quarter + RPL * (i0 + i) + lane / CPR, q = it.first + 128 * t + rb, tk = q / rep;
-            x[i] = make_uint4(0, 0, 0, 0);
-            if (128 * t + rb < it.rows)
-              x[i] = *reinterpret_cast<const uint4*>(a.q + (it.row0 + tk) * a.q_stride + (int64_t)(it.g * rep + q - tk * rep) * HD + 8 * c);
-          }
-#pragma unroll
-          for (int i = 0; i < HALF; ++i) {
-            uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-            if (FP8) {
-              float top = 0.f;
-#pragma unroll
-              for (int j = 0; j < 4; ++j) top = fmaxf(top, fmaxf(fabsf(bf16_lo(w[j])), fabsf(bf16_hi(w[j]))));
-#pragma unroll
-              for (int d = CPR / 2; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-              const int e = max(-120, min(120, (int)(__float_as_uint(top) >> 23) - 127));
-              const float down = kv_pow2(-e);
-#pragma unroll
-              for (int j = 0; j < 4; ++j) w[j] = pack_f16x2(bf16_lo(w[j]) * down, bf16_hi(w[j]) * down);
-              const int own = __shfl_sync(0xffffffffu, e, (lane % RPL) * CPR);
-              if (lane / RPL == i0 + i) e_row = own;
-            }
-            st_shared_v4(base + t * C::TILE + (uint32_t)(c >> 3) * TC_BOX + swz(32 * quarter + RPL * (i0 + i) + lane / CPR, c & 7),
-                         w[0], w[1], w[2], w[3]);
-          }
+        for (int i = 0; i < LOADS; ++i) {
+          const int rb = 32 * quarter + RPL * i + lane / CPR, q = it.first + 128 * t + rb, tk = q / rep;
+          x[i] = make_uint4(0, 0, 0, 0);
+          if (128 * t + rb < it.rows)
+            x[i] = *reinterpret_cast<const uint4*>(a.q + (it.row0 + tk) * a.q_stride + (int64_t)(it.g * rep + q - tk * rep) * HD + 8 * c);
         }
-        if (FP8) qa *= kv_pow2(e_row);
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i)
+          st_shared_v4(base + t * C::TILE + (uint32_t)(c >> 3) * TC_BOX + swz(32 * quarter + RPL * i + lane / CPR, c & 7),
+                       x[i].x, x[i].y, x[i].z, x[i].w);
         fence_proxy_async_smem();
         tc_fence_before();
         __syncwarp();
@@ -493,28 +415,28 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
       for (int u = 0; ok && t < tiles && u < n; ++u, seq += 2) {
         const uint32_t blk = seq >> 1;
         if (!row_wait(s_full0 + 8 * t, count & 1u)) break;
-        // (bf16: the values' exponents come with their tile)
-        if (!FP8 && !row_wait(full0 + 8 * ((seq + 1) % C::NS), ((seq + 1) / C::NS) & 1u)) break;
         tc_fence_after();
         if (band) {
-          const uint32_t scales = base + C::EXP + (blk & 3) * 64;
+          const uint32_t there0 = base + C::THERE + (blk & 3) * 16;
           uint32_t s0[32];  // 32 scores
-          // ---- the row's largest score
-          float top = -INFINITY;
-          auto largest = [&](uint32_t (&s)[32], int c) {
-            const float4 scale = ld_shared_v4(scales + 16 * c);
-            const uint32_t there = __float_as_uint(scale.w);
+          auto mask = [&](uint32_t (&s)[32], int c) {  // keys that are not there
+            const uint32_t there = __float_as_uint(ld_shared_f32(there0 + 4 * c));
             if (there != 0xffffffffu) {
 #pragma unroll
               for (int i = 0; i < 32; ++i) s[i] = there >> i & 1 ? s[i] : 0xff800000u;
             }
+          };
+          // ---- the row's largest score
+          float top = -INFINITY;
+          auto largest = [&](uint32_t (&s)[32], int c) {
+            mask(s, c);
             float a0 = -INFINITY, a1 = -INFINITY;
 #pragma unroll
             for (int i = 0; i < 32; i += 4) {
               a0 = max3f(a0, f32(s[i]), f32(s[i + 1]));
               a1 = max3f(a1, f32(s[i + 2]), f32(s[i + 3]));
             }
-            top = fmaxf(top, fmaf(fmaxf(a0, a1), qa * scale.x, scale.y));
+            top = fmaxf(top, fmaxf(a0, a1) * qf);
           };
 #pragma unroll 1
           for (int c = 0; c < 4; ++c) {
@@ -522,10 +444,10 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
             tmem_ld_wait();
             largest(s0, c);
           }
-          // ---- a larger reference where that passes it by more than 15, or is the row's first
-          const bool grew = top > m + 15.f;
+          // ---- a larger reference where that passes it too far, or is the row's first
+          const bool grew = top > m - (TC_ABOVE - TC_SLACK);
           if (__any_sync(0xffffffffu, grew)) {
-            const float mn = grew ? top - 7.f : m, alpha = grew ? ex2_approx(m - mn) : 1.f;
+            const float mn = grew ? top + TC_ABOVE : m, alpha = grew ? ex2_approx(m - mn) : 1.f;
             m = mn;
             l *= alpha;
             if (u > 0) {  // (the product before this unit's scores is done: they came after it)
@@ -542,19 +464,12 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
               }
             }
           }
-          // ---- P, into the places of its scores: per 32 keys 16 columns of fp16 pairs, and 16 of what they leave
+          // ---- P, into the places of its scores: per 32 keys 16 columns of bf16 pairs, and 16 of what they leave
           const float ref = m == -INFINITY ? 0.f : m;
           auto weigh = [&](uint32_t (&s)[32], int c) {
-            const float4 scale = ld_shared_v4(scales + 16 * c);
-            const uint32_t there = __float_as_uint(scale.w);
-            const float qf = fmaxf(qa * scale.x, 1.2e-38f), add = scale.y - ref;  // (not 0: a masked score is -inf)
-            const unsigned long long qf2 = pk2(qf, qf), add2 = pk2(add, add);
-            const unsigned long long minus1 = pk2(-1.f, -1.f);
+            mask(s, c);
+            const unsigned long long qf2 = pk2(qf, qf), add2 = pk2(-ref, -ref), minus1 = pk2(-1.f, -1.f);
             unsigned long long sum2 = pk2(0.f, 0.f);
-            if (there != 0xffffffffu) {
-#pragma unroll
-              for (int i = 0; i < 32; ++i) s[i] = there >> i & 1 ? s[i] : 0xff800000u;
-            }
 #pragma unroll
             for (int i0 = 0; i0 < 32; i0 += 16) {
               uint32_t w[8], rest[8];
@@ -564,17 +479,18 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
                 upk2(ffma2(pk2(f32(s[i]), f32(s[i + 1])), qf2, add2), x0, x1);
                 const float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
                 sum2 = fadd2(pk2(p0, p1), sum2);
-                const float h0 = f32(__float_as_uint(p0) & 0xffffe000u), h1 = f32(__float_as_uint(p1) & 0xffffe000u);
-                w[(i - i0) / 2] = pack_f16x2(h0, h1);
-                upk2(ffma2(pk2(h0, h1), minus1, pk2(p0, p1)), x0, x1);
-                rest[(i - i0) / 2] = pack_f16x2(x0, x1);
+                // (the upper halves: 8 bits cut off)
+                const uint32_t b0 = __float_as_uint(p0), b1 = __float_as_uint(p1);
+                w[(i - i0) / 2] = __byte_perm(b0, b1, 0x7632);
+                upk2(ffma2(pk2(f32(b0 & 0xffff0000u), f32(b1 & 0xffff0000u)), minus1, pk2(p0, p1)), x0, x1);
+                rest[(i - i0) / 2] = pack_bf16x2(x0, x1);
               }
               tmem_st8(s_at + 32 * c + i0 / 2, w);
               tmem_st8(s_at + 32 * c + 16 + i0 / 2, rest);
             }
             float lo, hi;
             upk2(sum2, lo, hi);
-            l = fmaf(lo + hi, scale.z, l);
+            l += lo + hi;
           };
 #pragma unroll 1
           for (int c = 3; c >= 0; --c) {  // (the last 32 are here still)

@@ -161,3 +161,47 @@ def test_sizes_at_both_ends_of_the_exponents(ops, kernel, hd):
     q[:, :, 0] = 1.0
     q = torch.from_numpy(q).to(torch.bfloat16).cuda()
     c.check(ops, q, scale=float(np.log(2.0)), wide=KERNELS[kernel][2])
+
+
+@pytest.mark.parametrize("kernel", list(KERNELS))
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("spread", [12, 20, 30])
+def test_a_row_that_sees_one_small_value_among_large_ones(ops, kernel, hd, spread):
+    """Values of sizes 2^-spread to 2^spread side by side."""
+    rng = np.random.default_rng(spread)
+    n = 200
+    k, v = rng.normal(0, 1, (2, n, 2, hd))
+    v *= np.exp2(rng.integers(-spread, spread + 1, (n, 2, 1)))
+    for fp8 in (True, False):
+        Case(ops, k, v, fp8).check(ops, _sharp(rng, kernel, k), wide=KERNELS[kernel][2])
+
+
+@pytest.mark.parametrize("kernel", list(KERNELS))
+def test_small_keys_beside_large_ones_that_have_no_weight(ops, kernel):
+    """Keys of 2^25 against the rows' direction, between keys of 2^-8 whose scores are small numbers."""
+    rng = np.random.default_rng(4)
+    n, hd = 150, 64
+    rep, new, wide = KERNELS[kernel]
+    k = 2.0 ** -8 * rng.normal(0, 1, (n, 1, hd))
+    k[:, :, 0] = 0.0
+    k[::5] = 0.0
+    k[::5, :, 0] = -2.0 ** 25
+    v = rng.normal(0, 1, (n, 1, hd))
+    q = 2.0 ** 8 * rng.normal(0, 1, (new, rep, hd))
+    q[:, :, 0] = 2.0 ** 8
+    q = torch.from_numpy(q).to(torch.bfloat16).cuda()
+    for fp8 in (True, False):
+        Case(ops, k, v, fp8).check(ops, q, wide=wide)
+
+
+@pytest.mark.parametrize("kernel", list(KERNELS))
+@pytest.mark.parametrize("down", [16, 24, 32, 50])
+def test_pages_of_zeros_between_small_values(ops, kernel, down):
+    rng = np.random.default_rng(down)
+    n, hd = 320, 64
+    k, v = rng.normal(0, 1, (2, n, 2, hd))
+    v *= 2.0 ** -down
+    for zero in (np.arange(n) // 32 % 2 == 0, rng.random(n) < 0.3):
+        for fp8 in (True, False):
+            c = Case(ops, k, np.where(zero[:, None, None], 0.0, v), fp8)
+            c.check(ops, _q(rng, kernel, 2, hd), wide=KERNELS[kernel][2])
