@@ -229,6 +229,7 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, RS>::THREADS, KA_CTAS) kv_atten
   using C = KaCfg<HD, FP8, RS>;
   constexpr int MT = C::MT;
   constexpr bool OWN_LO = RS > 1;  // the weights' second parts are products of their own
+  constexpr float ABOVE = FP8 ? -7.f : 32.f, SLACK = 8.f;  // the reference above the largest score, and how far that may be passed
   constexpr int KS = HD / 16;  // k steps of S, and pairs of column tiles of O
   constexpr int NT = HD / 8;   // column tiles of O
   constexpr int KT = C::KT, NK = C::NK;
@@ -473,9 +474,10 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, RS>::THREADS, KA_CTAS) kv_atten
               for (int k = 0; k < 2; ++k)
                 if (key + 8 * j + 2 * place + k >= lim[i] || (skip >> (j >> 1) & 1)) s[i >> 1][j][2 * (i & 1) + k] = -INFINITY;
         }
-        // The reference m of a row, 7 below its largest score when it is taken, moves only when a score passes
-        // it by more than 15 (P <= 2^15), so that most steps neither exchange maxima nor scale O; P fills
-        // fp16's range, for the sake of small ones that carry large values.
+        // The reference m of a row is taken ABOVE its largest score and moves only when a later one passes
+        // that by more than SLACK, so that most steps neither exchange maxima nor scale O.  FP8: below it, P <=
+        // 2^15 fills fp16's range, for the sake of small ones that carry large values.  bf16: far above, so that
+        // P times the largest values, and their sums, do not overflow.
         float top[RS];
         auto grew = [&]() {
           bool any = false;
@@ -485,7 +487,7 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, RS>::THREADS, KA_CTAS) kv_atten
 #pragma unroll
             for (int j = 0; j < NK; ++j)
               top[i] = fmaxf(top[i], fmaxf(term(s[i >> 1][j][2 * (i & 1)], ev[j].x), term(s[i >> 1][j][2 * (i & 1) + 1], ev[j].y)));
-            any |= top[i] > m[i] + 15.f;
+            any |= top[i] > m[i] - (ABOVE - SLACK);
           }
           return __any_sync(0xffffffffu, any);
         };
@@ -500,7 +502,7 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, RS>::THREADS, KA_CTAS) kv_atten
           for (int i = 0; i < RS; ++i) {
             top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
             top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
-            const float mn = fmaxf(m[i], top[i] - 7.f);
+            const float mn = fmaxf(m[i], top[i] + ABOVE);
             // (in two steps: l may be as far above 1 as the factor is below it)
             const float half = exp2_fast(0.5f * (m[i] - (mn == -INFINITY ? 0.f : mn))), alpha = half * half;
             m[i] = mn;

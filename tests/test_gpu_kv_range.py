@@ -205,3 +205,13 @@ def test_pages_of_zeros_between_small_values(ops, kernel, down):
         for fp8 in (True, False):
             c = Case(ops, k, np.where(zero[:, None, None], 0.0, v), fp8)
             c.check(ops, _q(rng, kernel, 2, hd), wide=KERNELS[kernel][2])
+
+
+@pytest.mark.parametrize("kernel", list(KERNELS))
+@pytest.mark.parametrize("fp8", [True, False])
+def test_the_largest_values(ops, kernel, fp8):
+    """Values up to 2^126: their weighted sum is no larger, and no step on the way may overflow."""
+    rng = np.random.default_rng(5)
+    k, v = rng.normal(0, 1, (2, 40, 1, 64))
+    v = np.clip(v, -3.9, 3.9) * 2.0 ** 124
+    Case(ops, k, v, fp8).check(ops, _q(rng, kernel, 1, 64), wide=KERNELS[kernel][2])
