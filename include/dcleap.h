@@ -351,7 +351,9 @@ dcl_status dcl_kv_read(dcl_ctx* ctx, const dcl_kv_cache* cache, const int32_t* s
  *   scale       > 0, or 0 for 1 / sqrt(head_dim).
  *   out_dev     bf16 [n_q][n_heads][head_dim]; lse_dev float [n_q][n_heads] or NULL.  A row that
  *               sees nothing gets zeros and -inf.
- * Scores, softmax statistics and sums are held in fp32 and reproduce bit for bit.
+ * Scores, softmax statistics and sums are held in fp32 and reproduce bit for bit; weights have 16 bits
+ * or more.  An infinite value is the result of its component for the rows that see it (NaN with one
+ * of the other sign, or where the row's weight for it is zero in fp32).
  * A context's first call that has rows allocates its scratch (41 MB, for calls of every size) and is
  * refused with STATE while the stream is being captured; every later call may be captured.
  * Errors: INVALID_ARG, STATE, OOM (scratch), CUDA. */

@@ -528,8 +528,9 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, RS>::THREADS, KA_CTAS) kv_atten
             const float x0 = exp2_fast(term(s0, ev[j].x) - ref), x1 = exp2_fast(term(s1, ev[j].y) - ref);
             // (fp16: 11 bits cut off, so that what they leave needs no widening)
             const float h0 = __uint_as_float(__float_as_uint(x0) & 0xffffe000u), h1 = __uint_as_float(__float_as_uint(x1) & 0xffffe000u);
-            const uint32_t hi = FP8 ? pack_f16x2(h0, h1) : pack_bf16x2(x0, x1);
-            const uint32_t lo = FP8 ? pack_f16x2(x0 - h0, x1 - h1) : pack_bf16x2(x0 - bf16_lo(hi), x1 - bf16_hi(hi));
+            const uint32_t hi = FP8 ? pack_f16x2(h0, h1) : upper_halves(x0, x1);
+            const uint32_t lo = FP8 ? pack_f16x2(x0 - h0, x1 - h1)
+                                    : pack_bf16x2(fmaf(x0, BF16_LO, minus_upper(x0)), fmaf(x1, BF16_LO, minus_upper(x1)));
             l[i] += FP8 ? exp2_fast(s0 - ref) + exp2_fast(s1 - ref) : x0 + x1;
             p[j >> 1][i >> 1][2 * (j & 1) + (i & 1)] = hi;
             if (OWN_LO)

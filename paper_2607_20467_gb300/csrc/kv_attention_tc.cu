@@ -468,7 +468,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
           const float ref = m == -INFINITY ? 0.f : m;
           auto weigh = [&](uint32_t (&s)[32], int c) {
             mask(s, c);
-            const unsigned long long qf2 = pk2(qf, qf), add2 = pk2(-ref, -ref), minus1 = pk2(-1.f, -1.f);
+            const unsigned long long qf2 = pk2(qf, qf), add2 = pk2(-ref, -ref), more2 = pk2(BF16_LO, BF16_LO);
             unsigned long long sum2 = pk2(0.f, 0.f);
 #pragma unroll
             for (int i0 = 0; i0 < 32; i0 += 16) {
@@ -479,10 +479,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
                 upk2(ffma2(pk2(f32(s[i]), f32(s[i + 1])), qf2, add2), x0, x1);
                 const float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
                 sum2 = fadd2(pk2(p0, p1), sum2);
-                // (the upper halves: 8 bits cut off)
-                const uint32_t b0 = __float_as_uint(p0), b1 = __float_as_uint(p1);
-                w[(i - i0) / 2] = __byte_perm(b0, b1, 0x7632);
-                upk2(ffma2(pk2(f32(b0 & 0xffff0000u), f32(b1 & 0xffff0000u)), minus1, pk2(p0, p1)), x0, x1);
+                w[(i - i0) / 2] = upper_halves(p0, p1);
+                upk2(ffma2(pk2(p0, p1), more2, pk2(minus_upper(p0), minus_upper(p1))), x0, x1);
                 rest[(i - i0) / 2] = pack_bf16x2(x0, x1);
               }
               tmem_st8(s_at + 32 * c + i0 / 2, w);

@@ -234,6 +234,14 @@ __device__ __forceinline__ float exp2_fast(float x) {
   return y;
 }
 
+// Two bf16 parts of a weight p: its upper half (8 bits), and what that leaves of p (1 + 2^-17).  The factor, the
+// same for all weights and half of what the parts may be off by, keeps the second above zero where the
+// first is: an infinite value then gives the infinity, where a part of zero would make it no number.
+constexpr float BF16_LO = 1.f + 1.f / 131072.f;
+__device__ __forceinline__ float minus_upper(float p) { return __uint_as_float((__float_as_uint(p) & 0xffff0000u) | 0x80000000u); }
+__device__ __forceinline__ uint32_t upper_halves(float p0, float p1) {
+  return __byte_perm(__float_as_uint(p0), __float_as_uint(p1), 0x7632);
+}
 // The root of a part's weight, the largest reference top: l is scaled by it twice, as l may be as far above
 // 1 as the weight is below it (values' exponents, which the references hold and l does not).
 __device__ __forceinline__ float part_half(float m, float top) { return m == -INFINITY ? 0.f : exp2_fast(0.5f * (m - top)); }

@@ -215,3 +215,39 @@ def test_the_largest_values(ops, kernel, fp8):
     k, v = rng.normal(0, 1, (2, 40, 1, 64))
     v = np.clip(v, -3.9, 3.9) * 2.0 ** 124
     Case(ops, k, v, fp8).check(ops, _q(rng, kernel, 1, 64), wide=KERNELS[kernel][2])
+
+
+@pytest.mark.parametrize("kernel", list(KERNELS))
+@pytest.mark.parametrize("hd", [64, 128])
+def test_infinite_values_of_bf16_pages(ops, kernel, hd):
+    """An infinity that a row sees is its component's result, two of unlike sign or a NaN are no number, and
+    the other components are what they were."""
+    rng = np.random.default_rng(6)
+    n = 700
+    k, v = rng.normal(0, 1, (2, n, 2, hd))
+    c = Case(ops, k, v, False)
+    at = rng.permutation(n)[:6]
+    w = c.v.clone()
+    for j, d, x in ((at[0], 3, np.inf), (at[1], 9, -np.inf), (at[2], 20, np.inf), (at[3], 20, -np.inf),
+                    (at[4], 33, np.nan), (at[5], 40, np.inf), (at[0], 40, np.inf)):
+        c.cache.v[int(c.order[j // 32]), 1, int(j % 32), d] = x
+        w[int(j), 1, d] = x
+    q = _q(rng, kernel, 2, hd)
+    rep = KERNELS[kernel][0]
+    for causal in (False, True):
+        o, A, _ = c.reference(q, causal)
+        out, _ = c.attend(ops, q, causal, wide=KERNELS[kernel][2])
+        seen = torch.ones(q.shape[0], n, dtype=torch.bool, device="cuda")
+        if causal:
+            j, i = torch.arange(n, device="cuda"), torch.arange(q.shape[0], device="cuda")
+            seen = j[None, :] <= (n - q.shape[0] + i)[:, None]
+        # the sum over the seen keys of what is no finite number of w, rows x hd
+        odd = torch.where(torch.isfinite(w[:, 1]), torch.zeros_like(w[:, 1]), w[:, 1])
+        odd = torch.where(seen[:, :, None], odd[None], torch.zeros_like(odd[None])).sum(1)
+        odd = odd[:, None].expand(-1, rep, -1)
+        got, fine = out[:, rep:], odd == 0
+        assert torch.equal(got.isnan(), odd.isnan())
+        assert (got[odd.isinf()] == odd[odd.isinf()]).all()
+        bad = (got - o[:, rep:]).abs() - (2.0 ** -8 * o[:, rep:].abs() + 2.0 ** -12 * A[:, rep:])
+        assert (bad[fine] <= 0).all()
+        assert ((out - o).abs()[:, :rep] <= 2.0 ** -8 * o.abs()[:, :rep] + 2.0 ** -12 * A[:, :rep]).all()
