@@ -342,7 +342,8 @@ dcl_status dcl_kv_read(dcl_ctx* ctx, const dcl_kv_cache* cache, const int32_t* s
  *   q_start_dev int32 [batch + 1]: rows [q_start[b], q_start[b + 1]) of the n_q rows are the new
  *               positions of sequence b (from none to many; rows of no sequence stay untouched).
  *   page_table_dev int32 [batch][max_pages], seq_len_dev int32 [batch]: the pages of sequence b
- *               and how many positions it has cached (entries past them are not read).
+ *               and how many positions it has cached (entries past them are not read); max_pages *
+ *               page_len at most 2^31 - 4096.
  *   max_new     no sequence has more rows than this (with batch, heads and max_pages it chooses the
  *               kernel: results do not depend on them beyond rounding; a table much wider than
  *               the sequences are long may get the one for long sequences).

@@ -1484,9 +1484,11 @@ dcl_status dcl_kv_attention(dcl_ctx* c, const dcl_kv_cache* cache, const void* q
   if (batch == 0 || n_q == 0) return DCL_OK;
   if (!q_dev || !q_start_dev || !page_table_dev || !seq_len_dev || !out_dev)
     return fail(c, DCL_ERR_INVALID_ARG, "kv_attention: NULL argument");
-  if (max_pages <= 0 || max_new <= 0 || (int64_t)max_pages * cache->page_len >= (1ll << 31) ||
+  // (4096: the kernels look up to a few units of keys past a sequence's end in 32 bits)
+  if (max_pages <= 0 || max_new <= 0 || (int64_t)max_pages * cache->page_len > (1ll << 31) - 4096 ||
       (int64_t)n_q * n_heads >= (1ll << 31))
-    return fail(c, DCL_ERR_INVALID_ARG, "kv_attention: max_pages, max_new must be > 0 and sizes below 2^31");
+    return fail(c, DCL_ERR_INVALID_ARG,
+                "kv_attention: max_pages, max_new must be > 0, max_pages * page_len at most 2^31 - 4096, n_q * n_heads below 2^31");
   if (q_stride < (int64_t)n_heads * kv.hd || q_stride % 8 || !aligned16(q_dev) || !aligned16(out_dev))
     return fail(c, DCL_ERR_INVALID_ARG, "kv_attention: q_stride must be a multiple of 8 and hold a row, q and out 16-byte aligned");
   if (!(scale >= 0.f) || scale > 3e38f) return fail(c, DCL_ERR_INVALID_ARG, "kv_attention: scale must be >= 0");
