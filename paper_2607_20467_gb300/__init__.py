@@ -172,14 +172,46 @@ def _dev(t, name, itemsize, count=0):
     return t.data_ptr()
 
 
-def _dev_rows(t, name, itemsize, rows, cols):
+# What a buffer of each kind holds: bytes of an element, and the torch types it may have (bit patterns of the
+# kind's size among them).  A type of another meaning is refused: its bits would be read as this one's.
+_KINDS = {"bf16": (2, ("torch.bfloat16", "torch.int16", "torch.uint16")), "f32": (4, ("torch.float32",)),
+          "i32": (4, ("torch.int32", "torch.uint32")), "e4m3": (1, ("torch.float8_e4m3fn", "torch.uint8", "torch.int8")),
+          "i8": (1, ("torch.int8", "torch.uint8"))}
+_fits = {kind: set() for kind in _KINDS}  # types that have been looked at and taken
+
+
+def _check_type(t, name, kind):
+    size, types = _KINDS[kind]
+    if t.element_size() != size:
+        raise TypeError(f"{name}: elements of {size} bytes expected, got {t.dtype}")
+    if str(t.dtype).startswith("torch.") and str(t.dtype) not in types:
+        raise TypeError(f"{name}: {types[0]} expected, got {t.dtype}")
+    _fits[kind].add(t.dtype)
+
+
+def _dev_of(t, name, kind, count=0):
+    """_dev of a kind: the type's meaning is checked, not its size alone."""
+    if t is None or isinstance(t, int):
+        return t
+    if not getattr(t, "is_cuda", False):
+        raise ValueError(f"{name}: a device buffer (a CUDA tensor) is required")
+    if t.dtype not in _fits[kind]:
+        _check_type(t, name, kind)
+    if t.numel() < count:
+        raise ValueError(f"{name}: at least {count} elements needed, {t.numel()} given")
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: must be contiguous")
+    return t.data_ptr()
+
+
+def _dev_rows(t, name, kind, rows, cols):
     """Device pointer and row stride (elements) of `rows` rows of `cols` elements each: a CUDA tensor
     whose first dimension may be strided and whose rows are contiguous (a column block of a
     wider matrix is)."""
     if not getattr(t, "is_cuda", False):
         raise ValueError(f"{name}: a device buffer (a CUDA tensor) is required")
-    if t.element_size() != itemsize:
-        raise TypeError(f"{name}: elements of {itemsize} bytes expected, got {t.dtype}")
+    if t.dtype not in _fits[kind]:
+        _check_type(t, name, kind)
     shape, stride = t.shape, t.stride()  # (looked at once each: a call's host time is a few microseconds)
     n, inner = shape[0], 1
     for i in range(len(shape) - 1, 0, -1):
@@ -210,14 +242,15 @@ class KvCache:
             raise ValueError("an FP8 cache needs k_exp and v_exp")
         if not fp8 and (k_exp is not None or v_exp is not None):
             raise ValueError("a bf16 cache has no exponents")
-        n, size = pages * heads * page_len, 1 if fp8 else 2
+        n, kind = pages * heads * page_len, "e4m3" if fp8 else "bf16"
         if tuple(v.shape) != tuple(k.shape):
             raise ValueError("k and v differ in shape")
         self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
         self.n_pages, self.n_kv_heads, self.page_len, self.head_dim = pages, heads, page_len, hd
         self.format = DCL_KV_FP8 if fp8 else DCL_KV_BF16
-        self.desc = KvCacheDesc(pages, page_len, heads, hd, self.format, _dev(k, "k", size, n * hd),
-                                _dev(v, "v", size, n * hd), _dev(k_exp, "k_exp", 1, n), _dev(v_exp, "v_exp", 1, n))
+        self.desc = KvCacheDesc(pages, page_len, heads, hd, self.format, _dev_of(k, "k", kind, n * hd),
+                                _dev_of(v, "v", kind, n * hd), _dev_of(k_exp, "k_exp", "i8", n),
+                                _dev_of(v_exp, "v_exp", "i8", n))
         self.ptr = ctypes.addressof(self.desc)
         self.row = heads * hd  # elements of a position's keys
 
@@ -413,22 +446,22 @@ class Context:
         """Store rows k, v [n][kv heads][head_dim] (bf16, rows may be strided) at slots (int32 [n],
         negative: skipped)."""
         n, cols = k.shape[0], cache.row
-        kp, ks = _dev_rows(k, "k", 2, n, cols)
-        vp, vs = _dev_rows(v, "v", 2, n, cols)
+        kp, ks = _dev_rows(k, "k", "bf16", n, cols)
+        vp, vs = _dev_rows(v, "v", "bf16", n, cols)
         if ks != vs and n > 1:
             raise ValueError("k and v differ in row stride")
-        st = self._L.dcl_kv_write(self.ptr, cache.ptr, kp, vp, ks, _dev(slots, "slots", 4, n), n)
+        st = self._L.dcl_kv_write(self.ptr, cache.ptr, kp, vp, ks, _dev_of(slots, "slots", "i32", n), n)
         if st:
             self._check(st)
 
     def kv_read(self, cache, slots, k, v):
         """Read the positions at slots (int32 [n], negative: zeros) into k, v [n][kv heads][head_dim]."""
         n, cols = slots.shape[0], cache.row
-        kp, ks = _dev_rows(k, "k", 2, n, cols)
-        vp, vs = _dev_rows(v, "v", 2, n, cols)
+        kp, ks = _dev_rows(k, "k", "bf16", n, cols)
+        vp, vs = _dev_rows(v, "v", "bf16", n, cols)
         if ks != vs and n > 1:
             raise ValueError("k and v differ in row stride")
-        st = self._L.dcl_kv_read(self.ptr, cache.ptr, _dev(slots, "slots", 4, n), n, kp, vp, ks)
+        st = self._L.dcl_kv_read(self.ptr, cache.ptr, _dev_of(slots, "slots", "i32", n), n, kp, vp, ks)
         if st:
             self._check(st)
 
@@ -440,23 +473,25 @@ class Context:
         batch, max_pages = page_table.shape
         if hd != cache.head_dim:
             raise ValueError(f"q: head_dim {cache.head_dim} expected, got {hd}")
-        qp, qs = _dev_rows(q, "q", 2, n_q, heads * hd)
+        qp, qs = _dev_rows(q, "q", "bf16", n_q, heads * hd)
         self._check(self._L.dcl_kv_attention(
-            self.ptr, cache.ptr, qp, qs, _dev(q_start, "q_start", 4, batch + 1), _dev(page_table, "page_table", 4),
-            max_pages, _dev(seq_len, "seq_len", 4, batch), batch, n_q, max_new, heads, int(bool(causal)), scale,
-            _dev(out, "out", 2, n_q * heads * hd), _dev(lse, "lse", 4, n_q * heads)))
+            self.ptr, cache.ptr, qp, qs, _dev_of(q_start, "q_start", "i32", batch + 1),
+            _dev_of(page_table, "page_table", "i32"), max_pages, _dev_of(seq_len, "seq_len", "i32", batch), batch, n_q,
+            max_new, heads, int(bool(causal)), scale, _dev_of(out, "out", "bf16", n_q * heads * hd),
+            _dev_of(lse, "lse", "f32", n_q * heads)))
 
     def sample(self, logits, token, noise=None, temperature=None, top_k=None, top_p=None, min_p=None, prob=None,
                conf=None):
         """Draw token [rows] from logits [rows][V] (bf16, rows may be strided) and Gumbel numbers noise
         [rows][V]; temperature, top_k, top_p, min_p, prob, conf [rows] each (see dcl_sample)."""
         rows, V = logits.shape
-        zp, zs = _dev_rows(logits, "logits", 2, rows, V)
-        np_, ns = _dev_rows(noise, "noise", 4, rows, V) if noise is not None else (None, V)
+        zp, zs = _dev_rows(logits, "logits", "bf16", rows, V)
+        np_, ns = _dev_rows(noise, "noise", "f32", rows, V) if noise is not None else (None, V)
         self._check(self._L.dcl_sample(
-            self.ptr, zp, zs, np_, ns, rows, V, _dev(temperature, "temperature", 4, rows),
-            _dev(top_k, "top_k", 4, rows), _dev(top_p, "top_p", 4, rows), _dev(min_p, "min_p", 4, rows),
-            _dev(token, "token", 4, rows), _dev(prob, "prob", 4, rows), _dev(conf, "conf", 4, rows)))
+            self.ptr, zp, zs, np_, ns, rows, V, _dev_of(temperature, "temperature", "f32", rows),
+            _dev_of(top_k, "top_k", "i32", rows), _dev_of(top_p, "top_p", "f32", rows),
+            _dev_of(min_p, "min_p", "f32", rows), _dev_of(token, "token", "i32", rows),
+            _dev_of(prob, "prob", "f32", rows), _dev_of(conf, "conf", "f32", rows)))
 
     def op_rmsnorm(self, x, gain, y, eps):
         rows, d = x.shape
