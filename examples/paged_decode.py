@@ -90,12 +90,23 @@ class PagedModel:
 
 def generate(model, prompts, gen_len, block=32, tau=0.7, temperature=0.0, top_k=0, top_p=1.0, min_p=0.0, seed=0):
     """Tokens [batch][gen_len] after prompts of any lengths, and the number of denoise steps."""
+    n = [len(p) for p in prompts]
+    pages = []
+    try:
+        for k in n:
+            pages.append(model.pages_for(k + gen_len))
+        return _decode(model, prompts, pages, gen_len, block, tau, seed, temperature, top_k, top_p, min_p)
+    finally:  # (also where there were not enough, or a step failed)
+        for p in pages:
+            model.release(p)
+
+
+def _decode(model, prompts, pages, gen_len, block, tau, seed, temperature, top_k, top_p, min_p):
+    """`generate` in these pages of the sequences."""
     ctx, s, P = model.ctx, model.shape, model.page_len
-    B = len(prompts)
+    B, n = len(prompts), [len(p) for p in prompts]
     i32 = lambda a: torch.tensor(np.asarray(a), dtype=torch.int32, device="cuda")
     gen = torch.Generator(device="cuda").manual_seed(seed)
-    n = [len(p) for p in prompts]
-    pages = [model.pages_for(k + gen_len) for k in n]
     width = max(len(p) for p in pages)
     table = i32([p + [-1] * (width - len(p)) for p in pages])
 
@@ -135,8 +146,6 @@ def generate(model, prompts, gen_len, block=32, tau=0.7, temperature=0.0, top_k=
             x = torch.where(take, token, x)
             done |= take
         out[:, b0:b0 + size] = x.view(B, size).cpu().numpy()
-    for p in pages:
-        model.release(p)
     ctx.synchronise()
     return out, steps
 
