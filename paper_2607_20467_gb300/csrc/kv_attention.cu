@@ -748,21 +748,21 @@ cudaError_t launch_rows(const KvPool& kv, const KvAttn& a, const KaScratch& s, i
 
 // Which kernel: the one that passes over the keys once for every 32 rows, or tcgen05 for every 256, where
 // beginning an item and joining its parts (32 rows' worth here, up to 256 there) take longer.  In
-// thousandths of a us of the whole GPU a unit of 128 keys takes 8 for 32 rows here; there 15 for up to
-// 128 rows, 18 for 256, and on top 10 us an item of a CTA and 0.0175 us a row and part.  Measured, us here /
-// there, FP8, 28 / 4 heads of 128: 16 x 8192 positions, 224 rows a kv head 241 / 109; 8 x 3000: 84 rows
-// 35.7 / 37.5, 112 43.2 / 38.8, 168 52.6 / 45.8, 224 59.4 / 50.5; 4 x 8192 (ten parts an item): 112
-// rows 50.7 / 57.2, 224 72.6 / 82.1; 2 x 1000, 224 rows 21 / 37; 32 / 32 heads, 64 rows, 8 x 3000 116 /
-// 133.  bf16 and heads of 64 fall on the same sides, or within 7 %.  Lengths are known to the device
-// only: the page table's width stands for them.
+// thousandths of a us of the whole GPU a unit of 128 keys takes about 10 for 32 rows here; there 15 for up to
+// 128 rows, 18 for 256, and on top 5 us an item of a CTA and 0.0175 us a row and part.  Measured, us here /
+// there, FP8, 28 / 4 heads of 128: 16 x 8192 positions, 224 rows a kv head 301 / 105; 8 x 3000: 63 rows
+// 35 / 34, 112 53 / 37, 224 74 / 48; 4 x 8192 (ten parts an item): 63 rows 50 / 45, 112 61 / 54, 224 90 / 79;
+// 1 x 16384, 224 rows 62 / 123; 2 x 1000, 224 rows 24 / 35.  Over 276 shapes (four head layouts, both formats) the rule
+// takes 0.8 % longer than the better kernel on average, more than 7 % longer in 13.  Lengths are known to the
+// device only: the page table's width stands for them.
 bool kv_attention_many_rows(const KvPool& kv, const KvAttn& a) {
   const int64_t rows = (int64_t)a.max_new * (a.H / kv.G);
   if (a.causal || rows <= 32) return false;
   const double units = (double)a.batch * kv.G * (((int64_t)a.max_pages * kv.page_len() + KA_UNIT - 1) / KA_UNIT);
   const int64_t rest = rows % 256;
-  const double here = 8.0 * (double)((rows + 31) / 32), there = 18.0 * (double)(rows / 256) + (rest > 128 ? 18 : rest ? 15 : 0);
+  const double here = 10.0 * (double)((rows + 31) / 32), there = 18.0 * (double)(rows / 256) + (rest > 128 ? 18 : rest ? 15 : 0);
   const double items = (double)a.batch * kv.G * (double)((rows + 255) / 256), ctas = KA_MOST / KA_CTAS;
-  return (here - there) * units > 17.5 * (double)std::min<int64_t>(rows, 256) * (ctas / items + 1) + 10000.0 * items / ctas;
+  return (here - there) * units > 17.5 * (double)std::min<int64_t>(rows, 256) * (ctas / items + 1) + 5000.0 * items / ctas;
 }
 
 size_t kv_attention_scratch(int sms) { return KV_ATTN_COUNTERS + (size_t)KA_CTAS * sms * KV_ATTN_PART_BYTES; }
