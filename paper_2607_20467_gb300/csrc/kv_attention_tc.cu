@@ -28,7 +28,7 @@
 // allocates TMEM and issues the MMAs.  17 warps leave 96 registers a thread: a row's warp holds 32 scores at
 // a time (the next 32 on their way as well spill: 137 us).  Two warps for a tile's 32 rows, half the
 // keys each, were no faster (115 us).  Every wait is bounded (DERR_WAIT_TIMEOUT).
-#include <cuda_fp8.h>
+#include <cuda_fp16.h>
 
 #include <algorithm>
 #include <type_traits>
@@ -92,27 +92,10 @@ __device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, u
       : "memory");
 }
 
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copy_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
-__device__ __forceinline__ uint4 lds128(uint32_t a) {
-  uint4 v;
-  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
-  return v;
-}
 // Two E4M3 codes times f (bf16 pairs), exactly: the code by way of fp16 and fp32, which hold it.
 __device__ __forceinline__ uint32_t widen(uint32_t w, int half, __nv_bfloat162 f) {
-  uint32_t r;
-  if (half)
-    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, h;\n\t}" : "=r"(r) : "r"(w));
-  else
-    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\t}" : "=r"(r) : "r"(w));
-  const float2 x = __half22float2(*reinterpret_cast<__half2*>(&r));
+  const uint32_t r = half ? widen_hi(w) : widen_lo(w);
+  const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&r));
   const __nv_bfloat162 y = __hmul2(__floats2bfloat162_rn(x.x, x.y), f);
   return *reinterpret_cast<const uint32_t*>(&y);
 }

@@ -1,4 +1,5 @@
-// How the kernels of kv_attention.cu and kv_attention_tc.cu share their work out.
+// How the kernels of kv_attention.cu and kv_attention_tc.cu share their work out, and what else they have
+// in common.
 //
 // An item is the rows of one row tile (new positions x the query heads of one kv head) of one
 // sequence; its keys come in units of 128.  All items of a launch stand in one line, each with
@@ -234,6 +235,31 @@ __device__ __forceinline__ float exp2_fast(float x) {
   return y;
 }
 
+// Copies of pages: 16 bytes a time, asynchronously.
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ uint4 lds128(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
+  return v;
+}
+// two E4M3 codes to two fp16
+__device__ __forceinline__ uint32_t widen_lo(uint32_t w) {
+  uint32_t r;
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\t}" : "=r"(r) : "r"(w));
+  return r;
+}
+__device__ __forceinline__ uint32_t widen_hi(uint32_t w) {
+  uint32_t r;
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, h;\n\t}" : "=r"(r) : "r"(w));
+  return r;
+}
 // Two bf16 parts of a weight p: its upper half (8 bits), and what that leaves of p (1 + 2^-17).  The factor, the
 // same for all weights and half of what the parts may be off by, keeps the second above zero where the
 // first is: an infinite value then gives the infinity, where a part of zero would make it no number.
