@@ -353,7 +353,8 @@ dcl_status dcl_kv_read(dcl_ctx* ctx, const dcl_kv_cache* cache, const int32_t* s
  *   out_dev     bf16 [n_q][n_heads][head_dim]; lse_dev float [n_q][n_heads] or NULL.  A row that
  *               sees nothing gets zeros and -inf.
  * Scores, softmax statistics and sums are held in fp32 and reproduce bit for bit; weights have 16 bits
- * or more.  An infinite value is the result of its component for the rows that see it (NaN with one
+ * or more (with FP8 pages and up to 32 rows a kv head: but for 2^-32 of a row's largest weight times
+ * value).  An infinite value is the result of its component for the rows that see it (NaN with one
  * of the other sign, or where the row's weight for it is zero in fp32).
  * A context's first call that has rows allocates its scratch (41 MB, for calls of every size) and is
  * refused with STATE while the stream is being captured; every later call may be captured.
@@ -377,7 +378,7 @@ dcl_status dcl_kv_attention(dcl_ctx* ctx, const dcl_kv_cache* cache, const void*
  * NaN) takes the largest logit.  Logits of -inf and NaN are never drawn; a row of nothing else gets token -1 and
  * zeros.  token_dev int32 [rows]; prob_dev float [rows] (may be NULL): the token's probability
  * among the kept ones; conf_dev float [rows] (may be NULL): its probability under softmax(z)
- * over all V, the confidence of Eq. threshold_pd.  V at most 2^19.
+ * over all V, the confidence of Eq. threshold_pd.  V at most 2^19, rows at most 2^24.
  * Errors: INVALID_ARG, UNSUPPORTED (V), CUDA. */
 dcl_status dcl_sample(dcl_ctx* ctx, const void* logits_dev, int64_t logits_stride, const float* noise_dev,
                       int64_t noise_stride, int32_t rows, int32_t V, const float* temperature_dev,

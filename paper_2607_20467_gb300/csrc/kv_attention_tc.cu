@@ -17,11 +17,11 @@
 // by more than 8; O is scaled then.  (P stays far below 1, so that no sum of large values overflows.)
 //
 // 16 sequences of 8192 positions, FP8, 28 / 4 heads of 128, 32 new positions each (224 rows a kv head;
-// 143 MB, 60 GFLOP): 108.5 us, 0.28 of the tensor rate.  Neither memory (0.18) nor the tensor pipe
+// 143 MB, 60 GFLOP): 109.5 us, 0.28 of the tensor rate.  Neither memory (0.19) nor the tensor pipe
 // (0.45 busy, P's second part included) bounds it but the chain S -> maximum -> weights -> O of a
-// tile, with two tiles in turn: of 6600 cycles a unit a row's warp takes 3300 for the weights, 650 for
-// the maximum, waits 1800 for S and has 900 for an item's q and results; leaving any one of them out
-// saves 5 us or less.  The CTAs' work spreads over 74 to 97 us, and the joins come after it.
+// tile, with two tiles in turn: of 6800 cycles a unit a row's warp takes 2200 to 3000 for the weights, 650
+// to 1200 for the maximum, waits 1900 to 2200 for S and has about 900 for an item's q and results.  The
+// CTAs' work ends after 88 to 102 us, and the joins come after it.
 //
 // Roles (544 threads): warps 0-3 and 4-7 have the rows of the two tiles; warps 8-11 copy and widen
 // keys, 12-15 values (one group for both was the slowest link: 7800 cycles a unit); warp 16
