@@ -10,8 +10,8 @@
 // sequence: 2 sequences of 131071 positions (271 MB) in 57.2 us, 4.7 TB/s over the whole launch, of
 // which beginning takes 2, joining 38 parts an item 7 to 9; 64 ragged sequences to 4096 (140 MB) in
 // 37 us, 3.8 TB/s: beginning 3.4, the keys 24 on average and 31 in the last CTA, joins 2; one of 512 positions,
-// 32 heads, 8.9 us, all latency (32 CTAs have an item: 1.9 to begin, 5.9 for its keys).  bf16 pages, 8 sequences of 1536, 32 heads, 32 rows each (201 MB):
-// 50 us, 4.1 TB/s, the products' issue (P in two parts) as near its limit as memory.
+// 32 heads, 8.9 us, all latency (32 CTAs have an item: 1.9 to begin, 5.9 for its keys).  bf16 pages, 8
+// sequences of 1536, 32 heads, 32 rows each (201 MB): 50 us, 4.1 TB/s, the products' issue (P in two parts) as near its limit as memory.
 //
 // Work is shared out in units of 128 keys of one (sequence, kv head, row tile), all of a launch in
 // one line, every CTA an equal part of it: a long sequence is spread over many CTAs, many short

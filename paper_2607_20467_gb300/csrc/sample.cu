@@ -19,7 +19,7 @@
 // Large calls are bound by memory: 512 rows of 152064 with noise for every token (467 MB) take
 // 92 us, 5.1 TB/s, 0.74 of the measured copy rate; the noise pass waits for the row's maximum, and
 // the CTAs of other rows (three to five an SM) fill that time.  Few rows are bound by latency: a row of 4095
-// tokens 10.5 us, 32 rows of 126464 with all three truncations 19.2, in steps of about 1 us (the
+// tokens 10.3 us, 32 rows of 126464 with all three truncations 18.1, in steps of about 1 us (the
 // maximum, the histogram, its scan, the boundaries, the draw, each with a barrier of the
 // cluster).  A row has up to eight CTAs (C doubles while V > 4096 C): what one CTA loads and counts is
 // what such a call waits for.
