@@ -305,6 +305,7 @@ dcl_status dcl_fp8_quantise(const uint16_t* w, int64_t rows, int64_t cols, uint8
 
 #define DCL_KV_BF16 0 /* keys and values in bf16 */
 #define DCL_KV_FP8 1  /* E4M3 codes and one exponent per (position, kv head) vector */
+#define DCL_KV_Q4 4   /* 4-bit codes and one scale byte per 32 components of a vector */
 /* Smallest exponent of a stored vector: components below 2^-74 are rounded to zero. */
 #define DCL_KV_EXP_MIN (-64)
 
@@ -313,7 +314,16 @@ dcl_status dcl_fp8_quantise(const uint16_t* w, int64_t rows, int64_t cols, uint8
  * [n_kv_heads][page_len].  A stored vector is code * 2^exp as in dcl_fp8_quantise (its format,
  * with the exponent at least DCL_KV_EXP_MIN), so that every stored value is a bf16 value (but for
  * components from 1.9375 * 2^127 on, whose nearest code stands for 2^128 and reads as infinity);
- * infinities and NaN are stored as NaN.  page_len 16, 32, 64, 128 or 256; head_dim 64 or 128;
+ * infinities and NaN are stored as NaN.
+ *   DCL_KV_Q4: codes uint8 [n_pages][n_kv_heads][page_len][head_dim / 2], scale bytes (in k_exp_dev,
+ * v_exp_dev) uint8 [n_pages][n_kv_heads][page_len][head_dim / 32].  Component c of a vector has the lower
+ * half of byte c / 2 where c is even, else the upper, and stands for (u - 8) s, u its 4 bits and s the
+ * scale of its group of 32.  Scale byte b stands for (4 + b % 4) 2^(b / 4 - 40), b < 252.  A group is
+ * stored with the least scale that has max abs a <= 7 s, and u = 8 + the whole number nearest to a / s
+ * (ties to even), from 1 to 15: a component is off by half its scale at most, and groups whose largest
+ * passes 7 * 7 * 2^22 = 2.05e8 are cut off there.  Every stored value is a bf16 value.  A group with an
+ * infinity or NaN in it has scale byte 255, which like 252 to 254 reads as NaN in all its components.
+ *   page_len 16, 32, 64, 128 or 256; head_dim 64 or 128;
  * n_kv_heads at most 1024; n_pages * page_len < 2^31; every pointer 16-byte aligned. */
 typedef struct {
   int32_t n_pages, page_len, n_kv_heads, head_dim, format;
@@ -321,7 +331,7 @@ typedef struct {
   int8_t *k_exp_dev, *v_exp_dev;
 } dcl_kv_cache;
 
-/* Store (and for DCL_KV_FP8 quantise) the keys and values of n positions: row i of k_dev / v_dev
+/* Store (and for DCL_KV_FP8 and DCL_KV_Q4 quantise) the keys and values of n positions: row i of k_dev / v_dev
  * (bf16 [n_kv_heads][head_dim], rows row_stride elements apart, so that they may stand in the
  * q | k | v rows of dcl_op_attention) goes to slot slot_dev[i] (int32; negative: the row is
  * skipped).  The slots of a call are distinct.  row_stride a multiple of 8, pointers 16-byte
@@ -363,6 +373,53 @@ dcl_status dcl_kv_attention(dcl_ctx* ctx, const dcl_kv_cache* cache, const void*
                             const int32_t* q_start_dev, const int32_t* page_table_dev, int32_t max_pages,
                             const int32_t* seq_len_dev, int32_t batch, int32_t n_q, int32_t max_new,
                             int32_t n_heads, int32_t causal, float scale, void* out_dev, float* lse_dev);
+
+/* Pages of many sequences in the caller's device memory, all int32: table_dev [batch][max_pages], of
+ * which the first held_dev[b] entries of row b are sequence b's pages, and a stack free_dev [n_pages] of
+ * the pages that no sequence has, n_free_dev[0] of them (its top is the last).  page_len as a cache's;
+ * n_pages * page_len < 2^31, max_pages * page_len at most 2^31 - 4096, batch * max_pages < 2^31. */
+typedef struct {
+  int32_t n_pages, page_len, batch, max_pages;
+  int32_t *table_dev, *held_dev, *free_dev, *n_free_dev;
+} dcl_kv_pages;
+
+/* Lay out a step: sequence b keeps the first start_dev[b] positions that it has cached and gets
+ * new_dev[b] new ones (int32 [batch] each; from none to many).
+ *   1. Pages past those that its start + new positions need go back onto the stack, in order of
+ *      sequence and place (entries -1 in the table).  A sequence that has ended has start and new 0.
+ *   2. In order, sequences get the pages they lack from the top of the stack, as long as those up to and
+ *      with a sequence are there; one whose pages are not gets none, keeps what it has and gets no rows
+ *      (q_start_dev tells), and so do those after it that lack any.
+ *   3. q_start_dev [batch + 1]: the rows of sequence b are [q_start[b], q_start[b + 1]); seq_len_dev
+ *      [batch]: start + new (start for one that got no rows): what dcl_kv_attention takes.  slot_dev,
+ *      pos_dev [n_rows]: the slot (for dcl_kv_write) and position (for dcl_qk_norm_rope) of every row,
+ *      -1 for rows past the last sequence's, so that a captured step may have room for more rows.
+ * A sequence whose numbers are negative or past its table, more rows than n_rows (those past it are
+ * left out), a page outside the pool (its rows get slot -1) and a stack that holds fewer than none or
+ * more than n_pages (no sequence gets rows, no page moves) are recorded as device-side faults.
+ * Errors: INVALID_ARG, CUDA. */
+dcl_status dcl_kv_plan(dcl_ctx* ctx, const dcl_kv_pages* pages, const int32_t* start_dev, const int32_t* new_dev,
+                       int32_t* q_start_dev, int32_t* seq_len_dev, int32_t* slot_dev, int32_t* pos_dev,
+                       int32_t n_rows);
+
+/* RMSNorm of every head of queries and keys, and the rotation by their positions, in one pass:
+ *   y = x / sqrt(mean(x^2) + eps) * gain over a head's components, then for i < rot_dim / 2
+ *   (y[i], y[i + rot_dim / 2]) -> (y[i] cos - y[i + rot_dim / 2] sin, y[i + rot_dim / 2] cos + y[i] sin)
+ * by the angle pos * theta^(-2 i / rot_dim); components from rot_dim on are not rotated.
+ *   q_dev, k_dev  bf16 rows of [n_heads][head_dim] and [n_kv_heads][head_dim], strides in elements
+ *                 (multiples of 8; they may stand in the q | k | v rows of one projection).
+ *   pos_dev       int32 [n]; the rows of a negative position are left out, their outputs untouched.
+ *   q_gain_dev, k_gain_dev  bf16 [head_dim], or NULL: not normed.  eps > 0 where either is given.
+ *   q_out_dev, k_out_dev    as q_dev, k_dev; either these themselves (in place, with the same strides)
+ *                 or apart from them.
+ * head_dim 64 or 128; rot_dim a multiple of 16 up to head_dim; theta at least 1; all pointers to bf16 16-byte
+ * aligned.  fp32 throughout, rounded once; angles are exact to 2^-21 at any position.
+ * Errors: INVALID_ARG, CUDA. */
+dcl_status dcl_qk_norm_rope(dcl_ctx* ctx, const void* q_dev, int64_t q_stride, const void* k_dev, int64_t k_stride,
+                            const int32_t* pos_dev, int32_t n, int32_t n_heads, int32_t n_kv_heads,
+                            int32_t head_dim, int32_t rot_dim, float theta, const void* q_gain_dev,
+                            const void* k_gain_dev, float eps, void* q_out_dev, int64_t q_out_stride,
+                            void* k_out_dev, int64_t k_out_stride);
 
 /* Draw one token per row of logits_dev (bf16 [rows][V], rows logits_stride elements apart).  With
  * y = (z - max z) / temperature and the tokens ordered by (z descending, index ascending), the

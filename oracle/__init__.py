@@ -16,10 +16,11 @@ Modules:
             Eq. draft_update for a block of positions)
   fp8     - the FP8 (E4M3) weight format with per-row power-of-two scales (a serving
             refinement outside the paper): the stored weights' values
+  q4      - the 4-bit format of the paged cache (groups of 32, a scale byte each)
 
 Every function is pinned by a ``-m "not gpu"`` test against something other than
 itself (closed forms, invariants, library routines, brute force); the model-level
 throughput and accuracy numbers of the paper need trained weights and are parity
 unpinned.
 """
-from . import model, decode, accept, fp8  # noqa: F401
+from . import model, decode, accept, fp8, q4  # noqa: F401

@@ -21,7 +21,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libdcleap.so")
 
 DCL_TILE_PAIR = 2
-DCL_KV_BF16, DCL_KV_FP8 = range(2)
+DCL_KV_BF16, DCL_KV_FP8, DCL_KV_Q4 = 0, 1, 4
 DCL_KV_EXP_MIN = -64
 DCL_OK, DCL_ERR_INVALID_ARG, DCL_ERR_STATE, DCL_ERR_OOM, DCL_ERR_CUDA, DCL_ERR_TIMEOUT, \
     DCL_ERR_UNSUPPORTED = range(7)
@@ -66,6 +66,12 @@ class KvCacheDesc(ctypes.Structure):
                 ("v_dev", ctypes.c_void_p), ("k_exp_dev", ctypes.c_void_p), ("v_exp_dev", ctypes.c_void_p)]
 
 
+class KvPagesDesc(ctypes.Structure):
+    _fields_ = [("n_pages", ctypes.c_int32), ("page_len", ctypes.c_int32), ("batch", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("table_dev", ctypes.c_void_p), ("held_dev", ctypes.c_void_p),
+                ("free_dev", ctypes.c_void_p), ("n_free_dev", ctypes.c_void_p)]
+
+
 _P = ctypes.c_void_p
 _I = ctypes.c_int32
 _L = ctypes.c_int64
@@ -92,6 +98,8 @@ SIGNATURES = {
     "dcl_kv_write": (_I, [_P, _P, _P, _P, _L, _P, _I]),
     "dcl_kv_read": (_I, [_P, _P, _P, _I, _P, _P, _L]),
     "dcl_kv_attention": (_I, [_P, _P, _P, _L, _P, _P, _I, _P, _I, _I, _I, _I, _I, _F, _P, _P]),
+    "dcl_kv_plan": (_I, [_P, _P, _P, _P, _P, _P, _P, _P, _I]),
+    "dcl_qk_norm_rope": (_I, [_P, _P, _L, _P, _L, _P, _I, _I, _I, _I, _I, _F, _P, _P, _F, _P, _L, _P, _L]),
     "dcl_sample": (_I, [_P, _P, _L, _P, _L, _I, _I, _P, _P, _P, _P, _P, _P, _P]),
     "dcl_synchronise": (_I, [_P]),
     "dcl_op_rmsnorm": (_I, [_P, _P, _P, _P, _I, _I, _F]),
@@ -176,7 +184,7 @@ def _dev(t, name, itemsize, count=0):
 # kind's size among them).  A type of another meaning is refused: its bits would be read as this one's.
 _KINDS = {"bf16": (2, ("torch.bfloat16", "torch.int16", "torch.uint16")), "f32": (4, ("torch.float32",)),
           "i32": (4, ("torch.int32", "torch.uint32")), "e4m3": (1, ("torch.float8_e4m3fn", "torch.uint8", "torch.int8")),
-          "i8": (1, ("torch.int8", "torch.uint8"))}
+          "i8": (1, ("torch.int8", "torch.uint8")), "u8": (1, ("torch.uint8", "torch.int8"))}
 _fits = {kind: set() for kind in _KINDS}  # types that have been looked at and taken
 
 
@@ -231,39 +239,76 @@ def _dev_rows(t, name, kind, rows, cols):
 class KvCache:
     """A paged key / value cache of one layer in the caller's tensors (dcl_kv_cache): k, v
     [pages][kv heads][page_len][head_dim], bf16, or 1-byte E4M3 codes with k_exp, v_exp int8
-    [pages][kv heads][page_len].  ``KvCache.empty`` allocates one."""
+    [pages][kv heads][page_len], or 4-bit codes uint8 [pages][kv heads][page_len][head_dim / 2] with
+    scale bytes k_exp, v_exp uint8 [pages][kv heads][page_len][head_dim / 32].  ``KvCache.empty``
+    allocates one."""
 
     def __init__(self, k, v, k_exp=None, v_exp=None):
         if len(k.shape) != 4:
             raise ValueError("k: [pages][kv heads][page_len][head_dim] expected")
         pages, heads, page_len, hd = k.shape
-        fp8 = k.element_size() == 1
-        if fp8 and (k_exp is None or v_exp is None):
-            raise ValueError("an FP8 cache needs k_exp and v_exp")
-        if not fp8 and (k_exp is not None or v_exp is not None):
+        small = k.element_size() == 1
+        if small and (k_exp is None or v_exp is None):
+            raise ValueError("an FP8 cache needs k_exp and v_exp, a 4-bit one its scales in their place")
+        if not small and (k_exp is not None or v_exp is not None):
             raise ValueError("a bf16 cache has no exponents")
-        n, kind = pages * heads * page_len, "e4m3" if fp8 else "bf16"
+        q4 = small and len(k_exp.shape) == 4
+        n, kind = pages * heads * page_len, "u8" if q4 else "e4m3" if small else "bf16"
         if tuple(v.shape) != tuple(k.shape):
             raise ValueError("k and v differ in shape")
+        codes, side = n * hd, n
+        if q4:
+            hd *= 2
+            side = n * (hd // 32)
+            for t, name in ((k_exp, "k_exp"), (v_exp, "v_exp")):
+                if tuple(t.shape) != (pages, heads, page_len, hd // 32):
+                    raise ValueError(f"{name}: [pages][kv heads][page_len][head_dim / 32] scales expected, got {tuple(t.shape)}")
         self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
         self.n_pages, self.n_kv_heads, self.page_len, self.head_dim = pages, heads, page_len, hd
-        self.format = DCL_KV_FP8 if fp8 else DCL_KV_BF16
-        self.desc = KvCacheDesc(pages, page_len, heads, hd, self.format, _dev_of(k, "k", kind, n * hd),
-                                _dev_of(v, "v", kind, n * hd), _dev_of(k_exp, "k_exp", "i8", n),
-                                _dev_of(v_exp, "v_exp", "i8", n))
+        self.format = DCL_KV_Q4 if q4 else DCL_KV_FP8 if small else DCL_KV_BF16
+        self.desc = KvCacheDesc(pages, page_len, heads, hd, self.format, _dev_of(k, "k", kind, codes),
+                                _dev_of(v, "v", kind, codes), _dev_of(k_exp, "k_exp", "u8" if q4 else "i8", side),
+                                _dev_of(v_exp, "v_exp", "u8" if q4 else "i8", side))
         self.ptr = ctypes.addressof(self.desc)
         self.row = heads * hd  # elements of a position's keys
 
     @classmethod
-    def empty(cls, n_pages, page_len, n_kv_heads, head_dim, fp8=True, device="cuda"):
-        """A cache in new, uninitialised memory (FP8 unless fp8 is False)."""
+    def empty(cls, n_pages, page_len, n_kv_heads, head_dim, fp8=True, device="cuda", q4=False):
+        """A cache in new, uninitialised memory (FP8 unless fp8 is False; 4 bits with q4)."""
         import torch
-        shape = (n_pages, n_kv_heads, page_len, head_dim)
+        shape = (n_pages, n_kv_heads, page_len)
         new = lambda s, t: torch.empty(s, dtype=t, device=device)
+        if q4:
+            return cls(*(new(shape + (head_dim // d,), torch.uint8) for d in (2, 2, 32, 32)))
+        shape += (head_dim,)
         if not fp8:
             return cls(new(shape, torch.bfloat16), new(shape, torch.bfloat16))
         return cls(new(shape, torch.uint8), new(shape, torch.uint8), new(shape[:3], torch.int8),
                    new(shape[:3], torch.int8))
+
+
+class KvPages:
+    """Pages of many sequences in the caller's int32 tensors (dcl_kv_pages): table [batch][max_pages],
+    held [batch], free [pages] (a stack, its top the last of n_free), n_free [1].  ``KvPages.new``
+    allocates them with every page free."""
+
+    def __init__(self, table, held, free, n_free, page_len):
+        if len(table.shape) != 2 or len(free.shape) != 1:
+            raise ValueError("table: [batch][max_pages], free: [pages] expected")
+        batch, width = table.shape
+        self.table, self.held, self.free, self.n_free, self.page_len = table, held, free, n_free, page_len
+        self.batch, self.max_pages, self.n_pages = batch, width, free.shape[0]
+        self.desc = KvPagesDesc(self.n_pages, page_len, batch, width, _dev_of(table, "table", "i32", batch * width),
+                                _dev_of(held, "held", "i32", batch), _dev_of(free, "free", "i32", self.n_pages),
+                                _dev_of(n_free, "n_free", "i32", 1))
+        self.ptr = ctypes.addressof(self.desc)
+
+    @classmethod
+    def new(cls, n_pages, page_len, batch, max_pages, device="cuda"):
+        import torch
+        i32 = lambda *s: torch.zeros(s, dtype=torch.int32, device=device)
+        return cls(i32(batch, max_pages) - 1, i32(batch), torch.arange(n_pages, dtype=torch.int32, device=device),
+                   i32(1) + n_pages, page_len)
 
 
 def weight_elements(shape, kind) -> int:
@@ -479,6 +524,33 @@ class Context:
             _dev_of(page_table, "page_table", "i32"), max_pages, _dev_of(seq_len, "seq_len", "i32", batch), batch, n_q,
             max_new, heads, int(bool(causal)), scale, _dev_of(out, "out", "bf16", n_q * heads * hd),
             _dev_of(lse, "lse", "f32", n_q * heads)))
+
+    def kv_plan(self, pages, start, new, q_start, seq_len, slots, pos):
+        """Lay out a step: sequence b keeps start[b] cached positions and gets new[b] rows (int32 [batch]).
+        Moves pages between the sequences and the stack; writes q_start [batch + 1], seq_len [batch], and
+        slots, pos [rows] (-1 past the last sequence's)."""
+        B, rows = pages.batch, slots.shape[0]
+        st = self._L.dcl_kv_plan(self.ptr, pages.ptr, _dev_of(start, "start", "i32", B), _dev_of(new, "new", "i32", B),
+                                 _dev_of(q_start, "q_start", "i32", B + 1), _dev_of(seq_len, "seq_len", "i32", B),
+                                 _dev_of(slots, "slots", "i32", rows), _dev_of(pos, "pos", "i32", rows), rows)
+        if st:
+            self._check(st)
+
+    def qk_norm_rope(self, q, k, pos, q_out, k_out, theta, q_gain=None, k_gain=None, eps=1e-6, rot_dim=None):
+        """Norm (where there is a gain, bf16 [head_dim]) and rotate by pos (int32 [n], negative: the row is left
+        out) every head of q [n][heads][head_dim] and k [n][kv heads][head_dim] (bf16, rows may be strided)
+        into q_out, k_out (as q, k, or these themselves)."""
+        n, H, hd = q.shape
+        G = k.shape[1]
+        qp, qs = _dev_rows(q, "q", "bf16", n, H * hd)
+        kp, ks = _dev_rows(k, "k", "bf16", n, G * hd)
+        qo, qos = (qp, qs) if q_out is q else _dev_rows(q_out, "q_out", "bf16", n, H * hd)
+        ko, kos = (kp, ks) if k_out is k else _dev_rows(k_out, "k_out", "bf16", n, G * hd)
+        st = self._L.dcl_qk_norm_rope(self.ptr, qp, qs, kp, ks, _dev_of(pos, "pos", "i32", n), n, H, G, hd,
+                                      hd if rot_dim is None else rot_dim, theta, _dev_of(q_gain, "q_gain", "bf16", hd),
+                                      _dev_of(k_gain, "k_gain", "bf16", hd), eps, qo, qos, ko, kos)
+        if st:
+            self._check(st)
 
     def sample(self, logits, token, noise=None, temperature=None, top_k=None, top_p=None, min_p=None, prob=None,
                conf=None):

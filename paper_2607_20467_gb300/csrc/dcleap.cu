@@ -1420,7 +1420,8 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 
 // The cache as the kernels see it; NULL, or why it is refused.
 const char* kv_pool(const dcl_kv_cache* kv, KvPool* out) {
   if (!kv || !kv->k_dev || !kv->v_dev) return "NULL cache";
-  if (kv->format != DCL_KV_BF16 && kv->format != DCL_KV_FP8) return "cache format must be DCL_KV_BF16 or DCL_KV_FP8";
+  if (kv->format != DCL_KV_BF16 && kv->format != DCL_KV_FP8 && kv->format != DCL_KV_Q4)
+    return "cache format must be DCL_KV_BF16, DCL_KV_FP8 or DCL_KV_Q4";
   int shift = 4;
   while (shift <= 8 && (1 << shift) != kv->page_len) ++shift;
   if (shift > 8) return "page_len must be 16, 32, 64, 128 or 256";
@@ -1428,10 +1429,11 @@ const char* kv_pool(const dcl_kv_cache* kv, KvPool* out) {
   if (kv->n_kv_heads <= 0 || kv->n_kv_heads > 1024 || kv->n_pages <= 0 || (int64_t)kv->n_pages * kv->page_len >= (1ll << 31))
     return "cache needs n_kv_heads in 1 .. 1024, n_pages > 0 and n_pages * page_len < 2^31";
   if (kv->format == DCL_KV_FP8 && (!kv->k_exp_dev || !kv->v_exp_dev)) return "an FP8 cache needs its exponents";
+  if (kv->format == DCL_KV_Q4 && (!kv->k_exp_dev || !kv->v_exp_dev)) return "a 4-bit cache needs its scales";
   if (!aligned16(kv->k_dev) || !aligned16(kv->v_dev) || !aligned16(kv->k_exp_dev) || !aligned16(kv->v_exp_dev))
     return "cache pointers must be 16-byte aligned";
   *out = KvPool{kv->k_dev, kv->v_dev, kv->k_exp_dev, kv->v_exp_dev, kv->n_pages, shift, kv->n_kv_heads,
-                kv->head_dim, kv->format == DCL_KV_FP8};
+                kv->head_dim, kv->format};
   return nullptr;
 }
 
@@ -1513,6 +1515,63 @@ dcl_status dcl_kv_attention(dcl_ctx* c, const dcl_kv_cache* cache, const void* q
   }
   CUDA_TRY(c, kv_attention_many_rows(kv, a) ? kv_attention_tc_launch(kv, a, c->kv_scratch, c->num_sms, c->derr, c->stream)
                                             : kv_attention_launch(kv, a, c->kv_scratch, c->num_sms, c->derr, c->stream));
+  return DCL_OK;
+}
+
+dcl_status dcl_kv_plan(dcl_ctx* c, const dcl_kv_pages* pages, const int32_t* start_dev, const int32_t* new_dev,
+                       int32_t* q_start_dev, int32_t* seq_len_dev, int32_t* slot_dev, int32_t* pos_dev, int32_t n_rows) {
+  if (!c) return DCL_ERR_INVALID_ARG;
+  if (!pages) return fail(c, DCL_ERR_INVALID_ARG, "kv_plan: NULL pages");
+  int shift = 4;
+  while (shift <= 8 && (1 << shift) != pages->page_len) ++shift;
+  if (shift > 8) return fail(c, DCL_ERR_INVALID_ARG, "kv_plan: page_len must be 16, 32, 64, 128 or 256");
+  if (pages->n_pages <= 0 || (int64_t)pages->n_pages * pages->page_len >= (1ll << 31))
+    return fail(c, DCL_ERR_INVALID_ARG, "kv_plan: n_pages must be > 0 and n_pages * page_len < 2^31");
+  if (pages->batch < 0 || n_rows < 0) return fail(c, DCL_ERR_INVALID_ARG, "kv_plan: batch and n_rows must be >= 0");
+  if (pages->max_pages <= 0 || (int64_t)pages->max_pages * pages->page_len > (1ll << 31) - 4096 ||
+      (int64_t)pages->batch * pages->max_pages >= (1ll << 31))
+    return fail(c, DCL_ERR_INVALID_ARG,
+                "kv_plan: max_pages must be > 0, max_pages * page_len at most 2^31 - 4096, batch * max_pages below 2^31");
+  if (!q_start_dev || (n_rows && (!slot_dev || !pos_dev)) ||
+      (pages->batch && (!pages->table_dev || !pages->held_dev || !pages->free_dev || !pages->n_free_dev || !start_dev || !new_dev || !seq_len_dev)))
+    return fail(c, DCL_ERR_INVALID_ARG, "kv_plan: NULL argument");
+  const KvPlan a{start_dev, new_dev, pages->table_dev, pages->held_dev, pages->free_dev, pages->n_free_dev, q_start_dev, seq_len_dev,
+                 slot_dev, pos_dev, pages->batch, pages->max_pages, shift, pages->n_pages, n_rows};
+  CUDA_TRY(c, kv_plan_launch(a, c->derr, c->stream));
+  return DCL_OK;
+}
+
+dcl_status dcl_qk_norm_rope(dcl_ctx* c, const void* q_dev, int64_t q_stride, const void* k_dev, int64_t k_stride,
+                            const int32_t* pos_dev, int32_t n, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                            int32_t rot_dim, float theta, const void* q_gain_dev, const void* k_gain_dev, float eps,
+                            void* q_out_dev, int64_t q_out_stride, void* k_out_dev, int64_t k_out_stride) {
+  if (!c) return DCL_ERR_INVALID_ARG;
+  if (head_dim != 64 && head_dim != 128) return fail(c, DCL_ERR_INVALID_ARG, "qk_norm_rope: head_dim must be 64 or 128");
+  if (rot_dim < 0 || rot_dim > head_dim || rot_dim % 16)
+    return fail(c, DCL_ERR_INVALID_ARG, "qk_norm_rope: rot_dim must be a multiple of 16 up to head_dim");
+  if (n < 0 || n_heads <= 0 || n_kv_heads <= 0 || (int64_t)n_heads + n_kv_heads > (1 << 20))
+    return fail(c, DCL_ERR_INVALID_ARG, "qk_norm_rope: n must be >= 0, n_heads and n_kv_heads > 0 and 2^20 together at most");
+  if (!(theta >= 1.f) || theta > 3e38f) return fail(c, DCL_ERR_INVALID_ARG, "qk_norm_rope: theta must be at least 1");
+  if ((q_gain_dev || k_gain_dev) && (!(eps > 0.f) || eps > 3e38f))
+    return fail(c, DCL_ERR_INVALID_ARG, "qk_norm_rope: eps must be > 0");
+  if (n == 0) return DCL_OK;
+  if (!q_dev || !k_dev || !pos_dev || !q_out_dev || !k_out_dev) return fail(c, DCL_ERR_INVALID_ARG, "qk_norm_rope: NULL argument");
+  const int64_t q_row = (int64_t)n_heads * head_dim, k_row = (int64_t)n_kv_heads * head_dim;
+  if (q_stride < q_row || q_out_stride < q_row || k_stride < k_row || k_out_stride < k_row ||
+      (q_stride | k_stride | q_out_stride | k_out_stride) % 8)
+    return fail(c, DCL_ERR_INVALID_ARG, "qk_norm_rope: strides must be multiples of 8 and hold a row");
+  if (!aligned16(q_dev) || !aligned16(k_dev) || !aligned16(q_out_dev) || !aligned16(k_out_dev) || !aligned16(q_gain_dev) ||
+      !aligned16(k_gain_dev))
+    return fail(c, DCL_ERR_INVALID_ARG, "qk_norm_rope: pointers must be 16-byte aligned");
+  if ((q_out_dev == q_dev && q_out_stride != q_stride) || (k_out_dev == k_dev && k_out_stride != k_stride))
+    return fail(c, DCL_ERR_INVALID_ARG, "qk_norm_rope: in place, a stride must be its own");
+  using bf = __nv_bfloat16;
+  QkRope a{static_cast<const bf*>(q_dev), static_cast<const bf*>(k_dev), static_cast<bf*>(q_out_dev), static_cast<bf*>(k_out_dev),
+           q_stride, k_stride, q_out_stride, k_out_stride, static_cast<const bf*>(q_gain_dev), static_cast<const bf*>(k_gain_dev),
+           pos_dev, n, n_heads, n_kv_heads, head_dim, rot_dim, eps, {}};
+  for (int i = 0; i < rot_dim / 2; ++i)
+    a.turns[i] = (uint64_t)ldexp(pow((double)theta, -2.0 * i / rot_dim) / 6.283185307179586476925, 64);
+  CUDA_TRY(c, qk_rope_launch(a, c->num_sms, c->stream));
   return DCL_OK;
 }
 

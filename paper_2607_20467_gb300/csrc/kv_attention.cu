@@ -41,6 +41,7 @@
 #include "common.cuh"
 #include "kv_cache.cuh"
 #include "kv_share.cuh"
+#include "q4.cuh"
 
 namespace dcl {
 namespace {
@@ -51,25 +52,28 @@ constexpr int KA_MOST = 304;  // most CTAs of a launch
 static_assert(KA_MOST * sizeof(int) <= KV_ATTN_COUNTERS, "a counter per CTA");
 
 // RS: rows of an item that a lane has (quad + 8 i), 8 rows of the item each.
-template <int HD, bool FP8, int RS>
+template <int HD, KvFormat F, int RS>
 struct KaCfg {
-  static constexpr int ES = FP8 ? 1 : 2;
+  static constexpr bool FP8 = F == KV_FP8, Q4 = F == KV_Q4, WIDEN = F != KV_BF16;
   static constexpr int MT = RS == 1 ? 1 : RS / 2;   // tiles of 16 rows (or of 8 and the second parts of their weights)
   static constexpr int WARPS = MT == 1 ? 6 : 4;     // (with KA_CTAS of them on an SM as many as the registers allow)
   static constexpr int THREADS = 32 * WARPS;
-  static constexpr int KT = FP8 && MT == 1 ? 32 : 16;  // keys that a warp takes at a time
+  static constexpr int KT = WIDEN && MT == 1 ? 32 : 16;  // keys that a warp takes at a time
   static constexpr int NK = KT / 8;                 // column tiles of S
   static constexpr int ROWS = 8 * RS;               // rows of an item
-  static constexpr int ROWB = HD * ES;              // bytes of a key
+  static constexpr int ROWB = Q4 ? HD / 2 : FP8 ? HD : 2 * HD;  // bytes of a key
   static constexpr int TILE = KT * ROWB;            // the keys (or values) of a step
-  static constexpr int STAGE = 2 * TILE + (FP8 ? 2 * KT : 0);
+  static constexpr int SIDE = Q4 ? HD / Q4_GROUP : FP8 ? 1 : 0;  // bytes of a key's scales or exponent
+  static constexpr int STAGE = 2 * TILE + 2 * KT * SIDE;
   static constexpr int LIMIT = 220 * 1024 / KA_CTAS / WARPS / STAGE;
   static constexpr int STAGES = LIMIT > 12 ? 12 : LIMIT;
   static constexpr int RING = STAGES * STAGE;       // one warp's
   // a warp's O takes the ring's place: [ROWS][O_PITCH] floats, a lane's runs of components 4 apart
   // from the next lane's, so that 16-byte stores meet all the banks
-  static constexpr int O_PITCH = FP8 ? HD + 36 : HD + HD / 2 + 4;
-  static constexpr int RING_B = RING > ROWS * O_PITCH * 4 ? RING : ROWS * O_PITCH * 4;
+  static constexpr int O_PITCH = WIDEN ? HD + 36 : HD + HD / 2 + 4;
+  static constexpr int O_B = ROWS * O_PITCH * 4;
+  static constexpr int JOIN_B = (ROWS * KA_MOST * 8 + WARPS - 1) / WARPS + 127 & ~127;  // (a join's weights: 4 bits, few components)
+  static constexpr int RING_B = RING > O_B ? (Q4 && JOIN_B > RING ? JOIN_B : RING) : Q4 && JOIN_B > O_B ? JOIN_B : O_B;
   static constexpr int ML = WARPS * RING_B;         // {m, l} [warp][ROWS]
   static constexpr int WT = ML + WARPS * ROWS * 8;  // weights of the warps' parts [ROWS][8], then {m, l} of the rows
   static constexpr int QF = WT + ROWS * (8 * 4 + 8);  // q fragments [MT][HD / 16][lane] of 16 bytes
@@ -97,6 +101,12 @@ __device__ __forceinline__ uint32_t lds_u8(uint32_t a) {
   asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(a));
   return v;
 }
+__device__ __forceinline__ uint32_t lds32(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ void sts8(uint32_t a, uint32_t v) { asm volatile("st.shared.u8 [%0], %1;" ::"r"(a), "r"(v) : "memory"); }
 __device__ __forceinline__ float2 lds_f2(uint32_t a) {
   float2 v;
   asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(a) : "memory");
@@ -130,17 +140,29 @@ template <int ROWB>
 __device__ __forceinline__ uint32_t chunk_at(int r, int c) {
   return (uint32_t)(r * ROWB + ((c ^ (ROWB == 64 ? (r >> 1) & 3 : r & 7)) << 4));
 }
+// The same of a tile of 4-bit codes.  Rows change places too, as a value's operand takes 8 (HD = 128) or 4
+// bytes of every other row: a half-warp's 8-byte loads, or a warp's 4-byte ones, then meet all the banks,
+// and a key's (16 or 8 bytes of neighbouring rows) as well.
+template <int ROWB>
+__device__ __forceinline__ uint32_t chunk4_at(int r, int c) {
+  if (ROWB == 64) {
+    const int x = r & 1 ? 4 + ((r >> 1 & 3) ^ 1) : r >> 1 & 3;
+    return (uint32_t)(((r & ~7) + x) * 64 + ((c ^ (x & 2)) << 4));
+  }
+  const int x = r & 1 ? 8 + ((r >> 1 & 7) ^ 2) : r >> 1 & 7;
+  return (uint32_t)(((r & ~15) + x) * 32 + (c << 4));
+}
 // The order in which hd enters the two products is free as long as q and k, and v and the output,
 // agree: a lane's operands are taken from whole 16-byte chunks.  k_chunk: the i-th chunk of 8
 // components of q that lane place t covers.  v_comp: the component of column n of product tile j.
-template <int HD, bool FP8>
+template <int HD, KvFormat F>
 __device__ __forceinline__ int k_chunk(int t, int i) {
-  if (FP8) return t * (HD / 32) + i;
+  if (F != KV_BF16) return t * (HD / 32) + i;
   return 2 * t + (i & 1) + 8 * (i >> 1);
 }
-template <int HD, bool FP8>
+template <int HD, KvFormat F>
 __device__ __forceinline__ int v_comp(int n, int j) {
-  if (FP8) return n * (HD / 8) + j;
+  if (F != KV_BF16) return n * (HD / 8) + j;
   return (j >> 3) * 64 + 8 * n + (j & 7);
 }
 
@@ -185,6 +207,18 @@ __device__ __noinline__ bool lower_zeros(uint32_t tile, uint32_t ev, int lane) {
   }
   return __any_sync(0xffffffffu, zero);
 }
+// 4-bit codes: groups that hold no numbers, by the scales' bytes of a step (N of them).
+template <int N>
+__device__ __noinline__ bool has_no_numbers(uint32_t scales, int lane) {
+  bool any = false;
+  for (int c = lane; c < N; c += 32) any |= lds_u8(scales + c) >= Q4_SCALES;
+  return any;
+}
+template <int N>
+__device__ __noinline__ void clear_no_numbers(uint32_t scales, int lane) {
+  for (int c = lane; c < N; c += 32)
+    if (lds_u8(scales + c) >= Q4_SCALES) sts8(scales + c, 0);
+}
 template <int ROWB, bool FP8>
 __device__ __forceinline__ float value_at(uint32_t tile, int row, int comp) {
   const int byte = comp * (FP8 ? 1 : 2);
@@ -195,15 +229,16 @@ __device__ __forceinline__ float value_at(uint32_t tile, int row, int comp) {
 }
 
 // Where component c of a row of O stands in a warp's part of shared memory.
-template <int HD, bool FP8>
+template <int HD, KvFormat F>
 __device__ __forceinline__ int o_place(int c) {
-  if (FP8) return c + 4 * (c / (HD / 8));
+  if (F != KV_BF16) return c + 4 * (c / (HD / 8));
   return (c >> 6) * 96 + ((c >> 3) & 7) * 12 + (c & 7);
 }
-template <int HD, bool FP8, int RS>
-__global__ void __launch_bounds__(KaCfg<HD, FP8, RS>::THREADS, KA_CTAS) kv_attention_kernel(KvPool kv, KvAttn a, KaScratch scratch, int* err) {
-  using C = KaCfg<HD, FP8, RS>;
-  constexpr int MT = C::MT;
+template <int HD, KvFormat F, int RS>
+__global__ void __launch_bounds__(KaCfg<HD, F, RS>::THREADS, KA_CTAS) kv_attention_kernel(KvPool kv, KvAttn a, KaScratch scratch, int* err) {
+  using C = KaCfg<HD, F, RS>;
+  constexpr int MT = C::MT, SIDE = C::SIDE;
+  constexpr bool FP8 = C::FP8, Q4 = C::Q4;
   constexpr bool OWN_LO = RS > 1;  // the weights' second parts are products of their own
   constexpr float ABOVE = FP8 ? -7.f : 32.f, SLACK = 8.f;  // the reference above the largest score, and how far that may be passed
   constexpr int KS = HD / 16;  // k steps of S, and pairs of column tiles of O
@@ -250,12 +285,13 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, RS>::THREADS, KA_CTAS) kv_atten
 #pragma unroll
       for (int c = 0; c < HD / 32; ++c) {
         raw[i][c] = make_uint4(0, 0, 0, 0);
-        if (live) raw[i][c] = *reinterpret_cast<const uint4*>(src + 8 * k_chunk<HD, FP8>(place, c));
+        if (live) raw[i][c] = *reinterpret_cast<const uint4*>(src + 8 * k_chunk<HD, F>(place, c));
       }
     }
 
     // ---- this warp's steps: keys key0 + KT warp on, then every WARPS-th
     const int stop = min(key1, lim_max);
+    auto tile_at = [](int r, int c) { return Q4 ? chunk4_at<C::ROWB>(r, c) : chunk_at<C::ROWB>(r, c); };
     const int* table = a.table + (int64_t)it.b * a.max_pages;
     int next = key0 + KT * warp;  // first key of the next step to copy
     uint32_t bad = 0;             // two bits a stage: 16 keys whose page is not the cache's
@@ -281,11 +317,14 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, RS>::THREADS, KA_CTAS) kv_atten
 #pragma unroll
             for (int i = 0; i < C::ROWB / 32; ++i) {
               const int c = i * 32 + lane;
-              const uint32_t at = chunk_at<C::ROWB>(16 * h + c / (C::ROWB / 16), c % (C::ROWB / 16));
+              const uint32_t at = tile_at(16 * h + c / (C::ROWB / 16), c % (C::ROWB / 16));
               copy16(dst + at, k + 512 * i);
               copy16(dst + C::TILE + at, v + 512 * i);
             }
-            if (FP8 && lane < 2) copy16(dst + 2 * C::TILE + KT * lane + 16 * h, (lane ? kv.v_exp : kv.k_exp) + vec);
+            if (SIDE && lane < 2 * SIDE) {  // exponents or scales, 16 bytes a lane
+              const int of = lane / (SIDE ? SIDE : 1), c = 16 * (lane - of * SIDE);
+              copy16(dst + 2 * C::TILE + SIDE * (KT * of + 16 * h) + c, (of ? kv.v_exp : kv.k_exp) + vec * SIDE + c);
+            }
           } else {
             bad |= 1u << (2 * slot + h);
             if (lane == 0) report_error(err, DERR_KV_RANGE);
@@ -336,8 +375,14 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, RS>::THREADS, KA_CTAS) kv_atten
           for (int s = 0; s < KS; ++s) {  // step s: components 4 s .. 4 s + 3 of this lane's
             const uint32_t* w0 = &raw[2 * mt][s >> 1].x + 2 * (s & 1);
             const uint32_t* w1 = &raw[RS > 1 ? 2 * mt + 1 : 0][s >> 1].x + 2 * (s & 1);
-            *reinterpret_cast<uint4*>(qs[mt * KS + s][lane]) =
-                RS > 1 ? make_uint4(w0[0], w1[0], w0[1], w1[1]) : make_uint4(w0[0], 0, w0[1], 0);
+            uint4 x = RS > 1 ? make_uint4(w0[0], w1[0], w0[1], w1[1]) : make_uint4(w0[0], 0, w0[1], 0);
+            if (Q4) {  // (of 8 components: 0 and 4, 1 and 5 of them, then 2 and 6, 3 and 7: as codes are widened)
+              const uint32_t *y0 = &raw[2 * mt][s >> 1].x + (s & 1), *y1 = &raw[RS > 1 ? 2 * mt + 1 : 0][s >> 1].x + (s & 1);
+              x = make_uint4(__byte_perm(y0[0], y0[2], 0x5410), __byte_perm(y1[0], y1[2], 0x5410),
+                             __byte_perm(y0[0], y0[2], 0x7632), __byte_perm(y1[0], y1[2], 0x7632));
+              if (RS == 1) x.y = x.w = 0;
+            }
+            *reinterpret_cast<uint4*>(qs[mt * KS + s][lane]) = x;
           }
         }
       }
@@ -370,10 +415,14 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, RS>::THREADS, KA_CTAS) kv_atten
       {
         const bool masked = key + KT > lim_min || skip;
         if (key + KT > lim_max || skip) {  // values that no row sees may be anything: 0 * NaN
-          for (int c = lane; c < C::TILE / 16; c += 32) {
+          for (int c = lane; !Q4 && c < C::TILE / 16; c += 32) {
             const int r = c / (C::ROWB / 16);
             if (key + r >= lim_max || (skip >> (r >> 4) & 1))
               sts128(sv + chunk_at<C::ROWB>(r, c % (C::ROWB / 16)), make_uint4(0, 0, 0, 0));
+          }
+          for (int c = lane; Q4 && c < KT * SIDE; c += 32) {  // (any codes are numbers)
+            const int r = c / (SIDE ? SIDE : 1);
+            if (key + r >= lim_max || (skip >> (r >> 4) & 1)) sts8(se + KT * SIDE + c, 0);
           }
         }
         if (FP8) {  // what a key's exponents give: 2^e of the key, e of the value
@@ -392,14 +441,27 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, RS>::THREADS, KA_CTAS) kv_atten
           for (int j = 0; j < NK; ++j)
 #pragma unroll
             for (int k = 0; k < 4; ++k) s[i][j][k] = 0.f;
-        constexpr int KCH = FP8 ? HD / 64 : HD / 32;  // 16-byte chunks of a key per lane
-        constexpr int SPC = FP8 ? 4 : 2;              // k steps of a chunk
+        constexpr int KCH = Q4 ? 1 : FP8 ? HD / 64 : HD / 32;    // 16-byte chunks of a key per lane
+        constexpr int SPC = Q4 ? HD / 16 : FP8 ? 4 : 2;          // k steps of a chunk
 #pragma unroll
         for (int c = 0; c < KCH; ++c) {
           uint4 w[NK];
+          Q4Scale ks[Q4 ? NK : 1];
 #pragma unroll
-          for (int j = 0; j < NK; ++j)
-            w[j] = lds128(sk + chunk_at<C::ROWB>(8 * j + quad, FP8 ? place * KCH + c : k_chunk<HD, FP8>(place, c)));
+          for (int j = 0; j < NK; ++j) {
+            if (Q4) {  // a lane has 32 components (one group) or 16
+              if (HD == 128) {
+                w[j] = lds128(sk + chunk4_at<C::ROWB>(8 * j + quad, place));
+              } else {
+                const uint2 two = lds64(sk + chunk4_at<C::ROWB>(8 * j + quad, place >> 1) + 8 * (place & 1));
+                w[j].x = two.x;
+                w[j].y = two.y;
+              }
+              ks[j] = q4_scale_twice(lds_u8(se + (8 * j + quad) * SIDE + place / (4 / (SIDE ? SIDE : 4))));
+              continue;
+            }
+            w[j] = lds128(sk + chunk_at<C::ROWB>(8 * j + quad, FP8 ? place * KCH + c : k_chunk<HD, F>(place, c)));
+          }
 #pragma unroll
           for (int x = 0; x < SPC; ++x) {
             const int st = c * SPC + x;
@@ -415,8 +477,8 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, RS>::THREADS, KA_CTAS) kv_atten
 #pragma unroll
             for (int j = 0; j < NK; ++j) {
               const uint32_t* ww = &w[j].x;
-              const uint32_t b0 = FP8 ? widen_lo(ww[x]) : ww[2 * (x & 1)];
-              const uint32_t b1 = FP8 ? widen_hi(ww[x]) : ww[2 * (x & 1) + 1];
+              const uint32_t b0 = Q4 ? q4_widen(ww[x >> 1], 2 * (x & 1), ks[j]) : FP8 ? widen_lo(ww[x]) : ww[2 * (x & 1)];
+              const uint32_t b1 = Q4 ? q4_widen(ww[x >> 1], 2 * (x & 1) + 1, ks[j]) : FP8 ? widen_hi(ww[x]) : ww[2 * (x & 1) + 1];
 #pragma unroll
               for (int i = 0; i < MT; ++i) mma16816<FP8>(s[i][j], qreg[i], b0, b1);
             }
@@ -517,7 +579,8 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, RS>::THREADS, KA_CTAS) kv_atten
         }
         // A value that is no number and that only some of the rows see (0 * NaN): it is added to the
         // rows that do, one by one, and out of the product.
-        if (masked && a.causal && __any_sync(0xffffffffu, has_nonfinite<FP8>(sv, C::TILE, lane))) {
+        if (masked && a.causal &&
+            __any_sync(0xffffffffu, Q4 ? has_no_numbers<KT * SIDE>(se + KT * SIDE, lane) : has_nonfinite<FP8>(sv, C::TILE, lane))) {
 #pragma unroll
           for (int half = 0; half < NK / 2; ++half)
 #pragma unroll 1
@@ -533,19 +596,55 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, RS>::THREADS, KA_CTAS) kv_atten
                 for (int j = 0; j < NT; ++j)
 #pragma unroll
                   for (int k = 0; k < 2; ++k) {
-                    const float v = value_at<C::ROWB, FP8>(sv, 16 * half + jj, v_comp<HD, FP8>(2 * place + k, j));
+                    const int row = 16 * half + jj, comp = v_comp<HD, F>(2 * place + k, j);
+                    float v;
+                    if (Q4) v = lds_u8(se + (KT + row) * SIDE + comp / Q4_GROUP) >= Q4_SCALES ? NAN : 0.f;
+                    else v = value_at<C::ROWB, FP8>(sv, row, comp);
                     if (!isfinite(v)) o[i >> 1][j][2 * (i & 1) + k] += pj * v;
                   }
               }
             }
           __syncwarp();
-          clear_nonfinite<FP8>(sv, C::TILE, lane);
+          if (Q4) clear_no_numbers<KT * SIDE>(se + KT * SIDE, lane);
+          else clear_nonfinite<FP8>(sv, C::TILE, lane);
           __syncwarp();
         }
         // O += P v, 16 keys at a time
 #pragma unroll
         for (int half = 0; half < NK / 2; ++half) {
-          if (FP8) {
+          if (Q4) {
+            constexpr int W = HD / 64;  // 8-code words of a value per lane, all of one group
+            uint32_t v[4][W], scale[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {  // keys 2 place, 2 place + 1, and 8 on
+              const int row = 16 * half + 2 * place + (r & 1) + 8 * (r >> 1);
+              if (W == 2) {
+                const uint2 x = lds64(sv + chunk4_at<C::ROWB>(row, quad >> 1) + 8 * (quad & 1));
+                v[r][0] = x.x;
+                v[r][W - 1] = x.y;
+              } else {
+                v[r][0] = lds32(sv + chunk4_at<C::ROWB>(row, quad >> 2) + 4 * (quad & 3));
+              }
+              scale[r] = lds_u8(se + (KT + row) * SIDE + quad / (8 / (SIDE ? SIDE : 8)));
+            }
+            const Q4Scale f0 = q4_scale(scale[0] | scale[1] << 16), f1 = q4_scale(scale[2] | scale[3] << 16);
+#pragma unroll
+            for (int w = 0; w < W; ++w)
+#pragma unroll
+              for (int up = 0; up < 2; ++up) {  // a word's lower four components, its upper four; two keys side by side
+                const uint32_t x0 = __byte_perm(v[0][w], v[1][w], up ? 0x7632 : 0x5410);
+                const uint32_t x1 = __byte_perm(v[2][w], v[3][w], up ? 0x7632 : 0x5410);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                  const uint32_t b0 = q4_widen(x0, j, f0), b1 = q4_widen(x1, j, f1);
+#pragma unroll
+                  for (int i = 0; i < MT; ++i) {
+                    mma16816<FP8>(o[i][8 * w + 4 * up + j], p[half][i], b0, b1);
+                    if (OWN_LO) mma16816<FP8>(o[i][8 * w + 4 * up + j], p_lo[OWN_LO ? half : 0][i], b0, b1);
+                  }
+                }
+              }
+          } else if (FP8) {
             constexpr int W = HD / 32;  // 4-code words of a value per lane
             uint32_t v[4][W];
 #pragma unroll
@@ -630,7 +729,7 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, RS>::THREADS, KA_CTAS) kv_atten
 #pragma unroll
           for (int k = 0; k < (RS > 1 ? 4 : 2); ++k)
             *reinterpret_cast<float4*>(mine + (16 * i + quad + 8 * (k >> 1)) * C::O_PITCH +
-                                       o_place<HD, FP8>(v_comp<HD, FP8>(2 * place + (k & 1), j))) =
+                                       o_place<HD, F>(v_comp<HD, F>(2 * place + (k & 1), j))) =
                 make_float4(o[i][j][k], o[i][j + 1][k], o[i][j + 2][k], o[i][j + 3][k]);
     }
     __syncthreads();
@@ -664,7 +763,7 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, RS>::THREADS, KA_CTAS) kv_atten
 #pragma unroll 4
     for (int t = threadIdx.x; t < it.rows * Q; t += C::THREADS) {
       const int r = t / Q, c = 4 * (t % Q);
-      const float* o_row = reinterpret_cast<const float*>(smem) + r * C::O_PITCH + o_place<HD, FP8>(c);
+      const float* o_row = reinterpret_cast<const float*>(smem) + r * C::O_PITCH + o_place<HD, F>(c);
       float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int w = 0; w < C::WARPS; ++w)
@@ -699,12 +798,12 @@ __global__ void __launch_bounds__(KaCfg<HD, FP8, RS>::THREADS, KA_CTAS) kv_atten
   }
 }
 
-template <int HD, bool FP8, int RS>
+template <int HD, KvFormat F, int RS>
 cudaError_t launch_as(const KvPool& kv, const KvAttn& a, const KaScratch& s, int ctas, int* err, cudaStream_t stream) {
-  using C = KaCfg<HD, FP8, RS>;
+  using C = KaCfg<HD, F, RS>;
   static_assert(KA_CTAS * (C::SMEM + 1024) <= 233472, "shared memory of an SM");
   static_assert(2 * C::ROWS * (HD + 4) * 4 <= KV_ATTN_PART_BYTES, "scratch per CTA");
-  auto kern = kv_attention_kernel<HD, FP8, RS>;
+  auto kern = kv_attention_kernel<HD, F, RS>;
   static const cudaError_t set =
       cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM);
   if (set != cudaSuccess) return set;
@@ -712,12 +811,12 @@ cudaError_t launch_as(const KvPool& kv, const KvAttn& a, const KaScratch& s, int
   return cudaGetLastError();
 }
 
-template <int HD, bool FP8>
+template <int HD, KvFormat F>
 cudaError_t launch_rows(const KvPool& kv, const KvAttn& a, const KaScratch& s, int ctas, int* err, cudaStream_t stream) {
   const int64_t rows = (int64_t)a.max_new * (a.H / kv.G);
-  if (rows <= 8) return launch_as<HD, FP8, 1>(kv, a, s, ctas, err, stream);
-  if (rows <= 16) return launch_as<HD, FP8, 2>(kv, a, s, ctas, err, stream);
-  return launch_as<HD, FP8, 4>(kv, a, s, ctas, err, stream);
+  if (rows <= 8) return launch_as<HD, F, 1>(kv, a, s, ctas, err, stream);
+  if (rows <= 16) return launch_as<HD, F, 2>(kv, a, s, ctas, err, stream);
+  return launch_as<HD, F, 4>(kv, a, s, ctas, err, stream);
 }
 
 }  // namespace
@@ -733,7 +832,7 @@ cudaError_t launch_rows(const KvPool& kv, const KvAttn& a, const KaScratch& s, i
 // device only: the page table's width stands for them.
 bool kv_attention_many_rows(const KvPool& kv, const KvAttn& a) {
   const int64_t rows = (int64_t)a.max_new * (a.H / kv.G);
-  if (a.causal || rows <= 32) return false;
+  if (a.causal || rows <= 32 || kv.format == KV_Q4) return false;
   const double units = (double)a.batch * kv.G * (((int64_t)a.max_pages * kv.page_len() + KA_UNIT - 1) / KA_UNIT);
   const int64_t rest = rows % 256;
   const double here = 10.0 * (double)((rows + 31) / 32), there = 18.0 * (double)(rows / 256) + (rest > 128 ? 18 : rest ? 15 : 0);
@@ -746,8 +845,13 @@ size_t kv_attention_scratch(int sms) { return KV_ATTN_COUNTERS + (size_t)KA_CTAS
 cudaError_t kv_attention_launch(const KvPool& kv, const KvAttn& a, void* scratch, int sms, int* err, cudaStream_t stream) {
   sms = std::min(sms, KA_MOST / KA_CTAS);
   KaScratch s{reinterpret_cast<float*>(static_cast<uint8_t*>(scratch) + KV_ATTN_COUNTERS), static_cast<int*>(scratch)};
-  if (kv.hd == 128) return kv.fp8 ? launch_rows<128, true>(kv, a, s, KA_CTAS * sms, err, stream) : launch_rows<128, false>(kv, a, s, KA_CTAS * sms, err, stream);
-  return kv.fp8 ? launch_rows<64, true>(kv, a, s, KA_CTAS * sms, err, stream) : launch_rows<64, false>(kv, a, s, KA_CTAS * sms, err, stream);
+  auto rows = [&](auto hd) {
+    constexpr int HD = decltype(hd)::value;
+    if (kv.format == KV_Q4) return launch_rows<HD, KV_Q4>(kv, a, s, KA_CTAS * sms, err, stream);
+    if (kv.format == KV_FP8) return launch_rows<HD, KV_FP8>(kv, a, s, KA_CTAS * sms, err, stream);
+    return launch_rows<HD, KV_BF16>(kv, a, s, KA_CTAS * sms, err, stream);
+  };
+  return kv.hd == 128 ? rows(std::integral_constant<int, 128>{}) : rows(std::integral_constant<int, 64>{});
 }
 
 }  // namespace dcl

@@ -570,8 +570,9 @@ size_t kv_attention_tc_scratch(int sms) { return KV_ATTN_COUNTERS + (size_t)std:
 cudaError_t kv_attention_tc_launch(const KvPool& kv, const KvAttn& a, void* scratch, int sms, int* err, cudaStream_t stream) {
   sms = std::min(sms, 152);
   KaScratch s{reinterpret_cast<float*>(static_cast<uint8_t*>(scratch) + KV_ATTN_COUNTERS), static_cast<int*>(scratch)};
-  if (kv.hd == 128) return kv.fp8 ? launch_as<128, true>(kv, a, s, sms, err, stream) : launch_as<128, false>(kv, a, s, sms, err, stream);
-  return kv.fp8 ? launch_as<64, true>(kv, a, s, sms, err, stream) : launch_as<64, false>(kv, a, s, sms, err, stream);
+  const bool fp8 = kv.format == KV_FP8;
+  if (kv.hd == 128) return fp8 ? launch_as<128, true>(kv, a, s, sms, err, stream) : launch_as<128, false>(kv, a, s, sms, err, stream);
+  return fp8 ? launch_as<64, true>(kv, a, s, sms, err, stream) : launch_as<64, false>(kv, a, s, sms, err, stream);
 }
 
 }  // namespace dcl

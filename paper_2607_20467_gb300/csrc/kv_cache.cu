@@ -14,8 +14,11 @@
 // writes).  32 positions: 2 to 3 us of kernel in a call of 5.1.
 #include <cuda_fp8.h>
 
+#include <type_traits>
+
 #include "common.cuh"
 #include "kv_cache.cuh"
+#include "q4.cuh"
 
 namespace dcl {
 namespace {
@@ -101,7 +104,49 @@ __device__ __forceinline__ uint4 quantise(KvBf16& a, int& e) {
   return make_uint4(out[0], out[1], out[2], out[3]);
 }
 
-template <int HD, bool FP8>
+// 1 / d for d = 4 .. 7 in two parts: the first has 16 bits, so that a bf16 value times it is exact, and
+// value / d comes out of one fused multiply-add with its one rounding.  (A quotient of 8 bits by 3 that
+// is not halfway between whole numbers is far from there; one that is stays exactly there.)
+struct Q4Over {
+  float hi, lo;
+  __device__ explicit Q4Over(int d) {
+    const float r = __fdividef(1.f, (float)d);
+    hi = __uint_as_float(__float_as_uint(r) & 0xffffff00u);
+    lo = fmaf(-hi, (float)d, 1.f) * r;
+  }
+};
+
+// Codes (16 of 4 bits) and the scale byte of a part's group, which two neighbouring threads share; all
+// threads of a warp call it.
+__device__ __forceinline__ uint2 quantise_q4(KvBf16& a, uint32_t& scale) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = __vmaxu2(m, a.word(i) & 0x7fff7fffu);
+  m = max(m & 0xffffu, m >> 16);
+  m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+  // The largest is f 2^x, f = 128 .. 255.  7 (4 + i) 2^k, the largest a scale reaches, passes 128 2^x,
+  // 140 2^x, ... in turn: 35, 42, 49 at k = x + 2, then 28 and 35 at x + 3.  Bytes count through them.
+  const int x = (int)(m >> 7) - 134, f = (int)(m & 0x7fu) + 128;
+  const int b = min(Q4_SCALES - 1, max(0, 4 * (x + 42) + 1 + (f > 140) + (f > 168) + (f > 196) + (f > 224)));
+  scale = m >= 0x7f80u ? Q4_NONE : (uint32_t)b;
+  const Q4Over over(4 + (b & 3));
+  const float down = __int_as_float((127 + 40 - (b >> 2)) << 23);
+  uint32_t out[2] = {0, 0};
+  if (m >= 0x7f80u) return make_uint2(0x88888888u, 0x88888888u);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t w = a.word(i);
+    // (a value above 7 times the largest scale: 7 of them; 8 added, and rounded, by 1.5 2^23)
+    auto code = [&](float v) {
+      const float y = fminf(7.f, fmaxf(-7.f, fmaf(v, over.lo, v * over.hi)));
+      return (__float_as_uint(y + 12582920.f)) & 15u;
+    };
+    out[i >> 2] |= (code(bf16_lo(w) * down) | code(bf16_hi(w) * down) << 4) << (8 * (i & 3));
+  }
+  return make_uint2(out[0], out[1]);
+}
+
+template <int HD, KvFormat F>
 __global__ void __launch_bounds__(KV_THREADS) kv_write_kernel(KvPool kv, const __nv_bfloat16* __restrict__ k,
                                                               const __nv_bfloat16* __restrict__ v, int64_t stride,
                                                               const int* __restrict__ slots, int n, uint32_t inverse,
@@ -127,15 +172,32 @@ __global__ void __launch_bounds__(KV_THREADS) kv_write_kernel(KvPool kv, const _
     const KvPart p = walk.at(i);
     int e = 0;
     uint4 codes;
-    if (FP8) codes = quantise<HD>(raw[i], e);
+    uint2 codes4;
+    uint32_t scales;
+    if (F == KV_FP8) codes = quantise<HD>(raw[i], e);
+    if (F == KV_Q4) {
+      codes4 = quantise_q4(raw[i], scales);
+      scales <<= 8 * (p.part >> 1);  // the vector's bytes side by side
+      scales |= __shfl_xor_sync(0xffffffffu, scales, 2);
+      if (HD == 128) scales |= __shfl_xor_sync(0xffffffffu, scales, 4);
+    }
     if (slot[i] < 0) continue;
     if (slot[i] >= kv.n_slots()) {
       report_error(err, DERR_KV_RANGE);
       continue;
     }
     const int64_t vec = kv.vector_of(slot[i], p.g);
-    uint4* to = reinterpret_cast<uint4*>(p.is_v ? kv.v : kv.k) + (vec * TPV + p.part) * (FP8 ? 1 : 2);
-    if (!FP8) {
+    if (F == KV_Q4) {
+      (reinterpret_cast<uint2*>(p.is_v ? kv.v : kv.k))[vec * TPV + p.part] = codes4;
+      if (p.part == 0) {
+        int8_t* to = (p.is_v ? kv.v_exp : kv.k_exp) + vec * (HD / Q4_GROUP);
+        if (HD == 128) *reinterpret_cast<uint32_t*>(to) = scales;
+        else *reinterpret_cast<uint16_t*>(to) = (uint16_t)scales;
+      }
+      continue;
+    }
+    uint4* to = reinterpret_cast<uint4*>(p.is_v ? kv.v : kv.k) + (vec * TPV + p.part) * (F == KV_FP8 ? 1 : 2);
+    if (F == KV_BF16) {
       to[0] = raw[i].x[0];
       to[1] = raw[i].x[1];
     } else {
@@ -145,7 +207,7 @@ __global__ void __launch_bounds__(KV_THREADS) kv_write_kernel(KvPool kv, const _
   }
 }
 
-template <int HD, bool FP8>
+template <int HD, KvFormat F>
 __global__ void __launch_bounds__(KV_THREADS) kv_read_kernel(KvPool kv, const int* __restrict__ slots, int n,
                                                              __nv_bfloat16* __restrict__ k, __nv_bfloat16* __restrict__ v,
                                                              int64_t stride, uint32_t inverse, int* err) {
@@ -168,16 +230,35 @@ __global__ void __launch_bounds__(KV_THREADS) kv_read_kernel(KvPool kv, const in
     raw[i].x[0] = raw[i].x[1] = make_uint4(0, 0, 0, 0);
     e[i] = 0;
     if (vec[i] < 0) continue;
-    const uint4* from = reinterpret_cast<const uint4*>(p.is_v ? kv.v : kv.k) + (vec[i] * TPV + p.part) * (FP8 ? 1 : 2);
+    if (F == KV_Q4) {
+      const uint2 codes = (reinterpret_cast<const uint2*>(p.is_v ? kv.v : kv.k))[vec[i] * TPV + p.part];
+      raw[i].x[0].x = codes.x;
+      raw[i].x[0].y = codes.y;
+      e[i] = (uint8_t)(p.is_v ? kv.v_exp : kv.k_exp)[vec[i] * (HD / Q4_GROUP) + (p.part >> 1)];
+      continue;
+    }
+    const uint4* from = reinterpret_cast<const uint4*>(p.is_v ? kv.v : kv.k) + (vec[i] * TPV + p.part) * (F == KV_FP8 ? 1 : 2);
     raw[i].x[0] = from[0];
-    if (!FP8) raw[i].x[1] = from[1];
-    if (FP8) e[i] = (p.is_v ? kv.v_exp : kv.k_exp)[vec[i]];
+    if (F == KV_BF16) raw[i].x[1] = from[1];
+    if (F == KV_FP8) e[i] = (p.is_v ? kv.v_exp : kv.k_exp)[vec[i]];
   }
 #pragma unroll
   for (int i = 0; i < KV_EACH; ++i) {
     const KvPart p = walk.at(i);
     if (p.row >= n) continue;
-    if (FP8) {
+    if (F == KV_Q4 && vec[i] >= 0) {
+      const Q4Scale f = q4_scale_twice((uint32_t)e[i]);
+      const uint32_t codes[2] = {raw[i].x[0].x, raw[i].x[0].y};
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        uint32_t y[4];  // components 0 and 4, 1 and 5, ...
+#pragma unroll
+        for (int z = 0; z < 4; ++z) y[z] = q4_widen(codes[j], z, f);
+        raw[i].x[j] = make_uint4(__byte_perm(y[0], y[1], 0x5410), __byte_perm(y[2], y[3], 0x5410),
+                                 __byte_perm(y[0], y[1], 0x7632), __byte_perm(y[2], y[3], 0x7632));
+      }
+    }
+    if (F == KV_FP8) {
       const float scale = kv_pow2(e[i]);
       const uint4 codes = raw[i].x[0];
       const uint32_t c[4] = {codes.x, codes.y, codes.z, codes.w};
@@ -205,6 +286,19 @@ bool kv_grid(const KvPool& kv, int n, unsigned* grid, uint32_t* inverse) {
   return true;
 }
 
+// The launch of a cache's head size and format.
+template <typename Launch>
+cudaError_t for_layout(const KvPool& kv, Launch launch) {
+  auto as = [&](auto hd) {
+    if (kv.format == KV_Q4) launch(hd, std::integral_constant<KvFormat, KV_Q4>{});
+    else if (kv.format == KV_FP8) launch(hd, std::integral_constant<KvFormat, KV_FP8>{});
+    else launch(hd, std::integral_constant<KvFormat, KV_BF16>{});
+  };
+  if (kv.hd == 128) as(std::integral_constant<int, 128>{});
+  else as(std::integral_constant<int, 64>{});
+  return cudaGetLastError();
+}
+
 }  // namespace
 
 cudaError_t kv_write_launch(const KvPool& kv, const __nv_bfloat16* k, const __nv_bfloat16* v, int64_t stride,
@@ -212,11 +306,9 @@ cudaError_t kv_write_launch(const KvPool& kv, const __nv_bfloat16* k, const __nv
   unsigned grid;
   uint32_t inv;
   if (!kv_grid(kv, n, &grid, &inv)) return cudaErrorInvalidValue;
-  if (kv.hd == 128 && kv.fp8) kv_write_kernel<128, true><<<grid, KV_THREADS, 0, stream>>>(kv, k, v, stride, slots, n, inv, err);
-  else if (kv.hd == 128) kv_write_kernel<128, false><<<grid, KV_THREADS, 0, stream>>>(kv, k, v, stride, slots, n, inv, err);
-  else if (kv.fp8) kv_write_kernel<64, true><<<grid, KV_THREADS, 0, stream>>>(kv, k, v, stride, slots, n, inv, err);
-  else kv_write_kernel<64, false><<<grid, KV_THREADS, 0, stream>>>(kv, k, v, stride, slots, n, inv, err);
-  return cudaGetLastError();
+  return for_layout(kv, [&](auto hd, auto format) {
+    kv_write_kernel<decltype(hd)::value, decltype(format)::value><<<grid, KV_THREADS, 0, stream>>>(kv, k, v, stride, slots, n, inv, err);
+  });
 }
 
 cudaError_t kv_read_launch(const KvPool& kv, const int* slots, int n, __nv_bfloat16* k, __nv_bfloat16* v, int64_t stride,
@@ -224,11 +316,9 @@ cudaError_t kv_read_launch(const KvPool& kv, const int* slots, int n, __nv_bfloa
   unsigned grid;
   uint32_t inv;
   if (!kv_grid(kv, n, &grid, &inv)) return cudaErrorInvalidValue;
-  if (kv.hd == 128 && kv.fp8) kv_read_kernel<128, true><<<grid, KV_THREADS, 0, stream>>>(kv, slots, n, k, v, stride, inv, err);
-  else if (kv.hd == 128) kv_read_kernel<128, false><<<grid, KV_THREADS, 0, stream>>>(kv, slots, n, k, v, stride, inv, err);
-  else if (kv.fp8) kv_read_kernel<64, true><<<grid, KV_THREADS, 0, stream>>>(kv, slots, n, k, v, stride, inv, err);
-  else kv_read_kernel<64, false><<<grid, KV_THREADS, 0, stream>>>(kv, slots, n, k, v, stride, inv, err);
-  return cudaGetLastError();
+  return for_layout(kv, [&](auto hd, auto format) {
+    kv_read_kernel<decltype(hd)::value, decltype(format)::value><<<grid, KV_THREADS, 0, stream>>>(kv, slots, n, k, v, stride, inv, err);
+  });
 }
 
 }  // namespace dcl

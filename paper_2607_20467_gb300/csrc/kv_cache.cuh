@@ -1,5 +1,4 @@
-// The paged key / value cache as the kernels see it, and their launches (kv_cache.cu,
-// kv_attention.cu).
+// The paged key / value cache and what stands around it as the kernels see them, and their launches.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -9,10 +8,13 @@ namespace dcl {
 
 constexpr int KV_EXP_MIN = -64;  // smallest exponent of a stored vector (DCL_KV_EXP_MIN)
 
+// How a pool holds its vectors (DCL_KV_*).
+enum KvFormat : int { KV_BF16 = 0, KV_FP8 = 1, KV_Q4 = 4 };
+
 struct KvPool {
-  void *k, *v;             // [pages][G][page_len][hd] bf16 or E4M3 codes
-  int8_t *k_exp, *v_exp;   // [pages][G][page_len], FP8 only
-  int pages, page_shift, G, hd, fp8;
+  void *k, *v;             // [pages][G][page_len][hd] bf16 or E4M3 codes, or [hd / 2] bytes of 4-bit codes
+  int8_t *k_exp, *v_exp;   // [pages][G][page_len] exponents (FP8), or [hd / 32] scale bytes each (Q4)
+  int pages, page_shift, G, hd, format;
   __host__ __device__ int page_len() const { return 1 << page_shift; }
   __host__ __device__ int n_slots() const { return pages << page_shift; }
   // index of the vector of slot (page * page_len + position) and kv head g
@@ -51,6 +53,30 @@ size_t kv_attention_scratch(int sms);
 size_t kv_attention_tc_scratch(int sms);
 cudaError_t kv_attention_launch(const KvPool& kv, const KvAttn& a, void* scratch, int sms, int* err, cudaStream_t stream);
 cudaError_t kv_attention_tc_launch(const KvPool& kv, const KvAttn& a, void* scratch, int sms, int* err, cudaStream_t stream);
+
+// The plan of a step (kv_plan.cu).
+struct KvPlan {
+  const int *start, *rows_new;  // [batch]: positions that stay, and new ones
+  int *table, *held;            // [batch][max_pages], [batch]: pages of each sequence
+  int *free, *n_free;           // [n_pages], [1]: a stack of the others
+  int *q_start, *seq_len;       // [batch + 1], [batch]
+  int *slot, *pos;              // [n_rows]
+  int batch, max_pages, page_shift, n_pages, n_rows;
+};
+cudaError_t kv_plan_launch(const KvPlan& a, int* err, cudaStream_t stream);
+
+// Norm and rotation of queries and keys (qk_rope.cu).
+struct QkRope {
+  const __nv_bfloat16 *q, *k;          // [n][H][hd], [n][G][hd]; strides in elements
+  __nv_bfloat16 *q_out, *k_out;
+  int64_t q_stride, k_stride, q_out_stride, k_out_stride;
+  const __nv_bfloat16 *q_gain, *k_gain;  // [hd], or NULL: no norm
+  const int* pos;                      // [n]; negative: the row is left out
+  int n, H, G, hd, rot;
+  float eps;
+  uint64_t turns[64];                  // of component i < rot / 2: its frequency, turns a position * 2^64
+};
+cudaError_t qk_rope_launch(const QkRope& a, int sms, cudaStream_t stream);
 
 // Drawing tokens (sample.cu).
 struct SampleArgs {
