@@ -122,6 +122,9 @@ struct dcl_ctx {
   // scratch of the single-kernel entry points, kept from call to call up to OP_SCRATCH_KEEP
   void* op_buf = nullptr;
   size_t op_cap = 0;
+  float rope_theta = 0.f;      // what rope_turns are for (qk_norm_rope): a position's turns * 2^64
+  int rope_rot = 0;
+  uint64_t rope_turns[64] = {};
   void* kv_scratch = nullptr;  // kv_attention's counters and parts, from the first call on
   cudaEvent_t ev_done[2] = {nullptr, nullptr};
 };
@@ -1537,7 +1540,7 @@ dcl_status dcl_kv_plan(dcl_ctx* c, const dcl_kv_pages* pages, const int32_t* sta
     return fail(c, DCL_ERR_INVALID_ARG, "kv_plan: NULL argument");
   const KvPlan a{start_dev, new_dev, pages->table_dev, pages->held_dev, pages->free_dev, pages->n_free_dev, q_start_dev, seq_len_dev,
                  slot_dev, pos_dev, pages->batch, pages->max_pages, shift, pages->n_pages, n_rows};
-  CUDA_TRY(c, kv_plan_launch(a, c->derr, c->stream));
+  CUDA_TRY(c, kv_plan_launch(a, c->num_sms, c->derr, c->stream));
   return DCL_OK;
 }
 
@@ -1569,8 +1572,13 @@ dcl_status dcl_qk_norm_rope(dcl_ctx* c, const void* q_dev, int64_t q_stride, con
   QkRope a{static_cast<const bf*>(q_dev), static_cast<const bf*>(k_dev), static_cast<bf*>(q_out_dev), static_cast<bf*>(k_out_dev),
            q_stride, k_stride, q_out_stride, k_out_stride, static_cast<const bf*>(q_gain_dev), static_cast<const bf*>(k_gain_dev),
            pos_dev, n, n_heads, n_kv_heads, head_dim, rot_dim, eps, {}};
-  for (int i = 0; i < rot_dim / 2; ++i)
-    a.turns[i] = (uint64_t)ldexp(pow((double)theta, -2.0 * i / rot_dim) / 6.283185307179586476925, 64);
+  if (c->rope_theta != theta || c->rope_rot != rot_dim) {  // (64 powers take longer than the rest of the call)
+    for (int i = 0; i < rot_dim / 2; ++i)
+      c->rope_turns[i] = (uint64_t)ldexp(pow((double)theta, -2.0 * i / rot_dim) / 6.283185307179586476925, 64);
+    c->rope_theta = theta;
+    c->rope_rot = rot_dim;
+  }
+  memcpy(a.turns, c->rope_turns, sizeof(a.turns));
   CUDA_TRY(c, qk_rope_launch(a, c->num_sms, c->stream));
   return DCL_OK;
 }

@@ -63,7 +63,7 @@ struct KvPlan {
   int *slot, *pos;              // [n_rows]
   int batch, max_pages, page_shift, n_pages, n_rows;
 };
-cudaError_t kv_plan_launch(const KvPlan& a, int* err, cudaStream_t stream);
+cudaError_t kv_plan_launch(const KvPlan& a, int sms, int* err, cudaStream_t stream);
 
 // Norm and rotation of queries and keys (qk_rope.cu).
 struct QkRope {

@@ -6,16 +6,19 @@
 //   q_start_b = new_0 + .. + new_(b - 1)                   of the sequences that got theirs
 //   slot = table[b][pos / page_len] * page_len + pos % page_len,  pos = start_b + row - q_start_b
 //
-// One CTA: prefix sums over the sequences, in pieces of as many as it has threads, a warp for a
-// sequence's pages, a thread for a row (its sequence by bisection in q_start).
+// A few numbers a sequence, a slot and a position a row: a call is bound by the chain of its steps.  Prefix
+// sums over the sequences in pieces of a CTA's threads; a warp for a sequence's pages; a thread for a few
+// rows (their sequence by bisection in q_start).  Steps of many rows or sequences: a cluster of 8 CTAs for the
+// pages, each of which has the sums for itself, and a second kernel for the rows.
 #include "common.cuh"
 #include "kv_cache.cuh"
 
 namespace dcl {
 namespace {
 
-constexpr int KP_THREADS = 512;
-constexpr int KP_WARPS = KP_THREADS / 32;
+constexpr int KP_CLUSTER = 8;
+constexpr int KP_STARTS = 2048;  // sequences whose starts are kept in shared memory
+constexpr int KP_ROW_THREADS = 256;
 
 // A sequence's numbers; one that is not within its table gets no rows and keeps what it has.
 struct KpSeq {
@@ -41,125 +44,223 @@ __device__ __forceinline__ KpSeq kp_seq(const KvPlan& a, int b) {
   return s;
 }
 
-// Inclusive prefix sum over the block's threads; total: of all of them.
-__device__ __forceinline__ int64_t kp_scan(int64_t x, int64_t* sums, int64_t& total) {
+// Inclusive prefix sum over the block's threads, and the sum of all.  Calls in turn take sums of their own.
+template <int T>
+__device__ __forceinline__ int64_t kp_scan(int64_t x, int64_t (&sums)[T / 32], int64_t& total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
     const int64_t y = __shfl_up_sync(0xffffffffu, x, d);
     if (lane >= d) x += y;
   }
-  __syncthreads();  // (the last scan's sums are read)
   if (lane == 31) sums[warp] = x;
   __syncthreads();
-  int64_t before = 0;
-  total = 0;
+  int64_t upto = lane < T / 32 ? sums[lane] : 0;
 #pragma unroll
-  for (int w = 0; w < KP_WARPS; ++w) {
-    const int64_t y = sums[w];
-    if (w < warp) before += y;
-    total += y;
+  for (int d = 1; d < 32; d <<= 1) {
+    const int64_t y = __shfl_up_sync(0xffffffffu, upto, d);
+    if (lane >= d) upto += y;
   }
-  return x + before;
+  total = __shfl_sync(0xffffffffu, upto, 31);
+  const int64_t before = __shfl_sync(0xffffffffu, upto, max(warp - 1, 0));
+  return warp ? x + before : x;
 }
 
-__global__ void __launch_bounds__(KP_THREADS) kv_plan_kernel(KvPlan a, int* err) {
-  __shared__ int64_t sums[KP_WARPS];
-  __shared__ int64_t off[KP_THREADS];            // where a sequence's pages go to, or come from
-  __shared__ int first[KP_THREADS], count[KP_THREADS];  // its first page to give or take, and how many
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, P = 1 << a.page_shift;
+// Slots and positions of rows first .. first + 3 and every step after; starts: q_start in shared memory, or NULL.
+__device__ __forceinline__ void kp_rows(const KvPlan& a, const int* starts, int64_t first, int64_t step, int* err) {
+  const int P = 1 << a.page_shift;
+  const bool wide = ((reinterpret_cast<uintptr_t>(a.slot) | reinterpret_cast<uintptr_t>(a.pos)) & 15) == 0;
+  auto start_of = [&](int b) { return starts ? starts[b] : __ldcg(a.q_start + b); };
+  const int live = start_of(a.batch);
+  for (; first < a.n_rows; first += step) {
+    const int r0 = (int)first;
+    int slot[4] = {-1, -1, -1, -1}, pos[4] = {-1, -1, -1, -1};
+    if (r0 < live) {
+      int lo = 0, hi = a.batch - 1;  // the first sequence that ends past r0
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (start_of(mid + 1) > r0) hi = mid;
+        else lo = mid + 1;
+      }
+      int q0 = start_of(lo), q1 = start_of(lo + 1), at = a.start[lo], have = -1, base = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = r0 + i;
+        if (r >= live) break;
+        if (r >= q1) {
+          do {
+            q0 = q1;
+            q1 = start_of(++lo + 1);
+          } while (r >= q1);
+          at = a.start[lo];
+          have = -1;
+        }
+        pos[i] = at + r - q0;
+        if (have != pos[i] >> a.page_shift) {
+          have = pos[i] >> a.page_shift;
+          base = __ldcg(a.table + (int64_t)lo * a.max_pages + have);
+          if (base < 0 || base >= a.n_pages) {
+            report_error(err, DERR_KV_RANGE);
+            base = -1;
+          }
+        }
+        slot[i] = base < 0 ? -1 : (base << a.page_shift) + (pos[i] & (P - 1));
+      }
+    }
+    if (wide && first + 4 <= a.n_rows) {
+      *reinterpret_cast<int4*>(a.slot + r0) = make_int4(slot[0], slot[1], slot[2], slot[3]);
+      *reinterpret_cast<int4*>(a.pos + r0) = make_int4(pos[0], pos[1], pos[2], pos[3]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (first + i < a.n_rows) {
+          a.slot[r0 + i] = slot[i];
+          a.pos[r0 + i] = pos[i];
+        }
+    }
+  }
+}
+
+template <int T, int CTAS, bool ROWS_TOO>
+__global__ void __launch_bounds__(T) kv_plan_kernel(KvPlan a, int* err) {
+  __shared__ int64_t sums[2][T / 32];
+  __shared__ int64_t off[T];             // where a sequence's pages go to, or come from
+  __shared__ int first[T], count[T];     // its first page to give or take, and how many
+  __shared__ int starts[KP_STARTS + 1];
+  __shared__ int most;                   // pages taken
+  const int tid = threadIdx.x, lane = tid & 31;
+  const int rank = CTAS > 1 ? (int)blockIdx.x : 0, warp = rank * (T / 32) + (tid >> 5);  // (one cluster is the grid)
+  auto meet = [] {  // what was written before is there for all CTAs
+    if (CTAS > 1) {
+      __syncwarp();
+      asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+      asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    } else {
+      __syncthreads();
+    }
+  };
+  if (!ROWS_TOO) pdl_launch_dependents();
+  const bool one = a.batch <= T, kept = ROWS_TOO && a.batch <= KP_STARTS;
   const int there = a.batch ? *a.n_free : 0;  // (no sequences: nothing but rows of none)
-  int64_t returned = 0, total;
-  for (int b0 = 0; b0 < a.batch; b0 += KP_THREADS) {
-    const KpSeq s = kp_seq(a, b0 + threadIdx.x);
-    if (s.bad) report_error(err, DERR_KV_RANGE);
-    kp_scan(s.back(), sums, total);
-    returned += total;
+  const KpSeq mine = kp_seq(a, tid);
+  auto seq = [&](int b0) { return one ? mine : kp_seq(a, b0 + tid); };
+  auto both = [](const KpSeq& s) { return (int64_t)s.back() << 32 | s.lack(); };  // (sums of either are below 2^31)
+  if (tid == 0) most = 0;
+
+  // ---- pages that come back; of at most T sequences all sums at once
+  int64_t total, sum = 0;
+  int64_t returned = 0;
+  for (int b0 = 0, i = 0; b0 < a.batch; b0 += T, i ^= 1) {
+    const KpSeq s = seq(b0);
+    if (s.bad && rank == 0) report_error(err, DERR_KV_RANGE);
+    sum = kp_scan<T>(both(s), sums[i], total);
+    returned += total >> 32;
   }
   // (a stack that is not one: nothing is planned)
   const bool broken = there < 0 || there + returned > a.n_pages;
-  if (broken && threadIdx.x == 0) report_error(err, DERR_KV_RANGE);
+  if (broken && tid == 0 && rank == 0) report_error(err, DERR_KV_RANGE);
   const int64_t pages = there + returned;
 
-  // ---- pages go back
-  int64_t carry = 0;
-  for (int b0 = 0; !broken && returned && b0 < a.batch; b0 += KP_THREADS) {
-    const KpSeq s = kp_seq(a, b0 + threadIdx.x);
-    const int64_t upto = carry + kp_scan(s.back(), sums, total);
-    off[threadIdx.x] = there + upto - s.back();
-    first[threadIdx.x] = s.need;
-    count[threadIdx.x] = s.back();
-    __syncthreads();
-    for (int i = warp; i < KP_THREADS && b0 + i < a.batch; i += KP_WARPS) {
-      int* row = a.table + (int64_t)(b0 + i) * a.max_pages + first[i];
-      for (int j = lane; j < count[i]; j += 32) {
-        a.free[off[i] + j] = row[j];
-        row[j] = -1;
+  if (!broken && returned) {
+    int64_t carry = 0;
+    for (int b0 = 0; b0 < a.batch; b0 += T) {
+      const KpSeq s = seq(b0);
+      __syncthreads();
+      if (!one) sum = kp_scan<T>(both(s), sums[0], total);
+      off[tid] = there + carry + (sum >> 32) - s.back();
+      first[tid] = s.need;
+      count[tid] = s.back();
+      __syncthreads();
+      for (int i = warp; i < T && b0 + i < a.batch; i += CTAS * (T / 32)) {
+        int* row = a.table + (int64_t)(b0 + i) * a.max_pages + first[i];
+        for (int j = lane; j < count[i]; j += 32) {
+          a.free[off[i] + j] = row[j];
+          row[j] = -1;
+        }
       }
+      carry += total >> 32;
     }
-    carry += total;
+    meet();
   }
-  __syncthreads();
 
   // ---- pages that are lacking, and the rows' starts
-  int64_t lacked = 0, rows = 0, taken = 0;
-  for (int b0 = 0; b0 < a.batch; b0 += KP_THREADS) {
-    const int b = b0 + threadIdx.x;
-    const KpSeq s = kp_seq(a, b);
-    const int64_t upto = lacked + kp_scan(s.lack(), sums, total);
-    lacked += total;
+  int64_t lacked = 0, rows = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += T) {
+    const int b = b0 + tid;
+    const KpSeq s = seq(b0);
+    if (!one) {
+      __syncthreads();
+      sum = kp_scan<T>(both(s), sums[0], total);
+    }
+    const int64_t upto = lacked + (sum & 0xffffffff);
+    lacked += total & 0xffffffff;
     const bool ok = !broken && !s.bad && (s.lack() == 0 || upto <= pages);
-    const int64_t end = rows + kp_scan(ok ? s.rows : 0, sums, total);
+    const int taken = (int)__reduce_max_sync(0xffffffffu, ok && s.lack() ? (unsigned)upto : 0u);  // (they ascend)
+    off[tid] = pages - 1 - (upto - s.lack());
+    first[tid] = s.held;
+    count[tid] = ok ? s.lack() : 0;
+    const int64_t end = rows + kp_scan<T>(ok ? s.rows : 0, sums[1], total);
     rows += total;
-    off[threadIdx.x] = pages - 1 - (upto - s.lack());
-    first[threadIdx.x] = s.held;
-    count[threadIdx.x] = ok ? s.lack() : 0;
-    kp_scan(count[threadIdx.x], sums, total);  // (orders the writes above, too)
-    taken += total;
+    if (lane == 0 && taken) atomicMax(&most, taken);
     if (b < a.batch) {
-      a.q_start[b + 1] = (int)min(end, (int64_t)a.n_rows);
-      a.seq_len[b] = ok ? s.start + s.rows : s.start;
-    }
-    for (int i = warp; i < KP_THREADS && b0 + i < a.batch; i += KP_WARPS) {
-      int* row = a.table + (int64_t)(b0 + i) * a.max_pages + first[i];
-      for (int j = lane; j < count[i]; j += 32) row[j] = a.free[off[i] - j];
-    }
-    __syncthreads();
-    if (b < a.batch && !broken && !s.bad && (ok || s.back())) a.held[b] = s.need;
-  }
-  if (threadIdx.x == 0) {
-    a.q_start[0] = 0;
-    if (a.batch && !broken) *a.n_free = (int)(pages - taken);
-    if (rows > a.n_rows) report_error(err, DERR_KV_RANGE);
-  }
-  __syncthreads();
-
-  // ---- rows
-  const int live = (int)min(rows, (int64_t)a.n_rows);
-  for (int r = threadIdx.x; r < a.n_rows; r += KP_THREADS) {
-    int slot = -1, pos = -1;
-    if (r < live) {
-      int lo = 0, hi = a.batch - 1;  // the first sequence that ends past r
-      while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (a.q_start[mid + 1] > r) hi = mid;
-        else lo = mid + 1;
+      const int q = (int)min(end, (int64_t)a.n_rows);
+      if (kept) starts[b + 1] = q;
+      if (rank == 0) {
+        a.q_start[b + 1] = q;
+        a.seq_len[b] = ok ? s.start + s.rows : s.start;
       }
-      pos = a.start[lo] + r - a.q_start[lo];
-      const int page = a.table[(int64_t)lo * a.max_pages + (pos >> a.page_shift)];
-      if (page >= 0 && page < a.n_pages) slot = (page << a.page_shift) + (pos & (P - 1));
-      else report_error(err, DERR_KV_RANGE);
     }
-    a.slot[r] = slot;
-    a.pos[r] = pos;
+    meet();  // (every CTA has read what the sequences hold)
+    for (int i = warp; i < T && b0 + i < a.batch; i += CTAS * (T / 32)) {
+      int* row = a.table + (int64_t)(b0 + i) * a.max_pages + first[i];
+      for (int j = lane; j < count[i]; j += 32) row[j] = __ldcg(a.free + off[i] - j);
+    }
+    if (rank == 0 && b < a.batch && !broken && !s.bad && (ok || s.back())) a.held[b] = s.need;
   }
+  if (tid == 0) {
+    starts[0] = 0;
+    if (rank == 0) {
+      a.q_start[0] = 0;
+      if (rows > a.n_rows) report_error(err, DERR_KV_RANGE);
+    }
+  }
+  meet();
+  if (rank == 0 && tid == 0 && a.batch && !broken) *a.n_free = (int)(pages - most);
+  if (!ROWS_TOO) return;
+  kp_rows(a, kept ? starts : nullptr, 4 * tid, 4 * T, err);
+}
+
+// The rows of a step that has many of them, by CTAs all over the GPU.
+__global__ void __launch_bounds__(KP_ROW_THREADS) kv_plan_rows_kernel(KvPlan a, int* err) {
+  __shared__ int starts[KP_STARTS + 1];
+  pdl_wait();
+  const bool kept = a.batch <= KP_STARTS;
+  for (int i = threadIdx.x; kept && i <= a.batch; i += KP_ROW_THREADS) starts[i] = a.q_start[i];
+  __syncthreads();
+  kp_rows(a, kept ? starts : nullptr, 4 * ((int64_t)blockIdx.x * KP_ROW_THREADS + threadIdx.x), 4 * (int64_t)gridDim.x * KP_ROW_THREADS, err);
 }
 
 }  // namespace
 
-cudaError_t kv_plan_launch(const KvPlan& a, int* err, cudaStream_t stream) {
-  kv_plan_kernel<<<1, KP_THREADS, 0, stream>>>(a, err);
-  return cudaGetLastError();
+cudaError_t kv_plan_launch(const KvPlan& a, int sms, int* err, cudaStream_t stream) {
+  if (a.n_rows <= 4096 && a.batch <= 256) {
+    kv_plan_kernel<512, 1, true><<<1, 512, 0, stream>>>(a, err);
+    return cudaGetLastError();
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(KP_CLUSTER);
+  cfg.blockDim = dim3(1024);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = KP_CLUSTER;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kv_plan_kernel<1024, KP_CLUSTER, false>, a, err);
+  if (e != cudaSuccess || a.n_rows == 0) return e;
+  const int64_t ctas = ((int64_t)a.n_rows + 4 * KP_ROW_THREADS - 1) / (4 * KP_ROW_THREADS), most = 8 * (int64_t)sms;
+  return launch_pdl(kv_plan_rows_kernel, dim3((unsigned)(ctas < most ? ctas : most)), dim3(KP_ROW_THREADS), 0, stream, a, err);
 }
 
 }  // namespace dcl
