@@ -85,28 +85,11 @@ struct KaCfg {
   static_assert(STAGES >= 2, "a step in flight");
 };
 
-__device__ __forceinline__ uint32_t smem_addr(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
-__device__ __forceinline__ uint2 lds64(uint32_t a) {
-  uint2 v;
-  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
-  return v;
-}
 __device__ __forceinline__ uint32_t lds_u16(uint32_t a) {
   uint16_t v;
   asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(a));
   return v;
 }
-__device__ __forceinline__ uint32_t lds_u8(uint32_t a) {
-  uint32_t v;
-  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(a));
-  return v;
-}
-__device__ __forceinline__ uint32_t lds32(uint32_t a) {
-  uint32_t v;
-  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a));
-  return v;
-}
-__device__ __forceinline__ void sts8(uint32_t a, uint32_t v) { asm volatile("st.shared.u8 [%0], %1;" ::"r"(a), "r"(v) : "memory"); }
 __device__ __forceinline__ float2 lds_f2(uint32_t a) {
   float2 v;
   asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(a) : "memory");
@@ -139,18 +122,6 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
 template <int ROWB>
 __device__ __forceinline__ uint32_t chunk_at(int r, int c) {
   return (uint32_t)(r * ROWB + ((c ^ (ROWB == 64 ? (r >> 1) & 3 : r & 7)) << 4));
-}
-// The same of a tile of 4-bit codes.  Rows change places too, as a value's operand takes 8 (HD = 128) or 4
-// bytes of every other row: a half-warp's 8-byte loads, or a warp's 4-byte ones, then meet all the banks,
-// and a key's (16 or 8 bytes of neighbouring rows) as well.
-template <int ROWB>
-__device__ __forceinline__ uint32_t chunk4_at(int r, int c) {
-  if (ROWB == 64) {
-    const int x = r & 1 ? 4 + ((r >> 1 & 3) ^ 1) : r >> 1 & 3;
-    return (uint32_t)(((r & ~7) + x) * 64 + ((c ^ (x & 2)) << 4));
-  }
-  const int x = r & 1 ? 8 + ((r >> 1 & 7) ^ 2) : r >> 1 & 7;
-  return (uint32_t)(((r & ~15) + x) * 32 + (c << 4));
 }
 // The order in which hd enters the two products is free as long as q and k, and v and the output,
 // agree: a lane's operands are taken from whole 16-byte chunks.  k_chunk: the i-th chunk of 8
@@ -250,6 +221,14 @@ __global__ void __launch_bounds__(KaCfg<HD, F, RS>::THREADS, KA_CTAS) kv_attenti
   const uint32_t ring = smem_addr(smem) + warp * C::RING_B;
   float2* ml = reinterpret_cast<float2*>(smem + C::ML);
 
+  // 4-bit tiles: where a lane's chunk of a copy, its part of keys 0 - 7, and those of two values' lie; 8
+  // keys on is EIGHT bytes further, 16 keys 16 rows
+  constexpr uint32_t EIGHT = C::ROWB == 64 ? 512 : 128;
+  const uint32_t lane_at = chunk4_at<C::ROWB>(lane / (C::ROWB / 16), lane % (C::ROWB / 16));
+  const uint32_t k_at = HD == 128 ? chunk4_at<C::ROWB>(quad, place) : chunk4_at<C::ROWB>(quad, place >> 1) + 8 * (place & 1);
+  const uint32_t v_at[2] = {chunk4_at<C::ROWB>(2 * place, quad * (HD / 16) >> 4) + (quad * (HD / 16) & 15),
+                            chunk4_at<C::ROWB>(2 * place + 1, quad * (HD / 16) >> 4) + (quad * (HD / 16) & 15)};
+
   const KaLine<C::ROWS, KA_START> line(kv, a);
 
   // ---- this CTA's part of the line of all items
@@ -291,7 +270,6 @@ __global__ void __launch_bounds__(KaCfg<HD, F, RS>::THREADS, KA_CTAS) kv_attenti
 
     // ---- this warp's steps: keys key0 + KT warp on, then every WARPS-th
     const int stop = min(key1, lim_max);
-    auto tile_at = [](int r, int c) { return Q4 ? chunk4_at<C::ROWB>(r, c) : chunk_at<C::ROWB>(r, c); };
     const int* table = a.table + (int64_t)it.b * a.max_pages;
     int next = key0 + KT * warp;  // first key of the next step to copy
     uint32_t bad = 0;             // two bits a stage: 16 keys whose page is not the cache's
@@ -317,7 +295,8 @@ __global__ void __launch_bounds__(KaCfg<HD, F, RS>::THREADS, KA_CTAS) kv_attenti
 #pragma unroll
             for (int i = 0; i < C::ROWB / 32; ++i) {
               const int c = i * 32 + lane;
-              const uint32_t at = tile_at(16 * h + c / (C::ROWB / 16), c % (C::ROWB / 16));
+              const uint32_t at = Q4 ? lane_at + 16 * C::ROWB * h + 512 * i
+                                     : chunk_at<C::ROWB>(16 * h + c / (C::ROWB / 16), c % (C::ROWB / 16));
               copy16(dst + at, k + 512 * i);
               copy16(dst + C::TILE + at, v + 512 * i);
             }
@@ -450,10 +429,11 @@ __global__ void __launch_bounds__(KaCfg<HD, F, RS>::THREADS, KA_CTAS) kv_attenti
 #pragma unroll
           for (int j = 0; j < NK; ++j) {
             if (Q4) {  // a lane has 32 components (one group) or 16
+              const uint32_t at = sk + k_at + (j >> 1) * (16 * C::ROWB) + (j & 1) * EIGHT;
               if (HD == 128) {
-                w[j] = lds128(sk + chunk4_at<C::ROWB>(8 * j + quad, place));
+                w[j] = lds128(at);
               } else {
-                const uint2 two = lds64(sk + chunk4_at<C::ROWB>(8 * j + quad, place >> 1) + 8 * (place & 1));
+                const uint2 two = lds64(at);
                 w[j].x = two.x;
                 w[j].y = two.y;
               }
@@ -618,12 +598,13 @@ __global__ void __launch_bounds__(KaCfg<HD, F, RS>::THREADS, KA_CTAS) kv_attenti
 #pragma unroll
             for (int r = 0; r < 4; ++r) {  // keys 2 place, 2 place + 1, and 8 on
               const int row = 16 * half + 2 * place + (r & 1) + 8 * (r >> 1);
+              const uint32_t at = sv + v_at[r & 1] + half * (16 * C::ROWB) + (r >> 1) * EIGHT;
               if (W == 2) {
-                const uint2 x = lds64(sv + chunk4_at<C::ROWB>(row, quad >> 1) + 8 * (quad & 1));
+                const uint2 x = lds64(at);
                 v[r][0] = x.x;
                 v[r][W - 1] = x.y;
               } else {
-                v[r][0] = lds32(sv + chunk4_at<C::ROWB>(row, quad >> 2) + 4 * (quad & 3));
+                v[r][0] = lds32(at);
               }
               scale[r] = lds_u8(se + (KT + row) * SIDE + quad / (8 / (SIDE ? SIDE : 8)));
             }

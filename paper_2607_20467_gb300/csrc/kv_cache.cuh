@@ -41,13 +41,15 @@ struct KvAttn {
   __nv_bfloat16* out;       // [rows][H][hd]
   float* lse;               // [rows][H] or NULL
 };
-// Two kernels: for up to 32 rows (new positions x query heads of a kv head) that share a kv head's keys,
-// and for more (not causal).  Scratch of a launch on `sms` SMs: counters, zero before the first launch
+// Three kernels: for up to 8 rows (new positions x query heads of a kv head) that share a kv head's keys in 4
+// bits, for up to 32 rows, and for more (not causal).  Scratch of a launch on `sms` SMs: counters, zero before the first launch
 // and left zero by each, then the parts of rows whose keys several CTAs share.  The launches of a
-// context run one after another on its stream, so that both kernels use the same.
+// context run one after another on its stream, so that all use the same.
 constexpr size_t KV_ATTN_COUNTERS = 4096;                                      // bytes (an int per CTA)
 constexpr size_t KV_ATTN_PART_BYTES = 2 * 32 * (128 + 4) * sizeof(float);      // per CTA
 constexpr size_t KV_ATTN_TC_PART_BYTES = 2 * 256 * (128 + 4) * sizeof(float);
+bool kv_attention_q4_few(const KvPool& kv, const KvAttn& a);
+cudaError_t kv_attention_q4_launch(const KvPool& kv, const KvAttn& a, void* scratch, int sms, int* err, cudaStream_t stream);
 bool kv_attention_many_rows(const KvPool& kv, const KvAttn& a);
 size_t kv_attention_scratch(int sms);
 size_t kv_attention_tc_scratch(int sms);

@@ -244,6 +244,23 @@ template <int N>
 __device__ __forceinline__ void copy_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
+__device__ __forceinline__ uint32_t smem_addr(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+__device__ __forceinline__ uint2 lds64(uint32_t a) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ uint32_t lds_u8(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ void sts8(uint32_t a, uint32_t v) { asm volatile("st.shared.u8 [%0], %1;" ::"r"(a), "r"(v) : "memory"); }
 __device__ __forceinline__ uint4 lds128(uint32_t a) {
   uint4 v;
   asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
@@ -259,6 +276,19 @@ __device__ __forceinline__ uint32_t widen_hi(uint32_t w) {
   uint32_t r;
   asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, h;\n\t}" : "=r"(r) : "r"(w));
   return r;
+}
+// Byte offset of 16-byte chunk c of row r of a tile of 4-bit codes.  Rows change places, as a value's operand
+// takes 8 (HD = 128) or 4 bytes of every other row: a half-warp's 8-byte loads, or a warp's 4-byte ones, then
+// meet all the banks, and a key's (16 or 8 bytes of neighbouring rows) as well.  8 rows on is 512 or 128 bytes
+// further, 16 rows 16 rows.
+template <int ROWB>
+__device__ __forceinline__ uint32_t chunk4_at(int r, int c) {
+  if (ROWB == 64) {
+    const int x = r & 1 ? 4 + ((r >> 1 & 3) ^ 1) : r >> 1 & 3;
+    return (uint32_t)(((r & ~7) + x) * 64 + ((c ^ (x & 2)) << 4));
+  }
+  const int x = r & 1 ? 8 + ((r >> 1 & 7) ^ 2) : r >> 1 & 7;
+  return (uint32_t)(((r & ~15) + x) * 32 + (c << 4));
 }
 // Two bf16 parts of a weight p: its upper half (8 bits), and what that leaves of p (1 + 2^-17).  The factor, the
 // same for all weights and half of what the parts may be off by, keeps the second above zero where the

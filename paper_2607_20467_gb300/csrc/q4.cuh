@@ -42,8 +42,12 @@ __device__ __forceinline__ Q4Scale q4_scale(uint32_t bytes) {
 __device__ __forceinline__ Q4Scale q4_scale_twice(uint32_t byte) { return q4_scale(byte * 0x10001u); }
 
 // The components i (in the lower half) and i + 4 of a word's eight, i < 4.
+// (One instruction for the mask and the exponents: left to the compiler they were two, and the integer pipe is
+// what bounds the attention.)
 __device__ __forceinline__ uint32_t q4_widen(uint32_t w, int i, const Q4Scale& f) {
-  return q4_fma((w >> (4 * i) & 0x000f000fu) | 0x43004300u, f.s, f.off);
+  uint32_t x;
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(x) : "r"(w >> (4 * i)), "r"(0x000f000fu), "r"(0x43004300u));
+  return q4_fma(x, f.s, f.off);
 }
 
 }  // namespace dcl
