@@ -44,8 +44,7 @@ struct K4Cfg {
   static constexpr int RING = STAGES * STAGE;
   static constexpr int O_PITCH = HD + 36;            // a warp's O in the ring's place: [ROWS][O_PITCH] floats, 16 components and 4 on
   static constexpr int O_B = K4_ROWS * O_PITCH * 4;
-  static constexpr int JOIN_B = (K4_ROWS * K4_MOST * 8 + WARPS - 1) / WARPS;  // the weights of an item's parts take it, too
-  static constexpr int RING_B = (std::max(RING, std::max(O_B, JOIN_B)) + 127) & ~127;
+  static constexpr int RING_B = (std::max(RING, O_B) + 127) & ~127;
   static constexpr int ML = WARPS * RING_B;          // {m, l} [warp][ROWS]
   static constexpr int WT = ML + WARPS * K4_ROWS * 8;  // weights of the warps' parts [ROWS][8], then {m, l} of the rows
   static constexpr int HEAD = WT + K4_ROWS * (8 * 4 + 8);  // the walk's variables
@@ -72,6 +71,59 @@ __device__ __noinline__ bool any_without_numbers(uint32_t scales, int lane) {
   bool any = false;
   for (int c = lane; c < BYTES; c += 32) any |= lds_u8(scales + c) >= Q4_SCALES;
   return __any_sync(0xffffffffu, any);
+}
+
+// The parts of an item, left by its CTAs, joined.  HD / 4 lanes have a row, a lane four of its components: it
+// copies those of many parts into shared memory (room for them, DEEP a thread) at once, as one takes about
+// 1000 cycles here; the weights come meanwhile, every lane those of every so many parts.
+template <int HD, int THREADS, int DEEP>
+__device__ __forceinline__ void join4(const KvAttn& a, const KaJoin& it, int rep, const float* parts, uint32_t room) {
+  using Part = KaPart<HD, K4_ROWS, false>;
+  constexpr int LPR = HD / 4;
+  static_assert(THREADS / LPR >= K4_ROWS, "a row for every so many threads");
+  const int l = threadIdx.x % LPR, r = threadIdx.x / LPR, n = it.parts;
+  if (r / (32 / LPR) * (32 / LPR) >= it.rows) return;  // (whole warps)
+  const int base_lane = (threadIdx.x & 31) / LPR * LPR, rr = min(r, it.rows - 1);
+  // (the first CTA's part is its second, the others' their first)
+  const float* first = parts + (2 * (int64_t)it.c0 + 1) * Part::FLOATS;
+  auto part_of = [&](int c) { return first + (int64_t)max(2 * c - 1, 0) * Part::FLOATS; };
+  const uint32_t mine = room + 16 * threadIdx.x;
+  auto ask = [&](int c0) {
+    const int m = min(n - c0, DEEP);
+    for (int i = 0; i < m; ++i) copy16(mine + 16 * THREADS * i, part_of(c0 + i) + Part::four(rr, l));
+    copy_commit();
+  };
+  ask(0);
+  auto ml_of = [&](int c) { return __ldcg(reinterpret_cast<const float2*>(part_of(c) + Part::ml(rr))); };
+  float2 x = ml_of(min(l, n - 1));
+  float top = x.x, sum = 0.f, w = 0.f;
+  for (int c = l + LPR; c < n; c += LPR) top = fmaxf(top, ml_of(c).x);
+#pragma unroll
+  for (int d = LPR / 2; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int c0 = 0; c0 < n; c0 += DEEP) {
+    if (c0) ask(c0);
+    copy_wait<0>();
+    const int m = min(n - c0, DEEP);
+    for (int i = 0; i < m; ++i) {
+      const int c = c0 + i;
+      if (c % LPR == 0) {  // weights of the next LPR parts
+        if (c) x = ml_of(min(c + l, n - 1));
+        const float half = c + l < n ? part_half(x.x, top) : 0.f;
+        w = half * half;
+        sum = fmaf(x.y * half, half, sum);
+      }
+      const uint4 y = lds128(mine + 16 * THREADS * i);
+      add_scaled(acc, make_float4(__uint_as_float(y.x), __uint_as_float(y.y), __uint_as_float(y.z), __uint_as_float(y.w)),
+                 __shfl_sync(0xffffffffu, w, base_lane + c % LPR));
+    }
+  }
+#pragma unroll
+  for (int d = LPR / 2; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+  if (r >= it.rows) return;
+  const int tok = (it.first + r) / rep, at = (it.row0 + tok) * a.H + it.head0 + it.first + r - tok * rep;
+  if (a.lse && l == 0) a.lse[at] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+  finish4<HD>(a, KaRow{sum == 0.f ? 0.f : 1.f / sum, at}, 4 * l, acc);
 }
 
 template <int HD>
@@ -138,15 +190,18 @@ __global__ void __launch_bounds__(K4Cfg<HD>::THREADS, K4_CTAS) kv_attention_q4_k
     int next = key0 + KT * warp;  // first key of the next step to copy
     uint32_t bad = 0;             // two bits a stage: 16 keys whose page is not the cache's
     uint32_t slot = 0;            // of the ring, in bytes
-    int page[KT / 16];
-    auto look_up = [&]() {  // (longer pages than 16 hold a step's keys together)
-      page[0] = next < stop ? table[next >> kv.page_shift] : 0;
-      page[1] = !small ? page[0] : next + 16 < stop ? table[(next + 16) >> kv.page_shift] : 0;
+    int pages[2];                 // of this warp's steps, a step a lane (longer pages than 16 hold a step's keys together)
+    int turn = 0;                 // the next step's lane
+    auto look_up = [&]() {
+      const uint32_t key = (uint32_t)next + KT * C::WARPS * lane;  // (which may pass 2^31)
+      pages[0] = key < (uint32_t)stop ? table[key >> kv.page_shift] : 0;
+      pages[1] = small && key + 16 < (uint32_t)stop ? table[(key + 16) >> kv.page_shift] : pages[0];
     };
     look_up();
     auto issue = [&]() {
       if (next < stop) {
         const uint32_t dst = ring + slot;
+        const int page[2] = {__shfl_sync(0xffffffffu, pages[0], turn), __shfl_sync(0xffffffffu, pages[1], turn)};
         uint32_t gone = 0;
 #pragma unroll
         for (int h = 0; h < KT / 16; ++h) {
@@ -166,7 +221,8 @@ __global__ void __launch_bounds__(K4Cfg<HD>::THREADS, K4_CTAS) kv_attention_q4_k
         }
         bad = bad << 2 | gone;
         next += KT * C::WARPS;
-        look_up();
+        turn = (turn + 1) & 31;
+        if (turn == 0) look_up();
       } else {
         bad <<= 2;
       }
@@ -408,23 +464,19 @@ __global__ void __launch_bounds__(K4Cfg<HD>::THREADS, K4_CTAS) kv_attention_q4_k
       line.sharers(walk, it, c0, c1);
       __syncthreads();
       if (threadIdx.x == 0) {
-        __threadfence();  // (the block's writes, which the barrier ordered before)
-        const int done = atomicAdd(&scratch.count[c0], 1);
+        int done;  // (the block's writes, which the barrier ordered before, come first, and what a join reads after)
+        asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;" : "=r"(done) : "l"(scratch.count + c0) : "memory");
         if (done == c1 - c0) {  // the last to come joins the parts, when it is through with its own
           scratch.count[c0] = 0;
           todo[todo[0].rows++ ? 2 : 1] = KaJoin{it.row0, it.g * rep, it.first, it.rows, c0, c1 - c0 + 1};
         }
-        __threadfence();
       }
+    } else {
+      __syncthreads();  // (the rings are free again)
     }
-    __syncthreads();
   }
-  for (int i = 0; i < todo[0].rows; ++i) {
-    const KaJoin j = todo[1 + i];
-    join_parts<HD, K4_ROWS, C::THREADS, false>(a, j, 0, rep, scratch.part, reinterpret_cast<float2*>(smem),
-                                               reinterpret_cast<KaRow*>(smem + C::WT + K4_ROWS * 32), threadIdx.x, [] { __syncthreads(); });
-    __syncthreads();
-  }
+  __syncthreads();
+  for (int i = 0; i < todo[0].rows; ++i) join4<HD, C::THREADS, C::ML / (16 * C::THREADS)>(a, todo[1 + i], rep, scratch.part, smem_addr(smem));
 }
 
 template <int HD>

@@ -106,29 +106,48 @@ struct KaLine {
       }
       return upto;
     };
-    int64_t total = 0, own, upto = 0;
-    for (int b0 = 0; b0 < a.batch; b0 += 32) {
-      upto = scan(b0, own);
-      total += __shfl_sync(0xffffffffu, upto, 31);
+    // (of up to 128 sequences every lane keeps its four: a look at the lengths again takes as long as all the rest)
+    int64_t total = 0, own4[4], upto4[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      own4[i] = upto4[i] = 0;
+      if (32 * i < a.batch) {
+        upto4[i] = scan(32 * i, own4[i]);
+        total += __shfl_sync(0xffffffffu, upto4[i], 31);
+      }
+    }
+    for (int b0 = 128; b0 < a.batch; b0 += 32) {
+      int64_t own;
+      total += __shfl_sync(0xffffffffu, scan(b0, own), 31);
     }
     const KaShare share(total, gridDim.x);
     // where the cut before CTA c goes: the position, its sequence and the positions before that
     auto cut = [&](int c, int& b, int64_t& before) -> int64_t {
       const int64_t u = share.start(c);
       before = 0;
-      for (int b0 = 0; b0 < a.batch; b0 += 32) {
-        if (a.batch > 32) upto = scan(b0, own);
+      auto here = [&](int b0, int64_t upto, int64_t own, int64_t& at) {  // whether it is among sequences b0 .. b0 + 31
         const unsigned hit = __ballot_sync(0xffffffffu, u < before + upto);
-        if (hit) {
-          const int l = __ffs(hit) - 1;
-          b = b0 + l;
-          before += __shfl_sync(0xffffffffu, upto - own, l);
-          const int line = line_of(seq_len(b));
-          const int64_t in = u - before;
-          const int pos = in < (1ll << 31) ? (int)in % line : (int)(in % line);
-          return u - pos + KaCut<START>::at(pos, line);
+        if (!hit) {
+          before += __shfl_sync(0xffffffffu, upto, 31);
+          return false;
         }
-        before += __shfl_sync(0xffffffffu, upto, 31);
+        const int l = __ffs(hit) - 1;
+        b = b0 + l;
+        before += __shfl_sync(0xffffffffu, upto - own, l);
+        const int line = line_of(seq_len(b));
+        const int64_t in = u - before;
+        const int pos = in < (1ll << 31) ? (int)in % line : (int)(in % line);
+        at = u - pos + KaCut<START>::at(pos, line);
+        return true;
+      };
+      int64_t at;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (32 * i < a.batch && here(32 * i, upto4[i], own4[i], at)) return at;
+      for (int b0 = 128; b0 < a.batch; b0 += 32) {
+        int64_t own;
+        const int64_t upto = scan(b0, own);
+        if (here(b0, upto, own, at)) return at;
       }
       b = a.batch;
       return total;
