@@ -59,6 +59,12 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// (the same without a sum to add to)
+__device__ __forceinline__ void mma_bf16_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+               : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
 // An 8 x 8 matrix of 16-bit elements, a row's pairs by four lanes, transposed.
 __device__ __forceinline__ uint32_t transposed(uint32_t x) {
   uint32_t y;
@@ -145,10 +151,10 @@ __global__ void __launch_bounds__(K4Cfg<HD>::THREADS, K4_CTAS) kv_attention_q4_k
   const uint32_t k_at = HD == 128 ? chunk4_at<ROWB>(quad, place) : chunk4_at<ROWB>(quad, place >> 1) + 8 * (place & 1);
   const uint32_t v_at[2] = {chunk4_at<ROWB>(2 * place, quad * (HD / 16) >> 4) + (quad * (HD / 16) & 15),
                             chunk4_at<ROWB>(2 * place + 1, quad * (HD / 16) >> 4) + (quad * (HD / 16) & 15)};
-  // a copy's addresses: chunk `lane` of 16 keys, and of the scales of the keys (half of the lanes) and the values
+  // a copy's addresses: chunk `lane` of 16 keys; of the scales of a page's keys (16 or 32), then of the values'
   const uint8_t* k_from = static_cast<const uint8_t*>(kv.k) + 16 * lane;
   const uint8_t* v_from = static_cast<const uint8_t*>(kv.v) + 16 * lane;
-  const int of = lane / SIDE & 1, side_chunk = 16 * (lane % SIDE);
+  const int side_chunks = small ? SIDE : 2 * SIDE, of = lane / side_chunks, side_chunk = 16 * (lane - of * side_chunks);
   const uint8_t* side_from = reinterpret_cast<const uint8_t*>(of ? kv.v_exp : kv.k_exp) + side_chunk;
   const uint32_t side_at = 2 * C::TILE + SIDE * KT * of + side_chunk, page_bytes = (uint32_t)(kv.G * P * ROWB);  // (2^24 at most)
   const int k_group = place * SIDE / 4, v_group = quad * SIDE / 8;
@@ -198,34 +204,42 @@ __global__ void __launch_bounds__(K4Cfg<HD>::THREADS, K4_CTAS) kv_attention_q4_k
       pages[1] = small && key + 16 < (uint32_t)stop ? table[(key + 16) >> kv.page_shift] : pages[0];
     };
     look_up();
+    const uint8_t *k_head = k_from + head_at, *v_head = v_from + head_at, *side_head = side_from + head_at / (ROWB / SIDE);
+    auto copy = [&](int page, int in_page, int h, auto rows_) {  // 16 keys or 32 of a page
+      constexpr int ROWS = decltype(rows_)::value;
+      const uint64_t at = (uint64_t)(unsigned)page * page_bytes + (uint32_t)(in_page * ROWB);
+      const uint8_t *k = k_head + at, *v = v_head + at;
+      const uint32_t dst = ring + slot + copy_at + 16 * ROWB * h;
+#pragma unroll
+      for (int i = 0; i < ROWS * ROWB / 512; ++i) {
+        copy16(dst + 512 * i, k + 512 * i);
+        copy16(dst + C::TILE + 512 * i, v + 512 * i);
+      }
+      if (lane < 2 * side_chunks) copy16(ring + slot + side_at + 16 * SIDE * h, side_head + at / (ROWB / SIDE));
+    };
     auto issue = [&]() {
+      uint32_t gone = 0;
       if (next < stop) {
-        const uint32_t dst = ring + slot;
-        const int page[2] = {__shfl_sync(0xffffffffu, pages[0], turn), __shfl_sync(0xffffffffu, pages[1], turn)};
-        uint32_t gone = 0;
-#pragma unroll
-        for (int h = 0; h < KT / 16; ++h) {
-          if (next + 16 * h >= stop) break;
-          if ((unsigned)page[h] < (unsigned)kv.pages) {
-            const uint64_t at = (uint64_t)(unsigned)page[h] * page_bytes + (uint32_t)(((next & (P - 1)) + (small ? 0 : 16 * h)) * ROWB + head_at);
-#pragma unroll
-            for (int i = 0; i < ROWB / 32; ++i) {
-              copy16(dst + copy_at + 16 * ROWB * h + 512 * i, k_from + at + 512 * i);
-              copy16(dst + copy_at + C::TILE + 16 * ROWB * h + 512 * i, v_from + at + 512 * i);
-            }
-            if (lane < 2 * SIDE) copy16(dst + side_at + 16 * SIDE * h, side_from + at / (ROWB / SIDE));
-          } else {
-            gone |= 1u << h;
-            if (lane == 0) report_error(err, DERR_KV_RANGE);
+        const int page = __shfl_sync(0xffffffffu, pages[0], turn);
+        const bool there = (unsigned)page < (unsigned)kv.pages;
+        if (!small) {  // (one page holds all 32, those past the sequence's end too)
+          if (there) copy(page, next & (P - 1), 0, std::integral_constant<int, 32>{});
+          else gone = 3;
+        } else {
+          const int page1 = __shfl_sync(0xffffffffu, pages[1], turn);
+          if (there) copy(page, 0, 0, std::integral_constant<int, 16>{});
+          else gone = 1;
+          if (next + 16 < stop) {
+            if ((unsigned)page1 < (unsigned)kv.pages) copy(page1, 0, 1, std::integral_constant<int, 16>{});
+            else gone |= 2;
           }
         }
-        bad = bad << 2 | gone;
+        if (gone && lane == 0) report_error(err, DERR_KV_RANGE);
         next += KT * C::WARPS;
         turn = (turn + 1) & 31;
         if (turn == 0) look_up();
-      } else {
-        bad <<= 2;
       }
+      bad = bad << 2 | gone;
       copy_commit();
       slot = slot == C::RING - C::STAGE ? 0 : slot + C::STAGE;
     };
@@ -295,12 +309,12 @@ __global__ void __launch_bounds__(K4Cfg<HD>::THREADS, K4_CTAS) kv_attention_q4_k
           f[i] = q4_scale_twice(lds_u8(se + (16 * t + 8 * i + quad) * SIDE + k_group));
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s[t][j] = 0.f;
-#pragma unroll
         for (int x = 0; x < KS; ++x) {
           const int i = 2 * (x & 1);
-          mma_bf16(s[t], q4_widen(w[0][x >> 1], i, f[0]), q4_widen(w[1][x >> 1], i, f[1]), q4_widen(w[0][x >> 1], i + 1, f[0]),
-                   q4_widen(w[1][x >> 1], i + 1, f[1]), q[x][0], q[x][1]);
+          const uint32_t a0 = q4_widen(w[0][x >> 1], i, f[0]), a1 = q4_widen(w[1][x >> 1], i, f[1]);
+          const uint32_t a2 = q4_widen(w[0][x >> 1], i + 1, f[0]), a3 = q4_widen(w[1][x >> 1], i + 1, f[1]);
+          if (x == 0) mma_bf16_first(s[t], a0, a1, a2, a3, q[x][0], q[x][1]);
+          else mma_bf16(s[t], a0, a1, a2, a3, q[x][0], q[x][1]);
         }
       }
       if (masked) {
