@@ -813,7 +813,7 @@ cudaError_t launch_rows(const KvPool& kv, const KvAttn& a, const KaScratch& s, i
 // device only: the page table's width stands for them.
 bool kv_attention_many_rows(const KvPool& kv, const KvAttn& a) {
   const int64_t rows = (int64_t)a.max_new * (a.H / kv.G);
-  if (a.causal || rows <= 32 || kv.format == KV_Q4) return false;
+  if (a.causal || rows <= 32) return false;
   const double units = (double)a.batch * kv.G * (((int64_t)a.max_pages * kv.page_len() + KA_UNIT - 1) / KA_UNIT);
   const int64_t rest = rows % 256;
   const double here = 10.0 * (double)((rows + 31) / 32), there = 18.0 * (double)(rows / 256) + (rest > 128 ? 18 : rest ? 15 : 0);

@@ -36,6 +36,7 @@
 #include "common.cuh"
 #include "kv_cache.cuh"
 #include "kv_share.cuh"
+#include "q4.cuh"
 #include "tc_ptx.cuh"
 
 namespace dcl {
@@ -49,14 +50,15 @@ constexpr int TC_THREADS = 544;
 constexpr int TC_BOX = 128 * 128; // 128 rows of 128 bytes, swizzled
 constexpr int TC_JOIN = 8000;     // rows x parts joined at a time
 
-template <int HD, bool FP8>
+template <int HD, KvFormat F>
 struct TcCfg {
   static constexpr int KB = HD / 64;                  // boxes along hd
   static constexpr int TILE = KB * TC_BOX;            // 128 rows of q, keys or values, 16 bits each
   static constexpr int NS = 4;                        // operand tiles of keys and values, in turn
   static constexpr int KV = 2 * TILE;                 // (q comes first)
-  static constexpr int RAW = KV + NS * TILE;          // FP8: codes of a unit's keys, then of its values
-  static constexpr int THERE = RAW + (FP8 ? 2 * 128 * HD : 0);  // [4 units][4 x 32 keys]: a bit for each key that is there
+  static constexpr int RAW = KV + NS * TILE;          // codes of a unit's keys, then of its values
+  static constexpr int CODES = F == KV_FP8 ? 128 * HD : F == KV_Q4 ? 128 * HD / 2 : 0;
+  static constexpr int THERE = RAW + 2 * CODES;       // [4 units][4 x 32 keys]: a bit for each key that is there
   static constexpr int BAR = THERE + 4 * 4 * 4;                 // (keys may be two units ahead)
   static constexpr int NBARS = 2 * NS + 4 * 2 + 1;
   static constexpr int HOLDER = BAR + 8 * NBARS;      // TMEM address, abort flag
@@ -102,10 +104,10 @@ __device__ __forceinline__ uint32_t widen(uint32_t w, int half, __nv_bfloat162 f
 
 // The MMAs of an item (the whole warp; one lane issues).  Its operands are made known as the warp's, in
 // uniform registers: else an issue takes about 100 cycles, more than most of the products.
-template <int HD, bool FP8>
+template <int HD, KvFormat F>
 __device__ __forceinline__ bool tc_mma(uint32_t base, uint32_t tmem, int tiles, int n, uint32_t& seq_, uint32_t& items,
                                        uint32_t& units, volatile int* abort_flag) {
-  using C = TcCfg<HD, FP8>;
+  using C = TcCfg<HD, F>;
   constexpr uint32_t idesc_s = make_idesc(128, 128);
   constexpr uint32_t idesc_o = make_idesc(128, HD) | IDESC_B_MN;
   base = (uint32_t)warp_uniform((int)base);
@@ -168,10 +170,10 @@ __device__ __forceinline__ bool tc_mma(uint32_t base, uint32_t tmem, int tiles, 
   return true;
 }
 
-template <int HD, bool FP8>
+template <int HD, KvFormat F>
 __global__ void __launch_bounds__(TC_THREADS, 1)
     kv_attention_tc_kernel(KvPool kv, KvAttn a, KaScratch scratch, int* err) {
-  using C = TcCfg<HD, FP8>;
+  using C = TcCfg<HD, F>;
   extern __shared__ __align__(1024) uint8_t smem[];
   uint32_t base = smem_u32(smem);
   asm volatile("" : "+r"(base));
@@ -230,12 +232,13 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     // Keys or values of a unit: warp w of the four has keys 32 w .. 32 w + 31, lane l knows of key 32 w + l
     // (its page and exponents); they are copied in chunks of 16 bytes.
     const int values = warp >= 12, w4 = warp & 3;
-    constexpr int CH = FP8 ? HD / 16 : HD / 8;       // chunks of a vector
-    constexpr int PK = CH / 4;                       // this lane's of a key: key (lane >> 2) + 8 i, chunk (lane & 3) + 4 j
-    const int shift = kv.page_shift, P = kv.page_len(), at_key = 32 * w4 + (lane >> 2), at_chunk = lane & 3;
+    constexpr bool WIDEN = F != KV_BF16;
+    constexpr int CH = F == KV_Q4 ? HD / 32 : F == KV_FP8 ? HD / 16 : HD / 8;  // chunks of a vector
+    constexpr int LK = CH < 4 ? CH : 4, PK = CH / LK, KP = 32 / LK;  // a lane's of a key: key lane / LK + KP i, chunk lane % LK + LK j
+    const int shift = kv.page_shift, P = kv.page_len(), at_key = 32 * w4 + lane / LK, at_chunk = lane % LK;
     const void* pool = values ? kv.v : kv.k;
     const int8_t* exps = values ? kv.v_exp : kv.k_exp;
-    const uint32_t raw = base + C::RAW + values * (128 * HD);
+    const uint32_t raw = base + C::RAW + values * C::CODES;
     uint32_t seq = values;  // operand tiles (keys and values in turn): stage seq % NS
     bool ok = true;
     // (codes: eight lanes read two keys, whose chunks lie in each other's halves of 128 bytes)
@@ -261,29 +264,58 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
           const int page = __shfl_sync(0xffffffffu, pages, 16 * h);
           if (page < 0) continue;
           const uint8_t* src = static_cast<const uint8_t*>(pool) + vec_of(page, first + unit * KA_UNIT + 16 * h) * (CH * 16) +
-                               ((lane >> 2) * CH + at_chunk) * 16;
+                               (lane / LK * CH + at_chunk) * 16;
 #pragma unroll
-          for (int i = 0; i < 2; ++i)
+          for (int i = 0; i < 16 / KP; ++i)
 #pragma unroll
             for (int j = 0; j < PK; ++j) {
-              const int k = at_key + 16 * h + 8 * i, c = at_chunk + 4 * j;
-              copy16(dst + (FP8 ? raw_at(k, c) : tile_at(k, c)), src + (8 * i * CH + 4 * j) * 16);
+              const int k = at_key + 16 * h + KP * i, c = at_chunk + LK * j;
+              copy16(dst + (WIDEN ? raw_at(k, c) : tile_at(k, c)), src + (KP * i * CH + LK * j) * 16);
             }
         }
         copy_commit();
       };
-      auto exp_at = [&](int unit, int page) {
-        return FP8 && page >= 0 ? (int)exps[vec_of(page, first + unit * KA_UNIT + lane)] : 0;
+      auto exp_at = [&](int unit, int page) {  // the key's exponent, or its groups' scale bytes
+        if (!WIDEN || page < 0) return 0;
+        const int64_t vec = vec_of(page, first + unit * KA_UNIT + lane);
+        if (F == KV_FP8) return (int)exps[vec];
+        if (HD == 64) return (int)reinterpret_cast<const uint16_t*>(exps)[vec];
+        return reinterpret_cast<const int*>(exps)[vec];
       };
       int pages = page_at(0), pages2 = page_at(1);
       int e = exp_at(0, pages);
-      if (!FP8) ok = wait_empty(seq);
-      if (ok) issue(0, pages, FP8 ? raw : stage_of(seq));
+      if (!WIDEN) ok = wait_empty(seq);
+      if (ok) issue(0, pages, WIDEN ? raw : stage_of(seq));
       for (int u = 0; ok && u < n; ++u) {
         const uint32_t dst = stage_of(seq), here = __ballot_sync(0xffffffffu, pages >= 0);
         copy_wait<0>();
         __syncwarp();
-        if (FP8) {
+        if (F == KV_Q4) {
+          ok = wait_empty(seq);
+          if (!ok) break;
+#pragma unroll
+          for (int i = 0; i < 32 / KP; ++i) {
+            const int k = at_key + KP * i;
+            const uint32_t bytes = __shfl_sync(0xffffffffu, (uint32_t)e, k & 31);
+            const Q4Scale f = q4_scale_twice(bytes >> (8 * at_chunk) & 0xffu);
+            const bool in = here >> (k & 31) & 1;
+            const uint4 x = lds128(raw + raw_at(k, at_chunk));
+            // (words 0 and 2, 1 and 3 in turn, so that eight lanes' stores - two keys' - meet all the banks)
+            const bool turn = at_chunk & 2;
+            const uint32_t w[4] = {turn ? x.z : x.x, turn ? x.w : x.y, turn ? x.x : x.z, turn ? x.y : x.w};
+#pragma unroll
+            for (int z = 0; z < 4; ++z) {  // 8 components: 0, 4, 1, 5, 2, 6, 3, 7 (q and the results are in that order, too)
+              uint32_t y[4];
+#pragma unroll
+              for (int j = 0; j < 4; ++j) y[j] = q4_widen(w[z], j, f);
+              if (here != 0xffffffffu) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) y[j] = in ? y[j] : 0u;
+              }
+              st_shared_v4(dst + tile_at(k, 4 * at_chunk + (turn ? z ^ 2 : z)), y[0], y[1], y[2], y[3]);
+            }
+          }
+        } else if (F == KV_FP8) {
           const float scale = kv_pow2(e);
           const uint32_t mine = pack_bf16x2(scale, scale);  // (exact)
           ok = wait_empty(seq);
@@ -325,9 +357,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
         if (lane == 0) mbar_arrive(full0 + 8 * (seq % C::NS));
         seq += 2;
         if (u + 1 < n) {
-          if (!FP8) ok = wait_empty(seq);
+          if (!WIDEN) ok = wait_empty(seq);
           if (!ok) break;
-          issue(u + 1, pages2, FP8 ? raw : stage_of(seq));
+          issue(u + 1, pages2, WIDEN ? raw : stage_of(seq));
           e = exp_at(u + 1, pages2);
           pages = pages2;
           pages2 = page_at(u + 2);
@@ -343,7 +375,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     bool ok = true;
     const bool leader = elect_one();
     while (warp_uniform(ok && line.next(walk, it)))
-      ok = tc_mma<HD, FP8>(base, tmem, it.rows > 128 ? 2 : 1, it.until - it.from, seq, items, units, abort_flag);
+      ok = tc_mma<HD, F>(base, tmem, it.rows > 128 ? 2 : 1, it.until - it.from, seq, items, units, abort_flag);
     if (!ok) gave_up();
     if (leader) umma_commit(drain);  // every MMA issued here completes before the end
     __syncwarp();
@@ -383,6 +415,10 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
           if (128 * t + rb < it.rows)
             x[i] = *reinterpret_cast<const uint4*>(a.q + (it.row0 + tk) * a.q_stride + (int64_t)(it.g * rep + q - tk * rep) * HD + 8 * c);
         }
+#pragma unroll
+        for (int i = 0; F == KV_Q4 && i < LOADS; ++i)  // (as 4-bit codes are widened)
+          x[i] = make_uint4(__byte_perm(x[i].x, x[i].z, 0x5410), __byte_perm(x[i].x, x[i].z, 0x7632),
+                            __byte_perm(x[i].y, x[i].w, 0x5410), __byte_perm(x[i].y, x[i].w, 0x7632));
 #pragma unroll
         for (int i = 0; i < LOADS; ++i)
           st_shared_v4(base + t * C::TILE + (uint32_t)(c >> 3) * TC_BOX + swz(32 * quarter + RPL * i + lane / CPR, c & 7),
@@ -505,7 +541,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
           if (!live) continue;
 #pragma unroll
           for (int i = 0; i < 32; i += 4) {
-            const float4 x = make_float4(f32(o[i]), f32(o[i + 1]), f32(o[i + 2]), f32(o[i + 3]));
+            const int b = i & ~7, h = i >> 2 & 1;
+            const float4 x = F == KV_Q4 ? make_float4(f32(o[b + h]), f32(o[b + h + 2]), f32(o[b + h + 4]), f32(o[b + h + 6]))
+                                        : make_float4(f32(o[i]), f32(o[i + 1]), f32(o[i + 2]), f32(o[i + 3]));
             if (it.whole())
               finish4<HD>(a, mine, 32 * c + i, x);
             else
@@ -552,11 +590,11 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
   }
 }
 
-template <int HD, bool FP8>
+template <int HD, KvFormat F>
 cudaError_t launch_as(const KvPool& kv, const KvAttn& a, const KaScratch& s, int ctas, int* err, cudaStream_t stream) {
-  using C = TcCfg<HD, FP8>;
+  using C = TcCfg<HD, F>;
   static_assert((size_t)2 * TC_ROWS * (HD + 4) * 4 <= KV_ATTN_TC_PART_BYTES, "scratch per CTA");
-  auto kern = kv_attention_tc_kernel<HD, FP8>;
+  auto kern = kv_attention_tc_kernel<HD, F>;
   static const cudaError_t set = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM);
   if (set != cudaSuccess) return set;
   kern<<<ctas, TC_THREADS, C::SMEM, stream>>>(kv, a, s, err);
@@ -570,9 +608,13 @@ size_t kv_attention_tc_scratch(int sms) { return KV_ATTN_COUNTERS + (size_t)std:
 cudaError_t kv_attention_tc_launch(const KvPool& kv, const KvAttn& a, void* scratch, int sms, int* err, cudaStream_t stream) {
   sms = std::min(sms, 152);
   KaScratch s{reinterpret_cast<float*>(static_cast<uint8_t*>(scratch) + KV_ATTN_COUNTERS), static_cast<int*>(scratch)};
-  const bool fp8 = kv.format == KV_FP8;
-  if (kv.hd == 128) return fp8 ? launch_as<128, true>(kv, a, s, sms, err, stream) : launch_as<128, false>(kv, a, s, sms, err, stream);
-  return fp8 ? launch_as<64, true>(kv, a, s, sms, err, stream) : launch_as<64, false>(kv, a, s, sms, err, stream);
+  auto as = [&](auto hd) {
+    constexpr int HD = decltype(hd)::value;
+    if (kv.format == KV_Q4) return launch_as<HD, KV_Q4>(kv, a, s, sms, err, stream);
+    if (kv.format == KV_FP8) return launch_as<HD, KV_FP8>(kv, a, s, sms, err, stream);
+    return launch_as<HD, KV_BF16>(kv, a, s, sms, err, stream);
+  };
+  return kv.hd == 128 ? as(std::integral_constant<int, 128>{}) : as(std::integral_constant<int, 64>{});
 }
 
 }  // namespace dcl
