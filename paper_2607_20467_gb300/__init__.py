@@ -236,6 +236,26 @@ def _dev_rows(t, name, kind, rows, cols):
     return t.data_ptr(), stride[0]
 
 
+_bf16_types = _fits["bf16"]
+_i32_types = _fits["i32"]
+
+
+def _dev_heads(t, name, n, heads, hd):
+    """_dev_rows of n rows [heads][hd] in bf16: the usual layout at once (a call's host time is several such looks)."""
+    if t.dtype in _bf16_types and t.is_cuda and t.shape == (n, heads, hd):
+        s0, s1, s2 = t.stride()
+        if s2 == 1 and s1 == hd and (s0 >= heads * hd or n == 1):
+            return t.data_ptr(), s0 if n > 1 else heads * hd
+    return _dev_rows(t, name, "bf16", n, heads * hd)
+
+
+def _dev_i32(t, name, count):
+    """_dev_of an int32 vector of `count` elements: the usual one at once."""
+    if t is not None and not isinstance(t, int) and t.dtype in _i32_types and t.is_cuda and t.numel() >= count and t.is_contiguous():
+        return t.data_ptr()
+    return _dev_of(t, name, "i32", count)
+
+
 class KvCache:
     """A paged key / value cache of one layer in the caller's tensors (dcl_kv_cache): k, v
     [pages][kv heads][page_len][head_dim], bf16, or 1-byte E4M3 codes with k_exp, v_exp int8
@@ -490,23 +510,23 @@ class Context:
     def kv_write(self, cache, k, v, slots):
         """Store rows k, v [n][kv heads][head_dim] (bf16, rows may be strided) at slots (int32 [n],
         negative: skipped)."""
-        n, cols = k.shape[0], cache.row
-        kp, ks = _dev_rows(k, "k", "bf16", n, cols)
-        vp, vs = _dev_rows(v, "v", "bf16", n, cols)
+        n, heads, hd = k.shape[0], cache.n_kv_heads, cache.head_dim
+        kp, ks = _dev_heads(k, "k", n, heads, hd)
+        vp, vs = _dev_heads(v, "v", n, heads, hd)
         if ks != vs and n > 1:
             raise ValueError("k and v differ in row stride")
-        st = self._L.dcl_kv_write(self.ptr, cache.ptr, kp, vp, ks, _dev_of(slots, "slots", "i32", n), n)
+        st = self._L.dcl_kv_write(self.ptr, cache.ptr, kp, vp, ks, _dev_i32(slots, "slots", n), n)
         if st:
             self._check(st)
 
     def kv_read(self, cache, slots, k, v):
         """Read the positions at slots (int32 [n], negative: zeros) into k, v [n][kv heads][head_dim]."""
-        n, cols = slots.shape[0], cache.row
-        kp, ks = _dev_rows(k, "k", "bf16", n, cols)
-        vp, vs = _dev_rows(v, "v", "bf16", n, cols)
+        n, heads, hd = slots.shape[0], cache.n_kv_heads, cache.head_dim
+        kp, ks = _dev_heads(k, "k", n, heads, hd)
+        vp, vs = _dev_heads(v, "v", n, heads, hd)
         if ks != vs and n > 1:
             raise ValueError("k and v differ in row stride")
-        st = self._L.dcl_kv_read(self.ptr, cache.ptr, _dev_of(slots, "slots", "i32", n), n, kp, vp, ks)
+        st = self._L.dcl_kv_read(self.ptr, cache.ptr, _dev_i32(slots, "slots", n), n, kp, vp, ks)
         if st:
             self._check(st)
 
@@ -518,21 +538,22 @@ class Context:
         batch, max_pages = page_table.shape
         if hd != cache.head_dim:
             raise ValueError(f"q: head_dim {cache.head_dim} expected, got {hd}")
-        qp, qs = _dev_rows(q, "q", "bf16", n_q, heads * hd)
-        self._check(self._L.dcl_kv_attention(
-            self.ptr, cache.ptr, qp, qs, _dev_of(q_start, "q_start", "i32", batch + 1),
-            _dev_of(page_table, "page_table", "i32"), max_pages, _dev_of(seq_len, "seq_len", "i32", batch), batch, n_q,
-            max_new, heads, int(bool(causal)), scale, _dev_of(out, "out", "bf16", n_q * heads * hd),
-            _dev_of(lse, "lse", "f32", n_q * heads)))
+        qp, qs = _dev_heads(q, "q", n_q, heads, hd)
+        st = self._L.dcl_kv_attention(
+            self.ptr, cache.ptr, qp, qs, _dev_i32(q_start, "q_start", batch + 1), _dev_i32(page_table, "page_table", 0),
+            max_pages, _dev_i32(seq_len, "seq_len", batch), batch, n_q, max_new, heads, 1 if causal else 0, scale,
+            _dev_of(out, "out", "bf16", n_q * heads * hd), _dev_of(lse, "lse", "f32", n_q * heads))
+        if st:
+            self._check(st)
 
     def kv_plan(self, pages, start, new, q_start, seq_len, slots, pos):
         """Lay out a step: sequence b keeps start[b] cached positions and gets new[b] rows (int32 [batch]).
         Moves pages between the sequences and the stack; writes q_start [batch + 1], seq_len [batch], and
         slots, pos [rows] (-1 past the last sequence's)."""
         B, rows = pages.batch, slots.shape[0]
-        st = self._L.dcl_kv_plan(self.ptr, pages.ptr, _dev_of(start, "start", "i32", B), _dev_of(new, "new", "i32", B),
-                                 _dev_of(q_start, "q_start", "i32", B + 1), _dev_of(seq_len, "seq_len", "i32", B),
-                                 _dev_of(slots, "slots", "i32", rows), _dev_of(pos, "pos", "i32", rows), rows)
+        st = self._L.dcl_kv_plan(self.ptr, pages.ptr, _dev_i32(start, "start", B), _dev_i32(new, "new", B),
+                                 _dev_i32(q_start, "q_start", B + 1), _dev_i32(seq_len, "seq_len", B),
+                                 _dev_i32(slots, "slots", rows), _dev_i32(pos, "pos", rows), rows)
         if st:
             self._check(st)
 
@@ -542,11 +563,11 @@ class Context:
         into q_out, k_out (as q, k, or these themselves)."""
         n, H, hd = q.shape
         G = k.shape[1]
-        qp, qs = _dev_rows(q, "q", "bf16", n, H * hd)
-        kp, ks = _dev_rows(k, "k", "bf16", n, G * hd)
-        qo, qos = (qp, qs) if q_out is q else _dev_rows(q_out, "q_out", "bf16", n, H * hd)
-        ko, kos = (kp, ks) if k_out is k else _dev_rows(k_out, "k_out", "bf16", n, G * hd)
-        st = self._L.dcl_qk_norm_rope(self.ptr, qp, qs, kp, ks, _dev_of(pos, "pos", "i32", n), n, H, G, hd,
+        qp, qs = _dev_heads(q, "q", n, H, hd)
+        kp, ks = _dev_heads(k, "k", n, G, hd)
+        qo, qos = (qp, qs) if q_out is q else _dev_heads(q_out, "q_out", n, H, hd)
+        ko, kos = (kp, ks) if k_out is k else _dev_heads(k_out, "k_out", n, G, hd)
+        st = self._L.dcl_qk_norm_rope(self.ptr, qp, qs, kp, ks, _dev_i32(pos, "pos", n), n, H, G, hd,
                                       hd if rot_dim is None else rot_dim, theta, _dev_of(q_gain, "q_gain", "bf16", hd),
                                       _dev_of(k_gain, "k_gain", "bf16", hd), eps, qo, qos, ko, kos)
         if st:
