@@ -104,20 +104,16 @@ __device__ __forceinline__ uint4 quantise(KvBf16& a, int& e) {
   return make_uint4(out[0], out[1], out[2], out[3]);
 }
 
-// 1 / d for d = 4 .. 7 in two parts: the first has 16 bits, so that a bf16 value times it is exact, and
-// value / d comes out of one fused multiply-add with its one rounding.  (A quotient of 8 bits by 3 that
-// is not halfway between whole numbers is far from there; one that is stays exactly there.)
-struct Q4Over {
-  float hi, lo;
-  __device__ explicit Q4Over(int d) {
-    const float r = __fdividef(1.f, (float)d);
-    hi = __uint_as_float(__float_as_uint(r) & 0xffffff00u);
-    lo = fmaf(-hi, (float)d, 1.f) * r;
-  }
-};
-
 // Codes (16 of 4 bits) and the scale byte of a part's group, which two neighbouring threads share; all
 // threads of a warp call it.
+//
+// The quotient by d = 4 .. 7 has to come out with one rounding, for the sake of ties: 1 / d in two parts,
+// the first of 16 bits, so that a bf16 value times it is exact and one fused multiply-add does the rest.  (A
+// quotient of 8 bits by 3 that is not halfway between whole numbers is far from there; one that is stays
+// exactly there.)  Adding 1.5 2^23 + 8 rounds it to a whole number, 8 above, in the low bits; eight of them
+// are put together by multiplying and adding, where what stands above their four bits comes to a constant.
+// Five instructions a component: with a look at each code by itself, its limits and its four bits, there were
+// ten, and 12288 positions of 32 heads x 128 took 55 us.
 __device__ __forceinline__ uint2 quantise_q4(KvBf16& a, uint32_t& scale) {
   uint32_t m = 0;
 #pragma unroll
@@ -127,22 +123,31 @@ __device__ __forceinline__ uint2 quantise_q4(KvBf16& a, uint32_t& scale) {
   // The largest is f 2^x, f = 128 .. 255.  7 (4 + i) 2^k, the largest a scale reaches, passes 128 2^x,
   // 140 2^x, ... in turn: 35, 42, 49 at k = x + 2, then 28 and 35 at x + 3.  Bytes count through them.
   const int x = (int)(m >> 7) - 134, f = (int)(m & 0x7fu) + 128;
-  const int b = min(Q4_SCALES - 1, max(0, 4 * (x + 42) + 1 + (f > 140) + (f > 168) + (f > 196) + (f > 224)));
+  const int fits = 4 * (x + 42) + 1 + (f > 140) + (f > 168) + (f > 196) + (f > 224), b = min(Q4_SCALES - 1, max(0, fits));
   scale = m >= 0x7f80u ? Q4_NONE : (uint32_t)b;
-  const Q4Over over(4 + (b & 3));
-  const float down = __int_as_float((127 + 40 - (b >> 2)) << 23);
-  uint32_t out[2] = {0, 0};
   if (m >= 0x7f80u) return make_uint2(0x88888888u, 0x88888888u);
+  const float d = (float)(4 + (b & 3)), r = __fdividef(1.f, d), down = __int_as_float((127 + 40 - (b >> 2)) << 23);
+  const float hi = __uint_as_float(__float_as_uint(r) & 0xffffff00u);
+  const float lo = fmaf(-hi, d, 1.f) * r * down, high = hi * down;
+  constexpr float ROUND = 12582920.f;                 // 1.5 2^23 + 8, bits 0x4b400008
+  constexpr uint32_t ABOVE = 0x4b400000u * 0x11111111u;  // (what the sums of eight have too much)
+  uint32_t out[2];
+  auto codes = [&](auto limit) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t w = a.word(i);
-    // (a value above 7 times the largest scale: 7 of them; 8 added, and rounded, by 1.5 2^23)
-    auto code = [&](float v) {
-      const float y = fminf(7.f, fmaxf(-7.f, fmaf(v, over.lo, v * over.hi)));
-      return (__float_as_uint(y + 12582920.f)) & 15u;
-    };
-    out[i >> 2] |= (code(bf16_lo(w) * down) | code(bf16_hi(w) * down) << 4) << (8 * (i & 3));
-  }
+    for (int i = 0; i < 2; ++i) {
+      uint32_t w = 0;
+#pragma unroll
+      for (int j = 3; j >= 0; --j) {
+        const uint32_t two = a.word(4 * i + j);
+        auto code = [&](float v) { return __float_as_uint(limit(fmaf(v, lo, v * high)) + ROUND); };
+        w = w * 16u + code(bf16_hi(two));
+        w = w * 16u + code(bf16_lo(two));
+      }
+      out[i] = w - ABOVE;
+    }
+  };
+  if (fits <= Q4_SCALES - 1) codes([](float y) { return y; });
+  else codes([](float y) { return fminf(7.f, fmaxf(-7.f, y)); });  // (past the largest scale)
   return make_uint2(out[0], out[1]);
 }
 
