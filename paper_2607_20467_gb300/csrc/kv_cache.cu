@@ -23,7 +23,7 @@
 namespace dcl {
 namespace {
 
-constexpr int KV_THREADS = 256;
+constexpr int KV_THREADS = 64;
 constexpr int KV_EACH = 2;   // parts of a vector that a thread has in flight
 constexpr int KV_COMP = 16;  // components of a part
 
