@@ -1517,7 +1517,7 @@ dcl_status dcl_kv_attention(dcl_ctx* c, const dcl_kv_cache* cache, const void* q
     c->kv_scratch = scratch;
   }
   CUDA_TRY(c, kv_attention_many_rows(kv, a) ? kv_attention_tc_launch(kv, a, c->kv_scratch, c->num_sms, c->derr, c->stream)
-              : kv.format == KV_Q4        ? kv_attention_q4_launch(kv, a, c->kv_scratch, c->num_sms, c->derr, c->stream)
+              : kv_attention_q4_few(kv, a)    ? kv_attention_q4_launch(kv, a, c->kv_scratch, c->num_sms, c->derr, c->stream)
                                           : kv_attention_launch(kv, a, c->kv_scratch, c->num_sms, c->derr, c->stream));
   return DCL_OK;
 }

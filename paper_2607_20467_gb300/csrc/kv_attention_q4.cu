@@ -24,17 +24,16 @@
 namespace dcl {
 namespace {
 
-constexpr int K4_START = 3;   // units of keys that beginning an item takes
+constexpr int K4_START = 2;   // units of keys that beginning an item takes (64 ragged sequences: 3 33.9 us, 2 32.9, 4 34.7)
 constexpr int K4_CTAS = 2;    // CTAs of an SM: one loads while the other begins or ends an item
 constexpr int K4_MOST = 304;  // most CTAs of a launch
 constexpr int K4_KEYS = 32;   // keys that a warp takes at a time
 constexpr float K4_ABOVE = 32.f, K4_SLACK = 8.f;  // the reference above the largest score, and how far that may be passed
 
-// NT: tiles of 8 rows of an item.
-template <int HD, int NT>
+template <int HD>
 struct K4Cfg {
-  static constexpr int ROWS = 8 * NT;
-  static constexpr int WARPS = 8;
+  static constexpr int ROWS = 8;                     // of an item
+  static constexpr int WARPS = 8;                    // (as many as the registers allow)
   static constexpr int THREADS = 32 * WARPS;
   static constexpr int ROWB = HD / 2;                // bytes of a key
   static constexpr int SIDE = HD / Q4_GROUP;         // its scales
@@ -48,8 +47,7 @@ struct K4Cfg {
   static constexpr int RING_B = (std::max(RING, O_B) + 127) & ~127;
   static constexpr int ML = WARPS * RING_B;          // {m, l} [warp][ROWS]
   static constexpr int WT = ML + WARPS * ROWS * 8;  // weights of the warps' parts [ROWS][8], then {m, l} of the rows
-  static constexpr int QF = WT + ROWS * (8 * 4 + 8);  // NT > 1: q as operands [HD / 16][NT][lane] of 8 bytes
-  static constexpr int HEAD = QF + (NT > 1 ? HD / 16 * NT * 32 * 8 : 0);  // the walk's variables
+  static constexpr int HEAD = WT + ROWS * (8 * 4 + 8);  // the walk's variables
   static constexpr int TODO = HEAD + 48;             // joins left to this CTA: their number, and two at most
   static constexpr size_t SMEM = TODO + 3 * 24;
   static_assert(WARPS <= 8 && STAGES >= 2 && K4_CTAS * (SMEM + 1024) <= 233472, "shared memory of an SM");
@@ -81,62 +79,74 @@ __device__ __noinline__ bool any_without_numbers(uint32_t scales, int lane) {
   return __any_sync(0xffffffffu, any);
 }
 
-// The parts of an item, left by its CTAs, joined.  HD / 4 lanes have a row, a lane four of its components: it
-// copies those of many parts into shared memory (room for them, DEEP a thread) at once, as one takes about
-// 1000 cycles here; the weights come meanwhile, every lane those of every so many parts.
-template <int HD, int ROWS, int THREADS, int DEEP>
-__device__ __forceinline__ void join4(const KvAttn& a, const KaJoin& it, int rep, const float* parts, uint32_t room) {
+// The parts of an item, left by its CTAs, joined.  HD / 4 lanes have a row, a lane four of its components, which
+// it copies into shared memory a few parts at a time, the next ones on their way (one takes about 1000
+// cycles here); the parts' {m, l} and then their weights stand there, too.  (The lanes' weights exchanged by
+// shuffles, 25 parts at a time without others on their way: 11000 cycles for 38 parts.)
+template <int HD, int ROWS, int THREADS, int ROOM>
+__device__ __forceinline__ void join4(const KvAttn& a, const KaJoin& it, int rep, const float* parts, uint8_t* smem) {
   using Part = KaPart<HD, ROWS, false>;
-  constexpr int LPR = HD / 4;
-  const int l = threadIdx.x % LPR, n = it.parts, base_lane = (threadIdx.x & 31) / LPR * LPR;
+  constexpr int LPR = HD / 4, CHUNK = 10;
+  static_assert(THREADS / LPR >= ROWS, "a row for every so many threads");
+  static_assert(2 * CHUNK * 16 * THREADS + ROWS * K4_MOST * 8 <= ROOM, "shared memory of a join");
+  const int l = threadIdx.x % LPR, r = threadIdx.x / LPR, n = it.parts;
+  if (r / (32 / LPR) * (32 / LPR) >= it.rows) return;  // (whole warps)
+  const int rr = min(r, it.rows - 1);
   // (the first CTA's part is its second, the others' their first)
   const float* first = parts + (2 * (int64_t)it.c0 + 1) * Part::FLOATS;
-  auto part_of = [&](int c) { return first + (int64_t)max(2 * c - 1, 0) * Part::FLOATS; };
-  const uint32_t mine = room + 16 * threadIdx.x;
-  for (int r = threadIdx.x / LPR; r / (32 / LPR) * (32 / LPR) < it.rows; r += THREADS / LPR) {  // (whole warps)
-    const int rr = min(r, it.rows - 1);
-    auto ask = [&](int c0) {
-      const int m = min(n - c0, DEEP);
-      for (int i = 0; i < m; ++i) copy16(mine + 16 * THREADS * i, part_of(c0 + i) + Part::four(rr, l));
-      copy_commit();
-    };
-    ask(0);
-    auto ml_of = [&](int c) { return __ldcg(reinterpret_cast<const float2*>(part_of(c) + Part::ml(rr))); };
-    float2 x = ml_of(min(l, n - 1));
-    float top = x.x, sum = 0.f, w = 0.f;
-    for (int c = l + LPR; c < n; c += LPR) top = fmaxf(top, ml_of(c).x);
+  auto part_of = [&](int c) { return first + max(2 * c - 1, 0) * Part::FLOATS; };
+  const uint32_t mine = smem_addr(smem) + 16 * threadIdx.x;
+  float2* weights = reinterpret_cast<float2*>(smem + 2 * CHUNK * 16 * THREADS) + r * K4_MOST;
+  auto ask = [&](int c0) {
+    const uint32_t to = mine + (c0 / CHUNK & 1) * (CHUNK * 16 * THREADS);
 #pragma unroll
-    for (int d = LPR / 2; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int c0 = 0; c0 < n; c0 += DEEP) {
-      if (c0) ask(c0);
-      copy_wait<0>();
-      const int m = min(n - c0, DEEP);
-      for (int i = 0; i < m; ++i) {
-        const int c = c0 + i;
-        if (c % LPR == 0) {  // weights of the next LPR parts
-          if (c) x = ml_of(min(c + l, n - 1));
-          const float half = c + l < n ? part_half(x.x, top) : 0.f;
-          w = half * half;
-          sum = fmaf(x.y * half, half, sum);
-        }
-        const uint4 y = lds128(mine + 16 * THREADS * i);
-        add_scaled(acc, make_float4(__uint_as_float(y.x), __uint_as_float(y.y), __uint_as_float(y.z), __uint_as_float(y.w)),
-                   __shfl_sync(0xffffffffu, w, base_lane + c % LPR));
-      }
-    }
-#pragma unroll
-    for (int d = LPR / 2; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    if (r >= it.rows) continue;
-    const int tok = (it.first + r) / rep, at = (it.row0 + tok) * a.H + it.head0 + it.first + r - tok * rep;
-    if (a.lse && l == 0) a.lse[at] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
-    finish4<HD>(a, KaRow{sum == 0.f ? 0.f : 1.f / sum, at}, 4 * l, acc);
+    for (int i = 0; i < CHUNK; ++i)
+      if (c0 + i < n) copy16(to + 16 * THREADS * i, part_of(c0 + i) + Part::four(rr, l));
+    copy_commit();
+  };
+  ask(0);
+  ask(CHUNK);
+  float top = -INFINITY, sum = 0.f;
+#pragma unroll 2
+  for (int c = l; c < n; c += LPR) {
+    const float2 x = __ldcg(reinterpret_cast<const float2*>(part_of(c) + Part::ml(rr)));
+    weights[c] = x;
+    top = fmaxf(top, x.x);
   }
+#pragma unroll
+  for (int d = LPR / 2; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+  for (int c = l; c < n; c += LPR) {  // (what this lane wrote)
+    const float2 x = weights[c];
+    const float half = part_half(x.x, top);
+    weights[c].x = half * half;
+    sum = fmaf(x.y * half, half, sum);
+  }
+#pragma unroll
+  for (int d = LPR / 2; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+  __syncwarp();
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int c0 = 0; c0 < n; c0 += CHUNK) {
+    copy_wait<1>();
+    const uint32_t from = mine + (c0 / CHUNK & 1) * (CHUNK * 16 * THREADS);
+#pragma unroll
+    for (int i = 0; i < CHUNK; ++i) {
+      if (c0 + i >= n) break;
+      const uint4 y = lds128(from + 16 * THREADS * i);
+      add_scaled(acc, make_float4(__uint_as_float(y.x), __uint_as_float(y.y), __uint_as_float(y.z), __uint_as_float(y.w)), weights[c0 + i].x);
+    }
+    ask(c0 + 2 * CHUNK);
+  }
+  copy_wait<0>();
+  __syncwarp();  // (the weights' places are free again)
+  if (r >= it.rows) return;
+  const int tok = (it.first + r) / rep, at = (it.row0 + tok) * a.H + it.head0 + it.first + r - tok * rep;
+  if (a.lse && l == 0) a.lse[at] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+  finish4<HD>(a, KaRow{sum == 0.f ? 0.f : 1.f / sum, at}, 4 * l, acc);
 }
 
-template <int HD, int NT>
-__global__ void __launch_bounds__(K4Cfg<HD, NT>::THREADS, K4_CTAS) kv_attention_q4_kernel(KvPool kv, KvAttn a, KaScratch scratch, int* err) {
-  using C = K4Cfg<HD, NT>;
+template <int HD>
+__global__ void __launch_bounds__(K4Cfg<HD>::THREADS, K4_CTAS) kv_attention_q4_kernel(KvPool kv, KvAttn a, KaScratch scratch, int* err) {
+  using C = K4Cfg<HD>;
   constexpr int ROWS = C::ROWS, KT = K4_KEYS, SIDE = C::SIDE, ROWB = C::ROWB, CPR = ROWB / 16;
   constexpr int KS = HD / 16;   // k steps of S
   constexpr int MT = HD / 16;   // tiles of 16 components of O
@@ -182,16 +192,14 @@ __global__ void __launch_bounds__(K4Cfg<HD, NT>::THREADS, K4_CTAS) kv_attention_
     const int lim_min = a.causal ? it.len - it.nq + it.first / rep + 1 : it.len;
     const int lim_max = a.causal ? min(it.len, it.len - it.nq + (it.first + it.rows - 1) / rep + 1) : it.len;
 
-    // ---- q of rows quad (and 8 on), this lane's quarter of its components; asked for before the keys, which would
-    // be in the way
+    // ---- q of row quad, this lane's quarter of its components; asked for before the keys, which would be in the way
     uint4 raw[HD / 32];
-    auto ask_q = [&](int r) {
-      const int rr = it.first + r, tok = rr / rep, h = it.g * rep + rr - tok * rep;
+    {
+      const int rr = it.first + quad, tok = rr / rep, h = it.g * rep + rr - tok * rep;
       const __nv_bfloat16* src = a.q + (it.row0 + tok) * a.q_stride + (int64_t)h * HD + place * (HD / 4);
 #pragma unroll
-      for (int c = 0; c < HD / 32; ++c) raw[c] = r < it.rows ? *reinterpret_cast<const uint4*>(src + 8 * c) : make_uint4(0, 0, 0, 0);
-    };
-    if (NT == 1 || warp < NT) ask_q(8 * (NT == 1 ? 0 : warp) + quad);
+      for (int c = 0; c < HD / 32; ++c) raw[c] = quad < it.rows ? *reinterpret_cast<const uint4*>(src + 8 * c) : make_uint4(0, 0, 0, 0);
+    }
 
     const uint32_t head_at = (uint32_t)(it.g * P * ROWB);
     // ---- this warp's steps: keys key0 + KT warp on, then every WARPS-th
@@ -250,41 +258,29 @@ __global__ void __launch_bounds__(K4Cfg<HD, NT>::THREADS, K4_CTAS) kv_attention_
 #pragma unroll
     for (int s = 0; s < C::STAGES - 1; ++s) issue();
 
-    // q as the product's operand: of 8 components 0 and 4, 1 and 5, then 2 and 6, 3 and 7, as codes are widened; in
-    // registers, or where there are more tiles of rows in shared memory, a tile by a warp
-    uint32_t q[NT == 1 ? KS : 1][2];
-    const uint32_t q_at = smem_addr(smem) + C::QF + 8 * lane;
+    // q as the product's operand: of 8 components 0 and 4, 1 and 5, then 2 and 6, 3 and 7, as codes are widened
+    uint32_t q[KS][2];
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
       const uint32_t* w = &raw[s >> 1].x + (s & 1);
-      const uint32_t q0 = __byte_perm(w[0], w[2], 0x5410), q1 = __byte_perm(w[0], w[2], 0x7632);
-      if (NT == 1) {
-        q[NT == 1 ? s : 0][0] = q0;
-        q[NT == 1 ? s : 0][1] = q1;
-      } else if (warp < NT) {
-        *reinterpret_cast<uint2*>(smem + C::QF + ((s * NT + warp) * 32 + lane) * 8) = make_uint2(q0, q1);
-      }
+      q[s][0] = __byte_perm(w[0], w[2], 0x5410);
+      q[s][1] = __byte_perm(w[0], w[2], 0x7632);
     }
-    if (NT > 1) __syncthreads();
 
-    // ---- rows 2 place and 2 place + 1 of a tile are this lane's in S^T and O^T
-    int lim[NT][2];  // keys each sees
-    float o[MT][NT][4], m[NT][2], l[NT][2];
+    // ---- rows 2 place and 2 place + 1 are this lane's in S^T and O^T
+    int lim[2];  // keys each sees
+    float o[MT][4], m[2], l[2];
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int r = 8 * n + 2 * place + i;
-        lim[n][i] = r >= it.rows ? 0 : a.causal ? min(it.len, it.len - it.nq + (it.first + r) / rep + 1) : it.len;
-        m[n][i] = -INFINITY;
-        l[n][i] = 0.f;
-      }
+    for (int i = 0; i < 2; ++i) {
+      const int r = 2 * place + i;
+      lim[i] = r >= it.rows ? 0 : a.causal ? min(it.len, it.len - it.nq + (it.first + r) / rep + 1) : it.len;
+      m[i] = -INFINITY;
+      l[i] = 0.f;
+    }
 #pragma unroll
     for (int c = 0; c < MT; ++c)
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) o[c][n][j] = 0.f;
+      for (int j = 0; j < 4; ++j) o[c][j] = 0.f;
 
     uint32_t cur = 0;
     for (int key = key0 + KT * warp; key < stop; key += KT * C::WARPS) {
@@ -308,148 +304,126 @@ __global__ void __launch_bounds__(K4Cfg<HD, NT>::THREADS, K4_CTAS) kv_attention_
         for (int j = 0; j < KT; ++j) {
           if (lds_u8(se + (KT + j) * SIDE + v_group) < Q4_SCALES) continue;
 #pragma unroll
-          for (int n = 0; n < NT; ++n)
+          for (int i = 0; i < 2; ++i)
+            if (key + j < lim[i])
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-              if (key + j < lim[n][i])
-#pragma unroll
-                for (int c = 0; c < MT; ++c) o[c][n][i] = o[c][n][2 + i] = NAN;
+              for (int c = 0; c < MT; ++c) o[c][i] = o[c][2 + i] = NAN;
         }
         __syncwarp();
         for (int c = lane; c < KT * SIDE; c += 32)
           if (lds_u8(se + KT * SIDE + c) >= Q4_SCALES) sts8(se + KT * SIDE + c, 0);
         __syncwarp();
       }
-      constexpr int TT = NT == 1 ? KT / 16 : 1;  // tiles of 16 keys at a time: as many as the registers allow
-#pragma unroll 1
-      for (int t0 = 0; t0 < KT / 16; t0 += TT) {
-        // ---- S^T = K q^T: tiles of 16 keys, this lane's are quad and quad + 8
-        float s[TT][NT][4];
+      // ---- S^T = K q^T: tiles of 16 keys, this lane's are quad and quad + 8
+      float s[KT / 16][4];
 #pragma unroll
-        for (int t = 0; t < TT; ++t) {
-          uint32_t w[2][2 * W];
-          Q4Scale f[2];
+      for (int t = 0; t < KT / 16; ++t) {
+        uint32_t w[2][2 * W];
+        Q4Scale f[2];
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const uint32_t at = sk + k_at + 16 * ROWB * (t0 + t) + EIGHT * i;
-            if (HD == 128) {
-              const uint4 x = lds128(at);
-              w[i][0] = x.x;
-              w[i][1] = x.y;
-              w[i][2 * W - 2] = x.z;
-              w[i][2 * W - 1] = x.w;
-            } else {
-              const uint2 x = lds64(at);
-              w[i][0] = x.x;
-              w[i][1] = x.y;
-            }
-            f[i] = q4_scale_twice(lds_u8(se + (16 * (t0 + t) + 8 * i + quad) * SIDE + k_group));
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t at = sk + k_at + 16 * ROWB * t + EIGHT * i;
+          if (HD == 128) {
+            const uint4 x = lds128(at);
+            w[i][0] = x.x;
+            w[i][1] = x.y;
+            w[i][2 * W - 2] = x.z;
+            w[i][2 * W - 1] = x.w;
+          } else {
+            const uint2 x = lds64(at);
+            w[i][0] = x.x;
+            w[i][1] = x.y;
           }
+          f[i] = q4_scale_twice(lds_u8(se + (16 * t + 8 * i + quad) * SIDE + k_group));
+        }
 #pragma unroll
-          for (int x = 0; x < KS; ++x) {
-            const int i = 2 * (x & 1);
-            const uint32_t a0 = q4_widen(w[0][x >> 1], i, f[0]), a1 = q4_widen(w[1][x >> 1], i, f[1]);
-            const uint32_t a2 = q4_widen(w[0][x >> 1], i + 1, f[0]), a3 = q4_widen(w[1][x >> 1], i + 1, f[1]);
+        for (int x = 0; x < KS; ++x) {
+          const int i = 2 * (x & 1);
+          const uint32_t a0 = q4_widen(w[0][x >> 1], i, f[0]), a1 = q4_widen(w[1][x >> 1], i, f[1]);
+          const uint32_t a2 = q4_widen(w[0][x >> 1], i + 1, f[0]), a3 = q4_widen(w[1][x >> 1], i + 1, f[1]);
+          if (x == 0) mma_bf16_first(s[t], a0, a1, a2, a3, q[x][0], q[x][1]);
+          else mma_bf16(s[t], a0, a1, a2, a3, q[x][0], q[x][1]);
+        }
+      }
+      if (masked) {
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-              const uint2 b = NT == 1 ? make_uint2(q[NT == 1 ? x : 0][0], q[NT == 1 ? x : 0][1]) : lds64(q_at + (x * NT + n) * 256);
-              if (x == 0) mma_bf16_first(s[t][n], a0, a1, a2, a3, b.x, b.y);
-              else mma_bf16(s[t][n], a0, a1, a2, a3, b.x, b.y);
-            }
+        for (int t = 0; t < KT / 16; ++t)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (key + 16 * t + quad + 8 * (j >> 1) >= lim[j & 1] || (skip >> t & 1)) s[t][j] = -INFINITY;
+      }
+      // ---- a larger reference where a row's largest score passes it too far, or is its first
+      float top[2];
+      bool grew = false;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float x = fmaxf(s[0][i], s[0][2 + i]);
+#pragma unroll
+        for (int t = 1; t < KT / 16; ++t) x = fmaxf(x, fmaxf(s[t][i], s[t][2 + i]));
+        top[i] = x * qa;
+        grew |= top[i] > m[i] - (K4_ABOVE - K4_SLACK);
+      }
+      if (__any_sync(0xffffffffu, grew)) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          float x = top[i];
+#pragma unroll
+          for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
+          const float mn = fmaxf(m[i], x + K4_ABOVE);
+          const float alpha = exp2_fast(m[i] - (mn == -INFINITY ? 0.f : mn));
+          m[i] = mn;
+          l[i] *= alpha;
+#pragma unroll
+          for (int c = 0; c < MT; ++c) {
+            o[c][i] *= alpha;
+            o[c][2 + i] *= alpha;
           }
         }
-        if (masked) {
+      }
+      // ---- P^T in two parts
+      uint32_t p[KT / 16][2], p_lo[KT / 16][2];
+      const float ref[2] = {m[0] == -INFINITY ? 0.f : m[0], m[1] == -INFINITY ? 0.f : m[1]};  // (nothing seen yet: exp2(-inf) = 0)
 #pragma unroll
-          for (int t = 0; t < TT; ++t)
+      for (int t = 0; t < KT / 16; ++t)
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-              for (int j = 0; j < 4; ++j)
-                if (key + 16 * (t0 + t) + quad + 8 * (j >> 1) >= lim[n][j & 1] || (skip >> (t0 + t) & 1)) s[t][n][j] = -INFINITY;
+        for (int i = 0; i < 2; ++i) {  // keys quad + 8 i
+          const float x0 = exp2_fast(fmaf(s[t][2 * i], qa, -ref[0])), x1 = exp2_fast(fmaf(s[t][2 * i + 1], qa, -ref[1]));
+          l[0] += x0;
+          l[1] += x1;
+          p[t][i] = transposed(upper_halves(x0, x1));
+          p_lo[t][i] = transposed(pack_bf16x2(fmaf(x0, BF16_LO, minus_upper(x0)), fmaf(x1, BF16_LO, minus_upper(x1))));
         }
-        // ---- a larger reference where a row's largest score passes it too far, or is its first
-        float top[NT][2];
-        bool grew = false;
+      // ---- O^T += V^T P^T, 16 keys at a time; a lane's components are quad * HD / 8 on
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+      for (int t = 0; t < KT / 16; ++t) {
+        uint32_t v[4][W], scale[4];
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            float x = fmaxf(s[0][n][i], s[0][n][2 + i]);
-#pragma unroll
-            for (int t = 1; t < TT; ++t) x = fmaxf(x, fmaxf(s[t][n][i], s[t][n][2 + i]));
-            top[n][i] = x * qa;
-            grew |= top[n][i] > m[n][i] - (K4_ABOVE - K4_SLACK);
+        for (int r = 0; r < 4; ++r) {  // keys 2 place, 2 place + 1, and 8 on
+          const uint32_t at = sv + v_at[r & 1] + 16 * ROWB * t + EIGHT * (r >> 1);
+          if (W == 2) {
+            const uint2 x = lds64(at);
+            v[r][0] = x.x;
+            v[r][W - 1] = x.y;
+          } else {
+            v[r][0] = lds32(at);
           }
-        if (__any_sync(0xffffffffu, grew)) {
-#pragma unroll
-          for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              float x = top[n][i];
-#pragma unroll
-              for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
-              const float mn = fmaxf(m[n][i], x + K4_ABOVE);
-              const float alpha = exp2_fast(m[n][i] - (mn == -INFINITY ? 0.f : mn));
-              m[n][i] = mn;
-              l[n][i] *= alpha;
-#pragma unroll
-              for (int c = 0; c < MT; ++c) {
-                o[c][n][i] *= alpha;
-                o[c][n][2 + i] *= alpha;
-              }
-            }
+          scale[r] = lds_u8(se + (KT + 16 * t + 2 * place + (r & 1) + 8 * (r >> 1)) * SIDE + v_group);
         }
-        // ---- P^T in two parts
-        uint32_t p[TT][NT][2], p_lo[TT][NT][2];
+        const Q4Scale f0 = q4_scale(scale[0] + (scale[1] << 16)), f1 = q4_scale(scale[2] + (scale[3] << 16));
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          const float ref[2] = {m[n][0] == -INFINITY ? 0.f : m[n][0], m[n][1] == -INFINITY ? 0.f : m[n][1]};  // (nothing seen yet: exp2(-inf) = 0)
+        for (int w = 0; w < W; ++w)
 #pragma unroll
-          for (int t = 0; t < TT; ++t)
+          for (int up = 0; up < 2; ++up) {  // a word's lower four components, its upper four; two keys side by side
+            const uint32_t x0 = __byte_perm(v[0][w], v[1][w], up ? 0x7632 : 0x5410);
+            const uint32_t x1 = __byte_perm(v[2][w], v[3][w], up ? 0x7632 : 0x5410);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {  // keys quad + 8 i
-              const float x0 = exp2_fast(fmaf(s[t][n][2 * i], qa, -ref[0])), x1 = exp2_fast(fmaf(s[t][n][2 * i + 1], qa, -ref[1]));
-              l[n][0] += x0;
-              l[n][1] += x1;
-              p[t][n][i] = transposed(upper_halves(x0, x1));
-              p_lo[t][n][i] = transposed(pack_bf16x2(fmaf(x0, BF16_LO, minus_upper(x0)), fmaf(x1, BF16_LO, minus_upper(x1))));
+            for (int j = 0; j < 4; j += 2) {
+              float(&acc)[4] = o[4 * w + 2 * up + j / 2];
+              const uint32_t a0 = q4_widen(x0, j, f0), a1 = q4_widen(x0, j + 1, f0), a2 = q4_widen(x1, j, f1), a3 = q4_widen(x1, j + 1, f1);
+              mma_bf16(acc, a0, a1, a2, a3, p[t][0], p[t][1]);
+              mma_bf16(acc, a0, a1, a2, a3, p_lo[t][0], p_lo[t][1]);
             }
-        }
-        // ---- O^T += V^T P^T, 16 keys at a time; a lane's components are quad * HD / 8 on
-#pragma unroll
-        for (int t = 0; t < TT; ++t) {
-          uint32_t v[4][W], scale[4];
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {  // keys 2 place, 2 place + 1, and 8 on
-            const uint32_t at = sv + v_at[r & 1] + 16 * ROWB * (t0 + t) + EIGHT * (r >> 1);
-            if (W == 2) {
-              const uint2 x = lds64(at);
-              v[r][0] = x.x;
-              v[r][W - 1] = x.y;
-            } else {
-              v[r][0] = lds32(at);
-            }
-            scale[r] = lds_u8(se + (KT + 16 * (t0 + t) + 2 * place + (r & 1) + 8 * (r >> 1)) * SIDE + v_group);
           }
-          const Q4Scale f0 = q4_scale(scale[0] + (scale[1] << 16)), f1 = q4_scale(scale[2] + (scale[3] << 16));
-#pragma unroll
-          for (int w = 0; w < W; ++w)
-#pragma unroll
-            for (int up = 0; up < 2; ++up) {  // a word's lower four components, its upper four; two keys side by side
-              const uint32_t x0 = __byte_perm(v[0][w], v[1][w], up ? 0x7632 : 0x5410);
-              const uint32_t x1 = __byte_perm(v[2][w], v[3][w], up ? 0x7632 : 0x5410);
-#pragma unroll
-              for (int j = 0; j < 4; j += 2) {
-                const uint32_t a0 = q4_widen(x0, j, f0), a1 = q4_widen(x0, j + 1, f0), a2 = q4_widen(x1, j, f1), a3 = q4_widen(x1, j + 1, f1);
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                  float(&acc)[4] = o[4 * w + 2 * up + j / 2][n];
-                  mma_bf16(acc, a0, a1, a2, a3, p[t][n][0], p[t][n][1]);
-                  mma_bf16(acc, a0, a1, a2, a3, p_lo[t][n][0], p_lo[t][n][1]);
-                }
-              }
-            }
-        }
       }
       __syncwarp();
     }
@@ -460,18 +434,16 @@ __global__ void __launch_bounds__(K4Cfg<HD, NT>::THREADS, K4_CTAS) kv_attention_
     constexpr int RUN = HD / 8;  // components of a lane
     float* mine = reinterpret_cast<float*>(smem + warp * C::RING_B) + quad * (RUN + 4);
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+    for (int i = 0; i < 2; ++i) {
+      const int r = 2 * place + i;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int r = 8 * n + 2 * place + i;
+      for (int d = 4; d < 32; d <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], d);
+      if (quad == 0) ml[warp * ROWS + r] = make_float2(m[i], l[i]);
+      if (key0 + KT * warp < stop)
 #pragma unroll
-        for (int d = 4; d < 32; d <<= 1) l[n][i] += __shfl_xor_sync(0xffffffffu, l[n][i], d);
-        if (quad == 0) ml[warp * ROWS + r] = make_float2(m[n][i], l[n][i]);
-        if (key0 + KT * warp < stop)
-#pragma unroll
-          for (int c = 0; c < MT; c += 2)
-            *reinterpret_cast<float4*>(mine + r * C::O_PITCH + 2 * c) = make_float4(o[c][n][i], o[c][n][2 + i], o[c + 1][n][i], o[c + 1][n][2 + i]);
-      }
+        for (int c = 0; c < MT; c += 2)
+          *reinterpret_cast<float4*>(mine + r * C::O_PITCH + 2 * c) = make_float4(o[c][i], o[c][2 + i], o[c + 1][i], o[c + 1][2 + i]);
+    }
     __syncthreads();
     // a row's weights by a thread, then four components of a row a thread
     float* wt = reinterpret_cast<float*>(smem + C::WT);
@@ -529,14 +501,14 @@ __global__ void __launch_bounds__(K4Cfg<HD, NT>::THREADS, K4_CTAS) kv_attention_
     }
   }
   __syncthreads();
-  for (int i = 0; i < todo[0].rows; ++i) join4<HD, ROWS, C::THREADS, C::ML / (16 * C::THREADS)>(a, todo[1 + i], rep, scratch.part, smem_addr(smem));
+  for (int i = 0; i < todo[0].rows; ++i) join4<HD, ROWS, C::THREADS, C::ML>(a, todo[1 + i], rep, scratch.part, smem);
 }
 
-template <int HD, int NT>
+template <int HD>
 cudaError_t launch_as(const KvPool& kv, const KvAttn& a, const KaScratch& s, int ctas, int* err, cudaStream_t stream) {
-  using C = K4Cfg<HD, NT>;
+  using C = K4Cfg<HD>;
   static_assert(2 * C::ROWS * (HD + 4) * 4 <= KV_ATTN_PART_BYTES && K4_MOST * sizeof(int) <= KV_ATTN_COUNTERS, "scratch");
-  auto kern = kv_attention_q4_kernel<HD, NT>;
+  auto kern = kv_attention_q4_kernel<HD>;
   static const cudaError_t set = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM);
   if (set != cudaSuccess) return set;
   kern<<<ctas, C::THREADS, C::SMEM, stream>>>(kv, a, s, err);
@@ -545,12 +517,12 @@ cudaError_t launch_as(const KvPool& kv, const KvAttn& a, const KaScratch& s, int
 
 }  // namespace
 
+bool kv_attention_q4_few(const KvPool& kv, const KvAttn& a) { return kv.format == KV_Q4 && (int64_t)a.max_new * (a.H / kv.G) <= 8; }
+
 cudaError_t kv_attention_q4_launch(const KvPool& kv, const KvAttn& a, void* scratch, int sms, int* err, cudaStream_t stream) {
   const int ctas = K4_CTAS * std::min(sms, K4_MOST / K4_CTAS);
   KaScratch s{reinterpret_cast<float*>(static_cast<uint8_t*>(scratch) + KV_ATTN_COUNTERS), static_cast<int*>(scratch)};
-  const bool few = (int64_t)a.max_new * (a.H / kv.G) <= 8;
-  if (kv.hd == 128) return few ? launch_as<128, 1>(kv, a, s, ctas, err, stream) : launch_as<128, 2>(kv, a, s, ctas, err, stream);
-  return few ? launch_as<64, 1>(kv, a, s, ctas, err, stream) : launch_as<64, 2>(kv, a, s, ctas, err, stream);
+  return kv.hd == 128 ? launch_as<128>(kv, a, s, ctas, err, stream) : launch_as<64>(kv, a, s, ctas, err, stream);
 }
 
 }  // namespace dcl

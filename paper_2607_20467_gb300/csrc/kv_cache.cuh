@@ -48,6 +48,7 @@ struct KvAttn {
 constexpr size_t KV_ATTN_COUNTERS = 4096;                                      // bytes (an int per CTA)
 constexpr size_t KV_ATTN_PART_BYTES = 2 * 32 * (128 + 4) * sizeof(float);      // per CTA
 constexpr size_t KV_ATTN_TC_PART_BYTES = 2 * 256 * (128 + 4) * sizeof(float);
+bool kv_attention_q4_few(const KvPool& kv, const KvAttn& a);
 cudaError_t kv_attention_q4_launch(const KvPool& kv, const KvAttn& a, void* scratch, int sms, int* err, cudaStream_t stream);
 bool kv_attention_many_rows(const KvPool& kv, const KvAttn& a);
 size_t kv_attention_scratch(int sms);
