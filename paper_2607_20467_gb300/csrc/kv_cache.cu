@@ -28,10 +28,14 @@ constexpr int KV_EACH = 2;   // parts of a vector that a thread has in flight
 constexpr int KV_COMP = 16;  // components of a part
 
 // A thread's parts: part `at` of the call's [row][k, v][kv head][HD / 16], in blocks of KV_THREADS *
-// KV_EACH.  per_row and its reciprocal (rounded up, exact for the few rows of a block) come from
-// the host: a 64-bit division per part took longer than the copy.
+// KV_EACH.  per_row and its reciprocals (rounded up: 2^32 of it, exact for the few rows of a block, and 2^64,
+// exact for all that a call has) come from the host: 64-bit divisions took longer than the copy.
 struct KvPart {
   int row, is_v, g, part;
+};
+struct KvOver {
+  uint64_t row64;
+  uint32_t row32;
 };
 template <int HD>
 struct KvWalk {
@@ -39,9 +43,9 @@ struct KvWalk {
   int64_t row0;
   uint32_t rest, per_row, inverse;
   int G;
-  __device__ KvWalk(int G_, uint32_t inverse_) : per_row(2 * G_ * TPV), inverse(inverse_), G(G_) {
-    const int64_t start = (int64_t)blockIdx.x * (KV_THREADS * KV_EACH);
-    row0 = start / per_row;
+  __device__ KvWalk(int G_, const KvOver& over) : per_row(2 * G_ * TPV), inverse(over.row32), G(G_) {
+    const uint64_t start = (uint64_t)blockIdx.x * (KV_THREADS * KV_EACH);
+    row0 = (int64_t)__umul64hi(start, over.row64);
     rest = (uint32_t)(start - row0 * per_row);
   }
   __device__ __forceinline__ KvPart at(int i) const {
@@ -107,13 +111,14 @@ __device__ __forceinline__ uint4 quantise(KvBf16& a, int& e) {
 // Codes (16 of 4 bits) and the scale byte of a part's group, which two neighbouring threads share; all
 // threads of a warp call it.
 //
-// The quotient by d = 4 .. 7 has to come out with one rounding, for the sake of ties: 1 / d in two parts,
-// the first of 16 bits, so that a bf16 value times it is exact and one fused multiply-add does the rest.  (A
-// quotient of 8 bits by 3 that is not halfway between whole numbers is far from there; one that is stays
-// exactly there.)  Adding 1.5 2^23 + 8 rounds it to a whole number, 8 above, in the low bits; eight of them
-// are put together by multiplying and adding, where what stands above their four bits comes to a constant.
-// Five instructions a component: with a look at each code by itself, its limits and its four bits, there were
-// ten, and 12288 positions of 32 heads x 128 took 55 us.
+// The quotient by d = 4 .. 7 times a power of two comes out in fp32 to 2^-24 of itself and is rounded to fp16,
+// which puts ties right: half a whole number is an fp16 number and nearer than the next by 2^-12 of
+// itself at least; a quotient of 8 bits by 3 that is not halfway is off that by 1/128 of itself or more, eight
+// times fp16's step.  Adding 1.5 2^10 + 8 rounds it to a whole number, 8 above, in the low bits.  Two at a
+// time, components i and i + 4 of a word's eight, as their codes lie in it; pairs are put together by
+// multiplying and adding, where what stands above their four bits comes to a constant.  That is 3.5 instructions
+// a component: with each code rounded and cut out by itself there were ten, and 12288 positions of 32 heads x
+// 128 took 55 us instead of 43.8.
 __device__ __forceinline__ uint2 quantise_q4(KvBf16& a, uint32_t& scale) {
   uint32_t m = 0;
 #pragma unroll
@@ -126,22 +131,20 @@ __device__ __forceinline__ uint2 quantise_q4(KvBf16& a, uint32_t& scale) {
   const int fits = 4 * (x + 42) + 1 + (f > 140) + (f > 168) + (f > 196) + (f > 224), b = min(Q4_SCALES - 1, max(0, fits));
   scale = m >= 0x7f80u ? Q4_NONE : (uint32_t)b;
   if (m >= 0x7f80u) return make_uint2(0x88888888u, 0x88888888u);
-  const float d = (float)(4 + (b & 3)), r = __fdividef(1.f, d), down = __int_as_float((127 + 40 - (b >> 2)) << 23);
-  const float hi = __uint_as_float(__float_as_uint(r) & 0xffffff00u);
-  const float lo = fmaf(-hi, d, 1.f) * r * down, high = hi * down;
-  constexpr float ROUND = 12582920.f;                 // 1.5 2^23 + 8, bits 0x4b400008
-  constexpr uint32_t ABOVE = 0x4b400000u * 0x11111111u;  // (what the sums of eight have too much)
+  const float over = __fdividef(1.f, (float)(4 + (b & 3))) * __int_as_float((127 + 40 - (b >> 2)) << 23);
+  const __half2 round = __halves2half2(__ushort_as_half(0x6608), __ushort_as_half(0x6608));  // 1.5 2^10 + 8
+  constexpr uint32_t ABOVE = 0x66006600u * 0x1111u;  // (what the sums of four have too much)
   uint32_t out[2];
   auto codes = [&](auto limit) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       uint32_t w = 0;
 #pragma unroll
-      for (int j = 3; j >= 0; --j) {
-        const uint32_t two = a.word(4 * i + j);
-        auto code = [&](float v) { return __float_as_uint(limit(fmaf(v, lo, v * high)) + ROUND); };
-        w = w * 16u + code(bf16_hi(two));
-        w = w * 16u + code(bf16_lo(two));
+      for (int j = 3; j >= 0; --j) {  // components j and j + 4
+        const uint32_t first = a.word(4 * i + j / 2), second = a.word(4 * i + 2 + j / 2);
+        const float v0 = j & 1 ? bf16_hi(first) : bf16_lo(first), v1 = j & 1 ? bf16_hi(second) : bf16_lo(second);
+        const __half2 y = __hadd2(__floats2half2_rn(limit(v0 * over), limit(v1 * over)), round);
+        w = w * 16u + *reinterpret_cast<const uint32_t*>(&y);
       }
       out[i] = w - ABOVE;
     }
@@ -154,9 +157,9 @@ __device__ __forceinline__ uint2 quantise_q4(KvBf16& a, uint32_t& scale) {
 template <int HD, KvFormat F>
 __global__ void __launch_bounds__(KV_THREADS) kv_write_kernel(KvPool kv, const __nv_bfloat16* __restrict__ k,
                                                               const __nv_bfloat16* __restrict__ v, int64_t stride,
-                                                              const int* __restrict__ slots, int n, uint32_t inverse,
+                                                              const int* __restrict__ slots, int n, KvOver over,
                                                               int* err) {
-  const KvWalk<HD> walk(kv.G, inverse);
+  const KvWalk<HD> walk(kv.G, over);
   constexpr int TPV = HD / KV_COMP;
   KvBf16 raw[KV_EACH];
   int slot[KV_EACH];
@@ -215,8 +218,8 @@ __global__ void __launch_bounds__(KV_THREADS) kv_write_kernel(KvPool kv, const _
 template <int HD, KvFormat F>
 __global__ void __launch_bounds__(KV_THREADS) kv_read_kernel(KvPool kv, const int* __restrict__ slots, int n,
                                                              __nv_bfloat16* __restrict__ k, __nv_bfloat16* __restrict__ v,
-                                                             int64_t stride, uint32_t inverse, int* err) {
-  const KvWalk<HD> walk(kv.G, inverse);
+                                                             int64_t stride, KvOver over, int* err) {
+  const KvWalk<HD> walk(kv.G, over);
   constexpr int TPV = HD / KV_COMP;
   int64_t vec[KV_EACH];  // -1: zeros
 #pragma unroll
@@ -282,12 +285,13 @@ __global__ void __launch_bounds__(KV_THREADS) kv_read_kernel(KvPool kv, const in
 
 // Blocks of a call, and the reciprocal of a row's parts for KvWalk: x / per_row is exact for the
 // x < per_row + KV_THREADS * KV_EACH that a block divides while x * per_row < 2^32.
-bool kv_grid(const KvPool& kv, int n, unsigned* grid, uint32_t* inverse) {
+bool kv_grid(const KvPool& kv, int n, unsigned* grid, KvOver* over) {
   const int64_t per_row = 2 * (int64_t)kv.G * (kv.hd / KV_COMP), per_block = KV_THREADS * KV_EACH;
   const int64_t blocks = (n * per_row + per_block - 1) / per_block;
   if (blocks > 0x7fffffff || (per_row + per_block) * per_row >= (1ll << 32)) return false;
   *grid = (unsigned)blocks;
-  *inverse = (uint32_t)(((1ll << 32) + per_row - 1) / per_row);
+  over->row32 = (uint32_t)(((1ll << 32) + per_row - 1) / per_row);
+  over->row64 = ~0ull / (uint64_t)per_row + 1;  // (x * per_row < 2^64 for the x < 2^38 of a grid)
   return true;
 }
 
@@ -309,20 +313,20 @@ cudaError_t for_layout(const KvPool& kv, Launch launch) {
 cudaError_t kv_write_launch(const KvPool& kv, const __nv_bfloat16* k, const __nv_bfloat16* v, int64_t stride,
                             const int* slots, int n, int* err, cudaStream_t stream) {
   unsigned grid;
-  uint32_t inv;
-  if (!kv_grid(kv, n, &grid, &inv)) return cudaErrorInvalidValue;
+  KvOver over;
+  if (!kv_grid(kv, n, &grid, &over)) return cudaErrorInvalidValue;
   return for_layout(kv, [&](auto hd, auto format) {
-    kv_write_kernel<decltype(hd)::value, decltype(format)::value><<<grid, KV_THREADS, 0, stream>>>(kv, k, v, stride, slots, n, inv, err);
+    kv_write_kernel<decltype(hd)::value, decltype(format)::value><<<grid, KV_THREADS, 0, stream>>>(kv, k, v, stride, slots, n, over, err);
   });
 }
 
 cudaError_t kv_read_launch(const KvPool& kv, const int* slots, int n, __nv_bfloat16* k, __nv_bfloat16* v, int64_t stride,
                            int* err, cudaStream_t stream) {
   unsigned grid;
-  uint32_t inv;
-  if (!kv_grid(kv, n, &grid, &inv)) return cudaErrorInvalidValue;
+  KvOver over;
+  if (!kv_grid(kv, n, &grid, &over)) return cudaErrorInvalidValue;
   return for_layout(kv, [&](auto hd, auto format) {
-    kv_read_kernel<decltype(hd)::value, decltype(format)::value><<<grid, KV_THREADS, 0, stream>>>(kv, slots, n, k, v, stride, inv, err);
+    kv_read_kernel<decltype(hd)::value, decltype(format)::value><<<grid, KV_THREADS, 0, stream>>>(kv, slots, n, k, v, stride, over, err);
   });
 }
 
