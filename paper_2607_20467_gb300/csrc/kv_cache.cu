@@ -215,6 +215,19 @@ __global__ void __launch_bounds__(KV_THREADS) kv_write_kernel(KvPool kv, const _
   }
 }
 
+// A part (32 bytes) stored by two neighbouring threads together with the neighbour's: each store of a warp then
+// covers whole sectors, where threads that store their own cover a half of each twice.
+__device__ __forceinline__ void store_pair(uint4* to, const KvBf16& a, bool live) {
+  const bool odd = threadIdx.x & 1;
+  const uint4 mine = odd ? a.x[0] : a.x[1];
+  const uint4 other = make_uint4(__shfl_xor_sync(0xffffffffu, mine.x, 1), __shfl_xor_sync(0xffffffffu, mine.y, 1),
+                                 __shfl_xor_sync(0xffffffffu, mine.z, 1), __shfl_xor_sync(0xffffffffu, mine.w, 1));
+  if (!live) return;
+  // the even thread's part, then the odd one's: their first halves by the even thread
+  to[odd ? -1 : 0] = odd ? other : a.x[0];
+  to[odd ? 1 : 2] = odd ? a.x[1] : other;
+}
+
 template <int HD, KvFormat F>
 __global__ void __launch_bounds__(KV_THREADS) kv_read_kernel(KvPool kv, const int* __restrict__ slots, int n,
                                                              __nv_bfloat16* __restrict__ k, __nv_bfloat16* __restrict__ v,
@@ -253,7 +266,6 @@ __global__ void __launch_bounds__(KV_THREADS) kv_read_kernel(KvPool kv, const in
 #pragma unroll
   for (int i = 0; i < KV_EACH; ++i) {
     const KvPart p = walk.at(i);
-    if (p.row >= n) continue;
     if (F == KV_Q4 && vec[i] >= 0) {
       const Q4Scale f = q4_scale_twice((uint32_t)e[i]);
       const uint32_t codes[2] = {raw[i].x[0].x, raw[i].x[0].y};
@@ -277,9 +289,7 @@ __global__ void __launch_bounds__(KV_THREADS) kv_read_kernel(KvPool kv, const in
         raw[i].word(j) = pack_bf16x2(f.x * scale, f.y * scale);
       }
     }
-    uint4* to = reinterpret_cast<uint4*>((p.is_v ? v : k) + p.row * stride + (p.g * HD + KV_COMP * p.part));
-    to[0] = raw[i].x[0];
-    to[1] = raw[i].x[1];
+    store_pair(reinterpret_cast<uint4*>((p.is_v ? v : k) + p.row * stride + (p.g * HD + KV_COMP * p.part)), raw[i], p.row < n);
   }
 }
 
