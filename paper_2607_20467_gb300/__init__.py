@@ -272,7 +272,7 @@ class KvCache:
             raise ValueError("an FP8 cache needs k_exp and v_exp, a 4-bit one its scales in their place")
         if not small and (k_exp is not None or v_exp is not None):
             raise ValueError("a bf16 cache has no exponents")
-        q4 = small and len(k_exp.shape) == 4
+        q4 = small and len(k_exp.shape) == 4 and 16 * k_exp.shape[3] == hd  # (hd / 2 bytes of codes, hd / 32 scales)
         n, kind = pages * heads * page_len, "u8" if q4 else "e4m3" if small else "bf16"
         if tuple(v.shape) != tuple(k.shape):
             raise ValueError("k and v differ in shape")

@@ -193,9 +193,22 @@ def test_a_page_outside_the_pool_gives_no_slot(ops):
     assert call.pos.tolist() == list(range(20)) * 2
 
 
-def test_a_captured_plan_follows_its_inputs():
+def test_rows_at_any_address(ops):
+    """Slots and positions that begin between 16-byte borders."""
+    for shift in (1, 2, 3):
+        pages, lists, call = dcl.KvPages.new(500, 16, 3, 400), Lists(500, 16, 3), Call(3, 0)
+        bufs = [torch.full((5010,), 99, dtype=torch.int32, device="cuda") for _ in range(2)]
+        call.slots, call.pos = (b[shift:5003] for b in bufs)
+        call(ops, pages, [0, 0, 0], [1, 4990, 3])
+        ops.synchronise()
+        _same(pages, lists, call, lists.plan([0, 0, 0], [1, 4990, 3]))
+        assert all((b[:shift] == 99).all() and (b[5003:] == 99).all() for b in bufs)
+
+
+@pytest.mark.parametrize("rows", [200, 5000])  # (one kernel, and two)
+def test_a_captured_plan_follows_its_inputs(rows):
     stream = torch.cuda.Stream()
-    B, P, width, n_pages, rows = 5, 16, 20, 60, 200
+    B, P, width, n_pages = 5, 16, 20, 60
     start, new = _i32([0] * B), _i32([0] * B)
     pages, lists, call = dcl.KvPages.new(n_pages, P, B, width), Lists(n_pages, P, B), Call(B, rows)
     with dcl.Context(None, 1, 1, stream=stream.cuda_stream) as ctx:

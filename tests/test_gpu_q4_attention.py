@@ -11,6 +11,7 @@ import pytest
 import torch
 
 import paper_2607_20467_gb300 as dcl
+import synthetic as syn
 from oracle import q4
 
 pytestmark = pytest.mark.gpu
@@ -147,6 +148,33 @@ def test_many_rows_of_a_kv_head(ops, hd, page_len):
     _check(ops, np.random.default_rng(hd + page_len), [3000, 1000, 64, 1], [33, 40, 20, 1], 28, 4, hd, page_len)
 
 
+@pytest.mark.parametrize("page_len,heads,kv", [(16, 28, 4), (64, 16, 1), (128, 33, 3)])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_many_rows_under_a_wide_table(ops, hd, page_len, heads, kv):
+    """Page tables as wide as those of long sequences: the kernel for many rows."""
+    _check(ops, np.random.default_rng(hd + page_len), [700, 0, 90, 129], [40, 3, 9, 32], heads, kv, hd, page_len, wide=40000)
+
+
+def test_pages_past_four_gigabytes(ops):
+    heads, hd, page_len, pages = 32, 128, 256, 8300  # 4.35 GB of codes each
+    cache = dcl.KvCache.empty(pages, page_len, heads, hd, q4=True)
+    rng = np.random.default_rng(4)
+    k, v = (syn.round_bf16(rng.normal(0, 1, (300, heads, hd)).astype(np.float32)) for _ in range(2))
+    table = torch.tensor([[8299, 8250]], dtype=torch.int32, device="cuda")
+    at = np.arange(300)
+    slots = torch.from_numpy((np.array([8299, 8250])[at // 256] * 256 + at % 256).astype(np.int32)).cuda()
+    bf = lambda a: torch.from_numpy(a).to(torch.bfloat16).cuda()
+    ops.kv_write(cache, bf(k), bf(v), slots)
+    i32 = lambda *a: torch.tensor(a, dtype=torch.int32, device="cuda")
+    for new in (1, 12, 40):
+        q = bf(rng.normal(0, 1, (new, heads, hd)).astype(np.float32))
+        out = torch.empty_like(q)
+        ops.kv_attention(cache, q, i32(0, new), table, i32(300), out, max_new=new)
+        ops.synchronise()
+        o, _, A, _ = _reference(q.double().cpu().numpy(), q4.decode(*q4.encode(k)), q4.decode(*q4.encode(v)), False, hd ** -0.5)
+        assert (np.abs(out.double().cpu().numpy() - o) <= 2.0 ** -8 * np.abs(o) + 2.0 ** -12 * A).all()
+
+
 def test_sizes_far_apart_and_sharp_scores(ops):
     rng = np.random.default_rng(11)
     _check(ops, rng, [500, 130], [3, 20], 8, 2, 128, 16, spread=14, k_scale=2.0 ** -10)  # groups 2^28 apart
@@ -157,12 +185,13 @@ def test_max_new_above_the_rows_there_are(ops):
     _check(ops, np.random.default_rng(5), [300, 200], [1, 3], 8, 8, 128, 32, max_new=17)
 
 
+@pytest.mark.parametrize("new,H", [(20, 4), (4, 2), (7, 1)])  # (a pass for many rows, and one for up to 8)
 @pytest.mark.parametrize("hd", [64, 128])
-def test_a_group_without_numbers_is_seen_by_its_rows_only(ops, hd):
+def test_a_group_without_numbers_is_seen_by_its_rows_only(ops, hd, new, H):
     """A key's group makes every row that sees it NaN, a value's group its components; rows before it (causal) and
     other groups are as without it."""
     rng = np.random.default_rng(hd)
-    n, new, H = 70, 20, 4
+    n = 70
     cache, table, _ = _pool(rng, [n], 1, hd, 16)
     q = torch.from_numpy(rng.normal(0, 1, (new, H, hd))).to(torch.bfloat16).cuda()
     i32 = lambda *a: torch.tensor(a, dtype=torch.int32, device="cuda")
@@ -173,7 +202,7 @@ def test_a_group_without_numbers_is_seen_by_its_rows_only(ops, hd):
         ops.synchronise()
         return out
     plain = run(True)
-    for pos in (5, 55, 69):  # 5 is seen by all rows, 69 by the last alone
+    for pos in (5, 55, 67, 69):  # 5 is seen by all rows, 69 by the last alone
         page, place = int(table[0, pos // 16]), pos % 16
         sees = np.arange(new) + n - new >= pos
         g = 1
@@ -194,18 +223,20 @@ def test_a_group_without_numbers_is_seen_by_its_rows_only(ops, hd):
         assert torch.isnan(out[sees]).all() and torch.equal(out[~sees], plain[~sees])
 
 
-def test_a_page_outside_the_cache_is_reported_and_left_out(ops):
+@pytest.mark.parametrize("P", [16, 32])
+@pytest.mark.parametrize("heads", [4, 24])
+def test_a_page_outside_the_cache_is_reported_and_left_out(ops, P, heads):
     rng = np.random.default_rng(2)
-    cache, table, values = _pool(rng, [48, 20], 2, 64, 16)
+    cache, table, values = _pool(rng, [3 * P, 20], 2, 64, P)
     table[0, 1] = 1 << 20
-    q = torch.from_numpy(rng.normal(0, 1, (2, 4, 64))).to(torch.bfloat16).cuda()
+    q = torch.from_numpy(rng.normal(0, 1, (2, heads, 64))).to(torch.bfloat16).cuda()
     i32 = lambda *a: torch.tensor(a, dtype=torch.int32, device="cuda")
     out = torch.empty_like(q)
-    ops.kv_attention(cache, q, i32(0, 1, 2), table, i32(48, 20), out, max_new=1)
+    ops.kv_attention(cache, q, i32(0, 1, 2), table, i32(3 * P, 20), out, max_new=1)
     with pytest.raises(dcl.DcleapError, match="outside the paged cache"):
         ops.synchronise()
     assert torch.isfinite(out.float()).all()
-    keep = np.r_[0:16, 32:48]
+    keep = np.r_[0:P, 2 * P:3 * P]
     for b, (k, v) in enumerate(((values["k"][0][keep], values["v"][0][keep]), (values["k"][1], values["v"][1]))):
         o, _, A, _ = _reference(q[b:b + 1].float().cpu().numpy().astype(np.float64), k, v, False, 0.125)
         assert (np.abs(out[b].float().cpu().numpy() - o[0]) <= 2.0 ** -8 * np.abs(o[0]) + 2.0 ** -12 * A[0]).all()
