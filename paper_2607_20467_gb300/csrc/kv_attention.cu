@@ -28,6 +28,11 @@
 // loses weights where exponents lie 100 apart.  A vector of zeros is stored with exponent 0 whatever the
 // others' sizes and has no term to bound: where one would move m it is given an exponent far down.
 //
+// 4-bit pages, 9 to 32 rows (up to 8: kv_attention_q4.cu).  Codes are widened to bf16 with their groups' scales
+// where they are operands (q4.cuh), and all else is as with bf16 pages.  8 sequences of 1536, 32 heads, 32 rows
+// each (58 MB): 47.5 us, as long as wider formats take: two warps a scheduler (255 registers) wait for one
+// another's products, maxima and weights more than for any pipe (0.35 instructions a cycle, HMMA 0.4 busy).
+//
 // P is given in two parts, fp16 with FP8 pages (2^-21 of itself; 2^-32 of the largest term where that is
 // more) and bf16 with bf16 pages (2^-16; the instruction wants both operands of one type).  One part
 // would leave up to 2^-11 or 2^-8 of a result, beside 2^-8 of the output's own rounding.  Up to 8 rows
@@ -356,10 +361,9 @@ __global__ void __launch_bounds__(KaCfg<HD, F, RS>::THREADS, KA_CTAS) kv_attenti
             const uint32_t* w1 = &raw[RS > 1 ? 2 * mt + 1 : 0][s >> 1].x + 2 * (s & 1);
             uint4 x = RS > 1 ? make_uint4(w0[0], w1[0], w0[1], w1[1]) : make_uint4(w0[0], 0, w0[1], 0);
             if (Q4) {  // (of 8 components: 0 and 4, 1 and 5 of them, then 2 and 6, 3 and 7: as codes are widened)
-              const uint32_t *y0 = &raw[2 * mt][s >> 1].x + (s & 1), *y1 = &raw[RS > 1 ? 2 * mt + 1 : 0][s >> 1].x + (s & 1);
+              const uint32_t *y0 = &raw[2 * mt][s >> 1].x + (s & 1), *y1 = &raw[RS > 1 ? 2 * mt + 1 : 0][s >> 1].x + (s & 1);  // (RS > 1)
               x = make_uint4(__byte_perm(y0[0], y0[2], 0x5410), __byte_perm(y1[0], y1[2], 0x5410),
                              __byte_perm(y0[0], y0[2], 0x7632), __byte_perm(y1[0], y1[2], 0x7632));
-              if (RS == 1) x.y = x.w = 0;
             }
             *reinterpret_cast<uint4*>(qs[mt * KS + s][lane]) = x;
           }
@@ -795,7 +799,9 @@ cudaError_t launch_as(const KvPool& kv, const KvAttn& a, const KaScratch& s, int
 template <int HD, KvFormat F>
 cudaError_t launch_rows(const KvPool& kv, const KvAttn& a, const KaScratch& s, int ctas, int* err, cudaStream_t stream) {
   const int64_t rows = (int64_t)a.max_new * (a.H / kv.G);
-  if (rows <= 8) return launch_as<HD, F, 1>(kv, a, s, ctas, err, stream);
+  if constexpr (F != KV_Q4) {  // (4 bits: kv_attention_q4.cu)
+    if (rows <= 8) return launch_as<HD, F, 1>(kv, a, s, ctas, err, stream);
+  }
   if (rows <= 16) return launch_as<HD, F, 2>(kv, a, s, ctas, err, stream);
   return launch_as<HD, F, 4>(kv, a, s, ctas, err, stream);
 }

@@ -6,10 +6,10 @@
 // the place of its scores there; O += P V in TMEM.  A thread owns a row, so its statistics need no
 // exchange.
 //
-// All operands are bf16, which holds every value that a cache stores: FP8 codes are widened with their
-// exponents, so that nothing is lost whatever the sizes of neighbouring keys and values, and the rows'
+// All operands are bf16, which holds every value that a cache stores: codes are widened with their
+// exponents or scales, so that nothing is lost whatever the sizes of neighbouring keys and values, and the rows'
 // loop knows of no exponents.  Eight warps copy the pages into shared memory (16-byte asynchronous
-// copies, one unit ahead), bf16 straight into the operand tiles, FP8 codes into a buffer from which
+// copies, one unit ahead), bf16 straight into the operand tiles, FP8 and 4-bit codes into a buffer from which
 // they widen them.  (fp16 operands, scaled by the largest exponent of 32 keys, lost those far below it.)
 // V's tile is [key][hd], the transposed ("MN-major") form of the B operand, as it comes.
 //
@@ -22,6 +22,8 @@
 // tile, with two tiles in turn: of 6800 cycles a unit a row's warp takes 2200 to 3000 for the weights, 650
 // to 1200 for the maximum, waits 1900 to 2200 for S and has about 900 for an item's q and results.  The
 // CTAs' work ends after 88 to 102 us, and the joins come after it.
+//
+// The same in 4 bits (79 MB): 114 us; its codes cost the copying warps no more than FP8's.
 //
 // Roles (544 threads): warps 0-3 and 4-7 have the rows of the two tiles; warps 8-11 copy and widen
 // keys, 12-15 values (one group for both was the slowest link: 7800 cycles a unit); warp 16

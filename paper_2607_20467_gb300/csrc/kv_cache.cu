@@ -7,11 +7,15 @@
 // finite component into 448 * 2^e (at least KV_EXP_MIN), so scaling by 2^-e and widening a code to
 // bf16 are both exact: the code's rounding is the only one.
 //
+// 4 bits: groups of 32 components, 4-bit multiples -7 .. 7 of a scale (q4.cuh), the least one that reaches
+// the largest, each code the nearest; a group with an infinity or NaN in it is marked as none.
+//
 // Both kernels are bound by memory.  A thread has 16 components of a vector (two 16-byte loads, one
-// 16-byte store of codes) of two vectors at once; hd / 16 threads find a vector's maximum by
-// shuffles.  12288 positions of 32 heads x 128 (302 MB): written in 47.2 us, 6.4 TB/s, 0.94 of the
-// measured copy rate; read back in 52.9 us, 5.7 TB/s, 0.84 (two thirds of that traffic are
-// writes).  32 positions: 2 to 3 us of kernel in a call of 5.1.
+// 16-byte or 8-byte store of codes) of two vectors at once; hd / 16 threads find a vector's maximum by
+// shuffles, two a group's.  12288 positions of 32 heads x 128, FP8 (302 MB): written in 44.8 us, 6.7 TB/s, 0.99 of
+// the measured copy rate; read back in 46.9 us, 0.95 (two thirds of that traffic are writes).  4 bits (255 MB):
+// 43.8 us, 0.86 (a component's 3.5 instructions beside it: 0.8 of the issue slots) and 44.4 us, 0.85 (four
+// fifths writes).  32 positions: 2 us of kernel in a call of 4.5.  (256 threads a block: 1.5 to 2 us more for each.)
 #include <cuda_fp8.h>
 
 #include <type_traits>

@@ -1,5 +1,5 @@
-// How the kernels of kv_attention.cu and kv_attention_tc.cu share their work out, and what else they have
-// in common.
+// How the kernels of kv_attention.cu, kv_attention_q4.cu and kv_attention_tc.cu share their work out, and what
+// else they have in common.
 //
 // An item is the rows of one row tile (new positions x the query heads of one kv head) of one
 // sequence; its keys come in units of 128.  All items of a launch stand in one line, each with
