@@ -364,8 +364,9 @@ dcl_status dcl_kv_read(dcl_ctx* ctx, const dcl_kv_cache* cache, const int32_t* s
  *               sees nothing gets zeros and -inf.
  * Scores, softmax statistics and sums are held in fp32 and reproduce bit for bit; weights have 16 bits
  * or more (with FP8 pages and up to 32 rows a kv head: but for 2^-32 of a row's largest weight times
- * value).  An infinite value is the result of its component for the rows that see it (NaN with one
- * of the other sign, or where the row's weight for it is zero in fp32).
+ * value; else but for 2^-93 of the largest weight).  An infinite value is the result of its component
+ * for the rows that see it (NaN with one of the other sign, or where the row's weight for it is zero
+ * in fp32).
  * A context's first call that has rows allocates its scratch (41 MB, for calls of every size) and is
  * refused with STATE while the stream is being captured; every later call may be captured.
  * Errors: INVALID_ARG, STATE, OOM (scratch), CUDA. */
