@@ -392,7 +392,8 @@ typedef struct {
  *      with a sequence are there; one whose pages are not gets none, keeps what it has and gets no rows
  *      (q_start_dev tells), and so do those after it that lack any.
  *   3. q_start_dev [batch + 1]: the rows of sequence b are [q_start[b], q_start[b + 1]); seq_len_dev
- *      [batch]: start + new (start for one that got no rows): what dcl_kv_attention takes.  slot_dev,
+ *      [batch]: start + new (start for one that got no rows): what dcl_kv_attention takes; it may be
+ *      start_dev itself, for a next step that goes on from there.  Nothing else overlaps.  slot_dev,
  *      pos_dev [n_rows]: the slot (for dcl_kv_write) and position (for dcl_qk_norm_rope) of every row,
  *      -1 for rows past the last sequence's, so that a captured step may have room for more rows.
  * A sequence whose numbers are negative or past its table, more rows than n_rows (those past it are

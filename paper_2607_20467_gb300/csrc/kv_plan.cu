@@ -10,8 +10,8 @@
 // sums over the sequences in pieces of a CTA's threads; a warp for a sequence's pages; a thread for a few
 // rows (their sequence by bisection in q_start).  Steps of many rows or sequences: a cluster of 8 CTAs for the
 // pages, each of which has the sums for itself, and a second kernel for the rows, launched as the first
-// begins.  8 sequences of 32 rows: 4.0 us in a graph, of which the launch is about 2.  256 prompts of up to 1536
-// positions (172 thousand rows, 1.4 MB): 7.5 us (one CTA for all 228; the cluster's CTAs for the rows, too, 16.5:
+// begins.  8 sequences of 32 rows: 4.2 us in a graph, of which the launch is about 2.  256 prompts of up to 1536
+// positions (172 thousand rows, 1.4 MB): 7.8 us (one CTA for all 228; the cluster's CTAs for the rows, too, 16.5:
 // ten of them were the rows' instructions on 8 SMs; 16 rows a thread there 20.6).
 #include "common.cuh"
 #include "kv_cache.cuh"
@@ -20,7 +20,7 @@ namespace dcl {
 namespace {
 
 constexpr int KP_CLUSTER = 8;
-constexpr int KP_STARTS = 2048;  // sequences whose starts are kept in shared memory
+constexpr int KP_STARTS = 2048;  // sequences whose first rows and positions are kept in shared memory
 constexpr int KP_ROW_THREADS = 256;
 
 // A sequence's numbers; one that is not within its table gets no rows and keeps what it has.
@@ -69,11 +69,16 @@ __device__ __forceinline__ int64_t kp_scan(int64_t x, int64_t (&sums)[T / 32], i
   return warp ? x + before : x;
 }
 
-// Slots and positions of rows first .. first + 3 and every step after; starts: q_start in shared memory, or NULL.
-__device__ __forceinline__ void kp_rows(const KvPlan& a, const int* starts, int64_t first, int64_t step, int* err) {
+// What a sequence that got its rows keeps: start is what seq_len tells, which may have taken its place.
+__device__ __forceinline__ int kp_kept(const KvPlan& a, int b) { return __ldcg(a.seq_len + b) - a.rows_new[b]; }
+
+// Slots and positions of rows first .. first + 3 and every step after; starts, keeps: q_start and what the sequences
+// keep in shared memory, or NULL.
+__device__ __forceinline__ void kp_rows(const KvPlan& a, const int* starts, const int* keeps, int64_t first, int64_t step, int* err) {
   const int P = 1 << a.page_shift;
   const bool wide = ((reinterpret_cast<uintptr_t>(a.slot) | reinterpret_cast<uintptr_t>(a.pos)) & 15) == 0;
   auto start_of = [&](int b) { return starts ? starts[b] : __ldcg(a.q_start + b); };
+  auto kept_of = [&](int b) { return starts ? keeps[b] : kp_kept(a, b); };
   const int live = start_of(a.batch);
   for (; first < a.n_rows; first += step) {
     const int r0 = (int)first;
@@ -85,7 +90,7 @@ __device__ __forceinline__ void kp_rows(const KvPlan& a, const int* starts, int6
         if (start_of(mid + 1) > r0) hi = mid;
         else lo = mid + 1;
       }
-      int q0 = start_of(lo), q1 = start_of(lo + 1), at = a.start[lo], have = -1, base = 0;
+      int q0 = start_of(lo), q1 = start_of(lo + 1), at = kept_of(lo), have = -1, base = 0;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int r = r0 + i;
@@ -95,7 +100,7 @@ __device__ __forceinline__ void kp_rows(const KvPlan& a, const int* starts, int6
             q0 = q1;
             q1 = start_of(++lo + 1);
           } while (r >= q1);
-          at = a.start[lo];
+          at = kept_of(lo);
           have = -1;
         }
         pos[i] = at + r - q0;
@@ -129,7 +134,7 @@ __global__ void __launch_bounds__(T) kv_plan_kernel(KvPlan a, int* err) {
   __shared__ int64_t sums[2][T / 32];
   __shared__ int64_t off[T];             // where a sequence's pages go to, or come from
   __shared__ int first[T], count[T];     // its first page to give or take, and how many
-  __shared__ int starts[KP_STARTS + 1];
+  __shared__ int starts[KP_STARTS + 1], keeps[KP_STARTS];
   __shared__ int most;                   // pages taken
   const int tid = threadIdx.x, lane = tid & 31;
   const int rank = CTAS > 1 ? (int)blockIdx.x : 0, warp = rank * (T / 32) + (tid >> 5);  // (one cluster is the grid)
@@ -207,18 +212,21 @@ __global__ void __launch_bounds__(T) kv_plan_kernel(KvPlan a, int* err) {
     if (lane == 0 && taken) atomicMax(&most, taken);
     if (b < a.batch) {
       const int q = (int)min(end, (int64_t)a.n_rows);
-      if (kept) starts[b + 1] = q;
-      if (rank == 0) {
-        a.q_start[b + 1] = q;
-        a.seq_len[b] = ok ? s.start + s.rows : s.start;
+      if (kept) {
+        starts[b + 1] = q;
+        keeps[b] = s.start;
       }
+      if (rank == 0) a.q_start[b + 1] = q;
     }
-    meet();  // (every CTA has read what the sequences hold)
+    meet();  // (every CTA has read what the sequences hold and keep)
     for (int i = warp; i < T && b0 + i < a.batch; i += CTAS * (T / 32)) {
       int* row = a.table + (int64_t)(b0 + i) * a.max_pages + first[i];
       for (int j = lane; j < count[i]; j += 32) row[j] = __ldcg(a.free + off[i] - j);
     }
-    if (rank == 0 && b < a.batch && !broken && !s.bad && (ok || s.back())) a.held[b] = s.need;
+    if (rank == 0 && b < a.batch) {
+      a.seq_len[b] = ok ? s.start + s.rows : s.start;
+      if (!broken && !s.bad && (ok || s.back())) a.held[b] = s.need;
+    }
   }
   if (tid == 0) {
     starts[0] = 0;
@@ -230,17 +238,20 @@ __global__ void __launch_bounds__(T) kv_plan_kernel(KvPlan a, int* err) {
   meet();
   if (rank == 0 && tid == 0 && a.batch && !broken) *a.n_free = (int)(pages - most);
   if (!ROWS_TOO) return;
-  kp_rows(a, kept ? starts : nullptr, 4 * tid, 4 * T, err);
+  kp_rows(a, kept ? starts : nullptr, keeps, 4 * tid, 4 * T, err);
 }
 
 // The rows of a step that has many of them, by CTAs all over the GPU.
 __global__ void __launch_bounds__(KP_ROW_THREADS) kv_plan_rows_kernel(KvPlan a, int* err) {
-  __shared__ int starts[KP_STARTS + 1];
+  __shared__ int starts[KP_STARTS + 1], keeps[KP_STARTS];
   pdl_wait();
   const bool kept = a.batch <= KP_STARTS;
-  for (int i = threadIdx.x; kept && i <= a.batch; i += KP_ROW_THREADS) starts[i] = a.q_start[i];
+  for (int i = threadIdx.x; kept && i <= a.batch; i += KP_ROW_THREADS) {
+    starts[i] = a.q_start[i];
+    if (i < a.batch) keeps[i] = kp_kept(a, i);
+  }
   __syncthreads();
-  kp_rows(a, kept ? starts : nullptr, 4 * ((int64_t)blockIdx.x * KP_ROW_THREADS + threadIdx.x), 4 * (int64_t)gridDim.x * KP_ROW_THREADS, err);
+  kp_rows(a, kept ? starts : nullptr, keeps, 4 * ((int64_t)blockIdx.x * KP_ROW_THREADS + threadIdx.x), 4 * (int64_t)gridDim.x * KP_ROW_THREADS, err);
 }
 
 }  // namespace

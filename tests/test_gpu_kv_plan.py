@@ -229,3 +229,23 @@ def test_a_captured_plan_follows_its_inputs(rows):
             _same(pages, lists, call, want)
             at = np.where(rng.random(B) < 0.4, 0, want[3])
         ctx.synchronise()
+
+
+@pytest.mark.parametrize("batch,rows", [(5, 60), (300, 2000), (1500, 9000), (3, 9000)])
+def test_lengths_that_take_the_place_of_the_starts(ops, batch, rows):
+    """seq_len is start: steps in a row, each from where the last one ended, with one kernel and with two (from 256
+    sequences or 4096 rows on), and more sequences than a block has threads; one that gets no pages stays where it is."""
+    rng = np.random.default_rng(batch)
+    P, width = 16, 1200
+    n_pages = batch + rows // 8
+    pages, lists = dcl.KvPages.new(n_pages, P, batch, width), Lists(n_pages, P, batch)
+    call = Call(batch, rows)
+    call.seq_len.zero_()
+    at = [0] * batch
+    for step in range(6):
+        new = rng.multinomial(int(rng.integers(rows // 2, rows + 1)), [1 / batch] * batch).tolist()
+        ops.kv_plan(pages, call.seq_len, _i32(new), call.q_start, call.seq_len, call.slots, call.pos)
+        ops.synchronise()
+        want = lists.plan(at, new)
+        _same(pages, lists, call, want)
+        at = want[3]
