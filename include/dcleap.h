@@ -411,7 +411,7 @@ dcl_status dcl_kv_plan(dcl_ctx* ctx, const dcl_kv_pages* pages, const int32_t* s
  *   q_dev, k_dev  bf16 rows of [n_heads][head_dim] and [n_kv_heads][head_dim], strides in elements
  *                 (multiples of 8; they may stand in the q | k | v rows of one projection).
  *   pos_dev       int32 [n]; the rows of a negative position are left out, their outputs untouched.
- *   q_gain_dev, k_gain_dev  bf16 [head_dim], or NULL: not normed.  eps > 0 where either is given.
+ *   q_gain_dev, k_gain_dev  bf16 [head_dim], or NULL: not normed.  eps from 1e-30 to 1e30 where either is given.
  *   q_out_dev, k_out_dev    as q_dev, k_dev; either these themselves (in place, with the same strides)
  *                 or apart from them.
  * head_dim 64 or 128; rot_dim a multiple of 16 up to head_dim; theta at least 1; all pointers to bf16 16-byte

@@ -1556,8 +1556,9 @@ dcl_status dcl_qk_norm_rope(dcl_ctx* c, const void* q_dev, int64_t q_stride, con
   if (n < 0 || n_heads <= 0 || n_kv_heads <= 0 || (int64_t)n_heads + n_kv_heads > (1 << 20))
     return fail(c, DCL_ERR_INVALID_ARG, "qk_norm_rope: n must be >= 0, n_heads and n_kv_heads > 0 and 2^20 together at most");
   if (!(theta >= 1.f) || theta > 3e38f) return fail(c, DCL_ERR_INVALID_ARG, "qk_norm_rope: theta must be at least 1");
-  if ((q_gain_dev || k_gain_dev) && (!(eps > 0.f) || eps > 3e38f))
-    return fail(c, DCL_ERR_INVALID_ARG, "qk_norm_rope: eps must be > 0");
+  // (squares are exact to fp32's 2^-24 of themselves from 1e-38 on, and mean + eps has to stay a number)
+  if ((q_gain_dev || k_gain_dev) && !(eps >= 1e-30f && eps <= 1e30f))
+    return fail(c, DCL_ERR_INVALID_ARG, "qk_norm_rope: eps must be from 1e-30 to 1e30");
   if (n == 0) return DCL_OK;
   if (!q_dev || !k_dev || !pos_dev || !q_out_dev || !k_out_dev) return fail(c, DCL_ERR_INVALID_ARG, "qk_norm_rope: NULL argument");
   const int64_t q_row = (int64_t)n_heads * head_dim, k_row = (int64_t)n_kv_heads * head_dim;

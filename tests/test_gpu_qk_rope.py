@@ -163,3 +163,10 @@ def test_outputs_reproduce_and_capture(ops):
             graph.replay()
             torch.cuda.synchronize()
             assert all(torch.equal(a, b) for a, b in zip(outs, eager))
+
+
+@pytest.mark.parametrize("eps", [1e-30, 1e30])
+def test_the_smallest_and_the_largest_eps(ops, eps):
+    """Values so small and so large that eps is all of the root, or none of it."""
+    _run(ops, 5, 4, 2, 64, 64, eps=eps, size=2.0 ** -60)
+    _run(ops, 5, 4, 2, 64, 64, eps=eps, size=2.0 ** 60)

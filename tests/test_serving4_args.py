@@ -122,7 +122,8 @@ def test_the_abi_refuses_bad_arguments(built):
         for kw, words in ((dict(hd=96), "head_dim"), (dict(rot=24), "rot_dim"), (dict(rot=80), "rot_dim"), (dict(rot=-16), "rot_dim"),
                           (dict(n=-1), "n must"), (dict(H=0), "n_heads"), (dict(G=0), "n_kv_heads"), (dict(theta=0.5), "theta"),
                           (dict(theta=float("nan")), "theta"), (dict(theta=float("inf")), "theta"), (dict(eps=0.0), "eps"),
-                          (dict(eps=-1.0), "eps"), (dict(eps=float("nan")), "eps"), (dict(q=None), "NULL"), (dict(k=None), "NULL"),
+                          (dict(eps=-1.0), "eps"), (dict(eps=float("nan")), "eps"), (dict(eps=3e38), "eps"), (dict(eps=1e-44), "eps"),
+                          (dict(eps=3e38, qg=None), "eps"), (dict(q=None), "NULL"), (dict(k=None), "NULL"),
                           (dict(pos=None), "NULL"), (dict(qo=None), "NULL"), (dict(ko=None), "NULL"), (dict(qs=255), "strides"),
                           (dict(ks=132), "strides"), (dict(qos=128), "strides"), (dict(kos=129), "strides"), (dict(q=P + 8), "aligned"),
                           (dict(kg=P + 2), "aligned"), (dict(ko=P + 4), "aligned"), (dict(qo=P, qos=512), "in place")):
