@@ -814,12 +814,13 @@ cudaError_t launch_rows(const KvPool& kv, const KvAttn& a, const KaScratch& s, i
 // 128 rows, 18 for 256, and on top 5 us an item of a CTA and 0.0175 us a row and part.  Measured, us here /
 // there, FP8, 28 / 4 heads of 128: 16 x 8192 positions, 224 rows a kv head 301 / 105; 8 x 3000: 63 rows
 // 35 / 34, 112 53 / 37, 224 74 / 48; 4 x 8192 (ten parts an item): 63 rows 50 / 45, 112 61 / 54, 224 90 / 79;
-// 1 x 16384, 224 rows 62 / 123; 2 x 1000, 224 rows 24 / 35.  Over 276 shapes (four head layouts, both formats) the rule
+// 1 x 16384, 224 rows 62 / 123; 2 x 1000, 224 rows 24 / 35.  Causal, 4 bits (there only of 4 bits): 4 x 8192, 448 rows
+// 155 / 84; 16 x 1024 90 / 49; 8 x 4096, 112 rows 58 / 45.  Over 276 shapes (four head layouts, both formats) the rule
 // takes 0.8 % longer than the better kernel on average, more than 7 % longer in 13.  Lengths are known to the
 // device only: the page table's width stands for them.
 bool kv_attention_many_rows(const KvPool& kv, const KvAttn& a) {
   const int64_t rows = (int64_t)a.max_new * (a.H / kv.G);
-  if (a.causal || rows <= 32) return false;
+  if ((a.causal && kv.format != KV_Q4) || rows <= 32) return false;
   const double units = (double)a.batch * kv.G * (((int64_t)a.max_pages * kv.page_len() + KA_UNIT - 1) / KA_UNIT);
   const int64_t rest = rows % 256;
   const double here = 10.0 * (double)((rows + 31) / 32), there = 18.0 * (double)(rows / 256) + (rest > 128 ? 18 : rest ? 15 : 0);

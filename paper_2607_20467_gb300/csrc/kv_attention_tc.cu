@@ -23,7 +23,9 @@
 // to 1200 for the maximum, waits 1900 to 2200 for S and has about 900 for an item's q and results.  The
 // CTAs' work ends after 88 to 102 us, and the joins come after it.
 //
-// The same in 4 bits (79 MB): 114 us; its codes cost the copying warps no more than FP8's.
+// The same in 4 bits (79 MB): 114 us; its codes cost the copying warps no more than FP8's.  Causal, 4 bits only
+// (a kernel of its own, as what it takes slowed the other by 2 %): 8 sequences of 2048 positions, the last 256 of
+// them new, 113 us (not causal 108); 4 x 8192, 64 new, 84 us, where 32 rows a pass take 155.
 //
 // Roles (544 threads): warps 0-3 and 4-7 have the rows of the two tiles; warps 8-11 copy and widen
 // keys, 12-15 values (one group for both was the slowest link: 7800 cycles a unit); warp 16
@@ -31,6 +33,7 @@
 // a time (the next 32 on their way as well spill: 137 us).  Two warps for a tile's 32 rows, half the
 // keys each, were no faster (115 us).  Every wait is bounded (DERR_WAIT_TIMEOUT).
 #include <cuda_fp16.h>
+#include <limits.h>
 
 #include <algorithm>
 #include <type_traits>
@@ -66,7 +69,8 @@ struct TcCfg {
   static constexpr int HOLDER = BAR + 8 * NBARS;      // TMEM address, abort flag
   static constexpr int WALK = HOLDER + 8;
   static constexpr int TODO = WALK + (int)sizeof(KaWalk);
-  static constexpr size_t SMEM = TODO + 3 * sizeof(KaJoin);
+  static constexpr int LOWEST = TODO + 3 * (int)sizeof(KaJoin);  // 4 bits: [4 items][4 warps][4 groups], lowest keys (TcSeen)
+  static constexpr size_t SMEM = LOWEST + (F == KV_Q4 ? 4 * 4 * 4 * 4 : 0);
   static_assert(SMEM <= 232448, "shared memory per CTA");
   static_assert(TC_JOIN * 8 + TC_ROWS * 8 <= THERE, "a join's weights take the place of the operands");
 };
@@ -103,6 +107,20 @@ __device__ __forceinline__ uint32_t widen(uint32_t w, int half, __nv_bfloat162 f
   const __nv_bfloat162 y = __hmul2(__floats2bfloat162_rn(x.x, x.y), f);
   return *reinterpret_cast<const uint32_t*>(&y);
 }
+
+// What the rows of an item see.  4-bit pages, causal: a row the keys up to its own; no key past its last row's
+// is read.  A value group that holds no numbers and that only some rows see may not enter the product (0 *
+// NaN); since rows see the first keys up to one, the lowest such key of a group tells which rows are to get NaN.
+struct TcSeen {
+  int few, most;  // keys that the first row sees, and the last (whichever is less than none: none)
+  int units;      // of the CTA's, those that any row sees; one at least
+  template <bool CAUSAL>
+  static __device__ __forceinline__ TcSeen of(const KaItem& it, int rep) {
+    if (!CAUSAL) return TcSeen{it.len, it.len, it.until - it.from};
+    const int before = it.len - it.nq + 1, most = min(it.len, before + (it.first + it.rows - 1) / rep);
+    return TcSeen{before + it.first / rep, most, max(1, (min(it.until * KA_UNIT, most) - it.from * KA_UNIT + KA_UNIT - 1) / KA_UNIT)};
+  }
+};
 
 // The MMAs of an item (the whole warp; one lane issues).  Its operands are made known as the warp's, in
 // uniform registers: else an issue takes about 100 cycles, more than most of the products.
@@ -172,10 +190,11 @@ __device__ __forceinline__ bool tc_mma(uint32_t base, uint32_t tmem, int tiles, 
   return true;
 }
 
-template <int HD, KvFormat F>
+template <int HD, KvFormat F, bool CAUSAL>
 __global__ void __launch_bounds__(TC_THREADS, 1)
     kv_attention_tc_kernel(KvPool kv, KvAttn a, KaScratch scratch, int* err) {
   using C = TcCfg<HD, F>;
+  static_assert(F == KV_Q4 || !CAUSAL, "the groups of other formats hold numbers and others side by side");
   extern __shared__ __align__(1024) uint8_t smem[];
   uint32_t base = smem_u32(smem);
   asm volatile("" : "+r"(base));
@@ -242,14 +261,16 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     const int8_t* exps = values ? kv.v_exp : kv.k_exp;
     const uint32_t raw = base + C::RAW + values * C::CODES;
     uint32_t seq = values;  // operand tiles (keys and values in turn): stage seq % NS
+    int nth = 0;            // items
     bool ok = true;
     // (codes: eight lanes read two keys, whose chunks lie in each other's halves of 128 bytes)
     auto raw_at = [&](int k, int c) { return (uint32_t)(k * CH + (CH == 8 ? c ^ (4 * (k & 1)) : c)) * 16; };
     auto tile_at = [&](int k, int c) { return (uint32_t)(c >> 3) * TC_BOX + swz(k, c & 7); };  // 16-bit elements
     auto stage_of = [&](uint32_t s) { return base + C::KV + (s % C::NS) * C::TILE; };
     auto wait_empty = [&](uint32_t s) { return wait(empty0 + 8 * (s % C::NS), ((s / C::NS) & 1u) ^ 1u); };
-    while (ok && line.next(walk, it)) {
-      const int stop = min(it.len, it.until * KA_UNIT), n = it.until - it.from, first = it.from * KA_UNIT + 32 * w4;
+    for (; ok && line.next(walk, it); ++nth) {
+      const TcSeen seen = TcSeen::of<CAUSAL>(it, rep);
+      const int stop = min(seen.most, it.until * KA_UNIT), n = seen.units, first = it.from * KA_UNIT + 32 * w4;
       const int* table = a.table + (int64_t)it.b * a.max_pages;
       auto page_at = [&](int unit) {  // of this lane's key; negative: it is not to be read
         const int key = first + unit * KA_UNIT + lane;
@@ -295,6 +316,24 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
         if (F == KV_Q4) {
           ok = wait_empty(seq);
           if (!ok) break;
+          if (CAUSAL && values) {  // (rows read an item's lowest keys before values two units on are written)
+            int* lowest = reinterpret_cast<int*>(smem + C::LOWEST) + ((nth & 3) * 4 + w4) * 4;
+            if (u == 0 && lane < 4) lowest[lane] = INT_MAX;
+            __syncwarp();
+            const int key = first + u * KA_UNIT + lane;
+            uint32_t none = 0;  // this lane's key's groups without numbers that some rows do not see
+#pragma unroll
+            for (int g = 0; g < HD / Q4_GROUP; ++g)
+              if (key >= seen.few && ((uint32_t)e >> (8 * g) & 0xffu) >= Q4_SCALES) none |= 1u << g;
+            if (__any_sync(0xffffffffu, none)) {
+#pragma unroll
+              for (int g = 0; g < HD / Q4_GROUP; ++g) {
+                const unsigned keys = __ballot_sync(0xffffffffu, none >> g & 1);
+                if (lane == 0 && keys) lowest[g] = min(lowest[g], key + __ffs(keys) - 1);
+                if (none >> g & 1) e &= (int)~(0xffu << (8 * g));  // (any scale that is a number)
+              }
+            }
+          }
 #pragma unroll
           for (int i = 0; i < 32 / KP; ++i) {
             const int k = at_key + KP * i;
@@ -377,7 +416,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     bool ok = true;
     const bool leader = elect_one();
     while (warp_uniform(ok && line.next(walk, it)))
-      ok = tc_mma<HD, F>(base, tmem, it.rows > 128 ? 2 : 1, it.until - it.from, seq, items, units, abort_flag);
+      ok = tc_mma<HD, F>(base, tmem, it.rows > 128 ? 2 : 1, warp_uniform(TcSeen::of<CAUSAL>(it, rep).units), seq, items, units, abort_flag);
     if (!ok) gave_up();
     if (leader) umma_commit(drain);  // every MMA issued here completes before the end
     __syncwarp();
@@ -391,6 +430,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     auto rows_bar = [] { asm volatile("bar.sync 1, 256;" ::: "memory"); };
     const float qf = fmaxf(a.scale * kLog2e, 1.2e-38f);  // (not 0: a masked score is -inf)
     uint32_t count = 0, seq = 0;
+    int nth = 0;  // items
     // After a wait that ran out a warp goes on through the items without work: the barrier of the rows'
     // warps has one count for all of them.
     bool ok = true;
@@ -401,9 +441,10 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
       }
       return ok;
     };
-    while (line.next(walk, it)) {
-      const int n = it.until - it.from, tiles = it.rows > 128 ? 2 : 1;
+    for (; line.next(walk, it); ++nth) {
+      const int n = TcSeen::of<CAUSAL>(it, rep).units, tiles = it.rows > 128 ? 2 : 1;
       const int row = 128 * t + r;
+      const int limit = CAUSAL ? it.len - it.nq + (it.first + row) / rep + 1 : INT_MAX;  // keys it sees
       const bool live = row < it.rows, band = 128 * t + 32 * quarter < it.rows;
       // ---- q: the band's rows into their tile, 16-byte chunks of a row by neighbouring lanes
       if (ok && t < tiles) {
@@ -441,7 +482,11 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
           const uint32_t there0 = base + C::THERE + (blk & 3) * 16;
           uint32_t s0[32];  // 32 scores
           auto mask = [&](uint32_t (&s)[32], int c) {  // keys that are not there
-            const uint32_t there = __float_as_uint(ld_shared_f32(there0 + 4 * c));
+            uint32_t there = __float_as_uint(ld_shared_f32(there0 + 4 * c));
+            if (CAUSAL) {  // and those past the row's own
+              const int more = limit - (it.from + u) * KA_UNIT - 32 * c;
+              there &= more > 0 ? ~0u >> max(32 - more, 0) : 0u;
+            }
             if (there != 0xffffffffu) {
 #pragma unroll
               for (int i = 0; i < 32; ++i) s[i] = there >> i & 1 ? s[i] : 0xff800000u;
@@ -541,6 +586,12 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
           tmem_ld32(o_at + 32 * c, o);
           tmem_ld_wait();
           if (!live) continue;
+          if (CAUSAL) {
+            const int* lowest = reinterpret_cast<const int*>(smem + C::LOWEST) + (nth & 3) * 16 + c;
+            if (limit > min(min(lowest[0], lowest[4]), min(lowest[8], lowest[12])))
+#pragma unroll
+              for (int i = 0; i < 32; ++i) o[i] = 0x7fc00000u;
+          }
 #pragma unroll
           for (int i = 0; i < 32; i += 4) {
             const int b = i & ~7, h = i >> 2 & 1;
@@ -569,6 +620,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
           __threadfence();
         }
         __syncwarp();  // (aligned instructions follow)
+      } else if (CAUSAL) {
+        rows_bar();  // (neither tile's rows are two items ahead of the other's, whose lowest keys would be lost)
       }
     }
   }
@@ -592,11 +645,11 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
   }
 }
 
-template <int HD, KvFormat F>
+template <int HD, KvFormat F, bool CAUSAL = false>
 cudaError_t launch_as(const KvPool& kv, const KvAttn& a, const KaScratch& s, int ctas, int* err, cudaStream_t stream) {
   using C = TcCfg<HD, F>;
   static_assert((size_t)2 * TC_ROWS * (HD + 4) * 4 <= KV_ATTN_TC_PART_BYTES, "scratch per CTA");
-  auto kern = kv_attention_tc_kernel<HD, F>;
+  auto kern = kv_attention_tc_kernel<HD, F, CAUSAL>;
   static const cudaError_t set = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM);
   if (set != cudaSuccess) return set;
   kern<<<ctas, TC_THREADS, C::SMEM, stream>>>(kv, a, s, err);
@@ -612,7 +665,7 @@ cudaError_t kv_attention_tc_launch(const KvPool& kv, const KvAttn& a, void* scra
   KaScratch s{reinterpret_cast<float*>(static_cast<uint8_t*>(scratch) + KV_ATTN_COUNTERS), static_cast<int*>(scratch)};
   auto as = [&](auto hd) {
     constexpr int HD = decltype(hd)::value;
-    if (kv.format == KV_Q4) return launch_as<HD, KV_Q4>(kv, a, s, sms, err, stream);
+    if (kv.format == KV_Q4) return a.causal ? launch_as<HD, KV_Q4, true>(kv, a, s, sms, err, stream) : launch_as<HD, KV_Q4>(kv, a, s, sms, err, stream);
     if (kv.format == KV_FP8) return launch_as<HD, KV_FP8>(kv, a, s, sms, err, stream);
     return launch_as<HD, KV_BF16>(kv, a, s, sms, err, stream);
   };

@@ -272,3 +272,56 @@ def test_a_captured_call_follows_the_lengths(ops):
             torch.cuda.synchronize()
             assert torch.equal(out, eager)
         ctx.synchronise()
+
+
+@pytest.mark.parametrize("page_len,heads,kv", [(16, 28, 4), (64, 16, 1), (128, 33, 3)])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_many_causal_rows_under_a_wide_table(ops, hd, page_len, heads, kv):
+    """The kernel for many rows, each of which sees the keys up to its own: as many new positions as there are (a
+    prompt), more, which leaves rows that see none, and few; lengths that end inside units and pages."""
+    lens, news = [700, 0, 90, 129, 300, 33, 257], [40, 3, 9, 32, 300, 50, 1]
+    _check(ops, np.random.default_rng(hd + page_len), lens, news, heads, kv, hd, page_len, causal=True, wide=200000)
+
+
+def test_a_long_causal_block_that_many_ctas_share(ops):
+    _check(ops, np.random.default_rng(21), [4500, 900], [90, 600], 14, 2, 128, 64, causal=True, wide=200000)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_a_group_without_numbers_under_many_causal_rows(ops, hd):
+    """As for few rows: every row that sees a key without numbers gets NaN, those before it nothing of it; two values'
+    groups at once, one of them in a unit that only some rows see."""
+    rng = np.random.default_rng(hd)
+    n, new, H = 300, 200, 7
+    cache, table, _ = _pool(rng, [n, 140], 1, hd, 16)
+    table = torch.cat([table, torch.full((2, 60000), -1, dtype=torch.int32, device="cuda")], 1).contiguous()
+    news = [new, 20]
+    q = torch.from_numpy(rng.normal(0, 1, (sum(news), H, hd))).to(torch.bfloat16).cuda()
+    i32 = lambda *a: torch.tensor(a, dtype=torch.int32, device="cuda")
+
+    def run():
+        out = torch.empty_like(q)
+        ops.kv_attention(cache, q, i32(0, new, sum(news)), table, i32(n, 140), out, max_new=new, causal=True)
+        ops.synchronise()
+        return out[:new], out[new:]
+
+    plain, plain2 = run()
+    last = hd // 32 - 1
+    for first, second in ((5, 101), (99, 100), (100, 127), (128, 299), (299, 200), (255, 256)):
+        sees = [torch.from_numpy(np.arange(new) + n - new >= pos).cuda() for pos in (first, second)]
+        where = [(int(table[0, pos // 16]), 0, pos % 16, g) for pos, g in ((first, 0), (second, last))]
+        was = [int(cache.v_exp[w]) for w in where]
+        for w, byte in zip(where, (252, 255)):
+            cache.v_exp[w] = byte
+        out, out2 = run()
+        for w, byte in zip(where, was):
+            cache.v_exp[w] = byte
+        want = torch.zeros(new, H, hd, dtype=torch.bool, device="cuda")
+        want[:, :, :32] |= sees[0][:, None, None]
+        want[:, :, 32 * last:] |= sees[1][:, None, None]
+        assert torch.equal(torch.isnan(out), want) and torch.equal(out[~want], plain[~want]) and torch.equal(out2, plain2)
+        was = int(cache.k_exp[where[1]])
+        cache.k_exp[where[1]] = 253
+        out, out2 = run()
+        cache.k_exp[where[1]] = was
+        assert torch.isnan(out[sees[1]]).all() and torch.equal(out[~sees[1]], plain[~sees[1]]) and torch.equal(out2, plain2)
