@@ -21,7 +21,7 @@
 // are walked.  The rest of a CTA's time: 4400 cycles to find its part of the line, 5000 until its first keys
 // are there, 4000 an item's end, 2800 a join of two parts.  (Keys and values on the N side, as for wider
 // formats: 57.5 us and 39.7.  Shifts by multiplication, for the other pipe: 53.6.  16 rows a pass this way
-// round: 8 sequences of 1536, 32 heads, 32 rows 52 us, 47.5 in kv_attention.cu.)
+// round: 8 sequences of 1536, 32 heads, 32 rows 52 us, 47.5 in kv_attention.cu, both cut.)
 #include <algorithm>
 #include <type_traits>
 
@@ -181,7 +181,7 @@ __global__ void __launch_bounds__(K4Cfg<HD>::THREADS, K4_CTAS) kv_attention_q4_k
   const int k_group = place * SIDE / 4, v_group = quad * SIDE / 8;
   const float qa = fmaxf(a.scale * kLog2e, 1.2e-38f);  // (not 0: a masked score is -inf)
 
-  const KaLine<ROWS, K4_START> line(kv, a);
+  const KaLine<ROWS, K4_START, KA_KEEP> line(kv, a);
 
   // ---- this CTA's part of the line of all items
   KaWalk& shared_walk = *reinterpret_cast<KaWalk*>(smem + C::HEAD);

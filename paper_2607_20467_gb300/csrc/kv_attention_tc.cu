@@ -33,7 +33,6 @@
 // a time (the next 32 on their way as well spill: 137 us).  Two warps for a tile's 32 rows, half the
 // keys each, were no faster (115 us).  Every wait is bounded (DERR_WAIT_TIMEOUT).
 #include <cuda_fp16.h>
-#include <limits.h>
 
 #include <algorithm>
 #include <type_traits>

@@ -8,6 +8,8 @@
 // for another's longer sequence.
 #pragma once
 
+#include <limits.h>
+
 #include "common.cuh"
 #include "kv_cache.cuh"
 
@@ -72,7 +74,12 @@ struct KaWalk {
   int b;
 };
 
-template <int ROWS, int START>  // rows of an item; positions for its beginning
+// How much longer than a share items may be that are not cut, where all of them are about as long: a cut costs two
+// CTAs a beginning and an end, and a join.  4 bits, us cut / whole: 64 sequences of 1024, 28 / 4 heads, one row
+// 20.8 / 17.8; 8 of 1536, 32 heads, one row 24.1 / 21.2, 16 rows 36.3 / 30.0, 32 rows 47.7 / 44.4.  (6: 16 sequences of
+// 1024 14.3 / 15.3.  Other formats are cut as before.)
+constexpr int KA_KEEP = 5;
+template <int ROWS, int START, int KEEP = 0>  // rows of an item; positions for its beginning
 struct KaLine {
   const KvAttn& a;
   int G, rep, room;
@@ -90,6 +97,7 @@ struct KaLine {
   // This CTA's part (a warp; lane 0 writes it).
   __device__ __forceinline__ void begin(KaWalk* walk, int* err) const {
     const int lane = threadIdx.x & 31;
+    int least = INT_MAX, most = 0;  // an item's positions
     auto scan = [&](int b0, int64_t& own) {  // positions of sequences b0 .. b0 + 31: inclusive prefix
       int row0;
       const int b = b0 + lane;
@@ -97,7 +105,12 @@ struct KaLine {
       if (b < a.batch) {
         const int raw = a.lens[b], nq = seq_rows(b, row0);
         if (raw != min(max(raw, 0), room) && blockIdx.x == 0) report_error(err, DERR_KV_RANGE);
-        if (nq) own = (int64_t)G * tiles_of(nq) * line_of(min(max(raw, 0), room));
+        if (nq) {
+          const int line = line_of(min(max(raw, 0), room));
+          own = (int64_t)G * tiles_of(nq) * line;
+          least = min(least, line);
+          most = max(most, line);
+        }
       }
       int64_t upto = own;
       for (int d = 1; d < 32; d <<= 1) {
@@ -121,6 +134,9 @@ struct KaLine {
       total += __shfl_sync(0xffffffffu, scan(b0, own), 31);
     }
     const KaShare share(total, gridDim.x);
+    // no longer than a share and KEEP (and no shorter, so that no CTA has two): a CTA each
+    const bool whole = KEEP && (int)__reduce_min_sync(0xffffffffu, (unsigned)least) >= share.each + (share.extra > 0) &&
+                       (int)__reduce_max_sync(0xffffffffu, (unsigned)most) <= share.each + KEEP;
     // where the cut before CTA c goes: the position, its sequence and the positions before that
     auto cut = [&](int c, int& b, int64_t& before) -> int64_t {
       const int64_t u = share.start(c);
@@ -137,7 +153,7 @@ struct KaLine {
         const int line = line_of(seq_len(b));
         const int64_t in = u - before;
         const int pos = in < (1ll << 31) ? (int)in % line : (int)(in % line);
-        at = u - pos + KaCut<START>::at(pos, line);
+        at = u - pos + (whole ? (2 * pos < line ? 0 : line) : KaCut<START>::at(pos, line));
         return true;
       };
       int64_t at;

@@ -146,6 +146,12 @@ def test_sequences_that_many_ctas_share(ops, lens, news, heads, kv, hd, wide):
     _check(ops, np.random.default_rng(lens[0]), lens, news, heads, kv, hd, 64, wide=wide)
 
 
+@pytest.mark.parametrize("lens,new", [([768] * 29, 1), ([768] * 28 + [897], 1), ([760, 768] * 14, 3), ([768] * 28 + [100], 2)])
+def test_as_many_items_as_there_are_ctas(ops, lens, new):
+    """Sequences of one length, about a CTA's share (none is cut), of almost one, and one that is none of it."""
+    _check(ops, np.random.default_rng(len(lens) + new), lens, [new] * len(lens), 4, 4, 64, 64)
+
+
 @pytest.mark.parametrize("page_len", [16, 256])
 @pytest.mark.parametrize("hd", [64, 128])
 def test_many_rows_of_a_kv_head(ops, hd, page_len):
