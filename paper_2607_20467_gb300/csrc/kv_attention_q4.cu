@@ -36,6 +36,7 @@ namespace {
 constexpr int K4_START = 2;   // units of keys that beginning an item takes (64 ragged sequences: 3 33.9 us, 2 32.9, 4 34.7)
 constexpr int K4_CTAS = 2;    // CTAs of an SM: one loads while the other begins or ends an item
 constexpr int K4_MOST = 304;  // most CTAs of a launch
+constexpr int K4_ONE = 48;    // parts of an item that are joined at once
 constexpr int K4_KEYS = 32;   // keys that a warp takes at a time
 constexpr float K4_ABOVE = 32.f, K4_SLACK = 8.f;  // the reference above the largest score, and how far that may be passed
 
@@ -88,29 +89,29 @@ __device__ __noinline__ bool any_without_numbers(uint32_t scales, int lane) {
   return __any_sync(0xffffffffu, any);
 }
 
-// The parts of an item, left by its CTAs, joined.  HD / 4 lanes have a row, a lane four of its components, which
+// Parts of an item, left by every stride-th CTA from c0 on, joined: into the rows' results, or (GROUP) into the
+// first of them.  HD / 4 lanes have a row, a lane four of its components, which
 // it copies into shared memory a few parts at a time, the next ones on their way (one takes about 1000
 // cycles here); the parts' {m, l} and then their weights stand there, too.  (The lanes' weights exchanged by
 // shuffles, 25 parts at a time without others on their way: 11000 cycles for 38 parts.)
 template <int HD, int ROWS, int THREADS, int ROOM>
-__device__ __forceinline__ void join4(const KvAttn& a, const KaJoin& it, int rep, const float* parts, uint8_t* smem) {
+__device__ __forceinline__ void join4(const KvAttn& a, const KaJoin& it, int c0, int stride, int n, bool group, int rep, float* parts, uint8_t* smem) {
   using Part = KaPart<HD, ROWS, false>;
   constexpr int LPR = HD / 4, CHUNK = 10;
   static_assert(THREADS / LPR >= ROWS, "a row for every so many threads");
   static_assert(2 * CHUNK * 16 * THREADS + ROWS * K4_MOST * 8 <= ROOM, "shared memory of a join");
-  const int l = threadIdx.x % LPR, r = threadIdx.x / LPR, n = it.parts;
+  const int l = threadIdx.x % LPR, r = threadIdx.x / LPR;
   if (r / (32 / LPR) * (32 / LPR) >= it.rows) return;  // (whole warps)
   const int rr = min(r, it.rows - 1);
-  // (the first CTA's part is its second, the others' their first)
-  const float* first = parts + (2 * (int64_t)it.c0 + 1) * Part::FLOATS;
-  auto part_of = [&](int c) { return first + max(2 * c - 1, 0) * Part::FLOATS; };
+  // (the item's first CTA's part is its second, the others' their first)
+  auto part_of = [&](int c) { return parts + (int64_t)(2 * (c0 + c * stride) + (c == 0 && c0 == it.c0)) * Part::FLOATS; };
   const uint32_t mine = smem_addr(smem) + 16 * threadIdx.x;
   float2* weights = reinterpret_cast<float2*>(smem + 2 * CHUNK * 16 * THREADS) + r * K4_MOST;
-  auto ask = [&](int c0) {
-    const uint32_t to = mine + (c0 / CHUNK & 1) * (CHUNK * 16 * THREADS);
+  auto ask = [&](int at) {
+    const uint32_t to = mine + (at / CHUNK & 1) * (CHUNK * 16 * THREADS);
 #pragma unroll
     for (int i = 0; i < CHUNK; ++i)
-      if (c0 + i < n) copy16(to + 16 * THREADS * i, part_of(c0 + i) + Part::four(rr, l));
+      if (at + i < n) copy16(to + 16 * THREADS * i, part_of(at + i) + Part::four(rr, l));
     copy_commit();
   };
   ask(0);
@@ -134,26 +135,52 @@ __device__ __forceinline__ void join4(const KvAttn& a, const KaJoin& it, int rep
   for (int d = LPR / 2; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
   __syncwarp();
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int c0 = 0; c0 < n; c0 += CHUNK) {
+  for (int at = 0; at < n; at += CHUNK) {
     copy_wait<1>();
-    const uint32_t from = mine + (c0 / CHUNK & 1) * (CHUNK * 16 * THREADS);
+    const uint32_t from = mine + (at / CHUNK & 1) * (CHUNK * 16 * THREADS);
 #pragma unroll
     for (int i = 0; i < CHUNK; ++i) {
-      if (c0 + i >= n) break;
+      if (at + i >= n) break;
       const uint4 y = lds128(from + 16 * THREADS * i);
-      add_scaled(acc, make_float4(__uint_as_float(y.x), __uint_as_float(y.y), __uint_as_float(y.z), __uint_as_float(y.w)), weights[c0 + i].x);
+      add_scaled(acc, make_float4(__uint_as_float(y.x), __uint_as_float(y.y), __uint_as_float(y.z), __uint_as_float(y.w)), weights[at + i].x);
     }
-    ask(c0 + 2 * CHUNK);
+    ask(at + 2 * CHUNK);
   }
   copy_wait<0>();
   __syncwarp();  // (the weights' places are free again)
   if (r >= it.rows) return;
+  if (group) {
+    *reinterpret_cast<float4*>(part_of(0) + Part::four(r, l)) = acc;
+    if (l == 0) *reinterpret_cast<float2*>(part_of(0) + Part::ml(r)) = make_float2(top, sum);
+    return;
+  }
   const int tok = (it.first + r) / rep, at = (it.row0 + tok) * a.H + it.head0 + it.first + r - tok * rep;
   if (a.lse && l == 0) a.lse[at] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
   finish4<HD>(a, KaRow{sum == 0.f ? 0.f : 1.f / sum, at}, 4 * l, acc);
 }
 
-template <int HD>
+// How an item's parts are joined: of more than K4_ONE in groups of about their number's root, each group by its
+// last CTA to come, and the groups' by the last of those (one SM reads parts at about 26 bytes a cycle).
+struct K4Groups {
+  int n, size, groups;
+  __device__ __forceinline__ K4Groups(int n_, bool may) : n(n_), size(n_), groups(1) {
+    if (!may || n <= K4_ONE) return;
+    size = (int)ceilf(sqrtf((float)n));
+    groups = (n + size - 1) / size;
+  }
+  __device__ __forceinline__ int of(int part) const { return groups > 1 ? part / size : 0; }
+  __device__ __forceinline__ int parts(int k) const { return min(size, n - k * size); }
+};
+// Whether this is the last of n to come (one thread of a block, after a barrier).  The block's writes come before it,
+// what a join reads after; the counter is zero again.
+__device__ __forceinline__ bool come(int* count, int n) {
+  int done;
+  asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;" : "=r"(done) : "l"(count) : "memory");
+  if (done == n - 1) *count = 0;
+  return done == n - 1;
+}
+
+template <int HD, bool GROUPS>
 __global__ void __launch_bounds__(K4Cfg<HD>::THREADS, K4_CTAS) kv_attention_q4_kernel(KvPool kv, KvAttn a, KaScratch scratch, int* err) {
   using C = K4Cfg<HD>;
   constexpr int ROWS = C::ROWS, KT = K4_KEYS, SIDE = C::SIDE, ROWB = C::ROWB, CPR = ROWB / 16;
@@ -498,26 +525,43 @@ __global__ void __launch_bounds__(K4Cfg<HD>::THREADS, K4_CTAS) kv_attention_q4_k
       line.sharers(walk, it, c0, c1);
       __syncthreads();
       if (threadIdx.x == 0) {
-        int done;  // (the block's writes, which the barrier ordered before, come first, and what a join reads after)
-        asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;" : "=r"(done) : "l"(scratch.count + c0) : "memory");
-        if (done == c1 - c0) {  // the last to come joins the parts, when it is through with its own
-          scratch.count[c0] = 0;
+        // the last to come joins the parts, those of its group first, when it is through with its own
+        const K4Groups by(c1 - c0 + 1, GROUPS);
+        const int k = by.of(blockIdx.x - c0), at = c0 + k * by.size;
+        if (come(by.groups == 1 ? scratch.count + c0 : scratch.count + K4_MOST + 2 * at + (k == 0), by.parts(k)))
           todo[todo[0].rows++ ? 2 : 1] = KaJoin{it.row0, it.g * rep, it.first, it.rows, c0, c1 - c0 + 1};
-        }
       }
     } else {
       __syncthreads();  // (the rings are free again)
     }
   }
   __syncthreads();
-  for (int i = 0; i < todo[0].rows; ++i) join4<HD, ROWS, C::THREADS, C::ML>(a, todo[1 + i], rep, scratch.part, smem);
+  for (int i = 0; i < todo[0].rows; ++i) {
+    const KaJoin j = todo[1 + i];
+    const K4Groups by(j.parts, GROUPS);
+    const int k = by.of(blockIdx.x - j.c0);
+    bool group = GROUPS && by.groups > 1;
+    int c0 = j.c0 + k * by.size, stride = 1, n = by.parts(k);
+    while (true) {
+      join4<HD, ROWS, C::THREADS, C::ML>(a, j, c0, stride, n, group, rep, scratch.part, smem);
+      if (!GROUPS || !group) break;
+      __syncthreads();
+      if (threadIdx.x == 0) todo[0].parts = come(scratch.count + j.c0, by.groups);
+      __syncthreads();
+      if (!todo[0].parts) break;
+      c0 = j.c0;
+      stride = by.size;
+      n = by.groups;
+      group = false;
+    }
+  }
 }
 
-template <int HD>
+template <int HD, bool GROUPS>
 cudaError_t launch_as(const KvPool& kv, const KvAttn& a, const KaScratch& s, int ctas, int* err, cudaStream_t stream) {
   using C = K4Cfg<HD>;
-  static_assert(2 * C::ROWS * (HD + 4) * 4 <= KV_ATTN_PART_BYTES && K4_MOST * sizeof(int) <= KV_ATTN_COUNTERS, "scratch");
-  auto kern = kv_attention_q4_kernel<HD>;
+  static_assert(2 * C::ROWS * (HD + 4) * 4 <= KV_ATTN_PART_BYTES && 3 * K4_MOST * sizeof(int) <= KV_ATTN_COUNTERS, "scratch");
+  auto kern = kv_attention_q4_kernel<HD, GROUPS>;
   static const cudaError_t set = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM);
   if (set != cudaSuccess) return set;
   kern<<<ctas, C::THREADS, C::SMEM, stream>>>(kv, a, s, err);
@@ -531,7 +575,16 @@ bool kv_attention_q4_few(const KvPool& kv, const KvAttn& a) { return kv.format =
 cudaError_t kv_attention_q4_launch(const KvPool& kv, const KvAttn& a, void* scratch, int sms, int* err, cudaStream_t stream) {
   const int ctas = K4_CTAS * std::min(sms, K4_MOST / K4_CTAS);
   KaScratch s{reinterpret_cast<float*>(static_cast<uint8_t*>(scratch) + KV_ATTN_COUNTERS), static_cast<int*>(scratch)};
-  return kv.hd == 128 ? launch_as<128>(kv, a, s, ctas, err, stream) : launch_as<64>(kv, a, s, ctas, err, stream);
+  // Joins in two steps, in a kernel of their own (the other's calls took 1 % longer with them), where so few long
+  // items may have more parts than K4_ONE.  28 / 4 heads, one row, us in one step / two: 1 x 65536 27.1 / 22.7, 1 x 131072
+  // 33.2 / 30.1; 38 parts an item: 2 x 131071 46.3 / 46.0, 32 / 8 heads 1 x 131072 44.6 / 45.0; 24 parts and fewer 1 to 2 us
+  // longer in two.
+  const bool groups = (int64_t)a.batch * kv.G * K4_ONE < ctas && (int64_t)a.max_pages << kv.page_shift > K4_ONE * KA_LEAST * KA_UNIT;
+  auto as = [&](auto hd) {
+    constexpr int HD = decltype(hd)::value;
+    return groups ? launch_as<HD, true>(kv, a, s, ctas, err, stream) : launch_as<HD, false>(kv, a, s, ctas, err, stream);
+  };
+  return kv.hd == 128 ? as(std::integral_constant<int, 128>{}) : as(std::integral_constant<int, 64>{});
 }
 
 }  // namespace dcl

@@ -152,6 +152,13 @@ def test_as_many_items_as_there_are_ctas(ops, lens, new):
     _check(ops, np.random.default_rng(len(lens) + new), lens, [new] * len(lens), 4, 4, 64, 64)
 
 
+@pytest.mark.parametrize("lens,news,heads,kv,hd", [
+    ([40000], [1], 1, 1, 64), ([33000], [7], 1, 1, 128), ([18000, 29000, 5], [1, 2, 1], 4, 1, 64), ([16500, 0, 29000], [1, 1, 1], 2, 2, 128)])
+def test_joins_in_two_steps(ops, lens, news, heads, kv, hd):
+    """Items that more than 48 CTAs share, beside ones that fewer do."""
+    _check(ops, np.random.default_rng(lens[0]), lens, news, heads, kv, hd, 128)
+
+
 @pytest.mark.parametrize("page_len", [16, 256])
 @pytest.mark.parametrize("hd", [64, 128])
 def test_many_rows_of_a_kv_head(ops, hd, page_len):
