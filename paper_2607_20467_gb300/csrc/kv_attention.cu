@@ -54,7 +54,8 @@ namespace {
 constexpr int KA_START = 3;   // units of keys that beginning an item takes
 constexpr int KA_CTAS = 2;    // CTAs of an SM: one loads while the other begins or ends an item
 constexpr int KA_MOST = 304;  // most CTAs of a launch
-static_assert(KA_MOST * sizeof(int) <= KV_ATTN_COUNTERS, "a counter per CTA");
+static_assert(3 * KA_MOST * sizeof(int) <= KV_ATTN_COUNTERS, "a counter per CTA, and two for groups of parts");
+constexpr int KA_ONE = 10;  // parts of an item that are joined at once (4 bits)
 
 // RS: rows of an item that a lane has (quad + 8 i), 8 rows of the item each.
 template <int HD, KvFormat F, int RS>
@@ -210,7 +211,7 @@ __device__ __forceinline__ int o_place(int c) {
   if (F != KV_BF16) return c + 4 * (c / (HD / 8));
   return (c >> 6) * 96 + ((c >> 3) & 7) * 12 + (c & 7);
 }
-template <int HD, KvFormat F, int RS>
+template <int HD, KvFormat F, int RS, bool GROUPS>
 __global__ void __launch_bounds__(KaCfg<HD, F, RS>::THREADS, KA_CTAS) kv_attention_kernel(KvPool kv, KvAttn a, KaScratch scratch, int* err) {
   using C = KaCfg<HD, F, RS>;
   constexpr int MT = C::MT, SIDE = C::SIDE;
@@ -764,10 +765,17 @@ __global__ void __launch_bounds__(KaCfg<HD, F, RS>::THREADS, KA_CTAS) kv_attenti
       __syncthreads();
       if (threadIdx.x == 0) {
         __threadfence();  // (the block's writes, which the barrier ordered before)
-        const int done = atomicAdd(&scratch.count[c0], 1);
-        if (done == c1 - c0) {  // the last to come joins the parts, when it is through with its own
-          scratch.count[c0] = 0;
-          todo[todo[0].rows++ ? 2 : 1] = KaJoin{it.row0, it.g * rep, it.first, it.rows, c0, c1 - c0 + 1};
+        const KaGroups by(c1 - c0 + 1, GROUPS ? KA_ONE : INT_MAX);
+        if (by.groups > 1) {  // the last of a group to come joins its parts, the last group's all
+          const int k = by.of(blockIdx.x - c0), at = c0 + k * by.size;
+          if (ka_come(scratch.count + KA_MOST + 2 * at + (k == 0), by.parts(k)))
+            todo[todo[0].rows++ ? 2 : 1] = KaJoin{it.row0, it.g * rep, it.first, it.rows, c0, c1 - c0 + 1};
+        } else {
+          const int done = atomicAdd(&scratch.count[c0], 1);
+          if (done == c1 - c0) {  // the last to come joins the parts, when it is through with its own
+            scratch.count[c0] = 0;
+            todo[todo[0].rows++ ? 2 : 1] = KaJoin{it.row0, it.g * rep, it.first, it.rows, c0, c1 - c0 + 1};
+          }
         }
         __threadfence();
       }
@@ -776,19 +784,29 @@ __global__ void __launch_bounds__(KaCfg<HD, F, RS>::THREADS, KA_CTAS) kv_attenti
   }
   for (int i = 0; i < todo[0].rows; ++i) {
     const KaJoin j = todo[1 + i];
-    join_parts<HD, C::ROWS, C::THREADS, false>(a, j, 0, rep, scratch.part, reinterpret_cast<float2*>(smem),
-                                        reinterpret_cast<KaRow*>(smem + C::WT + C::ROWS * 32), threadIdx.x,
-                                        [] { __syncthreads(); });
-    __syncthreads();
+    const KaGroups by(j.parts, GROUPS ? KA_ONE : INT_MAX);
+    const int k = by.of(blockIdx.x - j.c0);
+    KaSome some{j.c0 + k * by.size, 1, by.parts(k), GROUPS && by.groups > 1};
+    while (true) {
+      join_parts<HD, C::ROWS, C::THREADS, false, GROUPS>(a, j, 0, rep, scratch.part, reinterpret_cast<float2*>(smem),
+                                          reinterpret_cast<KaRow*>(smem + C::WT + C::ROWS * 32), threadIdx.x,
+                                          [] { __syncthreads(); }, some);
+      __syncthreads();
+      if (!GROUPS || !some.group) break;
+      if (threadIdx.x == 0) todo[0].parts = ka_come(scratch.count + j.c0, by.groups);
+      __syncthreads();
+      if (!todo[0].parts) break;
+      some = KaSome{j.c0, by.size, by.groups, false};
+    }
   }
 }
 
-template <int HD, KvFormat F, int RS>
+template <int HD, KvFormat F, int RS, bool GROUPS = false>
 cudaError_t launch_as(const KvPool& kv, const KvAttn& a, const KaScratch& s, int ctas, int* err, cudaStream_t stream) {
   using C = KaCfg<HD, F, RS>;
   static_assert(KA_CTAS * (C::SMEM + 1024) <= 233472, "shared memory of an SM");
   static_assert(2 * C::ROWS * (HD + 4) * 4 <= KV_ATTN_PART_BYTES, "scratch per CTA");
-  auto kern = kv_attention_kernel<HD, F, RS>;
+  auto kern = kv_attention_kernel<HD, F, RS, GROUPS>;
   static const cudaError_t set =
       cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM);
   if (set != cudaSuccess) return set;
@@ -801,6 +819,11 @@ cudaError_t launch_rows(const KvPool& kv, const KvAttn& a, const KaScratch& s, i
   const int64_t rows = (int64_t)a.max_new * (a.H / kv.G);
   if constexpr (F != KV_Q4) {  // (4 bits: kv_attention_q4.cu)
     if (rows <= 8) return launch_as<HD, F, 1>(kv, a, s, ctas, err, stream);
+    // Joins in two steps, a kernel of their own, where so few items may have more parts than KA_ONE.  28 / 4 heads, us in one
+    // step / two: 28 rows, 1 x 6000 (12 parts) 30.0 / 26.4, 1 x 16384 (33) 41.5 / 33.3, 1 x 65536 (76) 70.5 / 54.8, 4 x 16384 51.2 /
+    // 44.7; 14 rows 19.3 / 19.7, 26.5 / 23.8, 43.6 / 35.4, 32.4 / 31.4 (9 parts: 18.4 / 20.6).
+  } else if ((int64_t)a.batch * kv.G * ((rows + 31) / 32) * KA_ONE < ctas && (int64_t)a.max_pages << kv.page_shift > KA_ONE * KA_LEAST * KA_UNIT) {
+    return rows <= 16 ? launch_as<HD, F, 2, true>(kv, a, s, ctas, err, stream) : launch_as<HD, F, 4, true>(kv, a, s, ctas, err, stream);
   }
   if (rows <= 16) return launch_as<HD, F, 2>(kv, a, s, ctas, err, stream);
   return launch_as<HD, F, 4>(kv, a, s, ctas, err, stream);

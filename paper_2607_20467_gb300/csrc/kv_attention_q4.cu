@@ -159,27 +159,6 @@ __device__ __forceinline__ void join4(const KvAttn& a, const KaJoin& it, int c0,
   finish4<HD>(a, KaRow{sum == 0.f ? 0.f : 1.f / sum, at}, 4 * l, acc);
 }
 
-// How an item's parts are joined: of more than K4_ONE in groups of about their number's root, each group by its
-// last CTA to come, and the groups' by the last of those (one SM reads parts at about 26 bytes a cycle).
-struct K4Groups {
-  int n, size, groups;
-  __device__ __forceinline__ K4Groups(int n_, bool may) : n(n_), size(n_), groups(1) {
-    if (!may || n <= K4_ONE) return;
-    size = (int)ceilf(sqrtf((float)n));
-    groups = (n + size - 1) / size;
-  }
-  __device__ __forceinline__ int of(int part) const { return groups > 1 ? part / size : 0; }
-  __device__ __forceinline__ int parts(int k) const { return min(size, n - k * size); }
-};
-// Whether this is the last of n to come (one thread of a block, after a barrier).  The block's writes come before it,
-// what a join reads after; the counter is zero again.
-__device__ __forceinline__ bool come(int* count, int n) {
-  int done;
-  asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;" : "=r"(done) : "l"(count) : "memory");
-  if (done == n - 1) *count = 0;
-  return done == n - 1;
-}
-
 template <int HD, bool GROUPS>
 __global__ void __launch_bounds__(K4Cfg<HD>::THREADS, K4_CTAS) kv_attention_q4_kernel(KvPool kv, KvAttn a, KaScratch scratch, int* err) {
   using C = K4Cfg<HD>;
@@ -526,9 +505,9 @@ __global__ void __launch_bounds__(K4Cfg<HD>::THREADS, K4_CTAS) kv_attention_q4_k
       __syncthreads();
       if (threadIdx.x == 0) {
         // the last to come joins the parts, those of its group first, when it is through with its own
-        const K4Groups by(c1 - c0 + 1, GROUPS);
+        const KaGroups by(c1 - c0 + 1, GROUPS ? K4_ONE : INT_MAX);
         const int k = by.of(blockIdx.x - c0), at = c0 + k * by.size;
-        if (come(by.groups == 1 ? scratch.count + c0 : scratch.count + K4_MOST + 2 * at + (k == 0), by.parts(k)))
+        if (ka_come(by.groups == 1 ? scratch.count + c0 : scratch.count + K4_MOST + 2 * at + (k == 0), by.parts(k)))
           todo[todo[0].rows++ ? 2 : 1] = KaJoin{it.row0, it.g * rep, it.first, it.rows, c0, c1 - c0 + 1};
       }
     } else {
@@ -538,7 +517,7 @@ __global__ void __launch_bounds__(K4Cfg<HD>::THREADS, K4_CTAS) kv_attention_q4_k
   __syncthreads();
   for (int i = 0; i < todo[0].rows; ++i) {
     const KaJoin j = todo[1 + i];
-    const K4Groups by(j.parts, GROUPS);
+    const KaGroups by(j.parts, GROUPS ? K4_ONE : INT_MAX);
     const int k = by.of(blockIdx.x - j.c0);
     bool group = GROUPS && by.groups > 1;
     int c0 = j.c0 + k * by.size, stride = 1, n = by.parts(k);
@@ -546,7 +525,7 @@ __global__ void __launch_bounds__(K4Cfg<HD>::THREADS, K4_CTAS) kv_attention_q4_k
       join4<HD, ROWS, C::THREADS, C::ML>(a, j, c0, stride, n, group, rep, scratch.part, smem);
       if (!GROUPS || !group) break;
       __syncthreads();
-      if (threadIdx.x == 0) todo[0].parts = come(scratch.count + j.c0, by.groups);
+      if (threadIdx.x == 0) todo[0].parts = ka_come(scratch.count + j.c0, by.groups);
       __syncthreads();
       if (!todo[0].parts) break;
       c0 = j.c0;

@@ -636,7 +636,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
       KaJoin k = j;
       k.first += r0;
       k.rows = min(some, j.rows - r0);
-      join_parts<HD, TC_ROWS, TC_THREADS, true>(a, k, r0, rep, scratch.part,
+      join_parts<HD, TC_ROWS, TC_THREADS, true, false>(a, k, r0, rep, scratch.part,
                                           reinterpret_cast<float2*>(smem + TC_ROWS * 8), reinterpret_cast<KaRow*>(smem),
                                           threadIdx.x, [] { __syncthreads(); });
       __syncthreads();

@@ -231,6 +231,28 @@ struct KaScratch {
   int* count;   // [CTAs], by the CTA that begins the item; zero between launches
 };
 
+// How an item's parts are joined: of more than `one` in groups of about their number's root, each group by its
+// last CTA to come, and the groups' by the last of those (one SM reads parts at about 26 bytes a cycle).  A group's
+// counter, beside an item's: of the CTA where it begins, which is an item's first (k = 0) or not.
+struct KaGroups {
+  int n, size, groups;
+  __device__ __forceinline__ KaGroups(int n_, int one) : n(n_), size(n_), groups(1) {
+    if (n <= one) return;
+    size = (int)ceilf(sqrtf((float)n));
+    groups = (n + size - 1) / size;
+  }
+  __device__ __forceinline__ int of(int part) const { return groups > 1 ? part / size : 0; }
+  __device__ __forceinline__ int parts(int k) const { return min(size, n - k * size); }
+};
+// Whether this is the last of n to come (one thread of a block, after a barrier).  The block's writes come before it,
+// what a join reads after; the counter is zero again.
+__device__ __forceinline__ bool ka_come(int* count, int n) {
+  int done;
+  asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;" : "=r"(done) : "l"(count) : "memory");
+  if (done == n - 1) *count = 0;
+  return done == n - 1;
+}
+
 // A joined row: 1 / l (0 for a row that sees nothing), and its place in the output.
 struct KaRow {
   float inv;
@@ -341,16 +363,27 @@ __device__ __forceinline__ float part_half(float m, float top) { return m == -IN
 // every part's {m, l} into shared memory (w, [rows][parts]) at once, a row's weights by a thread or
 // a warp (what its components need in row); then four components of a row a thread, 12 to 16 loads in
 // flight (one takes about 1000 cycles here: a warp per row, part after part, took 35000 for 38
-// parts and 17000 for two parts of 32 rows).  it's rows begin at row r0 of the parts.
-template <int HD, int ROWS, int THREADS, bool BY_FOUR, typename Sync>
-__device__ __forceinline__ void join_parts(const KvAttn& a, const KaJoin& it, int r0, int rep, const float* parts, float2* w,
-                                           KaRow* row, int tid, Sync sync) {
+// parts and 17000 for two parts of 32 rows).  it's rows begin at row r0 of the parts.  STEPS: of some of the parts, into
+// the first of them (a group) or the rows' results.
+struct KaSome {
+  int c0, stride, n;  // those of every stride-th CTA from c0 on
+  bool group;
+};
+template <int HD, int ROWS, int THREADS, bool BY_FOUR, bool STEPS, typename Sync>
+__device__ __forceinline__ void join_parts(const KvAttn& a, const KaJoin& it, int r0, int rep, float* parts, float2* w,
+                                           KaRow* row, int tid, Sync sync, const KaSome& some = {}) {
   using P = KaPart<HD, ROWS, BY_FOUR>;
   constexpr int Q = HD / 4;
-  const int warp = tid >> 5, lane = tid & 31, n = it.parts;
-  // (the first CTA's part is its second, the others' their first)
-  const float* first = parts + (2 * (int64_t)it.c0 + 1) * P::FLOATS;
-  auto part_of = [&](int c) { return first + (int64_t)max(2 * c - 1, 0) * P::FLOATS; };
+  const int warp = tid >> 5, lane = tid & 31, n = STEPS ? some.n : it.parts;
+  // (the item's first CTA's part is its second, the others' their first)
+  const int c0 = STEPS ? some.c0 : it.c0, begins = !STEPS || c0 == it.c0;
+  float* first = parts + (2 * (int64_t)c0 + begins) * P::FLOATS;
+  auto part_at = [&](int c) { return (int64_t)max(2 * c * (STEPS ? some.stride : 1) - begins, 0) * P::FLOATS; };
+  auto part_of = [&](int c) { return first + part_at(c); };
+  auto done = [&](int r, float top, float sum) {
+    if (STEPS && some.group) *reinterpret_cast<float2*>(first + P::ml(r0 + r)) = make_float2(top, sum);
+    else row[r] = finish_row(a, it.row0, it.head0, it.first, rep, r, top, sum);
+  };
   for (int i = tid; i < it.rows * n; i += THREADS) {
     const int c = i / it.rows, r = i - c * it.rows;
     w[r * n + c] = __ldcg(reinterpret_cast<const float2*>(part_of(c) + P::ml(r0 + r)));
@@ -367,7 +400,7 @@ __device__ __forceinline__ void join_parts(const KvAttn& a, const KaJoin& it, in
         wr[c].x = half * half;
         sum = fmaf(x.y * half, half, sum);
       }
-      row[r] = finish_row(a, it.row0, it.head0, it.first, rep, r, top, sum);
+      done(r, top, sum);
     }
   } else {
     for (int r = warp; r < it.rows; r += THREADS / 32) {
@@ -382,7 +415,7 @@ __device__ __forceinline__ void join_parts(const KvAttn& a, const KaJoin& it, in
         sum = fmaf(x.y * half, half, sum);
       }
       sum = warp_sum(sum);
-      if (lane == 0) row[r] = finish_row(a, it.row0, it.head0, it.first, rep, r, top, sum);
+      if (lane == 0) done(r, top, sum);
     }
   }
   sync();
@@ -411,7 +444,7 @@ __device__ __forceinline__ void join_parts(const KvAttn& a, const KaJoin& it, in
         for (int i = 0; i < U; ++i)  // (past the end: the last again, without weight)
 #pragma unroll
           for (int k = 0; k < T; ++k)
-            y[k][i] = __ldcg(reinterpret_cast<const float4*>(from[k] + (int64_t)max(2 * min(c + i, n - 1) - 1, 0) * P::FLOATS));
+            y[k][i] = __ldcg(reinterpret_cast<const float4*>(from[k] + part_at(min(c + i, n - 1))));
 #pragma unroll
         for (int i = 0; i < U; ++i)
 #pragma unroll
@@ -422,7 +455,8 @@ __device__ __forceinline__ void join_parts(const KvAttn& a, const KaJoin& it, in
       for (int k = 0; k < T; ++k) {
         const int t = t0 + k * THREADS;
         if (t >= all) break;
-        if (!BY_FOUR || row_of(t) < it.rows) finish4<HD>(a, row[row_of(t)], 4 * four_of(t), acc[k]);
+        if (STEPS && some.group) *reinterpret_cast<float4*>(first + P::four(r0 + row_of(t), four_of(t))) = acc[k];
+        else if (!BY_FOUR || row_of(t) < it.rows) finish4<HD>(a, row[row_of(t)], 4 * four_of(t), acc[k]);
       }
     }
   };

@@ -153,9 +153,10 @@ def test_as_many_items_as_there_are_ctas(ops, lens, new):
 
 
 @pytest.mark.parametrize("lens,news,heads,kv,hd", [
+    ([9000], [3], 5, 1, 64), ([7000], [29], 1, 1, 128), ([6100, 9300, 50], [8, 4, 1], 3, 1, 128), ([6000, 15000], [14, 2], 1, 1, 64),
     ([40000], [1], 1, 1, 64), ([33000], [7], 1, 1, 128), ([18000, 29000, 5], [1, 2, 1], 4, 1, 64), ([16500, 0, 29000], [1, 1, 1], 2, 2, 128)])
 def test_joins_in_two_steps(ops, lens, news, heads, kv, hd):
-    """Items that more than 48 CTAs share, beside ones that fewer do."""
+    """Items that more than 10 CTAs share (48 of up to 8 rows), beside ones that fewer do."""
     _check(ops, np.random.default_rng(lens[0]), lens, news, heads, kv, hd, 128)
 
 
