@@ -14,12 +14,12 @@
 // above the largest score and moves seldom, as in kv_attention.cu with bf16 pages.  Work is shared out and
 // joined as there (kv_share.cuh).
 //
-// 28 / 4 heads of 128, one row a sequence: 2 sequences of 131071 positions (143 MB) in 46.0 us, 3.1 TB/s, 0.46 of the
-// measured copy rate; 64 ragged sequences to 4096 (74 MB) in 32.9 us; one of 512, 32 heads, 7.7 us.  A warp takes
+// 28 / 4 heads of 128, one row a sequence: 2 sequences of 131071 positions (143 MB) in 45.8 us, 3.1 TB/s, 0.46 of the
+// measured copy rate; 64 ragged sequences to 4096 (74 MB) in 32.8 us; one of 512, 32 heads, 7.7 us.  A warp takes
 // 197 instructions for 8 keys and their values, 94 of them on the integer pipe, which has one for two cycles: 56
-// bring codes into place (a shift and a mask for two components), and that pipe is 0.7 to 0.8 busy while keys
-// are walked.  The rest of a CTA's time: 4400 cycles to find its part of the line, 5000 until its first keys
-// are there, 4000 an item's end, 2800 a join of two parts.  (Keys and values on the N side, as for wider
+// bring codes into place (a shift and a mask for two components), and that pipe is 0.6 to 0.8 busy while keys
+// are walked.  The rest of a CTA's time: 3900 cycles to find its part of the line, 4700 until its first keys
+// are there, 2700 an item's end, 2800 a join of two parts.  (Keys and values on the N side, as for wider
 // formats: 57.5 us and 39.7.  Shifts by multiplication, for the other pipe: 53.6.  16 rows a pass this way
 // round: 8 sequences of 1536, 32 heads, 32 rows 52 us, 47.5 in kv_attention.cu, both cut.)
 #include <algorithm>

@@ -45,7 +45,7 @@ struct KvAttn {
 // bits, for up to 32 rows, and for more (not causal, or 4 bits).  Scratch of a launch on `sms` SMs: counters, zero before
 // the first launch and left zero by each, then the parts of rows whose keys several CTAs share.  The launches of a
 // context run one after another on its stream, so that all use the same.
-constexpr size_t KV_ATTN_COUNTERS = 4096;                                      // bytes (an int per CTA)
+constexpr size_t KV_ATTN_COUNTERS = 4096;                                      // bytes (up to three ints a CTA)
 constexpr size_t KV_ATTN_PART_BYTES = 2 * 32 * (128 + 4) * sizeof(float);      // per CTA
 constexpr size_t KV_ATTN_TC_PART_BYTES = 2 * 256 * (128 + 4) * sizeof(float);
 bool kv_attention_q4_few(const KvPool& kv, const KvAttn& a);
