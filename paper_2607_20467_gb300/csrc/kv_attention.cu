@@ -235,7 +235,7 @@ __global__ void __launch_bounds__(KaCfg<HD, F, RS>::THREADS, KA_CTAS) kv_attenti
   const uint32_t v_at[2] = {chunk4_at<C::ROWB>(2 * place, quad * (HD / 16) >> 4) + (quad * (HD / 16) & 15),
                             chunk4_at<C::ROWB>(2 * place + 1, quad * (HD / 16) >> 4) + (quad * (HD / 16) & 15)};
 
-  const KaLine<C::ROWS, KA_START, Q4 ? KA_KEEP : 0> line(kv, a);
+  const KaLine<C::ROWS, KA_START, Q4 ? KA_KEEP : 0, Q4 ? KA_FINE : KA_LEAST> line(kv, a);
 
   // ---- this CTA's part of the line of all items
   KaWalk& shared_walk = *reinterpret_cast<KaWalk*>(smem + C::HEAD);
@@ -820,9 +820,9 @@ cudaError_t launch_rows(const KvPool& kv, const KvAttn& a, const KaScratch& s, i
   if constexpr (F != KV_Q4) {  // (4 bits: kv_attention_q4.cu)
     if (rows <= 8) return launch_as<HD, F, 1>(kv, a, s, ctas, err, stream);
     // Joins in two steps, a kernel of their own, where so few items may have more parts than KA_ONE.  28 / 4 heads, us in one
-    // step / two: 28 rows, 1 x 6000 (12 parts) 30.0 / 26.4, 1 x 16384 (33) 41.5 / 33.3, 1 x 65536 (76) 70.5 / 54.8, 4 x 16384 51.2 /
+    // step / two, cut as other formats: 28 rows, 1 x 6000 (12 parts) 30.0 / 26.4, 1 x 16384 (33) 41.5 / 33.3, 1 x 65536 (76) 70.5 / 54.8, 4 x 16384 51.2 /
     // 44.7; 14 rows 19.3 / 19.7, 26.5 / 23.8, 43.6 / 35.4, 32.4 / 31.4 (9 parts: 18.4 / 20.6).
-  } else if ((int64_t)a.batch * kv.G * ((rows + 31) / 32) * KA_ONE < ctas && (int64_t)a.max_pages << kv.page_shift > KA_ONE * KA_LEAST * KA_UNIT) {
+  } else if ((int64_t)a.batch * kv.G * ((rows + 31) / 32) * KA_ONE < ctas && (int64_t)a.max_pages << kv.page_shift > KA_ONE * KA_FINE * KA_UNIT) {
     return rows <= 16 ? launch_as<HD, F, 2, true>(kv, a, s, ctas, err, stream) : launch_as<HD, F, 4, true>(kv, a, s, ctas, err, stream);
   }
   if (rows <= 16) return launch_as<HD, F, 2>(kv, a, s, ctas, err, stream);
@@ -838,7 +838,7 @@ cudaError_t launch_rows(const KvPool& kv, const KvAttn& a, const KaScratch& s, i
 // there, FP8, 28 / 4 heads of 128: 16 x 8192 positions, 224 rows a kv head 301 / 105; 8 x 3000: 63 rows
 // 35 / 34, 112 53 / 37, 224 74 / 48; 4 x 8192 (ten parts an item): 63 rows 50 / 45, 112 61 / 54, 224 90 / 79;
 // 1 x 16384, 224 rows 62 / 123; 2 x 1000, 224 rows 24 / 35.  Causal, 4 bits (there only of 4 bits): 4 x 8192, 448 rows
-// 155 / 84; 16 x 1024 90 / 49; 8 x 4096, 112 rows 58 / 45.  Over 276 shapes (four head layouts, both formats) the rule
+// 155 / 84; 16 x 1024 90 / 40; 8 x 4096, 112 rows 58 / 44.  Over 276 shapes (four head layouts, both formats) the rule
 // takes 0.8 % longer than the better kernel on average, more than 7 % longer in 13.  Lengths are known to the
 // device only: the page table's width stands for them.
 bool kv_attention_many_rows(const KvPool& kv, const KvAttn& a) {

@@ -187,7 +187,7 @@ __global__ void __launch_bounds__(K4Cfg<HD>::THREADS, K4_CTAS) kv_attention_q4_k
   const int k_group = place * SIDE / 4, v_group = quad * SIDE / 8;
   const float qa = fmaxf(a.scale * kLog2e, 1.2e-38f);  // (not 0: a masked score is -inf)
 
-  const KaLine<ROWS, K4_START, KA_KEEP> line(kv, a);
+  const KaLine<ROWS, K4_START, KA_KEEP, KA_FINE> line(kv, a);
 
   // ---- this CTA's part of the line of all items
   KaWalk& shared_walk = *reinterpret_cast<KaWalk*>(smem + C::HEAD);
@@ -558,7 +558,7 @@ cudaError_t kv_attention_q4_launch(const KvPool& kv, const KvAttn& a, void* scra
   // items may have more parts than K4_ONE.  28 / 4 heads, one row, us in one step / two: 1 x 65536 27.1 / 22.7, 1 x 131072
   // 33.2 / 30.1; 38 parts an item: 2 x 131071 46.3 / 46.0, 32 / 8 heads 1 x 131072 44.6 / 45.0; 24 parts and fewer 1 to 2 us
   // longer in two.
-  const bool groups = (int64_t)a.batch * kv.G * K4_ONE < ctas && (int64_t)a.max_pages << kv.page_shift > K4_ONE * KA_LEAST * KA_UNIT;
+  const bool groups = (int64_t)a.batch * kv.G * K4_ONE < ctas && (int64_t)a.max_pages << kv.page_shift > K4_ONE * KA_FINE * KA_UNIT;
   auto as = [&](auto hd) {
     constexpr int HD = decltype(hd)::value;
     return groups ? launch_as<HD, true>(kv, a, s, ctas, err, stream) : launch_as<HD, false>(kv, a, s, ctas, err, stream);

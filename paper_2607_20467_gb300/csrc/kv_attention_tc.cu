@@ -25,7 +25,7 @@
 //
 // The same in 4 bits (79 MB): 114 us; its codes cost the copying warps no more than FP8's.  Causal, 4 bits only
 // (a kernel of its own, as what it takes slowed the other by 2 %): 8 sequences of 2048 positions, the last 256 of
-// them new, 113 us (not causal 108); 4 x 8192, 64 new, 84 us, where 32 rows a pass take 155.
+// them new, 113 us (not causal 108); 4 x 8192, 64 new, 84 us, where 32 rows a pass take 155.  (Cut as finely as few rows are: 111 us, but 64 x 512, 32 new 58 for 49.)
 //
 // Roles (544 threads): warps 0-3 and 4-7 have the rows of the two tiles; warps 8-11 copy and widen
 // keys, 12-15 values (one group for both was the slowest link: 7800 cycles a unit); warp 16
@@ -209,7 +209,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::HOLDER + 4);
   KaWalk& shared_walk = *reinterpret_cast<KaWalk*>(smem + C::WALK);
   KaJoin* todo = reinterpret_cast<KaJoin*>(smem + C::TODO);
-  const KaLine<TC_ROWS, TC_START> line(kv, a);
+  const KaLine<TC_ROWS, TC_START, F == KV_Q4 ? KA_KEEP : 0> line(kv, a);
 
   if (warp == 0) line.begin(&shared_walk, err);
   if (warp == 16) {

@@ -20,12 +20,16 @@ constexpr int KA_UNIT = 128;  // keys of a unit of work
 // START: units that beginning an item takes.  Sharing an item costs each of its CTAs the writing of a
 // part and one of them the join (for up to 32 rows 3 and 4 to 20 thousand cycles; a unit of 16 rows
 // takes about 1500).  So a cut that falls less than START + 3 positions after an item's beginning or
-// START + 1 before its end goes there, and a CTA has at least KA_LEAST positions where the launch is
-// small.
+// START + 1 before its end (KA_FINE: START + 1, 2) goes there, and a CTA has at least KA_LEAST positions where the
+// launch is small.
 constexpr int KA_LEAST = 4;
-template <int START>
+// 4 bits, up to 32 rows: finer, as few units of work take long beside what a cut costs.  us with the others' cuts /
+// these, 28 / 4 heads: one row, 1 x 1000 10.9 / 8.8, 1 x 4096 11.9 / 9.8, 1 x 16384 17.3 / 13.9, 16 x 1000 14.5 / 11.2; 28
+// rows, 1 x 1000 22.6 / 16.7, 1 x 16384 33.6 / 28.6, 20 ragged to 1500 26.8 / 19.7; 64 ragged to 4096, one row 32.7 / 32.5.  (Shares of one unit: 28 rows, 1 x 16384 39; cuts a unit before an end: 1 x 2000, 28 rows 22.7 for 18.5.)
+constexpr int KA_FINE = 2;
+template <int START, int LEAST>
 struct KaCut {
-  static constexpr int LOW = START + 3, HIGH = START + 1;
+  static constexpr int LOW = START + (LEAST < KA_LEAST ? 1 : 3), HIGH = LEAST < KA_LEAST ? 2 : START + 1;
   static __device__ __forceinline__ int at(int pos, int line) {
     if (line < LOW + HIGH) return 2 * pos < line ? 0 : line;
     return pos < LOW ? 0 : pos > line - HIGH ? line : pos;
@@ -37,8 +41,8 @@ struct KaCut {
 struct KaShare {
   int64_t each;
   int extra, n;
-  __device__ KaShare(int64_t total, int ctas) {
-    n = (int)min((int64_t)ctas, (total + KA_LEAST - 1) / KA_LEAST);  // (CTAs past it have nothing)
+  __device__ KaShare(int64_t total, int ctas, int least) {
+    n = (int)min((int64_t)ctas, (total + least - 1) / least);  // (CTAs past it have nothing)
     if (total < (1ll << 31)) {
       each = n ? (int)total / n : 0;
     } else {
@@ -76,10 +80,10 @@ struct KaWalk {
 
 // How much longer than a share items may be that are not cut, where all of them are about as long: a cut costs two
 // CTAs a beginning and an end, and a join.  4 bits, us cut / whole: 64 sequences of 1024, 28 / 4 heads, one row
-// 20.8 / 17.8; 8 of 1536, 32 heads, one row 24.1 / 21.2, 16 rows 36.3 / 30.0, 32 rows 47.7 / 44.4.  (6: 16 sequences of
-// 1024 14.3 / 15.3.  Other formats are cut as before.)
+// 20.8 / 17.8; 8 of 1536, 32 heads, one row 24.1 / 21.2, 16 rows 36.3 / 30.0, 32 rows 47.7 / 44.4; 16 of 1024,
+// 28 / 4 heads, 448 rows 48.6 / 40.0.  (6: 16 sequences of 1024, one row 14.3 / 15.3.  Other formats are always cut.)
 constexpr int KA_KEEP = 5;
-template <int ROWS, int START, int KEEP = 0>  // rows of an item; positions for its beginning
+template <int ROWS, int START, int KEEP = 0, int LEAST = KA_LEAST>  // rows of an item; positions for its beginning
 struct KaLine {
   const KvAttn& a;
   int G, rep, room;
@@ -133,7 +137,7 @@ struct KaLine {
       int64_t own;
       total += __shfl_sync(0xffffffffu, scan(b0, own), 31);
     }
-    const KaShare share(total, gridDim.x);
+    const KaShare share(total, gridDim.x, LEAST);
     // no longer than a share and KEEP (and no shorter, so that no CTA has two): a CTA each
     const bool whole = KEEP && (int)__reduce_min_sync(0xffffffffu, (unsigned)least) >= share.each + (share.extra > 0) &&
                        (int)__reduce_max_sync(0xffffffffu, (unsigned)most) <= share.each + KEEP;
@@ -153,7 +157,7 @@ struct KaLine {
         const int line = line_of(seq_len(b));
         const int64_t in = u - before;
         const int pos = in < (1ll << 31) ? (int)in % line : (int)(in % line);
-        at = u - pos + (whole ? (2 * pos < line ? 0 : line) : KaCut<START>::at(pos, line));
+        at = u - pos + (whole ? (2 * pos < line ? 0 : line) : KaCut<START, LEAST>::at(pos, line));
         return true;
       };
       int64_t at;
@@ -210,9 +214,9 @@ struct KaLine {
   }
   // The CTAs c0 .. c1 that share an item that is not whole.
   __device__ __forceinline__ void sharers(const KaWalk& w, const KaItem& it, int& c0, int& c1) const {
-    const KaShare share(w.total, gridDim.x);
-    c0 = share.owner(it.item0 + KaCut<START>::LOW - 1);
-    c1 = share.owner(it.item0 + it.line - KaCut<START>::HIGH);
+    const KaShare share(w.total, gridDim.x, LEAST);
+    c0 = share.owner(it.item0 + KaCut<START, LEAST>::LOW - 1);
+    c1 = share.owner(it.item0 + it.line - KaCut<START, LEAST>::HIGH);
   }
 };
 
