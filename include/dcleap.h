@@ -392,13 +392,15 @@ typedef struct {
  *      with a sequence are there; one whose pages are not gets none, keeps what it has and gets no rows
  *      (q_start_dev tells), and so do those after it that lack any.
  *   3. q_start_dev [batch + 1]: the rows of sequence b are [q_start[b], q_start[b + 1]); seq_len_dev
- *      [batch]: start + new (start for one that got no rows): what dcl_kv_attention takes; it may be
- *      start_dev itself, for a next step that goes on from there.  Nothing else overlaps.  slot_dev,
- *      pos_dev [n_rows]: the slot (for dcl_kv_write) and position (for dcl_qk_norm_rope) of every row,
- *      -1 for rows past the last sequence's, so that a captured step may have room for more rows.
- * A sequence whose numbers are negative or past its table, more rows than n_rows (those past it are
- * left out), a page outside the pool (its rows get slot -1) and a stack that holds fewer than none or
- * more than n_pages (no sequence gets rows, no page moves) are recorded as device-side faults.
+ *      [batch]: start + new, what dcl_kv_attention takes; it may be start_dev itself, for a next step that
+ *      goes on from there.  Nothing else overlaps.  slot_dev, pos_dev [n_rows]: the slot (for dcl_kv_write) and
+ *      position (for dcl_qk_norm_rope) of every row, -1 for rows past the last sequence's, so that a
+ *      captured step may have room for more rows.
+ * A sequence that is given no rows (by 2, or as its numbers or the stack are not right) has seq_len start, or 0
+ * where start is no position of its table.  Recorded as device-side faults are: a sequence whose start, new or
+ * held is negative or past its table (it keeps its pages and gets no rows), a stack that holds fewer than none or
+ * more than n_pages (no sequence gets rows, no page moves), a page outside the pool (its rows get slot -1), and
+ * more rows than n_rows (those past it are left out; their sequences have the pages, and seq_len counts them).
  * Errors: INVALID_ARG, CUDA. */
 dcl_status dcl_kv_plan(dcl_ctx* ctx, const dcl_kv_pages* pages, const int32_t* start_dev, const int32_t* new_dev,
                        int32_t* q_start_dev, int32_t* seq_len_dev, int32_t* slot_dev, int32_t* pos_dev,

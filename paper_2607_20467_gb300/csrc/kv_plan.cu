@@ -23,7 +23,8 @@ constexpr int KP_CLUSTER = 8;
 constexpr int KP_STARTS = 2048;  // sequences whose first rows and positions are kept in shared memory
 constexpr int KP_ROW_THREADS = 256;
 
-// A sequence's numbers; one that is not within its table gets no rows and keeps what it has.
+// A sequence's numbers; one that is not within its table gets no rows and keeps what it has: its pages, and its
+// start, which is 0 only where that is no position of the table.
 struct KpSeq {
   int start, rows, held, need;
   bool bad;
@@ -37,9 +38,11 @@ __device__ __forceinline__ KpSeq kp_seq(const KvPlan& a, int b) {
   s.start = a.start[b];
   s.rows = a.rows_new[b];
   s.held = min(max(held, 0), a.max_pages);
-  s.bad = held != s.held || s.start < 0 || s.rows < 0 || (int64_t)s.start + s.rows > (int64_t)a.max_pages << a.page_shift;
+  const int64_t room = (int64_t)a.max_pages << a.page_shift;
+  s.bad = held != s.held || s.start < 0 || s.rows < 0 || (int64_t)s.start + s.rows > room;
   if (s.bad) {
-    s.start = s.rows = 0;
+    if (s.start < 0 || s.start > room) s.start = 0;
+    s.rows = 0;
     s.need = s.held;
   } else {
     s.need = (int)(((int64_t)s.start + s.rows + (1 << a.page_shift) - 1) >> a.page_shift);
