@@ -13,6 +13,16 @@ def pytest_configure(config):
     config.addinivalue_line("markers", "slow: long-running CPU test")
 
 
+# Cases that expect a length of 0 of a sequence that does not fit its table, where the header gives it its start: they
+# fail, and run last, so that a run that ends at its first failure has run all the others.
+LAST = ("test_a_sequence_past_its_table_is_reported_and_left_out[3--2]",
+        "test_a_sequence_past_its_table_is_reported_and_left_out[40-9]")
+
+
+def pytest_collection_modifyitems(items):
+    items.sort(key=lambda item: item.name in LAST)
+
+
 @pytest.fixture(scope="session")
 def golden_dir():
     return os.path.join(ROOT, "tests", "golden")
