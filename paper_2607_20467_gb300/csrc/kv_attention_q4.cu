@@ -218,7 +218,7 @@ __global__ void __launch_bounds__(K4Cfg<HD>::THREADS, K4_CTAS) kv_attention_q4_k
 
     const uint32_t head_at = (uint32_t)(it.g * P * ROWB);
     // ---- this warp's steps: keys key0 + KT warp on, then every WARPS-th
-    const int stop = min(key1, lim_max);
+    const int stop = max(0, min(key1, lim_max));  // (rows that see nothing may be before key 0)
     const int* table = a.table + (int64_t)it.b * a.max_pages;
     int next = key0 + KT * warp;  // first key of the next step to copy
     uint32_t bad = 0;             // two bits a stage: 16 keys whose page is not the cache's
