@@ -272,7 +272,8 @@ class KvCache:
             raise ValueError("an FP8 cache needs k_exp and v_exp, a 4-bit one its scales in their place")
         if not small and (k_exp is not None or v_exp is not None):
             raise ValueError("a bf16 cache has no exponents")
-        q4 = small and len(k_exp.shape) == 4 and 16 * k_exp.shape[3] == hd  # (hd / 2 bytes of codes, hd / 32 scales)
+        side_shape = tuple(getattr(k_exp, "shape", ()))  # (a raw address has none)
+        q4 = small and len(side_shape) == 4 and 16 * side_shape[3] == hd  # (hd / 2 bytes of codes, hd / 32 scales)
         n, kind = pages * heads * page_len, "u8" if q4 else "e4m3" if small else "bf16"
         if tuple(v.shape) != tuple(k.shape):
             raise ValueError("k and v differ in shape")
@@ -281,8 +282,9 @@ class KvCache:
             hd *= 2
             side = n * (hd // 32)
             for t, name in ((k_exp, "k_exp"), (v_exp, "v_exp")):
-                if tuple(t.shape) != (pages, heads, page_len, hd // 32):
-                    raise ValueError(f"{name}: [pages][kv heads][page_len][head_dim / 32] scales expected, got {tuple(t.shape)}")
+                shape = tuple(getattr(t, "shape", ()))
+                if shape != (pages, heads, page_len, hd // 32):
+                    raise ValueError(f"{name}: [pages][kv heads][page_len][head_dim / 32] scales expected, got {shape}")
         self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
         self.n_pages, self.n_kv_heads, self.page_len, self.head_dim = pages, heads, page_len, hd
         self.format = DCL_KV_Q4 if q4 else DCL_KV_FP8 if small else DCL_KV_BF16
