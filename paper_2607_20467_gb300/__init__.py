@@ -260,8 +260,8 @@ class KvCache:
     """A paged key / value cache of one layer in the caller's tensors (dcl_kv_cache): k, v
     [pages][kv heads][page_len][head_dim], bf16, or 1-byte E4M3 codes with k_exp, v_exp int8
     [pages][kv heads][page_len], or 4-bit codes uint8 [pages][kv heads][page_len][head_dim / 2] with
-    scale bytes k_exp, v_exp uint8 [pages][kv heads][page_len][head_dim / 32].  ``KvCache.empty``
-    allocates one."""
+    scale bytes k_exp, v_exp uint8 [pages][kv heads][page_len][head_dim / 32], a shape that tells them from
+    exponents: as many bytes in another are refused.  ``KvCache.empty`` allocates one."""
 
     def __init__(self, k, v, k_exp=None, v_exp=None):
         if len(k.shape) != 4:
@@ -285,6 +285,11 @@ class KvCache:
                 shape = tuple(getattr(t, "shape", ()))
                 if shape != (pages, heads, page_len, hd // 32):
                     raise ValueError(f"{name}: [pages][kv heads][page_len][head_dim / 32] scales expected, got {shape}")
+        elif small and hd in (32, 64) and "float8" not in str(k.dtype):  # (4-bit codes of 64 or 128 components have as many bytes)
+            for t, name in ((k_exp, "k_exp"), (v_exp, "v_exp")):
+                if hasattr(t, "shape") and t.numel() == n * (hd // 16):
+                    raise ValueError(f"{name}: {n * (hd // 16)} bytes are scales of a 4-bit cache, which are [pages][kv heads][page_len]"
+                                     f"[head_dim / 32], or more than the {n} exponents of an FP8 one; got {tuple(t.shape)}")
         self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
         self.n_pages, self.n_kv_heads, self.page_len, self.head_dim = pages, heads, page_len, hd
         self.format = DCL_KV_Q4 if q4 else DCL_KV_FP8 if small else DCL_KV_BF16
