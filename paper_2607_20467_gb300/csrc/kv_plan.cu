@@ -20,7 +20,8 @@ namespace dcl {
 namespace {
 
 constexpr int KP_CLUSTER = 8;
-constexpr int KP_STARTS = 2048;  // sequences whose first rows and positions are kept in shared memory
+constexpr int KP_ONE_SEQS = 256, KP_ONE_ROWS = 4096;  // most of a step that one block lays out (kv_plan_launch)
+constexpr int KP_STARTS = 2048;  // sequences whose first rows and positions the rows' kernel keeps in shared memory
 constexpr int KP_ROW_THREADS = 256;
 
 // A sequence's numbers; one that is not within its table gets no rows and keeps what it has: its pages, and its
@@ -137,7 +138,8 @@ __global__ void __launch_bounds__(T) kv_plan_kernel(KvPlan a, int* err) {
   __shared__ int64_t sums[2][T / 32];
   __shared__ int64_t off[T];             // where a sequence's pages go to, or come from
   __shared__ int first[T], count[T];     // its first page to give or take, and how many
-  __shared__ int starts[KP_STARTS + 1], keeps[KP_STARTS];
+  constexpr int KEPT = ROWS_TOO ? KP_ONE_SEQS : 0;  // what the rows here need of the sequences
+  __shared__ int starts[KEPT + 1], keeps[KEPT + 1];
   __shared__ int most;                   // pages taken
   const int tid = threadIdx.x, lane = tid & 31;
   const int rank = CTAS > 1 ? (int)blockIdx.x : 0, warp = rank * (T / 32) + (tid >> 5);  // (one cluster is the grid)
@@ -151,7 +153,8 @@ __global__ void __launch_bounds__(T) kv_plan_kernel(KvPlan a, int* err) {
     }
   };
   if (!ROWS_TOO) pdl_launch_dependents();
-  const bool one = a.batch <= T, kept = ROWS_TOO && a.batch <= KP_STARTS;
+  static_assert(KEPT <= T, "all sequences of a block's step at once");
+  const bool one = ROWS_TOO || a.batch <= T;
   const int there = a.batch ? *a.n_free : 0;  // (no sequences: nothing but rows of none)
   const KpSeq mine = kp_seq(a, tid);
   auto seq = [&](int b0) { return one ? mine : kp_seq(a, b0 + tid); };
@@ -215,7 +218,7 @@ __global__ void __launch_bounds__(T) kv_plan_kernel(KvPlan a, int* err) {
     if (lane == 0 && taken) atomicMax(&most, taken);
     if (b < a.batch) {
       const int q = (int)min(end, (int64_t)a.n_rows);
-      if (kept) {
+      if (ROWS_TOO) {
         starts[b + 1] = q;
         keeps[b] = s.start;
       }
@@ -228,11 +231,11 @@ __global__ void __launch_bounds__(T) kv_plan_kernel(KvPlan a, int* err) {
     }
     if (rank == 0 && b < a.batch) {
       a.seq_len[b] = ok ? s.start + s.rows : s.start;
-      if (!broken && !s.bad && (ok || s.back())) a.held[b] = s.need;
+      if (ok) a.held[b] = s.need;  // (one with pages to return lacks none)
     }
   }
   if (tid == 0) {
-    starts[0] = 0;
+    if (ROWS_TOO) starts[0] = 0;
     if (rank == 0) {
       a.q_start[0] = 0;
       if (rows > a.n_rows) report_error(err, DERR_KV_RANGE);
@@ -240,8 +243,7 @@ __global__ void __launch_bounds__(T) kv_plan_kernel(KvPlan a, int* err) {
   }
   meet();
   if (rank == 0 && tid == 0 && a.batch && !broken) *a.n_free = (int)(pages - most);
-  if (!ROWS_TOO) return;
-  kp_rows(a, kept ? starts : nullptr, keeps, 4 * tid, 4 * T, err);
+  if (ROWS_TOO) kp_rows(a, starts, keeps, 4 * tid, 4 * T, err);
 }
 
 // The rows of a step that has many of them, by CTAs all over the GPU.
@@ -262,7 +264,7 @@ __global__ void __launch_bounds__(KP_ROW_THREADS) kv_plan_rows_kernel(KvPlan a, 
 cudaError_t kv_plan_launch(const KvPlan& a, int sms, int* err, cudaStream_t stream) {
   // One kernel while the rows are a few a thread, in us, one / two: 256 rows of 8 sequences 4.0 / 6.1, 4096 of 8
   // 5.2 / 6.2, 4096 of 64 6.2 / 6.7, 32000 of 16 18.8 / 6.5.
-  if (a.n_rows <= 4096 && a.batch <= 256) {
+  if (a.n_rows <= KP_ONE_ROWS && a.batch <= KP_ONE_SEQS) {
     kv_plan_kernel<512, 1, true><<<1, 512, 0, stream>>>(a, err);
     return cudaGetLastError();
   }
