@@ -97,8 +97,8 @@ __device__ __forceinline__ void kp_rows(const KvPlan& a, const int* starts, cons
       int q0 = start_of(lo), q1 = start_of(lo + 1), at = kept_of(lo), have = -1, base = 0;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
+        if (i >= live - r0) break;  // (r0 + 3 may pass 2^31)
         const int r = r0 + i;
-        if (r >= live) break;
         if (r >= q1) {
           do {
             q0 = q1;
