@@ -235,7 +235,7 @@ __global__ void __launch_bounds__(KaCfg<HD, F, RS>::THREADS, KA_CTAS) kv_attenti
   const uint32_t v_at[2] = {chunk4_at<C::ROWB>(2 * place, quad * (HD / 16) >> 4) + (quad * (HD / 16) & 15),
                             chunk4_at<C::ROWB>(2 * place + 1, quad * (HD / 16) >> 4) + (quad * (HD / 16) & 15)};
 
-  const KaLine<C::ROWS, KA_START, Q4 ? KA_KEEP : 0, Q4 ? KA_FINE : KA_LEAST> line(kv, a);
+  const KaLine<C::ROWS, KA_START, Q4 ? KA_KEEP : 0, Q4 ? KA_FINE : KA_LEAST, Q4 || RS == 1 ? 4 : 1> line(kv, a);
 
   // ---- this CTA's part of the line of all items
   KaWalk& shared_walk = *reinterpret_cast<KaWalk*>(smem + C::HEAD);

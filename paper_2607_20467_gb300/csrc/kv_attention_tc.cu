@@ -209,7 +209,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::HOLDER + 4);
   KaWalk& shared_walk = *reinterpret_cast<KaWalk*>(smem + C::WALK);
   KaJoin* todo = reinterpret_cast<KaJoin*>(smem + C::TODO);
-  const KaLine<TC_ROWS, TC_START, F == KV_Q4 ? KA_KEEP : 0> line(kv, a);
+  const KaLine<TC_ROWS, TC_START, F == KV_Q4 ? KA_KEEP : 0, KA_LEAST, F == KV_Q4 ? 4 : 1> line(kv, a);
 
   if (warp == 0) line.begin(&shared_walk, err);
   if (warp == 16) {
@@ -254,8 +254,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     const int values = warp >= 12, w4 = warp & 3;
     constexpr bool WIDEN = F != KV_BF16;
     constexpr int CH = F == KV_Q4 ? HD / 32 : F == KV_FP8 ? HD / 16 : HD / 8;  // chunks of a vector
-    constexpr int LK = CH < 4 ? CH : 4, PK = CH / LK, KP = 32 / LK;  // a lane's of a key: key lane / LK + KP i, chunk lane % LK + LK j
-    const int shift = kv.page_shift, P = kv.page_len(), at_key = 32 * w4 + lane / LK, at_chunk = lane % LK;
+    static_assert(CH >= 4 || CH == 2, "a key's chunks by two or four lanes");
+    constexpr int LK = CH < 4 ? CH : 4, LS = LK == 4 ? 2 : 1, PK = CH / LK, KP = 32 / LK;  // a lane's of a key: key lane / LK + KP i, chunk lane % LK + LK j
+    const int shift = kv.page_shift, P = kv.page_len(), at_key = 32 * w4 + (lane >> LS), at_chunk = lane & (LK - 1);
     const void* pool = values ? kv.v : kv.k;
     const int8_t* exps = values ? kv.v_exp : kv.k_exp;
     const uint32_t raw = base + C::RAW + values * C::CODES;
@@ -286,7 +287,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
           const int page = __shfl_sync(0xffffffffu, pages, 16 * h);
           if (page < 0) continue;
           const uint8_t* src = static_cast<const uint8_t*>(pool) + vec_of(page, first + unit * KA_UNIT + 16 * h) * (CH * 16) +
-                               (lane / LK * CH + at_chunk) * 16;
+                               ((lane >> LS) * CH + at_chunk) * 16;
 #pragma unroll
           for (int i = 0; i < 16 / KP; ++i)
 #pragma unroll

@@ -83,7 +83,12 @@ struct KaWalk {
 // 20.8 / 17.8; 8 of 1536, 32 heads, one row 24.1 / 21.2, 16 rows 36.3 / 30.0, 32 rows 47.7 / 44.4; 16 of 1024,
 // 28 / 4 heads, 448 rows 48.6 / 40.0.  (6: 16 sequences of 1024, one row 14.3 / 15.3.  Other formats are always cut.)
 constexpr int KA_KEEP = 5;
-template <int ROWS, int START, int KEEP = 0, int LEAST = KA_LEAST>  // rows of an item; positions for its beginning
+// ROWS of an item; positions for its beginning (START); SEQS: sequences, in 32s, of which a lane keeps the positions
+// while it looks for its CTA's part.  A second look at the lengths of the others takes as long as all the rest, but what is
+// kept adds to the registers of a kernel whose loop has none left: 9 rows and more of FP8 and bf16 pages keep 32.  us, 32 kept
+// / 128: FP8, one row, 120 sequences 22.6 / 21.5; FP8, 32 heads, 8 of 1536, 16 rows 35.9 / 37.6; causal 4 x 8192, 64 new
+// 160.2 / 165.1; bf16, 32 heads, 8 of 1536, 32 rows 50.0 / 50.9; tcgen05, FP8, 16 x 8192, 224 rows 112.2 / 113.7.
+template <int ROWS, int START, int KEEP = 0, int LEAST = KA_LEAST, int SEQS = 4>
 struct KaLine {
   const KvAttn& a;
   int G, rep, room;
@@ -123,19 +128,26 @@ struct KaLine {
       }
       return upto;
     };
-    // (of up to 128 sequences every lane keeps its four: a look at the lengths again takes as long as all the rest)
-    int64_t total = 0, own4[4], upto4[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      own4[i] = upto4[i] = 0;
-      if (32 * i < a.batch) {
-        upto4[i] = scan(32 * i, own4[i]);
-        total += __shfl_sync(0xffffffffu, upto4[i], 31);
+    int64_t total = 0, owns[SEQS], uptos[SEQS];
+    if constexpr (SEQS == 1) {
+      uptos[0] = 0;
+      for (int b0 = 0; b0 < a.batch; b0 += 32) {
+        uptos[0] = scan(b0, owns[0]);
+        total += __shfl_sync(0xffffffffu, uptos[0], 31);
       }
-    }
-    for (int b0 = 128; b0 < a.batch; b0 += 32) {
-      int64_t own;
-      total += __shfl_sync(0xffffffffu, scan(b0, own), 31);
+    } else {
+#pragma unroll
+      for (int i = 0; i < SEQS; ++i) {
+        owns[i] = uptos[i] = 0;
+        if (32 * i < a.batch) {
+          uptos[i] = scan(32 * i, owns[i]);
+          total += __shfl_sync(0xffffffffu, uptos[i], 31);
+        }
+      }
+      for (int b0 = 32 * SEQS; b0 < a.batch; b0 += 32) {
+        int64_t own;
+        total += __shfl_sync(0xffffffffu, scan(b0, own), 31);
+      }
     }
     const KaShare share(total, gridDim.x, LEAST);
     // no longer than a share and KEEP (and no shorter, so that no CTA has two): a CTA each
@@ -161,13 +173,20 @@ struct KaLine {
         return true;
       };
       int64_t at;
+      if constexpr (SEQS == 1) {
+        for (int b0 = 0; b0 < a.batch; b0 += 32) {
+          if (a.batch > 32) uptos[0] = scan(b0, owns[0]);
+          if (here(b0, uptos[0], owns[0], at)) return at;
+        }
+      } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (32 * i < a.batch && here(32 * i, upto4[i], own4[i], at)) return at;
-      for (int b0 = 128; b0 < a.batch; b0 += 32) {
-        int64_t own;
-        const int64_t upto = scan(b0, own);
-        if (here(b0, upto, own, at)) return at;
+        for (int i = 0; i < SEQS; ++i)
+          if (32 * i < a.batch && here(32 * i, uptos[i], owns[i], at)) return at;
+        for (int b0 = 32 * SEQS; b0 < a.batch; b0 += 32) {
+          int64_t own;
+          const int64_t upto = scan(b0, own);
+          if (here(b0, upto, own, at)) return at;
+        }
       }
       b = a.batch;
       return total;
