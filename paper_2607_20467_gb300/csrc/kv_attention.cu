@@ -52,9 +52,6 @@ namespace dcl {
 namespace {
 
 constexpr int KA_START = 3;   // units of keys that beginning an item takes
-constexpr int KA_CTAS = 2;    // CTAs of an SM: one loads while the other begins or ends an item
-constexpr int KA_MOST = 304;  // most CTAs of a launch
-static_assert(3 * KA_MOST * sizeof(int) <= KV_ATTN_COUNTERS, "a counter per CTA, and two for groups of parts");
 constexpr int KA_ONE = 10;  // parts of an item that are joined at once (4 bits)
 
 // RS: rows of an item that a lane has (quad + 8 i), 8 rows of the item each.

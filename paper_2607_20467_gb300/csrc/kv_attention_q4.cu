@@ -34,8 +34,6 @@ namespace dcl {
 namespace {
 
 constexpr int K4_START = 2;   // units of keys that beginning an item takes (64 ragged sequences: 3 33.9 us, 2 32.9, 4 34.7)
-constexpr int K4_CTAS = 2;    // CTAs of an SM: one loads while the other begins or ends an item
-constexpr int K4_MOST = 304;  // most CTAs of a launch
 constexpr int K4_ONE = 48;    // parts of an item that are joined at once
 constexpr int K4_KEYS = 32;   // keys that a warp takes at a time
 constexpr float K4_ABOVE = 32.f, K4_SLACK = 8.f;  // the reference above the largest score, and how far that may be passed
@@ -49,7 +47,7 @@ struct K4Cfg {
   static constexpr int SIDE = HD / Q4_GROUP;         // its scales
   static constexpr int TILE = K4_KEYS * ROWB;
   static constexpr int STAGE = 2 * TILE + 2 * K4_KEYS * SIDE;
-  static constexpr int LIMIT = 220 * 1024 / K4_CTAS / WARPS / STAGE;
+  static constexpr int LIMIT = 220 * 1024 / KA_CTAS / WARPS / STAGE;
   static constexpr int STAGES = LIMIT > 6 ? 6 : LIMIT;
   static constexpr int RING = STAGES * STAGE;
   static constexpr int O_PITCH = HD + 36;            // a warp's O in the ring's place: [ROWS][O_PITCH] floats, 16 components and 4 on
@@ -60,7 +58,7 @@ struct K4Cfg {
   static constexpr int HEAD = WT + ROWS * (8 * 4 + 8);  // the walk's variables
   static constexpr int TODO = HEAD + 48;             // joins left to this CTA: their number, and two at most
   static constexpr size_t SMEM = TODO + 3 * 24;
-  static_assert(WARPS <= 8 && STAGES >= 2 && K4_CTAS * (SMEM + 1024) <= 233472, "shared memory of an SM");
+  static_assert(WARPS <= 8 && STAGES >= 2 && KA_CTAS * (SMEM + 1024) <= 233472, "shared memory of an SM");
   static_assert(sizeof(KaWalk) <= 48 && sizeof(KaJoin) == 24, "their places");
 };
 
@@ -99,14 +97,14 @@ __device__ __forceinline__ void join4(const KvAttn& a, const KaJoin& it, int c0,
   using Part = KaPart<HD, ROWS, false>;
   constexpr int LPR = HD / 4, CHUNK = 10;
   static_assert(THREADS / LPR >= ROWS, "a row for every so many threads");
-  static_assert(2 * CHUNK * 16 * THREADS + ROWS * K4_MOST * 8 <= ROOM, "shared memory of a join");
+  static_assert(2 * CHUNK * 16 * THREADS + ROWS * KA_MOST * 8 <= ROOM, "shared memory of a join");
   const int l = threadIdx.x % LPR, r = threadIdx.x / LPR;
   if (r / (32 / LPR) * (32 / LPR) >= it.rows) return;  // (whole warps)
   const int rr = min(r, it.rows - 1);
   // (the item's first CTA's part is its second, the others' their first)
   auto part_of = [&](int c) { return parts + (int64_t)(2 * (c0 + c * stride) + (c == 0 && c0 == it.c0)) * Part::FLOATS; };
   const uint32_t mine = smem_addr(smem) + 16 * threadIdx.x;
-  float2* weights = reinterpret_cast<float2*>(smem + 2 * CHUNK * 16 * THREADS) + r * K4_MOST;
+  float2* weights = reinterpret_cast<float2*>(smem + 2 * CHUNK * 16 * THREADS) + r * KA_MOST;
   auto ask = [&](int at) {
     const uint32_t to = mine + (at / CHUNK & 1) * (CHUNK * 16 * THREADS);
 #pragma unroll
@@ -160,7 +158,7 @@ __device__ __forceinline__ void join4(const KvAttn& a, const KaJoin& it, int c0,
 }
 
 template <int HD, bool GROUPS>
-__global__ void __launch_bounds__(K4Cfg<HD>::THREADS, K4_CTAS) kv_attention_q4_kernel(KvPool kv, KvAttn a, KaScratch scratch, int* err) {
+__global__ void __launch_bounds__(K4Cfg<HD>::THREADS, KA_CTAS) kv_attention_q4_kernel(KvPool kv, KvAttn a, KaScratch scratch, int* err) {
   using C = K4Cfg<HD>;
   constexpr int ROWS = C::ROWS, KT = K4_KEYS, SIDE = C::SIDE, ROWB = C::ROWB, CPR = ROWB / 16;
   constexpr int KS = HD / 16;   // k steps of S
@@ -507,7 +505,7 @@ __global__ void __launch_bounds__(K4Cfg<HD>::THREADS, K4_CTAS) kv_attention_q4_k
         // the last to come joins the parts, those of its group first, when it is through with its own
         const KaGroups by(c1 - c0 + 1, GROUPS ? K4_ONE : INT_MAX);
         const int k = by.of(blockIdx.x - c0), at = c0 + k * by.size;
-        if (ka_come(by.groups == 1 ? scratch.count + c0 : scratch.count + K4_MOST + 2 * at + (k == 0), by.parts(k)))
+        if (ka_come(by.groups == 1 ? scratch.count + c0 : scratch.count + KA_MOST + 2 * at + (k == 0), by.parts(k)))
           todo[todo[0].rows++ ? 2 : 1] = KaJoin{it.row0, it.g * rep, it.first, it.rows, c0, c1 - c0 + 1};
       }
     } else {
@@ -539,7 +537,7 @@ __global__ void __launch_bounds__(K4Cfg<HD>::THREADS, K4_CTAS) kv_attention_q4_k
 template <int HD, bool GROUPS>
 cudaError_t launch_as(const KvPool& kv, const KvAttn& a, const KaScratch& s, int ctas, int* err, cudaStream_t stream) {
   using C = K4Cfg<HD>;
-  static_assert(2 * C::ROWS * (HD + 4) * 4 <= KV_ATTN_PART_BYTES && 3 * K4_MOST * sizeof(int) <= KV_ATTN_COUNTERS, "scratch");
+  static_assert(2 * C::ROWS * (HD + 4) * 4 <= KV_ATTN_PART_BYTES, "scratch");
   auto kern = kv_attention_q4_kernel<HD, GROUPS>;
   static const cudaError_t set = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM);
   if (set != cudaSuccess) return set;
@@ -552,7 +550,7 @@ cudaError_t launch_as(const KvPool& kv, const KvAttn& a, const KaScratch& s, int
 bool kv_attention_q4_few(const KvPool& kv, const KvAttn& a) { return kv.format == KV_Q4 && (int64_t)a.max_new * (a.H / kv.G) <= 8; }
 
 cudaError_t kv_attention_q4_launch(const KvPool& kv, const KvAttn& a, void* scratch, int sms, int* err, cudaStream_t stream) {
-  const int ctas = K4_CTAS * std::min(sms, K4_MOST / K4_CTAS);
+  const int ctas = KA_CTAS * std::min(sms, KA_MOST / KA_CTAS);
   KaScratch s{reinterpret_cast<float*>(static_cast<uint8_t*>(scratch) + KV_ATTN_COUNTERS), static_cast<int*>(scratch)};
   // Joins in two steps, in a kernel of their own (the other's calls took 1 % longer with them), where so few long
   // items may have more parts than K4_ONE.  28 / 4 heads, one row, us in one step / two: 1 x 65536 27.1 / 22.7, 1 x 131072

@@ -17,6 +17,10 @@ namespace dcl {
 namespace {
 
 constexpr int KA_UNIT = 128;  // keys of a unit of work
+// The kernels for up to 32 rows, which have one scratch:
+constexpr int KA_CTAS = 2;    // CTAs of an SM: one loads while the other begins or ends an item
+constexpr int KA_MOST = 304;  // most CTAs of a launch
+static_assert(3 * KA_MOST * sizeof(int) <= KV_ATTN_COUNTERS, "a counter per CTA, and two for groups of parts");
 // START: units that beginning an item takes.  Sharing an item costs each of its CTAs the writing of a
 // part and one of them the join (for up to 32 rows 3 and 4 to 20 thousand cycles; a unit of 16 rows
 // takes about 1500).  So a cut that falls less than START + 3 positions after an item's beginning or
