@@ -115,10 +115,10 @@ __device__ __forceinline__ uint4 quantise(KvBf16& a, int& e) {
 // Codes (16 of 4 bits) and the scale byte of a part's group, which two neighbouring threads share; all
 // threads of a warp call it.
 //
-// The quotient by d = 4 .. 7 times a power of two comes out in fp32 to 2^-24 of itself and is rounded to fp16,
-// which puts ties right: half a whole number is an fp16 number and nearer than the next by 2^-12 of
-// itself at least; a quotient of 8 bits by 3 that is not halfway is off that by 1/128 of itself or more, eight
-// times fp16's step.  Adding 1.5 2^10 + 8 rounds it to a whole number, 8 above, in the low bits.  Two at a
+// The quotient by d = 4 .. 7 times a power of two comes out in fp32 to 2^-21 of itself (a reciprocal to two units
+// of its last place, and a product) and is rounded to fp16, which puts ties right: half a whole number is an fp16
+// number and nearer than the next by 2^-12 of itself at least; a quotient of 8 bits by 3 that is not halfway is off
+// that by 1/255 of itself or more, eight times fp16's half step.  Adding 1.5 2^10 + 8 rounds it to a whole number, 8 above, in the low bits.  Two at a
 // time, components i and i + 4 of a word's eight, as their codes lie in it; pairs are put together by
 // multiplying and adding, where what stands above their four bits comes to a constant.  That is 3.5 instructions
 // a component: with each code rounded and cut out by itself there were ten, and 12288 positions of 32 heads x
