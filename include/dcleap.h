@@ -417,7 +417,7 @@ dcl_status dcl_kv_plan(dcl_ctx* ctx, const dcl_kv_pages* pages, const int32_t* s
  *   q_out_dev, k_out_dev    as q_dev, k_dev; either these themselves (in place, with the same strides)
  *                 or apart from them.
  * head_dim 64 or 128; rot_dim a multiple of 16 up to head_dim; theta at least 1; all pointers to bf16 16-byte
- * aligned.  fp32 throughout, rounded once; angles are exact to 2^-21 at any position.
+ * aligned.  fp32 throughout, rounded once; angles are off by 2^-21 at most up to position 2^28, by 2^-20 at any.
  * Errors: INVALID_ARG, CUDA. */
 dcl_status dcl_qk_norm_rope(dcl_ctx* ctx, const void* q_dev, int64_t q_stride, const void* k_dev, int64_t k_stride,
                             const int32_t* pos_dev, int32_t n, int32_t n_heads, int32_t n_kv_heads,
