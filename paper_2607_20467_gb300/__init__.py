@@ -556,7 +556,8 @@ class Context:
     def kv_plan(self, pages, start, new, q_start, seq_len, slots, pos):
         """Lay out a step: sequence b keeps start[b] cached positions and gets new[b] rows (int32 [batch]).
         Moves pages between the sequences and the stack; writes q_start [batch + 1], seq_len [batch], and
-        slots, pos [rows] (-1 past the last sequence's).  seq_len may be start itself: the next step goes on from it."""
+        slots, pos [rows] (-1 past the last sequence's).  A sequence that is given no rows has seq_len start.  seq_len
+        may be start itself: the next step goes on from it."""
         B, rows = pages.batch, slots.shape[0]
         st = self._L.dcl_kv_plan(self.ptr, pages.ptr, _dev_i32(start, "start", B), _dev_i32(new, "new", B),
                                  _dev_i32(q_start, "q_start", B + 1), _dev_i32(seq_len, "seq_len", B),

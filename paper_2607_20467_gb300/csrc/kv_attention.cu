@@ -30,7 +30,7 @@
 //
 // 4-bit pages, 9 to 32 rows (up to 8: kv_attention_q4.cu).  Codes are widened to bf16 with their groups' scales
 // where they are operands (q4.cuh), and all else is as with bf16 pages.  8 sequences of 1536, 32 heads, 32 rows
-// each (58 MB): 44.3 us (bf16 pages 49.4): two warps a scheduler (255 registers) wait for one
+// each (58 MB): 44.3 us (bf16 pages 49.4): two warps a scheduler (251 registers) wait for one
 // another's products, maxima and weights more than for any pipe (0.35 instructions a cycle, HMMA 0.4 busy).
 //
 // P is given in two parts, fp16 with FP8 pages (2^-21 of itself; 2^-32 of the largest term where that is

@@ -2,7 +2,7 @@
 // bits: a decode step's.  More rows take the kernels of kv_attention.cu and kv_attention_tc.cu.
 //
 // Half a byte a component: at the rate at which memory delivers codes an SM has to widen 45 of them a cycle,
-// and the instructions that do so bound the call, not memory.  So the products stand the other way
+// which costs more than their arrival.  So the products stand the other way
 // round than those of wider formats: keys and value components are the M side,
 //   S^T [16 keys][8 rows] = K q^T,   O^T [16 components][8 rows] += V^T P^T  (m16n8k16, bf16),
 // which leaves no half of an operand or of an accumulator empty, so that O takes 32 registers of a lane, not
@@ -18,7 +18,9 @@
 // measured copy rate; 64 ragged sequences to 4096 (74 MB) in 32.8 us; one of 512, 32 heads, 7.7 us.  A warp takes
 // 197 instructions for 8 keys and their values, 94 of them on the integer pipe, which has one for two cycles: 56
 // bring codes into place (a shift and a mask for two components), and that pipe is 0.6 to 0.8 busy while keys
-// are walked.  The rest of a CTA's time: 3900 cycles to find its part of the line, 4700 until its first keys
+// are walked.  Over the whole call neither it (0.45, 21 us of the 45.8) nor the issue slots (0.48) are full: the rest are
+// waits of fixed latency in a warp's chain (S, maximum, exp2, movmatrix, then the values), with four warps a scheduler
+// to cover them.  The rest of a CTA's time: 3900 cycles to find its part of the line, 4700 until its first keys
 // are there, 2700 an item's end, 2800 a join of two parts.  (Keys and values on the N side, as for wider
 // formats: 57.5 us and 39.7.  Shifts by multiplication, for the other pipe: 53.6.  16 rows a pass this way
 // round: 8 sequences of 1536, 32 heads, 32 rows 52 us, 47.5 in kv_attention.cu, both cut.)

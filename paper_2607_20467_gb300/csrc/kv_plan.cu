@@ -10,9 +10,11 @@
 // sums over the sequences in pieces of a CTA's threads; a warp for a sequence's pages; a thread for a few
 // rows (their sequence by bisection in q_start).  Steps of many rows or sequences: a cluster of 8 CTAs for the
 // pages, each of which has the sums for itself, and a second kernel for the rows, launched as the first
-// begins.  8 sequences of 32 rows: 4.2 us in a graph, of which the launch is about 2.  256 prompts of up to 1536
-// positions (172 thousand rows, 1.4 MB): 7.8 us (one CTA for all 228; the cluster's CTAs for the rows, too, 16.5:
-// ten of them were the rows' instructions on 8 SMs; 16 rows a thread there 20.6).
+// begins.  In a graph, where no page moves: 8 sequences of 32 rows 3.6 us, of which the launch is about 2; 256 prompts of
+// up to 1536 positions (172 thousand rows, 1.4 MB) 7.7 (one CTA for all 96; the cluster's CTAs for the rows, too, 16.5: ten of
+// them were the rows' instructions on 8 SMs; 16 rows a thread there 20.6).  Pages add a warp's two dependent looks at memory
+// for each sequence it has: of a call that takes them and one that returns them, together, 8 sequences' 8 pages 0.6 us, 64
+// sequences' 64 2 to 3, the prompts' 10875 3.1 (with the prompts' rows and without: 7.7 + 6.0, and 16.8 with the pages).
 #include "common.cuh"
 #include "kv_cache.cuh"
 
@@ -262,8 +264,10 @@ __global__ void __launch_bounds__(KP_ROW_THREADS) kv_plan_rows_kernel(KvPlan a, 
 }  // namespace
 
 cudaError_t kv_plan_launch(const KvPlan& a, int sms, int* err, cudaStream_t stream) {
-  // One kernel while the rows are a few a thread, in us, one / two: 256 rows of 8 sequences 4.0 / 6.1, 4096 of 8
-  // 5.2 / 6.2, 4096 of 64 6.2 / 6.7, 32000 of 16 18.8 / 6.5.
+  // One kernel while the rows are a few a thread, in us, one / two, no page moved: 256 rows of 8 sequences 3.2 / 5.7,
+  // 4096 of 8 4.2 / 6.0, 4096 of 64 4.6 / 6.3, 256 of 256 5.2 / 7.7, 4096 of 256 5.7 / 7.0, 32000 of 16 14.8 / 6.0.  A call that
+  // takes a page for every sequence and one that returns them, together: 8 sequences 6.3 / 11.5, 64 10.0 / 12.8, 128
+  // 11.3 / 13.7, 256 18.3 / 14.9 (16 a warp, one after another; most steps of decoding move a page for few).
   if (a.n_rows <= KP_ONE_ROWS && a.batch <= KP_ONE_SEQS) {
     kv_plan_kernel<512, 1, true><<<1, 512, 0, stream>>>(a, err);
     return cudaGetLastError();
