@@ -287,7 +287,7 @@ class KvCache:
                     raise ValueError(f"{name}: [pages][kv heads][page_len][head_dim / 32] scales expected, got {shape}")
         elif small and hd in (32, 64) and "float8" not in str(k.dtype):  # (4-bit codes of 64 or 128 components have as many bytes)
             for t, name in ((k_exp, "k_exp"), (v_exp, "v_exp")):
-                if hasattr(t, "shape") and t.numel() == n * (hd // 16):
+                if getattr(t, "is_cuda", False) and t.numel() == n * (hd // 16):
                     raise ValueError(f"{name}: {n * (hd // 16)} bytes are scales of a 4-bit cache, which are [pages][kv heads][page_len]"
                                      f"[head_dim / 32], or more than the {n} exponents of an FP8 one; got {tuple(t.shape)}")
         self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp

@@ -1,4 +1,5 @@
 """Which format a cache is taken for, by its tensors (CPU only)."""
+import numpy as np
 import pytest
 
 import paper_2607_20467_gb300 as dcl
@@ -39,3 +40,11 @@ def test_exponents_of_other_shapes_are():
     codes = FakeCuda((4, 2, 16, 64), 1)
     codes.dtype = "torch.float8_e4m3fn"  # (which says what it is)
     assert dcl.KvCache(codes, codes, FakeCuda((512,), 1), FakeCuda((512,), 1)).format == dcl.DCL_KV_FP8
+
+
+@pytest.mark.parametrize("bytes_", [32, 64, 128])
+def test_host_arrays_are_no_exponents(bytes_):
+    codes = FakeCuda((4, 2, 16, bytes_), 1)
+    for exps in (np.zeros((4, 2, 16), np.int8), np.zeros((4, 2, 16, bytes_ // 16), np.uint8)):
+        with pytest.raises(ValueError):
+            dcl.KvCache(codes, codes, exps, exps)
